@@ -342,6 +342,108 @@ int rr_attend_token_ranges(const int32_t* ranges, int32_t rows, int32_t slots, i
                            const void* q, const void* keys, const void* values, int32_t tokens,
                            int32_t dh, int32_t dtype, float scale, float* out, void* stream);
 
+/* ---- The paged key/value cache behind the routes -------------------------------------------------
+ * A serving program keeps the keys and values that the routes select in pages.  Three operators work
+ * on such a cache: rr_kv_append writes new tokens into it and rotates them by their positions,
+ * rr_attend_shared attends to it for a batch whose sequences begin with the same tokens, and
+ * rr_attend_paged_ranges attends to the token ranges of the routes.
+ *
+ * Conventions of the three
+ *   - Token s of sequence b lies in page page_table[b * table_stride + s / page_tokens] at place
+ *     s % page_tokens: element (page, head, place, e) of k and of v is at
+ *     page * page_stride + head * head_stride + place * token_stride + e.
+ *   - All pointers are device pointers of the device that is current at the call, strides count elements and
+ *     may be anything >= 0 (token-major and head-major pages, keys and values interleaved in one pool, slices of a
+ *     projection's output); the entries of one head are contiguous.
+ *   - Calls only enqueue work on `stream` and may be captured into a graph.  Nothing is kept between
+ *     calls.  Calls that can overlap on the GPU need workspaces of their own.
+ *   - Lengths, tables and ranges are read on the device.  An id outside [0, num_pages), or a position
+ *     behind the table's end, sets RR_STATUS_BAD_INDEX in *status (if given) and the token is left out: not
+ *     written by an append, not seen by an attention.  Nothing out of range is read or written.
+ *   - What a query may not see -- by the causal mask, by its length, by its ranges -- does not reach it, whatever
+ *     the memory holds, NaN and infinities included.  A query that sees nothing gets zeros; one whose logits are
+ *     all -inf has no softmax and gets NaN.
+ *   - Logits, softmax sums and outputs are accumulated in FP32.  bf16: the softmax's weights are rounded to bf16
+ *     where the product with the values runs on the tensor cores (dh 64 and 128).
+ *   - The results do not depend on timing: the same call on the same inputs gives the same bits. */
+typedef struct rr_paged_kv {
+  void* k;                   /* pages of keys and of values                                       */
+  void* v;
+  const int32_t* page_table; /* [batch, pages_per_seq], rows table_stride apart                   */
+  uint32_t* status;          /* [1] RR_STATUS_* bits are OR-ed into it; may be NULL               */
+  int64_t page_stride, head_stride, token_stride;
+  int64_t table_stride;
+  int32_t dtype;             /* RR_BF16 or RR_F32, of the cache and of all queries, keys, values, outputs */
+  int32_t num_pages, page_tokens, kv_heads;
+  int32_t dh;                /* entries of a head, <= 256                                         */
+  int32_t batch, pages_per_seq;
+} rr_paged_kv;
+
+/* Appends `tokens` new tokens.  Sequence b owns the tokens [cu[b], cu[b + 1]); its first one gets position
+ * lens[b].  cu == NULL: one token per sequence (tokens == batch).  Tokens behind cu[batch] are padding: nothing is
+ * written for them, in the cache or in q_out.
+ * With rot > 0 the first `rot` entries of every key head, and of every query head, are rotated by the
+ * token's position p: pair j is turned by the angle p * inv_freq[j]; the pair is (j, j + rot / 2), or with
+ * interleaved != 0 (2 j, 2 j + 1).  The product p * inv_freq[j] is formed and reduced in 64 bits, at any position.
+ * Writes lens[b] + number of new tokens to new_lens[b] if new_lens is given (not lens itself). */
+typedef struct rr_append_args {
+  const void* k;             /* [tokens, kv_heads, dh]                                            */
+  const void* v;
+  const void* q;             /* [tokens, q_heads, dh] rotated into q_out; NULL: keys and values only */
+  void* q_out;               /* may be q itself                                                   */
+  const int32_t* lens;       /* [batch] tokens in the cache before this call                      */
+  const int32_t* cu;         /* [batch + 1] ascending, cu[0] = 0; or NULL                         */
+  int32_t* new_lens;         /* [batch] or NULL                                                   */
+  const float* inv_freq;     /* [rot / 2]; may be NULL if rot == 0                                */
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+  int32_t tokens, q_heads;
+  int32_t rot;               /* even, 0 <= rot <= dh                                              */
+  int32_t interleaved;
+} rr_append_args;
+int rr_kv_append(const rr_paged_kv* kv, const rr_append_args* a, void* stream);
+
+/* Attention of a batch that shares a prefix:  out = softmax(q K^T * scale) V  for the queries q of the tokens
+ * [cu[b], cu[b + 1]) of each sequence b, over the sequence's tokens s < lens[b].
+ *   causal != 0   the queries are the sequence's last tokens: the i-th of its n sees s <= lens[b] - n + i
+ *   causal == 0   every query sees all tokens (attention to states of another length, e.g. an encoder's)
+ * Tokens s < prefix_tokens are the same for all sequences and are read once for all, from the pages
+ * prefix_pages (NULL: those of sequence 0's table); a sequence shorter than the prefix sees its first lens[b] tokens.  Query
+ * head h reads key head h / (heads / kv_heads).  prefix_tokens == 0: nothing is shared. */
+typedef struct rr_shared_args {
+  const void* q;             /* [tokens, heads, dh]                                               */
+  void* out;                 /* [tokens, heads, dh]; rows behind cu[batch] are left as they were  */
+  const int32_t* lens;       /* [batch] tokens in the cache, the new ones among them              */
+  const int32_t* cu;         /* [batch + 1] or NULL: one query token per sequence                 */
+  const int32_t* prefix_pages;
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+  int32_t tokens, heads, prefix_tokens, causal;
+  float scale;
+} rr_shared_args;
+int rr_attend_shared_workspace(const rr_paged_kv* kv, const rr_shared_args* a, size_t* bytes);
+int rr_attend_shared(const rr_paged_kv* kv, const rr_shared_args* a, void* workspace, size_t bytes, void* stream);
+
+/* Attention over the token ranges of the routes (views.token_ranges, per slot or coalesced), the tokens read through
+ * the page table.  A range row (b, route head r, chunk i) holds `slots` ranges [start, end) of sequence b's tokens ((-1,-1)
+ * = empty; tokens from lens[b] on are left out) for the queries of the heads / route_heads query heads of route head r and
+ * of the `m` tokens of query chunk i.  m == 1: one query per row, as rr_attend_token_ranges; a decoding step has n_q == 1 too.
+ *   causal != 0   the n_q * m query tokens are the sequence's last ones, and a query sees no token behind its own
+ * kv_heads divides route_heads, which divides heads.  slots <= RR_MAX_RANGE_SLOTS.  How a row's tokens are split depends on
+ * their numbers in the order of the slots only: coalesced and per-slot ranges of one route give the same bits. */
+#define RR_MAX_RANGE_SLOTS 1024
+typedef struct rr_ranges_args {
+  const void* q;             /* [batch, heads, n_q * m, dh]                                       */
+  void* out;                 /* [batch, heads, n_q * m, dh]                                       */
+  const int32_t* ranges;     /* [batch * route_heads * n_q, slots, 2]                             */
+  const int32_t* lens;       /* [batch]                                                           */
+  int64_t q_batch_stride, q_head_stride, q_token_stride;
+  int64_t out_batch_stride, out_head_stride, out_token_stride;
+  int32_t heads, route_heads, n_q, m, slots, causal;
+  float scale;
+} rr_ranges_args;
+int rr_attend_paged_ranges_workspace(const rr_paged_kv* kv, const rr_ranges_args* a, size_t* bytes);
+int rr_attend_paged_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, void* workspace, size_t bytes, void* stream);
+
 /* Per-kernel device timing for benchmarks.  Between rr_profile_begin and rr_profile_end
  * every kernel the layer calls launch is bracketed by CUDA events on the caller's stream
  * (this adds event records to the stream; do not leave it on in production).

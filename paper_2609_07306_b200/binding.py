@@ -21,6 +21,7 @@ RR_ERR_TIMEOUT = -5
 RR_ERR_TOO_SMALL = -6
 RR_ERR_TOO_LARGE = -7
 RR_NOALLOC_MAX_TILES = 65536
+RR_MAX_RANGE_SLOTS = 1024
 RR_BF16 = 0
 RR_F32 = 1
 RR_STATUS_TIMEOUT = 1
@@ -54,6 +55,36 @@ class rr_bucket_info(C.Structure):
     _fields_ = [("k", C.c_int32), ("problems", C.c_int32), ("first_slot", C.c_int32),
                 ("ledger_offset", C.c_size_t), ("scratch_offset", C.c_size_t),
                 ("ledger_bytes", C.c_size_t), ("scratch_bytes", C.c_size_t)]
+
+
+class rr_paged_kv(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p), ("status", C.c_void_p),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("table_stride", C.c_int64), ("dtype", C.c_int32), ("num_pages", C.c_int32),
+                ("page_tokens", C.c_int32), ("kv_heads", C.c_int32), ("dh", C.c_int32),
+                ("batch", C.c_int32), ("pages_per_seq", C.c_int32)]
+
+
+class rr_append_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "q", "q_out", "lens", "cu", "new_lens", "inv_freq")] + \
+               [(n, C.c_int64) for n in (
+                   "k_token_stride", "k_head_stride", "v_token_stride", "v_head_stride",
+                   "q_token_stride", "q_head_stride", "out_token_stride", "out_head_stride")] + \
+               [(n, C.c_int32) for n in ("tokens", "q_heads", "rot", "interleaved")]
+
+
+class rr_shared_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "lens", "cu", "prefix_pages")] + \
+               [(n, C.c_int64) for n in ("q_token_stride", "q_head_stride", "out_token_stride", "out_head_stride")] + \
+               [(n, C.c_int32) for n in ("tokens", "heads", "prefix_tokens", "causal")] + [("scale", C.c_float)]
+
+
+class rr_ranges_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "ranges", "lens")] + \
+               [(n, C.c_int64) for n in ("q_batch_stride", "q_head_stride", "q_token_stride",
+                                         "out_batch_stride", "out_head_stride", "out_token_stride")] + \
+               [(n, C.c_int32) for n in ("heads", "route_heads", "n_q", "m", "slots", "causal")] + \
+               [("scale", C.c_float)]
 
 
 class RouteRelayError(RuntimeError):
@@ -115,6 +146,15 @@ def lib() -> C.CDLL:
         for name in ("rr_bucket_plan", "rr_bucket_set_init", "rr_bucket_set_destroy",
                      "rr_bucket_set_count", "rr_bucket_set_info", "rr_bucket_set_reset",
                      "rr_bucket_route_layer", "rr_bucket_set_status", "rr_attend_token_ranges"):
+            getattr(L, name).restype = C.c_int
+        kvp, szp = C.POINTER(rr_paged_kv), C.POINTER(sz)
+        L.rr_kv_append.argtypes = [kvp, C.POINTER(rr_append_args), vp]
+        L.rr_attend_shared_workspace.argtypes = [kvp, C.POINTER(rr_shared_args), szp]
+        L.rr_attend_shared.argtypes = [kvp, C.POINTER(rr_shared_args), vp, sz, vp]
+        L.rr_attend_paged_ranges_workspace.argtypes = [kvp, C.POINTER(rr_ranges_args), szp]
+        L.rr_attend_paged_ranges.argtypes = [kvp, C.POINTER(rr_ranges_args), vp, sz, vp]
+        for name in ("rr_kv_append", "rr_attend_shared_workspace", "rr_attend_shared",
+                     "rr_attend_paged_ranges_workspace", "rr_attend_paged_ranges"):
             getattr(L, name).restype = C.c_int
         L.rr_profile_begin.argtypes = [vp]
         L.rr_profile_begin.restype = C.c_int
@@ -301,6 +341,34 @@ def rr_attend_token_ranges(ranges: int, rows: int, slots: int, n_q: int, q: int,
                            stream: int) -> None:
     _check(lib().rr_attend_token_ranges(ranges, rows, slots, n_q, q, keys, values, tokens, dh,
                                         dtype, scale, out, stream), "rr_attend_token_ranges")
+
+
+def rr_kv_append(kv: rr_paged_kv, args: rr_append_args, stream: int) -> None:
+    _check(lib().rr_kv_append(C.byref(kv), C.byref(args), stream), "rr_kv_append")
+
+
+def rr_attend_shared_workspace(kv: rr_paged_kv, args: rr_shared_args) -> int:
+    n = C.c_size_t()
+    _check(lib().rr_attend_shared_workspace(C.byref(kv), C.byref(args), C.byref(n)),
+           "rr_attend_shared_workspace")
+    return n.value
+
+
+def rr_attend_shared(kv: rr_paged_kv, args: rr_shared_args, workspace: int, nbytes: int, stream: int) -> None:
+    _check(lib().rr_attend_shared(C.byref(kv), C.byref(args), workspace, nbytes, stream), "rr_attend_shared")
+
+
+def rr_attend_paged_ranges_workspace(kv: rr_paged_kv, args: rr_ranges_args) -> int:
+    n = C.c_size_t()
+    _check(lib().rr_attend_paged_ranges_workspace(C.byref(kv), C.byref(args), C.byref(n)),
+           "rr_attend_paged_ranges_workspace")
+    return n.value
+
+
+def rr_attend_paged_ranges(kv: rr_paged_kv, args: rr_ranges_args, workspace: int, nbytes: int,
+                           stream: int) -> None:
+    _check(lib().rr_attend_paged_ranges(C.byref(kv), C.byref(args), workspace, nbytes, stream),
+           "rr_attend_paged_ranges")
 
 
 def rr_profile_begin(h: int) -> None:

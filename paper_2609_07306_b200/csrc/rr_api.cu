@@ -260,6 +260,8 @@ int route_layer(rr_ledger* L, const void* qc, const void* kc, int layer, bool an
 
 }  // namespace
 
+int rr_cuda_fail(cudaError_t e, const char* what) { return cuda_fail(e, what); }
+
 void rr_count_launch(int n) { g_launches.fetch_add((unsigned long long)n); }
 
 std::mutex& rr_attr_mutex() {

@@ -1,0 +1,579 @@
+// rr_attend_shared and rr_attend_paged_ranges: checks, workspace, the plan and join kernels, and the kernel that
+// processes segments on the ordinary pipes (fp32, and bf16 widths other than 64 and 128).
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+#include "rr_attend_paged.cuh"
+
+using namespace rrattn;
+
+namespace {
+
+constexpr unsigned FULL = 0xFFFFFFFFu;
+
+// ---- plan --------------------------------------------------------------------------------------------------
+// cum[b] = tiles of all items before sequence b's: the prefix's, then the sequences' own, in their order.
+constexpr int PLAN_NT = 1024;
+__global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ Params P) {
+  __shared__ long long s_warp[PLAN_NT / 32];
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  long long run = P.kv_heads * prefix_row_tiles(P) * prefix_tiles(P);
+  for (int b0 = 0; b0 < P.batch; b0 += PLAN_NT) {
+    const int b = b0 + tid;
+    const long long mine = b < P.batch ? (long long)P.kv_heads * own_row_tiles(P, b) * own_tiles(P, b) : 0;
+    long long incl = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) { const long long x = __shfl_up_sync(FULL, incl, off); if (lane >= off) incl += x; }
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    long long before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < PLAN_NT / 32; ++w) { if (w < warp) before += s_warp[w]; all += s_warp[w]; }
+    if (b < P.batch) P.cum[b] = run + before + incl - mine;
+    run += all;
+    __syncthreads();
+  }
+  if (tid == 0) P.cum[P.batch] = run;
+}
+
+// ---- join --------------------------------------------------------------------------------------------------
+// A warp joins the partials of one row: o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i, in the order of their tokens.
+template <typename T>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params P) {
+  constexpr int E = RR_PAGED_MAX_DH / 32;
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int H = P.heads;
+  // up to two lists of partials: `n` in all, the first n0 of list 0
+  long long home[2] = {0, 0};
+  int c0[2] = {0, 0}, cnt[2] = {0, 0}, st[2] = {1, 1}, r_in[2] = {0, 0};
+  long long out;
+  if (P.slots == 0) {
+    if (row >= (long long)P.tokens * H) return;
+    const int t = (int)(row / H), h = (int)(row % H), kvh = h / P.group, g = h % P.group;
+    int b = t;
+    if (P.cu) {
+      b = rr_sequence_of_warp(P.cu, P.batch, t);
+      if (b < 0) return;                               // padding: left as it was
+    }
+    const long long all = __ldg(P.cum + P.batch), per = (long long)P.tokens * P.group;
+    out = t * P.ot + h * P.oh;
+    const long long np = prefix_tiles(P), qtp = prefix_row_tiles(P);
+    if (np > 0) {
+      const long long idx = (long long)t * P.group + g, first = (kvh * qtp + idx / ROWS) * np;
+      home[0] = kvh * per + idx;
+      r_in[0] = (int)(idx % ROWS);
+      c0[0] = cta_of(P, first, all);
+      cnt[0] = cta_of(P, first + np - 1, all) - c0[0] + 1;
+      st[0] = P.streams == 2 && min((long long)ROWS, per - idx / ROWS * ROWS) <= TILE ? 2 : 1;
+    }
+    const int no = own_tiles(P, b);
+    if (no > 0) {
+      const int t0 = seq_first(P, b), n = seq_count(P, b), qt = own_row_tiles(P, b);
+      const long long idx = (long long)(t - t0) * P.group + g;
+      const long long first = __ldg(P.cum + b) + (kvh * (long long)qt + idx / ROWS) * no;
+      home[1] = (P.kv_heads + kvh) * per + (long long)t0 * P.group + idx;
+      r_in[1] = (int)(idx % ROWS);
+      c0[1] = cta_of(P, first, all);
+      cnt[1] = cta_of(P, first + no - 1, all) - c0[1] + 1;
+      st[1] = P.streams == 2 && min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS) <= TILE ? 2 : 1;
+    }
+  } else {
+    const int mg = P.m * P.group;
+    if (row >= P.range_rows * mg) return;
+    const long long rr = row / mg;
+    const int idx = (int)(row % mg), i = (int)(rr % P.n_q), r = (int)(rr / P.n_q % P.route_heads), b = (int)(rr / P.n_q / P.route_heads);
+    st[0] = P.streams == 2 && min(ROWS, mg - idx / ROWS * ROWS) <= TILE ? 2 : 1;
+    if (P.direct && st[0] == 1) return;
+    home[0] = row;
+    cnt[0] = P.splits;
+    out = b * P.ob + (r * P.group + idx % P.group) * P.oh + (i * P.m + idx / P.group) * P.ot;
+  }
+  const int n0 = cnt[0] * st[0], n = n0 + cnt[1] * st[1];
+  const long long cta_rows = 2 * (long long)P.tokens * H, split_rows = P.slots ? P.range_rows * P.m * P.group : 0;
+  auto place = [&](int k) -> long long {               // partial row of the k-th partial
+    const int w = k >= n0;
+    if (w) k -= n0;
+    const int s = st[w], c = k / s;
+    const long long at = P.slots ? home[0] + c * split_rows : c == 0 ? home[w] : cta_rows + (long long)(c0[w] + c) * ROWS + r_in[w];
+    return (k % s) * P.part_rows + at;
+  };
+  float M = NINF;
+  for (int k = lane; k < n; k += 32) M = fmaxf(M, P.part_ml[place(k)].x);
+#pragma unroll
+  for (int off = 16; off; off >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, off));
+  float l = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int k0 = 0; k0 < n; k0 += 32) {
+    const int k = k0 + lane;
+    float w = 0.f;
+    long long at = -1;
+    if (k < n) {
+      at = place(k);
+      const float2 ml = P.part_ml[at];
+      if (ml.x == NINF || (ml.x == LOWEST && ml.y == 0.f)) at = -1;      // nothing in it (and no output written)
+      else { w = exp2f(ml.x - M); l = fmaf(w, ml.y, l); }
+    }
+    const int lim = min(32, n - k0);
+    for (int u = 0; u < lim; ++u) {
+      const long long au = __shfl_sync(FULL, at, u);
+      const float wu = __shfl_sync(FULL, w, u);
+      if (au < 0) continue;
+      const float* const src = P.part_o + au * P.dh;
+#pragma unroll
+      for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) o[e] = fmaf(wu, src[lane + 32 * e], o[e]);
+    }
+  }
+#pragma unroll
+  for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(FULL, l, off);
+  // no weight at all: zeros for a row without tokens, NaN for one whose tokens are all at -inf
+  const float inv = l == 0.f ? (M == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (lane + 32 * e < P.dh) ((T*)P.out)[out + lane + 32 * e] = rr_from_f32<T>(o[e] * inv);
+}
+
+// ---- segments on the ordinary pipes --------------------------------------------------------------------------
+// A CTA takes BM = 16 * MR rows at a time through the segment's tokens, BT at a time: thread (ty, tx) of 16 x 16 has the
+// logits of rows ty + 16 i and tokens tx + 16 j, and of the output the same rows and 4-column groups tx + 16 j.  Queries, and keys
+// and values in turn, stand in shared memory as FP32 rows of dh + 4 entries (16-byte reads of 8 neighbouring rows meet 32
+// different banks).  Bound by FP32 multiply-adds where rows are many, by the cache's traffic where they are few (MR = 1).
+constexpr int BT = 64, SNT = 256;
+
+__host__ __device__ constexpr int padded(int dh) { return (dh + 3) / 4 * 4 + 4; }
+struct SmemPlan { int q, kv, p, ids, slots, total; };
+__host__ __device__ inline SmemPlan smem_plan(int dh, int n_slots) {
+  SmemPlan s;
+  const int row = padded(dh) * 4;
+  s.q = 0;
+  s.kv = s.q + 64 * row;
+  s.p = s.kv + BT * row;
+  s.ids = s.p + 64 * (BT + 4) * 4;
+  s.slots = s.ids + BT * 16;
+  s.total = s.slots + (2 * n_slots + 1) * 4;
+  return s;
+}
+
+template <typename T> __device__ __forceinline__ float4 load4(const T* p, bool vec, int n);
+template <> __device__ __forceinline__ float4 load4<float>(const float* p, bool vec, int n) {
+  if (vec) return *(const float4*)p;
+  return make_float4(p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
+}
+template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p, bool vec, int n) {
+  if (vec) {
+    const uint2 t = *(const uint2*)p;
+    return make_float4(__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xFFFF0000u), __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xFFFF0000u));
+  }
+  return make_float4(__bfloat162float(p[0]), n > 1 ? __bfloat162float(p[1]) : 0.f, n > 2 ? __bfloat162float(p[2]) : 0.f, n > 3 ? __bfloat162float(p[3]) : 0.f);
+}
+
+struct Ctx {
+  float *q, *kv, *p;
+  int* id;
+  long long* at;
+  int *first, *base;                                   // ranges: number of a slot's first token, and its start minus that
+  int n_tok;
+  bool vq, vk;                                         // queries / cache rows split into aligned groups of four
+};
+
+template <typename T, int NV, int MR>
+__device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, uint32_t* s_bad) {
+  constexpr int BM = 16 * MR;
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, dh = P.dh, ld = padded(dh), groups = (dh + 3) / 4;
+  for (int u = tid; u < BM * groups; u += SNT) {
+    const int r = u / groups, e = (u - r * groups) * 4;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r0 + r < s.rows) {
+      const int idx = s.row0 + r0 + r, dt = idx / P.group;
+      const RowAt a{s.t_base + dt, s.h0 + idx - dt * P.group, 0};
+      x = load4<T>((const T*)P.q + q_at(P, s, a) + e, c.vq, dh - e);
+    }
+    *(float4*)(c.q + r * ld + e) = x;
+  }
+  int limit[MR];
+  bool mixed = false;                                  // a token of the list was masked for one of this thread's rows
+#pragma unroll
+  for (int i = 0; i < MR; ++i) limit[i] = r0 + ty + 16 * i < s.rows ? row_at(P, s, r0 + ty + 16 * i).limit : 0;
+  float m[MR], l[MR];
+  float4 o[MR][NV];
+#pragma unroll
+  for (int i = 0; i < MR; ++i) {
+    m[i] = NINF; l[i] = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) o[i][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  uint32_t seen = 0;
+  const int num_end = s.tile1 * TILE;
+  for (int num0 = s.tile0 * TILE; num0 < num_end; num0 += BT) {
+    __syncthreads();                                   // the tile before is done
+    if (tid < BT) {
+      const int num = num0 + tid;
+      int id = NO_TOKEN;
+      if (s.slots) {
+        if (num < c.n_tok) {
+          int lo = 0, hi = P.slots;
+          while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (c.first[mid] <= num) lo = mid; else hi = mid; }
+          id = c.base[lo] + num;
+        }
+      } else if (num < s.tok1 - s.tok0) {
+        id = s.tok0 + num;
+      }
+      long long at = -1;
+      if (id != NO_TOKEN) { at = token_at(P, s, id); if (at < 0) id = NO_TOKEN; }
+      c.id[tid] = id;
+      c.at[tid] = at;
+    }
+    __syncthreads();
+    for (int u = tid; u < BT * groups; u += SNT) {
+      const int r = u / groups, e = (u - r * groups) * 4;
+      const long long at = c.at[r];
+      *(float4*)(c.kv + r * ld + e) = at < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : load4<T>((const T*)P.k + at + e, c.vk, dh - e);
+    }
+    __syncthreads();
+    float x[MR][4];
+#pragma unroll
+    for (int i = 0; i < MR; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
+#pragma unroll 4
+    for (int e = 0; e < groups * 4; e += 4) {
+      float4 a[MR], b[4];
+#pragma unroll
+      for (int i = 0; i < MR; ++i) a[i] = *(const float4*)(c.q + (ty + 16 * i) * ld + e);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[j] = *(const float4*)(c.kv + (tx + 16 * j) * ld + e);
+#pragma unroll
+      for (int i = 0; i < MR; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[i][j] = fmaf(a[i].w, b[j].w, fmaf(a[i].z, b[j].z, fmaf(a[i].y, b[j].y, fmaf(a[i].x, b[j].x, x[i][j]))));
+    }
+    __syncthreads();                                   // the keys are read: the values take their place
+    for (int u = tid; u < BT * groups; u += SNT) {
+      const int r = u / groups, e = (u - r * groups) * 4;
+      const long long at = c.at[r];
+      *(float4*)(c.kv + r * ld + e) = at < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : load4<T>((const T*)P.v + at + e, c.vk, dh - e);
+    }
+#pragma unroll
+    for (int i = 0; i < MR; ++i) {
+      float top = NINF;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int id = c.id[tx + 16 * j];
+        const bool sees = id < limit[i];
+        if (sees) seen |= 1u << i;
+        else if (id != NO_TOKEN) mixed = true;
+        x[i][j] = sees ? x[i][j] * P.scale_log2 : NINF;
+        top = fmaxf(top, x[i][j]);
+      }
+#pragma unroll
+      for (int off = 8; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, off));
+      const float m_new = fmaxf(m[i], top), ref = m_new == NINF ? 0.f : m_new, f = exp2f(m[i] - ref);
+      m[i] = m_new;
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float w = exp2f(x[i][j] - ref);
+        sum += w;
+        c.p[(ty + 16 * i) * (BT + 4) + tx + 16 * j] = w;
+      }
+      l[i] = fmaf(l[i], f, sum);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) { o[i][v].x *= f; o[i][v].y *= f; o[i][v].z *= f; o[i][v].w *= f; }
+    }
+    __syncthreads();
+#pragma unroll 2
+    for (int j = 0; j < BT; j += 4) {
+      float4 p[MR];
+#pragma unroll
+      for (int i = 0; i < MR; ++i) p[i] = *(const float4*)(c.p + (ty + 16 * i) * (BT + 4) + j);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int e = (tx + 16 * v) * 4;
+        if (e >= groups * 4) continue;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float4 y = *(const float4*)(c.kv + (j + u) * ld + e);
+#pragma unroll
+          for (int i = 0; i < MR; ++i) {
+            const float w = u == 0 ? p[i].x : u == 1 ? p[i].y : u == 2 ? p[i].z : p[i].w;
+            o[i][v].x = fmaf(w, y.x, o[i][v].x); o[i][v].y = fmaf(w, y.y, o[i][v].y);
+            o[i][v].z = fmaf(w, y.z, o[i][v].z); o[i][v].w = fmaf(w, y.w, o[i][v].w);
+          }
+        }
+      }
+    }
+  }
+  // sums over the row's sixteen threads, partial rows out
+  __syncthreads();                                     // (the block before has read its bits)
+  if (tid < 2) s_bad[tid] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < MR; ++i) {
+    float sum = l[i];
+    int any = seen >> i & 1, masked = mixed;
+    bool odd = false;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) odd = odd || !(isfinite(o[i][v].x) && isfinite(o[i][v].y) && isfinite(o[i][v].z) && isfinite(o[i][v].w));
+#pragma unroll
+    for (int off = 8; off; off >>= 1) {
+      sum += __shfl_xor_sync(FULL, sum, off);
+      any |= __shfl_xor_sync(FULL, any, off);
+      masked |= __shfl_xor_sync(FULL, masked, off);
+    }
+    const int r = ty + 16 * i;
+    if (odd && masked) atomicOr(&s_bad[r >> 5], 1u << (r & 31));
+    if (r0 + r >= s.rows) continue;
+    if (any && m[i] == NINF) m[i] = LOWEST;
+    const RowAt a = row_at(P, s, r0 + r);
+    const long long at = s.part + r0 + r;
+    if (!P.direct && tx == 0) P.part_ml[at] = make_float2(m[i], sum);
+    const float inv = sum == 0.f ? (m[i] == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / sum;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const float y[4] = {o[i][v].x, o[i][v].y, o[i][v].z, o[i][v].w};
+      const int e = (tx + 16 * v) * 4;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (e + u < dh) {
+          if (P.direct) ((T*)P.out)[out_at(P, s, a) + e + u] = rr_from_f32<T>(y[u] * inv);
+          else P.part_o[at * dh + e + u] = y[u];
+        }
+    }
+  }
+  __syncthreads();
+  for (int r = tid >> 5; r < BM && r0 + r < s.rows; r += SNT / 32) {
+    if (!(s_bad[r >> 5] >> (r & 31) & 1)) continue;
+    float mm, ll, oo[RR_PAGED_MAX_DH / 32];
+    repair_row<T>(P, s, r0 + r, 0, 1, mm, ll, oo);
+    const int lane = tid & 31;
+    const RowAt a = row_at(P, s, r0 + r);
+    const long long at = s.part + r0 + r;
+    if (!P.direct && lane == 0) P.part_ml[at] = make_float2(mm, ll);
+    const float inv = ll == 0.f ? (mm == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / ll;
+#pragma unroll
+    for (int e = 0; e < RR_PAGED_MAX_DH / 32; ++e)
+      if (lane + 32 * e < dh) {
+        if (P.direct) ((T*)P.out)[out_at(P, s, a) + lane + 32 * e] = rr_from_f32<T>(oo[e] * inv);
+        else P.part_o[at * dh + lane + 32 * e] = oo[e];
+      }
+  }
+}
+
+template <typename T, int NV>
+__global__ void __launch_bounds__(SNT) attend_simt_kernel(const __grid_constant__ Params P, bool vq, bool vk) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ uint32_t s_bad[2];
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  const SmemPlan L = smem_plan(P.dh, P.slots);
+  Ctx c;
+  c.q = (float*)(smem + L.q); c.kv = (float*)(smem + L.kv); c.p = (float*)(smem + L.p);
+  c.at = (long long*)(smem + L.ids); c.id = (int*)(c.at + BT);
+  c.first = (int*)(smem + L.slots); c.base = c.first + P.slots + 1;
+  c.n_tok = 0; c.vq = vq; c.vk = vk;
+  const int lane = threadIdx.x & 31, mg = P.m * P.group;
+  long long u, u0 = 0, u1;
+  if (P.slots) { u = blockIdx.x; u1 = P.range_rows * ((mg + ROWS - 1) / ROWS) * P.splits; }
+  else { const long long W = __ldg(P.cum + P.batch); u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
+  while (u < u1) {
+    Seg s;
+    if (P.slots) {
+      range_segment(P, u, s);
+      u += gridDim.x;
+      __syncthreads();                                 // the table before is no longer read
+      if (threadIdx.x < 32) {
+        int run = 0;
+        for (int j0 = 0; j0 < P.slots; j0 += 32) {
+          const int j = j0 + lane;
+          int lo = 0, hi = 0;
+          if (j < P.slots) slot_span(s, j, lo, hi);
+          int incl = hi - lo;
+#pragma unroll
+          for (int off = 1; off < 32; off <<= 1) { const int x = __shfl_up_sync(FULL, incl, off); if (lane >= off) incl += x; }
+          if (j < P.slots) { c.first[j] = run + incl - (hi - lo); c.base[j] = lo - c.first[j]; }
+          run += __shfl_sync(FULL, incl, 31);
+        }
+        if (lane == 0) c.first[P.slots] = run;
+      }
+      __syncthreads();
+      c.n_tok = c.first[P.slots];
+      split_tiles(P, (c.n_tok + TILE - 1) / TILE, s);
+    } else {
+      u += segment_at(P, blockIdx.x, u, u0, u1, s);
+    }
+    if (s.rows <= 16) rows_block<T, NV, 1>(P, s, c, 0, s_bad);
+    else for (int r0 = 0; r0 < s.rows; r0 += 64) rows_block<T, NV, 4>(P, s, c, r0, s_bad);
+  }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------
+template <typename T>
+cudaError_t launch_simt(const Params& P, int grid, cudaStream_t st) {
+  const SmemPlan L = smem_plan(P.dh, P.slots);
+  const uintptr_t b = 4 * sizeof(T) - 1;
+  const bool vq = P.dh % 4 == 0 && ((uintptr_t)P.q & b) == 0 && (P.qb | P.qh | P.qt) % 4 == 0;
+  const bool vk = P.dh % 4 == 0 && (((uintptr_t)P.k | (uintptr_t)P.v) & b) == 0 && (P.page_stride | P.head_stride | P.token_stride) % 4 == 0;
+  auto go = [&](auto kernel, unsigned long long& done) {
+    cudaError_t e = rr_once_per_device(done, [&] {
+      return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_plan(RR_PAGED_MAX_DH, RR_MAX_RANGE_SLOTS).total);
+    });
+    if (e != cudaSuccess) return e;
+    return rr_launch_pdl(kernel, grid, SNT, (size_t)L.total, st, P, vq, vk);
+  };
+  static unsigned long long done[4];
+  switch ((P.dh + 63) / 64) {
+    case 1: return go(attend_simt_kernel<T, 1>, done[0]);
+    case 2: return go(attend_simt_kernel<T, 2>, done[1]);
+    case 3: return go(attend_simt_kernel<T, 3>, done[2]);
+    default: return go(attend_simt_kernel<T, 4>, done[3]);
+  }
+}
+
+size_t up(size_t x) { return (x + 255) / 256 * 256; }
+// Offsets in the workspace: cum, part_ml, part_o.
+size_t lay_out(Params& P, uint8_t* ws) {
+  size_t at = 0;
+  P.cum = (long long*)(ws + at); at += up(P.slots ? 0 : (size_t)(P.batch + 1) * 8);
+  const size_t rows = (size_t)P.part_rows * P.streams;
+  P.part_ml = (float2*)(ws + at); at += up(rows * sizeof(float2));
+  P.part_o = (float*)(ws + at); at += up(rows * P.dh * sizeof(float));
+  return at;
+}
+
+int fill(const rr_paged_kv* kv, Params& P) {
+  const int rc = rr_paged_check(kv);
+  if (rc != RR_OK) return rc;
+  P = Params{};
+  P.k = kv->k; P.v = kv->v; P.table = kv->page_table; P.status = kv->status;
+  P.page_stride = kv->page_stride; P.head_stride = kv->head_stride; P.token_stride = kv->token_stride; P.table_stride = kv->table_stride;
+  P.num_pages = kv->num_pages; P.page_tokens = kv->page_tokens; P.kv_heads = kv->kv_heads; P.dh = kv->dh;
+  P.batch = kv->batch; P.pages_per_seq = kv->pages_per_seq;
+  if ((long long)kv->pages_per_seq * kv->page_tokens > 0x7FFFFFFFLL - ROWS) return RR_ERR_TOO_LARGE;
+  return RR_OK;
+}
+
+bool misaligned(const void* q, const void* out, int dtype) {
+  return (((uintptr_t)q | (uintptr_t)out) & (dtype == RR_BF16 ? 1 : 3)) != 0;
+}
+
+int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
+  const int rc = fill(kv, P);
+  if (rc != RR_OK) return rc;
+  if (!a || !a->q || !a->out || !a->lens) return RR_ERR_INVALID_ARG;
+  if (a->tokens < 0 || (!a->cu && a->tokens != kv->batch) || a->heads < 1 || a->heads % kv->kv_heads != 0) return RR_ERR_INVALID_ARG;
+  if (a->prefix_tokens < 0 || (a->causal != 0 && a->causal != 1) || !std::isfinite(a->scale)) return RR_ERR_INVALID_ARG;
+  if (!a->prefix_pages && a->prefix_tokens > (long long)kv->pages_per_seq * kv->page_tokens) return RR_ERR_INVALID_ARG;
+  if (a->prefix_tokens > 0x7FFFFFFF - ROWS) return RR_ERR_TOO_LARGE;
+  if (a->q_token_stride < 0 || a->q_head_stride < 0 || a->out_token_stride < 0 || a->out_head_stride < 0) return RR_ERR_INVALID_ARG;
+  if (misaligned(a->q, a->out, kv->dtype) || (((uintptr_t)a->lens | (uintptr_t)a->cu | (uintptr_t)a->prefix_pages) & 3)) return RR_ERR_INVALID_ARG;
+  if ((long long)a->tokens * a->heads > (1LL << 30)) return RR_ERR_TOO_LARGE;
+  P.q = a->q; P.out = a->out; P.lens = a->lens; P.cu = a->cu; P.prefix_pages = a->prefix_pages;
+  P.qt = a->q_token_stride; P.qh = a->q_head_stride; P.ot = a->out_token_stride; P.oh = a->out_head_stride;
+  P.tokens = a->tokens; P.heads = a->heads; P.group = a->heads / kv->kv_heads; P.causal = a->causal; P.prefix = a->prefix_tokens;
+  P.scale_log2 = a->scale * 1.4426950408889634f;
+  P.splits = 1;
+  P.streams = 1;
+  P.ctas = rr_sm_count() * 2;
+  P.part_rows = 2LL * P.tokens * P.heads + (long long)P.ctas * ROWS;
+  return RR_OK;
+}
+
+int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
+  const int rc = fill(kv, P);
+  if (rc != RR_OK) return rc;
+  if (!a || !a->q || !a->out || !a->lens || !a->ranges) return RR_ERR_INVALID_ARG;
+  if (a->heads < 1 || a->route_heads < 1 || a->n_q < 1 || a->m < 1 || a->slots < 1) return RR_ERR_INVALID_ARG;
+  if (a->route_heads % kv->kv_heads != 0 || a->heads % a->route_heads != 0) return RR_ERR_INVALID_ARG;
+  if ((a->causal != 0 && a->causal != 1) || !std::isfinite(a->scale)) return RR_ERR_INVALID_ARG;
+  if (a->q_batch_stride < 0 || a->q_head_stride < 0 || a->q_token_stride < 0 || a->out_batch_stride < 0 || a->out_head_stride < 0 || a->out_token_stride < 0)
+    return RR_ERR_INVALID_ARG;
+  if (misaligned(a->q, a->out, kv->dtype) || (((uintptr_t)a->lens | (uintptr_t)a->ranges) & 3)) return RR_ERR_INVALID_ARG;
+  if (a->slots > RR_MAX_RANGE_SLOTS || (long long)a->slots * kv->pages_per_seq * kv->page_tokens > 0x7FFFFFFFLL - ROWS) return RR_ERR_TOO_LARGE;
+  if ((long long)a->n_q * a->m > 0x7FFFFFFFLL - ROWS || (long long)a->m * (a->heads / a->route_heads) > 0x7FFFFFFFLL - ROWS) return RR_ERR_TOO_LARGE;
+  const double all = (double)kv->batch * a->heads * a->n_q * a->m;
+  if (all > (double)(1LL << 30)) return RR_ERR_TOO_LARGE;
+  P.q = a->q; P.out = a->out; P.lens = a->lens; P.ranges = a->ranges;
+  P.qb = a->q_batch_stride; P.qh = a->q_head_stride; P.qt = a->q_token_stride;
+  P.ob = a->out_batch_stride; P.oh = a->out_head_stride; P.ot = a->out_token_stride;
+  P.heads = a->heads; P.route_heads = a->route_heads; P.group = a->heads / a->route_heads; P.causal = a->causal;
+  P.n_q = a->n_q; P.m = a->m; P.slots = a->slots;
+  P.scale_log2 = a->scale * 1.4426950408889634f;
+  P.range_rows = (long long)kv->batch * a->route_heads * a->n_q;
+  P.streams = 1;
+  P.ctas = rr_sm_count() * 2;
+  // few rows: each is cut into parts, so that every SM has one
+  const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS);
+  P.splits = (int)(items >= P.ctas ? 1 : ceil_div(P.ctas, items));
+  if (P.splits > 64) P.splits = 64;
+  P.direct = P.splits == 1;
+  P.part_rows = P.direct && P.streams == 1 ? 0 : P.splits * P.range_rows * P.m * P.group;
+  return RR_OK;
+}
+
+int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, const char* what) {
+  const size_t need = lay_out(P, (uint8_t*)workspace);
+  if (need && !workspace) return RR_ERR_INVALID_ARG;
+  if ((uintptr_t)workspace & 255) return RR_ERR_INVALID_ARG;
+  if (bytes < need) return RR_ERR_TOO_SMALL;
+  cudaError_t e = cudaSuccess;
+  int launches = 0;
+  if (!P.slots) { e = rr_launch_pdl(plan_kernel, 1, PLAN_NT, 0, st, P); ++launches; }
+  if (e == cudaSuccess) {
+    long long grid = P.ctas;
+    if (P.slots) grid = std::min<long long>(grid, P.range_rows * ceil_div((long long)P.m * P.group, ROWS) * P.splits);
+    e = dtype == RR_BF16 ? launch_simt<__nv_bfloat16>(P, (int)grid, st) : launch_simt<float>(P, (int)grid, st);
+    ++launches;
+  }
+  if (e == cudaSuccess && P.part_rows > 0) {
+    const long long rows = P.slots ? P.range_rows * P.m * P.group : (long long)P.tokens * P.heads;
+    const int grid = (int)ceil_div(rows, 8);
+    e = dtype == RR_BF16 ? rr_launch_pdl(join_kernel<__nv_bfloat16>, grid, 256, 0, st, P) : rr_launch_pdl(join_kernel<float>, grid, 256, 0, st, P);
+    ++launches;
+  }
+  rr_count_launch(launches);
+  if (e == cudaSuccess) e = cudaPeekAtLastError();
+  return e == cudaSuccess ? RR_OK : rr_cuda_fail(e, what);
+}
+
+}  // namespace
+
+extern "C" {
+
+int rr_attend_shared_workspace(const rr_paged_kv* kv, const rr_shared_args* a, size_t* bytes) {
+  if (!bytes) return RR_ERR_INVALID_ARG;
+  Params P;
+  const int rc = fill_shared(kv, a, P);
+  if (rc == RR_OK) *bytes = lay_out(P, nullptr);
+  return rc;
+}
+
+int rr_attend_shared(const rr_paged_kv* kv, const rr_shared_args* a, void* workspace, size_t bytes, void* stream) {
+  Params P;
+  const int rc = fill_shared(kv, a, P);
+  if (rc != RR_OK) return rc;
+  if (a->tokens == 0) return RR_OK;
+  return run(P, kv->dtype, workspace, bytes, (cudaStream_t)stream, "rr_attend_shared");
+}
+
+int rr_attend_paged_ranges_workspace(const rr_paged_kv* kv, const rr_ranges_args* a, size_t* bytes) {
+  if (!bytes) return RR_ERR_INVALID_ARG;
+  Params P;
+  const int rc = fill_ranges(kv, a, P);
+  if (rc == RR_OK) *bytes = lay_out(P, nullptr);
+  return rc;
+}
+
+int rr_attend_paged_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, void* workspace, size_t bytes, void* stream) {
+  Params P;
+  const int rc = fill_ranges(kv, a, P);
+  if (rc != RR_OK) return rc;
+  return run(P, kv->dtype, workspace, bytes, (cudaStream_t)stream, "rr_attend_paged_ranges");
+}
+
+}  // extern "C"

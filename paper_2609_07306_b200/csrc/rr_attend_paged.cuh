@@ -1,0 +1,252 @@
+// Attention over a paged key/value cache: how the work of rr_attend_shared and rr_attend_paged_ranges is cut
+// into segments, where a segment's partial results go, and how they are joined.  Two kernels process segments: the tensor cores'
+// (rr_attend_paged_tc.cu) and the one for every other type and width (rr_attend_paged.cu).
+//
+// An ITEM is up to ROWS query rows that attend to one list of tokens of one key head:
+//   shared, prefix   the queries of all sequences and of the G = heads / kv_heads query heads of a key head (row t * G + g),
+//                    over the prefix's tokens
+//   shared, own      the same rows of one sequence, over its tokens behind the prefix
+//   ranges           the m * G queries of a range row, over the tokens of its slots
+// A list is walked in tiles of TILE tokens.  A SEGMENT is a run of tiles of an item; it leaves per row a
+// partial result: reference maximum m (of logit * log2 e), sum l of 2^(x - m), and the unnormalised output.  The partials
+// of a row are joined in a fixed order by join_kernel.
+//
+// shared: the tiles of all items in one row, N CTAs take equal shares of it (an item may be cut anywhere, a
+// CTA's share may span many items), so neither a long prefix of few rows nor one long sequence among short ones leaves SMs idle.
+// plan_kernel counts the tiles on the device, where the lengths are.  A segment that begins its item has its partial rows at
+// the rows' own places; a CTA has at most one segment that does not, whose rows go to the CTA's own ROWS places.
+// ranges: items are alike, and each is cut into `splits` parts by its own number of tiles.
+#pragma once
+#include "rr_paged.cuh"
+
+namespace rrattn {
+
+constexpr int TILE = 128, ROWS = 256;
+constexpr int NO_TOKEN = 0x7FFFFFFF;                   // id of a place without a token: above every limit
+constexpr float NINF = -__builtin_huge_valf();
+constexpr float LOWEST = -3.402823466e38f;             // m of a row that saw tokens, all of them at -inf
+
+struct Params {
+  // cache
+  const void *k, *v;
+  const int32_t* table;
+  uint32_t* status;
+  long long page_stride, head_stride, token_stride, table_stride;
+  int num_pages, page_tokens, kv_heads, dh, batch, pages_per_seq;
+  // queries
+  const void* q;
+  void* out;
+  long long qb, qh, qt, ob, oh, ot;                    // strides: batch (ranges), head, token
+  const int32_t *lens, *cu, *prefix_pages, *ranges;
+  int tokens, heads, group, causal;                    // group: query heads of an item
+  int prefix;                                          // shared
+  int n_q, m, slots, route_heads;                      // ranges (slots > 0)
+  float scale_log2;                                    // scale * log2 e
+  // schedule
+  int ctas, splits, streams;                           // streams: partials per segment and row (1, or 2: see Seg::paired)
+  long long range_rows;                                // batch * route_heads * n_q
+  // workspace
+  long long* cum;                                      // shared: [batch + 1] tiles before sequence b's items; [batch] = all tiles
+  float* part_o;                                       // [streams][part_rows][dh]
+  float2* part_ml;                                     // [streams][part_rows]
+  long long part_rows;
+  int direct;                                          // ranges, splits == 1: no partials where one stream has the row
+};
+
+struct Seg {
+  int rows, row0;                                      // rows row0 .. row0 + rows - 1 of the item's group, row = (t - t_base) * group + g
+  int t_base, t_seq0, n_seq;                           // first token; own / ranges: first token and number of the sequence's queries
+  int b;                                               // sequence, -1: prefix (rows of all sequences)
+  int kvh, h0;                                         // key head, first query head
+  int tok0, tok1;                                      // dense: the list's tokens
+  const int32_t* pages;                                // page list of the tokens
+  const int32_t* slots;                                // ranges: the row's slots, else null
+  int tile0, tile1;                                    // the segment's tiles of the list (ranges: of `split`, once counted)
+  int split;
+  long long part;                                      // partial row of row 0
+};
+
+__host__ __device__ inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// Tokens that sequence b has in the cache (never more than its table holds).
+__device__ __forceinline__ int seq_len(const Params& P, int b) {
+  const long long cap = (long long)P.pages_per_seq * P.page_tokens;
+  const int n = max(__ldg(P.lens + b), 0);
+  return n > cap ? (int)cap : n;
+}
+__device__ __forceinline__ int seq_first(const Params& P, int b) { return P.cu ? __ldg(P.cu + b) : b; }
+__device__ __forceinline__ int seq_count(const Params& P, int b) {
+  if (!P.cu) return 1;
+  const int a = __ldg(P.cu + b), e = min(__ldg(P.cu + b + 1), P.tokens);
+  return a < 0 ? 0 : max(e - a, 0);
+}
+__device__ __forceinline__ long long prefix_tiles(const Params& P) { return (P.prefix + TILE - 1) / TILE; }
+__device__ __forceinline__ long long prefix_row_tiles(const Params& P) { return ceil_div((long long)P.tokens * P.group, ROWS); }
+__device__ __forceinline__ int own_tiles(const Params& P, int b) { return (max(seq_len(P, b) - P.prefix, 0) + TILE - 1) / TILE; }
+__device__ __forceinline__ int own_row_tiles(const Params& P, int b) { return (int)ceil_div((long long)seq_count(P, b) * P.group, ROWS); }
+
+// With N = min(ctas, W) CTAs at work, CTA c's share of W tiles is [c W / N, (c + 1) W / N), at least one tile: an item that
+// is cut is in consecutive CTAs.  cta_of: the CTA that has tile u.
+__device__ __forceinline__ long long share(const Params& P, int c, long long W) {
+  const long long N = min((long long)P.ctas, W);
+  return c >= N ? W : c * W / N;
+}
+__device__ __forceinline__ int cta_of(const Params& P, long long u, long long W) {
+  const long long N = min((long long)P.ctas, W);
+  return (int)(((u + 1) * N + W - 1) / W - 1);
+}
+
+// The segment at tile u of CTA c's share, which ends at u1; returns its number of tiles.
+__device__ __forceinline__ int segment_at(const Params& P, int c, long long u, long long u0, long long u1, Seg& s) {
+  const long long np = prefix_tiles(P), qtp = prefix_row_tiles(P), before = P.kv_heads * qtp * np;
+  long long first;                                     // first tile of the item
+  int tiles;
+  long long home;
+  const long long row_all = (long long)P.tokens * P.group;
+  s.slots = nullptr;
+  s.split = 0;
+  if (u < before) {
+    const long long item = u / np;
+    first = item * np;
+    tiles = (int)np;
+    s.kvh = (int)(item / qtp);
+    s.row0 = (int)(item % qtp) * ROWS;
+    s.rows = (int)min((long long)ROWS, row_all - s.row0);
+    s.b = -1;
+    s.t_base = 0; s.t_seq0 = 0; s.n_seq = 0;
+    s.tok0 = 0; s.tok1 = P.prefix;
+    s.pages = P.prefix_pages ? P.prefix_pages : P.table;
+    home = s.kvh * row_all + s.row0;
+  } else {
+    int lo = 0, hi = P.batch;                          // last b with cum[b] <= u
+    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (__ldg(P.cum + mid) <= u) lo = mid; else hi = mid; }
+    const int b = lo, qt = own_row_tiles(P, b);
+    tiles = own_tiles(P, b);
+    const long long base = __ldg(P.cum + b), item = (u - base) / tiles;
+    first = base + item * tiles;
+    s.kvh = (int)(item / qt);
+    s.row0 = (int)(item % qt) * ROWS;
+    s.n_seq = seq_count(P, b);
+    s.rows = (int)min((long long)ROWS, (long long)s.n_seq * P.group - s.row0);
+    s.b = b;
+    s.t_base = s.t_seq0 = seq_first(P, b);
+    s.tok0 = P.prefix; s.tok1 = seq_len(P, b);
+    s.pages = P.table + b * P.table_stride;
+    home = (P.kv_heads + s.kvh) * row_all + (long long)s.t_base * P.group + s.row0;
+  }
+  s.h0 = s.kvh * P.group;
+  s.tile0 = (int)(u - first);
+  s.tile1 = (int)min((long long)tiles, u1 - first);
+  s.part = s.tile0 == 0 ? home : 2 * (long long)P.tokens * P.heads + (long long)c * ROWS;
+  return s.tile1 - s.tile0;
+}
+
+// Segment x of a ranges call (x < range_rows * row tiles * splits); its tiles are counted by who reads the slots.
+__device__ __forceinline__ void range_segment(const Params& P, long long x, Seg& s) {
+  const int mg = P.m * P.group, qt = (mg + ROWS - 1) / ROWS;
+  s.split = (int)(x % P.splits);
+  const long long item = x / P.splits, row = item / qt;
+  s.row0 = (int)(item % qt) * ROWS;
+  s.rows = min(ROWS, mg - s.row0);
+  const int i = (int)(row % P.n_q), r = (int)(row / P.n_q % P.route_heads);
+  s.b = (int)(row / P.n_q / P.route_heads);
+  s.t_seq0 = 0; s.n_seq = P.n_q * P.m;
+  s.t_base = i * P.m;
+  s.kvh = r / (P.route_heads / P.kv_heads);
+  s.h0 = r * P.group;
+  s.tok0 = 0; s.tok1 = seq_len(P, s.b);
+  s.pages = P.table + s.b * P.table_stride;
+  s.slots = P.ranges + row * P.slots * 2;
+  s.tile0 = s.tile1 = 0;
+  s.part = (s.split * P.range_rows + row) * mg + s.row0;
+}
+// The part of `tiles` tiles that split s has.
+__device__ __forceinline__ void split_tiles(const Params& P, int tiles, Seg& s) {
+  s.tile0 = (int)((long long)tiles * s.split / P.splits);
+  s.tile1 = (int)((long long)tiles * (s.split + 1) / P.splits);
+}
+// Tokens of one slot: [lo, hi) clipped to the sequence.
+__device__ __forceinline__ void slot_span(const Seg& s, int j, int& lo, int& hi) {
+  lo = __ldg(s.slots + 2 * j);
+  hi = min(__ldg(s.slots + 2 * j + 1), s.tok1);
+  if (lo < 0 || hi < lo) lo = hi = 0;
+}
+
+struct RowAt { int t, h, limit; };                     // query token, head, tokens below `limit` are seen
+__device__ __forceinline__ RowAt row_at(const Params& P, const Seg& s, int r) {
+  const int idx = s.row0 + r, dt = idx / P.group;
+  RowAt a;
+  a.t = s.t_base + dt;
+  a.h = s.h0 + idx - dt * P.group;
+  int b = s.b, first = s.t_seq0, n = s.n_seq;
+  if (b < 0) {
+    b = P.cu ? rr_sequence_of(P.cu, P.batch, a.t) : a.t;
+    if (b < 0) { a.limit = 0; return a; }
+    first = seq_first(P, b);
+    n = seq_count(P, b);
+  }
+  const int len = seq_len(P, b);
+  a.limit = P.causal ? max(len - n + (a.t - first) + 1, 0) : len;
+  return a;
+}
+__device__ __forceinline__ long long q_at(const Params& P, const Seg& s, const RowAt& a) { return (s.slots ? s.b * P.qb : 0) + a.h * P.qh + a.t * P.qt; }
+__device__ __forceinline__ long long out_at(const Params& P, const Seg& s, const RowAt& a) { return (s.slots ? s.b * P.ob : 0) + a.h * P.oh + a.t * P.ot; }
+
+// Element offset of token `tok` of the segment's list, -1 if its page id is bad.
+__device__ __forceinline__ long long token_at(const Params& P, const Seg& s, int tok) {
+  const int col = tok / P.page_tokens, page = __ldg(s.pages + col);
+  if (page < 0 || page >= P.num_pages) { if (P.status) atomicOr(P.status, RR_STATUS_BAD_INDEX); return -1; }
+  return page * P.page_stride + s.kvh * P.head_stride + (tok - col * P.page_tokens) * P.token_stride;
+}
+
+// ---- exact repair ------------------------------------------------------------------------------------------
+// A tile is multiplied whole, so a value that a row may not see enters the row's sums with weight 0: nothing, unless it is an
+// infinity or NaN.  A row with such a result that has masked tokens of its list is computed again here, token by
+// token, by a warp: only what it sees is read.  (Rows that see an infinity come here as well, and keep it.)
+// Tiles tile0 + first, tile0 + first + step, ... of the segment.
+template <typename T>
+__device__ __noinline__ void repair_row(const Params& P, const Seg& s, int r, int first, int step, float& m, float& l, float (&o)[RR_PAGED_MAX_DH / 32]) {
+  constexpr int E = RR_PAGED_MAX_DH / 32;
+  const int lane = threadIdx.x & 31;
+  const RowAt a = row_at(P, s, r);
+  const T* const q = (const T*)P.q + q_at(P, s, a);
+  float qv[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) { qv[e] = lane + 32 * e < P.dh ? rr_to_f32(q[lane + 32 * e]) : 0.f; o[e] = 0.f; }
+  m = NINF; l = 0.f;
+  bool seen = false;
+  long long num = 0;                                   // number of the span's first token in the list
+  const int spans = s.slots ? P.slots : 1;
+  for (int j = 0; j < spans; ++j) {
+    int lo = s.tok0, hi = s.tok1;
+    if (s.slots) slot_span(s, j, lo, hi);
+    for (int tok = lo; tok < hi; ++tok) {
+      const long long n = num + (tok - lo), tile = n / TILE;
+      if (tile < s.tile0 + first || tile >= s.tile1 || (tile - s.tile0 - first) % step != 0) continue;
+      if (tok >= a.limit) continue;
+      const long long at = token_at(P, s, tok);
+      if (at < 0) continue;
+      seen = true;
+      float x = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) x = fmaf(qv[e], rr_to_f32(((const T*)P.k)[at + lane + 32 * e]), x);
+#pragma unroll
+      for (int off = 16; off; off >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, off);
+      x *= P.scale_log2;
+      const float m_new = fmaxf(m, x), ref = m_new == NINF ? 0.f : m_new;
+      const float f = exp2f(m - ref), w = exp2f(x - ref);
+      l = l * f + w;
+      m = m_new;
+#pragma unroll
+      for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) o[e] = fmaf(w, rr_to_f32(((const T*)P.v)[at + lane + 32 * e]), o[e] * f);
+    }
+    num += hi - lo;
+  }
+  if (seen && m == NINF) m = LOWEST;
+}
+
+}  // namespace rrattn
+
+// One CTA per SM; dh 64 or 128, bf16, strides in whole rows of dh entries.
+bool rr_attend_tc_supported(const rrattn::Params& p, int dtype);
+cudaError_t rr_launch_attend_tc(const rrattn::Params& p, cudaStream_t st);

@@ -205,6 +205,8 @@ cudaError_t rr_launch_expand(const RRParams& p, int is_anchor, cudaStream_t st);
 cudaError_t rr_launch_reset(const RRParams& p, cudaStream_t st);
 
 void rr_count_launch(int n = 1);
+// Records the error for rr_last_cuda_error and returns RR_ERR_CUDA.
+int rr_cuda_fail(cudaError_t e, const char* what);
 
 // SMs of the current device (148 where the query fails).
 inline int rr_sm_count() {
