@@ -478,8 +478,9 @@ int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   P.tokens = a->tokens; P.heads = a->heads; P.group = a->heads / kv->kv_heads; P.causal = a->causal; P.prefix = a->prefix_tokens;
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.splits = 1;
-  P.streams = 1;
-  P.ctas = rr_sm_count() * 2;
+  P.tc = rr_attend_tc_supported(P, kv->dtype);
+  P.streams = P.tc ? 2 : 1;
+  P.ctas = rr_sm_count() * (P.tc ? 1 : 2);
   P.part_rows = 2LL * P.tokens * P.heads + (long long)P.ctas * ROWS;
   return RR_OK;
 }
@@ -505,14 +506,17 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.n_q = a->n_q; P.m = a->m; P.slots = a->slots;
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.range_rows = (long long)kv->batch * a->route_heads * a->n_q;
-  P.streams = 1;
-  P.ctas = rr_sm_count() * 2;
+  P.tc = rr_attend_tc_supported(P, kv->dtype);
+  P.streams = P.tc ? 2 : 1;
+  P.ctas = rr_sm_count() * (P.tc ? 1 : 2);
   // few rows: each is cut into parts, so that every SM has one
   const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS);
   P.splits = (int)(items >= P.ctas ? 1 : ceil_div(P.ctas, items));
   if (P.splits > 64) P.splits = 64;
   P.direct = P.splits == 1;
-  P.part_rows = P.direct && P.streams == 1 ? 0 : P.splits * P.range_rows * P.m * P.group;
+  // (a row of an item with more than TILE rows has one stream: the last item of a range row may have fewer)
+  const int mg = P.m * P.group, last = mg % ROWS;
+  P.part_rows = P.direct && (P.streams == 1 || last == 0 || last > TILE) ? 0 : P.splits * P.range_rows * P.m * P.group;
   return RR_OK;
 }
 
@@ -527,7 +531,8 @@ int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, co
   if (e == cudaSuccess) {
     long long grid = P.ctas;
     if (P.slots) grid = std::min<long long>(grid, P.range_rows * ceil_div((long long)P.m * P.group, ROWS) * P.splits);
-    e = dtype == RR_BF16 ? launch_simt<__nv_bfloat16>(P, (int)grid, st) : launch_simt<float>(P, (int)grid, st);
+    if (P.tc) e = rr_launch_attend_tc(P, (int)grid, st);
+    else e = dtype == RR_BF16 ? launch_simt<__nv_bfloat16>(P, (int)grid, st) : launch_simt<float>(P, (int)grid, st);
     ++launches;
   }
   if (e == cudaSuccess && P.part_rows > 0) {

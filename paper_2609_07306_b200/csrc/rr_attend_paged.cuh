@@ -43,7 +43,7 @@ struct Params {
   int n_q, m, slots, route_heads;                      // ranges (slots > 0)
   float scale_log2;                                    // scale * log2 e
   // schedule
-  int ctas, splits, streams;                           // streams: partials per segment and row (1, or 2: see Seg::paired)
+  int tc, ctas, splits, streams;                         // streams: partials per segment and row (1, or 2: see Seg::paired)
   long long range_rows;                                // batch * route_heads * n_q
   // workspace
   long long* cum;                                      // shared: [batch + 1] tiles before sequence b's items; [batch] = all tiles
@@ -249,4 +249,4 @@ __device__ __noinline__ void repair_row(const Params& P, const Seg& s, int r, in
 
 // One CTA per SM; dh 64 or 128, bf16, strides in whole rows of dh entries.
 bool rr_attend_tc_supported(const rrattn::Params& p, int dtype);
-cudaError_t rr_launch_attend_tc(const rrattn::Params& p, cudaStream_t st);
+cudaError_t rr_launch_attend_tc(const rrattn::Params& p, int grid, cudaStream_t st);

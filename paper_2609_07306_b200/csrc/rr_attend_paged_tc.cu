@@ -1,0 +1,553 @@
+// Segments of attention over a paged cache on the 5th-generation tensor cores: bf16, dh 64 or 128 (see rr_attend_paged.cuh
+// for items, segments and how their partial results are joined).
+//
+// One CTA per SM walks its segments.  Per tile of 128 tokens and 128 query rows:  S = Q K^T (TMEM, FP32), softmax against a
+// running reference, P (bf16, written over S in TMEM) and O += P V (TMEM, FP32).  Two streams of four warps
+// keep the tensor pipe and the exponentials busy in turn:
+//   a segment of more than 128 rows is paired: stream 0 has rows 0..127, stream 1 the others, each tile of keys and values is
+//   read once for both;
+//   one of up to 128 rows is split: both streams have the same rows, stream 0 the even tiles and stream 1 the odd ones, and
+//   each leaves a partial result of its own.
+// The tensor pipe takes 2 x 520 cycles for a 128 x 128 x 128 tile's two products, the 16384 exponentials take 1024: many rows are
+// bound by both about equally, few rows by the cache's traffic.
+//
+// Warps 0-3, 4-7: the streams, a thread per row.  8: copies (tile::gather4, four token rows of 64 entries each, through
+// whatever pages they lie in; a place without a token is a row behind the map's end and arrives as zeros).  9: issues the products.
+// 10: finds the segments.  11: brings query rows and their limits.  Segments go round in a ring of
+// P.ring, so that the next one's look-ups and queries are there before it begins.
+// Step k of a segment is (stream k % 2, tile k / 2 if paired, else k):  S(k) is issued behind the product with P(k - 2) of the
+// same stream, which reads the same columns; the tensor pipe keeps that order.
+//
+// The reference of the softmax follows the row's maximum only when that has grown by more than 8 (a factor of
+// 256): weights up to 2^8 lose nothing in bf16 and FP32, and the output is rescaled in TMEM a few times per
+// segment instead of at every tile.
+//
+// Every wait is bounded; one that runs out sets RR_STATUS_TIMEOUT, and the CTA waits for its copies and
+// products in flight, frees its TMEM and returns.
+#include <cmath>
+#include "rr_attend_paged.cuh"
+#include "rr_sm100.cuh"
+
+using namespace rrattn;
+using namespace sm100;
+
+namespace {
+
+constexpr unsigned FULL = 0xFFFFFFFFu;
+constexpr int NT = 384, IDS = 8, MAX_RING = 4;
+constexpr float GROWTH = 8.f;
+
+template <int D> struct Shape {
+  static constexpr int HALVES = D / 64, STAGES = D == 128 ? 4 : 8;
+  static constexpr int HALF_BYTES = TILE * 128, TILE_BYTES = HALVES * HALF_BYTES;
+};
+
+struct Ctl {
+  uint64_t full[8], empty[8], s_full[2], p_full[2], o_full[2], q_full[2], q_empty[2], ids_full[IDS], seg_full[MAX_RING], seg_empty[MAX_RING],
+      rows_full[MAX_RING], drain;
+  uint32_t tmem_base, abort_flag;
+  Seg seg[MAX_RING];
+  int limit[MAX_RING][ROWS];
+  int ids[IDS][TILE];
+  int max_id[IDS];
+};
+
+struct Smem {
+  template <int D> __host__ __device__ static constexpr int ctl() { return (2 + Shape<D>::STAGES) * Shape<D>::TILE_BYTES; }
+  template <int D> __host__ __device__ static constexpr int slots() { return ctl<D>() + (int)((sizeof(Ctl) + 15) / 16 * 16); }
+  template <int D> static int total(int n_slots, int ring) { return 1024 + slots<D>() + (n_slots > 0 ? ring * (2 * n_slots + 1) * 4 : 0); }
+};
+
+__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, int col, const int (&r)[4], uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(col), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(smem_u32(bar)) : "memory");
+}
+// The values as second operand: its rows are the product's summed dimension (tokens), 128 bytes apart, the 64 columns of a half contiguous
+// (MN-major, 128-byte swizzle): groups of 8 rows 1024 bytes apart, halves HALF_BYTES apart.
+__device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t addr, uint32_t half_bytes) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(half_bytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__host__ __device__ constexpr uint32_t idesc_b_mn(int M, int N) { return umma_idesc_bf16(M, N) | 1u << 16; }
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// No use of these registers is moved above this point.
+__device__ __forceinline__ void tie(uint32_t (&r)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  uint32_t y; asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo)); return y;
+}
+
+// (a negative scale is taken as its magnitude with the queries negated, so that the largest product has the largest logit)
+struct RowStrides { int page, head, token, rows; };    // in rows of dh entries; rows: the map's
+
+template <int D>
+__global__ void __launch_bounds__(NT, 1)
+attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                 const RowStrides rs, const int ring, const float scale, const int negate) {
+  using S = Shape<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* const sQ = smem;
+  const uint32_t q_addr = smem_u32(smem), kv_addr = q_addr + 2 * S::TILE_BYTES;
+  Ctl* const c = (Ctl*)(smem + Smem::ctl<D>());
+  int* const slot_table = (int*)(smem + Smem::slots<D>());
+  volatile uint32_t* const abort_flag = &c->abort_flag;
+  const int warp = __shfl_sync(FULL, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S::STAGES; ++i) { mbar_init(&c->full[i], 1); mbar_init(&c->empty[i], 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&c->s_full[i], 1); mbar_init(&c->p_full[i], 128); mbar_init(&c->o_full[i], 1);
+      mbar_init(&c->q_full[i], 1); mbar_init(&c->q_empty[i], 1);
+    }
+    for (int i = 0; i < IDS; ++i) mbar_init(&c->ids_full[i], 1);
+    for (int i = 0; i < MAX_RING; ++i) { mbar_init(&c->seg_full[i], 1); mbar_init(&c->seg_empty[i], 11); mbar_init(&c->rows_full[i], 1); }
+    mbar_init(&c->drain, 1);
+    c->abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&map_k);
+    tma_prefetch_desc(&map_v);
+  }
+  if (warp == 9) tmem_alloc(&c->tmem_base, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(FULL, c->tmem_base, 0);
+  rr_pdl_wait();
+  rr_pdl_trigger();
+
+  // The segment ring as its readers see it: n counts segments.
+  auto seg_wait = [&](int n) -> bool { return __all_sync(FULL, mbar_wait_spin(&c->seg_full[n % ring], n / ring & 1, abort_flag)); };
+  auto seg_done = [&](int n) { __syncwarp(); if (lane == 0) mbar_arrive(&c->seg_empty[n % ring]); };
+
+  if (warp == 10) {
+    // ===== the segments =====
+    long long u, u0 = 0, u1;
+    if (P.slots) { u = blockIdx.x; u1 = P.range_rows * ((P.m * P.group + ROWS - 1) / ROWS) * P.splits; }
+    else { const long long W = __ldg(P.cum + P.batch); u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
+    for (int n = 0;; ++n) {
+      Seg s;
+      const bool end = u >= u1;
+      if (end) { s.rows = 0; }
+      else if (P.slots) { range_segment(P, u, s); u += gridDim.x; }
+      else u += segment_at(P, blockIdx.x, u, u0, u1, s);
+      if (!__all_sync(FULL, mbar_wait_spin(&c->seg_empty[n % ring], (n / ring & 1) ^ 1, abort_flag))) break;
+      if (!end && P.slots) {                           // number the row's tokens
+        int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
+        int* const base = first + P.slots + 1;
+        int run = 0;
+        for (int j0 = 0; j0 < P.slots; j0 += 32) {
+          const int j = j0 + lane;
+          int lo = 0, hi = 0;
+          if (j < P.slots) slot_span(s, j, lo, hi);
+          int incl = hi - lo;
+#pragma unroll
+          for (int off = 1; off < 32; off <<= 1) { const int x = __shfl_up_sync(FULL, incl, off); if (lane >= off) incl += x; }
+          if (j < P.slots) { first[j] = run + incl - (hi - lo); base[j] = lo - first[j]; }
+          run += __shfl_sync(FULL, incl, 31);
+        }
+        if (lane == 0) first[P.slots] = run;
+        split_tiles(P, (run + TILE - 1) / TILE, s);
+      }
+      if (lane == 0) c->seg[n % ring] = s;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&c->seg_full[n % ring]);
+      if (end) break;
+    }
+  } else if (warp == 11) {
+    // ===== query rows: into Q places 0 and 1 in turn, two for a paired segment =====
+    int place = 0;
+    for (int n = 0; seg_wait(n); ++n) {
+      const Seg s = c->seg[n % ring];
+      if (s.rows == 0) break;
+      for (int r = lane; r < s.rows; r += 32) c->limit[n % ring][r] = row_at(P, s, r).limit;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&c->rows_full[n % ring]);
+      bool ok = true;
+      for (int h = 0; h < (s.rows > TILE ? 2 : 1) && s.tile1 > s.tile0; ++h, ++place) {
+        const int at = place & 1;
+        ok = __all_sync(FULL, mbar_wait(&c->q_empty[at], (place >> 1 & 1) ^ 1, abort_flag));
+        if (!ok) break;
+        constexpr int CPR = D / 8;
+        const int rows = min(s.rows - h * TILE, TILE);
+        const uint32_t flip = negate ? 0x80008000u : 0u;
+        for (int c0 = lane; c0 < rows * CPR; c0 += 32 * 8) {
+          uint4 v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int ch = c0 + 32 * i;
+            if (ch >= rows * CPR) continue;
+            const int idx = s.row0 + h * TILE + ch / CPR, dt = idx / P.group;
+            const RowAt a{s.t_base + dt, s.h0 + idx - dt * P.group, 0};
+            v[i] = __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)P.q + q_at(P, s, a) + ch % CPR * 8));
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int ch = c0 + 32 * i;
+            if (ch >= rows * CPR) continue;
+            const int r = ch / CPR, c16 = ch % CPR;
+            v[i].x ^= flip; v[i].y ^= flip; v[i].z ^= flip; v[i].w ^= flip;
+            *reinterpret_cast<uint4*>(sQ + at * S::TILE_BYTES + (c16 >> 3) * S::HALF_BYTES + r * 128 + (((c16 & 7) ^ (r & 7)) << 4)) = v[i];
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c->q_full[at]);
+      }
+      if (!ok) break;
+      seg_done(n);
+    }
+  } else if (warp == 8) {
+    // ===== copies: fills 2 i (keys) and 2 i + 1 (values) of the CTA's i-th tile =====
+    int tiles = 0;                                     // of all segments so far
+    uint32_t fills = 0;
+    bool ok = true;
+    for (int n = 0; ok && seg_wait(n); ++n) {
+      const Seg s = c->seg[n % ring];
+      if (s.rows == 0) break;
+      const int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
+      const int* const base = first + P.slots + 1;
+      const int n_tok = P.slots ? first[P.slots] : s.tok1 - s.tok0;
+      int row[4], next[4];
+      auto find = [&](int tile, int cnt, int (&row)[4]) {   // this lane's four tokens of a tile: ids for the streams, rows of the map
+        int id[4], top = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int num = tile * TILE + lane * 4 + j;
+          id[j] = NO_TOKEN;
+          row[j] = rs.rows;
+          if (num < n_tok) {
+            int tok;
+            if (P.slots) {
+              int lo = 0, hi = P.slots;
+              while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (first[mid] <= num) lo = mid; else hi = mid; }
+              tok = base[lo] + num;
+            } else {
+              tok = s.tok0 + num;
+            }
+            const int col = tok / P.page_tokens, page = __ldg(s.pages + col);
+            if (page >= 0 && page < P.num_pages) {
+              id[j] = tok;
+              row[j] = page * rs.page + s.kvh * rs.head + (tok - col * P.page_tokens) * rs.token;
+            } else if (P.status) {
+              atomicOr(P.status, RR_STATUS_BAD_INDEX);
+            }
+          }
+          top = max(top, id[j]);
+        }
+        top = __reduce_max_sync(FULL, top);
+        *reinterpret_cast<int4*>(&c->ids[cnt % IDS][lane * 4]) = make_int4(id[0], id[1], id[2], id[3]);
+        if (lane == 0) c->max_id[cnt % IDS] = top;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c->ids_full[cnt % IDS]);
+      };
+      auto load = [&](const CUtensorMap* map, const int (&row)[4]) -> bool {
+        const int st = fills % S::STAGES;
+        if (!__all_sync(FULL, mbar_wait_spin(&c->empty[st], (fills / S::STAGES & 1) ^ 1, abort_flag))) return false;
+        if (lane == 0) mbar_expect_tx(&c->full[st], S::TILE_BYTES);
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < S::HALVES; ++h)
+          gather4(kv_addr + st * S::TILE_BYTES + h * S::HALF_BYTES + lane * 512, map, h * 64, row, &c->full[st]);
+        ++fills;
+        return true;
+      };
+      if (s.tile0 < s.tile1) find(s.tile0, tiles, next);
+      for (int t = s.tile0; t < s.tile1; ++t) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) row[j] = next[j];
+        ok = load(&map_k, row);
+        if (!ok) break;
+        if (t + 1 < s.tile1) find(t + 1, tiles + 1, next);
+        ok = load(&map_v, row);
+        if (!ok) break;
+        ++tiles;
+      }
+      if (ok) seg_done(n);
+    }
+    // do not leave while copies into this CTA's shared memory may be in flight
+    for (uint32_t f = fills > S::STAGES ? fills - S::STAGES : 0; f < fills; ++f)
+      for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->full[f % S::STAGES], f / S::STAGES & 1); ++it) __nanosleep(64);
+    __syncwarp();
+  } else if (warp == 9) {
+    // ===== products =====
+    constexpr uint32_t idesc_s = umma_idesc_bf16(TILE, TILE), idesc_o = idesc_b_mn(TILE, D);
+    int place = 0;
+    uint32_t tiles = 0, p_cnt[2] = {0, 0};
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL, mbar_wait_spin(bar, parity & 1, abort_flag)); };
+    for (int n = 0; ok && seg_wait(n); ++n) {
+      const int rows = __shfl_sync(FULL, c->seg[n % ring].rows, 0);
+      const int nt = __shfl_sync(FULL, c->seg[n % ring].tile1 - c->seg[n % ring].tile0, 0);
+      if (rows == 0) break;
+      const bool paired = rows > TILE;
+      const int steps = paired ? 2 * nt : nt;
+      if (steps == 0) { seg_done(n); continue; }
+      ok = wait(&c->q_full[place & 1], place >> 1);
+      if (ok && paired) ok = wait(&c->q_full[(place + 1) & 1], (place + 1) >> 1);
+      for (int k = 0; ok && k < steps + 2; ++k) {
+        if (k >= 2) {
+          const int kk = k - 2, st = kk & 1;
+          const uint32_t f = 2 * (tiles + (paired ? kk >> 1 : kk)) + 1, stage = f % S::STAGES;
+          ok = wait(&c->p_full[st], p_cnt[st]) && wait(&c->full[stage], f / S::STAGES);
+          if (!ok) break;
+          ++p_cnt[st];
+          tc_fence_after();
+          const uint64_t vd = desc_mn_sw128(kv_addr + stage * S::TILE_BYTES, S::HALF_BYTES);
+#pragma unroll
+          for (int j = 0; j < TILE / 16; ++j)
+            umma_bf16_ts_warp(tmem + 256 + st * 128, tmem + st * 128 + j * 8, vd + (uint64_t)(j * 128), idesc_o, (kk >= 2 || j > 0) ? 1u : 0u);
+          if (!paired || st == 1) umma_commit_warp(&c->empty[stage]);
+          if (kk + 2 >= steps) umma_commit_warp(&c->o_full[st]);
+        }
+        if (k < steps) {
+          const int st = k & 1;
+          const uint32_t f = 2 * (tiles + (paired ? k >> 1 : k)), stage = f % S::STAGES;
+          const int at = (place + (paired ? st : 0)) & 1;
+          ok = wait(&c->full[stage], f / S::STAGES);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t qd = umma_desc_k_sw128(q_addr + at * S::TILE_BYTES), kd = umma_desc_k_sw128(kv_addr + stage * S::TILE_BYTES);
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) {
+            const uint64_t o = (uint64_t)((j >> 2) * (S::HALF_BYTES >> 4) + (j & 3) * 2);
+            umma_bf16_warp(tmem + st * 128, qd + o, kd + o, idesc_s, j > 0 ? 1u : 0u);
+          }
+          umma_commit_warp(&c->s_full[st]);
+          if (!paired || st == 1) umma_commit_warp(&c->empty[stage]);
+          if (paired ? k + 2 >= steps : k + 1 == steps) umma_commit_warp(&c->q_empty[at]);
+        }
+      }
+      if (!ok) break;
+      tiles += nt;
+      place += paired ? 2 : 1;
+      seg_done(n);
+    }
+    umma_commit_warp(&c->drain);
+    for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->drain, 0); ++it) __nanosleep(64);
+    __syncwarp();
+  } else {
+    // ===== a stream: thread = row =====
+    const int st = warp >> 2, quarter = warp & 3;
+    const int r_in = quarter * 32 + lane;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t s_tm = tmem + lanes + st * 128, o_tm = tmem + lanes + 256 + st * 128;
+    uint32_t s_cnt = 0, o_cnt = 0;
+    int tiles = 0;
+    bool ok = true;
+    for (int n = 0; ok && seg_wait(n); ++n) {
+      const Seg s = c->seg[n % ring];
+      if (s.rows == 0) break;
+      const bool paired = s.rows > TILE;
+      const int nt = s.tile1 - s.tile0, r = paired ? st * TILE + r_in : r_in;
+      const int steps = paired ? nt : (nt - st + 1) / 2;
+      const bool live = r < s.rows, warp_live = r - lane < s.rows;
+      ok = __all_sync(FULL, mbar_wait_spin(&c->rows_full[n % ring], n / ring & 1, abort_flag));
+      if (!ok) break;
+      const int limit = live ? c->limit[n % ring][r] : 0;
+      float ref = NINF, sum = 0.f;
+      bool seen = false, mixed = false;
+      for (int k = 0; k < steps; ++k) {
+        const int cnt = tiles + (paired ? k : 2 * k + st);
+        ok = __all_sync(FULL, mbar_wait(&c->ids_full[cnt % IDS], cnt / IDS & 1, abort_flag) && mbar_wait(&c->s_full[st], s_cnt & 1, abort_flag));
+        if (!ok) break;
+        ++s_cnt;
+        tc_fence_after();
+        if (warp_live) {
+          uint32_t x[4][32];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tmem_ld32(s_tm + i * 32, x[i]);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tie(x[i]);
+          const int top_id = c->max_id[cnt % IDS];
+          if (__any_sync(FULL, live && top_id >= limit)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int j = 0; j < 32; j += 4) {
+                const int4 id = *reinterpret_cast<const int4*>(&c->ids[cnt % IDS][i * 32 + j]);
+                const int e[4] = {id.x, id.y, id.z, id.w};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                  const bool sees = e[w] < limit;
+                  seen = seen || sees;
+                  mixed = mixed || (!sees && e[w] != NO_TOKEN);
+                  if (!sees) x[i][j + w] = 0xFF800000u;
+                }
+              }
+          } else {
+            seen = true;
+          }
+          float top = NINF;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) top = fmaxf(top, __uint_as_float(x[i][j]));
+          const float m = live && top != NINF ? top * scale : NINF;
+          if (__any_sync(FULL, m > ref + GROWTH)) {    // (ref = -inf: the first finite maximum)
+            const float now = m > ref + GROWTH ? m : ref;
+            const float f = now == ref ? 1.f : ex2(ref - now);
+            ref = now;
+            sum *= f;
+            if (k > 0) {
+#pragma unroll 1
+              for (int i = 0; i < D / 32; ++i) {
+                uint32_t o[32];
+                tmem_ld32(o_tm + i * 32, o);
+                tmem_ld_wait();
+                tie(o);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                tmem_st_32x32(o_tm + i * 32, o);
+              }
+            }
+          }
+          const float sub = ref == NINF ? 0.f : ref;
+          float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            uint32_t p[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const float e0 = ex2(fmaf(__uint_as_float(x[i + j / 16][2 * (j % 16)]), scale, -sub));
+              const float e1 = ex2(fmaf(__uint_as_float(x[i + j / 16][2 * (j % 16) + 1]), scale, -sub));
+              a0 += e0; a1 += e1;
+              p[j] = pack(e0, e1);
+            }
+            tmem_st_32x32(s_tm + i * 16, p);
+          }
+          sum += a0 + a1;
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        mbar_arrive(&c->p_full[st]);
+      }
+      if (!ok) break;
+      tiles += nt;
+      if (steps > 0) {
+        ok = __all_sync(FULL, mbar_wait(&c->o_full[st], o_cnt & 1, abort_flag));
+        if (!ok) break;
+        ++o_cnt;
+        tc_fence_after();
+      }
+      const bool direct = P.direct && paired;
+      if (warp_live) {
+        if (seen && ref == NINF) ref = LOWEST;
+        const long long at = (paired ? 0 : st * P.part_rows) + s.part + r;
+        const float inv = sum == 0.f ? (ref == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / sum;
+        const RowAt a{s.t_base + (s.row0 + r) / P.group, s.h0 + (s.row0 + r) % P.group, 0};
+        __nv_bfloat16* const out = (__nv_bfloat16*)P.out + out_at(P, s, a);
+        if (live && !direct) P.part_ml[at] = make_float2(ref, sum);
+        bool odd = false;
+        if (direct || steps > 0) {
+#pragma unroll 1
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32];
+            if (steps > 0) {
+              tmem_ld32(o_tm + i * 32, o);
+              tmem_ld_wait();
+              tie(o);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = 0;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) odd = odd || !isfinite(__uint_as_float(o[j]));
+            if (live) {
+              if (direct) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) {
+                  uint4 y;
+                  y.x = pack(__uint_as_float(o[j]) * inv, __uint_as_float(o[j + 1]) * inv);
+                  y.y = pack(__uint_as_float(o[j + 2]) * inv, __uint_as_float(o[j + 3]) * inv);
+                  y.z = pack(__uint_as_float(o[j + 4]) * inv, __uint_as_float(o[j + 5]) * inv);
+                  y.w = pack(__uint_as_float(o[j + 6]) * inv, __uint_as_float(o[j + 7]) * inv);
+                  *reinterpret_cast<uint4*>(out + i * 32 + j) = y;
+                }
+              } else {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4)
+                  *reinterpret_cast<uint4*>(P.part_o + at * D + i * 32 + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+              }
+            }
+          }
+        }
+        unsigned again = __ballot_sync(FULL, live && odd && mixed);
+        while (again) {
+          const int who = __ffs(again) - 1;
+          again &= again - 1;
+          float m, l, y[RR_PAGED_MAX_DH / 32];
+          repair_row<__nv_bfloat16>(P, s, r - lane + who, paired ? 0 : st, paired ? 1 : 2, m, l, y);
+          const long long atw = __shfl_sync(FULL, at, who);
+          __nv_bfloat16* const outw = (__nv_bfloat16*)__shfl_sync(FULL, (unsigned long long)out, who);
+          if (!direct && lane == 0) P.part_ml[atw] = make_float2(m, l);
+          const float iw = l == 0.f ? (m == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / l;
+#pragma unroll
+          for (int e = 0; e < D / 32; ++e) {
+            if (direct) outw[lane + 32 * e] = __float2bfloat16_rn(y[e] * iw);
+            else P.part_o[atw * D + lane + 32 * e] = y[e];
+          }
+        }
+      }
+      tc_fence_before();
+      seg_done(n);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+    if (lane == 0 && c->abort_flag && P.status) atomicOr(P.status, RR_STATUS_TIMEOUT);
+  }
+}
+
+long long map_rows(const Params& p) {
+  return ((p.num_pages - 1) * p.page_stride + (p.kv_heads - 1) * p.head_stride + (p.page_tokens - 1) * p.token_stride) / p.dh + 1;
+}
+
+template <int D>
+cudaError_t launch(const Params& p, int grid, cudaStream_t st) {
+  CUtensorMap mk, mv;
+  const long long rows = map_rows(p);
+  cudaError_t e = rr_encode_tmap_bf16_rows(&mk, p.k, D, rows);
+  if (e == cudaSuccess) e = rr_encode_tmap_bf16_rows(&mv, p.v, D, rows);
+  if (e != cudaSuccess) return e;
+  const int ring = p.slots > 256 ? 2 : MAX_RING;
+  static unsigned long long done = 0;
+  e = rr_once_per_device(done, [] {
+    const int a = Smem::total<D>(256, MAX_RING), b = Smem::total<D>(RR_MAX_RANGE_SLOTS, 2);
+    return cudaFuncSetAttribute(attend_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, a > b ? a : b);
+  });
+  if (e != cudaSuccess) return e;
+  const RowStrides rs{(int)(p.page_stride / D), (int)(p.head_stride / D), (int)(p.token_stride / D), (int)rows};
+  return rr_launch_pdl(attend_tc_kernel<D>, grid, NT, (size_t)Smem::total<D>(p.slots, ring), st, p, mk, mv, rs, ring, std::fabs(p.scale_log2), p.scale_log2 < 0.f ? 1 : 0);
+}
+
+}  // namespace
+
+bool rr_attend_tc_supported(const Params& p, int dtype) {
+  if (dtype != RR_BF16 || (p.dh != 64 && p.dh != 128) || !(std::fabs(p.scale_log2) > 1e-30f)) return false;
+  if ((p.page_stride | p.head_stride | p.token_stride) % p.dh != 0 || p.page_stride / p.dh > 0x7FFFFFFF || map_rows(p) > 0x7FFFFFF0LL) return false;
+  if (((uintptr_t)p.k | (uintptr_t)p.v | (uintptr_t)p.q | (uintptr_t)p.out) & 15) return false;
+  return (p.qb | p.qh | p.qt | p.ob | p.oh | p.ot) % 8 == 0;
+}
+
+cudaError_t rr_launch_attend_tc(const Params& p, int grid, cudaStream_t st) { return p.dh == 64 ? launch<64>(p, grid, st) : launch<128>(p, grid, st); }
