@@ -11,10 +11,10 @@
 // The tensor pipe takes 2 x 520 cycles for a 128 x 128 x 128 tile's two products, the 16384 exponentials take 1024: many rows are
 // bound by both about equally, few rows by the cache's traffic.
 //
-// Warps 0-3, 4-7: the streams, a thread per row.  8: copies (tile::gather4, four token rows of 64 entries each, through
-// whatever pages they lie in; a place without a token is a row behind the map's end and arrives as zeros).  9: issues the products.
-// 10: finds the segments.  11: brings query rows and their limits.  Segments go round in a ring of
-// P.ring, so that the next one's look-ups and queries are there before it begins.
+// Warps 0-3, 4-7: the streams, a thread per row.  8: issues the products.  9: finds the segments.  10: brings query rows and their
+// limits.  12-15: copies, 32 token rows each, 16 bytes per thread through whatever pages they lie in; a place without a token
+// is filled with zeros.  Segments go round in a ring, so that the next one's look-ups and queries are there before it begins.
+// (TMA's tile::gather4, four token rows per copy, took about 100 cycles of issue per copy: 8 us per tile.)
 // Step k of a segment is (stream k % 2, tile k / 2 if paired, else k):  S(k) is issued behind the product with P(k - 2) of the
 // same stream, which reads the same columns; the tensor pipe keeps that order.
 //
@@ -34,7 +34,7 @@ using namespace sm100;
 namespace {
 
 constexpr unsigned FULL = 0xFFFFFFFFu;
-constexpr int NT = 384, IDS = 8, MAX_RING = 4;
+constexpr int NT = 512, IDS = 8, MAX_RING = 4;
 constexpr float GROWTH = 8.f;
 
 template <int D> struct Shape {
@@ -49,7 +49,7 @@ struct Ctl {
   Seg seg[MAX_RING];
   int limit[MAX_RING][ROWS];
   int ids[IDS][TILE];
-  int max_id[IDS];
+  int max_id[IDS][4];
 };
 
 struct Smem {
@@ -58,11 +58,14 @@ struct Smem {
   template <int D> static int total(int n_slots, int ring) { return 1024 + slots<D>() + (n_slots > 0 ? ring * (2 * n_slots + 1) * 4 : 0); }
 };
 
-__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, int col, const int (&r)[4], uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(col), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(smem_u32(bar)) : "memory");
+// 16 bytes from global to shared memory, zeros if n == 0.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 // The values as second operand: its rows are the product's summed dimension (tokens), 128 bytes apart, the 64 columns of a half contiguous
 // (MN-major, 128-byte swizzle): groups of 8 rows 1024 bytes apart, halves HALF_BYTES apart.
 __device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t addr, uint32_t half_bytes) {
@@ -94,12 +97,11 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
 }
 
 // (a negative scale is taken as its magnitude with the queries negated, so that the largest product has the largest logit)
-struct RowStrides { int page, head, token, rows; };    // in rows of dh entries; rows: the map's
+struct RowStrides { int page, head, token; };          // in rows of dh entries
 
 template <int D>
 __global__ void __launch_bounds__(NT, 1)
-attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                 const RowStrides rs, const int ring, const float scale, const int negate) {
+attend_tc_kernel(const __grid_constant__ Params P, const RowStrides rs, const int ring, const float scale, const int negate) {
   using S = Shape<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -111,238 +113,31 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ CUten
   const int warp = __shfl_sync(FULL, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < S::STAGES; ++i) { mbar_init(&c->full[i], 1); mbar_init(&c->empty[i], 1); }
+    for (int i = 0; i < S::STAGES; ++i) { mbar_init(&c->full[i], 4); mbar_init(&c->empty[i], 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&c->s_full[i], 1); mbar_init(&c->p_full[i], 128); mbar_init(&c->o_full[i], 1);
       mbar_init(&c->q_full[i], 1); mbar_init(&c->q_empty[i], 1);
     }
-    for (int i = 0; i < IDS; ++i) mbar_init(&c->ids_full[i], 1);
-    for (int i = 0; i < MAX_RING; ++i) { mbar_init(&c->seg_full[i], 1); mbar_init(&c->seg_empty[i], 11); mbar_init(&c->rows_full[i], 1); }
+    for (int i = 0; i < IDS; ++i) mbar_init(&c->ids_full[i], 4);
+    for (int i = 0; i < MAX_RING; ++i) { mbar_init(&c->seg_full[i], 1); mbar_init(&c->seg_empty[i], 14); mbar_init(&c->rows_full[i], 1); }
     mbar_init(&c->drain, 1);
     c->abort_flag = 0;
     mbar_fence_init();
-    tma_prefetch_desc(&map_k);
-    tma_prefetch_desc(&map_v);
   }
-  if (warp == 9) tmem_alloc(&c->tmem_base, 512);
+  if (warp == 8) tmem_alloc(&c->tmem_base, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(FULL, c->tmem_base, 0);
   rr_pdl_wait();
   rr_pdl_trigger();
-
   // The segment ring as its readers see it: n counts segments.
   auto seg_wait = [&](int n) -> bool { return __all_sync(FULL, mbar_wait_spin(&c->seg_full[n % ring], n / ring & 1, abort_flag)); };
   auto seg_done = [&](int n) { __syncwarp(); if (lane == 0) mbar_arrive(&c->seg_empty[n % ring]); };
 
-  if (warp == 10) {
-    // ===== the segments =====
-    long long u, u0 = 0, u1;
-    if (P.slots) { u = blockIdx.x; u1 = P.range_rows * ((P.m * P.group + ROWS - 1) / ROWS) * P.splits; }
-    else { const long long W = __ldg(P.cum + P.batch); u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
-    for (int n = 0;; ++n) {
-      Seg s;
-      const bool end = u >= u1;
-      if (end) { s.rows = 0; }
-      else if (P.slots) { range_segment(P, u, s); u += gridDim.x; }
-      else u += segment_at(P, blockIdx.x, u, u0, u1, s);
-      if (!__all_sync(FULL, mbar_wait_spin(&c->seg_empty[n % ring], (n / ring & 1) ^ 1, abort_flag))) break;
-      if (!end && P.slots) {                           // number the row's tokens
-        int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
-        int* const base = first + P.slots + 1;
-        int run = 0;
-        for (int j0 = 0; j0 < P.slots; j0 += 32) {
-          const int j = j0 + lane;
-          int lo = 0, hi = 0;
-          if (j < P.slots) slot_span(s, j, lo, hi);
-          int incl = hi - lo;
-#pragma unroll
-          for (int off = 1; off < 32; off <<= 1) { const int x = __shfl_up_sync(FULL, incl, off); if (lane >= off) incl += x; }
-          if (j < P.slots) { first[j] = run + incl - (hi - lo); base[j] = lo - first[j]; }
-          run += __shfl_sync(FULL, incl, 31);
-        }
-        if (lane == 0) first[P.slots] = run;
-        split_tiles(P, (run + TILE - 1) / TILE, s);
-      }
-      if (lane == 0) c->seg[n % ring] = s;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&c->seg_full[n % ring]);
-      if (end) break;
-    }
-  } else if (warp == 11) {
-    // ===== query rows: into Q places 0 and 1 in turn, two for a paired segment =====
-    int place = 0;
-    for (int n = 0; seg_wait(n); ++n) {
-      const Seg s = c->seg[n % ring];
-      if (s.rows == 0) break;
-      for (int r = lane; r < s.rows; r += 32) c->limit[n % ring][r] = row_at(P, s, r).limit;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&c->rows_full[n % ring]);
-      bool ok = true;
-      for (int h = 0; h < (s.rows > TILE ? 2 : 1) && s.tile1 > s.tile0; ++h, ++place) {
-        const int at = place & 1;
-        ok = __all_sync(FULL, mbar_wait(&c->q_empty[at], (place >> 1 & 1) ^ 1, abort_flag));
-        if (!ok) break;
-        constexpr int CPR = D / 8;
-        const int rows = min(s.rows - h * TILE, TILE);
-        const uint32_t flip = negate ? 0x80008000u : 0u;
-        for (int c0 = lane; c0 < rows * CPR; c0 += 32 * 8) {
-          uint4 v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int ch = c0 + 32 * i;
-            if (ch >= rows * CPR) continue;
-            const int idx = s.row0 + h * TILE + ch / CPR, dt = idx / P.group;
-            const RowAt a{s.t_base + dt, s.h0 + idx - dt * P.group, 0};
-            v[i] = __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)P.q + q_at(P, s, a) + ch % CPR * 8));
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int ch = c0 + 32 * i;
-            if (ch >= rows * CPR) continue;
-            const int r = ch / CPR, c16 = ch % CPR;
-            v[i].x ^= flip; v[i].y ^= flip; v[i].z ^= flip; v[i].w ^= flip;
-            *reinterpret_cast<uint4*>(sQ + at * S::TILE_BYTES + (c16 >> 3) * S::HALF_BYTES + r * 128 + (((c16 & 7) ^ (r & 7)) << 4)) = v[i];
-          }
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&c->q_full[at]);
-      }
-      if (!ok) break;
-      seg_done(n);
-    }
-  } else if (warp == 8) {
-    // ===== copies: fills 2 i (keys) and 2 i + 1 (values) of the CTA's i-th tile =====
-    int tiles = 0;                                     // of all segments so far
-    uint32_t fills = 0;
-    bool ok = true;
-    for (int n = 0; ok && seg_wait(n); ++n) {
-      const Seg s = c->seg[n % ring];
-      if (s.rows == 0) break;
-      const int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
-      const int* const base = first + P.slots + 1;
-      const int n_tok = P.slots ? first[P.slots] : s.tok1 - s.tok0;
-      int row[4], next[4];
-      auto find = [&](int tile, int cnt, int (&row)[4]) {   // this lane's four tokens of a tile: ids for the streams, rows of the map
-        int id[4], top = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int num = tile * TILE + lane * 4 + j;
-          id[j] = NO_TOKEN;
-          row[j] = rs.rows;
-          if (num < n_tok) {
-            int tok;
-            if (P.slots) {
-              int lo = 0, hi = P.slots;
-              while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (first[mid] <= num) lo = mid; else hi = mid; }
-              tok = base[lo] + num;
-            } else {
-              tok = s.tok0 + num;
-            }
-            const int col = tok / P.page_tokens, page = __ldg(s.pages + col);
-            if (page >= 0 && page < P.num_pages) {
-              id[j] = tok;
-              row[j] = page * rs.page + s.kvh * rs.head + (tok - col * P.page_tokens) * rs.token;
-            } else if (P.status) {
-              atomicOr(P.status, RR_STATUS_BAD_INDEX);
-            }
-          }
-          top = max(top, id[j]);
-        }
-        top = __reduce_max_sync(FULL, top);
-        *reinterpret_cast<int4*>(&c->ids[cnt % IDS][lane * 4]) = make_int4(id[0], id[1], id[2], id[3]);
-        if (lane == 0) c->max_id[cnt % IDS] = top;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&c->ids_full[cnt % IDS]);
-      };
-      auto load = [&](const CUtensorMap* map, const int (&row)[4]) -> bool {
-        const int st = fills % S::STAGES;
-        if (!__all_sync(FULL, mbar_wait_spin(&c->empty[st], (fills / S::STAGES & 1) ^ 1, abort_flag))) return false;
-        if (lane == 0) mbar_expect_tx(&c->full[st], S::TILE_BYTES);
-        __syncwarp();
-#pragma unroll
-        for (int h = 0; h < S::HALVES; ++h)
-          gather4(kv_addr + st * S::TILE_BYTES + h * S::HALF_BYTES + lane * 512, map, h * 64, row, &c->full[st]);
-        ++fills;
-        return true;
-      };
-      if (s.tile0 < s.tile1) find(s.tile0, tiles, next);
-      for (int t = s.tile0; t < s.tile1; ++t) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) row[j] = next[j];
-        ok = load(&map_k, row);
-        if (!ok) break;
-        if (t + 1 < s.tile1) find(t + 1, tiles + 1, next);
-        ok = load(&map_v, row);
-        if (!ok) break;
-        ++tiles;
-      }
-      if (ok) seg_done(n);
-    }
-    // do not leave while copies into this CTA's shared memory may be in flight
-    for (uint32_t f = fills > S::STAGES ? fills - S::STAGES : 0; f < fills; ++f)
-      for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->full[f % S::STAGES], f / S::STAGES & 1); ++it) __nanosleep(64);
-    __syncwarp();
-  } else if (warp == 9) {
-    // ===== products =====
-    constexpr uint32_t idesc_s = umma_idesc_bf16(TILE, TILE), idesc_o = idesc_b_mn(TILE, D);
-    int place = 0;
-    uint32_t tiles = 0, p_cnt[2] = {0, 0};
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL, mbar_wait_spin(bar, parity & 1, abort_flag)); };
-    for (int n = 0; ok && seg_wait(n); ++n) {
-      const int rows = __shfl_sync(FULL, c->seg[n % ring].rows, 0);
-      const int nt = __shfl_sync(FULL, c->seg[n % ring].tile1 - c->seg[n % ring].tile0, 0);
-      if (rows == 0) break;
-      const bool paired = rows > TILE;
-      const int steps = paired ? 2 * nt : nt;
-      if (steps == 0) { seg_done(n); continue; }
-      ok = wait(&c->q_full[place & 1], place >> 1);
-      if (ok && paired) ok = wait(&c->q_full[(place + 1) & 1], (place + 1) >> 1);
-      for (int k = 0; ok && k < steps + 2; ++k) {
-        if (k >= 2) {
-          const int kk = k - 2, st = kk & 1;
-          const uint32_t f = 2 * (tiles + (paired ? kk >> 1 : kk)) + 1, stage = f % S::STAGES;
-          ok = wait(&c->p_full[st], p_cnt[st]) && wait(&c->full[stage], f / S::STAGES);
-          if (!ok) break;
-          ++p_cnt[st];
-          tc_fence_after();
-          const uint64_t vd = desc_mn_sw128(kv_addr + stage * S::TILE_BYTES, S::HALF_BYTES);
-#pragma unroll
-          for (int j = 0; j < TILE / 16; ++j)
-            umma_bf16_ts_warp(tmem + 256 + st * 128, tmem + st * 128 + j * 8, vd + (uint64_t)(j * 128), idesc_o, (kk >= 2 || j > 0) ? 1u : 0u);
-          if (!paired || st == 1) umma_commit_warp(&c->empty[stage]);
-          if (kk + 2 >= steps) umma_commit_warp(&c->o_full[st]);
-        }
-        if (k < steps) {
-          const int st = k & 1;
-          const uint32_t f = 2 * (tiles + (paired ? k >> 1 : k)), stage = f % S::STAGES;
-          const int at = (place + (paired ? st : 0)) & 1;
-          ok = wait(&c->full[stage], f / S::STAGES);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t qd = umma_desc_k_sw128(q_addr + at * S::TILE_BYTES), kd = umma_desc_k_sw128(kv_addr + stage * S::TILE_BYTES);
-#pragma unroll
-          for (int j = 0; j < D / 16; ++j) {
-            const uint64_t o = (uint64_t)((j >> 2) * (S::HALF_BYTES >> 4) + (j & 3) * 2);
-            umma_bf16_warp(tmem + st * 128, qd + o, kd + o, idesc_s, j > 0 ? 1u : 0u);
-          }
-          umma_commit_warp(&c->s_full[st]);
-          if (!paired || st == 1) umma_commit_warp(&c->empty[stage]);
-          if (paired ? k + 2 >= steps : k + 1 == steps) umma_commit_warp(&c->q_empty[at]);
-        }
-      }
-      if (!ok) break;
-      tiles += nt;
-      place += paired ? 2 : 1;
-      seg_done(n);
-    }
-    umma_commit_warp(&c->drain);
-    for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->drain, 0); ++it) __nanosleep(64);
-    __syncwarp();
-  } else {
+  // of the launch's 512 x 128 registers: 256 threads x 184 for the streams, 256 x 72 for the others
+  if (warp < 8) {
+    regs_up<184>();
     // ===== a stream: thread = row =====
     const int st = warp >> 2, quarter = warp & 3;
     const int r_in = quarter * 32 + lane;
@@ -352,7 +147,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ CUten
     int tiles = 0;
     bool ok = true;
     for (int n = 0; ok && seg_wait(n); ++n) {
-      const Seg s = c->seg[n % ring];
+      const Seg& s = c->seg[n % ring];
       if (s.rows == 0) break;
       const bool paired = s.rows > TILE;
       const int nt = s.tile1 - s.tile0, r = paired ? st * TILE + r_in : r_in;
@@ -376,7 +171,8 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ CUten
           tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < 4; ++i) tie(x[i]);
-          const int top_id = c->max_id[cnt % IDS];
+          const int4 tops = *reinterpret_cast<const int4*>(c->max_id[cnt % IDS]);
+          const int top_id = max(max(tops.x, tops.y), max(tops.z, tops.w));
           if (__any_sync(FULL, live && top_id >= limit)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -509,43 +305,258 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ CUten
       tc_fence_before();
       seg_done(n);
     }
+  } else {
+    regs_down<72>();
+    if (warp == 9) {
+      // ===== the segments =====
+      long long u, u0 = 0, u1;
+      if (P.slots) { u = blockIdx.x; u1 = P.range_rows * ((P.m * P.group + ROWS - 1) / ROWS) * P.splits; }
+      else { const long long W = __ldg(P.cum + P.batch); u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
+      for (int n = 0;; ++n) {
+        Seg s;
+        const bool end = u >= u1;
+        if (end) { s.rows = 0; }
+        else if (P.slots) { range_segment(P, u, s); u += gridDim.x; }
+        else u += segment_at(P, blockIdx.x, u, u0, u1, s);
+        if (!__all_sync(FULL, mbar_wait_spin(&c->seg_empty[n % ring], (n / ring & 1) ^ 1, abort_flag))) break;
+        if (!end && P.slots) {                           // number the row's tokens
+          int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
+          int* const base = first + P.slots + 1;
+          int run = 0;
+          for (int j0 = 0; j0 < P.slots; j0 += 32) {
+            const int j = j0 + lane;
+            int lo = 0, hi = 0;
+            if (j < P.slots) slot_span(s, j, lo, hi);
+            int incl = hi - lo;
+  #pragma unroll
+            for (int off = 1; off < 32; off <<= 1) { const int x = __shfl_up_sync(FULL, incl, off); if (lane >= off) incl += x; }
+            if (j < P.slots) { first[j] = run + incl - (hi - lo); base[j] = lo - first[j]; }
+            run += __shfl_sync(FULL, incl, 31);
+          }
+          if (lane == 0) first[P.slots] = run;
+          split_tiles(P, (run + TILE - 1) / TILE, s);
+        }
+        if (lane == 0) c->seg[n % ring] = s;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c->seg_full[n % ring]);
+        if (end) break;
+      }
+    } else if (warp == 10) {
+      // ===== query rows: into Q places 0 and 1 in turn, two for a paired segment =====
+      int place = 0;
+      for (int n = 0; seg_wait(n); ++n) {
+        const Seg& s = c->seg[n % ring];
+        if (s.rows == 0) break;
+        for (int r = lane; r < s.rows; r += 32) c->limit[n % ring][r] = row_at(P, s, r).limit;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c->rows_full[n % ring]);
+        bool ok = true;
+        for (int h = 0; h < (s.rows > TILE ? 2 : 1) && s.tile1 > s.tile0; ++h, ++place) {
+          const int at = place & 1;
+          ok = __all_sync(FULL, mbar_wait(&c->q_empty[at], (place >> 1 & 1) ^ 1, abort_flag));
+          if (!ok) break;
+          constexpr int CPR = D / 8;
+          const int rows = min(s.rows - h * TILE, TILE);
+          const uint32_t flip = negate ? 0x80008000u : 0u;
+          for (int c0 = lane; c0 < rows * CPR; c0 += 32 * 4) {
+            uint4 v[4];
+  #pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int ch = c0 + 32 * i;
+              if (ch >= rows * CPR) continue;
+              const int idx = s.row0 + h * TILE + ch / CPR, dt = idx / P.group;
+              const RowAt a{s.t_base + dt, s.h0 + idx - dt * P.group, 0};
+              v[i] = __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)P.q + q_at(P, s, a) + ch % CPR * 8));
+            }
+  #pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int ch = c0 + 32 * i;
+              if (ch >= rows * CPR) continue;
+              const int r = ch / CPR, c16 = ch % CPR;
+              v[i].x ^= flip; v[i].y ^= flip; v[i].z ^= flip; v[i].w ^= flip;
+              *reinterpret_cast<uint4*>(sQ + at * S::TILE_BYTES + (c16 >> 3) * S::HALF_BYTES + r * 128 + (((c16 & 7) ^ (r & 7)) << 4)) = v[i];
+            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&c->q_full[at]);
+        }
+        if (!ok) break;
+        seg_done(n);
+      }
+    } else if (warp >= 12) {
+      // ===== copies: fills 2 i (keys) and 2 i + 1 (values) of the CTA's i-th tile; warp w has rows 32 w .. 32 w + 31 =====
+      const int w = warp - 12;
+      const uint32_t dst0 = kv_addr + (w * 32 + (lane >> 3)) * 128;      // row lane / 8 of this warp's, 16-byte piece lane % 8
+      int tiles = 0;                                     // of all segments so far
+      uint32_t fills = 0, landed = 0;
+      bool ok = true;
+      auto settle = [&](uint32_t upto) {                 // this warp's part of every fill before `upto` is in shared memory
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) for (uint32_t f = landed; f < upto; ++f) mbar_arrive(&c->full[f % S::STAGES]);
+        landed = upto;
+      };
+      for (int n = 0; ok && seg_wait(n); ++n) {
+        const Seg& s = c->seg[n % ring];
+        if (s.rows == 0) break;
+        const int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
+        const int* const base = first + P.slots + 1;
+        const int n_tok = P.slots ? first[P.slots] : s.tok1 - s.tok0;
+        auto find = [&](int tile, int cnt) -> int {      // this lane's token of a tile: its id for the streams, its row in the cache
+          const int num = tile * TILE + w * 32 + lane;
+          int id = NO_TOKEN, row = -1;
+          if (num < n_tok) {
+            int tok;
+            if (P.slots) {
+              int lo = 0, hi = P.slots;
+              while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (first[mid] <= num) lo = mid; else hi = mid; }
+              tok = base[lo] + num;
+            } else {
+              tok = s.tok0 + num;
+            }
+            const int col = tok / P.page_tokens, page = __ldg(s.pages + col);
+            if (page >= 0 && page < P.num_pages) {
+              id = tok;
+              row = page * rs.page + s.kvh * rs.head + (tok - col * P.page_tokens) * rs.token;
+            } else if (P.status) {
+              atomicOr(P.status, RR_STATUS_BAD_INDEX);
+            }
+          }
+          const int top = __reduce_max_sync(FULL, id);
+          c->ids[cnt % IDS][w * 32 + lane] = id;
+          if (lane == 0) c->max_id[cnt % IDS][w] = top;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&c->ids_full[cnt % IDS]);
+          return row;
+        };
+        auto load = [&](const void* cache, int row) -> bool {
+          const uint32_t st = fills % S::STAGES, parity = (fills / S::STAGES & 1) ^ 1;
+          if (!__all_sync(FULL, mbar_try_wait(&c->empty[st], parity))) {
+            cp_async_wait<0>();                          // nothing that has arrived waits for the next fill
+            settle(fills);
+            if (!__all_sync(FULL, mbar_wait_spin(&c->empty[st], parity, abort_flag))) return false;
+          }
+          const uint8_t* const src0 = (const uint8_t*)cache + (lane & 7) * 16;
+          const uint32_t dst = dst0 + st * S::TILE_BYTES;
+  #pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = __shfl_sync(FULL, row, i * 4 + (lane >> 3));
+            const uint8_t* const src = src0 + (size_t)max(r, 0) * (D * 2);
+            const uint32_t at = dst + i * 512 + (((lane & 7) ^ ((i * 4 + (lane >> 3)) & 7)) << 4);
+  #pragma unroll
+            for (int h = 0; h < S::HALVES; ++h) cp_async16(at + h * S::HALF_BYTES, src + h * 128, r >= 0 ? 16u : 0u);
+          }
+          cp_async_commit();
+          ++fills;
+          cp_async_wait<2>();
+          if (fills >= 2 + landed) settle(fills - 2);
+          return true;
+        };
+        int next = s.tile0 < s.tile1 ? find(s.tile0, tiles) : -1;
+        for (int t = s.tile0; t < s.tile1; ++t) {
+          const int row = next;
+          ok = load(P.k, row);
+          if (!ok) break;
+          if (t + 1 < s.tile1) next = find(t + 1, tiles + 1);
+          ok = load(P.v, row);
+          if (!ok) break;
+          ++tiles;
+        }
+        if (ok) seg_done(n);
+      }
+      cp_async_wait<0>();                                // (do not leave with copies in flight)
+      settle(fills);
+    } else if (warp == 8) {
+      // ===== products =====
+      constexpr uint32_t idesc_s = umma_idesc_bf16(TILE, TILE), idesc_o = idesc_b_mn(TILE, D);
+      int place = 0;
+      uint32_t tiles = 0, p_cnt[2] = {0, 0};
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL, mbar_wait_spin(bar, parity & 1, abort_flag)); };
+      for (int n = 0; ok && seg_wait(n); ++n) {
+        const int rows = __shfl_sync(FULL, c->seg[n % ring].rows, 0);
+        const int nt = __shfl_sync(FULL, c->seg[n % ring].tile1 - c->seg[n % ring].tile0, 0);
+        if (rows == 0) break;
+        const bool paired = rows > TILE;
+        const int steps = paired ? 2 * nt : nt;
+        if (steps == 0) { seg_done(n); continue; }
+        ok = wait(&c->q_full[place & 1], place >> 1);
+        if (ok && paired) ok = wait(&c->q_full[(place + 1) & 1], (place + 1) >> 1);
+        for (int k = 0; ok && k < steps + 2; ++k) {
+          if (k >= 2) {
+            const int kk = k - 2, st = kk & 1;
+            const uint32_t f = 2 * (tiles + (paired ? kk >> 1 : kk)) + 1, stage = f % S::STAGES;
+            ok = wait(&c->p_full[st], p_cnt[st]) && wait(&c->full[stage], f / S::STAGES);
+            if (!ok) break;
+            ++p_cnt[st];
+            tc_fence_after();
+            const uint64_t vd = desc_mn_sw128(kv_addr + stage * S::TILE_BYTES, S::HALF_BYTES);
+  #pragma unroll
+            for (int j = 0; j < TILE / 16; ++j)
+              umma_bf16_ts_warp(tmem + 256 + st * 128, tmem + st * 128 + j * 8, vd + (uint64_t)(j * 128), idesc_o, (kk >= 2 || j > 0) ? 1u : 0u);
+            if (!paired || st == 1) umma_commit_warp(&c->empty[stage]);
+            if (kk + 2 >= steps) umma_commit_warp(&c->o_full[st]);
+          }
+          if (k < steps) {
+            const int st = k & 1;
+            const uint32_t f = 2 * (tiles + (paired ? k >> 1 : k)), stage = f % S::STAGES;
+            const int at = (place + (paired ? st : 0)) & 1;
+            ok = wait(&c->full[stage], f / S::STAGES);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t qd = umma_desc_k_sw128(q_addr + at * S::TILE_BYTES), kd = umma_desc_k_sw128(kv_addr + stage * S::TILE_BYTES);
+  #pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+              const uint64_t o = (uint64_t)((j >> 2) * (S::HALF_BYTES >> 4) + (j & 3) * 2);
+              umma_bf16_warp(tmem + st * 128, qd + o, kd + o, idesc_s, j > 0 ? 1u : 0u);
+            }
+            umma_commit_warp(&c->s_full[st]);
+            if (!paired || st == 1) umma_commit_warp(&c->empty[stage]);
+            if (paired ? k + 2 >= steps : k + 1 == steps) umma_commit_warp(&c->q_empty[at]);
+          }
+        }
+        if (!ok) break;
+        tiles += nt;
+        place += paired ? 2 : 1;
+        seg_done(n);
+      }
+      umma_commit_warp(&c->drain);
+      for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->drain, 0); ++it) __nanosleep(64);
+      __syncwarp();
+    }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 8) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
     if (lane == 0 && c->abort_flag && P.status) atomicOr(P.status, RR_STATUS_TIMEOUT);
   }
 }
 
-long long map_rows(const Params& p) {
+long long cache_rows(const Params& p) {
   return ((p.num_pages - 1) * p.page_stride + (p.kv_heads - 1) * p.head_stride + (p.page_tokens - 1) * p.token_stride) / p.dh + 1;
 }
 
 template <int D>
 cudaError_t launch(const Params& p, int grid, cudaStream_t st) {
-  CUtensorMap mk, mv;
-  const long long rows = map_rows(p);
-  cudaError_t e = rr_encode_tmap_bf16_rows(&mk, p.k, D, rows);
-  if (e == cudaSuccess) e = rr_encode_tmap_bf16_rows(&mv, p.v, D, rows);
-  if (e != cudaSuccess) return e;
   const int ring = p.slots > 256 ? 2 : MAX_RING;
   static unsigned long long done = 0;
-  e = rr_once_per_device(done, [] {
+  const cudaError_t e = rr_once_per_device(done, [] {
     const int a = Smem::total<D>(256, MAX_RING), b = Smem::total<D>(RR_MAX_RANGE_SLOTS, 2);
     return cudaFuncSetAttribute(attend_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, a > b ? a : b);
   });
   if (e != cudaSuccess) return e;
-  const RowStrides rs{(int)(p.page_stride / D), (int)(p.head_stride / D), (int)(p.token_stride / D), (int)rows};
-  return rr_launch_pdl(attend_tc_kernel<D>, grid, NT, (size_t)Smem::total<D>(p.slots, ring), st, p, mk, mv, rs, ring, std::fabs(p.scale_log2), p.scale_log2 < 0.f ? 1 : 0);
+  const RowStrides rs{(int)(p.page_stride / D), (int)(p.head_stride / D), (int)(p.token_stride / D)};
+  return rr_launch_pdl(attend_tc_kernel<D>, grid, NT, (size_t)Smem::total<D>(p.slots, ring), st, p, rs, ring, std::fabs(p.scale_log2), p.scale_log2 < 0.f ? 1 : 0);
 }
 
 }  // namespace
 
 bool rr_attend_tc_supported(const Params& p, int dtype) {
   if (dtype != RR_BF16 || (p.dh != 64 && p.dh != 128) || !(std::fabs(p.scale_log2) > 1e-30f)) return false;
-  if ((p.page_stride | p.head_stride | p.token_stride) % p.dh != 0 || p.page_stride / p.dh > 0x7FFFFFFF || map_rows(p) > 0x7FFFFFF0LL) return false;
+  if ((p.page_stride | p.head_stride | p.token_stride) % p.dh != 0 || p.page_stride / p.dh > 0x7FFFFFFF || cache_rows(p) > 0x7FFFFFF0LL) return false;
   if (((uintptr_t)p.k | (uintptr_t)p.v | (uintptr_t)p.q | (uintptr_t)p.out) & 15) return false;
   return (p.qb | p.qh | p.qt | p.ob | p.oh | p.ot) % 8 == 0;
 }

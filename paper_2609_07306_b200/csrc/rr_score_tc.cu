@@ -127,19 +127,6 @@ cudaError_t rr_encode_tmap_bf16_tile(CUtensorMap* out, const void* base, int d, 
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-cudaError_t rr_encode_tmap_bf16_rows(CUtensorMap* out, const void* base, int d, long long rows) {
-  EncodeTiledFn enc = get_encode();
-  if (!enc) return cudaErrorNotSupported;
-  cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {(cuuint64_t)d * 2};
-  cuuint32_t box[2] = {64, 1};
-  cuuint32_t estr[2] = {1, 1};
-  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
-                   box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
-
 cudaError_t rr_launch_score_tc(const RRParams& p, const void* qc, const void* kc,
                                const int32_t* row_list, cudaStream_t st) {
   CUtensorMap tmap;

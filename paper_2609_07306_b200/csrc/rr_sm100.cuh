@@ -387,5 +387,3 @@ cudaError_t rr_encode_tmap_bf16_3d(CUtensorMap* out, const void* base, int d, in
 // copy brings box_rows whole rows, K-half by K-half.
 cudaError_t rr_encode_tmap_bf16_tile(CUtensorMap* out, const void* base, int d, int rows, int planes,
                                      int box_rows);
-// [rows][d] as a 2-D map with a {64, 1} box: tile::gather4 loads of four rows each; rows from `rows` on read as zeros.
-cudaError_t rr_encode_tmap_bf16_rows(CUtensorMap* out, const void* base, int d, long long rows);
