@@ -247,6 +247,6 @@ __device__ __noinline__ void repair_row(const Params& P, const Seg& s, int r, in
 
 }  // namespace rrattn
 
-// One CTA per SM; dh 64 or 128, bf16, strides in whole rows of dh entries.
+// bf16, dh 64 or 128, a positive scale, rows on 16-byte boundaries.
 bool rr_attend_tc_supported(const rrattn::Params& p, int dtype);
 cudaError_t rr_launch_attend_tc(const rrattn::Params& p, int grid, cudaStream_t st);

@@ -11,9 +11,9 @@
 // The tensor pipe takes 2 x 520 cycles for a 128 x 128 x 128 tile's two products, the 16384 exponentials take 1024: many rows are
 // bound by both about equally, few rows by the cache's traffic.
 //
-// Warps 0-3, 4-7: the streams, a thread per row.  8: issues the products.  9: finds the segments.  10: brings query rows and their
-// limits.  12-15: copies, 32 token rows each, 16 bytes per thread through whatever pages they lie in; a place without a token
-// is filled with zeros.  Segments go round in a ring, so that the next one's look-ups and queries are there before it begins.
+// Warps 0-3, 4-7: the streams, a thread per row.  8: issues the products.  9: finds the segments.  10: the rows' limits.
+// 12-15: copies of token and query rows, 32 rows each, 16 bytes per thread, tokens through whatever pages they lie in; a place
+// without a token is filled with zeros.  Segments go round in a ring, so that the next one's look-ups and queries are there before it begins.
 // (TMA's tile::gather4, four token rows per copy, took about 100 cycles of issue per copy: 8 us per tile.)
 // Step k of a segment is (stream k % 2, tile k / 2 if paired, else k):  S(k) is issued behind the product with P(k - 2) of the
 // same stream, which reads the same columns; the tensor pipe keeps that order.
@@ -24,7 +24,6 @@
 //
 // Every wait is bounded; one that runs out sets RR_STATUS_TIMEOUT, and the CTA waits for its copies and
 // products in flight, frees its TMEM and returns.
-#include <cmath>
 #include "rr_attend_paged.cuh"
 #include "rr_sm100.cuh"
 
@@ -96,16 +95,12 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   uint32_t y; asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo)); return y;
 }
 
-// (a negative scale is taken as its magnitude with the queries negated, so that the largest product has the largest logit)
-struct RowStrides { int page, head, token; };          // in rows of dh entries
-
 template <int D>
 __global__ void __launch_bounds__(NT, 1)
-attend_tc_kernel(const __grid_constant__ Params P, const RowStrides rs, const int ring, const float scale, const int negate) {
+attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
   using S = Shape<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* const sQ = smem;
   const uint32_t q_addr = smem_u32(smem), kv_addr = q_addr + 2 * S::TILE_BYTES;
   Ctl* const c = (Ctl*)(smem + Smem::ctl<D>());
   int* const slot_table = (int*)(smem + Smem::slots<D>());
@@ -116,7 +111,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const RowStrides rs, const in
     for (int i = 0; i < S::STAGES; ++i) { mbar_init(&c->full[i], 4); mbar_init(&c->empty[i], 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&c->s_full[i], 1); mbar_init(&c->p_full[i], 128); mbar_init(&c->o_full[i], 1);
-      mbar_init(&c->q_full[i], 1); mbar_init(&c->q_empty[i], 1);
+      mbar_init(&c->q_full[i], 4); mbar_init(&c->q_empty[i], 1);
     }
     for (int i = 0; i < IDS; ++i) mbar_init(&c->ids_full[i], 4);
     for (int i = 0; i < MAX_RING; ++i) { mbar_init(&c->seg_full[i], 1); mbar_init(&c->seg_empty[i], 14); mbar_init(&c->rows_full[i], 1); }
@@ -196,7 +191,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const RowStrides rs, const in
           for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 32; ++j) top = fmaxf(top, __uint_as_float(x[i][j]));
-          const float m = live && top != NINF ? top * scale : NINF;
+          const float m = live && top != NINF ? top * P.scale_log2 : NINF;
           if (__any_sync(FULL, m > ref + GROWTH)) {    // (ref = -inf: the first finite maximum)
             const float now = m > ref + GROWTH ? m : ref;
             const float f = now == ref ? 1.f : ex2(ref - now);
@@ -222,8 +217,8 @@ attend_tc_kernel(const __grid_constant__ Params P, const RowStrides rs, const in
             uint32_t p[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-              const float e0 = ex2(fmaf(__uint_as_float(x[i + j / 16][2 * (j % 16)]), scale, -sub));
-              const float e1 = ex2(fmaf(__uint_as_float(x[i + j / 16][2 * (j % 16) + 1]), scale, -sub));
+              const float e0 = ex2(fmaf(__uint_as_float(x[i + j / 16][2 * (j % 16)]), P.scale_log2, -sub));
+              const float e1 = ex2(fmaf(__uint_as_float(x[i + j / 16][2 * (j % 16) + 1]), P.scale_log2, -sub));
               a0 += e0; a1 += e1;
               p[j] = pack(e0, e1);
             }
@@ -342,70 +337,79 @@ attend_tc_kernel(const __grid_constant__ Params P, const RowStrides rs, const in
         if (end) break;
       }
     } else if (warp == 10) {
-      // ===== query rows: into Q places 0 and 1 in turn, two for a paired segment =====
-      int place = 0;
+      // ===== the rows' limits =====
       for (int n = 0; seg_wait(n); ++n) {
         const Seg& s = c->seg[n % ring];
         if (s.rows == 0) break;
-        for (int r = lane; r < s.rows; r += 32) c->limit[n % ring][r] = row_at(P, s, r).limit;
+        if (s.b >= 0) {                                // one sequence: the limit goes up by one from token to token
+          const int len = s.slots ? s.tok1 : seq_len(P, s.b), past = len - s.n_seq + (s.t_base - s.t_seq0) + 1;
+          for (int r = lane; r < s.rows; r += 32) c->limit[n % ring][r] = P.causal ? max(past + (s.row0 + r) / P.group, 0) : len;
+        } else {
+          for (int r = lane; r < s.rows; r += 32) c->limit[n % ring][r] = row_at(P, s, r).limit;
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(&c->rows_full[n % ring]);
-        bool ok = true;
-        for (int h = 0; h < (s.rows > TILE ? 2 : 1) && s.tile1 > s.tile0; ++h, ++place) {
-          const int at = place & 1;
-          ok = __all_sync(FULL, mbar_wait(&c->q_empty[at], (place >> 1 & 1) ^ 1, abort_flag));
-          if (!ok) break;
-          constexpr int CPR = D / 8;
-          const int rows = min(s.rows - h * TILE, TILE);
-          const uint32_t flip = negate ? 0x80008000u : 0u;
-          for (int c0 = lane; c0 < rows * CPR; c0 += 32 * 4) {
-            uint4 v[4];
-  #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int ch = c0 + 32 * i;
-              if (ch >= rows * CPR) continue;
-              const int idx = s.row0 + h * TILE + ch / CPR, dt = idx / P.group;
-              const RowAt a{s.t_base + dt, s.h0 + idx - dt * P.group, 0};
-              v[i] = __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)P.q + q_at(P, s, a) + ch % CPR * 8));
-            }
-  #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int ch = c0 + 32 * i;
-              if (ch >= rows * CPR) continue;
-              const int r = ch / CPR, c16 = ch % CPR;
-              v[i].x ^= flip; v[i].y ^= flip; v[i].z ^= flip; v[i].w ^= flip;
-              *reinterpret_cast<uint4*>(sQ + at * S::TILE_BYTES + (c16 >> 3) * S::HALF_BYTES + r * 128 + (((c16 & 7) ^ (r & 7)) << 4)) = v[i];
-            }
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&c->q_full[at]);
-        }
-        if (!ok) break;
         seg_done(n);
       }
     } else if (warp >= 12) {
-      // ===== copies: fills 2 i (keys) and 2 i + 1 (values) of the CTA's i-th tile; warp w has rows 32 w .. 32 w + 31 =====
+      // ===== copies: fills 2 i (keys) and 2 i + 1 (values) of the CTA's i-th tile, and behind a segment's first keys its queries,
+      // into Q places 0 and 1 in turn (a paired segment takes two).  Warp w has rows 32 w .. 32 w + 31 =====
       const int w = warp - 12;
-      const uint32_t dst0 = kv_addr + (w * 32 + (lane >> 3)) * 128;      // row lane / 8 of this warp's, 16-byte piece lane % 8
-      int tiles = 0;                                     // of all segments so far
-      uint32_t fills = 0, landed = 0;
-      bool ok = true;
-      auto settle = [&](uint32_t upto) {                 // this warp's part of every fill before `upto` is in shared memory
+      const uint32_t dst0 = (w * 32 + (lane >> 3)) * 128;              // row lane / 8 of this warp's, 16-byte piece lane % 8
+      int tiles = 0, place = 0;                        // of all segments so far
+      uint32_t fills = 0;
+      // Up to two groups of copies are in flight unannounced: with a third one committed the oldest has landed (wait_group 2), the
+      // warp's part of it is made visible to the tensor pipe and its barrier told.
+      uint64_t *older = nullptr, *newer = nullptr;
+      auto tell = [&](uint64_t* bar) { if (lane == 0 && bar) mbar_arrive(bar); };
+      auto commit = [&](uint64_t* bar) {
+        cp_async_commit();
+        if (older) {
+          cp_async_wait<2>();
+          fence_proxy_async_smem();
+          __syncwarp();
+          tell(older);
+        }
+        older = newer;
+        newer = bar;
+      };
+      auto flush = [&]() {
+        cp_async_wait<0>();
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) for (uint32_t f = landed; f < upto; ++f) mbar_arrive(&c->full[f % S::STAGES]);
-        landed = upto;
+        tell(older);
+        tell(newer);
+        older = newer = nullptr;
       };
+      auto free_slot = [&](uint64_t* bar, uint32_t parity) -> bool {
+        if (__all_sync(FULL, mbar_try_wait(bar, parity))) return true;
+        flush();                                       // nothing that has arrived waits for the next fill
+        return __all_sync(FULL, mbar_wait_spin(bar, parity, abort_flag));
+      };
+      // 32 rows of D entries; `at`: the lane's row as an element offset, -1 for zeros
+      auto rows32 = [&](const void* from, long long at, uint32_t dst) {
+        const uint8_t* const src0 = (const uint8_t*)from + (lane & 7) * 16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = i * 4 + (lane >> 3);
+          const long long o = __shfl_sync(FULL, at, r);
+          const uint8_t* const src = src0 + max(o, 0LL) * 2;
+          const uint32_t to = dst + dst0 + i * 512 + (((lane & 7) ^ (r & 7)) << 4);
+#pragma unroll
+          for (int h = 0; h < S::HALVES; ++h) cp_async16(to + h * S::HALF_BYTES, src + h * 128, o >= 0 ? 16u : 0u);
+        }
+      };
+      bool ok = true;
       for (int n = 0; ok && seg_wait(n); ++n) {
         const Seg& s = c->seg[n % ring];
         if (s.rows == 0) break;
         const int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
         const int* const base = first + P.slots + 1;
-        const int n_tok = P.slots ? first[P.slots] : s.tok1 - s.tok0;
-        auto find = [&](int tile, int cnt) -> int {      // this lane's token of a tile: its id for the streams, its row in the cache
+        const int n_tok = P.slots ? first[P.slots] : s.tok1 - s.tok0, tile0 = s.tile0, tile1 = s.tile1;
+        auto find = [&](int tile, int cnt) -> long long {   // this lane's token of a tile: its id for the streams, its place in the cache
           const int num = tile * TILE + w * 32 + lane;
-          int id = NO_TOKEN, row = -1;
+          int id = NO_TOKEN;
+          long long at = -1;
           if (num < n_tok) {
             int tok;
             if (P.slots) {
@@ -415,58 +419,53 @@ attend_tc_kernel(const __grid_constant__ Params P, const RowStrides rs, const in
             } else {
               tok = s.tok0 + num;
             }
-            const int col = tok / P.page_tokens, page = __ldg(s.pages + col);
-            if (page >= 0 && page < P.num_pages) {
-              id = tok;
-              row = page * rs.page + s.kvh * rs.head + (tok - col * P.page_tokens) * rs.token;
-            } else if (P.status) {
-              atomicOr(P.status, RR_STATUS_BAD_INDEX);
-            }
+            at = token_at(P, s, tok);
+            if (at >= 0) id = tok;
           }
           const int top = __reduce_max_sync(FULL, id);
           c->ids[cnt % IDS][w * 32 + lane] = id;
           if (lane == 0) c->max_id[cnt % IDS][w] = top;
           __syncwarp();
           if (lane == 0) mbar_arrive(&c->ids_full[cnt % IDS]);
-          return row;
+          return at;
         };
-        auto load = [&](const void* cache, int row) -> bool {
-          const uint32_t st = fills % S::STAGES, parity = (fills / S::STAGES & 1) ^ 1;
-          if (!__all_sync(FULL, mbar_try_wait(&c->empty[st], parity))) {
-            cp_async_wait<0>();                          // nothing that has arrived waits for the next fill
-            settle(fills);
-            if (!__all_sync(FULL, mbar_wait_spin(&c->empty[st], parity, abort_flag))) return false;
-          }
-          const uint8_t* const src0 = (const uint8_t*)cache + (lane & 7) * 16;
-          const uint32_t dst = dst0 + st * S::TILE_BYTES;
-  #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int r = __shfl_sync(FULL, row, i * 4 + (lane >> 3));
-            const uint8_t* const src = src0 + (size_t)max(r, 0) * (D * 2);
-            const uint32_t at = dst + i * 512 + (((lane & 7) ^ ((i * 4 + (lane >> 3)) & 7)) << 4);
-  #pragma unroll
-            for (int h = 0; h < S::HALVES; ++h) cp_async16(at + h * S::HALF_BYTES, src + h * 128, r >= 0 ? 16u : 0u);
-          }
-          cp_async_commit();
+        auto load = [&](const void* cache, long long at) -> bool {
+          const uint32_t st = fills % S::STAGES;
+          if (!free_slot(&c->empty[st], (fills / S::STAGES & 1) ^ 1)) return false;
+          rows32(cache, at, kv_addr + st * S::TILE_BYTES);
+          commit(&c->full[st]);
           ++fills;
-          cp_async_wait<2>();
-          if (fills >= 2 + landed) settle(fills - 2);
           return true;
         };
-        int next = s.tile0 < s.tile1 ? find(s.tile0, tiles) : -1;
-        for (int t = s.tile0; t < s.tile1; ++t) {
-          const int row = next;
-          ok = load(P.k, row);
+        long long next = tile0 < tile1 ? find(tile0, tiles) : -1;
+        for (int t = tile0; t < tile1; ++t) {
+          const long long at = next;
+          ok = load(P.k, at);
           if (!ok) break;
-          if (t + 1 < s.tile1) next = find(t + 1, tiles + 1);
-          ok = load(P.v, row);
+          if (t == tile0) {
+            const int rows = s.rows;
+            for (int h = 0; ok && h < (rows > TILE ? 2 : 1); ++h, ++place) {
+              const int q = place & 1, r = h * TILE + w * 32 + lane;
+              ok = free_slot(&c->q_empty[q], (place >> 1 & 1) ^ 1);
+              if (!ok) break;
+              long long o = -1;
+              if (r < rows) {
+                const int idx = s.row0 + r, dt = idx / P.group;
+                o = q_at(P, s, RowAt{s.t_base + dt, s.h0 + idx - dt * P.group, 0});
+              }
+              if (h * TILE + w * 32 < rows) rows32(P.q, o, q_addr + q * S::TILE_BYTES);
+              commit(&c->q_full[q]);
+            }
+            if (!ok) break;
+          }
+          if (t + 1 < tile1) next = find(t + 1, tiles + 1);
+          ok = load(P.v, at);
           if (!ok) break;
           ++tiles;
         }
         if (ok) seg_done(n);
       }
-      cp_async_wait<0>();                                // (do not leave with copies in flight)
-      settle(fills);
+      flush();                                         // (do not leave with copies in flight)
     } else if (warp == 8) {
       // ===== products =====
       constexpr uint32_t idesc_s = umma_idesc_bf16(TILE, TILE), idesc_o = idesc_b_mn(TILE, D);
@@ -535,10 +534,6 @@ attend_tc_kernel(const __grid_constant__ Params P, const RowStrides rs, const in
   }
 }
 
-long long cache_rows(const Params& p) {
-  return ((p.num_pages - 1) * p.page_stride + (p.kv_heads - 1) * p.head_stride + (p.page_tokens - 1) * p.token_stride) / p.dh + 1;
-}
-
 template <int D>
 cudaError_t launch(const Params& p, int grid, cudaStream_t st) {
   const int ring = p.slots > 256 ? 2 : MAX_RING;
@@ -548,17 +543,15 @@ cudaError_t launch(const Params& p, int grid, cudaStream_t st) {
     return cudaFuncSetAttribute(attend_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, a > b ? a : b);
   });
   if (e != cudaSuccess) return e;
-  const RowStrides rs{(int)(p.page_stride / D), (int)(p.head_stride / D), (int)(p.token_stride / D)};
-  return rr_launch_pdl(attend_tc_kernel<D>, grid, NT, (size_t)Smem::total<D>(p.slots, ring), st, p, rs, ring, std::fabs(p.scale_log2), p.scale_log2 < 0.f ? 1 : 0);
+  return rr_launch_pdl(attend_tc_kernel<D>, grid, NT, (size_t)Smem::total<D>(p.slots, ring), st, p, ring);
 }
 
 }  // namespace
 
 bool rr_attend_tc_supported(const Params& p, int dtype) {
-  if (dtype != RR_BF16 || (p.dh != 64 && p.dh != 128) || !(std::fabs(p.scale_log2) > 1e-30f)) return false;
-  if ((p.page_stride | p.head_stride | p.token_stride) % p.dh != 0 || p.page_stride / p.dh > 0x7FFFFFFF || cache_rows(p) > 0x7FFFFFF0LL) return false;
+  if (dtype != RR_BF16 || (p.dh != 64 && p.dh != 128) || !(p.scale_log2 > 1e-30f)) return false;   // (the largest product has the largest logit)
   if (((uintptr_t)p.k | (uintptr_t)p.v | (uintptr_t)p.q | (uintptr_t)p.out) & 15) return false;
-  return (p.qb | p.qh | p.qt | p.ob | p.oh | p.ot) % 8 == 0;
+  return (p.page_stride | p.head_stride | p.token_stride | p.qb | p.qh | p.qt | p.ob | p.oh | p.ot) % 8 == 0;
 }
 
 cudaError_t rr_launch_attend_tc(const Params& p, int grid, cudaStream_t st) { return p.dh == 64 ? launch<64>(p, grid, st) : launch<128>(p, grid, st); }
