@@ -96,7 +96,7 @@ __device__ __forceinline__ int cta_of(const Params& P, long long u, long long W)
   return (int)(((u + 1) * N + W - 1) / W - 1);
 }
 
-// The segment at tile u of CTA c's share, which ends at u1; returns its number of tiles.
+// The segment at tile u of CTA c's share, which ends at u1; returns how many tiles of the share it takes.
 __device__ __forceinline__ int segment_at(const Params& P, int c, long long u, long long u0, long long u1, Seg& s) {
   const long long np = prefix_tiles(P), qtp = prefix_row_tiles(P), before = P.kv_heads * qtp * np;
   long long first;                                     // first tile of the item
@@ -137,8 +137,13 @@ __device__ __forceinline__ int segment_at(const Params& P, int c, long long u, l
   s.h0 = s.kvh * P.group;
   s.tile0 = (int)(u - first);
   s.tile1 = (int)min((long long)tiles, u1 - first);
+  const int took = s.tile1 - s.tile0;
+  if (P.causal && s.b >= 0) {                          // no row sees the tiles from the last row's limit on
+    const int limit = s.tok1 - s.n_seq + (s.row0 + s.rows - 1) / P.group + 1;
+    s.tile1 = max(s.tile0, min(s.tile1, limit <= s.tok0 ? 0 : (limit - s.tok0 + TILE - 1) / TILE));
+  }
   s.part = s.tile0 == 0 ? home : 2 * (long long)P.tokens * P.heads + (long long)c * ROWS;
-  return s.tile1 - s.tile0;
+  return took;
 }
 
 // Segment x of a ranges call (x < range_rows * row tiles * splits); its tiles are counted by who reads the slots.

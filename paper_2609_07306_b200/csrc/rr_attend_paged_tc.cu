@@ -48,7 +48,7 @@ struct Ctl {
   Seg seg[MAX_RING];
   int limit[MAX_RING][ROWS];
   int ids[IDS][TILE];
-  int max_id[IDS][4];
+  int4 info[IDS][4];                                   // per copying warp: largest, first, last id; whether they ascend
 };
 
 struct Smem {
@@ -166,25 +166,41 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
           tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < 4; ++i) tie(x[i]);
-          const int4 tops = *reinterpret_cast<const int4*>(c->max_id[cnt % IDS]);
-          const int top_id = max(max(tops.x, tops.y), max(tops.z, tops.w));
-          if (__any_sync(FULL, live && top_id >= limit)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                const int4 id = *reinterpret_cast<const int4*>(&c->ids[cnt % IDS][i * 32 + j]);
-                const int e[4] = {id.x, id.y, id.z, id.w};
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                  const bool sees = e[w] < limit;
-                  seen = seen || sees;
-                  mixed = mixed || (!sees && e[w] != NO_TOKEN);
-                  if (!sees) x[i][j + w] = 0xFF800000u;
-                }
-              }
-          } else {
+          const int4* const info = c->info[cnt % IDS];
+          const int top_id = max(max(info[0].x, info[1].x), max(info[2].x, info[3].x));
+          if (!__any_sync(FULL, live && top_id >= limit)) {
             seen = true;
+          } else {
+            const int4 i0 = info[0], i1 = info[1], i2 = info[2], i3 = info[3];
+            const int* const ids = c->ids[cnt % IDS];
+            if (i0.w && i1.w && i2.w && i3.w && i0.z <= i1.y && i1.z <= i2.y && i2.z <= i3.y) {
+              // ids ascend (every list in order, without bad pages inside): the row sees the first `see` columns
+              int see = 0;
+#pragma unroll
+              for (int step = TILE / 2; step; step >>= 1) if (ids[see + step - 1] < limit) see += step;
+              see += ids[see] < limit;
+              seen = seen || see > 0;
+              mixed = mixed || (see < TILE && ids[min(see, TILE - 1)] != NO_TOKEN);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x[i][j] = i * 32 + j < see ? x[i][j] : 0xFF800000u;
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                  const int4 id = *reinterpret_cast<const int4*>(ids + i * 32 + j);
+                  const int e[4] = {id.x, id.y, id.z, id.w};
+#pragma unroll
+                  for (int w = 0; w < 4; ++w) {
+                    const bool sees = e[w] < limit;
+                    seen = seen || sees;
+                    mixed = mixed || (!sees && e[w] != NO_TOKEN);
+                    if (!sees) x[i][j + w] = 0xFF800000u;
+                  }
+                }
+            }
           }
           float top = NINF;
 #pragma unroll
@@ -424,7 +440,10 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
           }
           const int top = __reduce_max_sync(FULL, id);
           c->ids[cnt % IDS][w * 32 + lane] = id;
-          if (lane == 0) c->max_id[cnt % IDS][w] = top;
+          const int after = __shfl_down_sync(FULL, id, 1);
+          const bool ascend = __all_sync(FULL, lane == 31 || id <= after);
+          const int last = __shfl_sync(FULL, id, 31);
+          if (lane == 0) c->info[cnt % IDS][w] = make_int4(top, id, last, ascend);
           __syncwarp();
           if (lane == 0) mbar_arrive(&c->ids_full[cnt % IDS]);
           return at;
