@@ -11,12 +11,13 @@
 // The tensor pipe takes 2 x 520 cycles for a 128 x 128 x 128 tile's two products, the 16384 exponentials take 1024: many rows are
 // bound by both about equally, few rows by the cache's traffic.
 //
-// Warps 0-3, 4-7: the streams, a thread per row.  8: issues the products.  9: finds the segments.  10: the rows' limits.
-// 12-15: copies of token and query rows, 32 rows each, 16 bytes per thread, tokens through whatever pages they lie in; a place
-// without a token is filled with zeros.  Segments go round in a ring, so that the next one's look-ups and queries are there before it begins.
-// (TMA's tile::gather4, four token rows per copy, took about 100 cycles of issue per copy: 8 us per tile.)
-// Step k of a segment is (stream k % 2, tile k / 2 if paired, else k):  S(k) is issued behind the product with P(k - 2) of the
-// same stream, which reads the same columns; the tensor pipe keeps that order.
+// Warps 0-3, 4-7: the streams, a thread per row.  8, 11: issue the products, one stream's each.  9: finds the segments.  10: the rows' limits.
+// 12-15: copies of token and query rows, 32 rows each.  Where those 32 tokens are runs of 32, 16 or 8 in a page, TMA brings
+// a run per copy (and half of 64 entries); else 16 bytes per thread, through whatever pages they lie in, and zeros
+// for a place without a token.  Segments go round in a ring, so that the next one's look-ups and queries are there before it begins.
+// (16 bytes per thread for every tile cost the copying warps 2000 cycles of a tile, and the streams issue slots; TMA's tile::gather4,
+// four token rows per copy, about 100 cycles of issue per copy, 8 us per tile.)
+// A stream's S(k) is issued behind its product with P(k - 1), which reads the same columns; the tensor pipe keeps that order.
 //
 // The reference of the softmax follows the row's maximum only when that has grown by more than 8 (a factor of
 // 256): weights up to 2^8 lose nothing in bf16 and FP32, and the output is rescaled in TMEM a few times per
@@ -24,6 +25,7 @@
 //
 // Every wait is bounded; one that runs out sets RR_STATUS_TIMEOUT, and the CTA waits for its copies and
 // products in flight, frees its TMEM and returns.
+#include <algorithm>
 #include "rr_attend_paged.cuh"
 #include "rr_sm100.cuh"
 
@@ -33,8 +35,9 @@ using namespace sm100;
 namespace {
 
 constexpr unsigned FULL = 0xFFFFFFFFu;
-constexpr int NT = 512, IDS = 8, MAX_RING = 4;
+constexpr int NT = 512, IDS = 16, MAX_RING = 4;
 constexpr float GROWTH = 8.f;
+constexpr int BY_FMA = 2;                              // of every 8 pairs of exponentials, by multiply-adds
 
 template <int D> struct Shape {
   static constexpr int HALVES = D / 64, STAGES = D == 128 ? 4 : 8;
@@ -42,7 +45,7 @@ template <int D> struct Shape {
 };
 
 struct Ctl {
-  uint64_t full[8], empty[8], s_full[2], p_full[2], o_full[2], q_full[2], q_empty[2], ids_full[IDS], seg_full[MAX_RING], seg_empty[MAX_RING],
+  uint64_t full[8], empty[8], s_full[2], p_full[2][2], o_full[2], q_full[2], q_empty[2], ids_full[IDS], seg_full[MAX_RING], seg_empty[MAX_RING],
       rows_full[MAX_RING], drain;
   uint32_t tmem_base, abort_flag;
   Seg seg[MAX_RING];
@@ -60,6 +63,17 @@ struct Smem {
 // 16 bytes from global to shared memory, zeros if n == 0.
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t n) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+// `rows` tokens from place y of a page on, 64 entries from x on; a converged warp calls, one lane issues.
+__device__ __forceinline__ void tma_rows_warp(uint32_t dst, const CUtensorMap* map, int x, int y, int head, int page, uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(head), "r"(page), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void expect_tx_warp(uint64_t* bar, uint32_t bytes) {
+  asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}"
+               ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -95,9 +109,43 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   uint32_t y; asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo)); return y;
 }
 
+// Where a token is: its page (-1: zeros) and place there; box: which of the maps' boxes bring the warp's rows (1, 2, 3: 32, 16, 8 tokens), 0: none
+struct Where { int page, place, box; };
+
+// Pairs of FP32 numbers: one instruction for both.
+__device__ __forceinline__ uint64_t two(float lo, float hi) { uint64_t y; asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(lo), "f"(hi)); return y; }
+__device__ __forceinline__ void split(uint64_t x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t y; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c)); return y; }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t y; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b)); return y; }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t y; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b)); return y; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float y; asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c)); return y; }
+__device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
+
+// 2^x of a pair by multiply-adds, beside the special-function unit (16 results a cycle and SM), which the exponentials of a tile
+// alone would keep busy as long as the tensor pipe.  x = n + r, |r| <= 1/2 (Cody and Waite's reduction; n by adding 1.5 * 2^23), and
+// 2^r by the polynomial of degree 4 with constant term 1 whose largest relative error there is smallest (2.9e-6, by linear
+// programming over 4001 points; the weights are rounded to bf16, 2^-9).  n <= -127 gives 0, NaN stays NaN.
+__device__ __forceinline__ uint64_t exp2_fma(uint64_t x) {
+  float x0, x1;
+  split(x, x0, x1);
+  x = two(max_nan(x0, -127.f), max_nan(x1, -127.f));
+  const uint64_t shift = two(12582912.f, 12582912.f), t = add2(x, shift), n = add2(t, two(-12582912.f, -12582912.f));
+  const uint64_t r = fma2(n, two(-1.f, -1.f), x);
+  uint64_t p = fma2(two(0.009582852944731712f, 0.009582852944731712f), r, two(0.055906426161527634f, 0.055906426161527634f));
+  p = fma2(p, r, two(0.24024099111557007f, 0.24024099111557007f));
+  p = fma2(p, r, two(0.6931241750717163f, 0.6931241750717163f));
+  p = fma2(p, r, two(1.f, 1.f));
+  float t0, t1;
+  split(t, t0, t1);
+  return mul2(p, two(__uint_as_float(__float_as_uint(t0) * 0x800000u + 0x3F800000u), __uint_as_float(__float_as_uint(t1) * 0x800000u + 0x3F800000u)));
+}
+
+// Keys and values as [pages][heads][page tokens][entries] with boxes of 32, 16 and 8 tokens.
+struct Maps { CUtensorMap k[3], v[3]; };
+
 template <int D>
 __global__ void __launch_bounds__(NT, 1)
-attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
+attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps maps, const int ring) {
   using S = Shape<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -108,16 +156,17 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
   const int warp = __shfl_sync(FULL, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < S::STAGES; ++i) { mbar_init(&c->full[i], 4); mbar_init(&c->empty[i], 1); }
+    for (int i = 0; i < S::STAGES; ++i) { mbar_init(&c->full[i], 4); mbar_init(&c->empty[i], 2); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&c->s_full[i], 1); mbar_init(&c->p_full[i], 128); mbar_init(&c->o_full[i], 1);
-      mbar_init(&c->q_full[i], 4); mbar_init(&c->q_empty[i], 1);
+      mbar_init(&c->s_full[i], 1); mbar_init(&c->p_full[i][0], 128); mbar_init(&c->p_full[i][1], 128); mbar_init(&c->o_full[i], 1);
+      mbar_init(&c->q_full[i], 4); mbar_init(&c->q_empty[i], 2);
     }
     for (int i = 0; i < IDS; ++i) mbar_init(&c->ids_full[i], 4);
-    for (int i = 0; i < MAX_RING; ++i) { mbar_init(&c->seg_full[i], 1); mbar_init(&c->seg_empty[i], 14); mbar_init(&c->rows_full[i], 1); }
-    mbar_init(&c->drain, 1);
+    for (int i = 0; i < MAX_RING; ++i) { mbar_init(&c->seg_full[i], 1); mbar_init(&c->seg_empty[i], 15); mbar_init(&c->rows_full[i], 1); }
+    mbar_init(&c->drain, 2);
     c->abort_flag = 0;
     mbar_fence_init();
+    for (int i = 0; i < 3; ++i) { tma_prefetch_desc(&maps.k[i]); tma_prefetch_desc(&maps.v[i]); }
   }
   if (warp == 8) tmem_alloc(&c->tmem_base, 512);
   tc_fence_before();
@@ -206,7 +255,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 32; ++j) top = fmaxf(top, __uint_as_float(x[i][j]));
+            for (int j = 0; j < 32; j += 2) top = max3(top, __uint_as_float(x[i][j]), __uint_as_float(x[i][j + 1]));
           const float m = live && top != NINF ? top * P.scale_log2 : NINF;
           if (__any_sync(FULL, m > ref + GROWTH)) {    // (ref = -inf: the first finite maximum)
             const float now = m > ref + GROWTH ? m : ref;
@@ -227,24 +276,41 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
             }
           }
           const float sub = ref == NINF ? 0.f : ref;
-          float a0 = 0.f, a1 = 0.f;
+          const uint64_t scale2 = two(P.scale_log2, P.scale_log2), sub2 = two(-sub, -sub);
+          uint64_t a[2] = {0, 0};
 #pragma unroll
-          for (int i = 0; i < 4; i += 2) {
+          for (int h = 0; h < 2; ++h) {
             uint32_t p[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-              const float e0 = ex2(fmaf(__uint_as_float(x[i + j / 16][2 * (j % 16)]), P.scale_log2, -sub));
-              const float e1 = ex2(fmaf(__uint_as_float(x[i + j / 16][2 * (j % 16) + 1]), P.scale_log2, -sub));
-              a0 += e0; a1 += e1;
+              const uint32_t* const y = &x[2 * h + j / 16][2 * (j % 16)];
+              const uint64_t v = fma2(two(__uint_as_float(y[0]), __uint_as_float(y[1])), scale2, sub2);
+              uint64_t e;
+              if (j % 8 < BY_FMA) {
+                e = exp2_fma(v);
+              } else {
+                float v0, v1;
+                split(v, v0, v1);
+                e = two(ex2(v0), ex2(v1));
+              }
+              a[j & 1] = add2(a[j & 1], e);
+              float e0, e1;
+              split(e, e0, e1);
               p[j] = pack(e0, e1);
             }
-            tmem_st_32x32(s_tm + i * 16, p);
+            tmem_st_32x32(s_tm + h * 32, p);
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(&c->p_full[st][h]);
           }
-          sum += a0 + a1;
-          tmem_st_wait();
+          float s0, s1;
+          split(add2(a[0], a[1]), s0, s1);
+          sum += s0 + s1;
+        } else {
+          tc_fence_before();
+          mbar_arrive(&c->p_full[st][0]);
+          mbar_arrive(&c->p_full[st][1]);
         }
-        tc_fence_before();
-        mbar_arrive(&c->p_full[st]);
       }
       if (!ok) break;
       tiles += nt;
@@ -339,7 +405,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
             int lo = 0, hi = 0;
             if (j < P.slots) slot_span(s, j, lo, hi);
             int incl = hi - lo;
-  #pragma unroll
+#pragma unroll
             for (int off = 1; off < 32; off <<= 1) { const int x = __shfl_up_sync(FULL, incl, off); if (lane >= off) incl += x; }
             if (j < P.slots) { first[j] = run + incl - (hi - lo); base[j] = lo - first[j]; }
             run += __shfl_sync(FULL, incl, 31);
@@ -368,8 +434,8 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
         seg_done(n);
       }
     } else if (warp >= 12) {
-      // ===== copies: fills 2 i (keys) and 2 i + 1 (values) of the CTA's i-th tile, and behind a segment's first keys its queries,
-      // into Q places 0 and 1 in turn (a paired segment takes two).  Warp w has rows 32 w .. 32 w + 31 =====
+      // ===== copies: keys two tiles ahead of the values, and behind a segment's first keys its queries, into Q places 0 and 1
+      // in turn (a paired segment takes two).  Warp w has rows 32 w .. 32 w + 31 =====
       const int w = warp - 12;
       const uint32_t dst0 = (w * 32 + (lane >> 3)) * 128;              // row lane / 8 of this warp's, 16-byte piece lane % 8
       int tiles = 0, place = 0;                        // of all segments so far
@@ -422,74 +488,119 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
         const int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
         const int* const base = first + P.slots + 1;
         const int n_tok = P.slots ? first[P.slots] : s.tok1 - s.tok0, tile0 = s.tile0, tile1 = s.tile1;
-        auto find = [&](int tile, int cnt) -> long long {   // this lane's token of a tile: its id for the streams, its place in the cache
+        // this lane's token of a tile: `seek` asks for its page, `find` has its id for the streams and its place in the cache
+        int tok = NO_TOKEN, page = -1;
+        auto seek = [&](int tile) {
           const int num = tile * TILE + w * 32 + lane;
-          int id = NO_TOKEN;
-          long long at = -1;
-          if (num < n_tok) {
-            int tok;
-            if (P.slots) {
-              int lo = 0, hi = P.slots;
-              while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (first[mid] <= num) lo = mid; else hi = mid; }
-              tok = base[lo] + num;
-            } else {
-              tok = s.tok0 + num;
-            }
-            at = token_at(P, s, tok);
-            if (at >= 0) id = tok;
+          tok = NO_TOKEN;
+          if (tile >= tile1 || num >= n_tok) return;
+          if (P.slots) {
+            int lo = 0, hi = P.slots;
+            while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (first[mid] <= num) lo = mid; else hi = mid; }
+            tok = base[lo] + num;
+          } else {
+            tok = s.tok0 + num;
           }
-          const int top = __reduce_max_sync(FULL, id);
-          c->ids[cnt % IDS][w * 32 + lane] = id;
-          const int after = __shfl_down_sync(FULL, id, 1);
-          const bool ascend = __all_sync(FULL, lane == 31 || id <= after);
-          const int last = __shfl_sync(FULL, id, 31);
-          if (lane == 0) c->info[cnt % IDS][w] = make_int4(top, id, last, ascend);
+          page = __ldg(s.pages + tok / P.page_tokens);
+        };
+        auto find = [&](int tile) -> Where {
+          Where at{-1, 0, 0};
+          if (tile >= tile1) return at;
+          const int cnt = tiles + tile - tile0;
+          if (tok != NO_TOKEN) {
+            if (page >= 0 && page < P.num_pages) {
+              at.page = page;
+              at.place = tok - tok / P.page_tokens * P.page_tokens;
+            } else {
+              tok = NO_TOKEN;
+              if (P.status) atomicOr(P.status, RR_STATUS_BAD_INDEX);
+            }
+          }
+          // the longest run of tokens that every aligned run of the warp's 32 places holds
+#pragma unroll
+          for (int run = 32, i = 1; run >= 8; run >>= 1, ++i) {
+            const int from = lane & ~(run - 1);
+            const int page0 = __shfl_sync(FULL, at.page, from), place0 = __shfl_sync(FULL, at.place, from);
+            const bool in = at.page >= 0 && page0 == at.page && place0 + lane - from == at.place;
+            const bool all = __all_sync(FULL, in);
+            if (at.box == 0 && all) at.box = i;
+          }
+          const int top = __reduce_max_sync(FULL, tok), after = __shfl_down_sync(FULL, tok, 1), last = __shfl_sync(FULL, tok, 31);
+          const bool ascend = __all_sync(FULL, lane == 31 || tok <= after);
+          c->ids[cnt % IDS][w * 32 + lane] = tok;
+          if (lane == 0) c->info[cnt % IDS][w] = make_int4(top, tok, last, ascend);
           __syncwarp();
           if (lane == 0) mbar_arrive(&c->ids_full[cnt % IDS]);
           return at;
         };
-        auto load = [&](const void* cache, long long at) -> bool {
+        auto load = [&](const void* cache, const CUtensorMap* map, const Where& at) -> bool {
           const uint32_t st = fills % S::STAGES;
           if (!free_slot(&c->empty[st], (fills / S::STAGES & 1) ^ 1)) return false;
-          rows32(cache, at, kv_addr + st * S::TILE_BYTES);
-          commit(&c->full[st]);
+          if (at.box) {
+            const int run = 64 >> at.box;
+            expect_tx_warp(&c->full[st], 32 * D * 2);
+#pragma unroll 1
+            for (int r = 0; r < 32; r += run) {
+              const int pg = __shfl_sync(FULL, at.page, r), pl = __shfl_sync(FULL, at.place, r);
+#pragma unroll
+              for (int h = 0; h < S::HALVES; ++h)
+                tma_rows_warp(kv_addr + st * S::TILE_BYTES + h * S::HALF_BYTES + (w * 32 + r) * 128, map + at.box - 1, h * 64, pl, s.kvh, pg, &c->full[st]);
+            }
+          } else {
+            rows32(cache, at.page < 0 ? -1 : at.page * P.page_stride + s.kvh * P.head_stride + at.place * P.token_stride, kv_addr + st * S::TILE_BYTES);
+            commit(&c->full[st]);
+          }
           ++fills;
           return true;
         };
-        long long next = tile0 < tile1 ? find(tile0, tiles) : -1;
-        for (int t = tile0; t < tile1; ++t) {
-          const long long at = next;
-          ok = load(P.k, at);
-          if (!ok) break;
-          if (t == tile0) {
-            const int rows = s.rows;
-            for (int h = 0; ok && h < (rows > TILE ? 2 : 1); ++h, ++place) {
-              const int q = place & 1, r = h * TILE + w * 32 + lane;
-              ok = free_slot(&c->q_empty[q], (place >> 1 & 1) ^ 1);
-              if (!ok) break;
-              long long o = -1;
-              if (r < rows) {
-                const int idx = s.row0 + r, dt = idx / P.group;
-                o = q_at(P, s, RowAt{s.t_base + dt, s.h0 + idx - dt * P.group, 0});
-              }
-              if (h * TILE + w * 32 < rows) rows32(P.q, o, q_addr + q * S::TILE_BYTES);
-              commit(&c->q_full[q]);
-            }
+        if (tile0 < tile1) {                           // K(0) queries K(1) V(0) K(2) V(1) ... K(n-1) V(n-2) V(n-1)
+          Where at[3];
+          seek(tile0);
+          at[0] = find(tile0);
+          seek(tile0 + 1);
+          ok = load(P.k, maps.k, at[0]);
+          const int rows = s.rows;
+          for (int h = 0; ok && h < (rows > TILE ? 2 : 1); ++h, ++place) {
+            const int q = place & 1, r = h * TILE + w * 32 + lane;
+            ok = free_slot(&c->q_empty[q], (place >> 1 & 1) ^ 1);
             if (!ok) break;
+            long long o = -1;
+            if (r < rows) {
+              const int idx = s.row0 + r, dt = idx / P.group;
+              o = q_at(P, s, RowAt{s.t_base + dt, s.h0 + idx - dt * P.group, 0});
+            }
+            if (h * TILE + w * 32 < rows) rows32(P.q, o, q_addr + q * S::TILE_BYTES);
+            commit(&c->q_full[q]);
           }
-          if (t + 1 < tile1) next = find(t + 1, tiles + 1);
-          ok = load(P.v, at);
+          at[1] = find(tile0 + 1);
+          seek(tile0 + 2);
+          if (ok && tile0 + 1 < tile1) ok = load(P.k, maps.k, at[1]);
+          if (ok) flush();                             // the queries
+          for (int t = tile0; ok && t < tile1; ++t) {
+            ok = load(P.v, maps.v, at[0]);
+            if (!ok) break;
+            at[2] = find(t + 2);
+            seek(t + 3);
+            if (t + 2 < tile1) ok = load(P.k, maps.k, at[2]);
+            at[0] = at[1];
+            at[1] = at[2];
+          }
           if (!ok) break;
-          ++tiles;
+          tiles += tile1 - tile0;
         }
         if (ok) seg_done(n);
       }
       flush();                                         // (do not leave with copies in flight)
-    } else if (warp == 8) {
-      // ===== products =====
+      for (uint32_t f = fills > S::STAGES ? fills - S::STAGES : 0; f < fills; ++f)
+        for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->full[f % S::STAGES], f / S::STAGES & 1); ++it) __nanosleep(64);
+      __syncwarp();
+    } else {
+      // ===== products: warp 8 those of stream 0, warp 11 those of stream 1, so that one's waits stand beside the other's products =====
       constexpr uint32_t idesc_s = umma_idesc_bf16(TILE, TILE), idesc_o = idesc_b_mn(TILE, D);
+      const int st = warp == 8 ? 0 : 1;
+      const uint32_t s_tm = tmem + st * 128, o_tm = tmem + 256 + st * 128;
       int place = 0;
-      uint32_t tiles = 0, p_cnt[2] = {0, 0};
+      uint32_t tiles = 0, p_cnt = 0;
       bool ok = true;
       auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL, mbar_wait_spin(bar, parity & 1, abort_flag)); };
       for (int n = 0; ok && seg_wait(n); ++n) {
@@ -497,48 +608,59 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
         const int nt = __shfl_sync(FULL, c->seg[n % ring].tile1 - c->seg[n % ring].tile0, 0);
         if (rows == 0) break;
         const bool paired = rows > TILE;
-        const int steps = paired ? 2 * nt : nt;
-        if (steps == 0) { seg_done(n); continue; }
-        ok = wait(&c->q_full[place & 1], place >> 1);
-        if (ok && paired) ok = wait(&c->q_full[(place + 1) & 1], (place + 1) >> 1);
-        for (int k = 0; ok && k < steps + 2; ++k) {
-          if (k >= 2) {
-            const int kk = k - 2, st = kk & 1;
-            const uint32_t f = 2 * (tiles + (paired ? kk >> 1 : kk)) + 1, stage = f % S::STAGES;
-            ok = wait(&c->p_full[st], p_cnt[st]) && wait(&c->full[stage], f / S::STAGES);
-            if (!ok) break;
-            ++p_cnt[st];
-            tc_fence_after();
+        const int steps = paired ? nt : (nt - st + 1) / 2;
+        if (nt == 0) { seg_done(n); continue; }
+        const int at = (place + (paired ? st : 0)) & 1;
+        ok = wait(&c->q_full[at], (place + (paired ? st : 0)) >> 1);
+        const uint64_t qd = umma_desc_k_sw128(q_addr + at * S::TILE_BYTES);
+        for (int k = 0; ok && k <= steps; ++k) {
+          if (k > 0) {
+            const int tile = paired ? k - 1 : 2 * (k - 1) + st;
+            const uint32_t f = 2 * tiles + (tile == nt - 1 ? 2 * nt - 1 : 2 * tile + 2), stage = f % S::STAGES;
+            ok = wait(&c->full[stage], f / S::STAGES);
             const uint64_t vd = desc_mn_sw128(kv_addr + stage * S::TILE_BYTES, S::HALF_BYTES);
-  #pragma unroll
-            for (int j = 0; j < TILE / 16; ++j)
-              umma_bf16_ts_warp(tmem + 256 + st * 128, tmem + st * 128 + j * 8, vd + (uint64_t)(j * 128), idesc_o, (kk >= 2 || j > 0) ? 1u : 0u);
-            if (!paired || st == 1) umma_commit_warp(&c->empty[stage]);
-            if (kk + 2 >= steps) umma_commit_warp(&c->o_full[st]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {              // weights of 64 tokens at a time, as they come
+              ok = ok && wait(&c->p_full[st][h], p_cnt);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll
+              for (int j = h * 4; j < h * 4 + 4; ++j)
+                umma_bf16_ts_warp(o_tm, s_tm + j * 8, vd + (uint64_t)(j * 128), idesc_o, (k > 1 || j > 0) ? 1u : 0u);
+            }
+            if (!ok) break;
+            ++p_cnt;
+            umma_commit_warp(&c->empty[stage]);
+            if (!paired) umma_commit_warp(&c->empty[stage]);
           }
           if (k < steps) {
-            const int st = k & 1;
-            const uint32_t f = 2 * (tiles + (paired ? k >> 1 : k)), stage = f % S::STAGES;
-            const int at = (place + (paired ? st : 0)) & 1;
+            const int tile = paired ? k : 2 * k + st;
+            const uint32_t f = 2 * tiles + (tile == 0 ? 0 : 2 * tile - 1), stage = f % S::STAGES;
             ok = wait(&c->full[stage], f / S::STAGES);
             if (!ok) break;
             tc_fence_after();
-            const uint64_t qd = umma_desc_k_sw128(q_addr + at * S::TILE_BYTES), kd = umma_desc_k_sw128(kv_addr + stage * S::TILE_BYTES);
-  #pragma unroll
+            const uint64_t kd = umma_desc_k_sw128(kv_addr + stage * S::TILE_BYTES);
+#pragma unroll
             for (int j = 0; j < D / 16; ++j) {
               const uint64_t o = (uint64_t)((j >> 2) * (S::HALF_BYTES >> 4) + (j & 3) * 2);
-              umma_bf16_warp(tmem + st * 128, qd + o, kd + o, idesc_s, j > 0 ? 1u : 0u);
+              umma_bf16_warp(s_tm, qd + o, kd + o, idesc_s, j > 0 ? 1u : 0u);
             }
             umma_commit_warp(&c->s_full[st]);
-            if (!paired || st == 1) umma_commit_warp(&c->empty[stage]);
-            if (paired ? k + 2 >= steps : k + 1 == steps) umma_commit_warp(&c->q_empty[at]);
+            umma_commit_warp(&c->empty[stage]);
+            if (!paired) umma_commit_warp(&c->empty[stage]);
+          }
+          if (k + 1 == steps || steps == 0) {          // the queries' place: both streams of a split segment have to be done with it
+            umma_commit_warp(&c->q_empty[at]);
+            if (paired) umma_commit_warp(&c->q_empty[at]);
           }
         }
         if (!ok) break;
+        if (steps > 0) umma_commit_warp(&c->o_full[st]);
         tiles += nt;
         place += paired ? 2 : 1;
         seg_done(n);
       }
+      // TMEM is not freed while a product can still write to it
       umma_commit_warp(&c->drain);
       for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->drain, 0); ++it) __nanosleep(64);
       __syncwarp();
@@ -555,6 +677,13 @@ attend_tc_kernel(const __grid_constant__ Params P, const int ring) {
 
 template <int D>
 cudaError_t launch(const Params& p, int grid, cudaStream_t st) {
+  Maps maps;
+  for (int i = 0; i < 3; ++i) {
+    const int box = std::min(32 >> i, p.page_tokens);
+    cudaError_t m = rr_encode_tmap_bf16_pages(&maps.k[i], p.k, p.dh, p.page_tokens, p.kv_heads, p.num_pages, p.token_stride, p.head_stride, p.page_stride, box);
+    if (m == cudaSuccess) m = rr_encode_tmap_bf16_pages(&maps.v[i], p.v, p.dh, p.page_tokens, p.kv_heads, p.num_pages, p.token_stride, p.head_stride, p.page_stride, box);
+    if (m != cudaSuccess) return m;
+  }
   const int ring = p.slots > 256 ? 2 : MAX_RING;
   static unsigned long long done = 0;
   const cudaError_t e = rr_once_per_device(done, [] {
@@ -562,7 +691,7 @@ cudaError_t launch(const Params& p, int grid, cudaStream_t st) {
     return cudaFuncSetAttribute(attend_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, a > b ? a : b);
   });
   if (e != cudaSuccess) return e;
-  return rr_launch_pdl(attend_tc_kernel<D>, grid, NT, (size_t)Smem::total<D>(p.slots, ring), st, p, ring);
+  return rr_launch_pdl(attend_tc_kernel<D>, grid, NT, (size_t)Smem::total<D>(p.slots, ring), st, p, maps, ring);
 }
 
 }  // namespace
@@ -570,6 +699,7 @@ cudaError_t launch(const Params& p, int grid, cudaStream_t st) {
 bool rr_attend_tc_supported(const Params& p, int dtype) {
   if (dtype != RR_BF16 || (p.dh != 64 && p.dh != 128) || !(p.scale_log2 > 1e-30f)) return false;   // (the largest product has the largest logit)
   if (((uintptr_t)p.k | (uintptr_t)p.v | (uintptr_t)p.q | (uintptr_t)p.out) & 15) return false;
+  if (p.page_stride < 8 || p.head_stride < 8 || p.token_stride < 8 || std::max({p.page_stride, p.head_stride, p.token_stride}) >= 1LL << 38) return false;
   return (p.page_stride | p.head_stride | p.token_stride | p.qb | p.qh | p.qt | p.ob | p.oh | p.ot) % 8 == 0;
 }
 

@@ -127,6 +127,20 @@ cudaError_t rr_encode_tmap_bf16_tile(CUtensorMap* out, const void* base, int d, 
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+cudaError_t rr_encode_tmap_bf16_pages(CUtensorMap* out, const void* base, int d, int page_tokens, int heads, int pages,
+                                      long long token_stride, long long head_stride, long long page_stride, int box_tokens) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return cudaErrorNotSupported;
+  cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)page_tokens, (cuuint64_t)heads, (cuuint64_t)pages};
+  cuuint64_t strides[3] = {(cuuint64_t)token_stride * 2, (cuuint64_t)head_stride * 2, (cuuint64_t)page_stride * 2};
+  cuuint32_t box[4] = {64, (cuuint32_t)box_tokens, 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides,
+                   box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 cudaError_t rr_launch_score_tc(const RRParams& p, const void* qc, const void* kc,
                                const int32_t* row_list, cudaStream_t st) {
   CUtensorMap tmap;

@@ -387,3 +387,6 @@ cudaError_t rr_encode_tmap_bf16_3d(CUtensorMap* out, const void* base, int d, in
 // copy brings box_rows whole rows, K-half by K-half.
 cudaError_t rr_encode_tmap_bf16_tile(CUtensorMap* out, const void* base, int d, int rows, int planes,
                                      int box_rows);
+// A paged cache [pages][heads][page_tokens][d], strides in elements (multiples of 8), with a {64, box_tokens, 1, 1} box.
+cudaError_t rr_encode_tmap_bf16_pages(CUtensorMap* out, const void* base, int d, int page_tokens, int heads, int pages,
+                                      long long token_stride, long long head_stride, long long page_stride, int box_tokens);
