@@ -454,6 +454,8 @@ int fill(const rr_paged_kv* kv, Params& P) {
   P.page_stride = kv->page_stride; P.head_stride = kv->head_stride; P.token_stride = kv->token_stride; P.table_stride = kv->table_stride;
   P.num_pages = kv->num_pages; P.page_tokens = kv->page_tokens; P.kv_heads = kv->kv_heads; P.dh = kv->dh;
   P.batch = kv->batch; P.pages_per_seq = kv->pages_per_seq;
+  P.page_shift = -1;
+  for (int i = 0; i < 31; ++i) if (P.page_tokens == 1 << i) P.page_shift = i;
   // (the stride of a dimension of one entry says nothing)
   if (P.num_pages == 1) P.page_stride = 256;
   if (P.kv_heads == 1) P.head_stride = 256;

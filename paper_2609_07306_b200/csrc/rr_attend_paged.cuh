@@ -32,7 +32,7 @@ struct Params {
   const int32_t* table;
   uint32_t* status;
   long long page_stride, head_stride, token_stride, table_stride;
-  int num_pages, page_tokens, kv_heads, dh, batch, pages_per_seq;
+  int num_pages, page_tokens, page_shift, kv_heads, dh, batch, pages_per_seq;   // page_shift: log2 of page_tokens, -1 if it is no power of two
   // queries
   const void* q;
   void* out;

@@ -45,7 +45,7 @@ template <int D> struct Shape {
 };
 
 struct Ctl {
-  uint64_t full[8], empty[8], s_full[2], p_full[2][2], o_full[2], q_full[2], q_empty[2], ids_full[IDS], seg_full[MAX_RING], seg_empty[MAX_RING],
+  uint64_t full[8], empty[8], s_full[2][2], p_full[2][2], o_done[2][2], q_full[2], q_empty[2], ids_full[IDS], seg_full[MAX_RING], seg_empty[MAX_RING],
       rows_full[MAX_RING], drain;
   uint32_t tmem_base, abort_flag;
   Seg seg[MAX_RING];
@@ -112,6 +112,30 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
 // Where a token is: its page (-1: zeros) and place there; box: which of the maps' boxes bring the warp's rows (1, 2, 3: 32, 16, 8 tokens), 0: none
 struct Where { int page, place, box; };
 
+// 16 rows x 32 columns: register 4 j + 0, 1 of lane 4 g + q has columns 8 j + 2 q, + 1 of row g, registers 4 j + 2, 3 those of row g + 8.
+__device__ __forceinline__ void tmem_ld_16x256_x4(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+}
+// Word j of lane q of every four lanes goes to word q of lane j.
+__device__ __forceinline__ void quad_transpose(uint32_t (&w)[4]) {
+  const int q = threadIdx.x & 3;
+#pragma unroll
+  for (int step = 1; step <= 2; step <<= 1) {
+    const bool up = q & step;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j & step) continue;
+      const uint32_t got = __shfl_xor_sync(FULL, up ? w[j] : w[j | step], step);
+      if (up) w[j] = got; else w[j | step] = got;
+    }
+  }
+}
+
 // Pairs of FP32 numbers: one instruction for both.
 __device__ __forceinline__ uint64_t two(float lo, float hi) { uint64_t y; asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(lo), "f"(hi)); return y; }
 __device__ __forceinline__ void split(uint64_t x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
@@ -158,7 +182,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::STAGES; ++i) { mbar_init(&c->full[i], 4); mbar_init(&c->empty[i], 2); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&c->s_full[i], 1); mbar_init(&c->p_full[i][0], 128); mbar_init(&c->p_full[i][1], 128); mbar_init(&c->o_full[i], 1);
+      for (int h = 0; h < 2; ++h) { mbar_init(&c->s_full[i][h], 1); mbar_init(&c->p_full[i][h], 128); mbar_init(&c->o_done[i][h], 1); }
       mbar_init(&c->q_full[i], 4); mbar_init(&c->q_empty[i], 2);
     }
     for (int i = 0; i < IDS; ++i) mbar_init(&c->ids_full[i], 4);
@@ -202,67 +226,68 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
       const int limit = live ? c->limit[n % ring][r] : 0;
       float ref = NINF, sum = 0.f;
       bool seen = false, mixed = false;
-      for (int k = 0; k < steps; ++k) {
-        const int cnt = tiles + (paired ? k : 2 * k + st);
-        ok = __all_sync(FULL, mbar_wait(&c->ids_full[cnt % IDS], cnt / IDS & 1, abort_flag) && mbar_wait(&c->s_full[st], s_cnt & 1, abort_flag));
+      for (int k = 0; ok && k < 2 * steps; ++k) {      // half a tile, 64 tokens, at a time
+        const int h = k & 1, cnt = tiles + (paired ? k >> 1 : (k & ~1) + st);
+        ok = __all_sync(FULL, mbar_wait(&c->ids_full[cnt % IDS], cnt / IDS & 1, abort_flag) && mbar_wait(&c->s_full[st][h], s_cnt & 1, abort_flag));
         if (!ok) break;
-        ++s_cnt;
+        s_cnt += h;
         tc_fence_after();
         if (warp_live) {
-          uint32_t x[4][32];
+          uint32_t x[2][32];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_ld32(s_tm + i * 32, x[i]);
+          for (int i = 0; i < 2; ++i) tmem_ld32(s_tm + h * 64 + i * 32, x[i]);
           tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 4; ++i) tie(x[i]);
-          const int4* const info = c->info[cnt % IDS];
-          const int top_id = max(max(info[0].x, info[1].x), max(info[2].x, info[3].x));
-          if (!__any_sync(FULL, live && top_id >= limit)) {
+          for (int i = 0; i < 2; ++i) tie(x[i]);
+          const int4 i0 = c->info[cnt % IDS][2 * h], i1 = c->info[cnt % IDS][2 * h + 1];
+          if (!__any_sync(FULL, live && max(i0.x, i1.x) >= limit)) {
             seen = true;
-          } else {
-            const int4 i0 = info[0], i1 = info[1], i2 = info[2], i3 = info[3];
-            const int* const ids = c->ids[cnt % IDS];
-            if (i0.w && i1.w && i2.w && i3.w && i0.z <= i1.y && i1.z <= i2.y && i2.z <= i3.y) {
-              // ids ascend (every list in order, without bad pages inside): the row sees the first `see` columns
-              int see = 0;
+          } else {                                     // which columns the row sees, a bit each
+            uint32_t see[2] = {0, 0};
+            const int* const ids = c->ids[cnt % IDS] + 64 * h;
+            if (i0.w && i1.w && i0.z <= i1.y) {
+              int n = 0;                               // ids ascend (every list in order, no bad page inside): the first n columns
 #pragma unroll
-              for (int step = TILE / 2; step; step >>= 1) if (ids[see + step - 1] < limit) see += step;
-              see += ids[see] < limit;
-              seen = seen || see > 0;
-              mixed = mixed || (see < TILE && ids[min(see, TILE - 1)] != NO_TOKEN);
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 32; ++j) x[i][j] = i * 32 + j < see ? x[i][j] : 0xFF800000u;
+              for (int step = 32; step; step >>= 1) if (ids[n + step - 1] < limit) n += step;
+              n += ids[n] < limit;
+              mixed = mixed || (n < 64 && ids[min(n, 63)] != NO_TOKEN);
+              see[0] = n >= 32 ? FULL : (1u << n) - 1;
+              see[1] = n >= 64 ? FULL : n <= 32 ? 0u : (1u << (n - 32)) - 1;
             } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                  const int4 id = *reinterpret_cast<const int4*>(ids + i * 32 + j);
-                  const int e[4] = {id.x, id.y, id.z, id.w};
-#pragma unroll
-                  for (int w = 0; w < 4; ++w) {
-                    const bool sees = e[w] < limit;
-                    seen = seen || sees;
-                    mixed = mixed || (!sees && e[w] != NO_TOKEN);
-                    if (!sees) x[i][j + w] = 0xFF800000u;
-                  }
+              for (int i = 0; i < 2; ++i)
+#pragma unroll 4
+                for (int j = 0; j < 32; ++j) {
+                  const int id = ids[i * 32 + j];
+                  if (id < limit) see[i] |= 1u << j;
+                  else mixed = mixed || id != NO_TOKEN;
                 }
             }
+            seen = seen || (see[0] | see[1]) != 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int j = 0; j < 32; ++j) if (!(see[i] >> j & 1)) x[i][j] = 0xFF800000u;
           }
-          float top = NINF;
+          float t[4];                                  // (four chains)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t* const y = &x[i >> 1][(i & 1) * 16];
+            t[i] = __uint_as_float(y[0]);
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) top = max3(top, __uint_as_float(x[i][j]), __uint_as_float(x[i][j + 1]));
-          const float m = live && top != NINF ? top * P.scale_log2 : NINF;
+            for (int j = 1; j < 15; j += 2) t[i] = max3(t[i], __uint_as_float(y[j]), __uint_as_float(y[j + 1]));
+            t[i] = fmaxf(t[i], __uint_as_float(y[15]));
+          }
+          const float top = fmaxf(max3(t[0], t[1], t[2]), t[3]), m = live && top != NINF ? top * P.scale_log2 : NINF;
           if (__any_sync(FULL, m > ref + GROWTH)) {    // (ref = -inf: the first finite maximum)
-            const float now = m > ref + GROWTH ? m : ref;
-            const float f = now == ref ? 1.f : ex2(ref - now);
+            const float now = m > ref + GROWTH ? m : ref, f = now == ref ? 1.f : ex2(ref - now);
             ref = now;
             sum *= f;
             if (k > 0) {
+              // the product with the half before may be under way (the one before that is not: this half's logits stand behind it)
+              ok = __all_sync(FULL, mbar_wait(&c->o_done[st][h ^ 1], (o_cnt + ((k - 1) >> 1)) & 1, abort_flag));
+              if (!ok) break;
+              tc_fence_after();
 #pragma unroll 1
               for (int i = 0; i < D / 32; ++i) {
                 uint32_t o[32];
@@ -278,46 +303,39 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           const float sub = ref == NINF ? 0.f : ref;
           const uint64_t scale2 = two(P.scale_log2, P.scale_log2), sub2 = two(-sub, -sub);
           uint64_t a[2] = {0, 0};
+          uint32_t p[32];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t p[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const uint32_t* const y = &x[2 * h + j / 16][2 * (j % 16)];
-              const uint64_t v = fma2(two(__uint_as_float(y[0]), __uint_as_float(y[1])), scale2, sub2);
-              uint64_t e;
-              if (j % 8 < BY_FMA) {
-                e = exp2_fma(v);
-              } else {
-                float v0, v1;
-                split(v, v0, v1);
-                e = two(ex2(v0), ex2(v1));
-              }
-              a[j & 1] = add2(a[j & 1], e);
-              float e0, e1;
-              split(e, e0, e1);
-              p[j] = pack(e0, e1);
+          for (int j = 0; j < 32; ++j) {
+            const uint32_t* const y = &x[j / 16][2 * (j % 16)];
+            const uint64_t v = fma2(two(__uint_as_float(y[0]), __uint_as_float(y[1])), scale2, sub2);
+            uint64_t e;
+            if (j % 8 < BY_FMA) {
+              e = exp2_fma(v);
+            } else {
+              float v0, v1;
+              split(v, v0, v1);
+              e = two(ex2(v0), ex2(v1));
             }
-            tmem_st_32x32(s_tm + h * 32, p);
-            tmem_st_wait();
-            tc_fence_before();
-            mbar_arrive(&c->p_full[st][h]);
+            a[j & 1] = add2(a[j & 1], e);
+            float e0, e1;
+            split(e, e0, e1);
+            p[j] = pack(e0, e1);
           }
           float s0, s1;
           split(add2(a[0], a[1]), s0, s1);
           sum += s0 + s1;
-        } else {
-          tc_fence_before();
-          mbar_arrive(&c->p_full[st][0]);
-          mbar_arrive(&c->p_full[st][1]);
+          tmem_st_32x32(s_tm + h * 64, p);
+          tmem_st_wait();
         }
+        tc_fence_before();
+        mbar_arrive(&c->p_full[st][h]);
       }
       if (!ok) break;
       tiles += nt;
       if (steps > 0) {
-        ok = __all_sync(FULL, mbar_wait(&c->o_full[st], o_cnt & 1, abort_flag));
+        o_cnt += steps;
+        ok = __all_sync(FULL, mbar_wait(&c->o_done[st][1], (o_cnt - 1) & 1, abort_flag));
         if (!ok) break;
-        ++o_cnt;
         tc_fence_after();
       }
       const bool direct = P.direct && paired;
@@ -328,41 +346,70 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         const RowAt a{s.t_base + (s.row0 + r) / P.group, s.h0 + (s.row0 + r) % P.group, 0};
         __nv_bfloat16* const out = (__nv_bfloat16*)P.out + out_at(P, s, a);
         if (live && !direct) P.part_ml[at] = make_float2(ref, sum);
-        bool odd = false;
+        const bool look = __any_sync(FULL, mixed);     // (only then can a value have come in that its row may not see)
+        unsigned odd_rows = 0;
         if (direct || steps > 0) {
+          // TMEM in blocks of 16 rows x 8 columns: lane 4 g + q has columns 2 q, 2 q + 1 of rows g and g + 8, so that after an exchange
+          // inside each four lanes these write 64 bytes of a row together (a thread per row would touch 32 lines per store)
+          const int g = lane >> 2, q = lane & 3;
 #pragma unroll 1
-          for (int i = 0; i < D / 32; ++i) {
-            uint32_t o[32];
-            if (steps > 0) {
-              tmem_ld32(o_tm + i * 32, o);
-              tmem_ld_wait();
-              tie(o);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = 0;
-            }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) odd = odd || !isfinite(__uint_as_float(o[j]));
-            if (live) {
-              if (direct) {
-#pragma unroll
-                for (int j = 0; j < 32; j += 8) {
-                  uint4 y;
-                  y.x = pack(__uint_as_float(o[j]) * inv, __uint_as_float(o[j + 1]) * inv);
-                  y.y = pack(__uint_as_float(o[j + 2]) * inv, __uint_as_float(o[j + 3]) * inv);
-                  y.z = pack(__uint_as_float(o[j + 4]) * inv, __uint_as_float(o[j + 5]) * inv);
-                  y.w = pack(__uint_as_float(o[j + 6]) * inv, __uint_as_float(o[j + 7]) * inv);
-                  *reinterpret_cast<uint4*>(out + i * 32 + j) = y;
-                }
+          for (int half = 0; half < 2; ++half) {
+            const float inv0 = __shfl_sync(FULL, inv, half * 16 + g), inv1 = __shfl_sync(FULL, inv, half * 16 + g + 8);
+            const unsigned long long out0 = __shfl_sync(FULL, (unsigned long long)out, half * 16 + g), out1 = __shfl_sync(FULL, (unsigned long long)out, half * 16 + g + 8);
+            const bool live0 = r - lane + half * 16 + g < s.rows, live1 = r - lane + half * 16 + g + 8 < s.rows;
+            float* const part0 = P.part_o + (at - lane + half * 16 + g) * D;
+            uint32_t odd0 = 0, odd1 = 0;
+#pragma unroll 1
+            for (int i = 0; i < D / 32; ++i) {
+              uint32_t o[16];
+              if (steps > 0) {
+                tmem_ld_16x256_x4(o_tm + ((uint32_t)(half * 16) << 16) + i * 32, o);
               } else {
 #pragma unroll
-                for (int j = 0; j < 32; j += 4)
-                  *reinterpret_cast<uint4*>(P.part_o + at * D + i * 32 + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                for (int j = 0; j < 16; ++j) o[j] = 0;
               }
+              if (look) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  odd0 = max(odd0, max(o[4 * j] & 0x7FFFFFFFu, o[4 * j + 1] & 0x7FFFFFFFu));
+                  odd1 = max(odd1, max(o[4 * j + 2] & 0x7FFFFFFFu, o[4 * j + 3] & 0x7FFFFFFFu));
+                }
+              }
+              if (direct) {
+                uint32_t w0[4], w1[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  w0[j] = pack(__uint_as_float(o[4 * j]) * inv0, __uint_as_float(o[4 * j + 1]) * inv0);
+                  w1[j] = pack(__uint_as_float(o[4 * j + 2]) * inv1, __uint_as_float(o[4 * j + 3]) * inv1);
+                }
+                quad_transpose(w0);                    // lane q: the 8 columns of block q
+                quad_transpose(w1);
+                if (live0) *reinterpret_cast<uint4*>((__nv_bfloat16*)out0 + i * 32 + q * 8) = make_uint4(w0[0], w0[1], w0[2], w0[3]);
+                if (live1) *reinterpret_cast<uint4*>((__nv_bfloat16*)out1 + i * 32 + q * 8) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
+              } else {
+#pragma unroll
+                for (int j = 0; j < 4; j += 2) {
+                  // even lanes take block j, odd lanes block j + 1: columns 2 (q & 2) .. + 3 of it
+#pragma unroll
+                  for (int up = 0; up < 2; ++up) {
+                    uint32_t m0 = o[4 * j + 2 * up], m1 = o[4 * j + 2 * up + 1], n0 = o[4 * j + 4 + 2 * up], n1 = o[4 * j + 5 + 2 * up];
+                    const uint32_t g0 = __shfl_xor_sync(FULL, q & 1 ? m0 : n0, 1), g1 = __shfl_xor_sync(FULL, q & 1 ? m1 : n1, 1);
+                    const uint4 y = q & 1 ? make_uint4(g0, g1, n0, n1) : make_uint4(m0, m1, g0, g1);
+                    if (up ? live1 : live0)
+                      *reinterpret_cast<uint4*>(part0 + up * 8 * D + i * 32 + (j + (q & 1)) * 8 + (q & 2) * 2) = y;
+                  }
+                }
+              }
+            }
+            if (look) {
+              const unsigned b0 = __ballot_sync(FULL, odd0 >= 0x7F800000u), b1 = __ballot_sync(FULL, odd1 >= 0x7F800000u);
+              const unsigned mine = lane >> 3 & 1 ? b1 : b0;                 // lanes 8 .. 15 of a half: the rows g + 8
+              if (lane >> 4 == half && (mine >> (4 * (lane & 7)) & 15u)) odd_rows = 1;
             }
           }
         }
-        unsigned again = __ballot_sync(FULL, live && odd && mixed);
+        __syncwarp();                                  // (the repair below writes rows that other lanes have written)
+        unsigned again = __ballot_sync(FULL, live && odd_rows && mixed);
         while (again) {
           const int who = __ffs(again) - 1;
           again &= again - 1;
@@ -489,19 +536,25 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         const int* const base = first + P.slots + 1;
         const int n_tok = P.slots ? first[P.slots] : s.tok1 - s.tok0, tile0 = s.tile0, tile1 = s.tile1;
         // this lane's token of a tile: `seek` asks for its page, `find` has its id for the streams and its place in the cache
-        int tok = NO_TOKEN, page = -1;
+        int tok = NO_TOKEN, page = -1, col = 0, cur = 0;
         auto seek = [&](int tile) {
           const int num = tile * TILE + w * 32 + lane;
           tok = NO_TOKEN;
           if (tile >= tile1 || num >= n_tok) return;
-          if (P.slots) {
-            int lo = 0, hi = P.slots;
-            while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (first[mid] <= num) lo = mid; else hi = mid; }
-            tok = base[lo] + num;
+          if (P.slots) {                               // the slot of the list's num-th token, from the tile before's on
+            if (first[min(cur + 4, P.slots)] <= num) {
+              int lo = cur + 4, hi = P.slots;
+              while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (first[mid] <= num) lo = mid; else hi = mid; }
+              cur = lo;
+            } else {
+              while (first[cur + 1] <= num) ++cur;
+            }
+            tok = base[cur] + num;
           } else {
             tok = s.tok0 + num;
           }
-          page = __ldg(s.pages + tok / P.page_tokens);
+          col = P.page_shift >= 0 ? tok >> P.page_shift : tok / P.page_tokens;
+          page = __ldg(s.pages + col);
         };
         auto find = [&](int tile) -> Where {
           Where at{-1, 0, 0};
@@ -510,23 +563,18 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           if (tok != NO_TOKEN) {
             if (page >= 0 && page < P.num_pages) {
               at.page = page;
-              at.place = tok - tok / P.page_tokens * P.page_tokens;
+              at.place = tok - col * P.page_tokens;
             } else {
               tok = NO_TOKEN;
               if (P.status) atomicOr(P.status, RR_STATUS_BAD_INDEX);
             }
           }
-          // the longest run of tokens that every aligned run of the warp's 32 places holds
-#pragma unroll
-          for (int run = 32, i = 1; run >= 8; run >>= 1, ++i) {
-            const int from = lane & ~(run - 1);
-            const int page0 = __shfl_sync(FULL, at.page, from), place0 = __shfl_sync(FULL, at.place, from);
-            const bool in = at.page >= 0 && page0 == at.page && place0 + lane - from == at.place;
-            const bool all = __all_sync(FULL, in);
-            if (at.box == 0 && all) at.box = i;
-          }
-          const int top = __reduce_max_sync(FULL, tok), after = __shfl_down_sync(FULL, tok, 1), last = __shfl_sync(FULL, tok, 31);
-          const bool ascend = __all_sync(FULL, lane == 31 || tok <= after);
+          // the longest runs (32, 16, 8 tokens of a page) that the warp's places, in groups of as many, hold; whether ids ascend
+          const int page_up = __shfl_up_sync(FULL, at.page, 1), place_up = __shfl_up_sync(FULL, at.place, 1), tok_up = __shfl_up_sync(FULL, tok, 1);
+          const unsigned breaks = __ballot_sync(FULL, page_up != at.page || place_up + 1 != at.place);
+          const bool all = __all_sync(FULL, at.page >= 0), ascend = __all_sync(FULL, lane == 0 || tok_up <= tok);
+          const int last = __shfl_sync(FULL, tok, 31), top = ascend ? last : __reduce_max_sync(FULL, tok);
+          if (all) at.box = !(breaks & ~1u) ? 1 : !(breaks & ~0x00010001u) ? 2 : !(breaks & ~0x01010101u) ? 3 : 0;
           c->ids[cnt % IDS][w * 32 + lane] = tok;
           if (lane == 0) c->info[cnt % IDS][w] = make_int4(top, tok, last, ascend);
           __syncwarp();
@@ -595,8 +643,9 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->full[f % S::STAGES], f / S::STAGES & 1); ++it) __nanosleep(64);
       __syncwarp();
     } else {
-      // ===== products: warp 8 those of stream 0, warp 11 those of stream 1, so that one's waits stand beside the other's products =====
-      constexpr uint32_t idesc_s = umma_idesc_bf16(TILE, TILE), idesc_o = idesc_b_mn(TILE, D);
+      // ===== products: warp 8 those of stream 0, warp 11 those of stream 1, so that one's waits
+      // stand beside the other's products =====
+      constexpr uint32_t idesc_s = umma_idesc_bf16(TILE, 64), idesc_o = idesc_b_mn(TILE, D);
       const int st = warp == 8 ? 0 : 1;
       const uint32_t s_tm = tmem + st * 128, o_tm = tmem + 256 + st * 128;
       int place = 0;
@@ -613,49 +662,52 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         const int at = (place + (paired ? st : 0)) & 1;
         ok = wait(&c->q_full[at], (place + (paired ? st : 0)) >> 1);
         const uint64_t qd = umma_desc_k_sw128(q_addr + at * S::TILE_BYTES);
+        // Half a tile (64 tokens) has its own columns of S: while one half's weights are made, the other half's logits are there
+        // or under way.  Logits of a tile's half stand behind the product with the weights of the same half of the tile before, which
+        // reads the same columns; the tensor pipe keeps that order.
         for (int k = 0; ok && k <= steps; ++k) {
-          if (k > 0) {
-            const int tile = paired ? k - 1 : 2 * (k - 1) + st;
-            const uint32_t f = 2 * tiles + (tile == nt - 1 ? 2 * nt - 1 : 2 * tile + 2), stage = f % S::STAGES;
-            ok = wait(&c->full[stage], f / S::STAGES);
-            const uint64_t vd = desc_mn_sw128(kv_addr + stage * S::TILE_BYTES, S::HALF_BYTES);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {              // weights of 64 tokens at a time, as they come
-              ok = ok && wait(&c->p_full[st][h], p_cnt);
+          const int tv = paired ? k - 1 : 2 * (k - 1) + st, tk = paired ? k : 2 * k + st;
+          const uint32_t fv = 2 * tiles + (tv == nt - 1 ? 2 * nt - 1 : 2 * tv + 2), fk = 2 * tiles + (tk == 0 ? 0 : 2 * tk - 1);
+          const uint32_t sv = fv % S::STAGES, sk = fk % S::STAGES;
+          if (k > 0) ok = wait(&c->full[sv], fv / S::STAGES);
+          for (int h = 0; ok && h < 2; ++h) {
+            if (k > 0) {
+              ok = wait(&c->p_full[st][h], p_cnt);
               if (!ok) break;
               tc_fence_after();
+              const uint64_t vd = desc_mn_sw128(kv_addr + sv * S::TILE_BYTES + h * 64 * 128, S::HALF_BYTES);
 #pragma unroll
-              for (int j = h * 4; j < h * 4 + 4; ++j)
-                umma_bf16_ts_warp(o_tm, s_tm + j * 8, vd + (uint64_t)(j * 128), idesc_o, (k > 1 || j > 0) ? 1u : 0u);
+              for (int j = 0; j < 4; ++j)
+                umma_bf16_ts_warp(o_tm, s_tm + h * 64 + j * 8, vd + (uint64_t)(j * 128), idesc_o, (k > 1 || h > 0 || j > 0) ? 1u : 0u);
+              umma_commit_warp(&c->o_done[st][h]);
             }
-            if (!ok) break;
+            if (k < steps) {
+              if (h == 0) { ok = wait(&c->full[sk], fk / S::STAGES); if (!ok) break; tc_fence_after(); }
+              const uint64_t kd = umma_desc_k_sw128(kv_addr + sk * S::TILE_BYTES + h * 64 * 128);
+#pragma unroll
+              for (int j = 0; j < D / 16; ++j) {
+                const uint64_t o = (uint64_t)((j >> 2) * (S::HALF_BYTES >> 4) + (j & 3) * 2);
+                umma_bf16_warp(s_tm + h * 64, qd + o, kd + o, idesc_s, j > 0 ? 1u : 0u);
+              }
+              umma_commit_warp(&c->s_full[st][h]);
+            }
+          }
+          if (!ok) break;
+          if (k > 0) {
             ++p_cnt;
-            umma_commit_warp(&c->empty[stage]);
-            if (!paired) umma_commit_warp(&c->empty[stage]);
+            umma_commit_warp(&c->empty[sv]);
+            if (!paired) umma_commit_warp(&c->empty[sv]);
           }
           if (k < steps) {
-            const int tile = paired ? k : 2 * k + st;
-            const uint32_t f = 2 * tiles + (tile == 0 ? 0 : 2 * tile - 1), stage = f % S::STAGES;
-            ok = wait(&c->full[stage], f / S::STAGES);
-            if (!ok) break;
-            tc_fence_after();
-            const uint64_t kd = umma_desc_k_sw128(kv_addr + stage * S::TILE_BYTES);
-#pragma unroll
-            for (int j = 0; j < D / 16; ++j) {
-              const uint64_t o = (uint64_t)((j >> 2) * (S::HALF_BYTES >> 4) + (j & 3) * 2);
-              umma_bf16_warp(s_tm, qd + o, kd + o, idesc_s, j > 0 ? 1u : 0u);
-            }
-            umma_commit_warp(&c->s_full[st]);
-            umma_commit_warp(&c->empty[stage]);
-            if (!paired) umma_commit_warp(&c->empty[stage]);
+            umma_commit_warp(&c->empty[sk]);
+            if (!paired) umma_commit_warp(&c->empty[sk]);
           }
-          if (k + 1 == steps || steps == 0) {          // the queries' place: both streams of a split segment have to be done with it
+          if (k == max(steps - 1, 0)) {                // the queries' place: both streams of a split segment have to be done with it
             umma_commit_warp(&c->q_empty[at]);
             if (paired) umma_commit_warp(&c->q_empty[at]);
           }
         }
         if (!ok) break;
-        if (steps > 0) umma_commit_warp(&c->o_full[st]);
         tiles += nt;
         place += paired ? 2 : 1;
         seg_done(n);
