@@ -147,12 +147,13 @@ def lib() -> C.CDLL:
                      "rr_bucket_set_count", "rr_bucket_set_info", "rr_bucket_set_reset",
                      "rr_bucket_route_layer", "rr_bucket_set_status", "rr_attend_token_ranges"):
             getattr(L, name).restype = C.c_int
-        kvp, szp = C.POINTER(rr_paged_kv), C.POINTER(sz)
-        L.rr_kv_append.argtypes = [kvp, C.POINTER(rr_append_args), vp]
-        L.rr_attend_shared_workspace.argtypes = [kvp, C.POINTER(rr_shared_args), szp]
-        L.rr_attend_shared.argtypes = [kvp, C.POINTER(rr_shared_args), vp, sz, vp]
-        L.rr_attend_paged_ranges_workspace.argtypes = [kvp, C.POINTER(rr_ranges_args), szp]
-        L.rr_attend_paged_ranges.argtypes = [kvp, C.POINTER(rr_ranges_args), vp, sz, vp]
+        # (descriptions as addresses or bytes: the callers in paged.py pack them)
+        szp = C.POINTER(sz)
+        L.rr_kv_append.argtypes = [vp, vp, vp]
+        L.rr_attend_shared_workspace.argtypes = [vp, vp, szp]
+        L.rr_attend_shared.argtypes = [vp, vp, vp, sz, vp]
+        L.rr_attend_paged_ranges_workspace.argtypes = [vp, vp, szp]
+        L.rr_attend_paged_ranges.argtypes = [vp, vp, vp, sz, vp]
         for name in ("rr_kv_append", "rr_attend_shared_workspace", "rr_attend_shared",
                      "rr_attend_paged_ranges_workspace", "rr_attend_paged_ranges"):
             getattr(L, name).restype = C.c_int

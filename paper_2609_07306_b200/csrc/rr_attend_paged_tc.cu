@@ -37,7 +37,7 @@ namespace {
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int NT = 512, IDS = 16, MAX_RING = 4;
 constexpr float GROWTH = 8.f;
-constexpr int BY_FMA = 2;                              // of every 8 pairs of exponentials, by multiply-adds
+constexpr int BY_FMA = 1;                              // of every 8 pairs of exponentials, by multiply-adds
 
 template <int D> struct Shape {
   static constexpr int HALVES = D / 64, STAGES = D == 128 ? 4 : 8;
@@ -228,7 +228,10 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
       bool seen = false, mixed = false;
       for (int k = 0; ok && k < 2 * steps; ++k) {      // half a tile, 64 tokens, at a time
         const int h = k & 1, cnt = tiles + (paired ? k >> 1 : (k & ~1) + st);
-        ok = __all_sync(FULL, mbar_wait(&c->ids_full[cnt % IDS], cnt / IDS & 1, abort_flag) && mbar_wait(&c->s_full[st][h], s_cnt & 1, abort_flag));
+        if (h == 0) ok = __all_sync(FULL, mbar_wait(&c->ids_full[cnt % IDS], cnt / IDS & 1, abort_flag));
+        const int4 i0 = c->info[cnt % IDS][2 * h], i1 = c->info[cnt % IDS][2 * h + 1];
+        const bool masked = __any_sync(FULL, live && max(i0.x, i1.x) >= limit);
+        ok = ok && __all_sync(FULL, mbar_wait(&c->s_full[st][h], s_cnt & 1, abort_flag));
         if (!ok) break;
         s_cnt += h;
         tc_fence_after();
@@ -239,8 +242,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < 2; ++i) tie(x[i]);
-          const int4 i0 = c->info[cnt % IDS][2 * h], i1 = c->info[cnt % IDS][2 * h + 1];
-          if (!__any_sync(FULL, live && max(i0.x, i1.x) >= limit)) {
+          if (!masked) {
             seen = true;
           } else {                                     // which columns the row sees, a bit each
             uint32_t see[2] = {0, 0};

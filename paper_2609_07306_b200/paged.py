@@ -3,10 +3,17 @@ with the position rotation, attention of a batch that shares a prefix, attention
 operator runs in the library's kernels; PyTorch is used for device memory and streams only."""
 from __future__ import annotations
 
+import ctypes as C
+import struct
+
 import torch
 
 from . import binding as B
-from .ledger import _raw_stream
+
+# rr_append_args, rr_shared_args and rr_ranges_args as bytes (a call's arguments in one step; 64-bit alignment throughout)
+_APPEND = struct.Struct("@8P8q4i")
+_SHARED = struct.Struct("@5P4q4if4x")
+_RANGES = struct.Struct("@4P6q6if4x")
 
 _DTYPES = {torch.bfloat16: B.RR_BF16, torch.float32: B.RR_F32}
 
@@ -46,55 +53,70 @@ class PagedKV:
             raise ValueError("the entries of a head must be contiguous")
         self.k_cache, self.v_cache, self.page_table, self.status = k_cache, v_cache, page_table, status
         self.device = k_cache.device
-        self._need(page_table, "page_table", torch.int32, 2)
-        if page_table.shape[1] > 1 and page_table.stride(1) != 1:
-            raise ValueError("the rows of page_table must be contiguous")
-        self._need(v_cache, "v_cache", k_cache.dtype, 4)
-        if status is not None:
-            self._need(status, "status", torch.int32, 1, (1,))
+        if self.device.type != "cuda":
+            raise ValueError("the cache must be on a CUDA device (there is no CPU path)")
+        self._index, self._dtype = self.device.index, k_cache.dtype
         self.batch = page_table.shape[0]
-        pages, self.kv_heads, page_tokens, self.dh = k_cache.shape
+        pages, self.kv_heads, self.page_tokens, self.dh = k_cache.shape
+        if v_cache.device != self.device:
+            raise ValueError(f"v_cache is on {v_cache.device}, the cache on {self.device}")
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be [batch, pages_per_seq]")
+        self._ints(page_table, "page_table", tuple(page_table.shape), rows_apart=True)
+        if status is not None:
+            self._ints(status, "status", (1,))
         self._kv = B.rr_paged_kv(
             k=k_cache.data_ptr(), v=v_cache.data_ptr(), page_table=page_table.data_ptr(), status=_ptr(status),
             page_stride=k_cache.stride(0), head_stride=k_cache.stride(1), token_stride=k_cache.stride(2),
             table_stride=page_table.stride(0), dtype=_DTYPES[k_cache.dtype], num_pages=pages,
-            page_tokens=page_tokens, kv_heads=self.kv_heads, dh=self.dh, batch=self.batch,
+            page_tokens=self.page_tokens, kv_heads=self.kv_heads, dh=self.dh, batch=self.batch,
             pages_per_seq=page_table.shape[1])
+        self._at = C.addressof(self._kv)
+        self._lib = B.lib()
 
-    def _need(self, t, name, dtype, dim, shape=None):
+    # -- checks: one comparison each for what is right, the reason where it is not ----------------------------
+    def _heads(self, t, name, shape):
+        """t has the cache's type and device, the given shape (its last entry dh), contiguous heads."""
+        if t.dtype is self._dtype and t.get_device() == self._index and t.shape == shape and t.stride(-1) == 1:
+            return
         if t.device != self.device:
             raise ValueError(f"{name} is on {t.device}, the cache on {self.device}")
-        if t.dtype != dtype:
-            raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-        if t.dim() != dim or (shape is not None and tuple(t.shape) != tuple(shape)):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}" + (f", expected {tuple(shape)}" if shape is not None else ""))
-
-    def _heads(self, t, name, dim, shape=None):
-        self._need(t, name, self.k_cache.dtype, dim, shape)
-        if t.shape[-1] != self.dh:
-            raise ValueError(f"{name} has heads of {t.shape[-1]} entries, the cache of {self.dh}")
-        if self.dh > 1 and t.stride(-1) != 1:
+        if t.dtype is not self._dtype:
+            raise TypeError(f"{name} must be {self._dtype}, not {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if self.dh > 1 and t.numel() > 0:
             raise ValueError(f"the entries of a head of {name} must be contiguous")
 
-    def _ints(self, t, name, shape):
-        self._need(t, name, torch.int32, len(shape), shape)
-        if not t.is_contiguous():
+    def _ints(self, t, name, shape, rows_apart=False):
+        if t.dtype is torch.int32 and t.get_device() == self._index and t.shape == shape and t.is_contiguous():
+            return
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the cache on {self.device}")
+        if t.dtype is not torch.int32:
+            raise TypeError(f"{name} must be torch.int32, not {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if not (rows_apart and (t.shape[1] <= 1 or t.stride(1) == 1)):
             raise ValueError(f"{name} must be contiguous")
 
-    def _launch(self, fn, workspace_bytes, args):
-        if self.device.index == torch.cuda.current_device():
-            return self._launch_here(fn, workspace_bytes, args)
-        with torch.cuda.device(self.device):
-            return self._launch_here(fn, workspace_bytes, args)
-
-    def _launch_here(self, fn, workspace_bytes, args):
-        stream = _raw_stream(self.device)
-        if workspace_bytes is None:
-            fn(self._kv, args, stream)
-            return
-        n = workspace_bytes(self._kv, args)
-        ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
-        fn(self._kv, args, _ptr(ws), n, stream)
+    def _run(self, name, args, workspace=None):
+        """One library call on the current stream of the cache's device."""
+        if self._index != torch.cuda.current_device():
+            with torch.cuda.device(self.device):
+                return self._run(name, args, workspace)
+        stream = torch._C._cuda_getCurrentRawStream(self._index)
+        if workspace is None:
+            rc = getattr(self._lib, name)(self._at, args, stream)
+        else:
+            n = C.c_size_t()
+            rc = getattr(self._lib, workspace)(self._at, args, C.byref(n))
+            if rc == B.RR_OK:
+                n = n.value
+                ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+                rc = getattr(self._lib, name)(self._at, args, _ptr(ws), n, stream)
+        if rc != B.RR_OK:
+            raise B.RouteRelayError(rc, name)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, *, cu: torch.Tensor | None = None,
                q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
@@ -109,43 +131,44 @@ class PagedKV:
         inv_freq  [rot / 2] float32, rotates the first rot entries of a head: the pairs (j, j + rot / 2), or with
                   interleaved=True (2 j, 2 j + 1); None: nothing is rotated
         new_lens  [batch] int32: gets lens + new tokens (another tensor than lens)"""
-        self._heads(k, "k", 3, (k.shape[0], self.kv_heads, self.dh))
-        self._heads(v, "v", 3, k.shape)
+        if k.dim() != 3:
+            raise ValueError("k must be [tokens, kv_heads, dh]")
+        n = k.shape[0]
+        shape = (n, self.kv_heads, self.dh)
+        self._heads(k, "k", shape)
+        self._heads(v, "v", shape)
         self._ints(lens, "lens", (self.batch,))
         if cu is not None:
             self._ints(cu, "cu", (self.batch + 1,))
         if new_lens is not None:
             self._ints(new_lens, "new_lens", (self.batch,))
+        rot = 0
         if inv_freq is not None:
-            self._need(inv_freq, "inv_freq", torch.float32, 1)
-            if not inv_freq.is_contiguous():
-                raise ValueError("inv_freq must be contiguous")
+            if inv_freq.dtype is not torch.float32 or inv_freq.get_device() != self._index or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+                raise ValueError(f"inv_freq must be contiguous float32 [rot / 2] on {self.device}")
+            rot = 2 * inv_freq.shape[0]
+        heads, q_strides = 0, (0, 0, 0, 0)
         if q is not None:
-            self._heads(q, "q", 3, (k.shape[0], q.shape[1], self.dh))
+            if q.dim() != 3:
+                raise ValueError("q must be [tokens, heads, dh]")
+            shape = (n, q.shape[1], self.dh)
+            self._heads(q, "q", shape)
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+                q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
             else:
-                self._heads(q_out, "q_out", 3, q.shape)
+                self._heads(q_out, "q_out", shape)
+            heads, q_strides = shape[1], (q.stride(0), q.stride(1), q_out.stride(0), q_out.stride(1))
         elif q_out is not None:
             raise ValueError("q_out without q")
-        if k.shape[0] == 0:
-            k = v = self.k_cache                                       # (an empty tensor has no address)
-            args = B.rr_append_args()
-            q_in = None
-        else:
-            q_in = q
-            args = B.rr_append_args(k_token_stride=k.stride(0), k_head_stride=k.stride(1),
-                                    v_token_stride=v.stride(0), v_head_stride=v.stride(1), tokens=k.shape[0])
-        args.k, args.v, args.lens = k.data_ptr(), v.data_ptr(), lens.data_ptr()
-        args.cu, args.new_lens = _ptr(cu), _ptr(new_lens)
-        if inv_freq is not None:
-            args.inv_freq, args.rot = inv_freq.data_ptr(), 2 * inv_freq.shape[0]
-        args.interleaved = 1 if interleaved else 0
-        if q_in is not None:
-            args.q, args.q_out, args.q_heads = q.data_ptr(), q_out.data_ptr(), q.shape[1]
-            args.q_token_stride, args.q_head_stride = q.stride(0), q.stride(1)
-            args.out_token_stride, args.out_head_stride = q_out.stride(0), q_out.stride(1)
-        self._launch(B.rr_kv_append, None, args)
+        if n == 0:                                     # (an empty tensor has no address)
+            if cu is None:
+                raise ValueError(f"no tokens for {self.batch} sequences")
+            k, v, heads = self.k_cache, self.v_cache, 0
+        self._run("rr_kv_append", _APPEND.pack(
+            k.data_ptr(), v.data_ptr(), q.data_ptr() if heads else 0, q_out.data_ptr() if heads else 0, lens.data_ptr(),
+            0 if cu is None else cu.data_ptr(), 0 if new_lens is None else new_lens.data_ptr(),
+            0 if rot == 0 else inv_freq.data_ptr(), k.stride(0), k.stride(1), v.stride(0), v.stride(1), *q_strides, n, heads, rot,
+            1 if interleaved else 0))
         return q_out
 
     def attend_shared(self, q: torch.Tensor, lens: torch.Tensor, prefix_tokens: int, scale: float, *,
@@ -158,27 +181,27 @@ class PagedKV:
         causal  the queries are their sequence's last tokens, and none sees a token behind its own; False: every query
                 sees all lens[b] tokens (attention to states of another length, e.g. an encoder's)
         A query without tokens gets zeros."""
-        self._heads(q, "q", 3)
+        if q.dim() != 3:
+            raise ValueError("q must be [tokens, heads, dh]")
+        shape = (q.shape[0], q.shape[1], self.dh)
+        self._heads(q, "q", shape)
         self._ints(lens, "lens", (self.batch,))
         if cu is not None:
             self._ints(cu, "cu", (self.batch + 1,))
         if prefix_pages is not None:
-            page = self.k_cache.shape[2]
-            self._ints(prefix_pages, "prefix_pages", prefix_pages.shape[:1])
-            if prefix_pages.shape[0] * page < prefix_tokens:
+            self._ints(prefix_pages, "prefix_pages", tuple(prefix_pages.shape[:1]))
+            if prefix_pages.shape[0] * self.page_tokens < prefix_tokens:
                 raise ValueError(f"prefix_pages holds {prefix_pages.shape[0]} pages, {prefix_tokens} tokens need more")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
         else:
-            self._heads(out, "out", 3, q.shape)
-        if q.shape[0] == 0 and (cu is not None or self.batch == 0):
+            self._heads(out, "out", shape)
+        if shape[0] == 0 and cu is not None:
             return out
-        args = B.rr_shared_args(
-            q=q.data_ptr(), out=out.data_ptr(), lens=lens.data_ptr(), cu=_ptr(cu), prefix_pages=_ptr(prefix_pages),
-            q_token_stride=q.stride(0), q_head_stride=q.stride(1), out_token_stride=out.stride(0),
-            out_head_stride=out.stride(1), tokens=q.shape[0], heads=q.shape[1], prefix_tokens=prefix_tokens,
-            causal=1 if causal else 0, scale=scale)
-        self._launch(B.rr_attend_shared, B.rr_attend_shared_workspace, args)
+        self._run("rr_attend_shared", _SHARED.pack(
+            q.data_ptr(), out.data_ptr(), lens.data_ptr(), 0 if cu is None else cu.data_ptr(),
+            0 if prefix_pages is None else prefix_pages.data_ptr(), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
+            shape[0], shape[1], prefix_tokens, 1 if causal else 0, scale), "rr_attend_shared_workspace")
         return out
 
     def attend_ranges(self, q: torch.Tensor, ranges: torch.Tensor, lens: torch.Tensor, n_q: int, scale: float, *,
@@ -189,24 +212,23 @@ class PagedKV:
         lens    [batch] int32 tokens in the cache: range tokens from there on are left out
         causal  the query tokens are the sequence's last n_q * m, and none sees a token behind its own
         A query without tokens gets zeros."""
-        self._heads(q, "q", 4)
+        if q.dim() != 4:
+            raise ValueError("q must be [batch, heads, n_q * m, dh]")
+        shape = (self.batch, q.shape[1], q.shape[2], self.dh)
+        self._heads(q, "q", shape)
         self._ints(lens, "lens", (self.batch,))
-        self._need(ranges, "ranges", torch.int32, 3)
-        if not ranges.is_contiguous() or ranges.shape[2] != 2:
-            raise ValueError("ranges must be contiguous [rows, slots, 2]")
-        if q.shape[0] != self.batch or n_q < 1 or q.shape[2] % n_q != 0:
-            raise ValueError(f"q has shape {tuple(q.shape)}, expected [{self.batch}, heads, {n_q} * m, {self.dh}]")
-        if ranges.shape[0] == 0 or ranges.shape[0] % (self.batch * n_q) != 0:
-            raise ValueError(f"ranges has {ranges.shape[0]} rows, not a multiple of batch * n_q = {self.batch * n_q}")
+        if ranges.dim() != 3:
+            raise ValueError("ranges must be [rows, slots, 2]")
+        rows, slots = ranges.shape[0], ranges.shape[1]
+        self._ints(ranges, "ranges", (rows, slots, 2))
+        if n_q < 1 or shape[2] % n_q != 0 or rows == 0 or rows % (self.batch * n_q) != 0:
+            raise ValueError(f"{rows} range rows and {shape[2]} query tokens do not make {n_q} chunks of {self.batch} sequences")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
         else:
-            self._heads(out, "out", 4, q.shape)
-        args = B.rr_ranges_args(
-            q=q.data_ptr(), out=out.data_ptr(), ranges=ranges.data_ptr(), lens=lens.data_ptr(),
-            q_batch_stride=q.stride(0), q_head_stride=q.stride(1), q_token_stride=q.stride(2),
-            out_batch_stride=out.stride(0), out_head_stride=out.stride(1), out_token_stride=out.stride(2),
-            heads=q.shape[1], route_heads=ranges.shape[0] // (self.batch * n_q), n_q=n_q, m=q.shape[2] // n_q,
-            slots=ranges.shape[1], causal=1 if causal else 0, scale=scale)
-        self._launch(B.rr_attend_paged_ranges, B.rr_attend_paged_ranges_workspace, args)
+            self._heads(out, "out", shape)
+        self._run("rr_attend_paged_ranges", _RANGES.pack(
+            q.data_ptr(), out.data_ptr(), ranges.data_ptr(), lens.data_ptr(), q.stride(0), q.stride(1), q.stride(2), out.stride(0),
+            out.stride(1), out.stride(2), shape[1], rows // (self.batch * n_q), n_q, shape[2] // n_q, slots, 1 if causal else 0,
+            scale), "rr_attend_paged_ranges_workspace")
         return out

@@ -55,6 +55,16 @@ def test_structs_match_the_header(name):
     assert want == [(n, C.sizeof(t)) for n, t in getattr(B, name)._fields_]
 
 
+def test_packed_arguments_match_the_structs():
+    from paper_2609_07306_b200 import paged
+    for packed, st in ((paged._APPEND, B.rr_append_args), (paged._SHARED, B.rr_shared_args), (paged._RANGES, B.rr_ranges_args)):
+        assert packed.size == C.sizeof(st)
+        n = len(st._fields_)
+        vals = [i + 1 for i in range(n)]
+        x = st.from_buffer_copy(packed.pack(*vals))
+        assert [getattr(x, f) for f, _ in st._fields_] == vals
+
+
 CACHE = [(dict(k=None), B.RR_ERR_INVALID_ARG), (dict(v=None), B.RR_ERR_INVALID_ARG), (dict(page_table=None), B.RR_ERR_INVALID_ARG),
          (dict(num_pages=0), B.RR_ERR_INVALID_ARG), (dict(page_tokens=0), B.RR_ERR_INVALID_ARG), (dict(kv_heads=0), B.RR_ERR_INVALID_ARG),
          (dict(batch=0), B.RR_ERR_INVALID_ARG), (dict(pages_per_seq=0), B.RR_ERR_INVALID_ARG), (dict(page_stride=-1), B.RR_ERR_INVALID_ARG),
