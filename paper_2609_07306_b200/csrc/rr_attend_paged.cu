@@ -147,10 +147,16 @@ constexpr int BT = 64, SNT = 256;
 
 __host__ __device__ constexpr int padded(int dh) { return (dh + 3) / 4 * 4 + 4; }
 struct SmemPlan { int q, kv, p, ids, slots, total; };
-__host__ __device__ inline SmemPlan smem_plan(int dh, int n_slots) {
+__host__ __device__ inline SmemPlan smem_plan(int dh, int n_slots, bool only_few) {
   SmemPlan s;
   const int row = padded(dh) * 4;
-  s.q = 0;
+  s.q = 0;                                             // (few rows: the warps' parts of 4 rows from here on)
+  if (only_few) {
+    s.kv = s.p = s.ids = 0;
+    s.slots = SNT / 32 * 4 * ((dh <= 64 ? 64 : dh <= 128 ? 128 : 256) * 4 + 8);
+    s.total = s.slots + (2 * n_slots + 1) * 4;
+    return s;
+  }
   s.kv = s.q + 64 * row;
   s.p = s.kv + BT * row;
   s.ids = s.p + 64 * (BT + 4) * 4;
@@ -365,13 +371,168 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
   }
 }
 
-template <typename T, int NV>
-__global__ void __launch_bounds__(SNT) attend_simt_kernel(const __grid_constant__ Params P, bool vq, bool vk) {
+// Up to FEW rows: nothing to share but the loads, so no tiles.  A warp takes 16 loads of 32 lanes x 4 entries at a time (32 tokens of up
+// to 64 entries, 16 tokens of more), all in flight at once, for R rows: the dot products' halves are exchanged so that a lane is left with one
+// token's logit (15 or 16 exchanges for 16 loads), and its weight goes back to the token's lanes for the values.  A
+// token that a row does not see is not multiplied, so nothing needs repair.  The eight warps' parts are joined at the end.
+// Bound by the cache's traffic (one query per row: through L2).
+constexpr int FEW = 8;
+
+template <typename T, int LPT, int W, int R>      // LPT lanes x W groups of 4 entries per token
+__device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, float* s_part) {
+  constexpr int TP = 32 / LPT, BLOCK = 16 * TP, ROW = LPT * W * 4;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane % LPT, grp = lane / LPT, dh = P.dh;
+  float4 q[R][W], acc[R][W];
+  int limit[R];
+  float m[R], l[R];
+  bool seen[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const bool live = r0 + r < s.rows;
+    const RowAt a = live ? row_at(P, s, r0 + r) : RowAt{0, 0, 0};
+    limit[r] = a.limit; m[r] = NINF; l[r] = 0.f; seen[r] = false;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const int e = (sub + LPT * w) * 4;
+      q[r][w] = live && e < dh ? load4<T>((const T*)P.q + q_at(P, s, a) + e, c.vq, dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
+      acc[r][w] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  const int end = min(s.tile1 * TILE, c.n_tok);
+  for (int num0 = s.tile0 * TILE + warp * BLOCK; num0 < end; num0 += SNT / 32 * BLOCK) {
+    const int num = num0 + lane;
+    int id = NO_TOKEN;
+    long long at = -1;
+    if (lane < BLOCK && num < end) {
+      if (s.slots) {
+        int lo = 0, hi = P.slots;
+        while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (c.first[mid] <= num) lo = mid; else hi = mid; }
+        id = c.base[lo] + num;
+      } else {
+        id = s.tok0 + num;
+      }
+      at = token_at(P, s, id);
+      if (at < 0) id = NO_TOKEN;
+    }
+    float4 x[16];
+    auto load = [&](const void* from, int w) {
+      const int e = (sub + LPT * w) * 4;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const long long o = __shfl_sync(FULL, at, i * TP + grp);
+        x[i] = o >= 0 && e < dh ? load4<T>((const T*)from + o + e, c.vk, dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    };
+    // lane's token: LPT 16: load `sub` of its half of the warp, LPT 32: load lane / 2
+    const int mine = LPT == 16 ? sub * TP + grp : lane >> 1, my_id = __shfl_sync(FULL, id, mine);
+    float wt[R];
+    unsigned sees[R];
+    if (W == 1) load(P.k, 0);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float d[16];
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        if (W > 1) load(P.k, w);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          d[i] = fmaf(q[r][w].w, x[i].w, fmaf(q[r][w].z, x[i].z, fmaf(q[r][w].y, x[i].y, fmaf(q[r][w].x, x[i].x, w ? d[i] : 0.f))));
+      }
+#pragma unroll
+      for (int n = 8, off = LPT / 2; n >= 1; n >>= 1, off >>= 1) {
+        const bool up = sub & off;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+          const float keep = up ? d[i + n] : d[i], give = up ? d[i] : d[i + n];
+          d[i] = keep + __shfl_xor_sync(FULL, give, off);
+        }
+      }
+      float z = d[0];
+      if (LPT == 32) z += __shfl_xor_sync(FULL, z, 1);
+      const bool see = my_id < limit[r];
+      sees[r] = __ballot_sync(FULL, see);
+      z = see ? z * P.scale_log2 : NINF;
+      float top = z;
+#pragma unroll
+      for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, off));
+      const float m_new = fmaxf(m[r], top), ref = m_new == NINF ? 0.f : m_new, f = exp2f(m[r] - ref);
+      seen[r] = seen[r] || sees[r] != 0;
+      m[r] = m_new;
+      wt[r] = exp2f(z - ref);
+      l[r] = fmaf(l[r], f, LPT == 32 && (lane & 1) ? 0.f : wt[r]);
+#pragma unroll
+      for (int w = 0; w < W; ++w) { acc[r][w].x *= f; acc[r][w].y *= f; acc[r][w].z *= f; acc[r][w].w *= f; }
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      load(P.v, w);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int from = LPT == 16 ? grp * 16 + i : 2 * i;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float u = __shfl_sync(FULL, wt[r], from);
+          if (sees[r] >> from & 1) {
+            acc[r][w].x = fmaf(u, x[i].x, acc[r][w].x); acc[r][w].y = fmaf(u, x[i].y, acc[r][w].y);
+            acc[r][w].z = fmaf(u, x[i].z, acc[r][w].z); acc[r][w].w = fmaf(u, x[i].w, acc[r][w].w);
+          }
+        }
+      }
+    }
+  }
+  // the warp's parts: outputs over the groups of lanes, sums over the lanes; then the warps'
+  __syncthreads();                                     // (what was in this memory has been read)
+  float2* const s_ml = (float2*)(s_part + SNT / 32 * R * ROW);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+#pragma unroll
+    for (int off = 16; off; off >>= 1) l[r] += __shfl_xor_sync(FULL, l[r], off);
+    if (seen[r] && m[r] == NINF) m[r] = LOWEST;
+    if (lane == 0) s_ml[warp * R + r] = make_float2(m[r], l[r]);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if (LPT == 16) {
+        acc[r][w].x += __shfl_xor_sync(FULL, acc[r][w].x, 16); acc[r][w].y += __shfl_xor_sync(FULL, acc[r][w].y, 16);
+        acc[r][w].z += __shfl_xor_sync(FULL, acc[r][w].z, 16); acc[r][w].w += __shfl_xor_sync(FULL, acc[r][w].w, 16);
+      }
+      if (grp == 0) *(float4*)(s_part + (warp * R + r) * ROW + (sub + LPT * w) * 4) = acc[r][w];
+    }
+  }
+  __syncthreads();
+  const int live = min(R, s.rows - r0);
+  for (int u = threadIdx.x; u < live * dh; u += SNT) {
+    const int r = u / dh, e = u - r * dh;
+    float M = NINF, L = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < SNT / 32; ++w) M = fmaxf(M, s_ml[w * R + r].x);
+#pragma unroll
+    for (int w = 0; w < SNT / 32; ++w) {
+      const float2 ml = s_ml[w * R + r];
+      if (ml.x == NINF) continue;
+      const float f = exp2f(ml.x - M);
+      L = fmaf(f, ml.y, L);
+      o = fmaf(f, s_part[(w * R + r) * ROW + e], o);
+    }
+    const long long at = s.part + r0 + r;
+    if (P.direct) {
+      const float inv = L == 0.f ? (M == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / L;
+      ((T*)P.out)[out_at(P, s, row_at(P, s, r0 + r)) + e] = rr_from_f32<T>(o * inv);
+    } else {
+      P.part_o[at * dh + e] = o;
+      if (e == 0) P.part_ml[at] = make_float2(M, L);
+    }
+  }
+  __syncthreads();
+}
+
+// ONLY_FEW: a call whose items all have up to FEW rows needs no tiles in shared memory, and more CTAs fit an SM.
+template <typename T, int NV, bool ONLY_FEW>
+__global__ void __launch_bounds__(SNT, 2) attend_simt_kernel(const __grid_constant__ Params P, bool vq, bool vk) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ uint32_t s_bad[2];
   rr_pdl_wait();
   rr_pdl_trigger();
-  const SmemPlan L = smem_plan(P.dh, P.slots);
+  const SmemPlan L = smem_plan(P.dh, P.slots, ONLY_FEW);
   Ctx c;
   c.q = (float*)(smem + L.q); c.kv = (float*)(smem + L.kv); c.p = (float*)(smem + L.p);
   c.at = (long long*)(smem + L.ids); c.id = (int*)(c.at + BT);
@@ -406,8 +567,13 @@ __global__ void __launch_bounds__(SNT) attend_simt_kernel(const __grid_constant_
       split_tiles(P, (c.n_tok + TILE - 1) / TILE, s);
     } else {
       u += segment_at(P, blockIdx.x, u, u0, u1, s);
+      c.n_tok = s.tok1 - s.tok0;
     }
-    if (s.rows <= 16) rows_block<T, NV, 1>(P, s, c, 0, s_bad);
+    constexpr int LPT = NV == 1 ? 16 : 32, W = NV > 2 ? 2 : 1, R = W == 1 ? 4 : 1;
+    if (ONLY_FEW || s.rows <= FEW) {
+      if (s.rows == 1) few_rows<T, LPT, W, 1>(P, s, c, 0, c.q);
+      else for (int r0 = 0; r0 < s.rows; r0 += R) few_rows<T, LPT, W, R>(P, s, c, r0, c.q);
+    } else if (s.rows <= 16) rows_block<T, NV, 1>(P, s, c, 0, s_bad);
     else for (int r0 = 0; r0 < s.rows; r0 += 64) rows_block<T, NV, 4>(P, s, c, r0, s_bad);
   }
 }
@@ -415,23 +581,28 @@ __global__ void __launch_bounds__(SNT) attend_simt_kernel(const __grid_constant_
 // ---- host ----------------------------------------------------------------------------------------------------
 template <typename T>
 cudaError_t launch_simt(const Params& P, int grid, cudaStream_t st) {
-  const SmemPlan L = smem_plan(P.dh, P.slots);
+  const bool few = P.slots && P.m * P.group <= FEW;
+  const SmemPlan L = smem_plan(P.dh, P.slots, few);
   const uintptr_t b = 4 * sizeof(T) - 1;
   const bool vq = P.dh % 4 == 0 && ((uintptr_t)P.q & b) == 0 && (P.qb | P.qh | P.qt) % 4 == 0;
   const bool vk = P.dh % 4 == 0 && (((uintptr_t)P.k | (uintptr_t)P.v) & b) == 0 && (P.page_stride | P.head_stride | P.token_stride) % 4 == 0;
   auto go = [&](auto kernel, unsigned long long& done) {
     cudaError_t e = rr_once_per_device(done, [&] {
-      return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_plan(RR_PAGED_MAX_DH, RR_MAX_RANGE_SLOTS).total);
+      return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_plan(RR_PAGED_MAX_DH, RR_MAX_RANGE_SLOTS, false).total);
     });
     if (e != cudaSuccess) return e;
     return rr_launch_pdl(kernel, grid, SNT, (size_t)L.total, st, P, vq, vk);
   };
-  static unsigned long long done[4];
-  switch ((P.dh + 63) / 64) {
-    case 1: return go(attend_simt_kernel<T, 1>, done[0]);
-    case 2: return go(attend_simt_kernel<T, 2>, done[1]);
-    case 3: return go(attend_simt_kernel<T, 3>, done[2]);
-    default: return go(attend_simt_kernel<T, 4>, done[3]);
+  static unsigned long long done[8];
+  switch ((P.dh + 63) / 64 + (few ? 4 : 0)) {
+    case 1: return go(attend_simt_kernel<T, 1, false>, done[0]);
+    case 2: return go(attend_simt_kernel<T, 2, false>, done[1]);
+    case 3: return go(attend_simt_kernel<T, 3, false>, done[2]);
+    case 4: return go(attend_simt_kernel<T, 4, false>, done[3]);
+    case 5: return go(attend_simt_kernel<T, 1, true>, done[4]);
+    case 6: return go(attend_simt_kernel<T, 2, true>, done[5]);
+    case 7: return go(attend_simt_kernel<T, 3, true>, done[6]);
+    default: return go(attend_simt_kernel<T, 4, true>, done[7]);
   }
 }
 
@@ -514,7 +685,7 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.range_rows = (long long)kv->batch * a->route_heads * a->n_q;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
   P.streams = P.tc ? 2 : 1;
-  P.ctas = rr_sm_count() * (P.tc ? 1 : 2);
+  P.ctas = rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 3 : 2);
   // few rows: each is cut into parts, so that every SM has one
   const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS);
   P.splits = (int)(items >= P.ctas ? 1 : ceil_div(P.ctas, items));
