@@ -153,7 +153,7 @@ __host__ __device__ inline SmemPlan smem_plan(int dh, int n_slots, bool only_few
   s.q = 0;                                             // (few rows: the warps' parts of 4 rows from here on)
   if (only_few) {
     s.kv = s.p = s.ids = 0;
-    s.slots = SNT / 32 * 4 * ((dh <= 64 ? 64 : dh <= 128 ? 128 : 256) * 4 + 8);
+    s.slots = 4 * 4 * ((dh <= 64 ? 64 : dh <= 128 ? 128 : 256) * 4 + 8);
     s.total = s.slots + (2 * n_slots + 1) * 4;
     return s;
   }
@@ -371,16 +371,16 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
   }
 }
 
-// Up to FEW rows: nothing to share but the loads, so no tiles.  A warp takes 16 loads of 32 lanes x 4 entries at a time (32 tokens of up
-// to 64 entries, 16 tokens of more), all in flight at once, for R rows: the dot products' halves are exchanged so that a lane is left with one
-// token's logit (15 or 16 exchanges for 16 loads), and its weight goes back to the token's lanes for the values.  A
-// token that a row does not see is not multiplied, so nothing needs repair.  The eight warps' parts are joined at the end.
-// Bound by the cache's traffic (one query per row: through L2).
+// Up to FEW rows: nothing to share but the loads, so no tiles.  A warp takes 8 loads of keys and 8 of values at a time, of 32 lanes
+// x 4 entries (16 tokens of up to 64 entries, 8 tokens of more), all in flight at once behind the next ones' page look-up, for R rows: the
+// dot products' halves are exchanged until a token's logit is left in LPT / 8 lanes, and its weight goes back to the
+// token's lanes for the values.  A token that a row does not see is not multiplied, so nothing needs repair.  The warps' parts
+// are joined at the end.  Bound by the cache's traffic (one query per row: through L2) and by latency.
 constexpr int FEW = 8;
 
-template <typename T, int LPT, int W, int R>      // LPT lanes x W groups of 4 entries per token
+template <typename T, int LPT, int W, int R, int WARPS>      // LPT lanes x W groups of 4 entries per token
 __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, float* s_part) {
-  constexpr int TP = 32 / LPT, BLOCK = 16 * TP, ROW = LPT * W * 4;
+  constexpr int N = 8, TP = 32 / LPT, BLOCK = N * TP, ROW = LPT * W * 4, DUP = LPT / N;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane % LPT, grp = lane / LPT, dh = P.dh;
   float4 q[R][W], acc[R][W];
   int limit[R];
@@ -399,47 +399,52 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
     }
   }
   const int end = min(s.tile1 * TILE, c.n_tok);
-  for (int num0 = s.tile0 * TILE + warp * BLOCK; num0 < end; num0 += SNT / 32 * BLOCK) {
+  auto seek = [&](int num0, int& id, long long& at) {
     const int num = num0 + lane;
-    int id = NO_TOKEN;
-    long long at = -1;
-    if (lane < BLOCK && num < end) {
-      if (s.slots) {
-        int lo = 0, hi = P.slots;
-        while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (c.first[mid] <= num) lo = mid; else hi = mid; }
-        id = c.base[lo] + num;
-      } else {
-        id = s.tok0 + num;
-      }
-      at = token_at(P, s, id);
-      if (at < 0) id = NO_TOKEN;
+    id = NO_TOKEN;
+    at = -1;
+    if (lane >= BLOCK || num >= end) return;
+    if (s.slots) {
+      int lo = 0, hi = P.slots;
+      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (c.first[mid] <= num) lo = mid; else hi = mid; }
+      id = c.base[lo] + num;
+    } else {
+      id = s.tok0 + num;
     }
-    float4 x[16];
-    auto load = [&](const void* from, int w) {
+    at = token_at(P, s, id);
+    if (at < 0) id = NO_TOKEN;
+  };
+  int id, next_id;
+  long long at, next_at;
+  seek(s.tile0 * TILE + warp * BLOCK, next_id, next_at);
+  for (int num0 = s.tile0 * TILE + warp * BLOCK; num0 < end; num0 += WARPS * BLOCK) {
+    id = next_id; at = next_at;
+    float4 x[N], y[N];
+    auto load = [&](const void* from, int w, float4 (&z)[N]) {
       const int e = (sub + LPT * w) * 4;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < N; ++i) {
         const long long o = __shfl_sync(FULL, at, i * TP + grp);
-        x[i] = o >= 0 && e < dh ? load4<T>((const T*)from + o + e, c.vk, dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
+        z[i] = o >= 0 && e < dh ? load4<T>((const T*)from + o + e, c.vk, dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
     };
-    // lane's token: LPT 16: load `sub` of its half of the warp, LPT 32: load lane / 2
-    const int mine = LPT == 16 ? sub * TP + grp : lane >> 1, my_id = __shfl_sync(FULL, id, mine);
+    if (W == 1) { load(P.k, 0, x); load(P.v, 0, y); }
+    seek(num0 + WARPS * BLOCK, next_id, next_at);
+    const int my_id = __shfl_sync(FULL, id, sub / DUP * TP + grp);     // lane's token: load sub / DUP of its group
     float wt[R];
     unsigned sees[R];
-    if (W == 1) load(P.k, 0);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      float d[16];
+      float d[N];
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        if (W > 1) load(P.k, w);
+        if (W > 1) load(P.k, w, x);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < N; ++i)
           d[i] = fmaf(q[r][w].w, x[i].w, fmaf(q[r][w].z, x[i].z, fmaf(q[r][w].y, x[i].y, fmaf(q[r][w].x, x[i].x, w ? d[i] : 0.f))));
       }
 #pragma unroll
-      for (int n = 8, off = LPT / 2; n >= 1; n >>= 1, off >>= 1) {
+      for (int n = N / 2, off = LPT / 2; n >= 1; n >>= 1, off >>= 1) {
         const bool up = sub & off;
 #pragma unroll
         for (int i = 0; i < n; ++i) {
@@ -448,7 +453,8 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
         }
       }
       float z = d[0];
-      if (LPT == 32) z += __shfl_xor_sync(FULL, z, 1);
+#pragma unroll
+      for (int off = DUP / 2; off; off >>= 1) z += __shfl_xor_sync(FULL, z, off);
       const bool see = my_id < limit[r];
       sees[r] = __ballot_sync(FULL, see);
       z = see ? z * P.scale_log2 : NINF;
@@ -459,22 +465,22 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
       seen[r] = seen[r] || sees[r] != 0;
       m[r] = m_new;
       wt[r] = exp2f(z - ref);
-      l[r] = fmaf(l[r], f, LPT == 32 && (lane & 1) ? 0.f : wt[r]);
+      l[r] = fmaf(l[r], f, sub % DUP ? 0.f : wt[r]);
 #pragma unroll
       for (int w = 0; w < W; ++w) { acc[r][w].x *= f; acc[r][w].y *= f; acc[r][w].z *= f; acc[r][w].w *= f; }
     }
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      load(P.v, w);
+      if (W > 1) load(P.v, w, y);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int from = LPT == 16 ? grp * 16 + i : 2 * i;
+      for (int i = 0; i < N; ++i) {
+        const int from = grp * LPT + i * DUP;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           const float u = __shfl_sync(FULL, wt[r], from);
           if (sees[r] >> from & 1) {
-            acc[r][w].x = fmaf(u, x[i].x, acc[r][w].x); acc[r][w].y = fmaf(u, x[i].y, acc[r][w].y);
-            acc[r][w].z = fmaf(u, x[i].z, acc[r][w].z); acc[r][w].w = fmaf(u, x[i].w, acc[r][w].w);
+            acc[r][w].x = fmaf(u, y[i].x, acc[r][w].x); acc[r][w].y = fmaf(u, y[i].y, acc[r][w].y);
+            acc[r][w].z = fmaf(u, y[i].z, acc[r][w].z); acc[r][w].w = fmaf(u, y[i].w, acc[r][w].w);
           }
         }
       }
@@ -482,7 +488,7 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
   }
   // the warp's parts: outputs over the groups of lanes, sums over the lanes; then the warps'
   __syncthreads();                                     // (what was in this memory has been read)
-  float2* const s_ml = (float2*)(s_part + SNT / 32 * R * ROW);
+  float2* const s_ml = (float2*)(s_part + WARPS * R * ROW);
 #pragma unroll
   for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -491,7 +497,7 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
     if (lane == 0) s_ml[warp * R + r] = make_float2(m[r], l[r]);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      if (LPT == 16) {
+      if (TP == 2) {
         acc[r][w].x += __shfl_xor_sync(FULL, acc[r][w].x, 16); acc[r][w].y += __shfl_xor_sync(FULL, acc[r][w].y, 16);
         acc[r][w].z += __shfl_xor_sync(FULL, acc[r][w].z, 16); acc[r][w].w += __shfl_xor_sync(FULL, acc[r][w].w, 16);
       }
@@ -500,13 +506,13 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
   }
   __syncthreads();
   const int live = min(R, s.rows - r0);
-  for (int u = threadIdx.x; u < live * dh; u += SNT) {
+  for (int u = threadIdx.x; u < live * dh; u += WARPS * 32) {
     const int r = u / dh, e = u - r * dh;
     float M = NINF, L = 0.f, o = 0.f;
 #pragma unroll
-    for (int w = 0; w < SNT / 32; ++w) M = fmaxf(M, s_ml[w * R + r].x);
+    for (int w = 0; w < WARPS; ++w) M = fmaxf(M, s_ml[w * R + r].x);
 #pragma unroll
-    for (int w = 0; w < SNT / 32; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
       const float2 ml = s_ml[w * R + r];
       if (ml.x == NINF) continue;
       const float f = exp2f(ml.x - M);
@@ -525,9 +531,11 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
   __syncthreads();
 }
 
-// ONLY_FEW: a call whose items all have up to FEW rows needs no tiles in shared memory, and more CTAs fit an SM.
+// ONLY_FEW: a call whose items all have up to FEW rows needs no tiles in shared memory; CTAs of four warps, four to an SM, have more
+// segments' latencies side by side (2048 rows of 396 tokens, fp32, dh 64: 98 us with eight warps and two to an SM, XX us).
+constexpr int FEW_NT = 128;
 template <typename T, int NV, bool ONLY_FEW>
-__global__ void __launch_bounds__(SNT, 2) attend_simt_kernel(const __grid_constant__ Params P, bool vq, bool vk) {
+__global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) attend_simt_kernel(const __grid_constant__ Params P, bool vq, bool vk) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ uint32_t s_bad[2];
   rr_pdl_wait();
@@ -569,12 +577,14 @@ __global__ void __launch_bounds__(SNT, 2) attend_simt_kernel(const __grid_consta
       u += segment_at(P, blockIdx.x, u, u0, u1, s);
       c.n_tok = s.tok1 - s.tok0;
     }
-    constexpr int LPT = NV == 1 ? 16 : 32, W = NV > 2 ? 2 : 1, R = W == 1 ? 4 : 1;
+    constexpr int LPT = NV == 1 ? 16 : 32, W = NV > 2 ? 2 : 1, R = W == 1 ? 4 : 1, WARPS = (ONLY_FEW ? FEW_NT : SNT) / 32;
     if (ONLY_FEW || s.rows <= FEW) {
-      if (s.rows == 1) few_rows<T, LPT, W, 1>(P, s, c, 0, c.q);
-      else for (int r0 = 0; r0 < s.rows; r0 += R) few_rows<T, LPT, W, R>(P, s, c, r0, c.q);
-    } else if (s.rows <= 16) rows_block<T, NV, 1>(P, s, c, 0, s_bad);
-    else for (int r0 = 0; r0 < s.rows; r0 += 64) rows_block<T, NV, 4>(P, s, c, r0, s_bad);
+      if (s.rows == 1) few_rows<T, LPT, W, 1, WARPS>(P, s, c, 0, c.q);
+      else for (int r0 = 0; r0 < s.rows; r0 += R) few_rows<T, LPT, W, R, WARPS>(P, s, c, r0, c.q);
+    } else if constexpr (!ONLY_FEW) {
+      if (s.rows <= 16) rows_block<T, NV, 1>(P, s, c, 0, s_bad);
+      else for (int r0 = 0; r0 < s.rows; r0 += 64) rows_block<T, NV, 4>(P, s, c, r0, s_bad);
+    }
   }
 }
 
@@ -591,7 +601,7 @@ cudaError_t launch_simt(const Params& P, int grid, cudaStream_t st) {
       return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_plan(RR_PAGED_MAX_DH, RR_MAX_RANGE_SLOTS, false).total);
     });
     if (e != cudaSuccess) return e;
-    return rr_launch_pdl(kernel, grid, SNT, (size_t)L.total, st, P, vq, vk);
+    return rr_launch_pdl(kernel, grid, few ? FEW_NT : SNT, (size_t)L.total, st, P, vq, vk);
   };
   static unsigned long long done[8];
   switch ((P.dh + 63) / 64 + (few ? 4 : 0)) {
@@ -685,7 +695,7 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.range_rows = (long long)kv->batch * a->route_heads * a->n_q;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
   P.streams = P.tc ? 2 : 1;
-  P.ctas = rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 3 : 2);
+  P.ctas = rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 4 : 2);
   // few rows: each is cut into parts, so that every SM has one
   const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS);
   P.splits = (int)(items >= P.ctas ? 1 : ceil_div(P.ctas, items));
