@@ -19,10 +19,23 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
   rr_pdl_wait();
   rr_pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  long long run = P.kv_heads * prefix_row_tiles(P) * prefix_tiles(P);
+  // the sequences apart: if their row tiles are at most an eighth more than those of all rows together
+  int mine_tiles = 0;
+  for (int b = tid; b < P.batch; b += PLAN_NT) if (seq_len(P, b) > 0) mine_tiles += own_row_tiles(P, b);
+#pragma unroll
+  for (int off = 16; off; off >>= 1) mine_tiles += __shfl_xor_sync(FULL, mine_tiles, off);
+  if (lane == 0) s_warp[warp] = mine_tiles;
+  __syncthreads();
+  long long row_tiles = 0;
+#pragma unroll
+  for (int w = 0; w < PLAN_NT / 32; ++w) row_tiles += s_warp[w];
+  const long long packed = prefix_row_tiles(P);
+  const bool apart = row_tiles <= packed + packed / 8;
+  __syncthreads();
+  long long run = apart ? 0 : P.kv_heads * packed * prefix_tiles(P);
   for (int b0 = 0; b0 < P.batch; b0 += PLAN_NT) {
     const int b = b0 + tid;
-    const long long mine = b < P.batch ? (long long)P.kv_heads * own_row_tiles(P, b) * own_tiles(P, b) : 0;
+    const long long mine = b < P.batch ? (long long)P.kv_heads * own_row_tiles(P, b) * own_tiles(P, b, apart) : 0;
     long long incl = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) { const long long x = __shfl_up_sync(FULL, incl, off); if (lane >= off) incl += x; }
@@ -35,82 +48,88 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
     run += all;
     __syncthreads();
   }
-  if (tid == 0) P.cum[P.batch] = run;
+  if (tid == 0) { P.cum[P.batch] = run; P.cum[P.batch + 1] = apart; }
 }
 
 // ---- join --------------------------------------------------------------------------------------------------
-// A warp joins the partials of one row: o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i, in the order of their tokens.
-template <typename T>
+// WPR warps join the partials of one row: o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Each warp takes every WPR-th partial, eight of
+// them in flight; their parts are added in the warps' order.  One warp where rows are many, eight where they are few (and
+// their partials many: a row of one short call has up to a hundred and fifty).
+template <typename T, int WPR>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params P) {
   constexpr int E = RR_PAGED_MAX_DH / 32;
+  __shared__ float s_o[WPR > 1 ? 8 : 1][RR_PAGED_MAX_DH], s_l[8], s_m[8];
   rr_pdl_wait();
   rr_pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % WPR;
+  const long long row = (long long)blockIdx.x * (8 / WPR) + warp / WPR;
   const int H = P.heads;
-  // up to two lists of partials: `n` in all, the first n0 of list 0
-  long long home[2] = {0, 0};
-  int c0[2] = {0, 0}, cnt[2] = {0, 0}, st[2] = {1, 1}, r_in[2] = {0, 0};
-  long long out;
+  // up to two lists of partials: the n0 first ones of list 0
+  long long home0 = 0, home1 = 0;
+  int c0 = 0, c1 = 0, cnt0 = 0, cnt1 = 0, st0 = 1, st1 = 1, r0 = 0, r1 = 0;
+  long long out = 0;
+  bool mine = true;
   if (P.slots == 0) {
-    if (row >= (long long)P.tokens * H) return;
-    const int t = (int)(row / H), h = (int)(row % H), kvh = h / P.group, g = h % P.group;
-    int b = t;
-    if (P.cu) {
-      b = rr_sequence_of_warp(P.cu, P.batch, t);
-      if (b < 0) return;                               // padding: left as it was
-    }
-    const long long all = __ldg(P.cum + P.batch), per = (long long)P.tokens * P.group;
-    out = t * P.ot + h * P.oh;
-    const long long np = prefix_tiles(P), qtp = prefix_row_tiles(P);
-    if (np > 0) {
-      const long long idx = (long long)t * P.group + g, first = (kvh * qtp + idx / ROWS) * np;
-      home[0] = kvh * per + idx;
-      r_in[0] = (int)(idx % ROWS);
-      c0[0] = cta_of(P, first, all);
-      cnt[0] = cta_of(P, first + np - 1, all) - c0[0] + 1;
-      st[0] = P.streams == 2 && min((long long)ROWS, per - idx / ROWS * ROWS) <= TILE ? 2 : 1;
-    }
-    const int no = own_tiles(P, b);
-    if (no > 0) {
-      const int t0 = seq_first(P, b), n = seq_count(P, b), qt = own_row_tiles(P, b);
-      const long long idx = (long long)(t - t0) * P.group + g;
-      const long long first = __ldg(P.cum + b) + (kvh * (long long)qt + idx / ROWS) * no;
-      home[1] = (P.kv_heads + kvh) * per + (long long)t0 * P.group + idx;
-      r_in[1] = (int)(idx % ROWS);
-      c0[1] = cta_of(P, first, all);
-      cnt[1] = cta_of(P, first + no - 1, all) - c0[1] + 1;
-      st[1] = P.streams == 2 && min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS) <= TILE ? 2 : 1;
+    mine = row < (long long)P.tokens * H;
+    const int t = (int)quot(mine ? row : 0, H), h = (int)((mine ? row : 0) - (long long)t * H), kvh = h / P.group, g = h - kvh * P.group;
+    const int b = P.cu ? rr_sequence_of_warp(P.cu, P.batch, t) : t;
+    mine = mine && b >= 0;                             // (padding: left as it was)
+    if (mine) {
+      const long long all = __ldg(P.cum + P.batch), per = (long long)P.tokens * P.group;
+      out = t * P.ot + h * P.oh;
+      const bool apart = __ldg(P.cum + P.batch + 1) != 0;
+      const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P);
+      if (np > 0) {
+        const long long idx = (long long)t * P.group + g, first = (kvh * qtp + idx / ROWS) * np;
+        home0 = kvh * per + idx;
+        r0 = (int)(idx % ROWS);
+        c0 = cta_of(P, first, all);
+        cnt0 = cta_of(P, first + np - 1, all) - c0 + 1;
+        st0 = partials_of(P.streams, min((long long)ROWS, per - idx / ROWS * ROWS));
+      }
+      const int no = own_tiles(P, b, apart);
+      if (no > 0) {
+        const int t0 = seq_first(P, b), n = seq_count(P, b), qt = own_row_tiles(P, b);
+        const long long idx = (long long)(t - t0) * P.group + g;
+        const long long first = __ldg(P.cum + b) + (kvh * (long long)qt + idx / ROWS) * no;
+        home1 = (P.kv_heads + kvh) * per + (long long)t0 * P.group + idx;
+        r1 = (int)(idx % ROWS);
+        c1 = cta_of(P, first, all);
+        cnt1 = cta_of(P, first + no - 1, all) - c1 + 1;
+        st1 = partials_of(P.streams, min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS));
+      }
+      if (no > 0 && P.tc && np == 0 && cnt1 == 1 && st1 == 1) mine = false;      // (one segment with all of the row's tiles wrote the output itself)
     }
   } else {
     const int mg = P.m * P.group;
-    if (row >= P.range_rows * mg) return;
-    const long long rr = row / mg;
-    const int idx = (int)(row % mg), i = (int)(rr % P.n_q), r = (int)(rr / P.n_q % P.route_heads), b = (int)(rr / P.n_q / P.route_heads);
-    st[0] = P.streams == 2 && min(ROWS, mg - idx / ROWS * ROWS) <= TILE ? 2 : 1;
-    if (P.direct && st[0] == 1) return;
-    home[0] = row;
-    cnt[0] = P.splits;
+    mine = row < P.range_rows * mg;
+    const long long rr = quot(mine ? row : 0, mg), per = quot(rr, P.n_q);
+    const int idx = (int)((mine ? row : 0) - rr * mg), i = (int)(rr - per * P.n_q), r = (int)per % P.route_heads, b = (int)per / P.route_heads;
+    st0 = partials_of(P.streams, min(ROWS, mg - idx / ROWS * ROWS));
+    mine = mine && !(P.direct && st0 == 1);
+    home0 = row;
+    cnt0 = mine ? P.splits : 0;
     out = b * P.ob + (r * P.group + idx % P.group) * P.oh + (i * P.m + idx / P.group) * P.ot;
   }
-  const int n0 = cnt[0] * st[0], n = n0 + cnt[1] * st[1];
+  if (WPR == 1 && !mine) return;
+  const int n0 = cnt0 * st0, n = n0 + cnt1 * st1;
   const long long cta_rows = 2 * (long long)P.tokens * H, split_rows = P.slots ? P.range_rows * P.m * P.group : 0;
   auto place = [&](int k) -> long long {               // partial row of the k-th partial
-    const int w = k >= n0;
+    const bool w = k >= n0;
     if (w) k -= n0;
-    const int s = st[w], c = k / s;
-    const long long at = P.slots ? home[0] + c * split_rows : c == 0 ? home[w] : cta_rows + (long long)(c0[w] + c) * ROWS + r_in[w];
-    return (k % s) * P.part_rows + at;
+    const int s = w ? st1 : st0, c = k / s;
+    const long long at = P.slots ? home0 + c * split_rows : c == 0 ? (w ? home1 : home0) : cta_rows + (long long)((w ? c1 : c0) + c) * ROWS + (w ? r1 : r0);
+    return (k - c * s) * P.part_rows + at;
   };
   float M = NINF;
-  for (int k = lane; k < n; k += 32) M = fmaxf(M, P.part_ml[place(k)].x);
+  for (int k = lane * WPR + part; k < n; k += 32 * WPR) M = fmaxf(M, P.part_ml[place(k)].x);
 #pragma unroll
   for (int off = 16; off; off >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, off));
   float l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int k0 = 0; k0 < n; k0 += 32) {
-    const int k = k0 + lane;
+  for (int k0 = part; k0 < n; k0 += 32 * WPR) {
+    const int k = k0 + lane * WPR;
     float w = 0.f;
     long long at = -1;
     if (k < n) {
@@ -119,18 +138,47 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
       if (ml.x == NINF || (ml.x == LOWEST && ml.y == 0.f)) at = -1;      // nothing in it (and no output written)
       else { w = exp2f(ml.x - M); l = fmaf(w, ml.y, l); }
     }
-    const int lim = min(32, n - k0);
-    for (int u = 0; u < lim; ++u) {
-      const long long au = __shfl_sync(FULL, at, u);
-      const float wu = __shfl_sync(FULL, w, u);
-      if (au < 0) continue;
-      const float* const src = P.part_o + au * P.dh;
+    const int lim = min(32, (n - k0 + WPR - 1) / WPR);
+    for (int u0 = 0; u0 < lim; u0 += 8) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) o[e] = fmaf(wu, src[lane + 32 * e], o[e]);
+      for (int e = 0; e < E; ++e) {
+        if (32 * e >= P.dh) break;
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const long long au = __shfl_sync(FULL, at, (u0 + u) & 31);
+          x[u] = u0 + u < lim && au >= 0 && lane + 32 * e < P.dh ? P.part_o[au * P.dh + lane + 32 * e] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) o[e] = fmaf(__shfl_sync(FULL, w, (u0 + u) & 31), x[u], o[e]);
+      }
     }
   }
 #pragma unroll
   for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(FULL, l, off);
+  if (WPR > 1) {
+    if (lane == 0) { s_l[warp] = l; s_m[warp] = M; }
+#pragma unroll
+    for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) s_o[warp][lane + 32 * e] = o[e];
+    __syncthreads();
+    if (part != 0 || !mine) return;
+    float top = M;
+#pragma unroll
+    for (int w = 1; w < WPR; ++w) top = fmaxf(top, s_m[warp + w]);
+    float f = M == NINF ? 0.f : exp2f(M - top);
+    l *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= f;
+#pragma unroll
+    for (int w = 1; w < WPR; ++w) {
+      if (s_m[warp + w] == NINF) continue;
+      f = exp2f(s_m[warp + w] - top);
+      l = fmaf(f, s_l[warp + w], l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) o[e] = fmaf(f, s_o[warp + w][lane + 32 * e], o[e]);
+    }
+    M = top;
+  }
   // no weight at all: zeros for a row without tokens, NaN for one whose tokens are all at -inf
   const float inv = l == 0.f ? (M == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / l;
 #pragma unroll
@@ -356,7 +404,7 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
   for (int r = tid >> 5; r < BM && r0 + r < s.rows; r += SNT / 32) {
     if (!(s_bad[r >> 5] >> (r & 31) & 1)) continue;
     float mm, ll, oo[RR_PAGED_MAX_DH / 32];
-    repair_row<T>(P, s, r0 + r, 0, 1, mm, ll, oo);
+    repair_row<T>(P, s, r0 + r, 0, 1, -1, mm, ll, oo);
     const int lane = tid & 31;
     const RowAt a = row_at(P, s, r0 + r);
     const long long at = s.part + r0 + r;
@@ -620,7 +668,7 @@ size_t up(size_t x) { return (x + 255) / 256 * 256; }
 // Offsets in the workspace: cum, part_ml, part_o.
 size_t lay_out(Params& P, uint8_t* ws) {
   size_t at = 0;
-  P.cum = (long long*)(ws + at); at += up(P.slots ? 0 : (size_t)(P.batch + 1) * 8);
+  P.cum = (long long*)(ws + at); at += up(P.slots ? 0 : (size_t)(P.batch + 2) * 8);
   const size_t rows = (size_t)P.part_rows * P.streams;
   P.part_ml = (float2*)(ws + at); at += up(rows * sizeof(float2));
   P.part_o = (float*)(ws + at); at += up(rows * P.dh * sizeof(float));
@@ -649,6 +697,9 @@ bool misaligned(const void* q, const void* out, int dtype) {
   return (((uintptr_t)q | (uintptr_t)out) & (dtype == RR_BF16 ? 1 : 3)) != 0;
 }
 
+// Few rows are quartered by the tensor cores' kernel where eight partials a row are no great workspace.
+int streams_of(const Params& P) { return !P.tc ? 1 : P.part_rows * P.dh * 32 <= 512LL << 20 ? 8 : 2; }
+
 int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   const int rc = fill(kv, P);
   if (rc != RR_OK) return rc;
@@ -666,9 +717,9 @@ int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.splits = 1;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
-  P.streams = P.tc ? 2 : 1;
   P.ctas = rr_sm_count() * (P.tc ? 1 : 2);
   P.part_rows = 2LL * P.tokens * P.heads + (long long)P.ctas * ROWS;
+  P.streams = streams_of(P);
   return RR_OK;
 }
 
@@ -694,16 +745,17 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.range_rows = (long long)kv->batch * a->route_heads * a->n_q;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
-  P.streams = P.tc ? 2 : 1;
   P.ctas = rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 4 : 2);
   // few rows: each is cut into parts, so that every SM has one
   const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS);
-  P.splits = (int)(items >= P.ctas ? 1 : ceil_div(P.ctas, items));
+  P.splits = (int)(items >= P.ctas ? 1 : P.ctas / items);
   if (P.splits > 64) P.splits = 64;
   P.direct = P.splits == 1;
-  // (a row of an item with more than TILE rows has one stream: the last item of a range row may have fewer)
+  P.part_rows = P.splits * P.range_rows * P.m * P.group;
+  P.streams = streams_of(P);
+  // (direct: an item whose rows have one partial needs none; the last item of a range row may have fewer rows than the others)
   const int mg = P.m * P.group, last = mg % ROWS;
-  P.part_rows = P.direct && (P.streams == 1 || last == 0 || last > TILE) ? 0 : P.splits * P.range_rows * P.m * P.group;
+  if (P.direct && partials_of(P.streams, std::min(mg, ROWS)) == 1 && (last == 0 || partials_of(P.streams, last) == 1)) P.part_rows = 0;
   return RR_OK;
 }
 
@@ -724,8 +776,10 @@ int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, co
   }
   if (e == cudaSuccess && P.part_rows > 0) {
     const long long rows = P.slots ? P.range_rows * P.m * P.group : (long long)P.tokens * P.heads;
-    const int grid = (int)ceil_div(rows, 8);
-    e = dtype == RR_BF16 ? rr_launch_pdl(join_kernel<__nv_bfloat16>, grid, 256, 0, st, P) : rr_launch_pdl(join_kernel<float>, grid, 256, 0, st, P);
+    const bool few = rows < 8 * rr_sm_count();
+    const int grid = (int)(few ? rows : ceil_div(rows, 8));
+    auto join = [&](auto one, auto eight) { return rr_launch_pdl(few ? eight : one, grid, 256, 0, st, P); };
+    e = dtype == RR_BF16 ? join(join_kernel<__nv_bfloat16, 1>, join_kernel<__nv_bfloat16, 8>) : join(join_kernel<float, 1>, join_kernel<float, 8>);
     ++launches;
   }
   rr_count_launch(launches);

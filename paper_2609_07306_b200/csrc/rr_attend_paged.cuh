@@ -6,6 +6,8 @@
 //   shared, prefix   the queries of all sequences and of the G = heads / kv_heads query heads of a key head (row t * G + g),
 //                    over the prefix's tokens
 //   shared, own      the same rows of one sequence, over its tokens behind the prefix
+//   shared, apart    where the sequences' own rows fill their tiles about as well as all rows together (prompts), there is nothing to share but
+//                    L2's copy of the prefix: the rows of one sequence over all of its tokens, and a row has one partial less
 //   ranges           the m * G queries of a range row, over the tokens of its slots
 // A list is walked in tiles of TILE tokens.  A SEGMENT is a run of tiles of an item; it leaves per row a
 // partial result: reference maximum m (of logit * log2 e), sum l of 2^(x - m), and the unnormalised output.  The partials
@@ -43,10 +45,10 @@ struct Params {
   int n_q, m, slots, route_heads;                      // ranges (slots > 0)
   float scale_log2;                                    // scale * log2 e
   // schedule
-  int tc, ctas, splits, streams;                         // streams: partials per segment and row (1, or 2: see Seg::paired)
+  int tc, ctas, splits, streams;                       // streams: most partials of a segment's row (see partials_of)
   long long range_rows;                                // batch * route_heads * n_q
   // workspace
-  long long* cum;                                      // shared: [batch + 1] tiles before sequence b's items; [batch] = all tiles
+  long long* cum;                                      // shared: [batch + 2] tiles before sequence b's items; [batch] = all tiles; [batch + 1] = apart
   float* part_o;                                       // [streams][part_rows][dh]
   float2* part_ml;                                     // [streams][part_rows]
   long long part_rows;
@@ -59,14 +61,21 @@ struct Seg {
   int b;                                               // sequence, -1: prefix (rows of all sequences)
   int kvh, h0;                                         // key head, first query head
   int tok0, tok1;                                      // dense: the list's tokens
-  const int32_t* pages;                                // page list of the tokens
+  const int32_t* pages;                                // page list of the tokens, from token `prefix` on
+  const int32_t* prefix_pages;
+  int prefix;
+  bool whole;                                          // all tiles of the rows' only item: nothing to join
   const int32_t* slots;                                // ranges: the row's slots, else null
   int tile0, tile1;                                    // the segment's tiles of the list (ranges: of `split`, once counted)
   int split;
   long long part;                                      // partial row of row 0
 };
 
-__host__ __device__ inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+// a / b for a >= 0, b > 0; mostly both fit 32 bits, whose division takes a fifth of the time
+__host__ __device__ inline long long quot(long long a, long long b) {
+  return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+__host__ __device__ inline long long ceil_div(long long a, long long b) { return quot(a + b - 1, b); }
 
 // Tokens that sequence b has in the cache (never more than its table holds).
 __device__ __forceinline__ int seq_len(const Params& P, int b) {
@@ -82,55 +91,58 @@ __device__ __forceinline__ int seq_count(const Params& P, int b) {
 }
 __device__ __forceinline__ long long prefix_tiles(const Params& P) { return (P.prefix + TILE - 1) / TILE; }
 __device__ __forceinline__ long long prefix_row_tiles(const Params& P) { return ceil_div((long long)P.tokens * P.group, ROWS); }
-__device__ __forceinline__ int own_tiles(const Params& P, int b) { return (max(seq_len(P, b) - P.prefix, 0) + TILE - 1) / TILE; }
+__device__ __forceinline__ int own_tiles(const Params& P, int b, bool apart) { return (max(seq_len(P, b) - (apart ? 0 : P.prefix), 0) + TILE - 1) / TILE; }
 __device__ __forceinline__ int own_row_tiles(const Params& P, int b) { return (int)ceil_div((long long)seq_count(P, b) * P.group, ROWS); }
 
 // With N = min(ctas, W) CTAs at work, CTA c's share of W tiles is [c W / N, (c + 1) W / N), at least one tile: an item that
 // is cut is in consecutive CTAs.  cta_of: the CTA that has tile u.
 __device__ __forceinline__ long long share(const Params& P, int c, long long W) {
   const long long N = min((long long)P.ctas, W);
-  return c >= N ? W : c * W / N;
+  return c >= N ? W : quot(c * W, N);
 }
 __device__ __forceinline__ int cta_of(const Params& P, long long u, long long W) {
   const long long N = min((long long)P.ctas, W);
-  return (int)(((u + 1) * N + W - 1) / W - 1);
+  return (int)(ceil_div((u + 1) * N, W) - 1);
 }
 
 // The segment at tile u of CTA c's share, which ends at u1; returns how many tiles of the share it takes.
 __device__ __forceinline__ int segment_at(const Params& P, int c, long long u, long long u0, long long u1, Seg& s) {
-  const long long np = prefix_tiles(P), qtp = prefix_row_tiles(P), before = P.kv_heads * qtp * np;
+  const bool apart = __ldg(P.cum + P.batch + 1) != 0;
+  const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P), before = P.kv_heads * qtp * np;
   long long first;                                     // first tile of the item
   int tiles;
   long long home;
   const long long row_all = (long long)P.tokens * P.group;
   s.slots = nullptr;
   s.split = 0;
+  s.prefix_pages = P.prefix_pages ? P.prefix_pages : P.table;
+  s.prefix = P.prefix;
   if (u < before) {
-    const long long item = u / np;
+    const long long item = quot(u, np);
     first = item * np;
     tiles = (int)np;
-    s.kvh = (int)(item / qtp);
-    s.row0 = (int)(item % qtp) * ROWS;
+    s.kvh = (int)quot(item, qtp);
+    s.row0 = (int)(item - s.kvh * qtp) * ROWS;
     s.rows = (int)min((long long)ROWS, row_all - s.row0);
     s.b = -1;
     s.t_base = 0; s.t_seq0 = 0; s.n_seq = 0;
     s.tok0 = 0; s.tok1 = P.prefix;
-    s.pages = P.prefix_pages ? P.prefix_pages : P.table;
+    s.pages = s.prefix_pages;
     home = s.kvh * row_all + s.row0;
   } else {
     int lo = 0, hi = P.batch;                          // last b with cum[b] <= u
     while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (__ldg(P.cum + mid) <= u) lo = mid; else hi = mid; }
     const int b = lo, qt = own_row_tiles(P, b);
-    tiles = own_tiles(P, b);
-    const long long base = __ldg(P.cum + b), item = (u - base) / tiles;
+    tiles = own_tiles(P, b, apart);
+    const long long base = __ldg(P.cum + b), item = quot(u - base, tiles);
     first = base + item * tiles;
-    s.kvh = (int)(item / qt);
-    s.row0 = (int)(item % qt) * ROWS;
+    s.kvh = (int)quot(item, qt);
+    s.row0 = (int)(item - (long long)s.kvh * qt) * ROWS;
     s.n_seq = seq_count(P, b);
     s.rows = (int)min((long long)ROWS, (long long)s.n_seq * P.group - s.row0);
     s.b = b;
     s.t_base = s.t_seq0 = seq_first(P, b);
-    s.tok0 = P.prefix; s.tok1 = seq_len(P, b);
+    s.tok0 = apart ? 0 : P.prefix; s.tok1 = seq_len(P, b);
     s.pages = P.table + b * P.table_stride;
     home = (P.kv_heads + s.kvh) * row_all + (long long)s.t_base * P.group + s.row0;
   }
@@ -138,6 +150,7 @@ __device__ __forceinline__ int segment_at(const Params& P, int c, long long u, l
   s.tile0 = (int)(u - first);
   s.tile1 = (int)min((long long)tiles, u1 - first);
   const int took = s.tile1 - s.tile0;
+  s.whole = took == tiles && u >= before && np == 0;
   if (P.causal && s.b >= 0) {                          // no row sees the tiles from the last row's limit on
     const int limit = s.tok1 - s.n_seq + (s.row0 + s.rows - 1) / P.group + 1;
     s.tile1 = max(s.tile0, min(s.tile1, limit <= s.tok0 ? 0 : (limit - s.tok0 + TILE - 1) / TILE));
@@ -149,12 +162,12 @@ __device__ __forceinline__ int segment_at(const Params& P, int c, long long u, l
 // Segment x of a ranges call (x < range_rows * row tiles * splits); its tiles are counted by who reads the slots.
 __device__ __forceinline__ void range_segment(const Params& P, long long x, Seg& s) {
   const int mg = P.m * P.group, qt = (mg + ROWS - 1) / ROWS;
-  s.split = (int)(x % P.splits);
-  const long long item = x / P.splits, row = item / qt;
-  s.row0 = (int)(item % qt) * ROWS;
+  const long long item = quot(x, P.splits), row = quot(item, qt);
+  s.split = (int)(x - item * P.splits);
+  s.row0 = (int)(item - row * qt) * ROWS;
   s.rows = min(ROWS, mg - s.row0);
-  const int i = (int)(row % P.n_q), r = (int)(row / P.n_q % P.route_heads);
-  s.b = (int)(row / P.n_q / P.route_heads);
+  const int per = (int)quot(row, P.n_q), i = (int)(row - (long long)per * P.n_q), r = per % P.route_heads;
+  s.b = per / P.route_heads;
   s.t_seq0 = 0; s.n_seq = P.n_q * P.m;
   s.t_base = i * P.m;
   s.kvh = r / (P.route_heads / P.kv_heads);
@@ -162,6 +175,8 @@ __device__ __forceinline__ void range_segment(const Params& P, long long x, Seg&
   s.tok0 = 0; s.tok1 = seq_len(P, s.b);
   s.pages = P.table + s.b * P.table_stride;
   s.slots = P.ranges + row * P.slots * 2;
+  s.prefix = 0;
+  s.whole = false;
   s.tile0 = s.tile1 = 0;
   s.part = (s.split * P.range_rows + row) * mg + s.row0;
 }
@@ -176,6 +191,9 @@ __device__ __forceinline__ void slot_span(const Seg& s, int j, int& lo, int& hi)
   hi = min(__ldg(s.slots + 2 * j + 1), s.tok1);
   if (lo < 0 || hi < lo) lo = hi = 0;
 }
+
+// Partials that a segment of `rows` rows leaves per row.
+__host__ __device__ inline int partials_of(int streams, long long rows) { return streams == 1 || rows > TILE ? 1 : streams > 2 && rows <= 32 ? 8 : 2; }
 
 struct RowAt { int t, h, limit; };                     // query token, head, tokens below `limit` are seen
 __device__ __forceinline__ RowAt row_at(const Params& P, const Seg& s, int r) {
@@ -199,7 +217,7 @@ __device__ __forceinline__ long long out_at(const Params& P, const Seg& s, const
 
 // Element offset of token `tok` of the segment's list, -1 if its page id is bad.
 __device__ __forceinline__ long long token_at(const Params& P, const Seg& s, int tok) {
-  const int col = tok / P.page_tokens, page = __ldg(s.pages + col);
+  const int col = tok / P.page_tokens, page = __ldg((tok < s.prefix ? s.prefix_pages : s.pages) + col);
   if (page < 0 || page >= P.num_pages) { if (P.status) atomicOr(P.status, RR_STATUS_BAD_INDEX); return -1; }
   return page * P.page_stride + s.kvh * P.head_stride + (tok - col * P.page_tokens) * P.token_stride;
 }
@@ -208,9 +226,9 @@ __device__ __forceinline__ long long token_at(const Params& P, const Seg& s, int
 // A tile is multiplied whole, so a value that a row may not see enters the row's sums with weight 0: nothing, unless it is an
 // infinity or NaN.  A row with such a result that has masked tokens of its list is computed again here, token by
 // token, by a warp: only what it sees is read.  (Rows that see an infinity come here as well, and keep it.)
-// Tiles tile0 + first, tile0 + first + step, ... of the segment.
+// Tiles tile0 + first, tile0 + first + step, ... of the segment; quarter >= 0: of every 64 tokens the 16 from 16 * quarter on.
 template <typename T>
-__device__ __noinline__ void repair_row(const Params& P, const Seg& s, int r, int first, int step, float& m, float& l, float (&o)[RR_PAGED_MAX_DH / 32]) {
+__device__ __noinline__ void repair_row(const Params& P, const Seg& s, int r, int first, int step, int quarter, float& m, float& l, float (&o)[RR_PAGED_MAX_DH / 32]) {
   constexpr int E = RR_PAGED_MAX_DH / 32;
   const int lane = threadIdx.x & 31;
   const RowAt a = row_at(P, s, r);
@@ -227,7 +245,7 @@ __device__ __noinline__ void repair_row(const Params& P, const Seg& s, int r, in
     if (s.slots) slot_span(s, j, lo, hi);
     for (int tok = lo; tok < hi; ++tok) {
       const long long n = num + (tok - lo), tile = n / TILE;
-      if (tile < s.tile0 + first || tile >= s.tile1 || (tile - s.tile0 - first) % step != 0) continue;
+      if (tile < s.tile0 + first || tile >= s.tile1 || (tile - s.tile0 - first) % step != 0 || (quarter >= 0 && (n >> 4 & 3) != quarter)) continue;
       if (tok >= a.limit) continue;
       const long long at = token_at(P, s, tok);
       if (at < 0) continue;

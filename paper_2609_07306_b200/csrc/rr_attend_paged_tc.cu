@@ -7,7 +7,9 @@
 //   a segment of more than 128 rows is paired: stream 0 has rows 0..127, stream 1 the others, each tile of keys and values is
 //   read once for both;
 //   one of up to 128 rows is split: both streams have the same rows, stream 0 the even tiles and stream 1 the odd ones, and
-//   each leaves a partial result of its own.
+//   each leaves a partial result of its own;
+//   one of up to 32 rows (a decoding step) is quartered besides: each of a stream's four warps has a copy of the rows in its 32 lanes and 16
+//   of every 64 tokens, whose weights alone are not zero there, so that the exponentials are spread over the SM.
 // The tensor pipe takes 2 x 520 cycles for a 128 x 128 x 128 tile's two products, the 16384 exponentials take 1024: many rows are
 // bound by both about equally, few rows by the cache's traffic.
 //
@@ -97,6 +99,18 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
         "=r"(r[31])
       : "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // No use of these registers is moved above this point.
 __device__ __forceinline__ void tie(uint32_t (&r)[32]) {
@@ -115,11 +129,15 @@ struct Where { int page, place, box; };
 // 16 rows x 32 columns: register 4 j + 0, 1 of lane 4 g + q has columns 8 j + 2 q, + 1 of row g, registers 4 j + 2, 3 those of row g + 8.
 __device__ __forceinline__ void tmem_ld_16x256_x4(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
         "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tie16(uint32_t (&r)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
 }
 // Word j of lane q of every four lanes goes to word q of lane j.
 __device__ __forceinline__ void quad_transpose(uint32_t (&w)[4]) {
@@ -218,7 +236,8 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
       const Seg& s = c->seg[n % ring];
       if (s.rows == 0) break;
       const bool paired = s.rows > TILE;
-      const int nt = s.tile1 - s.tile0, r = paired ? st * TILE + r_in : r_in;
+      const bool quart = P.streams > 2 && s.rows <= 32;
+      const int nt = s.tile1 - s.tile0, r = paired ? st * TILE + r_in : quart ? lane : r_in;
       const int steps = paired ? nt : (nt - st + 1) / 2;
       const bool live = r < s.rows, warp_live = r - lane < s.rows;
       ok = __all_sync(FULL, mbar_wait_spin(&c->rows_full[n % ring], n / ring & 1, abort_flag));
@@ -236,51 +255,79 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         s_cnt += h;
         tc_fence_after();
         if (warp_live) {
+          // The columns of this warp: all 64 of the half, or 16 of a quartered segment.  First their logits and which of them the row
+          // sees, a bit each.
           uint32_t x[2][32];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) tmem_ld32(s_tm + h * 64 + i * 32, x[i]);
-          tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < 2; ++i) tie(x[i]);
-          if (!masked) {
-            seen = true;
-          } else {                                     // which columns the row sees, a bit each
-            uint32_t see[2] = {0, 0};
-            const int* const ids = c->ids[cnt % IDS] + 64 * h;
-            if (i0.w && i1.w && i0.z <= i1.y) {
-              int n = 0;                               // ids ascend (every list in order, no bad page inside): the first n columns
-#pragma unroll
-              for (int step = 32; step; step >>= 1) if (ids[n + step - 1] < limit) n += step;
-              n += ids[n] < limit;
-              mixed = mixed || (n < 64 && ids[min(n, 63)] != NO_TOKEN);
-              see[0] = n >= 32 ? FULL : (1u << n) - 1;
-              see[1] = n >= 64 ? FULL : n <= 32 ? 0u : (1u << (n - 32)) - 1;
+          float top;
+          const int* const ids = c->ids[cnt % IDS] + 64 * h;
+          if (quart) {
+            tmem_ld16(s_tm + h * 64 + quarter * 16, x[0]);
+            if (!masked) {
+              seen = true;
             } else {
 #pragma unroll
-              for (int i = 0; i < 2; ++i)
-#pragma unroll 4
-                for (int j = 0; j < 32; ++j) {
-                  const int id = ids[i * 32 + j];
-                  if (id < limit) see[i] |= 1u << j;
-                  else mixed = mixed || id != NO_TOKEN;
+              for (int j = 0; j < 16; j += 4) {
+                const int4 id = *reinterpret_cast<const int4*>(ids + quarter * 16 + j);
+                const int e[4] = {id.x, id.y, id.z, id.w};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                  const bool sees = e[w] < limit;
+                  seen = seen || sees;
+                  mixed = mixed || (!sees && e[w] != NO_TOKEN);
+                  if (!sees) x[0][j + w] = 0xFF800000u;
                 }
+              }
             }
-            seen = seen || (see[0] | see[1]) != 0;
+            top = __uint_as_float(x[0][0]);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int j = 1; j < 15; j += 2) top = max3(top, __uint_as_float(x[0][j]), __uint_as_float(x[0][j + 1]));
+            top = fmaxf(top, __uint_as_float(x[0][15]));
+          } else {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) if (!(see[i] >> j & 1)) x[i][j] = 0xFF800000u;
+            for (int i = 0; i < 2; ++i) tmem_ld32(s_tm + h * 64 + i * 32, x[i]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) tie(x[i]);
+            if (!masked) {
+              seen = true;
+            } else {                                     // which columns the row sees, a bit each
+              uint32_t see[2] = {0, 0};
+              if (i0.w && i1.w && i0.z <= i1.y) {
+                int n = 0;                               // ids ascend (every list in order, no bad page inside): the first n columns
+#pragma unroll
+                for (int step = 32; step; step >>= 1) if (ids[n + step - 1] < limit) n += step;
+                n += ids[n] < limit;
+                mixed = mixed || (n < 64 && ids[min(n, 63)] != NO_TOKEN);
+                see[0] = n >= 32 ? FULL : (1u << n) - 1;
+                see[1] = n >= 64 ? FULL : n <= 32 ? 0u : (1u << (n - 32)) - 1;
+              } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll 4
+                  for (int j = 0; j < 32; ++j) {
+                    const int id = ids[i * 32 + j];
+                    if (id < limit) see[i] |= 1u << j;
+                    else mixed = mixed || id != NO_TOKEN;
+                  }
+              }
+              seen = seen || (see[0] | see[1]) != 0;
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) if (!(see[i] >> j & 1)) x[i][j] = 0xFF800000u;
+            }
+            float t[4];                                  // (four chains)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t* const y = &x[i >> 1][(i & 1) * 16];
+              t[i] = __uint_as_float(y[0]);
+#pragma unroll
+              for (int j = 1; j < 15; j += 2) t[i] = max3(t[i], __uint_as_float(y[j]), __uint_as_float(y[j + 1]));
+              t[i] = fmaxf(t[i], __uint_as_float(y[15]));
+            }
+            top = fmaxf(max3(t[0], t[1], t[2]), t[3]);
           }
-          float t[4];                                  // (four chains)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t* const y = &x[i >> 1][(i & 1) * 16];
-            t[i] = __uint_as_float(y[0]);
-#pragma unroll
-            for (int j = 1; j < 15; j += 2) t[i] = max3(t[i], __uint_as_float(y[j]), __uint_as_float(y[j + 1]));
-            t[i] = fmaxf(t[i], __uint_as_float(y[15]));
-          }
-          const float top = fmaxf(max3(t[0], t[1], t[2]), t[3]), m = live && top != NINF ? top * P.scale_log2 : NINF;
+          const float m = live && top != NINF ? top * P.scale_log2 : NINF;
           if (__any_sync(FULL, m > ref + GROWTH)) {    // (ref = -inf: the first finite maximum)
             const float now = m > ref + GROWTH ? m : ref, f = now == ref ? 1.f : ex2(ref - now);
             ref = now;
@@ -306,9 +353,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           const uint64_t scale2 = two(P.scale_log2, P.scale_log2), sub2 = two(-sub, -sub);
           uint64_t a[2] = {0, 0};
           uint32_t p[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const uint32_t* const y = &x[j / 16][2 * (j % 16)];
+          auto weight = [&](const uint32_t* y, int j) -> uint32_t {
             const uint64_t v = fma2(two(__uint_as_float(y[0]), __uint_as_float(y[1])), scale2, sub2);
             uint64_t e;
             if (j % 8 < BY_FMA) {
@@ -321,12 +366,24 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
             a[j & 1] = add2(a[j & 1], e);
             float e0, e1;
             split(e, e0, e1);
-            p[j] = pack(e0, e1);
+            return pack(e0, e1);
+          };
+          if (quart) {                                 // the other quarters' columns weigh nothing for this copy of the rows
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[j] = weight(&x[0][2 * j], j + 1);
+#pragma unroll
+            for (int j = 8; j < 16; ++j) p[j] = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              if (w == quarter) tmem_st8(s_tm + h * 64 + w * 8, p); else tmem_st8(s_tm + h * 64 + w * 8, p + 8);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) p[j] = weight(&x[j / 16][2 * (j % 16)], j);
+            tmem_st_32x32(s_tm + h * 64, p);
           }
           float s0, s1;
           split(add2(a[0], a[1]), s0, s1);
           sum += s0 + s1;
-          tmem_st_32x32(s_tm + h * 64, p);
           tmem_st_wait();
         }
         tc_fence_before();
@@ -340,15 +397,17 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         if (!ok) break;
         tc_fence_after();
       }
-      const bool direct = P.direct && paired;
+      const bool direct = paired && (P.direct || s.whole);
       if (warp_live) {
         if (seen && ref == NINF) ref = LOWEST;
-        const long long at = (paired ? 0 : st * P.part_rows) + s.part + r;
+        const long long at = (paired ? 0 : quart ? (st * 4 + quarter) * P.part_rows : st * P.part_rows) + s.part + r;
         const float inv = sum == 0.f ? (ref == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / sum;
         const RowAt a{s.t_base + (s.row0 + r) / P.group, s.h0 + (s.row0 + r) % P.group, 0};
         __nv_bfloat16* const out = (__nv_bfloat16*)P.out + out_at(P, s, a);
         if (live && !direct) P.part_ml[at] = make_float2(ref, sum);
-        const bool look = __any_sync(FULL, mixed);     // (only then can a value have come in that its row may not see)
+        // only then can a value have come in that its row may not see, or that belongs to another quarter
+        mixed = mixed || quart;
+        const bool look = __any_sync(FULL, mixed);
         unsigned odd_rows = 0;
         if (direct || steps > 0) {
           // TMEM in blocks of 16 rows x 8 columns: lane 4 g + q has columns 2 q, 2 q + 1 of rows g and g + 8, so that after an exchange
@@ -360,16 +419,22 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
             const unsigned long long out0 = __shfl_sync(FULL, (unsigned long long)out, half * 16 + g), out1 = __shfl_sync(FULL, (unsigned long long)out, half * 16 + g + 8);
             const bool live0 = r - lane + half * 16 + g < s.rows, live1 = r - lane + half * 16 + g + 8 < s.rows;
             float* const part0 = P.part_o + (at - lane + half * 16 + g) * D;
-            uint32_t odd0 = 0, odd1 = 0;
-#pragma unroll 1
+            if (r - lane + half * 16 >= s.rows) continue;
+            uint32_t odd0 = 0, odd1 = 0, all[D / 32][16];
+#pragma unroll
             for (int i = 0; i < D / 32; ++i) {
-              uint32_t o[16];
               if (steps > 0) {
-                tmem_ld_16x256_x4(o_tm + ((uint32_t)(half * 16) << 16) + i * 32, o);
+                tmem_ld_16x256_x4(o_tm + ((uint32_t)(half * 16) << 16) + i * 32, all[i]);
               } else {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] = 0;
+                for (int j = 0; j < 16; ++j) all[i][j] = 0;
               }
+            }
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+              uint32_t (&o)[16] = all[i];
+              tie16(o);
               if (look) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -416,7 +481,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           const int who = __ffs(again) - 1;
           again &= again - 1;
           float m, l, y[RR_PAGED_MAX_DH / 32];
-          repair_row<__nv_bfloat16>(P, s, r - lane + who, paired ? 0 : st, paired ? 1 : 2, m, l, y);
+          repair_row<__nv_bfloat16>(P, s, r - lane + who, paired ? 0 : st, paired ? 1 : 2, quart ? quarter : -1, m, l, y);
           const long long atw = __shfl_sync(FULL, at, who);
           __nv_bfloat16* const outw = (__nv_bfloat16*)__shfl_sync(FULL, (unsigned long long)out, who);
           if (!direct && lane == 0) P.part_ml[atw] = make_float2(m, l);
@@ -556,7 +621,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
             tok = s.tok0 + num;
           }
           col = P.page_shift >= 0 ? tok >> P.page_shift : tok / P.page_tokens;
-          page = __ldg(s.pages + col);
+          page = __ldg((tok < s.prefix ? s.prefix_pages : s.pages) + col);
         };
         auto find = [&](int tile) -> Where {
           Where at{-1, 0, 0};
@@ -611,7 +676,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           ok = load(P.k, maps.k, at[0]);
           const int rows = s.rows;
           for (int h = 0; ok && h < (rows > TILE ? 2 : 1); ++h, ++place) {
-            const int q = place & 1, r = h * TILE + w * 32 + lane;
+            const int q = place & 1, r = h * TILE + (P.streams > 2 && rows <= 32 ? 0 : w * 32) + lane;   // (quartered: four copies)
             ok = free_slot(&c->q_empty[q], (place >> 1 & 1) ^ 1);
             if (!ok) break;
             long long o = -1;
@@ -619,7 +684,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
               const int idx = s.row0 + r, dt = idx / P.group;
               o = q_at(P, s, RowAt{s.t_base + dt, s.h0 + idx - dt * P.group, 0});
             }
-            if (h * TILE + w * 32 < rows) rows32(P.q, o, q_addr + q * S::TILE_BYTES);
+            if (r - lane < rows) rows32(P.q, o, q_addr + q * S::TILE_BYTES);
             commit(&c->q_full[q]);
           }
           at[1] = find(tile0 + 1);

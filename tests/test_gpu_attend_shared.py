@@ -105,6 +105,20 @@ def test_token_major_pages_and_large_logits(dtype, dh):
 
 @pytest.mark.parametrize("dtype,dh", KINDS)
 @pytest.mark.parametrize("bad", [float("inf"), NAN])
+def test_values_that_a_prompt_may_not_see(dtype, dh, bad):
+    """The same for one sequence alone, and for few rows."""
+    for n, G in ((64, 4), (20, 1), (3, 5)):
+        def hurt(k, v, table):
+            p = int(table[0, (100 + n // 2) // 16])
+            v[p, 0, (100 + n // 2) % 16, 7] = bad
+        out = run(dtype, G, 1, dh, 16, 100, [100 + n], [n], seed=6, hurt=hurt)
+        seen = torch.zeros((n, G, dh), dtype=torch.bool)
+        seen[n // 2:, :, 7] = True
+        assert torch.equal(~out.isfinite().cpu(), seen)
+
+
+@pytest.mark.parametrize("dtype,dh", KINDS)
+@pytest.mark.parametrize("bad", [float("inf"), NAN])
 def test_values_that_a_row_may_not_see(dtype, dh, bad):
     """An infinity or NaN at a token reaches the queries that see it and no other, in its column only."""
     lens, news = [100 + 60, 100 + 20], [50, 20]
@@ -166,6 +180,32 @@ def test_prefix_pages_of_their_own(dtype, dh):
     table[0] = table[1]
     want, bound = shared(q, k, v, table, lens, [0, 1, 2, 3], 0.1, True)
     assert_within(out, want, bound)
+
+
+@pytest.mark.parametrize("dtype,dh", KINDS)
+@pytest.mark.parametrize("lens,news", [([100 + 70], [70]), ([100 + 64, 100 + 90, 700], [64, 64, 128]), ([40, 100 + 64], [64, 64]), ([0, 164], [64, 64])])
+def test_prompts_that_fill_their_row_tiles(dtype, dh, lens, news):
+    """Whole row tiles per sequence (and one sequence alone): each attends by itself, also where it is shorter than the prefix."""
+    run(dtype, 4, 1, dh, 16, 100, lens, news, seed=len(lens))
+    run(dtype, 4, 1, dh, 24, 100, lens, news, seed=7, causal=False)
+
+
+@pytest.mark.parametrize("dtype,dh", [(torch.bfloat16, 128), (torch.bfloat16, 64), (torch.float32, 64)])
+@pytest.mark.parametrize("page", [16, 24])
+def test_prompts_with_prefix_pages_of_their_own(dtype, dh, page):
+    """The sequences' tables hold nothing for the prefix's whole pages; it ends inside a page, whose rest is the sequences' own."""
+    lens, news, prefix = [180, 164], [64, 64], 100
+    g, k, v, table = build(dtype, 1, dh, page, prefix, lens, 14)
+    pages = table[0, :-(-prefix // page)].clone().contiguous()
+    bare = table.clone()
+    bare[:, :prefix // page] = -5
+    q = torch.randn((128, 4, dh), generator=g, device="cuda").to(dtype)
+    cu = torch.tensor([0, 64, 128], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = PagedKV(k, v, bare, status).attend_shared(q, torch.tensor(lens, dtype=torch.int32, device="cuda"), prefix, 0.1, cu=cu, prefix_pages=pages)
+    want, bound = shared(q, k, v, table, lens, [0, 64, 128], 0.1, True)
+    assert_within(out, want, bound)
+    assert status.item() == 0
 
 
 @pytest.mark.parametrize("dtype,dh", [(torch.bfloat16, 128), (torch.float32, 64)])
