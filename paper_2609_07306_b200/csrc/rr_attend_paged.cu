@@ -53,12 +53,11 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
 
 // ---- join --------------------------------------------------------------------------------------------------
 // WPR warps join the partials of one row: o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Each warp takes every WPR-th partial, eight of
-// them in flight; their parts are added in the warps' order.  One warp where rows are many, eight where they are few (and
-// their partials many: a row of one short call has up to a hundred and fifty).
+// them in flight, a lane four columns (and four more 128 further on); the warps' parts are added in their order.  One warp where rows
+// are many, eight where they are few (and their partials many: up to a hundred and fifty for a row of one short call).
 template <typename T, int WPR>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params P) {
-  constexpr int E = RR_PAGED_MAX_DH / 32;
-  __shared__ float s_o[WPR > 1 ? 8 : 1][RR_PAGED_MAX_DH], s_l[8], s_m[8];
+  __shared__ __align__(16) float s_o[WPR > 1 ? 8 : 1][RR_PAGED_MAX_DH], s_l[8], s_m[8];
   rr_pdl_wait();
   rr_pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % WPR;
@@ -125,9 +124,11 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   for (int k = lane * WPR + part; k < n; k += 32 * WPR) M = fmaxf(M, P.part_ml[place(k)].x);
 #pragma unroll
   for (int off = 16; off; off >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, off));
-  float l = 0.f, o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  const bool vec = P.dh % 4 == 0;
+  const int e0 = lane * 4;
+  float l = 0.f;
+  float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+  auto add = [](float4& y, float w, const float4& x) { y.x = fmaf(w, x.x, y.x); y.y = fmaf(w, x.y, y.y); y.z = fmaf(w, x.z, y.z); y.w = fmaf(w, x.w, y.w); };
   for (int k0 = part; k0 < n; k0 += 32 * WPR) {
     const int k = k0 + lane * WPR;
     float w = 0.f;
@@ -140,17 +141,25 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
     }
     const int lim = min(32, (n - k0 + WPR - 1) / WPR);
     for (int u0 = 0; u0 < lim; u0 += 8) {
+      float4 x[8][2];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (32 * e >= P.dh) break;
-        float x[8];
+      for (int u = 0; u < 8; ++u) {
+        const long long au = __shfl_sync(FULL, at, (u0 + u) & 31);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const long long au = __shfl_sync(FULL, at, (u0 + u) & 31);
-          x[u] = u0 + u < lim && au >= 0 && lane + 32 * e < P.dh ? P.part_o[au * P.dh + lane + 32 * e] : 0.f;
+        for (int v = 0; v < 2; ++v) {
+          const int e = e0 + 128 * v;
+          x[u][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (u0 + u >= lim || au < 0 || e >= P.dh) continue;
+          const float* const src = P.part_o + au * P.dh + e;
+          if (vec) x[u][v] = *(const float4*)src;
+          else x[u][v] = make_float4(src[0], e + 1 < P.dh ? src[1] : 0.f, e + 2 < P.dh ? src[2] : 0.f, e + 3 < P.dh ? src[3] : 0.f);
         }
+      }
 #pragma unroll
-        for (int u = 0; u < 8; ++u) o[e] = fmaf(__shfl_sync(FULL, w, (u0 + u) & 31), x[u], o[e]);
+      for (int u = 0; u < 8; ++u) {
+        const float wu = __shfl_sync(FULL, w, (u0 + u) & 31);
+        add(o[0], wu, x[u][0]);
+        add(o[1], wu, x[u][1]);
       }
     }
   }
@@ -158,32 +167,34 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(FULL, l, off);
   if (WPR > 1) {
     if (lane == 0) { s_l[warp] = l; s_m[warp] = M; }
-#pragma unroll
-    for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) s_o[warp][lane + 32 * e] = o[e];
+    *(float4*)&s_o[warp][e0] = o[0];
+    *(float4*)&s_o[warp][e0 + 128] = o[1];
     __syncthreads();
     if (part != 0 || !mine) return;
     float top = M;
 #pragma unroll
     for (int w = 1; w < WPR; ++w) top = fmaxf(top, s_m[warp + w]);
-    float f = M == NINF ? 0.f : exp2f(M - top);
-    l *= f;
+    l = 0.f;
+    o[0] = o[1] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] *= f;
-#pragma unroll
-    for (int w = 1; w < WPR; ++w) {
+    for (int w = 0; w < WPR; ++w) {
       if (s_m[warp + w] == NINF) continue;
-      f = exp2f(s_m[warp + w] - top);
+      const float f = exp2f(s_m[warp + w] - top);
       l = fmaf(f, s_l[warp + w], l);
-#pragma unroll
-      for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) o[e] = fmaf(f, s_o[warp + w][lane + 32 * e], o[e]);
+      add(o[0], f, *(const float4*)&s_o[warp + w][e0]);
+      add(o[1], f, *(const float4*)&s_o[warp + w][e0 + 128]);
     }
     M = top;
   }
   // no weight at all: zeros for a row without tokens, NaN for one whose tokens are all at -inf
   const float inv = l == 0.f ? (M == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / l;
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (lane + 32 * e < P.dh) ((T*)P.out)[out + lane + 32 * e] = rr_from_f32<T>(o[e] * inv);
+  for (int v = 0; v < 2; ++v) {
+    const float y[4] = {o[v].x, o[v].y, o[v].z, o[v].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (e0 + 128 * v + j < P.dh) ((T*)P.out)[out + e0 + 128 * v + j] = rr_from_f32<T>(y[j] * inv);
+  }
 }
 
 // ---- segments on the ordinary pipes --------------------------------------------------------------------------

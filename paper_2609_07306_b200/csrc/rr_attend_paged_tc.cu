@@ -99,7 +99,7 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
         "=r"(r[31])
       : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
@@ -254,106 +254,116 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         if (!ok) break;
         s_cnt += h;
         tc_fence_after();
-        if (warp_live) {
-          // The columns of this warp: all 64 of the half, or 16 of a quartered segment.  First their logits and which of them the row
-          // sees, a bit each.
-          uint32_t x[2][32];
-          float top;
-          const int* const ids = c->ids[cnt % IDS] + 64 * h;
-          if (quart) {
-            tmem_ld16(s_tm + h * 64 + quarter * 16, x[0]);
-            if (!masked) {
-              seen = true;
-            } else {
+        const int* const ids = c->ids[cnt % IDS] + 64 * h;
+        // The reference goes up with the largest logit, and what is there is scaled down (ref = -inf: the first finite maximum).
+        auto follow = [&](float top) -> bool {
+          const float m = live && top != NINF ? top * P.scale_log2 : NINF;
+          if (!__any_sync(FULL, m > ref + GROWTH)) return true;
+          const float now = m > ref + GROWTH ? m : ref, f = now == ref ? 1.f : ex2(ref - now);
+          ref = now;
+          sum *= f;
+          if (k == 0) return true;
+          // the product with the half before may be under way (the one before that is not: this half's logits stand behind it)
+          if (!__all_sync(FULL, mbar_wait(&c->o_done[st][h ^ 1], (o_cnt + ((k - 1) >> 1)) & 1, abort_flag))) return false;
+          tc_fence_after();
+#pragma unroll 1
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32];
+            tmem_ld32(o_tm + i * 32, o);
+            tmem_ld_wait();
+            tie(o);
 #pragma unroll
-              for (int j = 0; j < 16; j += 4) {
-                const int4 id = *reinterpret_cast<const int4*>(ids + quarter * 16 + j);
-                const int e[4] = {id.x, id.y, id.z, id.w};
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                  const bool sees = e[w] < limit;
-                  seen = seen || sees;
-                  mixed = mixed || (!sees && e[w] != NO_TOKEN);
-                  if (!sees) x[0][j + w] = 0xFF800000u;
-                }
-              }
-            }
-            top = __uint_as_float(x[0][0]);
-#pragma unroll
-            for (int j = 1; j < 15; j += 2) top = max3(top, __uint_as_float(x[0][j]), __uint_as_float(x[0][j + 1]));
-            top = fmaxf(top, __uint_as_float(x[0][15]));
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_st_32x32(o_tm + i * 32, o);
+          }
+          return true;
+        };
+        if (quart) {
+          // 16 of the 64 columns; the others weigh nothing for this copy of the rows
+          uint32_t x[16], p[16];
+          tmem_ld16(s_tm + h * 64 + quarter * 16, x);
+          if (!masked) {
+            seen = true;
           } else {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) tmem_ld32(s_tm + h * 64 + i * 32, x[i]);
-            tmem_ld_wait();
+            for (int j = 0; j < 16; ++j) {
+              const int id = ids[quarter * 16 + j];
+              const bool sees = id < limit;
+              seen = seen || sees;
+              if (!sees) x[j] = 0xFF800000u;
+            }
+          }
+          float top = __uint_as_float(x[0]);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) tie(x[i]);
-            if (!masked) {
-              seen = true;
-            } else {                                     // which columns the row sees, a bit each
-              uint32_t see[2] = {0, 0};
-              if (i0.w && i1.w && i0.z <= i1.y) {
-                int n = 0;                               // ids ascend (every list in order, no bad page inside): the first n columns
+          for (int j = 1; j < 15; j += 2) top = max3(top, __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
+          ok = follow(fmaxf(top, __uint_as_float(x[15])));
+          if (!ok) break;
+          const float sub = ref == NINF ? 0.f : ref;
+          float part = 0.f;
 #pragma unroll
-                for (int step = 32; step; step >>= 1) if (ids[n + step - 1] < limit) n += step;
-                n += ids[n] < limit;
-                mixed = mixed || (n < 64 && ids[min(n, 63)] != NO_TOKEN);
-                see[0] = n >= 32 ? FULL : (1u << n) - 1;
-                see[1] = n >= 64 ? FULL : n <= 32 ? 0u : (1u << (n - 32)) - 1;
-              } else {
+          for (int j = 0; j < 8; ++j) {
+            const float e0 = ex2(fmaf(__uint_as_float(x[2 * j]), P.scale_log2, -sub)), e1 = ex2(fmaf(__uint_as_float(x[2 * j + 1]), P.scale_log2, -sub));
+            part += e0 + e1;
+            p[j] = pack(e0, e1);
+            p[8 + j] = 0;
+          }
+          sum += part;
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll 4
-                  for (int j = 0; j < 32; ++j) {
-                    const int id = ids[i * 32 + j];
-                    if (id < limit) see[i] |= 1u << j;
-                    else mixed = mixed || id != NO_TOKEN;
-                  }
-              }
-              seen = seen || (see[0] | see[1]) != 0;
+          for (int w = 0; w < 4; ++w) if (w == quarter) tmem_st8(s_tm + h * 64 + w * 8, p); else tmem_st8(s_tm + h * 64 + w * 8, p + 8);
+          tmem_st_wait();
+        } else if (warp_live) {
+          uint32_t x[2][32];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) tmem_ld32(s_tm + h * 64 + i * 32, x[i]);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 2; ++i) tie(x[i]);
+          if (!masked) {
+            seen = true;
+          } else {                                     // which columns the row sees, a bit each
+            uint32_t see[2] = {0, 0};
+            if (i0.w && i1.w && i0.z <= i1.y) {
+              int n = 0;                               // ids ascend (every list in order, no bad page inside): the first n columns
+#pragma unroll
+              for (int step = 32; step; step >>= 1) if (ids[n + step - 1] < limit) n += step;
+              n += ids[n] < limit;
+              mixed = mixed || (n < 64 && ids[min(n, 63)] != NO_TOKEN);
+              see[0] = n >= 32 ? FULL : (1u << n) - 1;
+              see[1] = n >= 64 ? FULL : n <= 32 ? 0u : (1u << (n - 32)) - 1;
+            } else {
 #pragma unroll
               for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 32; ++j) if (!(see[i] >> j & 1)) x[i][j] = 0xFF800000u;
+#pragma unroll 4
+                for (int j = 0; j < 32; ++j) {
+                  const int id = ids[i * 32 + j];
+                  if (id < limit) see[i] |= 1u << j;
+                  else mixed = mixed || id != NO_TOKEN;
+                }
             }
-            float t[4];                                  // (four chains)
+            seen = seen || (see[0] | see[1]) != 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t* const y = &x[i >> 1][(i & 1) * 16];
-              t[i] = __uint_as_float(y[0]);
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-              for (int j = 1; j < 15; j += 2) t[i] = max3(t[i], __uint_as_float(y[j]), __uint_as_float(y[j + 1]));
-              t[i] = fmaxf(t[i], __uint_as_float(y[15]));
-            }
-            top = fmaxf(max3(t[0], t[1], t[2]), t[3]);
+              for (int j = 0; j < 32; ++j) if (!(see[i] >> j & 1)) x[i][j] = 0xFF800000u;
           }
-          const float m = live && top != NINF ? top * P.scale_log2 : NINF;
-          if (__any_sync(FULL, m > ref + GROWTH)) {    // (ref = -inf: the first finite maximum)
-            const float now = m > ref + GROWTH ? m : ref, f = now == ref ? 1.f : ex2(ref - now);
-            ref = now;
-            sum *= f;
-            if (k > 0) {
-              // the product with the half before may be under way (the one before that is not: this half's logits stand behind it)
-              ok = __all_sync(FULL, mbar_wait(&c->o_done[st][h ^ 1], (o_cnt + ((k - 1) >> 1)) & 1, abort_flag));
-              if (!ok) break;
-              tc_fence_after();
-#pragma unroll 1
-              for (int i = 0; i < D / 32; ++i) {
-                uint32_t o[32];
-                tmem_ld32(o_tm + i * 32, o);
-                tmem_ld_wait();
-                tie(o);
+          float t[4];                                  // (four chains)
 #pragma unroll
-                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                tmem_st_32x32(o_tm + i * 32, o);
-              }
-            }
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t* const y = &x[i >> 1][(i & 1) * 16];
+            t[i] = __uint_as_float(y[0]);
+#pragma unroll
+            for (int j = 1; j < 15; j += 2) t[i] = max3(t[i], __uint_as_float(y[j]), __uint_as_float(y[j + 1]));
+            t[i] = fmaxf(t[i], __uint_as_float(y[15]));
           }
+          ok = follow(fmaxf(max3(t[0], t[1], t[2]), t[3]));
+          if (!ok) break;
           const float sub = ref == NINF ? 0.f : ref;
           const uint64_t scale2 = two(P.scale_log2, P.scale_log2), sub2 = two(-sub, -sub);
           uint64_t a[2] = {0, 0};
           uint32_t p[32];
-          auto weight = [&](const uint32_t* y, int j) -> uint32_t {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const uint32_t* const y = &x[j / 16][2 * (j % 16)];
             const uint64_t v = fma2(two(__uint_as_float(y[0]), __uint_as_float(y[1])), scale2, sub2);
             uint64_t e;
             if (j % 8 < BY_FMA) {
@@ -366,24 +376,12 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
             a[j & 1] = add2(a[j & 1], e);
             float e0, e1;
             split(e, e0, e1);
-            return pack(e0, e1);
-          };
-          if (quart) {                                 // the other quarters' columns weigh nothing for this copy of the rows
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = weight(&x[0][2 * j], j + 1);
-#pragma unroll
-            for (int j = 8; j < 16; ++j) p[j] = 0;
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-              if (w == quarter) tmem_st8(s_tm + h * 64 + w * 8, p); else tmem_st8(s_tm + h * 64 + w * 8, p + 8);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) p[j] = weight(&x[j / 16][2 * (j % 16)], j);
-            tmem_st_32x32(s_tm + h * 64, p);
+            p[j] = pack(e0, e1);
           }
           float s0, s1;
           split(add2(a[0], a[1]), s0, s1);
           sum += s0 + s1;
+          tmem_st_32x32(s_tm + h * 64, p);
           tmem_st_wait();
         }
         tc_fence_before();
