@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
         cnt1 = cta_of(P, first + no - 1, all) - c1 + 1;
         st1 = partials_of(P.streams, min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS));
       }
-      if (no > 0 && P.tc && np == 0 && cnt1 == 1 && st1 == 1) mine = false;      // (one segment with all of the row's tiles wrote the output itself)
+      if (no > 0 && np == 0 && cnt1 == 1 && st1 == 1) mine = false;      // (one segment with all of the row's tiles wrote the output itself)
     }
   } else {
     const int mg = P.m * P.group;
@@ -105,19 +105,25 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
     const long long rr = quot(mine ? row : 0, mg), per = quot(rr, P.n_q);
     const int idx = (int)((mine ? row : 0) - rr * mg), i = (int)(rr - per * P.n_q), r = (int)per % P.route_heads, b = (int)per / P.route_heads;
     st0 = partials_of(P.streams, min(ROWS, mg - idx / ROWS * ROWS));
-    mine = mine && !(P.direct && st0 == 1);
     home0 = row;
-    cnt0 = mine ? P.splits : 0;
+    cnt0 = 1;
+    if (P.units) {
+      const long long W = range_units(P), first = (rr * ((mg + ROWS - 1) / ROWS) + idx / ROWS) * P.units;
+      c0 = cta_of(P, first, W);
+      cnt0 = cta_of(P, first + P.units - 1, W) - c0 + 1;
+      r0 = idx % ROWS;
+    }
+    if (cnt0 == 1 && st0 == 1) mine = false;           // (one segment with all of the row's tiles wrote the output itself)
     out = b * P.ob + (r * P.group + idx % P.group) * P.oh + (i * P.m + idx / P.group) * P.ot;
   }
   if (WPR == 1 && !mine) return;
   const int n0 = cnt0 * st0, n = n0 + cnt1 * st1;
-  const long long cta_rows = 2 * (long long)P.tokens * H, split_rows = P.slots ? P.range_rows * P.m * P.group : 0;
+  const long long cta_rows = P.slots ? P.range_rows * P.m * P.group : 2 * (long long)P.tokens * H;
   auto place = [&](int k) -> long long {               // partial row of the k-th partial
     const bool w = k >= n0;
     if (w) k -= n0;
     const int s = w ? st1 : st0, c = k / s;
-    const long long at = P.slots ? home0 + c * split_rows : c == 0 ? (w ? home1 : home0) : cta_rows + (long long)((w ? c1 : c0) + c) * ROWS + (w ? r1 : r0);
+    const long long at = c == 0 ? (w ? home1 : home0) : cta_rows + (long long)((w ? c1 : c0) + c) * ROWS + (w ? r1 : r0);
     return (k - c * s) * P.part_rows + at;
   };
   float M = NINF;
@@ -397,7 +403,7 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
     if (any && m[i] == NINF) m[i] = LOWEST;
     const RowAt a = row_at(P, s, r0 + r);
     const long long at = s.part + r0 + r;
-    if (!P.direct && tx == 0) P.part_ml[at] = make_float2(m[i], sum);
+    if (!s.whole && tx == 0) P.part_ml[at] = make_float2(m[i], sum);
     const float inv = sum == 0.f ? (m[i] == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / sum;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -406,7 +412,7 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (e + u < dh) {
-          if (P.direct) ((T*)P.out)[out_at(P, s, a) + e + u] = rr_from_f32<T>(y[u] * inv);
+          if (s.whole) ((T*)P.out)[out_at(P, s, a) + e + u] = rr_from_f32<T>(y[u] * inv);
           else P.part_o[at * dh + e + u] = y[u];
         }
     }
@@ -419,12 +425,12 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
     const int lane = tid & 31;
     const RowAt a = row_at(P, s, r0 + r);
     const long long at = s.part + r0 + r;
-    if (!P.direct && lane == 0) P.part_ml[at] = make_float2(mm, ll);
+    if (!s.whole && lane == 0) P.part_ml[at] = make_float2(mm, ll);
     const float inv = ll == 0.f ? (mm == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / ll;
 #pragma unroll
     for (int e = 0; e < RR_PAGED_MAX_DH / 32; ++e)
       if (lane + 32 * e < dh) {
-        if (P.direct) ((T*)P.out)[out_at(P, s, a) + lane + 32 * e] = rr_from_f32<T>(oo[e] * inv);
+        if (s.whole) ((T*)P.out)[out_at(P, s, a) + lane + 32 * e] = rr_from_f32<T>(oo[e] * inv);
         else P.part_o[at * dh + lane + 32 * e] = oo[e];
       }
   }
@@ -579,7 +585,7 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
       o = fmaf(f, s_part[(w * R + r) * ROW + e], o);
     }
     const long long at = s.part + r0 + r;
-    if (P.direct) {
+    if (s.whole) {
       const float inv = L == 0.f ? (M == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / L;
       ((T*)P.out)[out_at(P, s, row_at(P, s, r0 + r)) + e] = rr_from_f32<T>(o * inv);
     } else {
@@ -607,13 +613,15 @@ __global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) att
   c.n_tok = 0; c.vq = vq; c.vk = vk;
   const int lane = threadIdx.x & 31, mg = P.m * P.group;
   long long u, u0 = 0, u1;
-  if (P.slots) { u = blockIdx.x; u1 = P.range_rows * ((mg + ROWS - 1) / ROWS) * P.splits; }
-  else { const long long W = __ldg(P.cum + P.batch); u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
+  const bool turns = P.slots && !P.units;              // whole items in turn
+  const long long W = P.slots ? range_units(P) : __ldg(P.cum + P.batch);
+  if (turns) { u = blockIdx.x; u1 = W; }
+  else { u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
   while (u < u1) {
     Seg s;
     if (P.slots) {
-      range_segment(P, u, s);
-      u += gridDim.x;
+      const int took = range_segment(P, blockIdx.x, u, u1, s);
+      u += turns ? gridDim.x : took;
       __syncthreads();                                 // the table before is no longer read
       if (threadIdx.x < 32) {
         int run = 0;
@@ -631,7 +639,7 @@ __global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) att
       }
       __syncthreads();
       c.n_tok = c.first[P.slots];
-      split_tiles(P, (c.n_tok + TILE - 1) / TILE, s);
+      unit_tiles(P, (c.n_tok + TILE - 1) / TILE, s);
     } else {
       u += segment_at(P, blockIdx.x, u, u0, u1, s);
       c.n_tok = s.tok1 - s.tok0;
@@ -726,7 +734,6 @@ int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   P.qt = a->q_token_stride; P.qh = a->q_head_stride; P.ot = a->out_token_stride; P.oh = a->out_head_stride;
   P.tokens = a->tokens; P.heads = a->heads; P.group = a->heads / kv->kv_heads; P.causal = a->causal; P.prefix = a->prefix_tokens;
   P.scale_log2 = a->scale * 1.4426950408889634f;
-  P.splits = 1;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
   P.ctas = rr_sm_count() * (P.tc ? 1 : 2);
   P.part_rows = 2LL * P.tokens * P.heads + (long long)P.ctas * ROWS;
@@ -757,16 +764,13 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.range_rows = (long long)kv->batch * a->route_heads * a->n_q;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
   P.ctas = rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 4 : 2);
-  // few rows: each is cut into parts, so that every SM has one
   const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS);
-  P.splits = (int)(items >= P.ctas ? 1 : P.ctas / items);
-  if (P.splits > 64) P.splits = 64;
-  P.direct = P.splits == 1;
-  P.part_rows = P.splits * P.range_rows * P.m * P.group;
+  P.units = items < 8LL * P.ctas ? UNITS : 0;
+  P.part_rows = P.range_rows * P.m * P.group + (long long)P.ctas * ROWS;
   P.streams = streams_of(P);
-  // (direct: an item whose rows have one partial needs none; the last item of a range row may have fewer rows than the others)
+  // (nothing to join: whole items, whose rows have one partial each; the last item of a range row may have fewer rows than the others)
   const int mg = P.m * P.group, last = mg % ROWS;
-  if (P.direct && partials_of(P.streams, std::min(mg, ROWS)) == 1 && (last == 0 || partials_of(P.streams, last) == 1)) P.part_rows = 0;
+  if (!P.units && partials_of(P.streams, std::min(mg, ROWS)) == 1 && (last == 0 || partials_of(P.streams, last) == 1)) P.part_rows = 0;
   return RR_OK;
 }
 
@@ -780,7 +784,7 @@ int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, co
   if (!P.slots) { e = rr_launch_pdl(plan_kernel, 1, PLAN_NT, 0, st, P); ++launches; }
   if (e == cudaSuccess) {
     long long grid = P.ctas;
-    if (P.slots) grid = std::min<long long>(grid, P.range_rows * ceil_div((long long)P.m * P.group, ROWS) * P.splits);
+    if (P.slots && !P.units) grid = std::min<long long>(grid, P.range_rows * ceil_div((long long)P.m * P.group, ROWS));
     if (P.tc) e = rr_launch_attend_tc(P, (int)grid, st);
     else e = dtype == RR_BF16 ? launch_simt<__nv_bfloat16>(P, (int)grid, st) : launch_simt<float>(P, (int)grid, st);
     ++launches;

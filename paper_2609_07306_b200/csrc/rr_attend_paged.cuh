@@ -17,13 +17,15 @@
 // CTA's share may span many items), so neither a long prefix of few rows nor one long sequence among short ones leaves SMs idle.
 // plan_kernel counts the tiles on the device, where the lengths are.  A segment that begins its item has its partial rows at
 // the rows' own places; a CTA has at most one segment that does not, whose rows go to the CTA's own ROWS places.
-// ranges: items are alike, and each is cut into `splits` parts by its own number of tiles.
+// ranges: items are alike.  Where there are fewer than eight per CTA each counts as UNITS units that the CTAs share equally, as the tiles above (a
+// segment has the tiles of its units by the item's own number of tiles); where there are more, CTAs take whole items in turn, so that
+// neighbouring rows, whose routes overlap, are read at the same time.
 #pragma once
 #include "rr_paged.cuh"
 
 namespace rrattn {
 
-constexpr int TILE = 128, ROWS = 256;
+constexpr int TILE = 128, ROWS = 256, UNITS = 64;
 constexpr int NO_TOKEN = 0x7FFFFFFF;                   // id of a place without a token: above every limit
 constexpr float NINF = -__builtin_huge_valf();
 constexpr float LOWEST = -3.402823466e38f;             // m of a row that saw tokens, all of them at -inf
@@ -45,14 +47,13 @@ struct Params {
   int n_q, m, slots, route_heads;                      // ranges (slots > 0)
   float scale_log2;                                    // scale * log2 e
   // schedule
-  int tc, ctas, splits, streams;                       // streams: most partials of a segment's row (see partials_of)
+  int tc, ctas, units, streams;                        // units: of a ranges item (0: whole items in turn); streams: most partials of a segment's row
   long long range_rows;                                // batch * route_heads * n_q
   // workspace
   long long* cum;                                      // shared: [batch + 2] tiles before sequence b's items; [batch] = all tiles; [batch + 1] = apart
   float* part_o;                                       // [streams][part_rows][dh]
   float2* part_ml;                                     // [streams][part_rows]
   long long part_rows;
-  int direct;                                          // ranges, splits == 1: no partials where one stream has the row
 };
 
 struct Seg {
@@ -66,8 +67,8 @@ struct Seg {
   int prefix;
   bool whole;                                          // all tiles of the rows' only item: nothing to join
   const int32_t* slots;                                // ranges: the row's slots, else null
-  int tile0, tile1;                                    // the segment's tiles of the list (ranges: of `split`, once counted)
-  int split;
+  int tile0, tile1;                                    // the segment's tiles of the list (ranges: once counted)
+  int unit0, unit1;                                    // ranges: the segment's units of the item's `units` (of 1 if whole)
   long long part;                                      // partial row of row 0
 };
 
@@ -114,7 +115,6 @@ __device__ __forceinline__ int segment_at(const Params& P, int c, long long u, l
   long long home;
   const long long row_all = (long long)P.tokens * P.group;
   s.slots = nullptr;
-  s.split = 0;
   s.prefix_pages = P.prefix_pages ? P.prefix_pages : P.table;
   s.prefix = P.prefix;
   if (u < before) {
@@ -159,11 +159,14 @@ __device__ __forceinline__ int segment_at(const Params& P, int c, long long u, l
   return took;
 }
 
-// Segment x of a ranges call (x < range_rows * row tiles * splits); its tiles are counted by who reads the slots.
-__device__ __forceinline__ void range_segment(const Params& P, long long x, Seg& s) {
-  const int mg = P.m * P.group, qt = (mg + ROWS - 1) / ROWS;
-  const long long item = quot(x, P.splits), row = quot(item, qt);
-  s.split = (int)(x - item * P.splits);
+// The segment at unit u (item u, if they are taken whole) of CTA c's share of a ranges call; its tiles are counted by who reads the
+// slots.  Returns how many units it takes.
+__device__ __forceinline__ int range_segment(const Params& P, int c, long long u, long long u1, Seg& s) {
+  const int mg = P.m * P.group, qt = (mg + ROWS - 1) / ROWS, n = P.units ? P.units : 1;
+  const long long item = quot(u, n), row = quot(item, qt), all = P.range_rows * mg;
+  s.unit0 = (int)(u - item * n);
+  s.unit1 = (int)min((long long)n, u1 - item * n);
+  s.whole = s.unit1 - s.unit0 == n;
   s.row0 = (int)(item - row * qt) * ROWS;
   s.rows = min(ROWS, mg - s.row0);
   const int per = (int)quot(row, P.n_q), i = (int)(row - (long long)per * P.n_q), r = per % P.route_heads;
@@ -176,15 +179,17 @@ __device__ __forceinline__ void range_segment(const Params& P, long long x, Seg&
   s.pages = P.table + s.b * P.table_stride;
   s.slots = P.ranges + row * P.slots * 2;
   s.prefix = 0;
-  s.whole = false;
   s.tile0 = s.tile1 = 0;
-  s.part = (s.split * P.range_rows + row) * mg + s.row0;
+  s.part = s.unit0 == 0 ? row * mg + s.row0 : all + (long long)c * ROWS;
+  return s.unit1 - s.unit0;
 }
-// The part of `tiles` tiles that split s has.
-__device__ __forceinline__ void split_tiles(const Params& P, int tiles, Seg& s) {
-  s.tile0 = (int)((long long)tiles * s.split / P.splits);
-  s.tile1 = (int)((long long)tiles * (s.split + 1) / P.splits);
+__device__ __forceinline__ void unit_tiles(const Params& P, int tiles, Seg& s) {
+  const int n = P.units ? P.units : 1;
+  s.tile0 = (int)((long long)tiles * s.unit0 / n);
+  s.tile1 = (int)((long long)tiles * s.unit1 / n);
 }
+// The units or tiles of all items: a ranges call's are known to the host.
+__device__ __forceinline__ long long range_units(const Params& P) { return P.range_rows * ((P.m * P.group + ROWS - 1) / ROWS) * (P.units ? P.units : 1); }
 // Tokens of one slot: [lo, hi) clipped to the sequence.
 __device__ __forceinline__ void slot_span(const Seg& s, int j, int& lo, int& hi) {
   lo = __ldg(s.slots + 2 * j);

@@ -39,7 +39,7 @@ namespace {
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int NT = 512, IDS = 16, MAX_RING = 4;
 constexpr float GROWTH = 8.f;
-constexpr int BY_FMA = 1;                              // of every 8 pairs of exponentials, by multiply-adds
+constexpr int BY_FMA = 2;                              // of every 8 pairs of exponentials, by multiply-adds
 
 template <int D> struct Shape {
   static constexpr int HALVES = D / 64, STAGES = D == 128 ? 4 : 8;
@@ -200,7 +200,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::STAGES; ++i) { mbar_init(&c->full[i], 4); mbar_init(&c->empty[i], 2); }
     for (int i = 0; i < 2; ++i) {
-      for (int h = 0; h < 2; ++h) { mbar_init(&c->s_full[i][h], 1); mbar_init(&c->p_full[i][h], 128); mbar_init(&c->o_done[i][h], 1); }
+      for (int h = 0; h < 2; ++h) { mbar_init(&c->s_full[i][h], 2); mbar_init(&c->p_full[i][h], 128); mbar_init(&c->o_done[i][h], 1); }
       mbar_init(&c->q_full[i], 4); mbar_init(&c->q_empty[i], 2);
     }
     for (int i = 0; i < IDS; ++i) mbar_init(&c->ids_full[i], 4);
@@ -247,10 +247,8 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
       bool seen = false, mixed = false;
       for (int k = 0; ok && k < 2 * steps; ++k) {      // half a tile, 64 tokens, at a time
         const int h = k & 1, cnt = tiles + (paired ? k >> 1 : (k & ~1) + st);
-        if (h == 0) ok = __all_sync(FULL, mbar_wait(&c->ids_full[cnt % IDS], cnt / IDS & 1, abort_flag));
-        const int4 i0 = c->info[cnt % IDS][2 * h], i1 = c->info[cnt % IDS][2 * h + 1];
-        const bool masked = __any_sync(FULL, live && max(i0.x, i1.x) >= limit);
-        ok = ok && __all_sync(FULL, mbar_wait(&c->s_full[st][h], s_cnt & 1, abort_flag));
+        // (the issuing warp has waited for the tile's ids before it issued the first half's logits)
+        ok = __all_sync(FULL, mbar_wait(&c->s_full[st][h], s_cnt & 1, abort_flag));
         if (!ok) break;
         s_cnt += h;
         tc_fence_after();
@@ -281,8 +279,9 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         if (quart) {
           // 16 of the 64 columns; the others weigh nothing for this copy of the rows
           uint32_t x[16], p[16];
+          const int top_id = max(c->info[cnt % IDS][2 * h].x, c->info[cnt % IDS][2 * h + 1].x);
           tmem_ld16(s_tm + h * 64 + quarter * 16, x);
-          if (!masked) {
+          if (!__any_sync(FULL, live && top_id >= limit)) {
             seen = true;
           } else {
 #pragma unroll
@@ -315,6 +314,8 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           uint32_t x[2][32];
 #pragma unroll
           for (int i = 0; i < 2; ++i) tmem_ld32(s_tm + h * 64 + i * 32, x[i]);
+          const int4 i0 = c->info[cnt % IDS][2 * h], i1 = c->info[cnt % IDS][2 * h + 1];
+          const bool masked = __any_sync(FULL, live && max(i0.x, i1.x) >= limit);
           tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < 2; ++i) tie(x[i]);
@@ -395,7 +396,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         if (!ok) break;
         tc_fence_after();
       }
-      const bool direct = paired && (P.direct || s.whole);
+      const bool direct = paired && s.whole;
       if (warp_live) {
         if (seen && ref == NINF) ref = LOWEST;
         const long long at = (paired ? 0 : quart ? (st * 4 + quarter) * P.part_rows : st * P.part_rows) + s.part + r;
@@ -499,13 +500,15 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
     if (warp == 9) {
       // ===== the segments =====
       long long u, u0 = 0, u1;
-      if (P.slots) { u = blockIdx.x; u1 = P.range_rows * ((P.m * P.group + ROWS - 1) / ROWS) * P.splits; }
-      else { const long long W = __ldg(P.cum + P.batch); u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
+      const bool turns = P.slots && !P.units;          // whole items in turn
+      const long long W = P.slots ? range_units(P) : __ldg(P.cum + P.batch);
+      if (turns) { u = blockIdx.x; u1 = W; }
+      else { u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
       for (int n = 0;; ++n) {
         Seg s;
         const bool end = u >= u1;
         if (end) { s.rows = 0; }
-        else if (P.slots) { range_segment(P, u, s); u += gridDim.x; }
+        else if (P.slots) { const int took = range_segment(P, blockIdx.x, u, u1, s); u += turns ? gridDim.x : took; }
         else u += segment_at(P, blockIdx.x, u, u0, u1, s);
         if (!__all_sync(FULL, mbar_wait_spin(&c->seg_empty[n % ring], (n / ring & 1) ^ 1, abort_flag))) break;
         if (!end && P.slots) {                           // number the row's tokens
@@ -523,7 +526,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
             run += __shfl_sync(FULL, incl, 31);
           }
           if (lane == 0) first[P.slots] = run;
-          split_tiles(P, (run + TILE - 1) / TILE, s);
+          unit_tiles(P, (run + TILE - 1) / TILE, s);
         }
         if (lane == 0) c->seg[n % ring] = s;
         __syncwarp();
@@ -747,13 +750,19 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
               umma_commit_warp(&c->o_done[st][h]);
             }
             if (k < steps) {
-              if (h == 0) { ok = wait(&c->full[sk], fk / S::STAGES); if (!ok) break; tc_fence_after(); }
+              if (h == 0) {
+                const int cnt = (int)tiles + tk;
+                ok = wait(&c->full[sk], fk / S::STAGES) && wait(&c->ids_full[cnt % IDS], cnt / IDS);
+                if (!ok) break;
+                tc_fence_after();
+              }
               const uint64_t kd = umma_desc_k_sw128(kv_addr + sk * S::TILE_BYTES + h * 64 * 128);
 #pragma unroll
               for (int j = 0; j < D / 16; ++j) {
                 const uint64_t o = (uint64_t)((j >> 2) * (S::HALF_BYTES >> 4) + (j & 3) * 2);
                 umma_bf16_warp(s_tm + h * 64, qd + o, kd + o, idesc_s, j > 0 ? 1u : 0u);
               }
+              if (lane == 0) mbar_arrive(&c->s_full[st][h]);   // (passes on the ids' arrival)
               umma_commit_warp(&c->s_full[st][h]);
             }
           }
