@@ -32,23 +32,36 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
   const long long packed = prefix_row_tiles(P);
   const bool apart = row_tiles <= packed + packed / 8;
   __syncthreads();
-  long long run = apart ? 0 : P.kv_heads * packed * prefix_tiles(P);
-  for (int b0 = 0; b0 < P.batch; b0 += PLAN_NT) {
-    const int b = b0 + tid;
-    const long long mine = b < P.batch ? (long long)P.kv_heads * own_row_tiles(P, b) * own_tiles(P, b, apart) : 0;
+  long long run = apart ? 0 : P.kv_heads * packed * prefix_tiles(P), run_few = 0;
+  auto scan = [&](long long mine, long long& run) -> long long {     // what is before this thread's, the block's sum added to run
     long long incl = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) { const long long x = __shfl_up_sync(FULL, incl, off); if (lane >= off) incl += x; }
     if (lane == 31) s_warp[warp] = incl;
     __syncthreads();
-    long long before = 0, all = 0;
+    long long before = run, all = 0;
 #pragma unroll
     for (int w = 0; w < PLAN_NT / 32; ++w) { if (w < warp) before += s_warp[w]; all += s_warp[w]; }
-    if (b < P.batch) P.cum[b] = run + before + incl - mine;
     run += all;
     __syncthreads();
+    return before + incl - mine;
+  };
+  for (int b0 = 0; b0 < P.batch; b0 += PLAN_NT) {
+    const int b = b0 + tid;
+    const bool few = b < P.batch && few_rows_of(P, b);
+    const long long mine = b < P.batch ? (long long)P.kv_heads * own_row_tiles(P, b) * own_tiles(P, b, apart) : 0;
+    const long long at = scan(few ? 0 : mine, run);
+    if (b < P.batch) P.main.cum[b] = at;
+    if (P.few.ctas > 0) {
+      const long long at_few = scan(few ? mine : 0, run_few);
+      if (b < P.batch) P.few.cum[b] = at_few;
+    }
   }
-  if (tid == 0) { P.cum[P.batch] = run; P.cum[P.batch + 1] = apart; }
+  if (tid == 0) {
+    P.main.cum[P.batch] = run;
+    if (P.few.ctas > 0) P.few.cum[P.batch] = run_few;
+    *P.apart = apart;
+  }
 }
 
 // ---- join --------------------------------------------------------------------------------------------------
@@ -67,35 +80,37 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   long long home0 = 0, home1 = 0;
   int c0 = 0, c1 = 0, cnt0 = 0, cnt1 = 0, st0 = 1, st1 = 1, r0 = 0, r1 = 0;
   long long out = 0;
-  bool mine = true;
+  bool mine = true, few1 = false;
   if (P.slots == 0) {
     mine = row < (long long)P.tokens * H;
     const int t = (int)quot(mine ? row : 0, H), h = (int)((mine ? row : 0) - (long long)t * H), kvh = h / P.group, g = h - kvh * P.group;
     const int b = P.cu ? rr_sequence_of_warp(P.cu, P.batch, t) : t;
     mine = mine && b >= 0;                             // (padding: left as it was)
     if (mine) {
-      const long long all = __ldg(P.cum + P.batch), per = (long long)P.tokens * P.group;
+      const long long all = __ldg(P.main.cum + P.batch), per = (long long)P.tokens * P.group;
       out = t * P.ot + h * P.oh;
-      const bool apart = __ldg(P.cum + P.batch + 1) != 0;
+      const bool apart = __ldg(P.apart) != 0;
       const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P);
       if (np > 0) {
         const long long idx = (long long)t * P.group + g, first = (kvh * qtp + idx / ROWS) * np;
         home0 = kvh * per + idx;
         r0 = (int)(idx % ROWS);
-        c0 = cta_of(P, first, all);
-        cnt0 = cta_of(P, first + np - 1, all) - c0 + 1;
+        c0 = cta_of(P.main, first, all);
+        cnt0 = cta_of(P.main, first + np - 1, all) - c0 + 1;
         st0 = partials_of(P.streams, min((long long)ROWS, per - idx / ROWS * ROWS));
       }
       const int no = own_tiles(P, b, apart);
       if (no > 0) {
         const int t0 = seq_first(P, b), n = seq_count(P, b), qt = own_row_tiles(P, b);
         const long long idx = (long long)(t - t0) * P.group + g;
-        const long long first = __ldg(P.cum + b) + (kvh * (long long)qt + idx / ROWS) * no;
+        few1 = few_rows_of(P, b);
+        const Sched& sc = few1 ? P.few : P.main;
+        const long long W = few1 ? __ldg(P.few.cum + P.batch) : all, first = __ldg(sc.cum + b) + (kvh * (long long)qt + idx / ROWS) * no;
         home1 = (P.kv_heads + kvh) * per + (long long)t0 * P.group + idx;
         r1 = (int)(idx % ROWS);
-        c1 = cta_of(P, first, all);
-        cnt1 = cta_of(P, first + no - 1, all) - c1 + 1;
-        st1 = partials_of(P.streams, min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS));
+        c1 = cta_of(sc, first, W);
+        cnt1 = cta_of(sc, first + no - 1, W) - c1 + 1;
+        st1 = few1 ? 1 : partials_of(P.streams, min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS));
       }
       if (no > 0 && np == 0 && cnt1 == 1 && st1 == 1) mine = false;      // (one segment with all of the row's tiles wrote the output itself)
     }
@@ -109,8 +124,9 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
     cnt0 = 1;
     if (P.units) {
       const long long W = range_units(P), first = (rr * ((mg + ROWS - 1) / ROWS) + idx / ROWS) * P.units;
-      c0 = cta_of(P, first, W);
-      cnt0 = cta_of(P, first + P.units - 1, W) - c0 + 1;
+      const Sched& sc = P.few.ctas > 0 ? P.few : P.main;
+      c0 = cta_of(sc, first, W);
+      cnt0 = cta_of(sc, first + P.units - 1, W) - c0 + 1;
       r0 = idx % ROWS;
     }
     if (cnt0 == 1 && st0 == 1) mine = false;           // (one segment with all of the row's tiles wrote the output itself)
@@ -118,12 +134,13 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   }
   if (WPR == 1 && !mine) return;
   const int n0 = cnt0 * st0, n = n0 + cnt1 * st1;
-  const long long cta_rows = P.slots ? P.range_rows * P.m * P.group : 2 * (long long)P.tokens * H;
+  const bool few0 = P.slots && P.few.ctas > 0;
   auto place = [&](int k) -> long long {               // partial row of the k-th partial
     const bool w = k >= n0;
     if (w) k -= n0;
     const int s = w ? st1 : st0, c = k / s;
-    const long long at = c == 0 ? (w ? home1 : home0) : cta_rows + (long long)((w ? c1 : c0) + c) * ROWS + (w ? r1 : r0);
+    const Sched& sc = (w ? few1 : few0) ? P.few : P.main;
+    const long long at = c == 0 ? (w ? home1 : home0) : sc.slots_at + (long long)((w ? c1 : c0) + c) * sc.slot_rows + (w ? r1 : r0);
     return (k - c * s) * P.part_rows + at;
   };
   float M = NINF;
@@ -611,16 +628,16 @@ __global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) att
   c.at = (long long*)(smem + L.ids); c.id = (int*)(c.at + BT);
   c.first = (int*)(smem + L.slots); c.base = c.first + P.slots + 1;
   c.n_tok = 0; c.vq = vq; c.vk = vk;
-  const int lane = threadIdx.x & 31, mg = P.m * P.group;
-  long long u, u0 = 0, u1;
+  const int lane = threadIdx.x & 31;
+  long long u, u1;
   const bool turns = P.slots && !P.units;              // whole items in turn
-  const long long W = P.slots ? range_units(P) : __ldg(P.cum + P.batch);
+  const long long W = P.slots ? range_units(P) : __ldg(P.main.cum + P.batch);
   if (turns) { u = blockIdx.x; u1 = W; }
-  else { u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
+  else { u = share(P.main, blockIdx.x, W); u1 = share(P.main, blockIdx.x + 1, W); }
   while (u < u1) {
     Seg s;
     if (P.slots) {
-      const int took = range_segment(P, blockIdx.x, u, u1, s);
+      const int took = range_segment(P, P.main, blockIdx.x, u, u1, s);
       u += turns ? gridDim.x : took;
       __syncthreads();                                 // the table before is no longer read
       if (threadIdx.x < 32) {
@@ -641,7 +658,7 @@ __global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) att
       c.n_tok = c.first[P.slots];
       unit_tiles(P, (c.n_tok + TILE - 1) / TILE, s);
     } else {
-      u += segment_at(P, blockIdx.x, u, u0, u1, s);
+      u += segment_at(P, P.main, blockIdx.x, u, u1, s);
       c.n_tok = s.tok1 - s.tok0;
     }
     constexpr int LPT = NV == 1 ? 16 : 32, W = NV > 2 ? 2 : 1, R = W == 1 ? 4 : 1, WARPS = (ONLY_FEW ? FEW_NT : SNT) / 32;
@@ -684,10 +701,14 @@ cudaError_t launch_simt(const Params& P, int grid, cudaStream_t st) {
 }
 
 size_t up(size_t x) { return (x + 255) / 256 * 256; }
-// Offsets in the workspace: cum, part_ml, part_o.
+// Offsets in the workspace: the plan, part_ml, part_o.
 size_t lay_out(Params& P, uint8_t* ws) {
   size_t at = 0;
-  P.cum = (long long*)(ws + at); at += up(P.slots ? 0 : (size_t)(P.batch + 2) * 8);
+  if (!P.slots) {
+    P.main.cum = (long long*)(ws + at); at += up((size_t)(P.batch + 1) * 8);
+    P.few.cum = (long long*)(ws + at); at += up((size_t)(P.batch + 1) * 8);
+    P.apart = (int*)(ws + at); at += up(sizeof(int));
+  }
   const size_t rows = (size_t)P.part_rows * P.streams;
   P.part_ml = (float2*)(ws + at); at += up(rows * sizeof(float2));
   P.part_o = (float*)(ws + at); at += up(rows * P.dh * sizeof(float));
@@ -735,8 +756,13 @@ int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   P.tokens = a->tokens; P.heads = a->heads; P.group = a->heads / kv->kv_heads; P.causal = a->causal; P.prefix = a->prefix_tokens;
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
-  P.ctas = rr_sm_count() * (P.tc ? 1 : 2);
-  P.part_rows = 2LL * P.tokens * P.heads + (long long)P.ctas * ROWS;
+  const long long homes = 2LL * P.tokens * P.heads;
+  P.main = Sched{rr_sm_count() * (P.tc ? 1 : 2), ROWS, nullptr, homes};
+  P.part_rows = homes + (long long)P.main.ctas * ROWS;
+  if (P.tc && P.group <= FEW_ROWS) {
+    P.few = Sched{rr_sm_count() * 3, FEW_ROWS, nullptr, P.part_rows};
+    P.part_rows += (long long)P.few.ctas * FEW_ROWS;
+  }
   P.streams = streams_of(P);
   return RR_OK;
 }
@@ -763,10 +789,14 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.range_rows = (long long)kv->batch * a->route_heads * a->n_q;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
-  P.ctas = rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 4 : 2);
-  const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS);
-  P.units = items < 8LL * P.ctas ? UNITS : 0;
-  P.part_rows = P.range_rows * P.m * P.group + (long long)P.ctas * ROWS;
+  const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS), homes = P.range_rows * P.m * P.group;
+  const bool few = P.tc && (long long)P.m * P.group <= FEW_ROWS;
+  if (few) P.tc = 0;
+  P.main = Sched{rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 4 : 2), ROWS, nullptr, homes};
+  if (few) P.few = Sched{rr_sm_count() * (P.m * P.group <= 2 ? 4 : 3), FEW_ROWS, nullptr, homes};
+  const Sched& sc = few ? P.few : P.main;
+  P.units = items < 8LL * sc.ctas ? UNITS : 0;
+  P.part_rows = homes + (long long)sc.ctas * sc.slot_rows;
   P.streams = streams_of(P);
   // (nothing to join: whole items, whose rows have one partial each; the last item of a range row may have fewer rows than the others)
   const int mg = P.m * P.group, last = mg % ROWS;
@@ -782,11 +812,19 @@ int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, co
   cudaError_t e = cudaSuccess;
   int launches = 0;
   if (!P.slots) { e = rr_launch_pdl(plan_kernel, 1, PLAN_NT, 0, st, P); ++launches; }
-  if (e == cudaSuccess) {
-    long long grid = P.ctas;
+  const bool few = P.few.ctas > 0;
+  // one token of each sequence, in up to four rows, and no prefix to share: the few kernel has everything
+  const bool only_few = few && (P.slots || (!P.cu && (P.prefix == 0 || P.batch == 1)));
+  P.few_waits = only_few;
+  if (e == cudaSuccess && !only_few) {
+    long long grid = P.main.ctas;
     if (P.slots && !P.units) grid = std::min<long long>(grid, P.range_rows * ceil_div((long long)P.m * P.group, ROWS));
     if (P.tc) e = rr_launch_attend_tc(P, (int)grid, st);
     else e = dtype == RR_BF16 ? launch_simt<__nv_bfloat16>(P, (int)grid, st) : launch_simt<float>(P, (int)grid, st);
+    ++launches;
+  }
+  if (e == cudaSuccess && few) {
+    e = rr_launch_attend_few(P, P.slots ? P.m * P.group : P.cu ? FEW_ROWS : P.group, st);
     ++launches;
   }
   if (e == cudaSuccess && P.part_rows > 0) {

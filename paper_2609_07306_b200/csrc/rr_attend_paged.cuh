@@ -25,10 +25,17 @@
 
 namespace rrattn {
 
-constexpr int TILE = 128, ROWS = 256, UNITS = 64;
+constexpr int TILE = 128, ROWS = 256, UNITS = 64, FEW_ROWS = 4;
 constexpr int NO_TOKEN = 0x7FFFFFFF;                   // id of a place without a token: above every limit
 constexpr float NINF = -__builtin_huge_valf();
 constexpr float LOWEST = -3.402823466e38f;             // m of a row that saw tokens, all of them at -inf
+
+// Who shares the items: CTAs, the tiles before each sequence's items, and where the CTAs' own places among the partial rows begin.
+struct Sched {
+  int ctas, slot_rows;                                 // slot_rows: rows of a CTA's place
+  long long* cum;                                      // shared: [batch + 1] tiles before sequence b's items; [batch] = all tiles
+  long long slots_at;
+};
 
 struct Params {
   // cache
@@ -47,10 +54,12 @@ struct Params {
   int n_q, m, slots, route_heads;                      // ranges (slots > 0)
   float scale_log2;                                    // scale * log2 e
   // schedule
-  int tc, ctas, units, streams;                        // units: of a ranges item (0: whole items in turn); streams: most partials of a segment's row
+  Sched main, few;                                     // few: items of up to FEW_ROWS rows in a kernel of their own (ctas == 0: no such kernel)
+  int tc, units, streams;                              // units: of a ranges item (0: whole items in turn); streams: most partials of a segment's row
+  int few_waits;                                       // the few kernel's inputs are its predecessor's (else it only ends after that)
   long long range_rows;                                // batch * route_heads * n_q
   // workspace
-  long long* cum;                                      // shared: [batch + 2] tiles before sequence b's items; [batch] = all tiles; [batch + 1] = apart
+  int* apart;                                          // shared: [1]
   float* part_o;                                       // [streams][part_rows][dh]
   float2* part_ml;                                     // [streams][part_rows]
   long long part_rows;
@@ -95,21 +104,23 @@ __device__ __forceinline__ long long prefix_row_tiles(const Params& P) { return 
 __device__ __forceinline__ int own_tiles(const Params& P, int b, bool apart) { return (max(seq_len(P, b) - (apart ? 0 : P.prefix), 0) + TILE - 1) / TILE; }
 __device__ __forceinline__ int own_row_tiles(const Params& P, int b) { return (int)ceil_div((long long)seq_count(P, b) * P.group, ROWS); }
 
+__device__ __forceinline__ bool few_rows_of(const Params& P, int b) { return P.few.ctas > 0 && (long long)seq_count(P, b) * P.group <= FEW_ROWS; }
+
 // With N = min(ctas, W) CTAs at work, CTA c's share of W tiles is [c W / N, (c + 1) W / N), at least one tile: an item that
 // is cut is in consecutive CTAs.  cta_of: the CTA that has tile u.
-__device__ __forceinline__ long long share(const Params& P, int c, long long W) {
-  const long long N = min((long long)P.ctas, W);
+__device__ __forceinline__ long long share(const Sched& sc, int c, long long W) {
+  const long long N = min((long long)sc.ctas, W);
   return c >= N ? W : quot(c * W, N);
 }
-__device__ __forceinline__ int cta_of(const Params& P, long long u, long long W) {
-  const long long N = min((long long)P.ctas, W);
+__device__ __forceinline__ int cta_of(const Sched& sc, long long u, long long W) {
+  const long long N = min((long long)sc.ctas, W);
   return (int)(ceil_div((u + 1) * N, W) - 1);
 }
 
 // The segment at tile u of CTA c's share, which ends at u1; returns how many tiles of the share it takes.
-__device__ __forceinline__ int segment_at(const Params& P, int c, long long u, long long u0, long long u1, Seg& s) {
-  const bool apart = __ldg(P.cum + P.batch + 1) != 0;
-  const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P), before = P.kv_heads * qtp * np;
+__device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int c, long long u, long long u1, Seg& s) {
+  const bool apart = __ldg(P.apart) != 0;
+  const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P), before = &sc == &P.few ? 0 : P.kv_heads * qtp * np;
   long long first;                                     // first tile of the item
   int tiles;
   long long home;
@@ -131,10 +142,10 @@ __device__ __forceinline__ int segment_at(const Params& P, int c, long long u, l
     home = s.kvh * row_all + s.row0;
   } else {
     int lo = 0, hi = P.batch;                          // last b with cum[b] <= u
-    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (__ldg(P.cum + mid) <= u) lo = mid; else hi = mid; }
+    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (__ldg(sc.cum + mid) <= u) lo = mid; else hi = mid; }
     const int b = lo, qt = own_row_tiles(P, b);
     tiles = own_tiles(P, b, apart);
-    const long long base = __ldg(P.cum + b), item = quot(u - base, tiles);
+    const long long base = __ldg(sc.cum + b), item = quot(u - base, tiles);
     first = base + item * tiles;
     s.kvh = (int)quot(item, qt);
     s.row0 = (int)(item - (long long)s.kvh * qt) * ROWS;
@@ -155,15 +166,15 @@ __device__ __forceinline__ int segment_at(const Params& P, int c, long long u, l
     const int limit = s.tok1 - s.n_seq + (s.row0 + s.rows - 1) / P.group + 1;
     s.tile1 = max(s.tile0, min(s.tile1, limit <= s.tok0 ? 0 : (limit - s.tok0 + TILE - 1) / TILE));
   }
-  s.part = s.tile0 == 0 ? home : 2 * (long long)P.tokens * P.heads + (long long)c * ROWS;
+  s.part = s.tile0 == 0 ? home : sc.slots_at + (long long)c * sc.slot_rows;
   return took;
 }
 
 // The segment at unit u (item u, if they are taken whole) of CTA c's share of a ranges call; its tiles are counted by who reads the
 // slots.  Returns how many units it takes.
-__device__ __forceinline__ int range_segment(const Params& P, int c, long long u, long long u1, Seg& s) {
+__device__ __forceinline__ int range_segment(const Params& P, const Sched& sc, int c, long long u, long long u1, Seg& s) {
   const int mg = P.m * P.group, qt = (mg + ROWS - 1) / ROWS, n = P.units ? P.units : 1;
-  const long long item = quot(u, n), row = quot(item, qt), all = P.range_rows * mg;
+  const long long item = quot(u, n), row = quot(item, qt);
   s.unit0 = (int)(u - item * n);
   s.unit1 = (int)min((long long)n, u1 - item * n);
   s.whole = s.unit1 - s.unit0 == n;
@@ -180,7 +191,7 @@ __device__ __forceinline__ int range_segment(const Params& P, int c, long long u
   s.slots = P.ranges + row * P.slots * 2;
   s.prefix = 0;
   s.tile0 = s.tile1 = 0;
-  s.part = s.unit0 == 0 ? row * mg + s.row0 : all + (long long)c * ROWS;
+  s.part = s.unit0 == 0 ? row * mg + s.row0 : sc.slots_at + (long long)c * sc.slot_rows;
   return s.unit1 - s.unit0;
 }
 __device__ __forceinline__ void unit_tiles(const Params& P, int tiles, Seg& s) {
@@ -189,7 +200,7 @@ __device__ __forceinline__ void unit_tiles(const Params& P, int tiles, Seg& s) {
   s.tile1 = (int)((long long)tiles * s.unit1 / n);
 }
 // The units or tiles of all items: a ranges call's are known to the host.
-__device__ __forceinline__ long long range_units(const Params& P) { return P.range_rows * ((P.m * P.group + ROWS - 1) / ROWS) * (P.units ? P.units : 1); }
+__host__ __device__ __forceinline__ long long range_units(const Params& P) { return P.range_rows * ((P.m * P.group + ROWS - 1) / ROWS) * (P.units ? P.units : 1); }
 // Tokens of one slot: [lo, hi) clipped to the sequence.
 __device__ __forceinline__ void slot_span(const Seg& s, int j, int& lo, int& hi) {
   lo = __ldg(s.slots + 2 * j);
@@ -275,6 +286,8 @@ __device__ __noinline__ void repair_row(const Params& P, const Seg& s, int r, in
 
 }  // namespace rrattn
 
-// bf16, dh 64 or 128, a positive scale, rows on 16-byte boundaries.
+// Up to four rows of each item: `rows` of the call's items.
+cudaError_t rr_launch_attend_few(const rrattn::Params& p, int rows, cudaStream_t st);
+// bf16, dh 64 or 128, a positive scale, rows on 16-byte boundaries.  (The few kernel needs the same.)
 bool rr_attend_tc_supported(const rrattn::Params& p, int dtype);
 cudaError_t rr_launch_attend_tc(const rrattn::Params& p, int grid, cudaStream_t st);

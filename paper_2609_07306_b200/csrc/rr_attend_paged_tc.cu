@@ -499,17 +499,17 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
     regs_down<72>();
     if (warp == 9) {
       // ===== the segments =====
-      long long u, u0 = 0, u1;
+      long long u, u1;
       const bool turns = P.slots && !P.units;          // whole items in turn
-      const long long W = P.slots ? range_units(P) : __ldg(P.cum + P.batch);
+      const long long W = P.slots ? range_units(P) : __ldg(P.main.cum + P.batch);
       if (turns) { u = blockIdx.x; u1 = W; }
-      else { u = u0 = share(P, blockIdx.x, W); u1 = share(P, blockIdx.x + 1, W); }
+      else { u = share(P.main, blockIdx.x, W); u1 = share(P.main, blockIdx.x + 1, W); }
       for (int n = 0;; ++n) {
         Seg s;
         const bool end = u >= u1;
         if (end) { s.rows = 0; }
-        else if (P.slots) { const int took = range_segment(P, blockIdx.x, u, u1, s); u += turns ? gridDim.x : took; }
-        else u += segment_at(P, blockIdx.x, u, u0, u1, s);
+        else if (P.slots) { const int took = range_segment(P, P.main, blockIdx.x, u, u1, s); u += turns ? gridDim.x : took; }
+        else u += segment_at(P, P.main, blockIdx.x, u, u1, s);
         if (!__all_sync(FULL, mbar_wait_spin(&c->seg_empty[n % ring], (n / ring & 1) ^ 1, abort_flag))) break;
         if (!end && P.slots) {                           // number the row's tokens
           int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
