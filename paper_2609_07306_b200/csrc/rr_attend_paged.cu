@@ -793,7 +793,7 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   const bool few = P.tc && (long long)P.m * P.group <= FEW_ROWS;
   if (few) P.tc = 0;
   P.main = Sched{rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 4 : 2), ROWS, nullptr, homes};
-  if (few) P.few = Sched{rr_sm_count() * (P.m * P.group <= 2 ? 4 : 3), FEW_ROWS, nullptr, homes};
+  if (few) P.few = Sched{rr_sm_count() * 3, FEW_ROWS, nullptr, homes};
   const Sched& sc = few ? P.few : P.main;
   P.units = items < 8LL * sc.ctas ? UNITS : 0;
   P.part_rows = homes + (long long)sc.ctas * sc.slot_rows;

@@ -2,12 +2,12 @@
 // results are joined).
 //
 // With so few rows the cache's traffic is all: 16 multiply-adds per byte at most.  The tensor cores' kernel holds two tiles of
-// keys and values in shared memory, and a load's latency goes by before a tile's place is free again; here the loads go to
-// registers, and an SM has 12 to 16 warps that ask for 8 KB each at a time.  A warp takes 8 loads of keys and 8 of values of 32 lanes x 16
-// bytes (16 tokens of 128 entries, 32 of 64), behind the look-up of the next ones' pages.  The dot products' halves are
-// exchanged until a token's logit is left in LPT / 8 lanes; its weight goes back to the token's lanes for the values.  A token that a
-// row does not see is not multiplied.  The four warps' parts of a segment are joined in shared memory.
-// Measured: 512 rows of 4096 tokens each, dh 128 (1.07 GB): XX us, the tensor cores' kernel 216.
+// keys and values in shared memory, and a load's latency goes by before a tile's place is free again.  Here every warp has
+// two blocks of its own, each 8 loads of keys and 8 of values of 32 lanes x 16 bytes (16 tokens of 128 entries, 32 of 64), which it asks for
+// with cp.async as soon as it has read what was there: 12 warps and 192 KB on an SM, and no barrier but the warp's.  The
+// dot products' halves are exchanged until a token's logit is left in LPT / 8 lanes; its weight goes back to the token's lanes for the
+// values.  A token that a row does not see is not multiplied.  The four warps' parts of a segment are joined at its end.
+// Measured: 512 rows of 4096 tokens each, dh 128 (1.07 GB): XX us; with the loads in registers 184; the tensor cores' kernel 216.
 #include <algorithm>
 #include "rr_attend_paged.cuh"
 
@@ -16,7 +16,12 @@ using namespace rrattn;
 namespace {
 
 constexpr unsigned FULL = 0xFFFFFFFFu;
-constexpr int WARPS = 4, NT = WARPS * 32, N = 8;
+constexpr int WARPS = 4, NT = WARPS * 32, N = 8, BLOCKS = 2;
+constexpr int BLOCK_BYTES = 2 * N * 512, RING_BYTES = WARPS * BLOCKS * BLOCK_BYTES;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t n) {      // zeros if n == 0
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
 
 __device__ __forceinline__ uint64_t two(float lo, float hi) { uint64_t y; asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(lo), "f"(hi)); return y; }
 __device__ __forceinline__ void split(uint64_t x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
@@ -25,16 +30,18 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t y; a
 __device__ __forceinline__ uint64_t widen(uint32_t x) { return two(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u)); }
 
 template <int D, int R>
-__global__ void __launch_bounds__(NT, R == 4 ? 3 : 4) attend_few_kernel(const __grid_constant__ Params P) {
+__global__ void __launch_bounds__(NT, 3) attend_few_kernel(const __grid_constant__ Params P) {
   constexpr int LPT = D / 8, TP = 32 / LPT, BLOCK = N * TP, DUP = LPT / N;     // lanes per token, tokens per load and per block
-  extern __shared__ int s_table[];
+  extern __shared__ __align__(16) uint8_t s_mem[];
   __shared__ __align__(16) float s_o[WARPS][R][D];
   __shared__ float2 s_ml[WARPS][R];
   // Behind the tensor cores' kernel of the same call this one needs nothing of it but that the plan is there (it is: that kernel
   // lets its successor start behind its own wait): CTAs start as that kernel's leave, and wait for its end before their own.
   if (P.few_waits) { rr_pdl_wait(); rr_pdl_trigger(); }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane % LPT, grp = lane / LPT;
-  int* const first = s_table;
+  const uint4* const ring = reinterpret_cast<const uint4*>(s_mem) + warp * (BLOCKS * BLOCK_BYTES / 16) + lane;
+  const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
+  int* const first = reinterpret_cast<int*>(s_mem + RING_BYTES);
   int* const base = first + P.slots + 1;
   const bool turns = P.slots && !P.units;
   const long long W = P.slots ? range_units(P) : __ldg(P.few.cum + P.batch);
@@ -106,30 +113,42 @@ __global__ void __launch_bounds__(NT, R == 4 ? 3 : 4) attend_few_kernel(const __
       at = token_at(P, s, id);
       if (at < 0) id = NO_TOKEN;
     };
-    int next_id;
+    // Block k of the warp: in place k % BLOCKS; `ids` of the blocks in flight, `next_*` of the one to be asked for.
+    const int step = WARPS * BLOCK, num_first = s.tile0 * TILE + warp * BLOCK;
+    int ids[BLOCKS], next_id;
     long long next_at;
-    seek(s.tile0 * TILE + warp * BLOCK, next_id, next_at);
-    for (int num0 = s.tile0 * TILE + warp * BLOCK; num0 < end; num0 += WARPS * BLOCK) {
-      const int id = next_id;
-      const long long at = next_at;
-      uint4 x[N], y[N];
+    auto ask = [&](int place) {
+      const uint32_t dst = ring_addr + place * BLOCK_BYTES;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const long long o = __shfl_sync(FULL, at, i * TP + grp);
-        x[i] = y[i] = make_uint4(0, 0, 0, 0);
-        if (o >= 0) {
-          x[i] = __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)P.k + o + sub * 8));
-          y[i] = __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)P.v + o + sub * 8));
-        }
+        const long long o = __shfl_sync(FULL, next_at, i * TP + grp), from = max(o, 0LL) + sub * 8;
+        cp_async16(dst + i * 512, (const __nv_bfloat16*)P.k + from, o >= 0 ? 16u : 0u);
+        cp_async16(dst + (N + i) * 512, (const __nv_bfloat16*)P.v + from, o >= 0 ? 16u : 0u);
       }
-      seek(num0 + WARPS * BLOCK, next_id, next_at);
+    };
+    seek(num_first, next_id, next_at);
+#pragma unroll
+    for (int k = 0; k < BLOCKS; ++k) {
+      ids[k] = next_id;
+      if (num_first + k * step < end) ask(k);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      seek(num_first + (k + 1) * step, next_id, next_at);
+    }
+    int place = 0;
+    for (int num0 = num_first; num0 < end; num0 += step) {
+      const int id = ids[0];
+      asm volatile("cp.async.wait_group %0;" ::"n"(BLOCKS - 1) : "memory");
+      __syncwarp();
+      const uint4* const x = ring + place * (BLOCK_BYTES / 16);
+      const uint4* const y = x + N * 32;
       const int my_id = __shfl_sync(FULL, id, sub / DUP * TP + grp);       // lane's token: load sub / DUP of its group
       float wt[R];
       unsigned sees[R];
       float d[R][N];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const uint64_t k0 = widen(x[i].x), k1 = widen(x[i].y), k2 = widen(x[i].z), k3 = widen(x[i].w);
+        const uint4 kk = x[i * 32];
+        const uint64_t k0 = widen(kk.x), k1 = widen(kk.y), k2 = widen(kk.z), k3 = widen(kk.w);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           float lo, hi;
@@ -169,7 +188,8 @@ __global__ void __launch_bounds__(NT, R == 4 ? 3 : 4) attend_few_kernel(const __
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int from = grp * LPT + i * DUP;
-        const uint64_t v0 = widen(y[i].x), v1 = widen(y[i].y), v2 = widen(y[i].z), v3 = widen(y[i].w);
+        const uint4 vv = y[i * 32];
+        const uint64_t v0 = widen(vv.x), v1 = widen(vv.y), v2 = widen(vv.z), v3 = widen(vv.w);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           const float w = __shfl_sync(FULL, wt[r], from);
@@ -180,7 +200,18 @@ __global__ void __launch_bounds__(NT, R == 4 ? 3 : 4) attend_few_kernel(const __
           }
         }
       }
+      __syncwarp();                                    // the place has been read
+#pragma unroll
+      for (int k = 0; k + 1 < BLOCKS; ++k) ids[k] = ids[k + 1];
+      ids[BLOCKS - 1] = next_id;
+      if (num0 + BLOCKS * step < end) {
+        ask(place);
+        seek(num0 + (BLOCKS + 1) * step, next_id, next_at);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      place = place + 1 == BLOCKS ? 0 : place + 1;
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     // the warp's parts: outputs over the groups of lanes, sums over the lanes; then the warps'
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -232,7 +263,16 @@ template <int D>
 cudaError_t launch(const Params& p, int rows, cudaStream_t st) {
   long long grid = p.few.ctas;
   if (p.slots && !p.units) grid = std::min(grid, p.range_rows);
-  const size_t smem = p.slots ? (2 * p.slots + 1) * sizeof(int) : 0;
+  const size_t smem = RING_BYTES + (p.slots ? (2 * p.slots + 1) * sizeof(int) : 0);
+  static unsigned long long done = 0;
+  const cudaError_t e = rr_once_per_device(done, [] {
+    const int most = RING_BYTES + (2 * RR_MAX_RANGE_SLOTS + 1) * (int)sizeof(int);
+    cudaError_t a = cudaFuncSetAttribute(attend_few_kernel<D, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (a == cudaSuccess) a = cudaFuncSetAttribute(attend_few_kernel<D, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (a == cudaSuccess) a = cudaFuncSetAttribute(attend_few_kernel<D, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return a;
+  });
+  if (e != cudaSuccess) return e;
   if (rows == 1) return rr_launch_pdl(attend_few_kernel<D, 1>, (int)grid, NT, smem, st, p);
   if (rows == 2) return rr_launch_pdl(attend_few_kernel<D, 2>, (int)grid, NT, smem, st, p);
   return rr_launch_pdl(attend_few_kernel<D, 4>, (int)grid, NT, smem, st, p);
