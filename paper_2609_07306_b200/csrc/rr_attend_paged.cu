@@ -614,7 +614,7 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
 }
 
 // ONLY_FEW: a call whose items all have up to FEW rows needs no tiles in shared memory; CTAs of four warps, four to an SM, have more
-// segments' latencies side by side (2048 rows of 396 tokens, fp32, dh 64: 98 us with eight warps and two to an SM, XX us).
+// segments' latencies side by side (2048 rows of 396 tokens, fp32, dh 64: 98 us with eight warps and two to an SM, 75 us).
 constexpr int FEW_NT = 128;
 template <typename T, int NV, bool ONLY_FEW>
 __global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) attend_simt_kernel(const __grid_constant__ Params P, bool vq, bool vk) {

@@ -7,8 +7,9 @@
 // with cp.async as soon as it has read what was there: 12 warps and 192 KB on an SM, and no barrier but the warp's.  The
 // dot products' halves are exchanged until a token's logit is left in LPT / 8 lanes; its weight goes back to the token's lanes for the
 // values.  A token that a row does not see is not multiplied.  The four warps' parts of a segment are joined at its end.
-// Measured: 512 rows of 4096 tokens each, dh 128 (1.07 GB): XX us; with the loads in registers 184; the tensor cores' kernel 216.
+// Measured: 512 rows of 4096 tokens each, dh 128 (1.07 GB): 166 us; with the loads in registers 184; the tensor cores' kernel 216.
 #include <algorithm>
+#include <type_traits>
 #include "rr_attend_paged.cuh"
 
 using namespace rrattn;
@@ -17,6 +18,7 @@ namespace {
 
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int WARPS = 4, NT = WARPS * 32, N = 8, BLOCKS = 2;
+constexpr float GROWTH = 8.f;                          // the reference follows a row's maximum when that has grown by more (a factor of 256)
 constexpr int BLOCK_BYTES = 2 * N * 512, RING_BYTES = WARPS * BLOCKS * BLOCK_BYTES;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t n) {      // zeros if n == 0
@@ -174,32 +176,41 @@ __global__ void __launch_bounds__(NT, 3) attend_few_kernel(const __grid_constant
         sees[r] = __ballot_sync(FULL, see);
         if (sees[r]) seen |= 1u << r;
         z = see ? z * P.scale_log2 : NINF;
-        float top = z;
+        if (__any_sync(FULL, z > m[r] + GROWTH)) {     // (m = -inf: the first finite logit)
+          float top = z;
 #pragma unroll
-        for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, off));
-        const float m_new = fmaxf(m[r], top), ref = m_new == NINF ? 0.f : m_new, f = exp2f(m[r] - ref);
-        m[r] = m_new;
-        wt[r] = exp2f(z - ref);
-        l[r] = fmaf(l[r], f, sub % DUP ? 0.f : wt[r]);
-        const uint64_t f2 = two(f, f);
+          for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, off));
+          const float now = fmaxf(m[r], top), f = exp2f(m[r] - now);
+          m[r] = now;
+          l[r] *= f;
+          const uint64_t f2 = two(f, f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[r][j] = mul2(acc[r][j], f2);
+          for (int j = 0; j < 4; ++j) acc[r][j] = mul2(acc[r][j], f2);
+        }
+        wt[r] = exp2f(z - (m[r] == NINF ? 0.f : m[r]));
+        if (sub % DUP == 0) l[r] += wt[r];
       }
+      unsigned common = FULL;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int from = grp * LPT + i * DUP;
-        const uint4 vv = y[i * 32];
-        const uint64_t v0 = widen(vv.x), v1 = widen(vv.y), v2 = widen(vv.z), v3 = widen(vv.w);
+      for (int r = 0; r < R; ++r) common &= sees[r];
+      auto weigh = [&](auto all) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const float w = __shfl_sync(FULL, wt[r], from);
-          if (sees[r] >> from & 1) {
-            const uint64_t w2 = two(w, w);
-            acc[r][0] = fma2(w2, v0, acc[r][0]); acc[r][1] = fma2(w2, v1, acc[r][1]);
-            acc[r][2] = fma2(w2, v2, acc[r][2]); acc[r][3] = fma2(w2, v3, acc[r][3]);
+        for (int i = 0; i < N; ++i) {
+          const int from = grp * LPT + i * DUP;
+          const uint4 vv = y[i * 32];
+          const uint64_t v0 = widen(vv.x), v1 = widen(vv.y), v2 = widen(vv.z), v3 = widen(vv.w);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float w = __shfl_sync(FULL, wt[r], from);
+            if (decltype(all)::value || (sees[r] >> from & 1)) {
+              const uint64_t w2 = two(w, w);
+              acc[r][0] = fma2(w2, v0, acc[r][0]); acc[r][1] = fma2(w2, v1, acc[r][1]);
+              acc[r][2] = fma2(w2, v2, acc[r][2]); acc[r][3] = fma2(w2, v3, acc[r][3]);
+            }
           }
         }
-      }
+      };
+      if (common == FULL) weigh(std::true_type()); else weigh(std::false_type());
       __syncwarp();                                    // the place has been read
 #pragma unroll
       for (int k = 0; k + 1 < BLOCKS; ++k) ids[k] = ids[k + 1];
