@@ -32,7 +32,8 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
   const long long packed = prefix_row_tiles(P);
   const bool apart = row_tiles <= packed + packed / 8;
   __syncthreads();
-  long long run = apart ? 0 : P.kv_heads * packed * prefix_tiles(P), run_few = 0;
+  const long long prefix_all = apart ? 0 : P.kv_heads * packed * prefix_tiles(P);
+  long long run = P.few_prefix ? 0 : prefix_all, run_few = P.few_prefix ? prefix_all : 0;
   auto scan = [&](long long mine, long long& run) -> long long {     // what is before this thread's, the block's sum added to run
     long long incl = mine;
 #pragma unroll
@@ -87,7 +88,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
     const int b = P.cu ? rr_sequence_of_warp(P.cu, P.batch, t) : t;
     mine = mine && b >= 0;                             // (padding: left as it was)
     if (mine) {
-      const long long all = __ldg(P.main.cum + P.batch), per = (long long)P.tokens * P.group;
+      const Sched& sp = P.few_prefix ? P.few : P.main;
+      const long long all = __ldg(P.main.cum + P.batch), all_p = P.few_prefix ? __ldg(P.few.cum + P.batch) : all, per = (long long)P.tokens * P.group;
       out = t * P.ot + h * P.oh;
       const bool apart = __ldg(P.apart) != 0;
       const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P);
@@ -95,9 +97,9 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
         const long long idx = (long long)t * P.group + g, first = (kvh * qtp + idx / ROWS) * np;
         home0 = kvh * per + idx;
         r0 = (int)(idx % ROWS);
-        c0 = cta_of(P.main, first, all);
-        cnt0 = cta_of(P.main, first + np - 1, all) - c0 + 1;
-        st0 = partials_of(P.streams, min((long long)ROWS, per - idx / ROWS * ROWS));
+        c0 = cta_of(sp, first, all_p);
+        cnt0 = cta_of(sp, first + np - 1, all_p) - c0 + 1;
+        st0 = P.few_prefix ? 1 : partials_of(P.streams, min((long long)ROWS, per - idx / ROWS * ROWS));
       }
       const int no = own_tiles(P, b, apart);
       if (no > 0) {
@@ -134,7 +136,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   }
   if (WPR == 1 && !mine) return;
   const int n0 = cnt0 * st0, n = n0 + cnt1 * st1;
-  const bool few0 = P.slots && P.few.ctas > 0;
+  const bool few0 = P.slots ? P.few.ctas > 0 : P.few_prefix;
   auto place = [&](int k) -> long long {               // partial row of the k-th partial
     const bool w = k >= n0;
     if (w) k -= n0;
@@ -762,6 +764,7 @@ int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   if (P.tc && P.group <= FEW_ROWS) {
     P.few = Sched{rr_sm_count() * 3, FEW_ROWS, nullptr, P.part_rows};
     P.part_rows += (long long)P.few.ctas * FEW_ROWS;
+    P.few_prefix = (long long)P.tokens * P.group <= FEW_ROWS;
   }
   P.streams = streams_of(P);
   return RR_OK;
@@ -813,8 +816,8 @@ int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, co
   int launches = 0;
   if (!P.slots) { e = rr_launch_pdl(plan_kernel, 1, PLAN_NT, 0, st, P); ++launches; }
   const bool few = P.few.ctas > 0;
-  // one token of each sequence, in up to four rows, and no prefix to share: the few kernel has everything
-  const bool only_few = few && (P.slots || (!P.cu && (P.prefix == 0 || P.batch == 1)));
+  // up to four rows in all, or one token of each sequence and no prefix to share: the few kernel has everything
+  const bool only_few = few && (P.slots || P.few_prefix || (!P.cu && P.prefix == 0));
   P.few_waits = only_few;
   if (e == cudaSuccess && !only_few) {
     long long grid = P.main.ctas;
@@ -824,7 +827,7 @@ int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, co
     ++launches;
   }
   if (e == cudaSuccess && few) {
-    e = rr_launch_attend_few(P, P.slots ? P.m * P.group : P.cu ? FEW_ROWS : P.group, st);
+    e = rr_launch_attend_few(P, P.slots ? P.m * P.group : P.few_prefix ? P.tokens * P.group : P.cu ? FEW_ROWS : P.group, st);
     ++launches;
   }
   if (e == cudaSuccess && P.part_rows > 0) {

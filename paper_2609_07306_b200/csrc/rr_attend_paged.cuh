@@ -56,6 +56,7 @@ struct Params {
   // schedule
   Sched main, few;                                     // few: items of up to FEW_ROWS rows in a kernel of their own (ctas == 0: no such kernel)
   int tc, units, streams;                              // units: of a ranges item (0: whole items in turn); streams: most partials of a segment's row
+  bool few_prefix;                                     // the few kernel has the prefix's items, too: all queries make up to FEW_ROWS rows
   int few_waits;                                       // the few kernel's inputs are its predecessor's (else it only ends after that)
   long long range_rows;                                // batch * route_heads * n_q
   // workspace
@@ -120,7 +121,7 @@ __device__ __forceinline__ int cta_of(const Sched& sc, long long u, long long W)
 // The segment at tile u of CTA c's share, which ends at u1; returns how many tiles of the share it takes.
 __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int c, long long u, long long u1, Seg& s) {
   const bool apart = __ldg(P.apart) != 0;
-  const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P), before = &sc == &P.few ? 0 : P.kv_heads * qtp * np;
+  const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P), before = (&sc == &P.few) == P.few_prefix ? P.kv_heads * qtp * np : 0;
   long long first;                                     // first tile of the item
   int tiles;
   long long home;

@@ -154,7 +154,7 @@ class PagedKV:
             shape = (n, q.shape[1], self.dh)
             self._heads(q, "q", shape)
             if q_out is None:
-                q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
+                q_out = q.new_empty(shape)
             else:
                 self._heads(q_out, "q_out", shape)
             heads, q_strides = shape[1], (q.stride(0), q.stride(1), q_out.stride(0), q_out.stride(1))
@@ -193,7 +193,7 @@ class PagedKV:
             if prefix_pages.shape[0] * self.page_tokens < prefix_tokens:
                 raise ValueError(f"prefix_pages holds {prefix_pages.shape[0]} pages, {prefix_tokens} tokens need more")
         if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(shape)
         else:
             self._heads(out, "out", shape)
         if shape[0] == 0 and cu is not None:
@@ -224,7 +224,7 @@ class PagedKV:
         if n_q < 1 or shape[2] % n_q != 0 or rows == 0 or rows % (self.batch * n_q) != 0:
             raise ValueError(f"{rows} range rows and {shape[2]} query tokens do not make {n_q} chunks of {self.batch} sequences")
         if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(shape)
         else:
             self._heads(out, "out", shape)
         self._run("rr_attend_paged_ranges", _RANGES.pack(
