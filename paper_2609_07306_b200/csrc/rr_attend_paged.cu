@@ -50,6 +50,7 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
   for (int b0 = 0; b0 < P.batch; b0 += PLAN_NT) {
     const int b = b0 + tid;
     const bool few = b < P.batch && few_rows_of(P, b);
+    if (b < P.batch) check_len(P, b);
     const long long mine = b < P.batch ? (long long)P.kv_heads * own_row_tiles(P, b) * own_tiles(P, b, apart) : 0;
     const long long at = scan(few ? 0 : mine, run);
     if (b < P.batch) P.main.cum[b] = at;
@@ -643,6 +644,7 @@ __global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) att
       u += turns ? gridDim.x : took;
       __syncthreads();                                 // the table before is no longer read
       if (threadIdx.x < 32) {
+        if (lane == 0) check_len(P, s.b);
         int run = 0;
         for (int j0 = 0; j0 < P.slots; j0 += 32) {
           const int j = j0 + lane;

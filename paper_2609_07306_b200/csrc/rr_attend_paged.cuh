@@ -88,10 +88,11 @@ __host__ __device__ inline long long quot(long long a, long long b) {
 }
 __host__ __device__ inline long long ceil_div(long long a, long long b) { return quot(a + b - 1, b); }
 
-// Tokens that sequence b has in the cache (never more than its table holds).
+// Tokens that sequence b has by its length, and of these those that its table has places for.
+__device__ __forceinline__ int seq_end(const Params& P, int b) { return max(__ldg(P.lens + b), 0); }
 __device__ __forceinline__ int seq_len(const Params& P, int b) {
   const long long cap = (long long)P.pages_per_seq * P.page_tokens;
-  const int n = max(__ldg(P.lens + b), 0);
+  const int n = seq_end(P, b);
   return n > cap ? (int)cap : n;
 }
 __device__ __forceinline__ int seq_first(const Params& P, int b) { return P.cu ? __ldg(P.cu + b) : b; }
@@ -164,8 +165,8 @@ __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int 
   const int took = s.tile1 - s.tile0;
   s.whole = took == tiles && u >= before && np == 0;
   if (P.causal && s.b >= 0) {                          // no row sees the tiles from the last row's limit on
-    const int limit = s.tok1 - s.n_seq + (s.row0 + s.rows - 1) / P.group + 1;
-    s.tile1 = max(s.tile0, min(s.tile1, limit <= s.tok0 ? 0 : (limit - s.tok0 + TILE - 1) / TILE));
+    const long long limit = (long long)seq_end(P, s.b) - s.n_seq + (s.row0 + s.rows - 1) / P.group + 1;
+    s.tile1 = max(s.tile0, limit <= s.tok0 ? 0 : (int)min((long long)s.tile1, (limit - s.tok0 + TILE - 1) / TILE));
   }
   s.part = s.tile0 == 0 ? home : sc.slots_at + (long long)c * sc.slot_rows;
   return took;
@@ -202,6 +203,10 @@ __device__ __forceinline__ void unit_tiles(const Params& P, int tiles, Seg& s) {
 }
 // The units or tiles of all items: a ranges call's are known to the host.
 __host__ __device__ __forceinline__ long long range_units(const Params& P) { return P.range_rows * ((P.m * P.group + ROWS - 1) / ROWS) * (P.units ? P.units : 1); }
+// A length that the table has no places for is reported; what is behind the table is left out.
+__device__ __forceinline__ void check_len(const Params& P, int b) {
+  if (P.status && seq_end(P, b) > seq_len(P, b)) atomicOr(P.status, RR_STATUS_BAD_INDEX);
+}
 // Tokens of one slot: [lo, hi) clipped to the sequence.
 __device__ __forceinline__ void slot_span(const Seg& s, int j, int& lo, int& hi) {
   lo = __ldg(s.slots + 2 * j);
@@ -225,7 +230,7 @@ __device__ __forceinline__ RowAt row_at(const Params& P, const Seg& s, int r) {
     first = seq_first(P, b);
     n = seq_count(P, b);
   }
-  const int len = seq_len(P, b);
+  const int len = seq_end(P, b);
   a.limit = P.causal ? max(len - n + (a.t - first) + 1, 0) : len;
   return a;
 }

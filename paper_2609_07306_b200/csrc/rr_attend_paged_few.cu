@@ -57,6 +57,7 @@ __global__ void __launch_bounds__(NT, 3) attend_few_kernel(const __grid_constant
       const int took = range_segment(P, P.few, blockIdx.x, u, u1, s);
       u += turns ? gridDim.x : took;
       if (warp == 0) {                                 // number the row's tokens
+        if (lane == 0) check_len(P, s.b);
         int run = 0;
         for (int j0 = 0; j0 < P.slots; j0 += 32) {
           const int j = j0 + lane;

@@ -512,6 +512,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         else u += segment_at(P, P.main, blockIdx.x, u, u1, s);
         if (!__all_sync(FULL, mbar_wait_spin(&c->seg_empty[n % ring], (n / ring & 1) ^ 1, abort_flag))) break;
         if (!end && P.slots) {                           // number the row's tokens
+          if (lane == 0) check_len(P, s.b);
           int* const first = slot_table + (n % ring) * (2 * P.slots + 1);
           int* const base = first + P.slots + 1;
           int run = 0;
@@ -539,7 +540,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         const Seg& s = c->seg[n % ring];
         if (s.rows == 0) break;
         if (s.b >= 0) {                                // one sequence: the limit goes up by one from token to token
-          const int len = s.slots ? s.tok1 : seq_len(P, s.b), past = len - s.n_seq + (s.t_base - s.t_seq0) + 1;
+          const int len = seq_end(P, s.b), past = len - s.n_seq + (s.t_base - s.t_seq0) + 1;
           for (int r = lane; r < s.rows; r += 32) c->limit[n % ring][r] = P.causal ? max(past + (s.row0 + r) / P.group, 0) : len;
         } else {
           for (int r = lane; r < s.rows; r += 32) c->limit[n % ring][r] = row_at(P, s, r).limit;
