@@ -1,6 +1,7 @@
 // Attention over a paged key/value cache: how the work of rr_attend_shared and rr_attend_paged_ranges is cut
-// into segments, where a segment's partial results go, and how they are joined.  Two kernels process segments: the tensor cores'
-// (rr_attend_paged_tc.cu) and the one for every other type and width (rr_attend_paged.cu).
+// into segments, where a segment's partial results go, and how they are joined.  Three kernels process segments: the tensor cores'
+// (rr_attend_paged_tc.cu), one for up to four rows of the same types (rr_attend_paged_few.cu) and the one for every other type and width
+// (rr_attend_paged.cu).
 //
 // An ITEM is up to ROWS query rows that attend to one list of tokens of one key head:
 //   shared, prefix   the queries of all sequences and of the G = heads / kv_heads query heads of a key head (row t * G + g),
@@ -15,8 +16,8 @@
 //
 // shared: the tiles of all items in one row, N CTAs take equal shares of it (an item may be cut anywhere, a
 // CTA's share may span many items), so neither a long prefix of few rows nor one long sequence among short ones leaves SMs idle.
-// plan_kernel counts the tiles on the device, where the lengths are.  A segment that begins its item has its partial rows at
-// the rows' own places; a CTA has at most one segment that does not, whose rows go to the CTA's own ROWS places.
+// plan_kernel counts the tiles on the device, where the lengths are, for the few-row kernel's items and the others apart.  A segment that begins
+// its item has its partial rows at the rows' own places; a CTA has at most one segment that does not, whose rows go to the CTA's own places.
 // ranges: items are alike.  Where there are fewer than eight per CTA each counts as UNITS units that the CTAs share equally, as the tiles above (a
 // segment has the tiles of its units by the item's own number of tiles); where there are more, CTAs take whole items in turn, so that
 // neighbouring rows, whose routes overlap, are read at the same time.

@@ -2,16 +2,16 @@
 // for items, segments and how their partial results are joined).
 //
 // One CTA per SM walks its segments.  Per tile of 128 tokens and 128 query rows:  S = Q K^T (TMEM, FP32), softmax against a
-// running reference, P (bf16, written over S in TMEM) and O += P V (TMEM, FP32).  Two streams of four warps
-// keep the tensor pipe and the exponentials busy in turn:
+// running reference, P (bf16, written over S in TMEM) and O += P V (TMEM, FP32).  Two streams of four warps:
 //   a segment of more than 128 rows is paired: stream 0 has rows 0..127, stream 1 the others, each tile of keys and values is
 //   read once for both;
 //   one of up to 128 rows is split: both streams have the same rows, stream 0 the even tiles and stream 1 the odd ones, and
 //   each leaves a partial result of its own;
 //   one of up to 32 rows (a decoding step) is quartered besides: each of a stream's four warps has a copy of the rows in its 32 lanes and 16
 //   of every 64 tokens, whose weights alone are not zero there, so that the exponentials are spread over the SM.
-// The tensor pipe takes 2 x 520 cycles for a 128 x 128 x 128 tile's two products, the 16384 exponentials take 1024: many rows are
-// bound by both about equally, few rows by the cache's traffic.
+// The tensor pipe takes 2 x 520 cycles for a 128 x 128 x 128 tile's two products, the 16384 exponentials take 1024 on the special-function
+// unit.  Measured: 545 us for 475 GFLOP of a routed prompt (870 TFLOP/s, tensor pipe 42 %), 650 us for 481 GFLOP of prompts behind a prefix; what
+// bounds them is a stream's chain of logits, maximum, exponentials and weights, about 2000 cycles per 64 tokens of two tiles.
 //
 // Warps 0-3, 4-7: the streams, a thread per row.  8, 11: issue the products, one stream's each.  9: finds the segments.  10: the rows' limits.
 // 12-15: copies of token and query rows, 32 rows each.  Where those 32 tokens are runs of 32, 16 or 8 in a page, TMA brings
@@ -19,7 +19,9 @@
 // for a place without a token.  Segments go round in a ring, so that the next one's look-ups and queries are there before it begins.
 // (16 bytes per thread for every tile cost the copying warps 2000 cycles of a tile, and the streams issue slots; TMA's tile::gather4,
 // four token rows per copy, about 100 cycles of issue per copy, 8 us per tile.)
-// A stream's S(k) is issued behind its product with P(k - 1), which reads the same columns; the tensor pipe keeps that order.
+// A stream has 64 columns of S per half tile: one half's logits are there or under way while the other's weights are made (whole tiles of S: 636
+// us instead of 595).  A half's logits are issued behind the product with the weights before, which reads the same columns; the tensor
+// pipe keeps that order.
 //
 // The reference of the softmax follows the row's maximum only when that has grown by more than 8 (a factor of
 // 256): weights up to 2^8 lose nothing in bf16 and FP32, and the output is rescaled in TMEM a few times per
@@ -39,7 +41,7 @@ namespace {
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int NT = 512, IDS = 16, MAX_RING = 4;
 constexpr float GROWTH = 8.f;
-constexpr int BY_FMA = 2;                              // of every 8 pairs of exponentials, by multiply-adds
+constexpr int BY_FMA = 2;                              // of every 8 pairs of exponentials, by multiply-adds (0: 567 us, 1: 551, 2: 544 of a routed prompt)
 
 template <int D> struct Shape {
   static constexpr int HALVES = D / 64, STAGES = D == 128 ? 4 : 8;
