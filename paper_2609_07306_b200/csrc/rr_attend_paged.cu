@@ -765,7 +765,8 @@ int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   P.main = Sched{rr_sm_count() * (P.tc ? 1 : 2), ROWS, nullptr, homes};
   P.part_rows = homes + (long long)P.main.ctas * ROWS;
   if (P.tc && P.group <= FEW_ROWS) {
-    P.few = Sched{rr_sm_count() * 3, FEW_ROWS, nullptr, P.part_rows};
+    // (three CTAs fit an SM; two rounds of them even out segments of unlike lengths: 64 sequences of 1 to 2000 tokens 172 -> 156 us, three: 163)
+    P.few = Sched{rr_sm_count() * 6, FEW_ROWS, nullptr, P.part_rows};
     P.part_rows += (long long)P.few.ctas * FEW_ROWS;
     P.few_prefix = (long long)P.tokens * P.group <= FEW_ROWS;
   }
@@ -799,6 +800,7 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   const bool few = P.tc && (long long)P.m * P.group <= FEW_ROWS;
   if (few) P.tc = 0;
   P.main = Sched{rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 4 : 2), ROWS, nullptr, homes};
+  // (three CTAs fit an SM; more of them lose: 2048 rows of 396 tokens 52 us, with nine 61)
   if (few) P.few = Sched{rr_sm_count() * 3, FEW_ROWS, nullptr, homes};
   const Sched& sc = few ? P.few : P.main;
   P.units = items < 8LL * sc.ctas ? UNITS : 0;
