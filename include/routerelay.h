@@ -360,6 +360,8 @@ int rr_attend_token_ranges(const int32_t* ranges, int32_t rows, int32_t slots, i
  *   - Lengths, tables and ranges are read on the device.  An id outside [0, num_pages), or a position
  *     behind the table's end, sets RR_STATUS_BAD_INDEX in *status (if given) and the token is left out: not
  *     written by an append, not seen by an attention.  Nothing out of range is read or written.
+ *   - A bounded wait inside a kernel that ran out (none does on a GPU that works) sets RR_STATUS_TIMEOUT in *status; the call's outputs
+ *     are not to be used then.
  *   - What a query may not see -- by the causal mask, by its length, by its ranges -- does not reach it, whatever
  *     the memory holds, NaN and infinities included.  A query that sees nothing gets zeros; one whose logits are
  *     all -inf has no softmax and gets NaN.
