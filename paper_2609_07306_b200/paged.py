@@ -76,9 +76,10 @@ class PagedKV:
 
     # -- checks: one comparison each for what is right, the reason where it is not ----------------------------
     def _heads(self, t, name, shape):
-        """t has the cache's type and device, the given shape (its last entry dh), contiguous heads."""
-        if t.dtype is self._dtype and t.get_device() == self._index and t.shape == shape and t.stride(-1) == 1:
-            return
+        """t has the cache's type and device, the given shape (its last entry dh), contiguous heads; its strides."""
+        strides = t.stride()
+        if t.dtype is self._dtype and t.get_device() == self._index and t.shape == shape and strides[-1] == 1:
+            return strides
         if t.device != self.device:
             raise ValueError(f"{name} is on {t.device}, the cache on {self.device}")
         if t.dtype is not self._dtype:
@@ -87,6 +88,7 @@ class PagedKV:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
         if self.dh > 1 and t.numel() > 0:
             raise ValueError(f"the entries of a head of {name} must be contiguous")
+        return strides
 
     def _ints(self, t, name, shape, rows_apart=False):
         if t.dtype is torch.int32 and t.get_device() == self._index and t.shape == shape and t.is_contiguous():
@@ -135,8 +137,8 @@ class PagedKV:
             raise ValueError("k must be [tokens, kv_heads, dh]")
         n = k.shape[0]
         shape = (n, self.kv_heads, self.dh)
-        self._heads(k, "k", shape)
-        self._heads(v, "v", shape)
+        ks = self._heads(k, "k", shape)
+        vs = self._heads(v, "v", shape)
         self._ints(lens, "lens", (self.batch,))
         if cu is not None:
             self._ints(cu, "cu", (self.batch + 1,))
@@ -152,12 +154,13 @@ class PagedKV:
             if q.dim() != 3:
                 raise ValueError("q must be [tokens, heads, dh]")
             shape = (n, q.shape[1], self.dh)
-            self._heads(q, "q", shape)
+            qs = self._heads(q, "q", shape)
             if q_out is None:
                 q_out = q.new_empty(shape)
+                os = (shape[1] * self.dh, self.dh)
             else:
-                self._heads(q_out, "q_out", shape)
-            heads, q_strides = shape[1], (q.stride(0), q.stride(1), q_out.stride(0), q_out.stride(1))
+                os = self._heads(q_out, "q_out", shape)
+            heads, q_strides = shape[1], (qs[0], qs[1], os[0], os[1])
         elif q_out is not None:
             raise ValueError("q_out without q")
         if n == 0:                                     # (an empty tensor has no address)
@@ -167,7 +170,7 @@ class PagedKV:
         self._run("rr_kv_append", _APPEND.pack(
             k.data_ptr(), v.data_ptr(), q.data_ptr() if heads else 0, q_out.data_ptr() if heads else 0, lens.data_ptr(),
             0 if cu is None else cu.data_ptr(), 0 if new_lens is None else new_lens.data_ptr(),
-            0 if rot == 0 else inv_freq.data_ptr(), k.stride(0), k.stride(1), v.stride(0), v.stride(1), *q_strides, n, heads, rot,
+            0 if rot == 0 else inv_freq.data_ptr(), ks[0], ks[1], vs[0], vs[1], *q_strides, n, heads, rot,
             1 if interleaved else 0))
         return q_out
 
@@ -184,7 +187,7 @@ class PagedKV:
         if q.dim() != 3:
             raise ValueError("q must be [tokens, heads, dh]")
         shape = (q.shape[0], q.shape[1], self.dh)
-        self._heads(q, "q", shape)
+        qs = self._heads(q, "q", shape)
         self._ints(lens, "lens", (self.batch,))
         if cu is not None:
             self._ints(cu, "cu", (self.batch + 1,))
@@ -194,13 +197,14 @@ class PagedKV:
                 raise ValueError(f"prefix_pages holds {prefix_pages.shape[0]} pages, {prefix_tokens} tokens need more")
         if out is None:
             out = q.new_empty(shape)
+            os = (shape[1] * self.dh, self.dh)
         else:
-            self._heads(out, "out", shape)
+            os = self._heads(out, "out", shape)
         if shape[0] == 0 and cu is not None:
             return out
         self._run("rr_attend_shared", _SHARED.pack(
             q.data_ptr(), out.data_ptr(), lens.data_ptr(), 0 if cu is None else cu.data_ptr(),
-            0 if prefix_pages is None else prefix_pages.data_ptr(), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
+            0 if prefix_pages is None else prefix_pages.data_ptr(), qs[0], qs[1], os[0], os[1],
             shape[0], shape[1], prefix_tokens, 1 if causal else 0, scale), "rr_attend_shared_workspace")
         return out
 
@@ -215,7 +219,7 @@ class PagedKV:
         if q.dim() != 4:
             raise ValueError("q must be [batch, heads, n_q * m, dh]")
         shape = (self.batch, q.shape[1], q.shape[2], self.dh)
-        self._heads(q, "q", shape)
+        qs = self._heads(q, "q", shape)
         self._ints(lens, "lens", (self.batch,))
         if ranges.dim() != 3:
             raise ValueError("ranges must be [rows, slots, 2]")
@@ -225,10 +229,11 @@ class PagedKV:
             raise ValueError(f"{rows} range rows and {shape[2]} query tokens do not make {n_q} chunks of {self.batch} sequences")
         if out is None:
             out = q.new_empty(shape)
+            os = (shape[1] * shape[2] * self.dh, shape[2] * self.dh, self.dh)
         else:
-            self._heads(out, "out", shape)
+            os = self._heads(out, "out", shape)
         self._run("rr_attend_paged_ranges", _RANGES.pack(
-            q.data_ptr(), out.data_ptr(), ranges.data_ptr(), lens.data_ptr(), q.stride(0), q.stride(1), q.stride(2), out.stride(0),
-            out.stride(1), out.stride(2), shape[1], rows // (self.batch * n_q), n_q, shape[2] // n_q, slots, 1 if causal else 0,
+            q.data_ptr(), out.data_ptr(), ranges.data_ptr(), lens.data_ptr(), *qs[:3], *os[:3],
+            shape[1], rows // (self.batch * n_q), n_q, shape[2] // n_q, slots, 1 if causal else 0,
             scale), "rr_attend_paged_ranges_workspace")
         return out
