@@ -10,7 +10,7 @@
 //   one of up to 32 rows (a decoding step) is quartered besides: each of a stream's four warps has a copy of the rows in its 32 lanes and 16
 //   of every 64 tokens, whose weights alone are not zero there, so that the exponentials are spread over the SM.
 // The tensor pipe takes 2 x 520 cycles for a 128 x 128 x 128 tile's two products, the 16384 exponentials take 1024 on the special-function
-// unit.  Measured: 545 us for 475 GFLOP of a routed prompt (870 TFLOP/s, tensor pipe 42 %), 650 us for 481 GFLOP of prompts behind a prefix; what
+// unit.  Measured: 545 to 600 us for 475 GFLOP of a routed prompt (up to 870 TFLOP/s, tensor pipe 42 %), 650 for 481 GFLOP of prompts behind a prefix; what
 // bounds them is a stream's chain of logits, maximum, exponentials and weights, about 2000 cycles per 64 tokens of two tiles.
 //
 // Warps 0-3, 4-7: the streams, a thread per row.  8, 11: issue the products, one stream's each.  9: finds the segments.  10: the rows' limits.
