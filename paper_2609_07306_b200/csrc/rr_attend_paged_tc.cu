@@ -706,6 +706,10 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           }
           if (!ok) break;
           tiles += tile1 - tile0;
+        } else {
+          // The last groups of the segment before may be unannounced.  With no copies of its own here this warp would go on to wait for
+          // a segment that is published only when that one is done, which waits for them.
+          flush();
         }
         if (ok) seg_done(n);
       }
