@@ -410,7 +410,8 @@ int rr_kv_append(const rr_paged_kv* kv, const rr_append_args* a, void* stream);
  *   causal != 0   the queries are the sequence's last tokens: the i-th of its n sees s <= lens[b] - n + i
  *   causal == 0   every query sees all tokens (attention to states of another length, e.g. an encoder's)
  * Tokens s < prefix_tokens are the same for all sequences and are read once for all, from the pages
- * prefix_pages (NULL: those of sequence 0's table); a sequence shorter than the prefix sees its first lens[b] tokens.  Query
+ * prefix_pages (NULL: those of sequence 0's table); a sequence shorter than the prefix sees its first lens[b] tokens.  With
+ * prefix_pages the table's columns of the prefix's whole pages are not read, and it may be shorter than the prefix.  Query
  * head h reads key head h / (heads / kv_heads).  prefix_tokens == 0: nothing is shared. */
 typedef struct rr_shared_args {
   const void* q;             /* [tokens, heads, dh]                                               */

@@ -89,10 +89,10 @@ __host__ __device__ inline long long quot(long long a, long long b) {
 }
 __host__ __device__ inline long long ceil_div(long long a, long long b) { return quot(a + b - 1, b); }
 
-// Tokens that sequence b has by its length, and of these those that its table has places for.
+// Tokens that sequence b has by its length, and of these those that have places: its table's, and the prefix's, which may have pages of its own.
 __device__ __forceinline__ int seq_end(const Params& P, int b) { return max(__ldg(P.lens + b), 0); }
 __device__ __forceinline__ int seq_len(const Params& P, int b) {
-  const long long cap = (long long)P.pages_per_seq * P.page_tokens;
+  const long long cap = max((long long)P.pages_per_seq * P.page_tokens, (long long)P.prefix);
   const int n = seq_end(P, b);
   return n > cap ? (int)cap : n;
 }
