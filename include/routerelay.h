@@ -409,10 +409,11 @@ int rr_kv_append(const rr_paged_kv* kv, const rr_append_args* a, void* stream);
  * [cu[b], cu[b + 1]) of each sequence b, over the sequence's tokens s < lens[b].
  *   causal != 0   the queries are the sequence's last tokens: the i-th of its n sees s <= lens[b] - n + i
  *   causal == 0   every query sees all tokens (attention to states of another length, e.g. an encoder's)
- * Tokens s < prefix_tokens are the same for all sequences and are read once for all, from the pages
- * prefix_pages (NULL: those of sequence 0's table); a sequence shorter than the prefix sees its first lens[b] tokens.  With
- * prefix_pages the table's columns of the prefix's whole pages are not read, and it may be shorter than the prefix.  Query
- * head h reads key head h / (heads / kv_heads).  prefix_tokens == 0: nothing is shared. */
+ * Tokens s < prefix_tokens are the same for all sequences and are read once for all, from the pages prefix_pages (with
+ * which the table's columns of the prefix's whole pages are not read, and it may be shorter than the prefix), or if that is NULL
+ * from those in the table's row of the first sequence that has all of the prefix (of the longest one, if none has).  A sequence
+ * shorter than the prefix sees its first lens[b] tokens.  Query head h reads key head h / (heads / kv_heads).
+ * prefix_tokens == 0: nothing is shared. */
 typedef struct rr_shared_args {
   const void* q;             /* [tokens, heads, dh]                                               */
   void* out;                 /* [tokens, heads, dh]; rows behind cu[batch] are left as they were  */

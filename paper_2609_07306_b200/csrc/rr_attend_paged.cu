@@ -12,27 +12,38 @@ namespace {
 constexpr unsigned FULL = 0xFFFFFFFFu;
 
 // ---- plan --------------------------------------------------------------------------------------------------
-// cum[b] = tiles of all items before sequence b's: the prefix's, then the sequences' own, in their order.
+// cum[b] = tiles of all items before sequence b's: the prefix's, then the sequences' own, in their order.  The prefix's pages stand in the row of
+// the first sequence that has all of the prefix (a row tells nothing of places behind its own sequence's length), or of the longest one.
 constexpr int PLAN_NT = 1024;
 __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ Params P) {
   __shared__ long long s_warp[PLAN_NT / 32];
+  __shared__ int3 s_plan[PLAN_NT / 32];
   rr_pdl_wait();
   rr_pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // the sequences apart: if their row tiles are at most an eighth more than those of all rows together
-  int mine_tiles = 0;
-  for (int b = tid; b < P.batch; b += PLAN_NT) if (seq_len(P, b) > 0) mine_tiles += own_row_tiles(P, b);
-#pragma unroll
-  for (int off = 16; off; off >>= 1) mine_tiles += __shfl_xor_sync(FULL, mine_tiles, off);
-  if (lane == 0) s_warp[warp] = mine_tiles;
+  int tiles = 0, len = -1, at = 0;                      // row tiles; tokens of the prefix, and the lowest b that has as many
+  for (int b = tid; b < P.batch; b += PLAN_NT) {
+    const int n = seq_len(P, b);
+    if (n > 0) tiles += own_row_tiles(P, b);
+    if (min(n, P.prefix) > len) { len = min(n, P.prefix); at = b; }
+  }
+  auto reduce = [&]() {
+    tiles = __reduce_add_sync(FULL, tiles);
+    const int most = __reduce_max_sync(FULL, len);
+    at = __reduce_min_sync(FULL, len == most ? at : 0x7FFFFFFF);
+    len = most;
+  };
+  reduce();
+  if (lane == 0) s_plan[warp] = make_int3(tiles, len, at);
   __syncthreads();
-  long long row_tiles = 0;
-#pragma unroll
-  for (int w = 0; w < PLAN_NT / 32; ++w) row_tiles += s_warp[w];
+  const int3 all = s_plan[lane];
+  tiles = all.x; len = all.y; at = all.z;
+  reduce();
   const long long packed = prefix_row_tiles(P);
-  const bool apart = row_tiles <= packed + packed / 8;
-  __syncthreads();
-  const long long prefix_all = apart ? 0 : P.kv_heads * packed * prefix_tiles(P);
+  const Plan plan{tiles <= packed + packed / 8, at, len};
+  const bool apart = plan.apart;
+  const long long prefix_all = P.kv_heads * packed * prefix_tiles(plan);
   long long run = P.few_prefix ? 0 : prefix_all, run_few = P.few_prefix ? prefix_all : 0;
   auto scan = [&](long long mine, long long& run) -> long long {     // what is before this thread's, the block's sum added to run
     long long incl = mine;
@@ -62,7 +73,7 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
   if (tid == 0) {
     P.main.cum[P.batch] = run;
     if (P.few.ctas > 0) P.few.cum[P.batch] = run_few;
-    *P.apart = apart;
+    *P.plan = plan;
   }
 }
 
@@ -92,8 +103,9 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
       const Sched& sp = P.few_prefix ? P.few : P.main;
       const long long all = __ldg(P.main.cum + P.batch), all_p = P.few_prefix ? __ldg(P.few.cum + P.batch) : all, per = (long long)P.tokens * P.group;
       out = t * P.ot + h * P.oh;
-      const bool apart = __ldg(P.apart) != 0;
-      const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P);
+      const Plan plan = plan_of(P);
+      const bool apart = plan.apart;
+      const long long np = prefix_tiles(plan), qtp = prefix_row_tiles(P);
       if (np > 0) {
         const long long idx = (long long)t * P.group + g, first = (kvh * qtp + idx / ROWS) * np;
         home0 = kvh * per + idx;
@@ -712,7 +724,7 @@ size_t lay_out(Params& P, uint8_t* ws) {
   if (!P.slots) {
     P.main.cum = (long long*)(ws + at); at += up((size_t)(P.batch + 1) * 8);
     P.few.cum = (long long*)(ws + at); at += up((size_t)(P.batch + 1) * 8);
-    P.apart = (int*)(ws + at); at += up(sizeof(int));
+    P.plan = (Plan*)(ws + at); at += up(sizeof(Plan));
   }
   const size_t rows = (size_t)P.part_rows * P.streams;
   P.part_ml = (float2*)(ws + at); at += up(rows * sizeof(float2));

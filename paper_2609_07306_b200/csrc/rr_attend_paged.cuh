@@ -38,6 +38,13 @@ struct Sched {
   long long slots_at;
 };
 
+// What plan_kernel finds out from the lengths besides the tiles before each sequence's items.
+struct Plan {
+  int apart;                                           // the sequences attend by themselves, to the prefix too
+  int source;                                          // whose row of the table has the prefix's pages
+  int prefix;                                          // tokens of the prefix that any sequence has
+};
+
 struct Params {
   // cache
   const void *k, *v;
@@ -61,7 +68,7 @@ struct Params {
   int few_waits;                                       // the few kernel's inputs are its predecessor's (else it only ends after that)
   long long range_rows;                                // batch * route_heads * n_q
   // workspace
-  int* apart;                                          // shared: [1]
+  Plan* plan;                                          // shared
   float* part_o;                                       // [streams][part_rows][dh]
   float2* part_ml;                                     // [streams][part_rows]
   long long part_rows;
@@ -102,7 +109,8 @@ __device__ __forceinline__ int seq_count(const Params& P, int b) {
   const int a = __ldg(P.cu + b), e = min(__ldg(P.cu + b + 1), P.tokens);
   return a < 0 ? 0 : max(e - a, 0);
 }
-__device__ __forceinline__ long long prefix_tiles(const Params& P) { return (P.prefix + TILE - 1) / TILE; }
+__device__ __forceinline__ Plan plan_of(const Params& P) { return Plan{__ldg(&P.plan->apart), __ldg(&P.plan->source), __ldg(&P.plan->prefix)}; }
+__device__ __forceinline__ long long prefix_tiles(const Plan& plan) { return plan.apart ? 0 : (plan.prefix + TILE - 1) / TILE; }
 __device__ __forceinline__ long long prefix_row_tiles(const Params& P) { return ceil_div((long long)P.tokens * P.group, ROWS); }
 __device__ __forceinline__ int own_tiles(const Params& P, int b, bool apart) { return (max(seq_len(P, b) - (apart ? 0 : P.prefix), 0) + TILE - 1) / TILE; }
 __device__ __forceinline__ int own_row_tiles(const Params& P, int b) { return (int)ceil_div((long long)seq_count(P, b) * P.group, ROWS); }
@@ -122,14 +130,15 @@ __device__ __forceinline__ int cta_of(const Sched& sc, long long u, long long W)
 
 // The segment at tile u of CTA c's share, which ends at u1; returns how many tiles of the share it takes.
 __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int c, long long u, long long u1, Seg& s) {
-  const bool apart = __ldg(P.apart) != 0;
-  const long long np = apart ? 0 : prefix_tiles(P), qtp = prefix_row_tiles(P), before = (&sc == &P.few) == P.few_prefix ? P.kv_heads * qtp * np : 0;
+  const Plan plan = plan_of(P);
+  const bool apart = plan.apart;
+  const long long np = prefix_tiles(plan), qtp = prefix_row_tiles(P), before = (&sc == &P.few) == P.few_prefix ? P.kv_heads * qtp * np : 0;
   long long first;                                     // first tile of the item
   int tiles;
   long long home;
   const long long row_all = (long long)P.tokens * P.group;
   s.slots = nullptr;
-  s.prefix_pages = P.prefix_pages ? P.prefix_pages : P.table;
+  s.prefix_pages = P.prefix_pages ? P.prefix_pages : P.table + plan.source * P.table_stride;
   s.prefix = P.prefix;
   if (u < before) {
     const long long item = quot(u, np);
@@ -140,7 +149,7 @@ __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int 
     s.rows = (int)min((long long)ROWS, row_all - s.row0);
     s.b = -1;
     s.t_base = 0; s.t_seq0 = 0; s.n_seq = 0;
-    s.tok0 = 0; s.tok1 = P.prefix;
+    s.tok0 = 0; s.tok1 = plan.prefix;
     s.pages = s.prefix_pages;
     home = s.kvh * row_all + s.row0;
   } else {

@@ -178,7 +178,8 @@ class PagedKV:
                       cu: torch.Tensor | None = None, causal: bool = True,
                       prefix_pages: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
         """Attention of the queries [tokens, heads, dh] to their sequences' tokens in the cache, the first prefix_tokens
-        of which are the same for all sequences and read once for all (from prefix_pages, or else sequence 0's table).
+        of which are the same for all sequences and read once for all (from prefix_pages [pages] int32, or else from the table's row of
+        the first sequence that has as many tokens).
         lens    [batch] int32 tokens in the cache, the queries' own among them
         cu      as in append; rows of out behind cu[batch] are left as they were
         causal  the queries are their sequence's last tokens, and none sees a token behind its own; False: every query

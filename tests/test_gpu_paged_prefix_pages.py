@@ -62,3 +62,48 @@ def test_lengths_behind_both(dtype, dh, lens, news):
         out.append([x.view(n, 4, dh).cpu() for x in exact.attend_rows(rows, kk[:, 0], vv[:, 0], seen.repeat_interleave(4, 0), 0.1, dtype == torch.bfloat16)])
     assert_within(got, torch.cat([o for o, _ in out]), torch.cat([e for _, e in out]))
     assert status.item() == B.RR_STATUS_BAD_INDEX
+
+
+@pytest.mark.parametrize("dtype,dh", KINDS)
+@pytest.mark.parametrize("lens,news,heads", [
+    ([0, 200, 230], [1, 1, 1], 2), ([0, 200, 230], [1, 1, 1], 8), ([90, 100, 231, 160], [3, 64, 64, 0], 8),
+    ([16, 164], [0, 64], 4), ([0, 300], [64, 64], 4), ([0] * 40 + [170, 190], [1] * 42, 4)])
+def test_rows_of_the_table_behind_their_lengths(dtype, dh, lens, news, heads):
+    """A free place in the batch, or a short sequence, in front: what its row holds behind its length (other sequences' pages, no pages)
+    is nobody's prefix."""
+    g, k, v, table = pool(dtype, len(lens), 1, dh, 16, 304, 7)
+    long = next(b for b, n in enumerate(lens) if n >= 100)
+    stale, sane = table.clone(), table.clone()
+    stale[:, :6] = table[long, :6]
+    sane[:, :6] = table[long, :6]                      # 96 of the 100 tokens in shared pages, the others in copies
+    for c in (k, v):
+        for b in range(len(lens)):
+            c[table[b, 6].long(), :, :4] = c[table[long, 6].long(), :, :4].clone()
+    for b, n in enumerate(lens):
+        stale[b, -(-n // 16):] = torch.arange(-3, 300, device="cuda")[:19 - -(-n // 16)].int() if b % 2 else table[(b + 1) % len(lens), 0]
+    cu = [0]
+    for n in news:
+        cu.append(cu[-1] + n)
+    q = torch.randn((cu[-1], heads, dh), generator=g, device="cuda").to(dtype)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = PagedKV(k, v, stale, status).attend_shared(q, torch.tensor(lens, dtype=torch.int32, device="cuda"), 100, 0.1,
+                                                     cu=torch.tensor(cu, dtype=torch.int32, device="cuda"))
+    want, bound = exact.shared(q, k, v, sane, lens, cu, 0.1)
+    assert_within(got, want, bound)
+    assert status.item() == 0
+
+
+@pytest.mark.parametrize("dtype,dh", KINDS)
+@pytest.mark.parametrize("lens,heads", [([5, 40, 33], 1), ([5, 40, 33], 8), ([0, 0, 0], 8)])
+def test_every_sequence_shorter_than_the_prefix(dtype, dh, lens, heads):
+    """Places of the prefix that no sequence has are not looked up."""
+    g, k, v, table = pool(dtype, 3, 1, dh, 16, 320, 8)
+    for b, n in enumerate(lens):
+        table[b, :-(-n // 16)] = table[1, :-(-n // 16)]
+        table[b, -(-n // 16):] = -7
+    q = torch.randn((3, heads, dh), generator=g, device="cuda").to(dtype)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = PagedKV(k, v, table, status).attend_shared(q, torch.tensor(lens, dtype=torch.int32, device="cuda"), 300, 0.1)
+    want, bound = exact.shared(q, k, v, table, lens, [0, 1, 2, 3], 0.1)
+    assert_within(got, want, bound)
+    assert status.item() == 0
