@@ -39,7 +39,7 @@ using namespace sm100;
 namespace {
 
 constexpr unsigned FULL = 0xFFFFFFFFu;
-constexpr int NT = 512, IDS = 16, MAX_RING = 4;
+constexpr int NT = 512, IDS = 16, FILLS = 16, MAX_RING = 4;
 constexpr float GROWTH = 8.f;
 constexpr int BY_FMA = 2;                              // of every 8 pairs of exponentials, by multiply-adds (0: 567 us, 1: 551, 2: 544 of a routed prompt)
 
@@ -48,8 +48,13 @@ template <int D> struct Shape {
   static constexpr int HALF_BYTES = TILE * 128, TILE_BYTES = HALVES * HALF_BYTES;
 };
 
+// A wait tells phases apart by their parity only.  In a split segment each issuing warp waits for the tiles of its own stream, so the one
+// before on the same place may be the other's, and may not be there yet: `full` goes by the count of fills (fill f in f % FILLS), not by place.
+// When a warp waits for fill f, fill f - 16 is long there: f - 16 and f - 16 + STAGES share a place, and the second was asked for, so the first
+// had arrived and been released, before the last fill that this warp waited for, or before the queries of this segment (at most 4 before f).
+// (The other barriers are waited for in every phase, or, the queries' and the ids', behind one that was told later.)
 struct Ctl {
-  uint64_t full[8], empty[8], s_full[2][2], p_full[2][2], o_done[2][2], q_full[2], q_empty[2], ids_full[IDS], seg_full[MAX_RING], seg_empty[MAX_RING],
+  uint64_t full[FILLS], empty[8], s_full[2][2], p_full[2][2], o_done[2][2], q_full[2], q_empty[2], ids_full[IDS], seg_full[MAX_RING], seg_empty[MAX_RING],
       rows_full[MAX_RING], drain;
   uint32_t tmem_base, abort_flag;
   Seg seg[MAX_RING];
@@ -200,7 +205,8 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
   const int warp = __shfl_sync(FULL, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < S::STAGES; ++i) { mbar_init(&c->full[i], 4); mbar_init(&c->empty[i], 2); }
+    for (int i = 0; i < FILLS; ++i) mbar_init(&c->full[i], 4);
+    for (int i = 0; i < S::STAGES; ++i) mbar_init(&c->empty[i], 2);
     for (int i = 0; i < 2; ++i) {
       for (int h = 0; h < 2; ++h) { mbar_init(&c->s_full[i][h], 2); mbar_init(&c->p_full[i][h], 128); mbar_init(&c->o_done[i][h], 1); }
       mbar_init(&c->q_full[i], 4); mbar_init(&c->q_empty[i], 2);
@@ -654,20 +660,21 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         };
         auto load = [&](const void* cache, const CUtensorMap* map, const Where& at) -> bool {
           const uint32_t st = fills % S::STAGES;
+          uint64_t* const full = &c->full[fills % FILLS];
           if (!free_slot(&c->empty[st], (fills / S::STAGES & 1) ^ 1)) return false;
           if (at.box) {
             const int run = 64 >> at.box;
-            expect_tx_warp(&c->full[st], 32 * D * 2);
+            expect_tx_warp(full, 32 * D * 2);
 #pragma unroll 1
             for (int r = 0; r < 32; r += run) {
               const int pg = __shfl_sync(FULL, at.page, r), pl = __shfl_sync(FULL, at.place, r);
 #pragma unroll
               for (int h = 0; h < S::HALVES; ++h)
-                tma_rows_warp(kv_addr + st * S::TILE_BYTES + h * S::HALF_BYTES + (w * 32 + r) * 128, map + at.box - 1, h * 64, pl, s.kvh, pg, &c->full[st]);
+                tma_rows_warp(kv_addr + st * S::TILE_BYTES + h * S::HALF_BYTES + (w * 32 + r) * 128, map + at.box - 1, h * 64, pl, s.kvh, pg, full);
             }
           } else {
             rows32(cache, at.page < 0 ? -1 : at.page * P.page_stride + s.kvh * P.head_stride + at.place * P.token_stride, kv_addr + st * S::TILE_BYTES);
-            commit(&c->full[st]);
+            commit(full);
           }
           ++fills;
           return true;
@@ -715,7 +722,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
       }
       flush();                                         // (do not leave with copies in flight)
       for (uint32_t f = fills > S::STAGES ? fills - S::STAGES : 0; f < fills; ++f)
-        for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->full[f % S::STAGES], f / S::STAGES & 1); ++it) __nanosleep(64);
+        for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(&c->full[f % FILLS], f / FILLS & 1); ++it) __nanosleep(64);
       __syncwarp();
     } else {
       // ===== products: warp 8 those of stream 0, warp 11 those of stream 1, so that one's waits
@@ -744,7 +751,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           const int tv = paired ? k - 1 : 2 * (k - 1) + st, tk = paired ? k : 2 * k + st;
           const uint32_t fv = 2 * tiles + (tv == nt - 1 ? 2 * nt - 1 : 2 * tv + 2), fk = 2 * tiles + (tk == 0 ? 0 : 2 * tk - 1);
           const uint32_t sv = fv % S::STAGES, sk = fk % S::STAGES;
-          if (k > 0) ok = wait(&c->full[sv], fv / S::STAGES);
+          if (k > 0) ok = wait(&c->full[fv % FILLS], fv / FILLS);
           for (int h = 0; ok && h < 2; ++h) {
             if (k > 0) {
               ok = wait(&c->p_full[st][h], p_cnt);
@@ -759,7 +766,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
             if (k < steps) {
               if (h == 0) {
                 const int cnt = (int)tiles + tk;
-                ok = wait(&c->full[sk], fk / S::STAGES) && wait(&c->ids_full[cnt % IDS], cnt / IDS);
+                ok = wait(&c->full[fk % FILLS], fk / FILLS) && wait(&c->ids_full[cnt % IDS], cnt / IDS);
                 if (!ok) break;
                 tc_fence_after();
               }
