@@ -77,10 +77,202 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
   }
 }
 
+// ---- rows looked at again ---------------------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ float4 load4(const T* p, bool vec, int n);
+template <> __device__ __forceinline__ float4 load4<float>(const float* p, bool vec, int n) {
+  if (vec) return *(const float4*)p;
+  return make_float4(p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
+}
+template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p, bool vec, int n) {
+  if (vec) {
+    const uint2 t = *(const uint2*)p;
+    return make_float4(__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xFFFF0000u), __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xFFFF0000u));
+  }
+  return make_float4(__bfloat162float(p[0]), n > 1 ? __bfloat162float(p[1]) : 0.f, n > 2 ? __bfloat162float(p[2]) : 0.f, n > 3 ? __bfloat162float(p[3]) : 0.f);
+}
+
+// A marked row's outputs are what they should be unless one of the tokens that it may not see but was multiplied with holds an infinity or NaN
+// among its values; a row that sees one of its own stays as it is.  Only these tokens are looked at: of the prefix those behind the row's
+// limit, of its own or a range row's list those that share a tile with the last one seen by some row of the item.  Where one is found the row is computed
+// from the definition: a token that it does not see is not read.  (Up to 32 rows on the tensor cores multiply the other quarters' tokens with weight 0, too.
+// A NaN among these is the row's own if the row sees it, as it does unless it is found; an infinity is an infinity in its quarter's partial
+// and NaN in the others': `force`.)  `parts` warps take 32 tokens in turn, 8 of them in flight; each leaves reference, sum and output, a lane's columns 4 lane ..
+// and 128 + 4 lane ...  Bound by these loads' latency, and by the cache's traffic where many
+// rows are computed again.  Measured, a prompt of 8192 tokens, 32 heads on 8 of 128, 1.24 ms: with a NaN that all rows see 6.1 ms (looked at),
+// that only the last token sees 13.4 ms (193 tokens' rows computed again).
+struct Part { float m, l; float4 o[2]; };
+
+// The query token, head and limit of row `row` of a ranges call.
+__device__ __forceinline__ RowAt range_row(const Params& P, long long row) {
+  const int mg = P.m * P.group;
+  const long long rr = quot(row, mg), per = quot(rr, P.n_q);
+  const int idx = (int)(row - rr * mg), i = (int)(rr - per * P.n_q), b = (int)per / P.route_heads, len = seq_end(P, b);
+  RowAt a;
+  a.t = i * P.m + idx / P.group;
+  a.h = (int)per % P.route_heads * P.group + idx % P.group;
+  a.limit = P.causal ? max(len - P.n_q * P.m + a.t + 1, 0) : len;
+  return a;
+}
+
+// Calls body(at) with the lanes' places of 32 tokens at a time (-1: none) for the list's tokens in [from, to), every parts-th time.
+template <class F>
+__device__ __forceinline__ void each_tokens(const Params& P, const Seg& s, int from, int to, int part, int parts, F&& body) {
+  const int lane = threadIdx.x & 31, spans = s.slots ? P.slots : 1;
+  int turn = 0;
+  for (int j = 0; j < spans; ++j) {
+    int lo = s.tok0, hi = s.tok1;
+    if (s.slots) slot_span(s, j, lo, hi);
+    lo = max(lo, from);
+    hi = min(hi, to);
+    for (int t = lo; t < hi; t += 32) {
+      if (turn == part) body(t + lane < hi ? token_at(P, s, t + lane) : -1LL);
+      turn = turn + 1 == parts ? 0 : turn + 1;
+    }
+  }
+}
+
+template <typename T, int NV>                          // NV groups of 128 columns
+__device__ __noinline__ bool look_again(const Params& P, long long row, bool force, int part, int parts, Part& y) {
+  constexpr int N = 8 / NV;                            // tokens' loads in flight
+  const int lane = threadIdx.x & 31, e0 = lane * 4;
+  Seg s;
+  s.prefix = 0; s.prefix_pages = nullptr; s.slots = nullptr; s.tok0 = 0;
+  long long q;
+  int limit, behind;                                   // behind: unseen tokens from there on were not multiplied
+  if (P.slots) {
+    const long long rr = quot(row, P.m * P.group), per = quot(rr, P.n_q);
+    const RowAt a = range_row(P, row);
+    s.b = (int)per / P.route_heads;
+    s.kvh = (int)per % P.route_heads / (P.route_heads / P.kv_heads);
+    s.slots = P.ranges + rr * P.slots * 2;
+    s.tok1 = seq_len(P, s.b);
+    q = s.b * P.qb + a.h * P.qh + a.t * P.qt;
+    limit = a.limit;
+    behind = s.tok1;
+  } else {
+    const int t = (int)quot(row, P.heads), h = (int)(row - (long long)t * P.heads);
+    const Plan plan = plan_of(P);
+    s.b = P.cu ? rr_sequence_of(P.cu, P.batch, t) : t;
+    s.kvh = h / P.group;
+    s.tok1 = seq_len(P, s.b);
+    s.prefix = P.prefix;
+    s.prefix_pages = P.prefix_pages ? P.prefix_pages : P.table + plan.source * P.table_stride;
+    const int n = seq_count(P, s.b), len = seq_end(P, s.b);
+    q = t * P.qt + h * P.qh;
+    limit = P.causal ? max(len - n + (t - seq_first(P, s.b)) + 1, 0) : len;
+    behind = (int)min((long long)s.tok1, (long long)limit + ROWS / P.group + 1 + TILE);
+    if (prefix_tiles(plan) > 0) behind = max(behind, plan.prefix);
+  }
+  s.pages = P.table + s.b * P.table_stride;
+  auto values = [&](const void* from, long long at, int i0, float4 (&x)[N][NV]) {
+    auto load = [&](bool vec) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const long long o = __shfl_sync(FULL, at, i0 + i);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const int e = e0 + 128 * v;
+          x[i][v] = o >= 0 && e < P.dh ? load4<T>((const T*)from + o + e, vec, P.dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+    };
+    if (P.vk) load(true); else load(false);            // (one branch for all loads: they are under way together)
+  };
+  if (!force) {
+    const int tok1 = s.tok1;
+    bool found = false;
+    s.tok1 = max(tok1, behind);                        // (a sequence shorter than the prefix has been multiplied with all of it)
+    each_tokens(P, s, limit, behind, 0, 1, [&](long long at) {
+#pragma unroll 1
+      for (int i0 = 0; i0 < 32; i0 += N) {
+        float4 x[N][NV];
+        values(P.v, at, i0, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+          for (int v = 0; v < NV; ++v) found = found || !(isfinite(x[i][v].x) && isfinite(x[i][v].y) && isfinite(x[i][v].z) && isfinite(x[i][v].w));
+      }
+    });
+    s.tok1 = tok1;
+    if (!__any_sync(FULL, found)) return false;
+  }
+  float4 qv[NV], o[2];
+  float m = NINF, l = 0.f;
+  bool seen = false;
+  o[0] = o[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int e = e0 + 128 * v;
+    qv[v] = e < P.dh ? load4<T>((const T*)P.q + q + e, P.vq, P.dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  each_tokens(P, s, 0, limit, part, parts, [&](long long at) {
+    const unsigned sees = __ballot_sync(FULL, at >= 0);
+    seen = seen || sees != 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < 32; i0 += N) {
+      if (!(sees >> i0 & ((1u << N) - 1))) continue;
+      float4 k[N][NV], w[N][NV];
+      values(P.k, at, i0, k);
+      values(P.v, at, i0, w);
+      float z[N], top = NINF;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        z[i] = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) z[i] = fmaf(qv[v].w, k[i][v].w, fmaf(qv[v].z, k[i][v].z, fmaf(qv[v].y, k[i][v].y, fmaf(qv[v].x, k[i][v].x, z[i]))));
+#pragma unroll
+        for (int off = 16; off; off >>= 1) z[i] += __shfl_xor_sync(FULL, z[i], off);
+        z[i] = sees >> (i0 + i) & 1 ? z[i] * P.scale_log2 : NINF;
+        top = fmaxf(top, z[i]);
+      }
+      const float now = fmaxf(m, top), ref = now == NINF ? 0.f : now, f = exp2f(m - ref);
+      m = now;
+      l *= f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) { o[v].x *= f; o[v].y *= f; o[v].z *= f; o[v].w *= f; }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (!(sees >> (i0 + i) & 1)) continue;
+        const float p = exp2f(z[i] - ref);
+        l += p;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          o[v].x = fmaf(p, w[i][v].x, o[v].x); o[v].y = fmaf(p, w[i][v].y, o[v].y);
+          o[v].z = fmaf(p, w[i][v].z, o[v].z); o[v].w = fmaf(p, w[i][v].w, o[v].w);
+        }
+      }
+    }
+  });
+  y.m = seen && m == NINF ? LOWEST : m;
+  y.l = l;
+  y.o[0] = o[0];
+  y.o[1] = o[1];
+  return true;
+}
+template <typename T>
+__device__ __forceinline__ bool look_again(const Params& P, long long row, bool force, int part, int parts, Part& y) {
+  return P.dh <= 128 ? look_again<T, 1>(P, row, force, part, parts, y) : look_again<T, 2>(P, row, force, part, parts, y);
+}
+
+// The row's output, a lane its columns.  No weight at all: zeros for a row without tokens, NaN for one whose tokens are all at -inf.
+template <typename T>
+__device__ __forceinline__ void write_row(const Params& P, long long out, float m, float l, const float4 (&o)[2]) {
+  const int e0 = (threadIdx.x & 31) * 4;
+  const float inv = l == 0.f ? (m == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / l;
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    const float y[4] = {o[v].x, o[v].y, o[v].z, o[v].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (e0 + 128 * v + j < P.dh) ((T*)P.out)[out + e0 + 128 * v + j] = rr_from_f32<T>(y[j] * inv);
+  }
+}
+
 // ---- join --------------------------------------------------------------------------------------------------
 // WPR warps join the partials of one row: o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Each warp takes every WPR-th partial, eight of
 // them in flight, a lane four columns (and four more 128 further on); the warps' parts are added in their order.  One warp where rows
 // are many, eight where they are few (and their partials many: up to a hundred and fifty for a row of one short call).
+// A row with a marked partial, or of a marked item, is looked at again, and computed again by the same warps if it has to be.
 template <typename T, int WPR>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params P) {
   __shared__ __align__(16) float s_o[WPR > 1 ? 8 : 1][RR_PAGED_MAX_DH], s_l[8], s_m[8];
@@ -93,7 +285,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   long long home0 = 0, home1 = 0;
   int c0 = 0, c1 = 0, cnt0 = 0, cnt1 = 0, st0 = 1, st1 = 1, r0 = 0, r1 = 0;
   long long out = 0;
-  bool mine = true, few1 = false;
+  bool mine = true, few1 = false, whole = false, again = false;
   if (P.slots == 0) {
     mine = row < (long long)P.tokens * H;
     const int t = (int)quot(mine ? row : 0, H), h = (int)((mine ? row : 0) - (long long)t * H), kvh = h / P.group, g = h - kvh * P.group;
@@ -125,9 +317,11 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
         r1 = (int)(idx % ROWS);
         c1 = cta_of(sc, first, W);
         cnt1 = cta_of(sc, first + no - 1, W) - c1 + 1;
-        st1 = few1 ? 1 : partials_of(P.streams, min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS));
+        const long long rows = min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS);
+        st1 = few1 ? 1 : partials_of(P.streams, rows);
+        whole = np == 0 && cnt1 == 1 && st1 == 1;      // (one segment with all of the row's tiles wrote the output itself)
+        again = whole && !few1 && leaves_marks(P, rows) && P.marks[kvh * per + (long long)t * P.group + g];
       }
-      if (no > 0 && np == 0 && cnt1 == 1 && st1 == 1) mine = false;      // (one segment with all of the row's tiles wrote the output itself)
     }
   } else {
     const int mg = P.m * P.group;
@@ -144,11 +338,13 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
       cnt0 = cta_of(sc, first + P.units - 1, W) - c0 + 1;
       r0 = idx % ROWS;
     }
-    if (cnt0 == 1 && st0 == 1) mine = false;           // (one segment with all of the row's tiles wrote the output itself)
+    whole = cnt0 == 1 && st0 == 1;                     // (one segment with all of the row's tiles wrote the output itself)
+    again = mine && whole && P.few.ctas == 0 && leaves_marks(P, min(ROWS, mg - idx / ROWS * ROWS)) && P.marks[row];
     out = b * P.ob + (r * P.group + idx % P.group) * P.oh + (i * P.m + idx / P.group) * P.ot;
   }
+  mine = mine && (!whole || again);
   if (WPR == 1 && !mine) return;
-  const int n0 = cnt0 * st0, n = n0 + cnt1 * st1;
+  const int n0 = whole ? 0 : cnt0 * st0, n = whole ? 0 : n0 + cnt1 * st1;
   const bool few0 = P.slots ? P.few.ctas > 0 : P.few_prefix;
   auto place = [&](int k) -> long long {               // partial row of the k-th partial
     const bool w = k >= n0;
@@ -175,7 +371,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
       at = place(k);
       const float2 ml = P.part_ml[at];
       if (ml.x == NINF || (ml.x == LOWEST && ml.y == 0.f)) at = -1;      // nothing in it (and no output written)
-      else { w = exp2f(ml.x - M); l = fmaf(w, ml.y, l); }
+      else { w = exp2f(ml.x - M); l = fmaf(w, fabsf(ml.y), l); }
+      again = again || has_mark(ml.y);
     }
     const int lim = min(32, (n - k0 + WPR - 1) / WPR);
     for (int u0 = 0; u0 < lim; u0 += 8) {
@@ -203,11 +400,29 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   }
 #pragma unroll
   for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(FULL, l, off);
-  if (WPR > 1) {
+  auto leave = [&]() {
     if (lane == 0) { s_l[warp] = l; s_m[warp] = M; }
     *(float4*)&s_o[warp][e0] = o[0];
     *(float4*)&s_o[warp][e0 + 128] = o[1];
-    __syncthreads();
+  };
+  if (WPR > 1) { leave(); again = __syncthreads_or(again); } else { again = __any_sync(FULL, again); }
+  if (again) {                                         // (all warps of the row are here, and agree)
+    bool force = false;
+    if (st0 == 8 || st1 == 8)
+      for (int k = 0; k < n; ++k) {
+        const float2 ml = P.part_ml[place(k)];
+        for (int e = lane; e < P.dh && has_mark(ml.y); e += 32) force = force || isinf(P.part_o[place(k) * P.dh + e]);
+      }
+    force = __any_sync(FULL, force);
+    Part y;
+    if (look_again<T>(P, row, force, part, WPR, y)) {
+      M = y.m; l = y.l; o[0] = y.o[0]; o[1] = y.o[1];
+      if (WPR > 1) { __syncthreads(); leave(); __syncthreads(); }
+    } else if (whole) {
+      return;                                          // what is there may stay
+    }
+  }
+  if (WPR > 1) {
     if (part != 0 || !mine) return;
     float top = M;
 #pragma unroll
@@ -224,14 +439,26 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
     }
     M = top;
   }
-  // no weight at all: zeros for a row without tokens, NaN for one whose tokens are all at -inf
-  const float inv = l == 0.f ? (M == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / l;
-#pragma unroll
-  for (int v = 0; v < 2; ++v) {
-    const float y[4] = {o[v].x, o[v].y, o[v].z, o[v].w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (e0 + 128 * v + j < P.dh) ((T*)P.out)[out + e0 + 128 * v + j] = rr_from_f32<T>(y[j] * inv);
+  write_row<T>(P, out, M, l, o);
+}
+
+// Marked rows of a ranges call whose items are all whole: nothing to join.
+template <typename T>
+__global__ void __launch_bounds__(256) marked_kernel(const __grid_constant__ Params P) {
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  const int lane = threadIdx.x & 31, mg = P.m * P.group;
+  const long long rows = P.range_rows * mg;
+  for (long long row0 = ((long long)blockIdx.x * 256 + threadIdx.x) / 32 * 32; row0 < rows; row0 += (long long)gridDim.x * 256) {
+    unsigned marked = __ballot_sync(FULL, row0 + lane < rows && P.marks[row0 + lane]);
+    while (marked) {
+      const long long row = row0 + __ffs(marked) - 1;
+      marked &= marked - 1;
+      Part y;
+      if (!look_again<T>(P, row, false, 0, 1, y)) continue;
+      const RowAt a = range_row(P, row);
+      write_row<T>(P, quot(row, mg) / P.n_q / P.route_heads * P.ob + a.h * P.oh + a.t * P.ot, y.m, y.l, y.o);
+    }
   }
 }
 
@@ -263,30 +490,16 @@ __host__ __device__ inline SmemPlan smem_plan(int dh, int n_slots, bool only_few
   return s;
 }
 
-template <typename T> __device__ __forceinline__ float4 load4(const T* p, bool vec, int n);
-template <> __device__ __forceinline__ float4 load4<float>(const float* p, bool vec, int n) {
-  if (vec) return *(const float4*)p;
-  return make_float4(p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
-}
-template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p, bool vec, int n) {
-  if (vec) {
-    const uint2 t = *(const uint2*)p;
-    return make_float4(__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xFFFF0000u), __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xFFFF0000u));
-  }
-  return make_float4(__bfloat162float(p[0]), n > 1 ? __bfloat162float(p[1]) : 0.f, n > 2 ? __bfloat162float(p[2]) : 0.f, n > 3 ? __bfloat162float(p[3]) : 0.f);
-}
-
 struct Ctx {
   float *q, *kv, *p;
   int* id;
   long long* at;
   int *first, *base;                                   // ranges: number of a slot's first token, and its start minus that
   int n_tok;
-  bool vq, vk;                                         // queries / cache rows split into aligned groups of four
 };
 
 template <typename T, int NV, int MR>
-__device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, uint32_t* s_bad) {
+__device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0) {
   constexpr int BM = 16 * MR;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, dh = P.dh, ld = padded(dh), groups = (dh + 3) / 4;
   for (int u = tid; u < BM * groups; u += SNT) {
@@ -295,7 +508,7 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
     if (r0 + r < s.rows) {
       const int idx = s.row0 + r0 + r, dt = idx / P.group;
       const RowAt a{s.t_base + dt, s.h0 + idx - dt * P.group, 0};
-      x = load4<T>((const T*)P.q + q_at(P, s, a) + e, c.vq, dh - e);
+      x = load4<T>((const T*)P.q + q_at(P, s, a) + e, P.vq, dh - e);
     }
     *(float4*)(c.q + r * ld + e) = x;
   }
@@ -336,7 +549,7 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
     for (int u = tid; u < BT * groups; u += SNT) {
       const int r = u / groups, e = (u - r * groups) * 4;
       const long long at = c.at[r];
-      *(float4*)(c.kv + r * ld + e) = at < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : load4<T>((const T*)P.k + at + e, c.vk, dh - e);
+      *(float4*)(c.kv + r * ld + e) = at < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : load4<T>((const T*)P.k + at + e, P.vk, dh - e);
     }
     __syncthreads();
     float x[MR][4];
@@ -361,7 +574,7 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
     for (int u = tid; u < BT * groups; u += SNT) {
       const int r = u / groups, e = (u - r * groups) * 4;
       const long long at = c.at[r];
-      *(float4*)(c.kv + r * ld + e) = at < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : load4<T>((const T*)P.v + at + e, c.vk, dh - e);
+      *(float4*)(c.kv + r * ld + e) = at < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : load4<T>((const T*)P.v + at + e, P.vk, dh - e);
     }
 #pragma unroll
     for (int i = 0; i < MR; ++i) {
@@ -414,29 +627,28 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
     }
   }
   // sums over the row's sixteen threads, partial rows out
-  __syncthreads();                                     // (the block before has read its bits)
-  if (tid < 2) s_bad[tid] = 0;
-  __syncthreads();
 #pragma unroll
   for (int i = 0; i < MR; ++i) {
     float sum = l[i];
-    int any = seen >> i & 1, masked = mixed;
-    bool odd = false;
+    int any = seen >> i & 1, masked = mixed, odd = 0;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) odd = odd || !(isfinite(o[i][v].x) && isfinite(o[i][v].y) && isfinite(o[i][v].z) && isfinite(o[i][v].w));
+    for (int v = 0; v < NV; ++v) odd |= !(isfinite(o[i][v].x) && isfinite(o[i][v].y) && isfinite(o[i][v].z) && isfinite(o[i][v].w));
 #pragma unroll
     for (int off = 8; off; off >>= 1) {
       sum += __shfl_xor_sync(FULL, sum, off);
       any |= __shfl_xor_sync(FULL, any, off);
       masked |= __shfl_xor_sync(FULL, masked, off);
+      odd |= __shfl_xor_sync(FULL, odd, off);
     }
     const int r = ty + 16 * i;
-    if (odd && masked) atomicOr(&s_bad[r >> 5], 1u << (r & 31));
     if (r0 + r >= s.rows) continue;
     if (any && m[i] == NINF) m[i] = LOWEST;
     const RowAt a = row_at(P, s, r0 + r);
     const long long at = s.part + r0 + r;
-    if (!s.whole && tx == 0) P.part_ml[at] = make_float2(m[i], sum);
+    if (tx == 0) {
+      if (s.whole) P.marks[s.mark + r0 + r] = odd && masked;
+      else P.part_ml[at] = make_float2(m[i], with_mark(sum, odd && masked));
+    }
     const float inv = sum == 0.f ? (m[i] == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / sum;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -450,32 +662,13 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0, 
         }
     }
   }
-  __syncthreads();
-  for (int r = tid >> 5; r < BM && r0 + r < s.rows; r += SNT / 32) {
-    if (!(s_bad[r >> 5] >> (r & 31) & 1)) continue;
-    float mm, ll, oo[RR_PAGED_MAX_DH / 32];
-    repair_row<T>(P, s, r0 + r, 0, 1, -1, mm, ll, oo);
-    const int lane = tid & 31;
-    const RowAt a = row_at(P, s, r0 + r);
-    const long long at = s.part + r0 + r;
-    if (!s.whole && lane == 0) P.part_ml[at] = make_float2(mm, ll);
-    const float inv = ll == 0.f ? (mm == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / ll;
-#pragma unroll
-    for (int e = 0; e < RR_PAGED_MAX_DH / 32; ++e)
-      if (lane + 32 * e < dh) {
-        if (s.whole) ((T*)P.out)[out_at(P, s, a) + lane + 32 * e] = rr_from_f32<T>(oo[e] * inv);
-        else P.part_o[at * dh + lane + 32 * e] = oo[e];
-      }
-  }
 }
 
 // Up to FEW rows: nothing to share but the loads, so no tiles.  A warp takes 8 loads of keys and 8 of values at a time, of 32 lanes
 // x 4 entries (16 tokens of up to 64 entries, 8 tokens of more), all in flight at once behind the next ones' page look-up, for R rows: the
 // dot products' halves are exchanged until a token's logit is left in LPT / 8 lanes, and its weight goes back to the
-// token's lanes for the values.  A token that a row does not see is not multiplied, so nothing needs repair.  The warps' parts
+// token's lanes for the values.  A token that a row does not see is not multiplied, so no row is marked.  The warps' parts
 // are joined at the end.  Bound by the cache's traffic (one query per row: through L2) and by latency.
-constexpr int FEW = 8;
-
 template <typename T, int LPT, int W, int R, int WARPS>      // LPT lanes x W groups of 4 entries per token
 __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, float* s_part) {
   constexpr int N = 8, TP = 32 / LPT, BLOCK = N * TP, ROW = LPT * W * 4, DUP = LPT / N;
@@ -492,7 +685,7 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const int e = (sub + LPT * w) * 4;
-      q[r][w] = live && e < dh ? load4<T>((const T*)P.q + q_at(P, s, a) + e, c.vq, dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
+      q[r][w] = live && e < dh ? load4<T>((const T*)P.q + q_at(P, s, a) + e, P.vq, dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
       acc[r][w] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
   }
@@ -523,7 +716,7 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const long long o = __shfl_sync(FULL, at, i * TP + grp);
-        z[i] = o >= 0 && e < dh ? load4<T>((const T*)from + o + e, c.vk, dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
+        z[i] = o >= 0 && e < dh ? load4<T>((const T*)from + o + e, P.vk, dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
     };
     if (W == 1) { load(P.k, 0, x); load(P.v, 0, y); }
@@ -623,7 +816,7 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
       ((T*)P.out)[out_at(P, s, row_at(P, s, r0 + r)) + e] = rr_from_f32<T>(o * inv);
     } else {
       P.part_o[at * dh + e] = o;
-      if (e == 0) P.part_ml[at] = make_float2(M, L);
+      if (e == 0) P.part_ml[at] = make_float2(M, with_mark(L, false));
     }
   }
   __syncthreads();
@@ -633,9 +826,8 @@ __device__ void few_rows(const Params& P, const Seg& s, const Ctx& c, int r0, fl
 // segments' latencies side by side (2048 rows of 396 tokens, fp32, dh 64: 98 us with eight warps and two to an SM, 75 us).
 constexpr int FEW_NT = 128;
 template <typename T, int NV, bool ONLY_FEW>
-__global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) attend_simt_kernel(const __grid_constant__ Params P, bool vq, bool vk) {
+__global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) attend_simt_kernel(const __grid_constant__ Params P) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ uint32_t s_bad[2];
   rr_pdl_wait();
   rr_pdl_trigger();
   const SmemPlan L = smem_plan(P.dh, P.slots, ONLY_FEW);
@@ -643,7 +835,7 @@ __global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) att
   c.q = (float*)(smem + L.q); c.kv = (float*)(smem + L.kv); c.p = (float*)(smem + L.p);
   c.at = (long long*)(smem + L.ids); c.id = (int*)(c.at + BT);
   c.first = (int*)(smem + L.slots); c.base = c.first + P.slots + 1;
-  c.n_tok = 0; c.vq = vq; c.vk = vk;
+  c.n_tok = 0;
   const int lane = threadIdx.x & 31;
   long long u, u1;
   const bool turns = P.slots && !P.units;              // whole items in turn
@@ -683,8 +875,8 @@ __global__ void __launch_bounds__(ONLY_FEW ? FEW_NT : SNT, ONLY_FEW ? 4 : 2) att
       if (s.rows == 1) few_rows<T, LPT, W, 1, WARPS>(P, s, c, 0, c.q);
       else for (int r0 = 0; r0 < s.rows; r0 += R) few_rows<T, LPT, W, R, WARPS>(P, s, c, r0, c.q);
     } else if constexpr (!ONLY_FEW) {
-      if (s.rows <= 16) rows_block<T, NV, 1>(P, s, c, 0, s_bad);
-      else for (int r0 = 0; r0 < s.rows; r0 += 64) rows_block<T, NV, 4>(P, s, c, r0, s_bad);
+      if (s.rows <= 16) rows_block<T, NV, 1>(P, s, c, 0);
+      else for (int r0 = 0; r0 < s.rows; r0 += 64) rows_block<T, NV, 4>(P, s, c, r0);
     }
   }
 }
@@ -694,15 +886,12 @@ template <typename T>
 cudaError_t launch_simt(const Params& P, int grid, cudaStream_t st) {
   const bool few = P.slots && P.m * P.group <= FEW;
   const SmemPlan L = smem_plan(P.dh, P.slots, few);
-  const uintptr_t b = 4 * sizeof(T) - 1;
-  const bool vq = P.dh % 4 == 0 && ((uintptr_t)P.q & b) == 0 && (P.qb | P.qh | P.qt) % 4 == 0;
-  const bool vk = P.dh % 4 == 0 && (((uintptr_t)P.k | (uintptr_t)P.v) & b) == 0 && (P.page_stride | P.head_stride | P.token_stride) % 4 == 0;
   auto go = [&](auto kernel, unsigned long long& done) {
     cudaError_t e = rr_once_per_device(done, [&] {
       return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_plan(RR_PAGED_MAX_DH, RR_MAX_RANGE_SLOTS, false).total);
     });
     if (e != cudaSuccess) return e;
-    return rr_launch_pdl(kernel, grid, few ? FEW_NT : SNT, (size_t)L.total, st, P, vq, vk);
+    return rr_launch_pdl(kernel, grid, few ? FEW_NT : SNT, (size_t)L.total, st, P);
   };
   static unsigned long long done[8];
   switch ((P.dh + 63) / 64 + (few ? 4 : 0)) {
@@ -718,7 +907,12 @@ cudaError_t launch_simt(const Params& P, int grid, cudaStream_t st) {
 }
 
 size_t up(size_t x) { return (x + 255) / 256 * 256; }
-// Offsets in the workspace: the plan, part_ml, part_o.
+// Rows that a whole item may write without partials and mark.
+size_t mark_rows(const Params& P) {
+  if (P.slots) return P.few.ctas == 0 && leaves_marks(P, (long long)P.m * P.group) ? (size_t)P.range_rows * P.m * P.group : 0;
+  return leaves_marks(P, (long long)P.tokens * P.group) ? (size_t)P.tokens * P.heads : 0;
+}
+// Offsets in the workspace: the plan, part_ml, part_o, marks.
 size_t lay_out(Params& P, uint8_t* ws) {
   size_t at = 0;
   if (!P.slots) {
@@ -729,7 +923,14 @@ size_t lay_out(Params& P, uint8_t* ws) {
   const size_t rows = (size_t)P.part_rows * P.streams;
   P.part_ml = (float2*)(ws + at); at += up(rows * sizeof(float2));
   P.part_o = (float*)(ws + at); at += up(rows * P.dh * sizeof(float));
+  P.marks = ws + at; at += up(mark_rows(P));
   return at;
+}
+
+void groups_of_four(Params& P, int dtype) {
+  const uintptr_t b = dtype == RR_BF16 ? 7 : 15;
+  P.vq = P.dh % 4 == 0 && ((uintptr_t)P.q & b) == 0 && (P.qb | P.qh | P.qt) % 4 == 0;
+  P.vk = P.dh % 4 == 0 && (((uintptr_t)P.k | (uintptr_t)P.v) & b) == 0 && (P.page_stride | P.head_stride | P.token_stride) % 4 == 0;
 }
 
 int fill(const rr_paged_kv* kv, Params& P) {
@@ -773,6 +974,7 @@ int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   P.tokens = a->tokens; P.heads = a->heads; P.group = a->heads / kv->kv_heads; P.causal = a->causal; P.prefix = a->prefix_tokens;
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
+  groups_of_four(P, kv->dtype);
   const long long homes = 2LL * P.tokens * P.heads;
   P.main = Sched{rr_sm_count() * (P.tc ? 1 : 2), ROWS, nullptr, homes};
   P.part_rows = homes + (long long)P.main.ctas * ROWS;
@@ -808,6 +1010,7 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.range_rows = (long long)kv->batch * a->route_heads * a->n_q;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
+  groups_of_four(P, kv->dtype);
   const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS), homes = P.range_rows * P.m * P.group;
   const bool few = P.tc && (long long)P.m * P.group <= FEW_ROWS;
   if (few) P.tc = 0;
@@ -853,6 +1056,11 @@ int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, co
     const int grid = (int)(few ? rows : ceil_div(rows, 8));
     auto join = [&](auto one, auto eight) { return rr_launch_pdl(few ? eight : one, grid, 256, 0, st, P); };
     e = dtype == RR_BF16 ? join(join_kernel<__nv_bfloat16, 1>, join_kernel<__nv_bfloat16, 8>) : join(join_kernel<float, 1>, join_kernel<float, 8>);
+    ++launches;
+  }
+  if (e == cudaSuccess && P.slots && P.part_rows == 0 && mark_rows(P) > 0) {
+    const int grid = (int)std::min<long long>(ceil_div(mark_rows(P), 256), 8 * rr_sm_count());
+    e = dtype == RR_BF16 ? rr_launch_pdl(marked_kernel<__nv_bfloat16>, grid, 256, 0, st, P) : rr_launch_pdl(marked_kernel<float>, grid, 256, 0, st, P);
     ++launches;
   }
   rr_count_launch(launches);

@@ -72,6 +72,8 @@ struct Params {
   float* part_o;                                       // [streams][part_rows][dh]
   float2* part_ml;                                     // [streams][part_rows]
   long long part_rows;
+  uint8_t* marks;                                      // of rows that are written without partials: [tokens * heads] or [range_rows * m * group]
+  int vq, vk;                                          // queries / cache rows split into aligned groups of four
 };
 
 struct Seg {
@@ -88,6 +90,7 @@ struct Seg {
   int tile0, tile1;                                    // the segment's tiles of the list (ranges: once counted)
   int unit0, unit1;                                    // ranges: the segment's units of the item's `units` (of 1 if whole)
   long long part;                                      // partial row of row 0
+  long long mark;                                      // row 0's place among the marks
 };
 
 // a / b for a >= 0, b > 0; mostly both fit 32 bits, whose division takes a fifth of the time
@@ -169,6 +172,7 @@ __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int 
     s.pages = P.table + b * P.table_stride;
     home = (P.kv_heads + s.kvh) * row_all + (long long)s.t_base * P.group + s.row0;
   }
+  s.mark = s.kvh * row_all + (long long)s.t_base * P.group + s.row0;
   s.h0 = s.kvh * P.group;
   s.tile0 = (int)(u - first);
   s.tile1 = (int)min((long long)tiles, u1 - first);
@@ -203,6 +207,7 @@ __device__ __forceinline__ int range_segment(const Params& P, const Sched& sc, i
   s.slots = P.ranges + row * P.slots * 2;
   s.prefix = 0;
   s.tile0 = s.tile1 = 0;
+  s.mark = row * mg + s.row0;
   s.part = s.unit0 == 0 ? row * mg + s.row0 : sc.slots_at + (long long)c * sc.slot_rows;
   return s.unit1 - s.unit0;
 }
@@ -254,51 +259,15 @@ __device__ __forceinline__ long long token_at(const Params& P, const Seg& s, int
   return page * P.page_stride + s.kvh * P.head_stride + (tok - col * P.page_tokens) * P.token_stride;
 }
 
-// ---- exact repair ------------------------------------------------------------------------------------------
+// ---- marks -------------------------------------------------------------------------------------------------
 // A tile is multiplied whole, so a value that a row may not see enters the row's sums with weight 0: nothing, unless it is an
-// infinity or NaN.  A row with such a result that has masked tokens of its list is computed again here, token by
-// token, by a warp: only what it sees is read.  (Rows that see an infinity come here as well, and keep it.)
-// Tiles tile0 + first, tile0 + first + step, ... of the segment; quarter >= 0: of every 64 tokens the 16 from 16 * quarter on.
-template <typename T>
-__device__ __noinline__ void repair_row(const Params& P, const Seg& s, int r, int first, int step, int quarter, float& m, float& l, float (&o)[RR_PAGED_MAX_DH / 32]) {
-  constexpr int E = RR_PAGED_MAX_DH / 32;
-  const int lane = threadIdx.x & 31;
-  const RowAt a = row_at(P, s, r);
-  const T* const q = (const T*)P.q + q_at(P, s, a);
-  float qv[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) { qv[e] = lane + 32 * e < P.dh ? rr_to_f32(q[lane + 32 * e]) : 0.f; o[e] = 0.f; }
-  m = NINF; l = 0.f;
-  bool seen = false;
-  long long num = 0;                                   // number of the span's first token in the list
-  const int spans = s.slots ? P.slots : 1;
-  for (int j = 0; j < spans; ++j) {
-    int lo = s.tok0, hi = s.tok1;
-    if (s.slots) slot_span(s, j, lo, hi);
-    for (int tok = lo; tok < hi; ++tok) {
-      const long long n = num + (tok - lo), tile = n / TILE;
-      if (tile < s.tile0 + first || tile >= s.tile1 || (tile - s.tile0 - first) % step != 0 || (quarter >= 0 && (n >> 4 & 3) != quarter)) continue;
-      if (tok >= a.limit) continue;
-      const long long at = token_at(P, s, tok);
-      if (at < 0) continue;
-      seen = true;
-      float x = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) x = fmaf(qv[e], rr_to_f32(((const T*)P.k)[at + lane + 32 * e]), x);
-#pragma unroll
-      for (int off = 16; off; off >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, off);
-      x *= P.scale_log2;
-      const float m_new = fmaxf(m, x), ref = m_new == NINF ? 0.f : m_new;
-      const float f = exp2f(m - ref), w = exp2f(x - ref);
-      l = l * f + w;
-      m = m_new;
-#pragma unroll
-      for (int e = 0; e < E; ++e) if (lane + 32 * e < P.dh) o[e] = fmaf(w, rr_to_f32(((const T*)P.v)[at + lane + 32 * e]), o[e] * f);
-    }
-    num += hi - lo;
-  }
-  if (seen && m == NINF) m = LOWEST;
-}
+// infinity or NaN.  A row with such a result that had masked tokens of its list is marked, by the sign of its partial's sum or, where it has
+// none, by a byte, and looked at again when everything else is done (look_again in rr_attend_paged.cu): the kernels' pipelines do not wait for it.
+__device__ __forceinline__ float with_mark(float l, bool mark) { return __uint_as_float((__float_as_uint(l) & 0x7FFFFFFFu) | (mark ? 0x80000000u : 0u)); }
+__device__ __forceinline__ bool has_mark(float l) { return __float_as_uint(l) >> 31; }
+// Whether a whole item of `rows` rows leaves marks: those of up to FEW rows multiply no masked token.
+constexpr int FEW = 8;
+__host__ __device__ inline bool leaves_marks(const Params& P, long long rows) { return rows > (P.tc ? TILE : FEW); }
 
 }  // namespace rrattn
 

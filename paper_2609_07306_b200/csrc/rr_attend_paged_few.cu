@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(NT, 3) attend_few_kernel(const __grid_constant
         ((__nv_bfloat16*)P.out)[out_at(P, s, RowAt{s.t_base + dt, s.h0 + idx - dt * P.group, 0}) + c] = __float2bfloat16_rn(o * inv);
       } else {
         P.part_o[(s.part + r) * D + c] = o;
-        if (c == 0) P.part_ml[s.part + r] = make_float2(M, L);
+        if (c == 0) P.part_ml[s.part + r] = make_float2(M, with_mark(L, false));
       }
     }
     __syncthreads();                                   // (the parts and the table are free)

@@ -411,7 +411,6 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         const float inv = sum == 0.f ? (ref == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / sum;
         const RowAt a{s.t_base + (s.row0 + r) / P.group, s.h0 + (s.row0 + r) % P.group, 0};
         __nv_bfloat16* const out = (__nv_bfloat16*)P.out + out_at(P, s, a);
-        if (live && !direct) P.part_ml[at] = make_float2(ref, sum);
         // only then can a value have come in that its row may not see, or that belongs to another quarter
         mixed = mixed || quart;
         const bool look = __any_sync(FULL, mixed);
@@ -482,22 +481,10 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
             }
           }
         }
-        __syncwarp();                                  // (the repair below writes rows that other lanes have written)
-        unsigned again = __ballot_sync(FULL, live && odd_rows && mixed);
-        while (again) {
-          const int who = __ffs(again) - 1;
-          again &= again - 1;
-          float m, l, y[RR_PAGED_MAX_DH / 32];
-          repair_row<__nv_bfloat16>(P, s, r - lane + who, paired ? 0 : st, paired ? 1 : 2, quart ? quarter : -1, m, l, y);
-          const long long atw = __shfl_sync(FULL, at, who);
-          __nv_bfloat16* const outw = (__nv_bfloat16*)__shfl_sync(FULL, (unsigned long long)out, who);
-          if (!direct && lane == 0) P.part_ml[atw] = make_float2(m, l);
-          const float iw = l == 0.f ? (m == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / l;
-#pragma unroll
-          for (int e = 0; e < D / 32; ++e) {
-            if (direct) outw[lane + 32 * e] = __float2bfloat16_rn(y[e] * iw);
-            else P.part_o[atw * D + lane + 32 * e] = y[e];
-          }
+        if (live) {
+          const bool mark = odd_rows && mixed;
+          if (direct) P.marks[s.mark + r] = mark;
+          else P.part_ml[at] = make_float2(ref, with_mark(sum, mark));
         }
       }
       tc_fence_before();
