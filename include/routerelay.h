@@ -367,6 +367,7 @@ int rr_attend_token_ranges(const int32_t* ranges, int32_t rows, int32_t slots, i
  *     all -inf has no softmax and gets NaN.
  *   - Logits, softmax sums and outputs are accumulated in FP32.  bf16: the softmax's weights are rounded to bf16
  *     where the product with the values runs on the tensor cores (dh 64 and 128).
+ *   - An output may be the queries' own memory (with the same strides), and may not overlap them otherwise.
  *   - The results do not depend on timing: the same call on the same inputs gives the same bits. */
 typedef struct rr_paged_kv {
   void* k;                   /* pages of keys and of values                                       */

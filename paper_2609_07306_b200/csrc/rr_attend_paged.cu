@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
         cnt1 = cta_of(sc, first + no - 1, W) - c1 + 1;
         const long long rows = min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS);
         st1 = few1 ? 1 : partials_of(P.streams, rows);
-        whole = np == 0 && cnt1 == 1 && st1 == 1;      // (one segment with all of the row's tiles wrote the output itself)
+        whole = np == 0 && cnt1 == 1 && st1 == 1 && !P.in_place;      // (one segment with all of the row's tiles wrote the output itself)
         again = whole && !few1 && leaves_marks(P, rows) && P.marks[kvh * per + (long long)t * P.group + g];
       }
     }
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
       cnt0 = cta_of(sc, first + P.units - 1, W) - c0 + 1;
       r0 = idx % ROWS;
     }
-    whole = cnt0 == 1 && st0 == 1;                     // (one segment with all of the row's tiles wrote the output itself)
+    whole = cnt0 == 1 && st0 == 1 && !P.in_place;      // (one segment with all of the row's tiles wrote the output itself)
     again = mine && whole && P.few.ctas == 0 && leaves_marks(P, min(ROWS, mg - idx / ROWS * ROWS)) && P.marks[row];
     out = b * P.ob + (r * P.group + idx % P.group) * P.oh + (i * P.m + idx / P.group) * P.ot;
   }
@@ -909,6 +909,7 @@ cudaError_t launch_simt(const Params& P, int grid, cudaStream_t st) {
 size_t up(size_t x) { return (x + 255) / 256 * 256; }
 // Rows that a whole item may write without partials and mark.
 size_t mark_rows(const Params& P) {
+  if (P.in_place) return 0;
   if (P.slots) return P.few.ctas == 0 && leaves_marks(P, (long long)P.m * P.group) ? (size_t)P.range_rows * P.m * P.group : 0;
   return leaves_marks(P, (long long)P.tokens * P.group) ? (size_t)P.tokens * P.heads : 0;
 }
@@ -971,6 +972,8 @@ int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   if ((long long)a->tokens * a->heads > (1LL << 30)) return RR_ERR_TOO_LARGE;
   P.q = a->q; P.out = a->out; P.lens = a->lens; P.cu = a->cu; P.prefix_pages = a->prefix_pages;
   P.qt = a->q_token_stride; P.qh = a->q_head_stride; P.ot = a->out_token_stride; P.oh = a->out_head_stride;
+  P.in_place = a->q == a->out;
+  if (P.in_place && ((a->tokens > 1 && P.qt != P.ot) || (a->heads > 1 && P.qh != P.oh))) return RR_ERR_INVALID_ARG;
   P.tokens = a->tokens; P.heads = a->heads; P.group = a->heads / kv->kv_heads; P.causal = a->causal; P.prefix = a->prefix_tokens;
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
@@ -1005,6 +1008,9 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.q = a->q; P.out = a->out; P.lens = a->lens; P.ranges = a->ranges;
   P.qb = a->q_batch_stride; P.qh = a->q_head_stride; P.qt = a->q_token_stride;
   P.ob = a->out_batch_stride; P.oh = a->out_head_stride; P.ot = a->out_token_stride;
+  P.in_place = a->q == a->out;
+  if (P.in_place && ((kv->batch > 1 && P.qb != P.ob) || (a->heads > 1 && P.qh != P.oh) || (all > (double)kv->batch * a->heads && P.qt != P.ot)))
+    return RR_ERR_INVALID_ARG;
   P.heads = a->heads; P.route_heads = a->route_heads; P.group = a->heads / a->route_heads; P.causal = a->causal;
   P.n_q = a->n_q; P.m = a->m; P.slots = a->slots;
   P.scale_log2 = a->scale * 1.4426950408889634f;
@@ -1023,7 +1029,7 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.streams = streams_of(P);
   // (nothing to join: whole items, whose rows have one partial each; the last item of a range row may have fewer rows than the others)
   const int mg = P.m * P.group, last = mg % ROWS;
-  if (!P.units && partials_of(P.streams, std::min(mg, ROWS)) == 1 && (last == 0 || partials_of(P.streams, last) == 1)) P.part_rows = 0;
+  if (!P.units && !P.in_place && partials_of(P.streams, std::min(mg, ROWS)) == 1 && (last == 0 || partials_of(P.streams, last) == 1)) P.part_rows = 0;
   return RR_OK;
 }
 

@@ -74,6 +74,7 @@ struct Params {
   long long part_rows;
   uint8_t* marks;                                      // of rows that are written without partials: [tokens * heads] or [range_rows * m * group]
   int vq, vk;                                          // queries / cache rows split into aligned groups of four
+  int in_place;                                        // the output is the queries' memory: only the join writes it, a row at a time
 };
 
 struct Seg {
@@ -85,7 +86,7 @@ struct Seg {
   const int32_t* pages;                                // page list of the tokens, from token `prefix` on
   const int32_t* prefix_pages;
   int prefix;
-  bool whole;                                          // all tiles of the rows' only item: nothing to join
+  bool whole;                                          // all tiles of the rows' only item, nothing to join: the segment writes the output
   const int32_t* slots;                                // ranges: the row's slots, else null
   int tile0, tile1;                                    // the segment's tiles of the list (ranges: once counted)
   int unit0, unit1;                                    // ranges: the segment's units of the item's `units` (of 1 if whole)
@@ -177,7 +178,7 @@ __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int 
   s.tile0 = (int)(u - first);
   s.tile1 = (int)min((long long)tiles, u1 - first);
   const int took = s.tile1 - s.tile0;
-  s.whole = took == tiles && u >= before && np == 0;
+  s.whole = took == tiles && u >= before && np == 0 && !P.in_place;
   if (P.causal && s.b >= 0) {                          // no row sees the tiles from the last row's limit on
     const long long limit = (long long)seq_end(P, s.b) - s.n_seq + (s.row0 + s.rows - 1) / P.group + 1;
     s.tile1 = max(s.tile0, limit <= s.tok0 ? 0 : (int)min((long long)s.tile1, (limit - s.tok0 + TILE - 1) / TILE));
@@ -193,7 +194,7 @@ __device__ __forceinline__ int range_segment(const Params& P, const Sched& sc, i
   const long long item = quot(u, n), row = quot(item, qt);
   s.unit0 = (int)(u - item * n);
   s.unit1 = (int)min((long long)n, u1 - item * n);
-  s.whole = s.unit1 - s.unit0 == n;
+  s.whole = s.unit1 - s.unit0 == n && !P.in_place;
   s.row0 = (int)(item - row * qt) * ROWS;
   s.rows = min(ROWS, mg - s.row0);
   const int per = (int)quot(row, P.n_q), i = (int)(row - (long long)per * P.n_q), r = per % P.route_heads;

@@ -184,6 +184,7 @@ class PagedKV:
         cu      as in append; rows of out behind cu[batch] are left as they were
         causal  the queries are their sequence's last tokens, and none sees a token behind its own; False: every query
                 sees all lens[b] tokens (attention to states of another length, e.g. an encoder's)
+        out     as q; may be q itself
         A query without tokens gets zeros."""
         if q.dim() != 3:
             raise ValueError("q must be [tokens, heads, dh]")
@@ -216,6 +217,7 @@ class PagedKV:
                 the heads / route_heads query heads of route head r and of the m query tokens of chunk i
         lens    [batch] int32 tokens in the cache: range tokens from there on are left out
         causal  the query tokens are the sequence's last n_q * m, and none sees a token behind its own
+        out     as q; may be q itself
         A query without tokens gets zeros."""
         if q.dim() != 4:
             raise ValueError("q must be [batch, heads, n_q * m, dh]")

@@ -142,3 +142,16 @@ def test_workspaces():
     assert B.rr_attend_shared_workspace(kv(), shared(tokens=0)) >= 0
     # a call without tokens has nothing to do
     assert lib.rr_attend_shared(C.byref(kv()), C.byref(shared(tokens=0)), None, 0, None) == B.RR_OK
+
+
+def test_outputs_over_the_queries():
+    """The same memory with the same strides, or none in common."""
+    lib = B.lib()
+    ws = lambda **kw: B.rr_attend_shared_workspace(kv(), shared(**kw))
+    assert ws(out=0x10000) > 0
+    assert ws(out=0x10000, tokens=3, heads=2, out_token_stride=256) > 0
+    for kw in (dict(out_token_stride=512), dict(out_head_stride=128)):
+        assert lib.rr_attend_shared(C.byref(kv()), C.byref(shared(out=0x10000, **kw)), 0x100, 1 << 40, None) == B.RR_ERR_INVALID_ARG
+    assert B.rr_attend_paged_ranges_workspace(kv(), ranges(out=0x10000)) > 0
+    for kw in (dict(out_batch_stride=2048), dict(out_head_stride=512), dict(out_token_stride=128)):
+        assert lib.rr_attend_paged_ranges(C.byref(kv()), C.byref(ranges(out=0x10000, **kw)), 0x100, 1 << 40, None) == B.RR_ERR_INVALID_ARG
