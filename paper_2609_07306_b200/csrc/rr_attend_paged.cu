@@ -3,13 +3,11 @@
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
-#include "rr_attend_paged.cuh"
+#include "rr_attend_paged_again.cuh"
 
 using namespace rrattn;
 
 namespace {
-
-constexpr unsigned FULL = 0xFFFFFFFFu;
 
 // ---- plan --------------------------------------------------------------------------------------------------
 // cum[b] = tiles of all items before sequence b's: the prefix's, then the sequences' own, in their order.  The prefix's pages stand in the row of
@@ -41,7 +39,7 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
   tiles = all.x; len = all.y; at = all.z;
   reduce();
   const long long packed = prefix_row_tiles(P);
-  const Plan plan{tiles <= packed + packed / 8, at, len};
+  const Plan plan{tiles <= packed + packed / 8, at, len, 0};
   const bool apart = plan.apart;
   const long long prefix_all = P.kv_heads * packed * prefix_tiles(plan);
   long long run = P.few_prefix ? 0 : prefix_all, run_few = P.few_prefix ? prefix_all : 0;
@@ -77,304 +75,124 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
   }
 }
 
-// ---- rows looked at again ---------------------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ float4 load4(const T* p, bool vec, int n);
-template <> __device__ __forceinline__ float4 load4<float>(const float* p, bool vec, int n) {
-  if (vec) return *(const float4*)p;
-  return make_float4(p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
-}
-template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p, bool vec, int n) {
-  if (vec) {
-    const uint2 t = *(const uint2*)p;
-    return make_float4(__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xFFFF0000u), __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xFFFF0000u));
-  }
-  return make_float4(__bfloat162float(p[0]), n > 1 ? __bfloat162float(p[1]) : 0.f, n > 2 ? __bfloat162float(p[2]) : 0.f, n > 3 ? __bfloat162float(p[3]) : 0.f);
-}
-
-// A marked row's outputs are what they should be unless one of the tokens that it may not see but was multiplied with holds an infinity or NaN
-// among its values; a row that sees one of its own stays as it is.  Only these tokens are looked at: of the prefix those behind the row's
-// limit, of its own or a range row's list those that share a tile with the last one seen by some row of the item.  Where one is found the row is computed
-// from the definition: a token that it does not see is not read.  (Up to 32 rows on the tensor cores multiply the other quarters' tokens with weight 0, too.
-// A NaN among these is the row's own if the row sees it, as it does unless it is found; an infinity is an infinity in its quarter's partial
-// and NaN in the others': `force`.)  `parts` warps take 32 tokens in turn, 8 of them in flight; each leaves reference, sum and output, a lane's columns 4 lane ..
-// and 128 + 4 lane ...  Bound by these loads' latency, and by the cache's traffic where many
-// rows are computed again.  Measured, a prompt of 8192 tokens, 32 heads on 8 of 128, 1.24 ms: with a NaN that all rows see 6.1 ms (looked at),
-// that only the last token sees 13.4 ms (193 tokens' rows computed again).
-struct Part { float m, l; float4 o[2]; };
-
-// The query token, head and limit of row `row` of a ranges call.
-__device__ __forceinline__ RowAt range_row(const Params& P, long long row) {
-  const int mg = P.m * P.group;
-  const long long rr = quot(row, mg), per = quot(rr, P.n_q);
-  const int idx = (int)(row - rr * mg), i = (int)(rr - per * P.n_q), b = (int)per / P.route_heads, len = seq_end(P, b);
-  RowAt a;
-  a.t = i * P.m + idx / P.group;
-  a.h = (int)per % P.route_heads * P.group + idx % P.group;
-  a.limit = P.causal ? max(len - P.n_q * P.m + a.t + 1, 0) : len;
-  return a;
-}
-
-// Calls body(at) with the lanes' places of 32 tokens at a time (-1: none) for the list's tokens in [from, to), every parts-th time.
-template <class F>
-__device__ __forceinline__ void each_tokens(const Params& P, const Seg& s, int from, int to, int part, int parts, F&& body) {
-  const int lane = threadIdx.x & 31, spans = s.slots ? P.slots : 1;
-  int turn = 0;
-  for (int j = 0; j < spans; ++j) {
-    int lo = s.tok0, hi = s.tok1;
-    if (s.slots) slot_span(s, j, lo, hi);
-    lo = max(lo, from);
-    hi = min(hi, to);
-    for (int t = lo; t < hi; t += 32) {
-      if (turn == part) body(t + lane < hi ? token_at(P, s, t + lane) : -1LL);
-      turn = turn + 1 == parts ? 0 : turn + 1;
-    }
-  }
-}
-
-template <typename T, int NV>                          // NV groups of 128 columns
-__device__ __noinline__ bool look_again(const Params& P, long long row, bool force, int part, int parts, Part& y) {
-  constexpr int N = 8 / NV;                            // tokens' loads in flight
-  const int lane = threadIdx.x & 31, e0 = lane * 4;
-  Seg s;
-  s.prefix = 0; s.prefix_pages = nullptr; s.slots = nullptr; s.tok0 = 0;
-  long long q;
-  int limit, behind;                                   // behind: unseen tokens from there on were not multiplied
-  if (P.slots) {
-    const long long rr = quot(row, P.m * P.group), per = quot(rr, P.n_q);
-    const RowAt a = range_row(P, row);
-    s.b = (int)per / P.route_heads;
-    s.kvh = (int)per % P.route_heads / (P.route_heads / P.kv_heads);
-    s.slots = P.ranges + rr * P.slots * 2;
-    s.tok1 = seq_len(P, s.b);
-    q = s.b * P.qb + a.h * P.qh + a.t * P.qt;
-    limit = a.limit;
-    behind = s.tok1;
-  } else {
-    const int t = (int)quot(row, P.heads), h = (int)(row - (long long)t * P.heads);
-    const Plan plan = plan_of(P);
-    s.b = P.cu ? rr_sequence_of(P.cu, P.batch, t) : t;
-    s.kvh = h / P.group;
-    s.tok1 = seq_len(P, s.b);
-    s.prefix = P.prefix;
-    s.prefix_pages = P.prefix_pages ? P.prefix_pages : P.table + plan.source * P.table_stride;
-    const int n = seq_count(P, s.b), len = seq_end(P, s.b);
-    q = t * P.qt + h * P.qh;
-    limit = P.causal ? max(len - n + (t - seq_first(P, s.b)) + 1, 0) : len;
-    behind = (int)min((long long)s.tok1, (long long)limit + ROWS / P.group + 1 + TILE);
-    if (prefix_tiles(plan) > 0) behind = max(behind, plan.prefix);
-  }
-  s.pages = P.table + s.b * P.table_stride;
-  auto values = [&](const void* from, long long at, int i0, float4 (&x)[N][NV]) {
-    auto load = [&](bool vec) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const long long o = __shfl_sync(FULL, at, i0 + i);
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          const int e = e0 + 128 * v;
-          x[i][v] = o >= 0 && e < P.dh ? load4<T>((const T*)from + o + e, vec, P.dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-      }
-    };
-    if (P.vk) load(true); else load(false);            // (one branch for all loads: they are under way together)
-  };
-  if (!force) {
-    const int tok1 = s.tok1;
-    bool found = false;
-    s.tok1 = max(tok1, behind);                        // (a sequence shorter than the prefix has been multiplied with all of it)
-    each_tokens(P, s, limit, behind, 0, 1, [&](long long at) {
-#pragma unroll 1
-      for (int i0 = 0; i0 < 32; i0 += N) {
-        float4 x[N][NV];
-        values(P.v, at, i0, x);
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-          for (int v = 0; v < NV; ++v) found = found || !(isfinite(x[i][v].x) && isfinite(x[i][v].y) && isfinite(x[i][v].z) && isfinite(x[i][v].w));
-      }
-    });
-    s.tok1 = tok1;
-    if (!__any_sync(FULL, found)) return false;
-  }
-  float4 qv[NV], o[2];
-  float m = NINF, l = 0.f;
-  bool seen = false;
-  o[0] = o[1] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int e = e0 + 128 * v;
-    qv[v] = e < P.dh ? load4<T>((const T*)P.q + q + e, P.vq, P.dh - e) : make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-  each_tokens(P, s, 0, limit, part, parts, [&](long long at) {
-    const unsigned sees = __ballot_sync(FULL, at >= 0);
-    seen = seen || sees != 0;
-#pragma unroll 1
-    for (int i0 = 0; i0 < 32; i0 += N) {
-      if (!(sees >> i0 & ((1u << N) - 1))) continue;
-      float4 k[N][NV], w[N][NV];
-      values(P.k, at, i0, k);
-      values(P.v, at, i0, w);
-      float z[N], top = NINF;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        z[i] = 0.f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) z[i] = fmaf(qv[v].w, k[i][v].w, fmaf(qv[v].z, k[i][v].z, fmaf(qv[v].y, k[i][v].y, fmaf(qv[v].x, k[i][v].x, z[i]))));
-#pragma unroll
-        for (int off = 16; off; off >>= 1) z[i] += __shfl_xor_sync(FULL, z[i], off);
-        z[i] = sees >> (i0 + i) & 1 ? z[i] * P.scale_log2 : NINF;
-        top = fmaxf(top, z[i]);
-      }
-      const float now = fmaxf(m, top), ref = now == NINF ? 0.f : now, f = exp2f(m - ref);
-      m = now;
-      l *= f;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) { o[v].x *= f; o[v].y *= f; o[v].z *= f; o[v].w *= f; }
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (!(sees >> (i0 + i) & 1)) continue;
-        const float p = exp2f(z[i] - ref);
-        l += p;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          o[v].x = fmaf(p, w[i][v].x, o[v].x); o[v].y = fmaf(p, w[i][v].y, o[v].y);
-          o[v].z = fmaf(p, w[i][v].z, o[v].z); o[v].w = fmaf(p, w[i][v].w, o[v].w);
-        }
-      }
-    }
-  });
-  y.m = seen && m == NINF ? LOWEST : m;
-  y.l = l;
-  y.o[0] = o[0];
-  y.o[1] = o[1];
-  return true;
-}
-template <typename T>
-__device__ __forceinline__ bool look_again(const Params& P, long long row, bool force, int part, int parts, Part& y) {
-  return P.dh <= 128 ? look_again<T, 1>(P, row, force, part, parts, y) : look_again<T, 2>(P, row, force, part, parts, y);
-}
-
-// The row's output, a lane its columns.  No weight at all: zeros for a row without tokens, NaN for one whose tokens are all at -inf.
-template <typename T>
-__device__ __forceinline__ void write_row(const Params& P, long long out, float m, float l, const float4 (&o)[2]) {
-  const int e0 = (threadIdx.x & 31) * 4;
-  const float inv = l == 0.f ? (m == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / l;
-#pragma unroll
-  for (int v = 0; v < 2; ++v) {
-    const float y[4] = {o[v].x, o[v].y, o[v].z, o[v].w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (e0 + 128 * v + j < P.dh) ((T*)P.out)[out + e0 + 128 * v + j] = rr_from_f32<T>(y[j] * inv);
-  }
-}
-
 // ---- join --------------------------------------------------------------------------------------------------
-// WPR warps join the partials of one row: o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Each warp takes every WPR-th partial, eight of
-// them in flight, a lane four columns (and four more 128 further on); the warps' parts are added in their order.  One warp where rows
-// are many, eight where they are few (and their partials many: up to a hundred and fifty for a row of one short call).
-// A row with a marked partial, or of a marked item, is looked at again, and computed again by the same warps if it has to be.
-template <typename T, int WPR>
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params P) {
-  __shared__ __align__(16) float s_o[WPR > 1 ? 8 : 1][RR_PAGED_MAX_DH], s_l[8], s_m[8];
-  rr_pdl_wait();
-  rr_pdl_trigger();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % WPR;
-  const long long row = (long long)blockIdx.x * (8 / WPR) + warp / WPR;
-  const int H = P.heads;
-  // up to two lists of partials: the n0 first ones of list 0
-  long long home0 = 0, home1 = 0;
-  int c0 = 0, c1 = 0, cnt0 = 0, cnt1 = 0, st0 = 1, st1 = 1, r0 = 0, r1 = 0;
-  long long out = 0;
-  bool mine = true, few1 = false, whole = false, again = false;
-  if (P.slots == 0) {
-    mine = row < (long long)P.tokens * H;
-    const int t = (int)quot(mine ? row : 0, H), h = (int)((mine ? row : 0) - (long long)t * H), kvh = h / P.group, g = h - kvh * P.group;
-    const int b = P.cu ? rr_sequence_of_warp(P.cu, P.batch, t) : t;
-    mine = mine && b >= 0;                             // (padding: left as it was)
-    if (mine) {
-      const Sched& sp = P.few_prefix ? P.few : P.main;
-      const long long all = __ldg(P.main.cum + P.batch), all_p = P.few_prefix ? __ldg(P.few.cum + P.batch) : all, per = (long long)P.tokens * P.group;
-      out = t * P.ot + h * P.oh;
-      const Plan plan = plan_of(P);
-      const bool apart = plan.apart;
-      const long long np = prefix_tiles(plan), qtp = prefix_row_tiles(P);
-      if (np > 0) {
-        const long long idx = (long long)t * P.group + g, first = (kvh * qtp + idx / ROWS) * np;
-        home0 = kvh * per + idx;
-        r0 = (int)(idx % ROWS);
-        c0 = cta_of(sp, first, all_p);
-        cnt0 = cta_of(sp, first + np - 1, all_p) - c0 + 1;
-        st0 = P.few_prefix ? 1 : partials_of(P.streams, min((long long)ROWS, per - idx / ROWS * ROWS));
-      }
-      const int no = own_tiles(P, b, apart);
-      if (no > 0) {
-        const int t0 = seq_first(P, b), n = seq_count(P, b), qt = own_row_tiles(P, b);
-        const long long idx = (long long)(t - t0) * P.group + g;
-        few1 = few_rows_of(P, b);
-        const Sched& sc = few1 ? P.few : P.main;
-        const long long W = few1 ? __ldg(P.few.cum + P.batch) : all, first = __ldg(sc.cum + b) + (kvh * (long long)qt + idx / ROWS) * no;
-        home1 = (P.kv_heads + kvh) * per + (long long)t0 * P.group + idx;
-        r1 = (int)(idx % ROWS);
-        c1 = cta_of(sc, first, W);
-        cnt1 = cta_of(sc, first + no - 1, W) - c1 + 1;
-        const long long rows = min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS);
-        st1 = few1 ? 1 : partials_of(P.streams, rows);
-        whole = np == 0 && cnt1 == 1 && st1 == 1 && !P.in_place;      // (one segment with all of the row's tiles wrote the output itself)
-        again = whole && !few1 && leaves_marks(P, rows) && P.marks[kvh * per + (long long)t * P.group + g];
-      }
-    }
-  } else {
-    const int mg = P.m * P.group;
-    mine = row < P.range_rows * mg;
-    const long long rr = quot(mine ? row : 0, mg), per = quot(rr, P.n_q);
-    const int idx = (int)((mine ? row : 0) - rr * mg), i = (int)(rr - per * P.n_q), r = (int)per % P.route_heads, b = (int)per / P.route_heads;
-    st0 = partials_of(P.streams, min(ROWS, mg - idx / ROWS * ROWS));
-    home0 = row;
-    cnt0 = 1;
-    if (P.units) {
-      const long long W = range_units(P), first = (rr * ((mg + ROWS - 1) / ROWS) + idx / ROWS) * P.units;
-      const Sched& sc = P.few.ctas > 0 ? P.few : P.main;
-      c0 = cta_of(sc, first, W);
-      cnt0 = cta_of(sc, first + P.units - 1, W) - c0 + 1;
-      r0 = idx % ROWS;
-    }
-    whole = cnt0 == 1 && st0 == 1 && !P.in_place;      // (one segment with all of the row's tiles wrote the output itself)
-    again = mine && whole && P.few.ctas == 0 && leaves_marks(P, min(ROWS, mg - idx / ROWS * ROWS)) && P.marks[row];
-    out = b * P.ob + (r * P.group + idx % P.group) * P.oh + (i * P.m + idx / P.group) * P.ot;
-  }
-  mine = mine && (!whole || again);
-  if (WPR == 1 && !mine) return;
-  const int n0 = whole ? 0 : cnt0 * st0, n = whole ? 0 : n0 + cnt1 * st1;
-  const bool few0 = P.slots ? P.few.ctas > 0 : P.few_prefix;
-  auto place = [&](int k) -> long long {               // partial row of the k-th partial
+// Where row `row`'s partials are: up to two lists, the n0 first ones of list 0, and n in all.
+struct Partials {
+  long long home0, home1, out;
+  int c0, c1, cnt0, cnt1, st0, st1, r0, r1, n0, n;
+  bool mine, few0, few1, whole, marked;                // whole: one segment with all of the row's tiles has written the output itself
+
+  // partial row of the k-th partial
+  __device__ __forceinline__ long long place(const Params& P, int k) const {
     const bool w = k >= n0;
     if (w) k -= n0;
     const int s = w ? st1 : st0, c = k / s;
     const Sched& sc = (w ? few1 : few0) ? P.few : P.main;
     const long long at = c == 0 ? (w ? home1 : home0) : sc.slots_at + (long long)((w ? c1 : c0) + c) * sc.slot_rows + (w ? r1 : r0);
     return (k - c * s) * P.part_rows + at;
-  };
+  }
+};
+
+template <bool MARKS>
+__device__ __forceinline__ Partials partials_at(const Params& P, long long row) {
+  Partials x;
+  x.home0 = x.home1 = x.out = 0;
+  x.c0 = x.c1 = x.cnt0 = x.cnt1 = x.r0 = x.r1 = 0;
+  x.st0 = x.st1 = 1;
+  x.few1 = x.whole = x.marked = false;
+  x.few0 = P.slots ? P.few.ctas > 0 : P.few_prefix;
+  if (P.slots == 0) {
+    const int H = P.heads;
+    x.mine = row < (long long)P.tokens * H;
+    const int t = (int)quot(x.mine ? row : 0, H), h = (int)((x.mine ? row : 0) - (long long)t * H), kvh = h / P.group, g = h - kvh * P.group;
+    const int b = P.cu ? rr_sequence_of_warp(P.cu, P.batch, t) : t;
+    x.mine = x.mine && b >= 0;                         // (padding: left as it was)
+    if (x.mine) {
+      const Sched& sp = P.few_prefix ? P.few : P.main;
+      const long long all = __ldg(P.main.cum + P.batch), all_p = P.few_prefix ? __ldg(P.few.cum + P.batch) : all, per = (long long)P.tokens * P.group;
+      x.out = t * P.ot + h * P.oh;
+      const Plan plan = plan_of(P);
+      const bool apart = plan.apart;
+      const long long np = prefix_tiles(plan), qtp = prefix_row_tiles(P);
+      if (np > 0) {
+        const long long idx = (long long)t * P.group + g, first = (kvh * qtp + idx / ROWS) * np;
+        x.home0 = kvh * per + idx;
+        x.r0 = (int)(idx % ROWS);
+        x.c0 = cta_of(sp, first, all_p);
+        x.cnt0 = cta_of(sp, first + np - 1, all_p) - x.c0 + 1;
+        x.st0 = P.few_prefix ? 1 : partials_of(P.streams, min((long long)ROWS, per - idx / ROWS * ROWS));
+      }
+      const int no = own_tiles(P, b, apart);
+      if (no > 0) {
+        const int t0 = seq_first(P, b), n = seq_count(P, b), qt = own_row_tiles(P, b);
+        const long long idx = (long long)(t - t0) * P.group + g;
+        x.few1 = few_rows_of(P, b);
+        const Sched& sc = x.few1 ? P.few : P.main;
+        const long long W = x.few1 ? __ldg(P.few.cum + P.batch) : all, first = __ldg(sc.cum + b) + (kvh * (long long)qt + idx / ROWS) * no;
+        x.home1 = (P.kv_heads + kvh) * per + (long long)t0 * P.group + idx;
+        x.r1 = (int)(idx % ROWS);
+        x.c1 = cta_of(sc, first, W);
+        x.cnt1 = cta_of(sc, first + no - 1, W) - x.c1 + 1;
+        const long long rows = min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS);
+        x.st1 = x.few1 ? 1 : partials_of(P.streams, rows);
+        x.whole = np == 0 && x.cnt1 == 1 && x.st1 == 1 && !P.in_place;
+        if (MARKS) x.marked = x.whole && plan.marked && !x.few1 && leaves_marks(P, rows) && P.marks[kvh * per + (long long)t * P.group + g];
+      }
+    }
+  } else {
+    const int mg = P.m * P.group;
+    x.mine = row < P.range_rows * mg;
+    const long long rr = quot(x.mine ? row : 0, mg), per = quot(rr, P.n_q);
+    const int idx = (int)((x.mine ? row : 0) - rr * mg), i = (int)(rr - per * P.n_q), r = (int)per % P.route_heads, b = (int)per / P.route_heads;
+    x.st0 = partials_of(P.streams, min(ROWS, mg - idx / ROWS * ROWS));
+    x.home0 = row;
+    x.cnt0 = 1;
+    if (P.units) {
+      const long long W = range_units(P), first = (rr * ((mg + ROWS - 1) / ROWS) + idx / ROWS) * P.units;
+      const Sched& sc = x.few0 ? P.few : P.main;
+      x.c0 = cta_of(sc, first, W);
+      x.cnt0 = cta_of(sc, first + P.units - 1, W) - x.c0 + 1;
+      x.r0 = idx % ROWS;
+    }
+    x.whole = x.cnt0 == 1 && x.st0 == 1 && !P.in_place;
+    if (MARKS) x.marked = x.mine && x.whole && !x.few0 && leaves_marks(P, min(ROWS, mg - idx / ROWS * ROWS)) && P.marks[row];
+    x.out = b * P.ob + (r * P.group + idx % P.group) * P.oh + (i * P.m + idx / P.group) * P.ot;
+  }
+  x.n0 = x.whole ? 0 : x.cnt0 * x.st0;
+  x.n = x.whole ? 0 : x.n0 + x.cnt1 * x.st1;
+  return x;
+}
+
+// The largest reference of every parts-th partial from `part` on; whether one of them is marked.
+__device__ __forceinline__ float largest(const Params& P, const Partials& p, int part, int parts, bool& marked) {
   float M = NINF;
-  for (int k = lane * WPR + part; k < n; k += 32 * WPR) M = fmaxf(M, P.part_ml[place(k)].x);
+  for (int k = (threadIdx.x & 31) * parts + part; k < p.n; k += 32 * parts) {
+    const float2 ml = P.part_ml[p.place(P, k)];
+    M = fmaxf(M, ml.x);
+    marked = marked || has_mark(ml.y);
+  }
 #pragma unroll
   for (int off = 16; off; off >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, off));
+  return M;
+}
+__device__ __forceinline__ void add(float4& y, float w, const float4& x) { y.x = fmaf(w, x.x, y.x); y.y = fmaf(w, x.y, y.y); y.z = fmaf(w, x.z, y.z); y.w = fmaf(w, x.w, y.w); }
+// Their sum l and output o against the reference M.
+__device__ __forceinline__ void joined(const Params& P, const Partials& p, int part, int parts, float M, float& l, float4 (&o)[2]) {
+  const int lane = threadIdx.x & 31, e0 = lane * 4, n = p.n;
   const bool vec = P.dh % 4 == 0;
-  const int e0 = lane * 4;
-  float l = 0.f;
-  float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-  auto add = [](float4& y, float w, const float4& x) { y.x = fmaf(w, x.x, y.x); y.y = fmaf(w, x.y, y.y); y.z = fmaf(w, x.z, y.z); y.w = fmaf(w, x.w, y.w); };
-  for (int k0 = part; k0 < n; k0 += 32 * WPR) {
-    const int k = k0 + lane * WPR;
+  l = 0.f;
+  o[0] = o[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = part; k0 < n; k0 += 32 * parts) {
+    const int k = k0 + lane * parts;
     float w = 0.f;
     long long at = -1;
     if (k < n) {
-      at = place(k);
+      at = p.place(P, k);
       const float2 ml = P.part_ml[at];
       if (ml.x == NINF || (ml.x == LOWEST && ml.y == 0.f)) at = -1;      // nothing in it (and no output written)
       else { w = exp2f(ml.x - M); l = fmaf(w, fabsf(ml.y), l); }
-      again = again || has_mark(ml.y);
     }
-    const int lim = min(32, (n - k0 + WPR - 1) / WPR);
+    const int lim = min(32, (n - k0 + parts - 1) / parts);
     for (int u0 = 0; u0 < lim; u0 += 8) {
       float4 x[8][2];
 #pragma unroll
@@ -400,33 +218,68 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   }
 #pragma unroll
   for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(FULL, l, off);
-  auto leave = [&]() {
+}
+
+// A marked row: true if it has been computed again.
+template <typename T>
+__device__ __noinline__ bool join_again(const Params& P, long long row, int part, int parts, Part y) {
+  const Partials p = partials_at<false>(P, row);
+  bool force = false;                                  // (see look_again)
+  if (p.st0 == 8 || p.st1 == 8)
+    for (int k = 0; k < p.n; ++k) {
+      const long long at = p.place(P, k);
+      if (!has_mark(P.part_ml[at].y)) continue;
+      for (int e = threadIdx.x & 31; e < P.dh; e += 32) force = force || isinf(P.part_o[at * P.dh + e]);
+    }
+  return look_again<T>(P, row, __any_sync(FULL, force), part, parts, y);
+}
+// By one warp, to the end.
+template <typename T>
+__device__ __noinline__ void join_marked(const Params& P, long long row) {
+  if (join_again<T>(P, row, 0, 1, Part{nullptr, nullptr, nullptr})) return;
+  const Partials p = partials_at<false>(P, row);
+  if (p.whole) return;                                 // what is there may stay
+  bool marked = false;
+  const float M = largest(P, p, 0, 1, marked);
+  float l;
+  float4 o[2];
+  joined(P, p, 0, 1, M, l, o);
+  write_row<T>(P, p.out, M, l, o);
+}
+
+// WPR warps join the partials of one row: o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Each warp takes every WPR-th partial, eight of
+// them in flight, a lane four columns (and four more 128 further on); the warps' parts are added in their order.  One warp where rows
+// are many, eight where they are few (and their partials many: up to a hundred and fifty for a row of one short call).
+// MARKS: a row with a marked partial, or of a marked item, is looked at again, and computed again by the same warps if it has to be.  (Calls whose
+// kernels leave no marks do without: four sequences of one token behind 2048, 20.0 us, with it 20.7.)
+template <typename T, int WPR, bool MARKS>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params P) {
+  __shared__ __align__(16) float s_o[WPR > 1 ? 8 : 1][RR_PAGED_MAX_DH], s_l[8], s_m[8];
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % WPR, e0 = lane * 4;
+  const long long row = (long long)blockIdx.x * (8 / WPR) + warp / WPR;
+  const Partials p = partials_at<MARKS>(P, row);
+  const bool mine = p.mine && (!p.whole || p.marked);
+  if (WPR == 1 && !mine) return;
+  bool again = p.marked;
+  float M = largest(P, p, part, WPR, again), l;
+  if (MARKS && WPR == 1 && __any_sync(FULL, again)) { join_marked<T>(P, row); return; }
+  float4 o[2];
+  joined(P, p, part, WPR, M, l, o);
+  if (WPR > 1) {
     if (lane == 0) { s_l[warp] = l; s_m[warp] = M; }
     *(float4*)&s_o[warp][e0] = o[0];
     *(float4*)&s_o[warp][e0 + 128] = o[1];
-  };
-  if (WPR > 1) { leave(); again = __syncthreads_or(again); } else { again = __any_sync(FULL, again); }
-  if (again) {                                         // (all warps of the row are here, and agree)
-    bool force = false;
-    if (st0 == 8 || st1 == 8)
-      for (int k = 0; k < n; ++k) {
-        const float2 ml = P.part_ml[place(k)];
-        for (int e = lane; e < P.dh && has_mark(ml.y); e += 32) force = force || isinf(P.part_o[place(k) * P.dh + e]);
-      }
-    force = __any_sync(FULL, force);
-    Part y;
-    if (look_again<T>(P, row, force, part, WPR, y)) {
-      M = y.m; l = y.l; o[0] = y.o[0]; o[1] = y.o[1];
-      if (WPR > 1) { __syncthreads(); leave(); __syncthreads(); }
-    } else if (whole) {
-      return;                                          // what is there may stay
+    if (MARKS) again = __syncthreads_or(again); else __syncthreads();
+    if (MARKS && again) {                              // (all warps of the row are here, and agree)
+      if (!join_again<T>(P, row, part, WPR, Part{s_o[warp], &s_m[warp], &s_l[warp]}) && p.whole) return;   // (what is there may stay)
+      __syncthreads();
     }
-  }
-  if (WPR > 1) {
     if (part != 0 || !mine) return;
-    float top = M;
+    float top = NINF;
 #pragma unroll
-    for (int w = 1; w < WPR; ++w) top = fmaxf(top, s_m[warp + w]);
+    for (int w = 0; w < WPR; ++w) top = fmaxf(top, s_m[warp + w]);
     l = 0.f;
     o[0] = o[1] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -439,25 +292,24 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
     }
     M = top;
   }
-  write_row<T>(P, out, M, l, o);
+  write_row<T>(P, p.out, M, l, o);
 }
 
-// Marked rows of a ranges call whose items are all whole: nothing to join.
+// Marked rows of a ranges call whose items are all whole: nothing to join.  (The tensor cores' kernel looks at its own.)
 template <typename T>
 __global__ void __launch_bounds__(256) marked_kernel(const __grid_constant__ Params P) {
   rr_pdl_wait();
   rr_pdl_trigger();
-  const int lane = threadIdx.x & 31, mg = P.m * P.group;
-  const long long rows = P.range_rows * mg;
-  for (long long row0 = ((long long)blockIdx.x * 256 + threadIdx.x) / 32 * 32; row0 < rows; row0 += (long long)gridDim.x * 256) {
-    unsigned marked = __ballot_sync(FULL, row0 + lane < rows && P.marks[row0 + lane]);
-    while (marked) {
-      const long long row = row0 + __ffs(marked) - 1;
-      marked &= marked - 1;
-      Part y;
-      if (!look_again<T>(P, row, false, 0, 1, y)) continue;
-      const RowAt a = range_row(P, row);
-      write_row<T>(P, quot(row, mg) / P.n_q / P.route_heads * P.ob + a.h * P.oh + a.t * P.ot, y.m, y.l, y.o);
+  const long long rows = P.range_rows * P.m * P.group;
+  for (long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 16; __any_sync(FULL, at < rows); at += (long long)gridDim.x * 256 * 16) {
+    const uint4 x = at < rows ? *(const uint4*)(P.marks + at) : make_uint4(0, 0, 0, 0);      // (behind the last row: anything)
+    unsigned some = __ballot_sync(FULL, x.x | x.y | x.z | x.w);
+    while (some) {
+      const int from = __ffs(some) - 1;
+      some &= some - 1;
+      const long long row0 = __shfl_sync(FULL, at, from);
+      for (long long row = row0; row < min(row0 + 16, rows); ++row)
+        if (P.marks[row]) look_again<T>(P, row, false, 0, 1, Part{nullptr, nullptr, nullptr});
     }
   }
 }
@@ -646,7 +498,7 @@ __device__ void rows_block(const Params& P, const Seg& s, const Ctx& c, int r0) 
     const RowAt a = row_at(P, s, r0 + r);
     const long long at = s.part + r0 + r;
     if (tx == 0) {
-      if (s.whole) P.marks[s.mark + r0 + r] = odd && masked;
+      if (s.whole) mark_row(P, s.mark + r0 + r, odd && masked);
       else P.part_ml[at] = make_float2(m[i], with_mark(sum, odd && masked));
     }
     const float inv = sum == 0.f ? (m[i] == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / sum;
@@ -1060,12 +912,18 @@ int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, co
     const long long rows = P.slots ? P.range_rows * P.m * P.group : (long long)P.tokens * P.heads;
     const bool few = rows < 8 * rr_sm_count();
     const int grid = (int)(few ? rows : ceil_div(rows, 8));
-    auto join = [&](auto one, auto eight) { return rr_launch_pdl(few ? eight : one, grid, 256, 0, st, P); };
-    e = dtype == RR_BF16 ? join(join_kernel<__nv_bfloat16, 1>, join_kernel<__nv_bfloat16, 8>) : join(join_kernel<float, 1>, join_kernel<float, 8>);
+    const bool marks = !only_few && (P.tc || (P.slots ? (long long)P.m : P.tokens) * P.group > FEW);
+    auto join = [&](auto type, auto look) {
+      using T = decltype(type);
+      constexpr bool M = decltype(look)::value;
+      return rr_launch_pdl(few ? join_kernel<T, 8, M> : join_kernel<T, 1, M>, grid, 256, 0, st, P);
+    };
+    auto typed = [&](auto look) { return dtype == RR_BF16 ? join(__nv_bfloat16(), look) : join(0.f, look); };
+    e = marks ? typed(std::true_type()) : typed(std::false_type());
     ++launches;
   }
-  if (e == cudaSuccess && P.slots && P.part_rows == 0 && mark_rows(P) > 0) {
-    const int grid = (int)std::min<long long>(ceil_div(mark_rows(P), 256), 8 * rr_sm_count());
+  if (e == cudaSuccess && P.slots && P.part_rows == 0 && !P.tc && mark_rows(P) > 0) {
+    const int grid = (int)std::min<long long>(ceil_div(mark_rows(P), 16 * 256), 2 * rr_sm_count());
     e = dtype == RR_BF16 ? rr_launch_pdl(marked_kernel<__nv_bfloat16>, grid, 256, 0, st, P) : rr_launch_pdl(marked_kernel<float>, grid, 256, 0, st, P);
     ++launches;
   }

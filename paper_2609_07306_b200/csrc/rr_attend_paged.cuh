@@ -43,6 +43,7 @@ struct Plan {
   int apart;                                           // the sequences attend by themselves, to the prefix too
   int source;                                          // whose row of the table has the prefix's pages
   int prefix;                                          // tokens of the prefix that any sequence has
+  int marked;                                          // a row without partials has been marked since
 };
 
 struct Params {
@@ -113,7 +114,10 @@ __device__ __forceinline__ int seq_count(const Params& P, int b) {
   const int a = __ldg(P.cu + b), e = min(__ldg(P.cu + b + 1), P.tokens);
   return a < 0 ? 0 : max(e - a, 0);
 }
-__device__ __forceinline__ Plan plan_of(const Params& P) { return Plan{__ldg(&P.plan->apart), __ldg(&P.plan->source), __ldg(&P.plan->prefix)}; }
+__device__ __forceinline__ Plan plan_of(const Params& P) {
+  const int4 x = __ldg((const int4*)P.plan);
+  return Plan{x.x, x.y, x.z, x.w};
+}
 __device__ __forceinline__ long long prefix_tiles(const Plan& plan) { return plan.apart ? 0 : (plan.prefix + TILE - 1) / TILE; }
 __device__ __forceinline__ long long prefix_row_tiles(const Params& P) { return ceil_div((long long)P.tokens * P.group, ROWS); }
 __device__ __forceinline__ int own_tiles(const Params& P, int b, bool apart) { return (max(seq_len(P, b) - (apart ? 0 : P.prefix), 0) + TILE - 1) / TILE; }
@@ -263,8 +267,12 @@ __device__ __forceinline__ long long token_at(const Params& P, const Seg& s, int
 // ---- marks -------------------------------------------------------------------------------------------------
 // A tile is multiplied whole, so a value that a row may not see enters the row's sums with weight 0: nothing, unless it is an
 // infinity or NaN.  A row with such a result that had masked tokens of its list is marked, by the sign of its partial's sum or, where it has
-// none, by a byte, and looked at again when everything else is done (look_again in rr_attend_paged.cu): the kernels' pipelines do not wait for it.
+// none, by a byte, and looked at again when everything else is done (look_again in rr_attend_paged_again.cuh): the kernels' pipelines do not wait for it.
 __device__ __forceinline__ float with_mark(float l, bool mark) { return __uint_as_float((__float_as_uint(l) & 0x7FFFFFFFu) | (mark ? 0x80000000u : 0u)); }
+__device__ __forceinline__ void mark_row(const Params& P, long long at, bool mark) {
+  P.marks[at] = mark;
+  if (mark && P.slots == 0) atomicOr(&P.plan->marked, 1);
+}
 __device__ __forceinline__ bool has_mark(float l) { return __float_as_uint(l) >> 31; }
 // Whether a whole item of `rows` rows leaves marks: those of up to FEW rows multiply no masked token.
 constexpr int FEW = 8;

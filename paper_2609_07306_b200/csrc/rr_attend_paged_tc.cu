@@ -30,7 +30,7 @@
 // Every wait is bounded; one that runs out sets RR_STATUS_TIMEOUT, and the CTA waits for its copies and
 // products in flight, frees its TMEM and returns.
 #include <algorithm>
-#include "rr_attend_paged.cuh"
+#include "rr_attend_paged_again.cuh"
 #include "rr_sm100.cuh"
 
 using namespace rrattn;
@@ -38,7 +38,6 @@ using namespace sm100;
 
 namespace {
 
-constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int NT = 512, IDS = 16, FILLS = 16, MAX_RING = 4;
 constexpr float GROWTH = 8.f;
 constexpr int BY_FMA = 2;                              // of every 8 pairs of exponentials, by multiply-adds (0: 567 us, 1: 551, 2: 544 of a routed prompt)
@@ -56,7 +55,7 @@ template <int D> struct Shape {
 struct Ctl {
   uint64_t full[FILLS], empty[8], s_full[2][2], p_full[2][2], o_done[2][2], q_full[2], q_empty[2], ids_full[IDS], seg_full[MAX_RING], seg_empty[MAX_RING],
       rows_full[MAX_RING], drain;
-  uint32_t tmem_base, abort_flag;
+  uint32_t tmem_base, abort_flag, marked;              // marked: a row of a call without a join
   Seg seg[MAX_RING];
   int limit[MAX_RING][ROWS];
   int ids[IDS][TILE];
@@ -192,6 +191,16 @@ __device__ __forceinline__ uint64_t exp2_fma(uint64_t x) {
 // Keys and values as [pages][heads][page tokens][entries] with boxes of 32, 16 and 8 tokens.
 struct Maps { CUtensorMap k[3], v[3]; };
 
+// Whole items in turn: no join comes behind, so each of the streams' warps looks at the rows that it has marked itself.
+__device__ __noinline__ void look_at_own(const Params& P) {
+  const int lane = threadIdx.x & 31, mg = P.m * P.group, qt = (mg + ROWS - 1) / ROWS;
+  for (long long u = blockIdx.x; u < range_units(P); u += gridDim.x) {
+    const long long row = quot(u, qt), row0 = (u - row * qt) * ROWS + (threadIdx.x & ~31u);
+    unsigned marked = __ballot_sync(FULL, row0 + lane < mg && P.marks[row * mg + row0 + lane]);
+    for (; marked; marked &= marked - 1) look_again<__nv_bfloat16, 1>(P, row * mg + row0 + __ffs(marked) - 1, false, 0, 1, Part{nullptr, nullptr, nullptr});
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(NT, 1)
 attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps maps, const int ring) {
@@ -214,7 +223,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
     for (int i = 0; i < IDS; ++i) mbar_init(&c->ids_full[i], 4);
     for (int i = 0; i < MAX_RING; ++i) { mbar_init(&c->seg_full[i], 1); mbar_init(&c->seg_empty[i], 15); mbar_init(&c->rows_full[i], 1); }
     mbar_init(&c->drain, 2);
-    c->abort_flag = 0;
+    c->abort_flag = c->marked = 0;
     mbar_fence_init();
     for (int i = 0; i < 3; ++i) { tma_prefetch_desc(&maps.k[i]); tma_prefetch_desc(&maps.v[i]); }
   }
@@ -483,8 +492,12 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
         }
         if (live) {
           const bool mark = odd_rows && mixed;
-          if (direct) P.marks[s.mark + r] = mark;
-          else P.part_ml[at] = make_float2(ref, with_mark(sum, mark));
+          if (direct) {
+            mark_row(P, s.mark + r, mark);
+            if (mark) c->marked = 1;
+          } else {
+            P.part_ml[at] = make_float2(ref, with_mark(sum, mark));
+          }
         }
       }
       tc_fence_before();
@@ -800,6 +813,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
     tmem_dealloc(tmem, 512);
     if (lane == 0 && c->abort_flag && P.status) atomicOr(P.status, RR_STATUS_TIMEOUT);
   }
+  if (c->marked && P.slots && P.part_rows == 0 && threadIdx.x < ROWS) look_at_own(P);
 }
 
 template <int D>
