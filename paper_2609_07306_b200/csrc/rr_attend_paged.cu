@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
   tiles = all.x; len = all.y; at = all.z;
   reduce();
   const long long packed = prefix_row_tiles(P);
-  const Plan plan{tiles <= packed + packed / 8, at, len, 0};
+  const Plan plan{P.always_apart || tiles <= packed + packed / 8, at, len, 0};
   const bool apart = plan.apart;
   const long long prefix_all = P.kv_heads * packed * prefix_tiles(plan);
   long long run = P.few_prefix ? 0 : prefix_all, run_few = P.few_prefix ? prefix_all : 0;
@@ -76,9 +76,10 @@ __global__ void __launch_bounds__(PLAN_NT) plan_kernel(const __grid_constant__ P
 }
 
 // ---- join --------------------------------------------------------------------------------------------------
-// Where row `row`'s partials are: up to two lists, the n0 first ones of list 0, and n in all.
+// Where row `row`'s partials are: up to two lists, the n0 first ones of list 0, and n in all.  ONE: each segment leaves one.
+template <bool ONE>
 struct Partials {
-  long long home0, home1, out;
+  long long home0, home1, more0, more1, out;           // first partials of the lists, and their further ones
   int c0, c1, cnt0, cnt1, st0, st1, r0, r1, n0, n;
   bool mine, few0, few1, whole, marked;                // whole: one segment with all of the row's tiles has written the output itself
 
@@ -86,17 +87,17 @@ struct Partials {
   __device__ __forceinline__ long long place(const Params& P, int k) const {
     const bool w = k >= n0;
     if (w) k -= n0;
-    const int s = w ? st1 : st0, c = k / s;
+    const int s = w ? st1 : st0, c = ONE ? k : k / s, j = ONE ? 0 : k - c * s, cta = (w ? c1 : c0) + c, r = w ? r1 : r0;
     const Sched& sc = (w ? few1 : few0) ? P.few : P.main;
-    const long long at = c == 0 ? (w ? home1 : home0) : sc.slots_at + (long long)((w ? c1 : c0) + c) * sc.slot_rows + (w ? r1 : r0);
-    return (k - c * s) * P.part_rows + at;
+    if (c == 0) return j == 0 ? (w ? home1 : home0) : (w ? more1 : more0) + (long long)(j - 1) * (w || P.slots ? P.own.step : P.step);
+    return sc.slots_at + (long long)cta * sc.cta_rows + r + (j == 0 ? 0 : sc.more_at + (long long)(j - 1) * P.step);
   }
 };
 
-template <bool MARKS>
-__device__ __forceinline__ Partials partials_at(const Params& P, long long row) {
-  Partials x;
-  x.home0 = x.home1 = x.out = 0;
+template <bool MARKS, bool ONE>
+__device__ __forceinline__ Partials<ONE> partials_at(const Params& P, long long row) {
+  Partials<ONE> x;
+  x.home0 = x.home1 = x.more0 = x.more1 = x.out = 0;
   x.c0 = x.c1 = x.cnt0 = x.cnt1 = x.r0 = x.r1 = 0;
   x.st0 = x.st1 = 1;
   x.few1 = x.whole = x.marked = false;
@@ -118,9 +119,10 @@ __device__ __forceinline__ Partials partials_at(const Params& P, long long row) 
         const long long idx = (long long)t * P.group + g, first = (kvh * qtp + idx / ROWS) * np;
         x.home0 = kvh * per + idx;
         x.r0 = (int)(idx % ROWS);
+        if (!ONE) x.more0 = prefix_more_of(P, kvh, x.r0);
         x.c0 = cta_of(sp, first, all_p);
         x.cnt0 = cta_of(sp, first + np - 1, all_p) - x.c0 + 1;
-        x.st0 = P.few_prefix ? 1 : partials_of(P.streams, min((long long)ROWS, per - idx / ROWS * ROWS));
+        x.st0 = ONE || P.few_prefix ? 1 : partials_of(P.streams, min((long long)ROWS, per - idx / ROWS * ROWS));
       }
       const int no = own_tiles(P, b, apart);
       if (no > 0) {
@@ -129,14 +131,17 @@ __device__ __forceinline__ Partials partials_at(const Params& P, long long row) 
         x.few1 = few_rows_of(P, b);
         const Sched& sc = x.few1 ? P.few : P.main;
         const long long W = x.few1 ? __ldg(P.few.cum + P.batch) : all, first = __ldg(sc.cum + b) + (kvh * (long long)qt + idx / ROWS) * no;
-        x.home1 = (P.kv_heads + kvh) * per + (long long)t0 * P.group + idx;
         x.r1 = (int)(idx % ROWS);
         x.c1 = cta_of(sc, first, W);
         x.cnt1 = cta_of(sc, first + no - 1, W) - x.c1 + 1;
         const long long rows = min((long long)ROWS, (long long)n * P.group - idx / ROWS * ROWS);
-        x.st1 = x.few1 ? 1 : partials_of(P.streams, rows);
+        x.st1 = ONE || x.few1 ? 1 : partials_of(P.streams, rows);
+        const long long item = (long long)b * P.kv_heads + kvh, at = kvh * per + (long long)t * P.group + g;
+        x.home1 = home_of(P, x.st1 > 1, item, at, x.r1);
+        if (x.home1 < 0) x.home1 = sc.slots_at + (long long)x.c1 * sc.cta_rows + sc.slot_rows + x.r1;
+        if (!ONE && x.st1 > 1) x.more1 = more_of(P, item, at, x.r1);
         x.whole = np == 0 && x.cnt1 == 1 && x.st1 == 1 && !P.in_place;
-        if (MARKS) x.marked = x.whole && plan.marked && !x.few1 && leaves_marks(P, rows) && P.marks[kvh * per + (long long)t * P.group + g];
+        if (MARKS) x.marked = x.whole && plan.marked && !x.few1 && leaves_marks(P, rows) && P.marks[at];
       }
     }
   } else {
@@ -144,16 +149,19 @@ __device__ __forceinline__ Partials partials_at(const Params& P, long long row) 
     x.mine = row < P.range_rows * mg;
     const long long rr = quot(x.mine ? row : 0, mg), per = quot(rr, P.n_q);
     const int idx = (int)((x.mine ? row : 0) - rr * mg), i = (int)(rr - per * P.n_q), r = (int)per % P.route_heads, b = (int)per / P.route_heads;
-    x.st0 = partials_of(P.streams, min(ROWS, mg - idx / ROWS * ROWS));
-    x.home0 = row;
+    x.st0 = ONE ? 1 : partials_of(P.streams, min(ROWS, mg - idx / ROWS * ROWS));
     x.cnt0 = 1;
+    x.r0 = idx % ROWS;
     if (P.units) {
       const long long W = range_units(P), first = (rr * ((mg + ROWS - 1) / ROWS) + idx / ROWS) * P.units;
       const Sched& sc = x.few0 ? P.few : P.main;
       x.c0 = cta_of(sc, first, W);
       x.cnt0 = cta_of(sc, first + P.units - 1, W) - x.c0 + 1;
-      x.r0 = idx % ROWS;
     }
+    const Sched& sc = x.few0 ? P.few : P.main;
+    x.home0 = home_of(P, x.st0 > 1, rr, row, x.r0);
+    if (x.home0 < 0) x.home0 = sc.slots_at + (long long)x.c0 * sc.cta_rows + sc.slot_rows + x.r0;
+    if (!ONE && x.st0 > 1) x.more0 = more_of(P, rr, row, x.r0);
     x.whole = x.cnt0 == 1 && x.st0 == 1 && !P.in_place;
     if (MARKS) x.marked = x.mine && x.whole && !x.few0 && leaves_marks(P, min(ROWS, mg - idx / ROWS * ROWS)) && P.marks[row];
     x.out = b * P.ob + (r * P.group + idx % P.group) * P.oh + (i * P.m + idx / P.group) * P.ot;
@@ -163,10 +171,21 @@ __device__ __forceinline__ Partials partials_at(const Params& P, long long row) 
   return x;
 }
 
-// The largest reference of every parts-th partial from `part` on; whether one of them is marked.
-__device__ __forceinline__ float largest(const Params& P, const Partials& p, int part, int parts, bool& marked) {
+// The largest reference of every parts-th partial from `part` on; whether one of them is marked; the lane's first one.
+struct First { long long at; float2 ml; };
+template <bool ONE>
+__device__ __forceinline__ float largest(const Params& P, const Partials<ONE>& p, int part, int parts, bool& marked, First& f) {
   float M = NINF;
-  for (int k = (threadIdx.x & 31) * parts + part; k < p.n; k += 32 * parts) {
+  int k = (threadIdx.x & 31) * parts + part;
+  f.at = -1;
+  f.ml = make_float2(NINF, 0.f);
+  if (k < p.n) {
+    f.at = p.place(P, k);
+    f.ml = P.part_ml[f.at];
+    M = f.ml.x;
+    marked = marked || has_mark(f.ml.y);
+  }
+  for (k += 32 * parts; k < p.n; k += 32 * parts) {
     const float2 ml = P.part_ml[p.place(P, k)];
     M = fmaxf(M, ml.x);
     marked = marked || has_mark(ml.y);
@@ -177,7 +196,8 @@ __device__ __forceinline__ float largest(const Params& P, const Partials& p, int
 }
 __device__ __forceinline__ void add(float4& y, float w, const float4& x) { y.x = fmaf(w, x.x, y.x); y.y = fmaf(w, x.y, y.y); y.z = fmaf(w, x.z, y.z); y.w = fmaf(w, x.w, y.w); }
 // Their sum l and output o against the reference M.
-__device__ __forceinline__ void joined(const Params& P, const Partials& p, int part, int parts, float M, float& l, float4 (&o)[2]) {
+template <bool ONE>
+__device__ __forceinline__ void joined(const Params& P, const Partials<ONE>& p, int part, int parts, const First& f, float M, float& l, float4 (&o)[2]) {
   const int lane = threadIdx.x & 31, e0 = lane * 4, n = p.n;
   const bool vec = P.dh % 4 == 0;
   l = 0.f;
@@ -185,10 +205,10 @@ __device__ __forceinline__ void joined(const Params& P, const Partials& p, int p
   for (int k0 = part; k0 < n; k0 += 32 * parts) {
     const int k = k0 + lane * parts;
     float w = 0.f;
-    long long at = -1;
+    long long at = f.at;
+    float2 ml = f.ml;
+    if (k0 != part && k < n) { at = p.place(P, k); ml = P.part_ml[at]; }
     if (k < n) {
-      at = p.place(P, k);
-      const float2 ml = P.part_ml[at];
       if (ml.x == NINF || (ml.x == LOWEST && ml.y == 0.f)) at = -1;      // nothing in it (and no output written)
       else { w = exp2f(ml.x - M); l = fmaf(w, fabsf(ml.y), l); }
     }
@@ -223,7 +243,7 @@ __device__ __forceinline__ void joined(const Params& P, const Partials& p, int p
 // A marked row: true if it has been computed again.
 template <typename T>
 __device__ __noinline__ bool join_again(const Params& P, long long row, int part, int parts, Part y) {
-  const Partials p = partials_at<false>(P, row);
+  const Partials<false> p = partials_at<false, false>(P, row);
   bool force = false;                                  // (see look_again)
   if (p.st0 == 8 || p.st1 == 8)
     for (int k = 0; k < p.n; ++k) {
@@ -237,13 +257,14 @@ __device__ __noinline__ bool join_again(const Params& P, long long row, int part
 template <typename T>
 __device__ __noinline__ void join_marked(const Params& P, long long row) {
   if (join_again<T>(P, row, 0, 1, Part{nullptr, nullptr, nullptr})) return;
-  const Partials p = partials_at<false>(P, row);
+  const Partials<false> p = partials_at<false, false>(P, row);
   if (p.whole) return;                                 // what is there may stay
   bool marked = false;
-  const float M = largest(P, p, 0, 1, marked);
+  First f;
+  const float M = largest(P, p, 0, 1, marked, f);
   float l;
   float4 o[2];
-  joined(P, p, 0, 1, M, l, o);
+  joined(P, p, 0, 1, f, M, l, o);
   write_row<T>(P, p.out, M, l, o);
 }
 
@@ -251,7 +272,7 @@ __device__ __noinline__ void join_marked(const Params& P, long long row) {
 // them in flight, a lane four columns (and four more 128 further on); the warps' parts are added in their order.  One warp where rows
 // are many, eight where they are few (and their partials many: up to a hundred and fifty for a row of one short call).
 // MARKS: a row with a marked partial, or of a marked item, is looked at again, and computed again by the same warps if it has to be.  (Calls whose
-// kernels leave no marks do without: four sequences of one token behind 2048, 20.0 us, with it 20.7.)
+// kernels leave no marks, nor more than one partial a segment, do without: four sequences of one token behind 2048, 20.0 us, with it 20.7.)
 template <typename T, int WPR, bool MARKS>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params P) {
   __shared__ __align__(16) float s_o[WPR > 1 ? 8 : 1][RR_PAGED_MAX_DH], s_l[8], s_m[8];
@@ -259,14 +280,15 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   rr_pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % WPR, e0 = lane * 4;
   const long long row = (long long)blockIdx.x * (8 / WPR) + warp / WPR;
-  const Partials p = partials_at<MARKS>(P, row);
+  const Partials<!MARKS> p = partials_at<MARKS, !MARKS>(P, row);
   const bool mine = p.mine && (!p.whole || p.marked);
   if (WPR == 1 && !mine) return;
   bool again = p.marked;
-  float M = largest(P, p, part, WPR, again), l;
+  First f;
+  float M = largest(P, p, part, WPR, again, f), l;
   if (MARKS && WPR == 1 && __any_sync(FULL, again)) { join_marked<T>(P, row); return; }
   float4 o[2];
-  joined(P, p, part, WPR, M, l, o);
+  joined(P, p, part, WPR, f, M, l, o);
   if (WPR > 1) {
     if (lane == 0) { s_l[warp] = l; s_m[warp] = M; }
     *(float4*)&s_o[warp][e0] = o[0];
@@ -773,7 +795,7 @@ size_t lay_out(Params& P, uint8_t* ws) {
     P.few.cum = (long long*)(ws + at); at += up((size_t)(P.batch + 1) * 8);
     P.plan = (Plan*)(ws + at); at += up(sizeof(Plan));
   }
-  const size_t rows = (size_t)P.part_rows * P.streams;
+  const size_t rows = (size_t)P.part_rows;
   P.part_ml = (float2*)(ws + at); at += up(rows * sizeof(float2));
   P.part_o = (float*)(ws + at); at += up(rows * P.dh * sizeof(float));
   P.marks = ws + at; at += up(mark_rows(P));
@@ -808,8 +830,37 @@ bool misaligned(const void* q, const void* out, int dtype) {
   return (((uintptr_t)q | (uintptr_t)out) & (dtype == RR_BF16 ? 1 : 3)) != 0;
 }
 
+// The partial rows of a call of `all` rows: items of several partials a row (`items` of up to `last` rows each), rows of an item at most; all_homes: every
+// row is joined; prefix_homes: and has a partial of the prefix; main_shares: the main kernel's CTAs cut items.
 // Few rows are quartered by the tensor cores' kernel where eight partials a row are no great workspace.
-int streams_of(const Params& P) { return !P.tc ? 1 : P.part_rows * P.dh * 32 <= 512LL << 20 ? 8 : 2; }
+void lay_out_partials(Params& P, long long all, long long items, int last, int most, bool all_homes, bool prefix_homes, bool main_shares) {
+  const int split = P.tc ? std::min(last, TILE) : 0, quart = P.tc && (!P.slots || last <= 32) ? std::min(last, 32) : 0;
+  for (P.streams = P.tc ? 8 : 1;; P.streams = 2) {
+    const int more = P.streams == 8 ? std::max(split, 7 * quart) : split;              // further partials of an item
+    long long at = 0, further = 0;
+    auto take = [&](long long n) { const long long a = at; at += n; return a; };
+    auto take_more = [&](long long n) { further += n; return take(n); };
+    P.all_homes = all_homes; P.more_rows = more; P.step = quart;
+    if (prefix_homes) { take(all); take_more((long long)P.kv_heads * more); }
+    P.own.home = take(all_homes ? all : std::min(items * split, all));
+    P.own.home_per_item = !all_homes && items * split <= all ? split : 0;
+    const long long by_row = (P.streams - 1) * all;
+    P.own.more = take_more(std::min(items * more, by_row));
+    P.own.more_per_item = items * more <= by_row ? more : 0;
+    P.own.step = (int)(items * more <= by_row ? quart : all);
+    auto places = [&](Sched& sc, int rows, int m) {
+      sc.slot_rows = rows;
+      sc.more_at = all_homes ? rows : 2 * rows;
+      sc.cta_rows = sc.more_at + m;
+      sc.slots_at = take((long long)sc.ctas * sc.cta_rows);
+      further += (long long)sc.ctas * m;
+    };
+    if (main_shares) places(P.main, most, more);
+    if (P.few.ctas > 0 && (!P.slots || P.units)) places(P.few, std::min(most, FEW_ROWS), 0);
+    P.part_rows = at;
+    if (P.streams != 8 || further * P.dh * 4 <= 192LL << 20) return;
+  }
+}
 
 int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   const int rc = fill(kv, P);
@@ -830,16 +881,20 @@ int fill_shared(const rr_paged_kv* kv, const rr_shared_args* a, Params& P) {
   P.scale_log2 = a->scale * 1.4426950408889634f;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
   groups_of_four(P, kv->dtype);
-  const long long homes = 2LL * P.tokens * P.heads;
-  P.main = Sched{rr_sm_count() * (P.tc ? 1 : 2), ROWS, nullptr, homes};
-  P.part_rows = homes + (long long)P.main.ctas * ROWS;
+  P.main.ctas = rr_sm_count() * (P.tc ? 1 : 2);
   if (P.tc && P.group <= FEW_ROWS) {
     // (three CTAs fit an SM; two rounds of them even out segments of unlike lengths: 64 sequences of 1 to 2000 tokens 172 -> 156 us, three: 163)
-    P.few = Sched{rr_sm_count() * 6, FEW_ROWS, nullptr, P.part_rows};
-    P.part_rows += (long long)P.few.ctas * FEW_ROWS;
+    P.few.ctas = rr_sm_count() * 6;
     P.few_prefix = (long long)P.tokens * P.group <= FEW_ROWS;
   }
-  P.streams = streams_of(P);
+  const long long rows = (long long)P.tokens * P.group, packed = ceil_div(rows, ROWS);
+  // up to four rows in all, or one token of each sequence and no prefix to share: the few kernel has everything
+  P.few_waits = P.few.ctas > 0 && (P.few_prefix || (!P.cu && P.prefix == 0));
+  // (the sequences' row tiles are at most one less per sequence more than those of all rows together)
+  P.always_apart = P.prefix == 0 || P.batch - 1 <= packed / 8;
+  const int most = (int)std::min<long long>(ROWS, rows);
+  lay_out_partials(P, (long long)P.tokens * P.heads, P.few_waits ? 0 : (long long)P.batch * P.kv_heads, std::min(most, TILE), most,
+                   P.in_place || !P.always_apart, !P.always_apart, !P.few_waits);
   return RR_OK;
 }
 
@@ -869,19 +924,15 @@ int fill_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, Params& P) {
   P.range_rows = (long long)kv->batch * a->route_heads * a->n_q;
   P.tc = rr_attend_tc_supported(P, kv->dtype);
   groups_of_four(P, kv->dtype);
-  const long long items = P.range_rows * ceil_div((long long)P.m * P.group, ROWS), homes = P.range_rows * P.m * P.group;
-  const bool few = P.tc && (long long)P.m * P.group <= FEW_ROWS;
-  if (few) P.tc = 0;
-  P.main = Sched{rr_sm_count() * (P.tc ? 1 : (long long)P.m * P.group <= FEW ? 4 : 2), ROWS, nullptr, homes};
+  const int mg = P.m * P.group, last = mg - (mg - 1) / ROWS * ROWS;              // rows of an item's last row tile
+  const long long items = P.range_rows * ceil_div(mg, ROWS);
+  P.few_waits = P.tc && mg <= FEW_ROWS;
+  if (P.few_waits) P.tc = 0;
+  P.main.ctas = rr_sm_count() * (P.tc ? 1 : mg <= FEW ? 4 : 2);
   // (three CTAs fit an SM; more of them lose: 2048 rows of 396 tokens 52 us, with nine 61)
-  if (few) P.few = Sched{rr_sm_count() * 3, FEW_ROWS, nullptr, homes};
-  const Sched& sc = few ? P.few : P.main;
-  P.units = items < 8LL * sc.ctas ? UNITS : 0;
-  P.part_rows = homes + (long long)sc.ctas * sc.slot_rows;
-  P.streams = streams_of(P);
-  // (nothing to join: whole items, whose rows have one partial each; the last item of a range row may have fewer rows than the others)
-  const int mg = P.m * P.group, last = mg % ROWS;
-  if (!P.units && !P.in_place && partials_of(P.streams, std::min(mg, ROWS)) == 1 && (last == 0 || partials_of(P.streams, last) == 1)) P.part_rows = 0;
+  if (P.few_waits) P.few.ctas = rr_sm_count() * 3;
+  P.units = items < 8LL * (P.few_waits ? P.few : P.main).ctas ? UNITS : 0;
+  lay_out_partials(P, P.range_rows * mg, P.tc && last <= TILE ? P.range_rows : 0, last <= TILE ? last : 0, std::min(ROWS, mg), P.in_place, false, P.units && !P.few_waits);
   return RR_OK;
 }
 
@@ -893,10 +944,7 @@ int run(Params& P, int dtype, void* workspace, size_t bytes, cudaStream_t st, co
   cudaError_t e = cudaSuccess;
   int launches = 0;
   if (!P.slots) { e = rr_launch_pdl(plan_kernel, 1, PLAN_NT, 0, st, P); ++launches; }
-  const bool few = P.few.ctas > 0;
-  // up to four rows in all, or one token of each sequence and no prefix to share: the few kernel has everything
-  const bool only_few = few && (P.slots || P.few_prefix || (!P.cu && P.prefix == 0));
-  P.few_waits = only_few;
+  const bool few = P.few.ctas > 0, only_few = P.few_waits;
   if (e == cudaSuccess && !only_few) {
     long long grid = P.main.ctas;
     if (P.slots && !P.units) grid = std::min<long long>(grid, P.range_rows * ceil_div((long long)P.m * P.group, ROWS));

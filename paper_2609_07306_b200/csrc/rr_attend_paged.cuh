@@ -16,8 +16,9 @@
 //
 // shared: the tiles of all items in one row, N CTAs take equal shares of it (an item may be cut anywhere, a
 // CTA's share may span many items), so neither a long prefix of few rows nor one long sequence among short ones leaves SMs idle.
-// plan_kernel counts the tiles on the device, where the lengths are, for the few-row kernel's items and the others apart.  A segment that begins
-// its item has its partial rows at the rows' own places; a CTA has at most one segment that does not, whose rows go to the CTA's own places.
+// plan_kernel counts the tiles on the device, where the lengths are, for the few-row kernel's items and the others apart.  A CTA has at most one segment
+// that does not begin its item and one that begins an item without ending it; their partial rows have places of the CTA's own.  Items whose rows are joined
+// although no CTA cuts them (behind a prefix, or of several partials) have homes by their rows.
 // ranges: items are alike.  Where there are fewer than eight per CTA each counts as UNITS units that the CTAs share equally, as the tiles above (a
 // segment has the tiles of its units by the item's own number of tiles); where there are more, CTAs take whole items in turn, so that
 // neighbouring rows, whose routes overlap, are read at the same time.
@@ -31,11 +32,21 @@ constexpr int NO_TOKEN = 0x7FFFFFFF;                   // id of a place without 
 constexpr float NINF = -__builtin_huge_valf();
 constexpr float LOWEST = -3.402823466e38f;             // m of a row that saw tokens, all of them at -inf
 
-// Who shares the items: CTAs, the tiles before each sequence's items, and where the CTAs' own places among the partial rows begin.
+// Who shares the items: CTAs, the tiles before each sequence's items, and the CTAs' own places among the partial rows: for the segment that does not begin
+// its item, behind it for one that begins an item without a home, and behind both for the first one's further partials.
 struct Sched {
-  int ctas, slot_rows;                                 // slot_rows: rows of a CTA's place
+  int ctas, slot_rows, more_at, cta_rows;              // rows of a segment's place; where a CTA's further partials begin; rows of a CTA's places
   long long* cum;                                      // shared: [batch + 1] tiles before sequence b's items; [batch] = all tiles
   long long slots_at;
+};
+
+// Homes of rows among the partial rows: of all rows (Params::all_homes), else of those of items whose segments leave several partials; further
+// partials are in `more`, `step` apart.  An item of several partials is a sequence's (or range row's) last row tile with a key head, at most
+// 128 rows: homes go by that (per_item rows each), or by the row's index (per_item == 0).  Of the prefix's items all rows have homes, by the
+// row's index from 0 on, and behind these the last row tile of each key head has its further partials, Params::more_rows rows.
+struct Homes {
+  long long home, more;
+  int home_per_item, more_per_item, step;
 };
 
 // What plan_kernel finds out from the lengths besides the tiles before each sequence's items.
@@ -66,13 +77,16 @@ struct Params {
   Sched main, few;                                     // few: items of up to FEW_ROWS rows in a kernel of their own (ctas == 0: no such kernel)
   int tc, units, streams;                              // units: of a ranges item (0: whole items in turn); streams: most partials of a segment's row
   bool few_prefix;                                     // the few kernel has the prefix's items, too: all queries make up to FEW_ROWS rows
-  int few_waits;                                       // the few kernel's inputs are its predecessor's (else it only ends after that)
+  int few_waits;                                       // the few kernel has everything, its inputs are its predecessor's (else it only ends after that)
+  int always_apart;                                    // whatever the lengths are
   long long range_rows;                                // batch * route_heads * n_q
   // workspace
   Plan* plan;                                          // shared
-  float* part_o;                                       // [streams][part_rows][dh]
-  float2* part_ml;                                     // [streams][part_rows]
+  float* part_o;                                       // [part_rows][dh]
+  float2* part_ml;                                     // [part_rows]
   long long part_rows;
+  Homes own;
+  int all_homes, more_rows, step;                      // further partials of a CTA's segment or a prefix item: rows, `step` apart
   uint8_t* marks;                                      // of rows that are written without partials: [tokens * heads] or [range_rows * m * group]
   int vq, vk;                                          // queries / cache rows split into aligned groups of four
   int in_place;                                        // the output is the queries' memory: only the join writes it, a row at a time
@@ -91,7 +105,8 @@ struct Seg {
   const int32_t* slots;                                // ranges: the row's slots, else null
   int tile0, tile1;                                    // the segment's tiles of the list (ranges: once counted)
   int unit0, unit1;                                    // ranges: the segment's units of the item's `units` (of 1 if whole)
-  long long part;                                      // partial row of row 0
+  long long part, more;                                // partial row of row 0; of its further partials, `step` apart
+  int step;
   long long mark;                                      // row 0's place among the marks
 };
 
@@ -136,6 +151,30 @@ __device__ __forceinline__ int cta_of(const Sched& sc, long long u, long long W)
   return (int)(ceil_div((u + 1) * N, W) - 1);
 }
 
+// Partials that a segment of `rows` rows leaves per row.
+__host__ __device__ inline int partials_of(int streams, long long rows) { return streams == 1 || rows > TILE ? 1 : streams > 2 && rows <= 32 ? 8 : 2; }
+
+// The home of row `at` of all, row r of its row tile, item `item` of several partials: its first partial (-1: none) and its further ones.
+__device__ __forceinline__ long long home_of(const Params& P, bool several, long long item, long long at, int r) {
+  return P.all_homes || several ? P.own.home + (P.own.home_per_item ? item * P.own.home_per_item + r : at) : -1;
+}
+__device__ __forceinline__ long long more_of(const Params& P, long long item, long long at, int r) { return P.own.more + (P.own.more_per_item ? item * P.own.more_per_item + r : at); }
+__device__ __forceinline__ long long prefix_more_of(const Params& P, int kvh, int r) { return (long long)P.tokens * P.heads + (long long)kvh * P.more_rows + r; }
+// Where a segment's partials go (s.mark: the index of its row 0).
+__device__ __forceinline__ void place_segment(const Params& P, const Sched& sc, int c, bool begins, long long item, Seg& s) {
+  const long long cta = sc.slots_at + (long long)c * sc.cta_rows;
+  if (!begins) {
+    s.part = cta; s.more = cta + sc.more_at; s.step = P.step;
+  } else if (s.b < 0) {
+    s.part = s.mark; s.more = prefix_more_of(P, s.kvh, 0); s.step = P.step;
+  } else {
+    const bool several = &sc == &P.main && partials_of(P.streams, s.rows) > 1;
+    s.part = home_of(P, several, item, s.mark, 0);
+    if (s.part < 0) s.part = cta + sc.slot_rows;
+    s.more = more_of(P, item, s.mark, 0); s.step = P.own.step;
+  }
+}
+
 // The segment at tile u of CTA c's share, which ends at u1; returns how many tiles of the share it takes.
 __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int c, long long u, long long u1, Seg& s) {
   const Plan plan = plan_of(P);
@@ -143,7 +182,6 @@ __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int 
   const long long np = prefix_tiles(plan), qtp = prefix_row_tiles(P), before = (&sc == &P.few) == P.few_prefix ? P.kv_heads * qtp * np : 0;
   long long first;                                     // first tile of the item
   int tiles;
-  long long home;
   const long long row_all = (long long)P.tokens * P.group;
   s.slots = nullptr;
   s.prefix_pages = P.prefix_pages ? P.prefix_pages : P.table + plan.source * P.table_stride;
@@ -159,7 +197,6 @@ __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int 
     s.t_base = 0; s.t_seq0 = 0; s.n_seq = 0;
     s.tok0 = 0; s.tok1 = plan.prefix;
     s.pages = s.prefix_pages;
-    home = s.kvh * row_all + s.row0;
   } else {
     int lo = 0, hi = P.batch;                          // last b with cum[b] <= u
     while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (__ldg(sc.cum + mid) <= u) lo = mid; else hi = mid; }
@@ -175,7 +212,6 @@ __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int 
     s.t_base = s.t_seq0 = seq_first(P, b);
     s.tok0 = apart ? 0 : P.prefix; s.tok1 = seq_len(P, b);
     s.pages = P.table + b * P.table_stride;
-    home = (P.kv_heads + s.kvh) * row_all + (long long)s.t_base * P.group + s.row0;
   }
   s.mark = s.kvh * row_all + (long long)s.t_base * P.group + s.row0;
   s.h0 = s.kvh * P.group;
@@ -187,7 +223,7 @@ __device__ __forceinline__ int segment_at(const Params& P, const Sched& sc, int 
     const long long limit = (long long)seq_end(P, s.b) - s.n_seq + (s.row0 + s.rows - 1) / P.group + 1;
     s.tile1 = max(s.tile0, limit <= s.tok0 ? 0 : (int)min((long long)s.tile1, (limit - s.tok0 + TILE - 1) / TILE));
   }
-  s.part = s.tile0 == 0 ? home : sc.slots_at + (long long)c * sc.slot_rows;
+  place_segment(P, sc, c, s.tile0 == 0, (long long)s.b * P.kv_heads + s.kvh, s);
   return took;
 }
 
@@ -213,7 +249,7 @@ __device__ __forceinline__ int range_segment(const Params& P, const Sched& sc, i
   s.prefix = 0;
   s.tile0 = s.tile1 = 0;
   s.mark = row * mg + s.row0;
-  s.part = s.unit0 == 0 ? row * mg + s.row0 : sc.slots_at + (long long)c * sc.slot_rows;
+  place_segment(P, sc, c, s.unit0 == 0, row, s);
   return s.unit1 - s.unit0;
 }
 __device__ __forceinline__ void unit_tiles(const Params& P, int tiles, Seg& s) {
@@ -233,9 +269,6 @@ __device__ __forceinline__ void slot_span(const Seg& s, int j, int& lo, int& hi)
   hi = min(__ldg(s.slots + 2 * j + 1), s.tok1);
   if (lo < 0 || hi < lo) lo = hi = 0;
 }
-
-// Partials that a segment of `rows` rows leaves per row.
-__host__ __device__ inline int partials_of(int streams, long long rows) { return streams == 1 || rows > TILE ? 1 : streams > 2 && rows <= 32 ? 8 : 2; }
 
 struct RowAt { int t, h, limit; };                     // query token, head, tokens below `limit` are seen
 __device__ __forceinline__ RowAt row_at(const Params& P, const Seg& s, int r) {

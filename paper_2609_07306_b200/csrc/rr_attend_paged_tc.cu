@@ -416,7 +416,8 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
       const bool direct = paired && s.whole;
       if (warp_live) {
         if (seen && ref == NINF) ref = LOWEST;
-        const long long at = (paired ? 0 : quart ? (st * 4 + quarter) * P.part_rows : st * P.part_rows) + s.part + r;
+        const int part = paired ? 0 : quart ? st * 4 + quarter : st;
+        const long long at = (part == 0 ? s.part : s.more + (long long)(part - 1) * s.step) + r;
         const float inv = sum == 0.f ? (ref == NINF ? 0.f : __int_as_float(0x7fc00000)) : 1.f / sum;
         const RowAt a{s.t_base + (s.row0 + r) / P.group, s.h0 + (s.row0 + r) % P.group, 0};
         __nv_bfloat16* const out = (__nv_bfloat16*)P.out + out_at(P, s, a);

@@ -155,3 +155,27 @@ def test_outputs_over_the_queries():
     assert B.rr_attend_paged_ranges_workspace(kv(), ranges(out=0x10000)) > 0
     for kw in (dict(out_batch_stride=2048), dict(out_head_stride=512), dict(out_token_stride=128)):
         assert lib.rr_attend_paged_ranges(C.byref(kv()), C.byref(ranges(out=0x10000, **kw)), 0x100, 1 << 40, None) == B.RR_ERR_INVALID_ARG
+
+
+def serving(tokens, batch, heads, prefix, dh=128, dtype=B.RR_BF16):
+    c = kv(kv_heads=8, dh=dh, batch=batch, pages_per_seq=8192, page_tokens=64, page_stride=1 << 16, head_stride=64 * dh, token_stride=dh, dtype=dtype)
+    return B.rr_attend_shared_workspace(c, shared(q_token_stride=heads * dh, q_head_stride=dh, out_token_stride=heads * dh, out_head_stride=dh,
+                                                  tokens=tokens, heads=heads, prefix_tokens=prefix))
+
+
+def test_workspaces_go_by_what_is_joined():
+    """A token of one sequence: some megabytes.  Long prompts: what the SMs cut, whatever the length; less than the outputs.  Rows behind a
+    shared prefix: one partial of the prefix and, in tiles of up to 128 rows, two of their own, of FP32."""
+    assert serving(1, 1, 32, 0) < 10 << 20 and serving(1, 1, 64, 4096) < 10 << 20
+    for n in (4096, 32768, 131072):
+        assert serving(n, 1, 32, 0) < 100 << 20 and serving(n, 4, 32, 8192) < 120 << 20
+    assert serving(131072, 1, 32, 8192) < 131072 * 32 * 128 * 2
+    for n, b in ((3000, 8), (4096, 256), (16384, 2048)):
+        assert serving(n, b, 32, 8192) < 3 * n * 32 * (128 * 4 + 8) + (100 << 20)
+    for dtype in (B.RR_BF16, B.RR_F32):
+        sizes = [serving(n, 2, 32, 0, dtype=dtype) for n in (2, 8, 64, 512, 4096, 32768, 262144)]
+        assert sizes == sorted(sizes)
+    c = kv(kv_heads=8, dh=128, batch=2, page_stride=1 << 20, head_stride=8192, token_stride=128, page_tokens=64, pages_per_seq=128)
+    whole = ranges(heads=32, route_heads=8, n_q=128, m=64, slots=32, q_token_stride=128, q_head_stride=1 << 20, q_batch_stride=1 << 25,
+                   out_token_stride=128, out_head_stride=1 << 20, out_batch_stride=1 << 25)
+    assert B.rr_attend_paged_ranges_workspace(c, whole) == 2 * 32 * 8192           # a byte a row
