@@ -36,7 +36,7 @@ class PagedKV:
     status            optional [1] int32: RR_STATUS_* bits are OR-ed into it (RR_STATUS_BAD_INDEX: a page id outside the
                       pool, or a position behind the table's end, was met and left out)
 
-    The object keeps the tensors, checks the descriptions of the arguments and passes addresses on; it keeps no results
+    The object keeps the tensors (they are written to, not exchanged: another table is another PagedKV), checks the descriptions of the arguments and passes addresses on; it keeps no results
     and no workspace, so calls on several streams do not meet (each call's workspace comes from torch's allocator on the
     current stream, and from a graph's pool while one is captured).  Work goes to the current stream of the cache's
     device, whichever device is the current one."""
@@ -51,7 +51,7 @@ class PagedKV:
             raise ValueError("k_cache and v_cache must have the same strides")
         if k_cache.shape[3] > 1 and k_cache.stride(3) != 1:
             raise ValueError("the entries of a head must be contiguous")
-        self.k_cache, self.v_cache, self.page_table, self.status = k_cache, v_cache, page_table, status
+        self._tensors = (k_cache, v_cache, page_table, status)
         self.device = k_cache.device
         if self.device.type != "cuda":
             raise ValueError("the cache must be on a CUDA device (there is no CPU path)")
@@ -73,6 +73,12 @@ class PagedKV:
             pages_per_seq=page_table.shape[1])
         self._at = C.addressof(self._kv)
         self._lib = B.lib()
+
+    # what the description points to: the tensors are written to, not exchanged
+    k_cache = property(lambda self: self._tensors[0])
+    v_cache = property(lambda self: self._tensors[1])
+    page_table = property(lambda self: self._tensors[2])
+    status = property(lambda self: self._tensors[3])
 
     # -- checks: one comparison each for what is right, the reason where it is not ----------------------------
     def _heads(self, t, name, shape):
