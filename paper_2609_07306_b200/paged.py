@@ -36,6 +36,7 @@ class PagedKV:
     status            optional [1] int32: RR_STATUS_* bits are OR-ed into it (RR_STATUS_BAD_INDEX: a page id outside the
                       pool, or a position behind the table's end, was met and left out)
 
+    Forward only: no operator has a gradient, and a tensor that requires one is refused (but under torch.no_grad()).
     The object keeps the tensors (they are written to, not exchanged: another table is another PagedKV), checks the descriptions of the arguments and passes addresses on; it keeps no results
     and no workspace, so calls on several streams do not meet (each call's workspace comes from torch's allocator on the
     current stream, and from a graph's pool while one is captured).  Work goes to the current stream of the cache's
@@ -51,6 +52,8 @@ class PagedKV:
             raise ValueError("k_cache and v_cache must have the same strides")
         if k_cache.shape[3] > 1 and k_cache.stride(3) != 1:
             raise ValueError("the entries of a head must be contiguous")
+        if k_cache.requires_grad or v_cache.requires_grad:
+            raise ValueError("the cache must not require a gradient (its operators have none)")
         self._tensors = (k_cache, v_cache, page_table, status)
         self.device = k_cache.device
         if self.device.type != "cuda":
@@ -84,15 +87,17 @@ class PagedKV:
     def _heads(self, t, name, shape):
         """t has the cache's type and device, the given shape (its last entry dh), contiguous heads; its strides."""
         strides = t.stride()
-        if t.dtype is self._dtype and t.get_device() == self._index and t.shape == shape and strides[-1] == 1:
+        if t.dtype is self._dtype and t.get_device() == self._index and t.shape == shape and strides[-1] == 1 and not t.requires_grad:
             return strides
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, which the cache's operators do not have: call them under torch.no_grad()")
         if t.device != self.device:
             raise ValueError(f"{name} is on {t.device}, the cache on {self.device}")
         if t.dtype is not self._dtype:
             raise TypeError(f"{name} must be {self._dtype}, not {t.dtype}")
         if t.shape != shape:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-        if self.dh > 1 and t.numel() > 0:
+        if self.dh > 1 and t.numel() > 0 and strides[-1] != 1:
             raise ValueError(f"the entries of a head of {name} must be contiguous")
         return strides
 
@@ -110,7 +115,7 @@ class PagedKV:
 
     def _run(self, name, args, workspace=None):
         """One library call on the current stream of the cache's device."""
-        if self._index != torch.cuda.current_device():
+        if self._index != torch._C._cuda_getDevice():
             with torch.cuda.device(self.device):
                 return self._run(name, args, workspace)
         stream = torch._C._cuda_getCurrentRawStream(self._index)
