@@ -322,7 +322,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) marked_kernel(const __grid_constant__ Params P) {
   rr_pdl_wait();
   rr_pdl_trigger();
-  const long long rows = P.range_rows * P.m * P.group;
+  const int mg = P.m * P.group;
+  const long long rows = P.range_rows * mg;
   for (long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 16; __any_sync(FULL, at < rows); at += (long long)gridDim.x * 256 * 16) {
     const uint4 x = at < rows ? *(const uint4*)(P.marks + at) : make_uint4(0, 0, 0, 0);      // (behind the last row: anything)
     unsigned some = __ballot_sync(FULL, x.x | x.y | x.z | x.w);
@@ -330,8 +331,10 @@ __global__ void __launch_bounds__(256) marked_kernel(const __grid_constant__ Par
       const int from = __ffs(some) - 1;
       some &= some - 1;
       const long long row0 = __shfl_sync(FULL, at, from);
-      for (long long row = row0; row < min(row0 + 16, rows); ++row)
-        if (P.marks[row]) look_again<T>(P, row, false, 0, 1, Part{nullptr, nullptr, nullptr});
+      for (long long row = row0; row < min(row0 + 16, rows); ++row) {
+        const int idx = (int)(row - quot(row, mg) * mg);
+        if (leaves_marks(P, min(ROWS, mg - idx / ROWS * ROWS)) && P.marks[row]) look_again<T>(P, row, false, 0, 1, Part{nullptr, nullptr, nullptr});
+      }
     }
   }
 }

@@ -152,3 +152,25 @@ def test_few_rows_on_the_tensor_cores(dh, heads, x):
     got, want = shared_call(g, k, v, table, heads, [3000, 2500], [1, 1])
     assert got[0, :, [5, 6, 0, 2]].isnan().all() if x != x else (got[0, :, [5, 6, 0, 2]] == x).all()
     assert got[0, :, 20].isnan().all() and got[1].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype,dh", [(torch.float32, 64), (torch.bfloat16, 80), (torch.bfloat16, 64)])
+@pytest.mark.parametrize("m,G", [(65, 4), (33, 8), (1, 260), (1, 9)])
+def test_what_the_workspace_held_does_not_matter(dtype, dh, m, G):
+    """Rows that leave no marks beside rows that do: the last row tile of an item may have up to eight."""
+    n_q = 2400
+    n = n_q * m + 20
+    g, k, v, table = pool(dtype, 1, 1, dh, 16, n, G)
+    lo = torch.arange(n_q, device="cuda") * m
+    rg = torch.stack((lo, lo + m + 10), 1)[:, None].int().contiguous()
+    for i in range(0, n_q, 5):
+        put(v, table, 0, i * m + m + 3, 0, i % 16, NAN)
+    q = torch.randn((1, G, n_q * m, dh), generator=g, device="cuda").to(dtype)
+    L = torch.tensor([n_q * m], dtype=torch.int32, device="cuda")
+    kv, outs = PagedKV(k, v, table), []
+    for fill in (0, 255):
+        held = [torch.full((size,), fill, dtype=torch.uint8, device="cuda") for size in (1 << 20, 1 << 22, 1 << 24, 1 << 26)]
+        del held
+        outs.append(kv.attend_ranges(q, rg, L, n_q, 0.1, causal=True))
+    ints = [x.view(torch.int16 if dtype == torch.bfloat16 else torch.int32) for x in outs]
+    assert torch.equal(*ints)
