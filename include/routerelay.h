@@ -425,7 +425,7 @@ typedef struct rr_shared_args {
   int32_t tokens, heads, prefix_tokens, causal;
   float scale;
 } rr_shared_args;
-/* The workspace holds partial results in FP32 (dh + 2 numbers a row): of what the SMs cut, at most 736 rows for each, of row tiles of up to 128 rows, two
+/* The workspace holds partial results in FP32 (dh + 2 numbers a row): of what the SMs cut, at most 1024 rows for each, of row tiles of up to 128 rows, two
  * to eight a row, and of rows whose prefix is computed with other sequences' (not where sequences have some eight row tiles of 256 or
  * more each), one more each.  64 MB for a prompt of 131072 tokens, 32 heads of 128; 4 MB for a single token. */
 int rr_attend_shared_workspace(const rr_paged_kv* kv, const rr_shared_args* a, size_t* bytes);

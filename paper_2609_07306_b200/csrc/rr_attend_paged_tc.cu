@@ -2,7 +2,9 @@
 // for items, segments and how their partial results are joined).
 //
 // One CTA per SM walks its segments.  Per tile of 128 tokens and 128 query rows:  S = Q K^T (TMEM, FP32), softmax against a
-// running reference, P (bf16, written over S in TMEM) and O += P V (TMEM, FP32).  Two streams of four warps:
+// running reference, P (bf16, written over S in TMEM) and O += P V (TMEM, FP32).  P has the values' 16 bits because the product takes operands of one
+// type; a high and a low part would take a third product and half the TMEM stores again.  The sum is of the unrounded weights.  Error against 64
+// bits 0.0022 to 0.0023 relative, 0.0017 for a bf16 output of FP32 weights.  Two streams of four warps:
 //   a segment of more than 128 rows is paired: stream 0 has rows 0..127, stream 1 the others, each tile of keys and values is
 //   read once for both;
 //   one of up to 128 rows is split: both streams have the same rows, stream 0 the even tiles and stream 1 the odd ones, and

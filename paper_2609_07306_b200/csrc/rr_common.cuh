@@ -142,11 +142,12 @@ __device__ __forceinline__ bool rr_challenge(const RRParams& p, int g, float alp
 //      itself has finished (the caller's copies and kernels, whose results are the inputs, included).
 //   2. Every path through a kernel waits before it ends, so a kernel's end means that all before it
 //      has ended, and a wait for the predecessor is a wait for everything before.
-//   3. All kernels but one trigger after their wait.  The one is the routing kernel at an anchor: its
+//   3. All kernels but two trigger after their wait.  One of the two is the routing kernel at an anchor: its
 //      predecessor is the anchor's fill, which by 1 has let it start when the inputs were complete and
 //      all earlier layers were done, and which writes nothing that it reads or writes.  It triggers and
 //      works without waiting for the fill and waits before it ends (by 2 its successor, which waits
-//      for it before anything else, finds both done).
+//      for it before anything else, finds both done).  The other is the few-row kernel of the paged attention behind the tensor cores'
+//      kernel of the same call: it reads what that kernel reads, writes other rows, and waits and triggers at its end.
 __device__ __forceinline__ void rr_pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void rr_pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <class... P, class... A>

@@ -2,9 +2,9 @@
 //
 // Token t of sequence b at position p = lens[b] + (t - cu[b]):
 //   K[page(b, p)][h][p % ps] = R(p) k[t, h],   V[...] = v[t, h],   q_out[t, h] = R(p) q[t, h]
-// R(p) turns pair j of a head's first `rot` entries by p * inv_freq[j].  In turns that is p * (inv_freq[j] / 2 pi), a
-// product of at most 31 + 24 bits that 64-bit arithmetic holds, as it does its fractional part; the sine and cosine of
-// what is left (at most half a turn) are FP32's.  All heads of a token share its angles.
+// R(p) turns pair j of a head's first `rot` entries by p * inv_freq[j].  In turns that is p * (inv_freq[j] / 2 pi), formed in 64 bits: both
+// roundings are below 2^-53 of it, 2^-22 of a turn at the last position, 2^-32 up to position 2^21.  Its fractional part is exact there; the
+// sine and cosine of what is left (at most half a turn) are FP32's.  All heads of a token share its angles.
 //
 // The work is one read and one write of every entry: bound by memory for prompts, by latency for a decoding
 // step.  A CTA takes a token; its threads take 16 bytes each (the two halves of eight or four pairs), read them before

@@ -62,7 +62,7 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Bounded wait: gives up after about a second, records it in *abort_flag (shared memory)
+// Bounded wait: gives up after some seconds (the one that ran out on a B200 ended its kernel 16 s after its launch), records it in *abort_flag (shared memory)
 // and returns false.  Every role checks the flag and leaves its loop, so the CTA can free
 // its TMEM and exit instead of hanging.
 constexpr uint32_t kSpinLimit = 1u << 22;
@@ -82,7 +82,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity,
 // Bounded wait without sleeping, for the single threads whose hand-offs are on the critical
 // path of a tile pipeline (TMA producer, MMA issuer): a sleep quantum between polls would be
 // added to every tile.  The limit is counted in polls (a failed try_wait itself blocks for a
-// hardware-defined slice, so this is of the order of a second).
+// hardware-defined slice, so this is of the order of ten seconds).
 __device__ __forceinline__ bool mbar_wait_spin(uint64_t* bar, uint32_t parity,
                                                volatile uint32_t* abort_flag) {
 #pragma unroll 1
