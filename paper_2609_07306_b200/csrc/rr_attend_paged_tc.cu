@@ -203,7 +203,8 @@ __device__ __noinline__ void look_at_own(const Params& P) {
   }
 }
 
-template <int D>
+// OWN: no join comes behind.  (A build of its own: the call's stack costs every launch of the kernel a hundredth.)
+template <int D, bool OWN>
 __global__ void __launch_bounds__(NT, 1)
 attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps maps, const int ring) {
   using S = Shape<D>;
@@ -497,7 +498,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
           const bool mark = odd_rows && mixed;
           if (direct) {
             mark_row(P, s.mark + r, mark);
-            if (mark) c->marked = 1;
+            if (OWN && mark) c->marked = 1;
           } else {
             P.part_ml[at] = make_float2(ref, with_mark(sum, mark));
           }
@@ -816,7 +817,7 @@ attend_tc_kernel(const __grid_constant__ Params P, const __grid_constant__ Maps 
     tmem_dealloc(tmem, 512);
     if (lane == 0 && c->abort_flag && P.status) atomicOr(P.status, RR_STATUS_TIMEOUT);
   }
-  if (c->marked && P.slots && P.part_rows == 0 && threadIdx.x < ROWS) look_at_own(P);
+  if (OWN && c->marked && threadIdx.x < ROWS) look_at_own(P);
 }
 
 template <int D>
@@ -831,11 +832,12 @@ cudaError_t launch(const Params& p, int grid, cudaStream_t st) {
   const int ring = p.slots > 256 ? 2 : MAX_RING;
   static unsigned long long done = 0;
   const cudaError_t e = rr_once_per_device(done, [] {
-    const int a = Smem::total<D>(256, MAX_RING), b = Smem::total<D>(RR_MAX_RANGE_SLOTS, 2);
-    return cudaFuncSetAttribute(attend_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, a > b ? a : b);
+    const int most = std::max(Smem::total<D>(256, MAX_RING), Smem::total<D>(RR_MAX_RANGE_SLOTS, 2));
+    const cudaError_t a = cudaFuncSetAttribute(attend_tc_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return a == cudaSuccess ? cudaFuncSetAttribute(attend_tc_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) : a;
   });
   if (e != cudaSuccess) return e;
-  return rr_launch_pdl(attend_tc_kernel<D>, grid, NT, (size_t)Smem::total<D>(p.slots, ring), st, p, maps, ring);
+  return rr_launch_pdl(p.slots && p.part_rows == 0 ? attend_tc_kernel<D, true> : attend_tc_kernel<D, false>, grid, NT, (size_t)Smem::total<D>(p.slots, ring), st, p, maps, ring);
 }
 
 }  // namespace
