@@ -299,13 +299,11 @@ def _prepare_verify(s, case, g, dt):
         p = torch.softmax(logits, 1)
         s.target = p.to(dt)
         # a draft model that agrees with the target by the given share and otherwise draws as for another row
-        q = (case["accept"] * p + (1 - case["accept"]) * p.roll((1, V // 3), (0, 1)))[~last]
-        s.draft = q.to(dt)
+        s.draft = (case["accept"] * p + (1 - case["accept"]) * p.roll((1, V // 3), (0, 1))).to(dt)
         s.uniform = torch.rand(T, generator=g, device="cuda")
         cum = s.draft.double().cumsum(1)
-        x = torch.searchsorted(cum, pick[~last].double()[:, None] * cum[:, -1:], right=True)
-        after = torch.zeros(T, dtype=torch.long, device="cuda")
-        after[~last] = x[:, 0].clamp_max(V - 1)
+        after = torch.searchsorted(cum, pick.double()[:, None] * cum[:, -1:], right=True)[:, 0].clamp_max(V - 1)
+        s.draft[last] = float("nan")                                         # (a sequence's last row drafted nothing)
     # the step's tokens: the last known one of a sequence, then its drafts
     s.tokens = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
     s.tokens[1:] = torch.where(last[:-1], s.tokens[1:], after[:-1].int())
@@ -462,17 +460,14 @@ def _verify(s):
         best = torch.where(z == z.amax(1, keepdim=True), torch.arange(V, device="cuda"), V).amin(1)
         ok = best[row] == x
     else:
-        at = (row - torch.arange(B, device="cuda")[:, None]).clamp(0, max(0, s.draft.shape[0] - 1))
-        q = s.draft[at, x].double() if s.draft.shape[0] else torch.zeros((B, most), dtype=torch.float64, device="cuda")
-        ok = s.target[row, x].double() > s.uniform.double()[row] * q
+        ok = s.target[row, x].double() > s.uniform.double()[row] * s.draft[row, x].double()
     accepted = (ok & is_draft).int().cumprod(1).sum(1)
     end = cu[:-1] + accepted
     if s.uniform is None:
         token = best[end]
     else:
         p = s.target[end].double()
-        rest = (p - s.draft[(end - torch.arange(B, device="cuda")).clamp_max(s.draft.shape[0] - 1)].double()).clamp_min(0.0) if s.draft.shape[0] else p
-        cum = torch.where((accepted < n)[:, None], rest, p).cumsum(1)
+        cum = torch.where((accepted < n)[:, None], (p - s.draft[end].double()).clamp_min(0.0), p).cumsum(1)
         token = torch.searchsorted(cum, s.uniform.double()[cu[1:] - 1, None] * cum[:, -1:], right=True)[:, 0].clamp_max(V - 1)
     out = torch.full((T,), -1, dtype=torch.int32, device="cuda")
     seq = torch.searchsorted(cu[1:].contiguous(), torch.arange(T, device="cuda"), right=True)
@@ -599,7 +594,7 @@ def _exact_verify(case, s):
             a = next((i for i in range(n) if best[i] != drafted[first + 1 + i]), n)
             token = best[a]
         else:
-            draft = s.draft[first - b:first - b + n].double().cpu().numpy()
+            draft = s.draft[first:first + n].double().cpu().numpy()
             x = drafted[first + 1:first + 1 + n]
             a = next((i for i in range(n) if not target[i][x[i]] > u[first + i] * draft[i][x[i]]), n)
             weight = target[a] if a == n else np.maximum(target[a] - draft[a], 0.0)
