@@ -58,6 +58,7 @@ extern "C" {
 /* bits of the device status word (rr_ledger_status) */
 #define RR_STATUS_TIMEOUT      1u  /* an mbarrier wait in a kernel gave up                     */
 #define RR_STATUS_BAD_INDEX    2u  /* a ledger entry outside [0, v_i) was met and skipped      */
+#define RR_STATUS_NO_PAGES     4u  /* rr_pages_reserve: fewer free pages than the call needs   */
 
 typedef struct rr_ledger rr_ledger;   /* opaque; owns only a small host struct */
 
@@ -406,6 +407,17 @@ typedef struct rr_append_args {
 } rr_append_args;
 int rr_kv_append(const rr_paged_kv* kv, const rr_append_args* a, void* stream);
 
+/* The same with positions of several axes (time, height and width of an image's or a video's patches): pair j of token t is
+ * turned by the angle positions[axis_of[j]][t] * inv_freq[j], whichever sections or turns the pairs take; the token's place in the cache is still
+ * lens[b] + its number.  A pair whose axis is outside [0, axes) is not turned and sets RR_STATUS_BAD_INDEX.  rot > 0. */
+typedef struct rr_axes_args {
+  const int32_t* positions;  /* [axes, tokens], any position                                      */
+  const int32_t* axis_of;    /* [rot / 2] the axis of every pair; NULL: the first                 */
+  int64_t axis_stride, token_stride;
+  int32_t axes;
+} rr_axes_args;
+int rr_kv_append_axes(const rr_paged_kv* kv, const rr_append_args* a, const rr_axes_args* x, void* stream);
+
 /* Attention of a batch that shares a prefix:  out = softmax(q K^T * scale) V  for the queries q of the tokens
  * [cu[b], cu[b + 1]) of each sequence b, over the sequence's tokens s < lens[b].
  *   causal != 0   the queries are the sequence's last tokens: the i-th of its n sees s <= lens[b] - n + i
@@ -451,6 +463,83 @@ typedef struct rr_ranges_args {
 } rr_ranges_args;
 int rr_attend_paged_ranges_workspace(const rr_paged_kv* kv, const rr_ranges_args* a, size_t* bytes);
 int rr_attend_paged_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, void* workspace, size_t bytes, void* stream);
+
+/* ---- Who owns which page ---------------------------------------------------------------------------
+ * The pages of a pool that serves the layers of a model (every layer has its own keys and values, all have one table), counted
+ * on the device.  The state is the caller's:
+ *   page_table  the first held[b] entries of row b are the sequence's pages, in order; the others are -1
+ *   refs        how many entries of the table hold a page; 0: the page is free.  (Entries outside the table that the caller keeps,
+ *               a prefix for later sequences for instance, count too: the caller adds them, and takes them off, when no call is in flight.)
+ *   free_pages  how many pages are free
+ * Pages are handed out in ascending order of their numbers, the lowest free ones first, to the sequences in their order: the
+ * results do not depend on timing.  Ids outside the pool, negative lengths and lengths behind the table's end set RR_STATUS_BAD_INDEX in
+ * *status; an id is left out, a length taken as the nearest that the table holds.
+ * Calls only enqueue work and may be captured.  A pool's calls change its state: order them on one stream (or
+ * by events), with the operators that read the table.  The workspace holds nothing between calls. */
+#define RR_PAGES_MAX_PAGES (1 << 28)
+typedef struct rr_page_pool {
+  int32_t* page_table;       /* [batch, pages_per_seq], rows table_stride apart                   */
+  int32_t* refs;             /* [num_pages]                                                       */
+  int32_t* held;             /* [batch]                                                           */
+  int32_t* free_pages;       /* [1]                                                               */
+  uint32_t* status;          /* [1] RR_STATUS_* bits are OR-ed into it; may be NULL               */
+  int64_t table_stride;
+  int32_t num_pages, page_tokens, batch, pages_per_seq;
+} rr_page_pool;
+int rr_pages_workspace(const rr_page_pool* pool, size_t* bytes);
+
+/* Row b becomes what row parents[b] was before the call, all rows at once: beams that descend from others, samples of one
+ * prompt.  parents[b] == b: the row stays, parents[b] == -1: the sequence has ended and its row is emptied.  A child holds the pages of its
+ * parent's lens tokens together with it, no page is copied.  Writes the new lengths to new_lens (not lens itself). */
+int rr_pages_fork(const rr_page_pool* pool, const int32_t* parents, const int32_t* lens, int32_t* new_lens,
+                  void* workspace, size_t bytes, void* stream);
+
+/* Room for new tokens.  Sequence b keeps its first lens[b] tokens and may be appended to by new_tokens[b] tokens (NULL: by new_each):
+ *   - pages behind the last of these tokens are released (lens 0 and nothing new: the sequence has ended), missing ones are given,
+ *   - a page that will be written and is held by others too becomes the sequence's own: one that begins with some of its tokens is
+ *     copied, as far as they reach, in all `n` caches; if all who hold it are to write to it, the first keeps it.
+ * If there are fewer free pages than the call needs, none is given: rows are only shortened, and RR_STATUS_NO_PAGES is set in *status (read it before
+ * tokens are appended, or see from free_pages that new / page_tokens + 2 pages a sequence are there).
+ * caches: host array of the layers' caches, with the pool's number and size of pages; heads, widths, types and strides are each one's own. */
+int rr_pages_reserve(const rr_page_pool* pool, const int32_t* lens, const int32_t* new_tokens, int32_t new_each,
+                     const rr_paged_kv* caches, int32_t n, void* workspace, size_t bytes, void* stream);
+
+/* The pages in use become the first ones of the pool: of L such pages, the i-th of those numbered L or higher moves to the i-th free page below
+ * L, in the table, in refs and in all caches.  free_pages is counted anew.  new_ids [num_pages] (may be NULL): where each page is after the
+ * call, for ids that the caller keeps outside the table; its own number for pages that did not move. */
+int rr_pages_compact(const rr_page_pool* pool, const rr_paged_kv* caches, int32_t n, int32_t* new_ids, void* workspace,
+                     size_t bytes, void* stream);
+
+/* ---- Verification of drafted tokens -------------------------------------------------------------------
+ * A step reads, for each sequence b, the rows [cu[b], cu[b + 1]): its last known token and n drafts behind it (cu == NULL: one row
+ * a sequence, no drafts).  Row t of `target` is what the target predicts behind token t, row t of `draft` what tokens[t + 1] was drawn from.
+ *   uniform given   target and draft hold probabilities p and q (>= 0; they need not sum to 1 exactly; NaN, infinite and negative
+ *                   entries count as 0).  Draft x behind row t is accepted if p_t(x) > uniform[t] * q_t(x).  Behind the accepted drafts comes one token more:
+ *                   where a draft was rejected in row t, from max(p_t - q_t, 0) (from p_t if that is 0 everywhere), else from p of the last row; it is the first j
+ *                   whose weights up to it sum to more than uniform[cu[b + 1] - 1] times all, -1 if all weights are 0.  draft == NULL: q is 1 at
+ *                   the drafted token.  Products, differences and sums are formed in 64 bits: the random numbers decide, not the rounding.
+ *   uniform NULL    target holds scores (logits).  Draft x is accepted if it is the row's best (the lowest of several; NaN is never best); the token more is
+ *                   the best of the next row.  draft is NULL.
+ * Writes, for each row of a sequence, the token that follows it: the accepted drafts, the token more, then -1; rows behind cu[batch] are left as they
+ * were.  accepted[b] is the number of accepted drafts, new_lens[b] (if given) = lens[b] + accepted[b] + 1, the tokens that stay of a sequence that had
+ * lens[b] before its rows were appended (a sequence without rows: 0 accepted, lens[b]).  A drafted token outside the vocabulary is rejected and sets
+ * RR_STATUS_BAD_INDEX in *status (if given).  Enqueues one kernel; no workspace. */
+typedef struct rr_verify_args {
+  const void* target;        /* [rows, vocab], rows target_stride apart                           */
+  const void* draft;         /* [rows, vocab], rows draft_stride apart, or NULL; a sequence's last row is not read */
+  const int32_t* tokens;     /* [rows]                                                            */
+  const int32_t* cu;         /* [batch + 1] ascending, cu[0] = 0; or NULL                         */
+  const float* uniform;      /* [rows] in [0, 1), or NULL                                         */
+  const int32_t* lens;       /* [batch], with new_lens                                            */
+  int32_t* out;              /* [rows]                                                            */
+  int32_t* accepted;         /* [batch]                                                           */
+  int32_t* new_lens;         /* [batch] or NULL; may be lens itself                               */
+  uint32_t* status;
+  int64_t target_stride, draft_stride;
+  int32_t dtype;             /* RR_BF16 or RR_F32, of target and draft                            */
+  int32_t rows, batch, vocab;
+} rr_verify_args;
+int rr_verify_drafts(const rr_verify_args* a, void* stream);
 
 /* Per-kernel device timing for benchmarks.  Between rr_profile_begin and rr_profile_end
  * every kernel the layer calls launch is bracketed by CUDA events on the caller's stream

@@ -26,6 +26,8 @@ RR_BF16 = 0
 RR_F32 = 1
 RR_STATUS_TIMEOUT = 1
 RR_STATUS_BAD_INDEX = 2
+RR_STATUS_NO_PAGES = 4
+RR_PAGES_MAX_PAGES = 1 << 28
 RR_NUM_COUNTERS = 8
 RR_NUM_KINDS = 12
 COUNTER_NAMES = ("layer_calls", "anchor_rows", "relay_rows", "flagged_rows", "cand_pairs",
@@ -73,6 +75,11 @@ class rr_append_args(C.Structure):
                [(n, C.c_int32) for n in ("tokens", "q_heads", "rot", "interleaved")]
 
 
+class rr_axes_args(C.Structure):
+    _fields_ = [("positions", C.c_void_p), ("axis_of", C.c_void_p), ("axis_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("axes", C.c_int32)]
+
+
 class rr_shared_args(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q", "out", "lens", "cu", "prefix_pages")] + \
                [(n, C.c_int64) for n in ("q_token_stride", "q_head_stride", "out_token_stride", "out_head_stride")] + \
@@ -85,6 +92,17 @@ class rr_ranges_args(C.Structure):
                                          "out_batch_stride", "out_head_stride", "out_token_stride")] + \
                [(n, C.c_int32) for n in ("heads", "route_heads", "n_q", "m", "slots", "causal")] + \
                [("scale", C.c_float)]
+
+
+class rr_page_pool(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("page_table", "refs", "held", "free_pages", "status")] + [("table_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("num_pages", "page_tokens", "batch", "pages_per_seq")]
+
+
+class rr_verify_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("target", "draft", "tokens", "cu", "uniform", "lens", "out", "accepted", "new_lens", "status")] + \
+               [("target_stride", C.c_int64), ("draft_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("dtype", "rows", "batch", "vocab")]
 
 
 class RouteRelayError(RuntimeError):
@@ -154,8 +172,15 @@ def lib() -> C.CDLL:
         L.rr_attend_shared.argtypes = [vp, vp, vp, sz, vp]
         L.rr_attend_paged_ranges_workspace.argtypes = [vp, vp, szp]
         L.rr_attend_paged_ranges.argtypes = [vp, vp, vp, sz, vp]
+        L.rr_kv_append_axes.argtypes = [vp, vp, vp, vp]
+        L.rr_pages_workspace.argtypes = [vp, szp]
+        L.rr_pages_fork.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+        L.rr_pages_reserve.argtypes = [vp, vp, vp, i32, vp, i32, vp, sz, vp]
+        L.rr_pages_compact.argtypes = [vp, vp, i32, vp, vp, sz, vp]
+        L.rr_verify_drafts.argtypes = [vp, vp]
         for name in ("rr_kv_append", "rr_attend_shared_workspace", "rr_attend_shared",
-                     "rr_attend_paged_ranges_workspace", "rr_attend_paged_ranges"):
+                     "rr_attend_paged_ranges_workspace", "rr_attend_paged_ranges", "rr_kv_append_axes", "rr_pages_workspace",
+                     "rr_pages_fork", "rr_pages_reserve", "rr_pages_compact", "rr_verify_drafts"):
             getattr(L, name).restype = C.c_int
         L.rr_profile_begin.argtypes = [vp]
         L.rr_profile_begin.restype = C.c_int
@@ -348,6 +373,10 @@ def rr_kv_append(kv: rr_paged_kv, args: rr_append_args, stream: int) -> None:
     _check(lib().rr_kv_append(C.byref(kv), C.byref(args), stream), "rr_kv_append")
 
 
+def rr_kv_append_axes(kv: rr_paged_kv, args: rr_append_args, axes: rr_axes_args, stream: int) -> None:
+    _check(lib().rr_kv_append_axes(C.byref(kv), C.byref(args), C.byref(axes), stream), "rr_kv_append_axes")
+
+
 def rr_attend_shared_workspace(kv: rr_paged_kv, args: rr_shared_args) -> int:
     n = C.c_size_t()
     _check(lib().rr_attend_shared_workspace(C.byref(kv), C.byref(args), C.byref(n)),
@@ -370,6 +399,32 @@ def rr_attend_paged_ranges(kv: rr_paged_kv, args: rr_ranges_args, workspace: int
                            stream: int) -> None:
     _check(lib().rr_attend_paged_ranges(C.byref(kv), C.byref(args), workspace, nbytes, stream),
            "rr_attend_paged_ranges")
+
+
+def rr_pages_workspace(pool: rr_page_pool) -> int:
+    n = C.c_size_t()
+    _check(lib().rr_pages_workspace(C.byref(pool), C.byref(n)), "rr_pages_workspace")
+    return n.value
+
+
+def rr_pages_fork(pool: rr_page_pool, parents: int, lens: int, new_lens: int, workspace: int, nbytes: int, stream: int) -> None:
+    _check(lib().rr_pages_fork(C.byref(pool), parents, lens, new_lens, workspace, nbytes, stream), "rr_pages_fork")
+
+
+def rr_pages_reserve(pool: rr_page_pool, lens: int, new_tokens, new_each: int, caches, workspace: int, nbytes: int,
+                     stream: int) -> None:
+    """caches: a sequence of rr_paged_kv, one per layer; new_tokens: an address or None."""
+    c = (rr_paged_kv * len(caches))(*caches)
+    _check(lib().rr_pages_reserve(C.byref(pool), lens, new_tokens, new_each, c, len(caches), workspace, nbytes, stream), "rr_pages_reserve")
+
+
+def rr_pages_compact(pool: rr_page_pool, caches, new_ids, workspace: int, nbytes: int, stream: int) -> None:
+    c = (rr_paged_kv * len(caches))(*caches)
+    _check(lib().rr_pages_compact(C.byref(pool), c, len(caches), new_ids, workspace, nbytes, stream), "rr_pages_compact")
+
+
+def rr_verify_drafts(args: rr_verify_args, stream: int) -> None:
+    _check(lib().rr_verify_drafts(C.byref(args), stream), "rr_verify_drafts")
 
 
 def rr_profile_begin(h: int) -> None:

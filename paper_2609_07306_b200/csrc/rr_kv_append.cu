@@ -5,6 +5,8 @@
 // R(p) turns pair j of a head's first `rot` entries by p * inv_freq[j].  In turns that is p * (inv_freq[j] / 2 pi), formed in 64 bits: both
 // roundings are below 2^-53 of it, 2^-22 of a turn at the last position, 2^-32 up to position 2^21.  Its fractional part is exact there; the
 // sine and cosine of what is left (at most half a turn) are FP32's.  All heads of a token share its angles.
+// With positions of several axes (time, height, width of a patch of an image or a video) pair j turns by positions[axis_of[j]][t] * inv_freq[j]; where
+// the token goes in the cache is still counted in tokens.  That build has one load in front of another more (the pair's axis, then its position).
 //
 // The work is one read and one write of every entry: bound by memory for prompts, by latency for a decoding
 // step.  A CTA takes a token; its threads take 16 bytes each (the two halves of eight or four pairs), read them before
@@ -20,11 +22,12 @@ constexpr int NT = 256;
 struct AppendParams {
   rr_paged_kv kv;
   rr_append_args a;
+  rr_axes_args x;                                      // read by the build with axes only
 };
 
 template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Piece { T x[VEC]; };
 
-template <typename T, int VEC>
+template <typename T, int VEC, bool AXES>
 __global__ void __launch_bounds__(NT)
 kv_append_kernel(const __grid_constant__ AppendParams P) {
   __shared__ float s_cos[RR_PAGED_MAX_DH / 2], s_sin[RR_PAGED_MAX_DH / 2];
@@ -65,7 +68,14 @@ kv_append_kernel(const __grid_constant__ AppendParams P) {
   if (pos < 0) return;                                 // padding
   const int half = a.rot / 2, dh = kv.dh;
   for (int j = tid; j < half; j += NT) {
-    const double turns = (double)pos * ((double)a.inv_freq[j] * 0.15915494309189533577);   // 1 / (2 pi)
+    int at_j = pos;
+    if constexpr (AXES) {
+      const int axis = P.x.axis_of ? P.x.axis_of[j] : 0;
+      at_j = 0;                                        // (a pair of no axis is not turned)
+      if (axis >= 0 && axis < P.x.axes) at_j = P.x.positions[axis * P.x.axis_stride + t * P.x.token_stride];
+      else if (kv.status) atomicOr(kv.status, RR_STATUS_BAD_INDEX);
+    }
+    const double turns = (double)at_j * ((double)a.inv_freq[j] * 0.15915494309189533577);  // 1 / (2 pi)
     sincospif(2.0f * (float)(turns - rint(turns)), &s_sin[j], &s_cos[j]);
   }
   __syncthreads();
@@ -137,9 +147,8 @@ bool pieces(const rr_paged_kv& kv, const rr_append_args& a, int vec, size_t byte
   return s % vec == 0 && (p & (bytes - 1)) == 0;
 }
 
-}  // namespace
-
-extern "C" int rr_kv_append(const rr_paged_kv* kv, const rr_append_args* a, void* stream) {
+template <bool AXES>
+int append(const rr_paged_kv* kv, const rr_append_args* a, const rr_axes_args* x, void* stream, const char* who) {
   const int rc = rr_paged_check(kv);
   if (rc != RR_OK) return rc;
   if (!a || !a->k || !a->v || !a->lens) return RR_ERR_INVALID_ARG;
@@ -153,18 +162,32 @@ extern "C" int rr_kv_append(const rr_paged_kv* kv, const rr_append_args* a, void
   const uintptr_t e = kv->dtype == RR_BF16 ? 1 : 3;
   if ((((uintptr_t)a->k | (uintptr_t)a->v | (uintptr_t)a->q | (uintptr_t)(a->q ? a->q_out : nullptr)) & e) ||
       (((uintptr_t)a->lens | (uintptr_t)a->cu | (uintptr_t)a->new_lens | (uintptr_t)a->inv_freq) & 3)) return RR_ERR_INVALID_ARG;
+  if constexpr (AXES) {
+    if (!x || !x->positions || a->rot == 0 || x->axes < 1 || x->axis_stride < 0 || x->token_stride < 0) return RR_ERR_INVALID_ARG;
+    if (((uintptr_t)x->positions | (uintptr_t)x->axis_of) & 3) return RR_ERR_INVALID_ARG;
+  }
   if (a->tokens == 0 && !a->new_lens) return RR_OK;
-  const AppendParams P{*kv, *a};
+  const AppendParams P{*kv, *a, x ? *x : rr_axes_args{}};
   const int grid = a->tokens > 0 ? a->tokens : 1;
   cudaStream_t st = (cudaStream_t)stream;
   if (kv->dtype == RR_BF16) {
-    if (pieces(*kv, *a, 8, 16)) kv_append_kernel<__nv_bfloat16, 8><<<grid, NT, 0, st>>>(P);
-    else kv_append_kernel<__nv_bfloat16, 1><<<grid, NT, 0, st>>>(P);
+    if (pieces(*kv, *a, 8, 16)) kv_append_kernel<__nv_bfloat16, 8, AXES><<<grid, NT, 0, st>>>(P);
+    else kv_append_kernel<__nv_bfloat16, 1, AXES><<<grid, NT, 0, st>>>(P);
   } else {
-    if (pieces(*kv, *a, 4, 16)) kv_append_kernel<float, 4><<<grid, NT, 0, st>>>(P);
-    else kv_append_kernel<float, 1><<<grid, NT, 0, st>>>(P);
+    if (pieces(*kv, *a, 4, 16)) kv_append_kernel<float, 4, AXES><<<grid, NT, 0, st>>>(P);
+    else kv_append_kernel<float, 1, AXES><<<grid, NT, 0, st>>>(P);
   }
   rr_count_launch();
   const cudaError_t err = cudaPeekAtLastError();
-  return err == cudaSuccess ? RR_OK : rr_cuda_fail(err, "rr_kv_append");
+  return err == cudaSuccess ? RR_OK : rr_cuda_fail(err, who);
+}
+
+}  // namespace
+
+extern "C" int rr_kv_append(const rr_paged_kv* kv, const rr_append_args* a, void* stream) {
+  return append<false>(kv, a, nullptr, stream, "rr_kv_append");
+}
+
+extern "C" int rr_kv_append_axes(const rr_paged_kv* kv, const rr_append_args* a, const rr_axes_args* x, void* stream) {
+  return append<true>(kv, a, x, stream, "rr_kv_append_axes");
 }

@@ -10,8 +10,9 @@ import torch
 
 from . import binding as B
 
-# rr_append_args, rr_shared_args and rr_ranges_args as bytes (a call's arguments in one step; 64-bit alignment throughout)
+# rr_append_args, rr_axes_args, rr_shared_args and rr_ranges_args as bytes (a call's arguments in one step; 64-bit alignment throughout)
 _APPEND = struct.Struct("@8P8q4i")
+_AXES = struct.Struct("@2P2qi4x")
 _SHARED = struct.Struct("@5P4q4if4x")
 _RANGES = struct.Struct("@4P6q6if4x")
 
@@ -26,6 +27,11 @@ def inv_freq(rot: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
     """base ** (-2 j / rot) for the rot / 2 pairs, computed in 64 bits."""
     j = torch.arange(0, rot, 2, dtype=torch.float64)
     return (base ** (-j / rot)).float().to(device)
+
+
+def axis_sections(sections, device="cuda") -> torch.Tensor:
+    """axis_of of append for sections of pairs one behind the other: (16, 24, 24) gives the first 16 pairs to axis 0, the next 24 to 1, the last to 2."""
+    return torch.tensor([a for a, n in enumerate(sections) for _ in range(n)], dtype=torch.int32, device=device)
 
 
 class PagedKV:
@@ -113,13 +119,15 @@ class PagedKV:
         if not (rows_apart and (t.shape[1] <= 1 or t.stride(1) == 1)):
             raise ValueError(f"{name} must be contiguous")
 
-    def _run(self, name, args, workspace=None):
+    def _run(self, name, args, workspace=None, more=None):
         """One library call on the current stream of the cache's device."""
         if self._index != torch._C._cuda_getDevice():
             with torch.cuda.device(self.device):
-                return self._run(name, args, workspace)
+                return self._run(name, args, workspace, more)
         stream = torch._C._cuda_getCurrentRawStream(self._index)
-        if workspace is None:
+        if more is not None:
+            rc = getattr(self._lib, name)(self._at, args, more, stream)
+        elif workspace is None:
             rc = getattr(self._lib, name)(self._at, args, stream)
         else:
             n = C.c_size_t()
@@ -134,7 +142,8 @@ class PagedKV:
     def append(self, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, *, cu: torch.Tensor | None = None,
                q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
                inv_freq: torch.Tensor | None = None, interleaved: bool = False,
-               new_lens: torch.Tensor | None = None) -> torch.Tensor | None:
+               new_lens: torch.Tensor | None = None, positions: torch.Tensor | None = None,
+               axis_of: torch.Tensor | None = None) -> torch.Tensor | None:
         """Writes the new tokens' keys and values [tokens, kv_heads, dh] (any token and head strides) into the cache, keys
         rotated by their positions; returns the same tokens' queries [tokens, heads, dh], rotated, if they are given
         (in q_out, which may be q itself; else in a new tensor).
@@ -143,7 +152,10 @@ class PagedKV:
                   and written nowhere; None: one token per sequence
         inv_freq  [rot / 2] float32, rotates the first rot entries of a head: the pairs (j, j + rot / 2), or with
                   interleaved=True (2 j, 2 j + 1); None: nothing is rotated
-        new_lens  [batch] int32: gets lens + new tokens (another tensor than lens)"""
+        new_lens  [batch] int32: gets lens + new tokens (another tensor than lens)
+        positions [axes, tokens] int32 (any strides): the tokens' positions on every axis -- time, height and width of the patches of images
+                  and videos, or one axis of other positions than the places in the cache; None: lens and on
+        axis_of   [rot / 2] int32: the axis that turns each pair (axis_sections makes one); None: there is one axis"""
         if k.dim() != 3:
             raise ValueError("k must be [tokens, kv_heads, dh]")
         n = k.shape[0]
@@ -160,6 +172,11 @@ class PagedKV:
             if inv_freq.dtype is not torch.float32 or inv_freq.get_device() != self._index or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
                 raise ValueError(f"inv_freq must be contiguous float32 [rot / 2] on {self.device}")
             rot = 2 * inv_freq.shape[0]
+        more = None
+        if positions is not None:
+            more = self._axes(positions, axis_of, n, rot)
+        elif axis_of is not None:
+            raise ValueError("axis_of without positions")
         heads, q_strides = 0, (0, 0, 0, 0)
         if q is not None:
             if q.dim() != 3:
@@ -178,12 +195,27 @@ class PagedKV:
             if cu is None:
                 raise ValueError(f"no tokens for {self.batch} sequences")
             k, v, heads = self.k_cache, self.v_cache, 0
-        self._run("rr_kv_append", _APPEND.pack(
+        self._run("rr_kv_append" if more is None else "rr_kv_append_axes", _APPEND.pack(
             k.data_ptr(), v.data_ptr(), q.data_ptr() if heads else 0, q_out.data_ptr() if heads else 0, lens.data_ptr(),
             0 if cu is None else cu.data_ptr(), 0 if new_lens is None else new_lens.data_ptr(),
             0 if rot == 0 else inv_freq.data_ptr(), ks[0], ks[1], vs[0], vs[1], *q_strides, n, heads, rot,
-            1 if interleaved else 0))
+            1 if interleaved else 0), None, more)
         return q_out
+
+    def _axes(self, positions, axis_of, tokens, rot):
+        """rr_axes_args as bytes."""
+        if rot == 0:
+            raise ValueError("positions without inv_freq: nothing is rotated")
+        if positions.dtype is not torch.int32 or positions.get_device() != self._index or positions.dim() != 2 or positions.shape[1] != tokens or \
+                positions.shape[0] < 1:
+            raise ValueError(f"positions must be int32 [axes, {tokens}] on {self.device}, not {positions.dtype} {tuple(positions.shape)} on {positions.device}")
+        if axis_of is not None:
+            self._ints(axis_of, "axis_of", (rot // 2,))
+        elif positions.shape[0] != 1:
+            raise ValueError(f"{positions.shape[0]} axes without axis_of")
+        # (no tokens: no address, and nothing is read)
+        return _AXES.pack(positions.data_ptr() if tokens else self._kv.page_table, 0 if axis_of is None else axis_of.data_ptr(), *positions.stride(),
+                          positions.shape[0])
 
     def attend_shared(self, q: torch.Tensor, lens: torch.Tensor, prefix_tokens: int, scale: float, *,
                       cu: torch.Tensor | None = None, causal: bool = True,
