@@ -523,7 +523,7 @@ int rr_pages_compact(const rr_page_pool* pool, const rr_paged_kv* caches, int32_
  * Writes, for each row of a sequence, the token that follows it: the accepted drafts, the token more, then -1; rows behind cu[batch] are left as they
  * were.  accepted[b] is the number of accepted drafts, new_lens[b] (if given) = lens[b] + accepted[b] + 1, the tokens that stay of a sequence that had
  * lens[b] before its rows were appended (a sequence without rows: 0 accepted, lens[b]).  A drafted token outside the vocabulary is rejected and sets
- * RR_STATUS_BAD_INDEX in *status (if given).  Enqueues one kernel; no workspace. */
+ * RR_STATUS_BAD_INDEX in *status (if given).  No workspace. */
 typedef struct rr_verify_args {
   const void* target;        /* [rows, vocab], rows target_stride apart                           */
   const void* draft;         /* [rows, vocab], rows draft_stride apart, or NULL; a sequence's last row is not read */

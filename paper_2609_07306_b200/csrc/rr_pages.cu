@@ -6,33 +6,38 @@
 //   compact   L pages in use; the i-th of those >= L goes to the i-th free one below L
 //
 // The bookkeeping is a few integers per row and one pass over refs: bound by latency, not by bytes.  It runs in one cluster of eight
-// CTAs, whose hardware barrier separates the steps (a barrier costs less than a launch, and no wait on memory is needed), a warp per row.  Free
-// pages are found by all threads together, 32 pages per thread (eight loads of four refs in flight), in rounds of 262144 pages; counts are
-// exchanged through distributed shared memory.  Which page goes where follows from ranks, never from the order of atomics, which only add to
-// counters.  Copies of pages are a second kernel over all SMs, which reads on the device how many there are; it is launched along with the first
-// and waits for it, for all layers at once.
+// CTAs, whose hardware barrier separates the steps (a barrier costs less than a launch, and no wait on memory is needed).  What is cheap to know
+// about the rows every CTA finds out for itself, a thread per row, instead of a barrier; work on the table's entries is shared by all warps, 256
+// entries of a row at a time.  Free pages are found by all threads together, 32 pages per thread, in rounds of 131072
+// pages; counts are exchanged through distributed shared memory, and the thread that holds a free page looks up which entry its rank belongs to.
+// Which page goes where follows from ranks, never from the order of atomics, which only add to counters.  Copies of pages are a second
+// kernel over all SMs, which reads on the device how many there are; it is launched along with the first and waits for it, for all layers at once.
 #include <cooperative_groups.h>
+#include <utility>
 #include "rr_paged.cuh"
+#include "rr_sm100.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int CL = 8, NT = 1024, NW = NT / 32;
+constexpr int CL = 8, NT = 512, NW = NT / 32;
 constexpr int WARP_PAGES = 1024, CTA_PAGES = NW * WARP_PAGES, ROUND = CL * CTA_PAGES;
+constexpr int COLS = 256;                               // entries of a row that a warp looks at
+constexpr int ROWS_ON_CHIP = 2048;                      // rows whose state fits shared memory
+constexpr int GIVEN = 4096;                             // pages that a CTA hands out at a time
 constexpr int MAX_LAYERS = 64;                          // of one launch of the copy
-constexpr int COPY_NT = 256, COPY_UNITS = 8 * COPY_NT;  // units of one step of a copying CTA
 
 struct Move { int32_t src, dst, tokens; };
 
-// The workspace.  `list`: free pages in rank order (reserve); `stage`: new rows (fork); src, dst and remap of a compaction.
+// The workspace.  `list`: new rows (fork), entries to be replaced or free pages in rank order (reserve), sources, destinations and new ids (compact).
 struct Work {
-  int32_t* moves;                                       // [1] how many
-  int32_t* want;                                        // [batch] the page that a row will go on writing, -1: none
-  int32_t* need;                                        // [batch] new pages of the row; of a fork, the pages that it takes, -1: it stays
-  int32_t* rank;                                        // [batch] rank of the row's first new page
+  int32_t* moves;                                       // [0] how many, [1] pages in use (compact)
+  int32_t* replaced;                                    // [batch] entries to be replaced behind the one that the row goes on writing
   int32_t* list;
+  int32_t* ranked;                                      // [num_pages]
   Move* move;
+  char* rows;                                           // a CTA's state of the rows where it does not fit shared memory
 };
 
 struct PoolParams {
@@ -42,27 +47,44 @@ struct PoolParams {
   const int32_t* lens;
   int32_t* new_lens;
   int32_t* remap;
-  int32_t new_each;
+  int32_t new_each, slots;                              // slots of the table of pages that rows go on writing
 };
 
-size_t list_ints(const rr_page_pool& p) {
-  const size_t rows = (size_t)p.batch * p.pages_per_seq, pages = 3 * (size_t)p.num_pages;
-  return ((rows > pages ? rows : pages) + 3) & ~(size_t)3;
+// A row of a call of reserve: tokens up to column c0 and `part` of it, room up to column c1, pages up to column `held` (of those that stay).
+struct Row {
+  int c0, part, c1, held;
+  int want;                                             // the page that the row goes on writing, -1: none
+  int replaced;                                         // twice the entries to be replaced, + 1 if that one is among them
+  int first;                                            // how many hold it; then the rank of the row's first new page
+};
+struct Slot { int page, n, first; };                    // how many rows go on writing a page, the first of them
+
+size_t up4(size_t n) { return (n + 3) & ~(size_t)3; }
+int slots_of(int batch) {
+  int n = 64;
+  while (n < 2 * batch) n *= 2;
+  return n;
 }
-size_t most_moves(const rr_page_pool& p) { return (size_t)(p.batch > p.num_pages / 2 ? p.batch : p.num_pages / 2) + 1; }
+size_t row_state(const rr_page_pool& p) { return sizeof(Row) * up4(p.batch) + sizeof(Slot) * slots_of(p.batch); }
+size_t list_ints(const rr_page_pool& p) {
+  const size_t rows = (size_t)p.batch * p.pages_per_seq, pages = 2 * (size_t)p.num_pages;
+  return up4(rows > pages ? rows : pages);
+}
+size_t move_bytes(const rr_page_pool& p) {
+  const size_t most = (size_t)(p.batch > p.num_pages / 2 ? p.batch : p.num_pages / 2) + 1;
+  return 4 * up4(3 * most);
+}
 size_t workspace_bytes(const rr_page_pool& p) {
-  const size_t rows = ((size_t)p.batch + 3) & ~(size_t)3;
-  return 64 + 4 * (3 * rows + list_ints(p)) + sizeof(Move) * most_moves(p);
+  return 64 + 4 * (up4(p.batch) + list_ints(p) + up4(p.num_pages)) + move_bytes(p) + (p.batch > ROWS_ON_CHIP ? CL * row_state(p) : 0);
 }
 Work work_of(const rr_page_pool& p, void* ws) {
-  const size_t rows = ((size_t)p.batch + 3) & ~(size_t)3;
   Work w;
   w.moves = (int32_t*)ws;
-  w.want = w.moves + 16;
-  w.need = w.want + rows;
-  w.rank = w.need + rows;
-  w.list = w.rank + rows;
-  w.move = (Move*)(w.list + list_ints(p));
+  w.replaced = w.moves + 16;
+  w.list = w.replaced + up4(p.batch);
+  w.ranked = w.list + list_ints(p);
+  w.move = (Move*)(w.ranked + up4(p.num_pages));
+  w.rows = (char*)w.move + move_bytes(p);
   return w;
 }
 
@@ -72,307 +94,390 @@ __device__ __forceinline__ int held_of(const rr_page_pool& p, int b) { return mi
 // One holder less; 1 if the page is free now.
 __device__ __forceinline__ int release(const rr_page_pool& p, int id) { return atomicSub(p.refs + id, 1) == 1; }
 __device__ __forceinline__ int warp_sum(int x) { return __reduce_add_sync(0xFFFFFFFFu, x); }
+__device__ __forceinline__ int warp_prefix(int x) {     // inclusive
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) { const int y = __shfl_up_sync(0xFFFFFFFFu, x, d); if (lane >= d) x += y; }
+  return x;
+}
+__device__ __forceinline__ void add_free(const rr_page_pool& p, int freed) {
+  freed = warp_sum(freed);
+  if ((threadIdx.x & 31) == 0 && freed) atomicAdd(p.free_pages, freed);
+}
 
-struct Shared { int warp[NW]; int cta[2]; };
+struct Shared { int warp[NW]; int cta[2][CL]; };
 
-// Exclusive prefix of the warps' counts over the cluster, and their sum.  Rounds alternate between the two places, so that a CTA that is a round ahead
-// overwrites nothing that another one still reads.
+// Exclusive prefix of the warps' counts over the cluster, and their sum; all that was written before is visible behind it.  Each CTA leaves its count with
+// all others before the barrier, so that none reads another one's memory behind it (and may end before the others do).  Rounds alternate between
+// two places: a CTA that is a round ahead overwrites nothing that another one still reads.
 __device__ __forceinline__ int2 cluster_prefix(cg::cluster_group& cl, Shared& s, int count, int& round) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (lane == 0) s.warp[warp] = count;
   __syncthreads();
-  int x = s.warp[lane];
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) { const int y = __shfl_up_sync(0xFFFFFFFFu, x, d); if (lane >= d) x += y; }
+  const int x = warp_prefix(lane < NW ? s.warp[lane] : 0);
   const int before = __shfl_sync(0xFFFFFFFFu, x, warp) - count, cta = __shfl_sync(0xFFFFFFFFu, x, 31);
-  int* const place = &s.cta[round & 1];
+  int* const places = s.cta[round & 1];
   ++round;
-  if (threadIdx.x == 0) *place = cta;
+  if (threadIdx.x < CL) *cl.map_shared_rank(places + cl.block_rank(), threadIdx.x) = cta;
   cl.sync();
-  const int theirs = lane < CL ? *cl.map_shared_rank(place, lane) : 0;
+  const int theirs = lane < CL ? places[lane] : 0;
   return make_int2(before + warp_sum(lane < (int)cl.block_rank() ? theirs : 0), warp_sum(theirs));
 }
 
-// Bit 4 i + e: page first + 128 i + 4 lane + e is free.
-__device__ __forceinline__ uint32_t free_bits(const rr_page_pool& p, long long first) {
+// Code is kept short, with loops left as loops where nothing waits for them: a kernel of this kind runs every instruction about once, and what it
+// spent most of its time on was fetching 70 KB of them.
+
+// Bit l of lane k: page first + 32 k + l is free.
+__device__ __noinline__ uint32_t free_bits(const int32_t* refs, int num_pages, long long first) {
   const int lane = threadIdx.x & 31;
-  const bool vec = ((uintptr_t)p.refs & 15) == 0;
+  if (first >= num_pages) return 0;
+  const int n = (int)min((long long)num_pages - first, (long long)WARP_PAGES) - lane;
+  int v[32];
+#pragma unroll
+  for (int k = 0; k < 32; ++k) v[k] = 32 * k < n ? __ldcg(refs + first + lane + 32 * k) : 1;
   uint32_t bits = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const long long g = first + i * 128 + lane * 4;
-    if (vec && g + 4 <= p.num_pages) {
-      const int4 v = __ldcg((const int4*)(p.refs + g));
-      bits |= (uint32_t)((v.x == 0) | (v.y == 0) << 1 | (v.z == 0) << 2 | (v.w == 0) << 3) << (4 * i);
-    } else {
-      for (int e = 0; e < 4; ++e)
-        if (g + e < p.num_pages && __ldcg(p.refs + g + e) == 0) bits |= 1u << (4 * i + e);
-    }
+  for (int k = 0; k < 32; ++k) {
+    const uint32_t word = __ballot_sync(0xFFFFFFFFu, v[k] == 0);
+    if (lane == k) bits = word;
   }
   return bits;
 }
 
-// f(page, rank, is free) for the pages of this thread in a round, rank = free pages before it, `before` of them before this warp's.
-template <class F>
-__device__ __forceinline__ void each_page(uint32_t bits, int before, long long first, F&& f) {
-  const int lane = threadIdx.x & 31;
-  uint32_t lo = 0, hi = 0;                              // a byte per i: free pages of the lanes up to this one (at most 128)
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    lo |= (uint32_t)__popc(bits >> (4 * i) & 15) << (8 * i);
-    hi |= (uint32_t)__popc(bits >> (16 + 4 * i) & 15) << (8 * i);
-  }
-  const uint32_t own_lo = lo, own_hi = hi;
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    const uint32_t a = __shfl_up_sync(0xFFFFFFFFu, lo, d), b = __shfl_up_sync(0xFFFFFFFFu, hi, d);
-    if (lane >= d) lo += a, hi += b;
-  }
-  const uint32_t all_lo = __shfl_sync(0xFFFFFFFFu, lo, 31), all_hi = __shfl_sync(0xFFFFFFFFu, hi, 31);
-  lo -= own_lo, hi -= own_hi;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t mine = i < 4 ? lo : hi, all = i < 4 ? all_lo : all_hi;
-    int rank = before + (int)(mine >> (8 * (i & 3)) & 255);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool is_free = bits >> (4 * i + e) & 1;
-      f(first + i * 128 + lane * 4 + e, rank, is_free);
-      rank += is_free;
-    }
-    before += (int)(all >> (8 * (i & 3)) & 255);
-  }
-}
-
-// The `need` lowest free pages into w.list (visible after the next barrier); how many were found, at least `need` if there are as many.
-__device__ __forceinline__ int find_free(cg::cluster_group& cl, const PoolParams& P, Shared& s, int need, int& round) {
-  int found = 0;
-  for (long long at = 0; at < P.p.num_pages && found < need; at += ROUND) {
-    const long long first = at + (long long)cl.block_rank() * CTA_PAGES + (threadIdx.x >> 5) * WARP_PAGES;
-    const uint32_t bits = free_bits(P.p, first);
-    const int2 n = cluster_prefix(cl, s, warp_sum(__popc(bits)), round);
-    if (found + n.x < need)
-      each_page(bits, found + n.x, first, [&](long long page, int rank, bool is_free) { if (is_free && rank < need) P.w.list[rank] = (int32_t)page; });
-    found += n.y;
-  }
-  return found;
+__device__ __forceinline__ long long first_page(cg::cluster_group& cl, long long round) {
+  return round + (long long)cl.block_rank() * CTA_PAGES + (threadIdx.x >> 5) * WARP_PAGES;
 }
 
 // ---- fork -------------------------------------------------------------------------------------------------------
 // A row is compared with its parent's: beams differ from one another in their last pages only, and equal entries cost two loads.  New entries
 // are staged, as a parent's row may be rewritten in the same call.
-__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT, 1)
+constexpr int FORK_NT = 1024;                           // (a warp per row for 256 rows)
+struct Heir { int parent, held, takes; };               // pages that the row held and takes (-1: it stays)
+
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(FORK_NT, 1)
 fork_kernel(const __grid_constant__ PoolParams P) {
+  extern __shared__ char on_chip[];
   cg::cluster_group cl = cg::this_cluster();
   const rr_page_pool& p = P.p;
-  const int lane = threadIdx.x & 31, warp = cl.block_rank() * NW + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, rank = cl.block_rank(), warp = (threadIdx.x >> 5) * CL + rank;
+  Heir* const heirs = p.batch > ROWS_ON_CHIP ? (Heir*)(P.w.rows + rank * (sizeof(Heir) * ((p.batch + 3) & ~3))) : (Heir*)on_chip;
   rr_pdl_wait();
   rr_pdl_trigger();
-  int freed = 0;
-  for (int b = warp; b < p.batch; b += CL * NW) {
-    int parent = P.arg[b];
-    if (parent < -1 || parent >= p.batch) {
-      if (lane == 0) report(p, RR_STATUS_BAD_INDEX);
-      parent = b;
+  for (int b = threadIdx.x; b < p.batch; b += FORK_NT) {     // in every CTA
+    const bool tell = rank == 0;
+    Heir h{P.arg[b], held_of(p, b), -1};
+    if (h.parent < -1 || h.parent >= p.batch) {
+      if (tell) report(p, RR_STATUS_BAD_INDEX);
+      h.parent = b;
     }
-    const int len = parent < 0 ? 0 : P.lens[parent];
-    if (lane == 0) {
+    const int len = h.parent < 0 ? 0 : P.lens[h.parent];
+    if (h.parent != b) h.takes = h.parent < 0 ? 0 : (int)min((unsigned)held_of(p, h.parent), ((unsigned)max(len, 0) + p.page_tokens - 1) / p.page_tokens);
+    if (tell) {
       if (len < 0) report(p, RR_STATUS_BAD_INDEX);
       P.new_lens[b] = max(len, 0);
     }
-    if (parent == b) {
-      if (lane == 0) P.w.need[b] = -1;
-      continue;
-    }
-    const int held = held_of(p, b);
-    int takes = 0;                                      // pages with tokens of the parent
-    if (parent >= 0) takes = (int)min((long long)held_of(p, parent), ((long long)max(len, 0) + p.page_tokens - 1) / p.page_tokens);
-    if (lane == 0) P.w.need[b] = takes;
+    heirs[b] = h;
+  }
+  __syncthreads();
+  const int parts = (p.pages_per_seq + COLS - 1) / COLS, units = p.batch * parts, each = (units + CL * (FORK_NT / 32) - 1) / (CL * (FORK_NT / 32));
+  int freed = 0;
+  for (int u = warp * each; u < min((warp + 1) * each, units); ++u) {
+    const int b = u / parts, c0 = (u - b * parts) * COLS;
+    const Heir h = heirs[b];
+    if (h.takes < 0) continue;
     const int32_t* const mine = p.page_table + b * p.table_stride;
-    const int32_t* const theirs = p.page_table + parent * p.table_stride;
+    const int32_t* const theirs = p.page_table + h.parent * p.table_stride;
     int32_t* const stage = P.w.list + (size_t)b * p.pages_per_seq;
-    for (int c = lane; c < max(held, takes); c += 32) {
-      const int was = c < held ? mine[c] : -1, is = c < takes ? theirs[c] : -1;
+    const int end = min(max(h.held, h.takes), c0 + COLS);
+#pragma unroll 2
+    for (int c = c0 + lane; c < end; c += 32) {
+      const int was = c < h.held ? mine[c] : -1, is = c < h.takes ? theirs[c] : -1;
       stage[c] = is;
       if (was == is) continue;
       if (in_pool(p, is)) freed -= atomicAdd(p.refs + is, 1) == 0;      // (one row may let go of a page before another takes it)
-      else if (c < takes) report(p, RR_STATUS_BAD_INDEX);
+      else if (c < h.takes) report(p, RR_STATUS_BAD_INDEX);
       if (in_pool(p, was)) freed += release(p, was);
-      else if (c < held) report(p, RR_STATUS_BAD_INDEX);
+      else if (c < h.held) report(p, RR_STATUS_BAD_INDEX);
     }
   }
-  freed = warp_sum(freed);
-  if (lane == 0 && freed) atomicAdd(p.free_pages, freed);
   cl.sync();
-  for (int b = warp; b < p.batch; b += CL * NW) {
-    const int takes = P.w.need[b];
-    if (takes < 0) continue;
-    const int held = held_of(p, b);
+  for (int u = warp * each; u < min((warp + 1) * each, units); ++u) {
+    const int b = u / parts, c0 = (u - b * parts) * COLS;
+    const Heir h = heirs[b];
+    if (h.takes < 0) continue;
     int32_t* const mine = p.page_table + b * p.table_stride;
     const int32_t* const stage = P.w.list + (size_t)b * p.pages_per_seq;
-    for (int c = lane; c < max(held, takes); c += 32)
-      if (const int is = stage[c]; mine[c] != is) mine[c] = is;
-    __syncwarp();                                       // every lane has read held
-    if (lane == 0) p.held[b] = takes;
+#pragma unroll 2
+    for (int c = c0 + lane; c < min(max(h.held, h.takes), c0 + COLS); c += 32) mine[c] = stage[c];
+    if (c0 == 0 && lane == 0) p.held[b] = h.takes;
   }
+  add_free(p, freed);
 }
 
 // ---- reserve ----------------------------------------------------------------------------------------------------
-struct Room { int c0, part, c1, held; bool writes; };
-
-// Columns of row b: tokens up to column c0 and `part` of it, room up to column c1.
-__device__ __forceinline__ Room room_of(const PoolParams& P, int b, bool tell) {
+__device__ __forceinline__ Row row_of(const PoolParams& P, int b, int& held, bool tell) {
   const rr_page_pool& p = P.p;
   const long long cap = (long long)p.page_tokens * p.pages_per_seq;
-  long long len = P.lens[b], more = P.arg ? P.arg[b] : P.new_each;
-  const bool bad = len < 0 || more < 0 || len + more > cap;
-  if (bad && tell) report(p, RR_STATUS_BAD_INDEX);
-  len = min(max(len, 0LL), cap);
-  more = min(max(more, 0LL), cap - len);
-  Room r;
-  r.c0 = (int)(len / p.page_tokens);
-  r.part = (int)(len - (long long)r.c0 * p.page_tokens);
-  r.c1 = (int)((len + more + p.page_tokens - 1) / p.page_tokens);
-  r.held = held_of(p, b);
-  r.writes = more > 0;
+  int len = P.lens[b], more = P.arg ? P.arg[b] : P.new_each;
+  held = held_of(p, b);
+  const bool bad = len < 0 || more < 0 || (long long)len + more > cap;
+  if (bad) {
+    if (tell) report(p, RR_STATUS_BAD_INDEX);
+    len = (int)min((long long)max(len, 0), cap);
+    more = (int)min((long long)max(more, 0), cap - len);
+  }
+  Row r;
+  const unsigned page = p.page_tokens, upto = (unsigned)len + (unsigned)more;
+  r.c0 = (int)((unsigned)len / page);
+  r.part = (int)((unsigned)len - (unsigned)r.c0 * page);
+  r.c1 = (int)(upto / page);
+  r.c1 += (unsigned)r.c1 * page != upto;
+  r.held = min(held, r.c1);
+  r.want = more > 0 && r.part > 0 && r.c0 < r.held ? 0 : -1;
+  r.replaced = r.first = 0;
   return r;
 }
 
-// An entry that gets a new page, until it has it: the page that it held, or that it held none of the pool.
-__device__ __forceinline__ int marked(int id) { return -2 - id; }
-constexpr int MARKED_NONE = INT32_MIN;
+// A row's entries to be replaced behind the one that it goes on writing.
+__device__ __forceinline__ int32_t* replaced_of(const PoolParams& P, int b) { return P.w.list + (size_t)b * P.p.pages_per_seq; }
 
-// Whether row b copies the page `want` that it goes on writing: others hold it too, and not all who hold it write it with b as the first of them.
-__device__ __forceinline__ bool copies(const PoolParams& P, int b, int want) {
-  const int lane = threadIdx.x & 31, holders = __ldcg(P.p.refs + want);
-  if (holders <= 1) return false;
-  int n = 0, before = 0;
-  for (int o = lane; o < P.p.batch; o += 32)
-    if (__ldcg(P.w.want + o) == want) ++n, before += o < b;
-  return warp_sum(before) > 0 || warp_sum(n) != holders;
+// The rows' new pages in the order of their ranks: for entries to be replaced, then for missing ones.
+struct Hand {
+  const PoolParams& P;
+  const Row* rows;
+  int b = 0, freed = 0;                                 // the row of the last page, pages come free
+  __device__ __forceinline__ void give(int page, int rank) {
+    const rr_page_pool& p = P.p;
+    if (rank < rows[b].first || (b + 1 < p.batch && rank >= rows[b + 1].first)) {
+      int lo = 0, n = p.batch;                          // the last row that begins at this rank or before it
+      while (n > 1) {
+        const int half = n / 2;
+        if (rows[lo + half].first <= rank) lo += half, n -= half;
+        else n = half;
+      }
+      b = lo;
+    }
+    const Row& r = rows[b];
+    const int m = rank - r.first, n = r.replaced >> 1;
+    int32_t* const row = p.page_table + b * p.table_stride;
+    int c = r.held + m - n;
+    if (m == 0 && (r.replaced & 1)) {                   // the page that the row goes on writing
+      c = r.c0;
+      freed += release(p, r.want);
+      P.w.move[atomicAdd(P.w.moves, 1)] = Move{r.want, page, r.part};
+    } else if (m < n) {
+      c = __ldcg(replaced_of(P, b) + m - (r.replaced & 1));
+      const int old = __ldcg(row + c);
+      if (in_pool(p, old)) freed += release(p, old);
+    }
+    row[c] = page;
+    p.refs[page] = 1;
+    --freed;
+  }
+};
+
+__device__ __forceinline__ Slot* slot_of(Slot* slots, int mask, int page, bool add) {
+  unsigned h = (unsigned)page * 2654435761u >> 7;
+  while (true) {                                        // (half of the slots at most are taken)
+    Slot* const t = slots + (h & mask);
+    const int k = add ? atomicCAS(&t->page, -1, page) : *(volatile int*)&t->page;
+    if (k == page || (add && k == -1)) return t;
+    ++h;
+  }
 }
+
+constexpr int LOOK = 8;                                 // entries of a row that a lane loads together
+constexpr int NEAR = 4;                                 // entries behind a row's tokens that its thread looks at itself
 
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT, 1)
 reserve_kernel(const __grid_constant__ PoolParams P) {
+  extern __shared__ char on_chip[];
   __shared__ Shared s;
-  __shared__ int s_warp[NW];
+  __shared__ int s_scan[NW];
   cg::cluster_group cl = cg::this_cluster();
   const rr_page_pool& p = P.p;
-  const int lane = threadIdx.x & 31, my_warp = threadIdx.x >> 5, warp = cl.block_rank() * NW + my_warp;
+  const int lane = threadIdx.x & 31, my_warp = threadIdx.x >> 5, rank = cl.block_rank(), warp = my_warp * CL + rank;
+  int32_t* const given = (int32_t*)on_chip;             // [GIVEN] the CTA's free pages by their rank
+  char* const state = p.batch > ROWS_ON_CHIP ? P.w.rows + rank * (sizeof(Row) * ((p.batch + 3) & ~3) + sizeof(Slot) * P.slots) : on_chip + GIVEN * 4;
+  Row* const rows = (Row*)state;
+  Slot* const slots = (Slot*)(state + sizeof(Row) * ((p.batch + 3) & ~3));
+  auto started = cl.barrier_arrive();
   rr_pdl_wait();
   rr_pdl_trigger();
-  int freed = 0, round = 0;
+  int round = 0, freed = 0;
   if (warp == 0 && lane == 0) *P.w.moves = 0;
-  // 1. pages behind the room are released; which page each row goes on writing
-  for (int b = warp; b < p.batch; b += CL * NW) {
-    const Room r = room_of(P, b, lane == 0);
-    int32_t* const row = p.page_table + b * p.table_stride;
-    for (int c = r.c1 + lane; c < r.held; c += 32) {
-      const int id = row[c];
-      if (in_pool(p, id)) freed += release(p, id);
-      else report(p, RR_STATUS_BAD_INDEX);
-      row[c] = -1;
+  // 1. the rows, in every CTA, and what the table holds where they will be written; pages behind a row's room are released
+  int ids[NEAR];                                        // of the thread's first row
+  bool longest = false, shorter = false;
+  for (int i = threadIdx.x; i < P.slots; i += NT) slots[i] = Slot{-1, 0, INT32_MAX};
+  for (int b = threadIdx.x; b < p.batch; b += NT) {
+    int held;
+    Row r = row_of(P, b, held, rank == 0);
+    const int32_t* const row = p.page_table + b * p.table_stride;
+    const int c = r.c0 + (r.part > 0);
+    if (r.want == 0) r.want = __ldcg(row + r.c0);
+    if (b == threadIdx.x) {
+#pragma unroll
+      for (int i = 0; i < NEAR; ++i) ids[i] = c + i < r.held ? __ldcg(row + c + i) : -1;
     }
-    __syncwarp();                                       // every lane has read held
-    if (lane == 0) {
-      int want = -1;
-      if (r.writes && r.part > 0 && r.c0 < min(r.held, r.c1)) {
-        want = row[r.c0];
-        if (!in_pool(p, want)) want = -1, report(p, RR_STATUS_BAD_INDEX);
+    if (r.want != -1 && !in_pool(p, r.want)) {
+      r.want = -1;
+      if (rank == 0) report(p, RR_STATUS_BAD_INDEX);
+    }
+    longest |= r.held - c > NEAR;
+    shorter |= held > r.c1;
+    rows[b] = r;
+  }
+  longest = __syncthreads_or(longest);
+  cl.barrier_wait(std::move(started));                  // all CTAs run: their memory may be written from here on
+  if (__syncthreads_or(shorter)) {                      // (the same in all CTAs)
+    const int parts = (p.pages_per_seq + COLS - 1) / COLS;
+    const int each = (p.batch * parts + CL * NW - 1) / (CL * NW);       // (neighbours by one warp: rows that end tend to alternate with such that stay)
+    for (int u = warp * each; u < min((warp + 1) * each, p.batch * parts); ++u) {
+      const int b = u / parts, c0 = (u - b * parts) * COLS, held = held_of(p, b);
+      int32_t* const row = p.page_table + b * p.table_stride;
+#pragma unroll 2
+      for (int c = max(rows[b].c1, c0) + lane; c < min(held, c0 + COLS); c += 32) {
+        const int id = row[c];
+        row[c] = -1;
+        if (in_pool(p, id)) freed += release(p, id);
+        else report(p, RR_STATUS_BAD_INDEX);
       }
-      P.w.want[b] = want;
-      if (r.c1 < r.held) p.held[b] = r.c1;
     }
-    __syncwarp();
+    cl.sync();
   }
-  cl.sync();
-  // 2. how many pages each row needs: a copy of the page that it goes on writing, its own ones for pages behind that others hold too, missing ones.
-  // Counted now, while nothing changes; what is to be replaced is marked in the table.
-  for (int b = warp; b < p.batch; b += CL * NW) {
-    const Room r = room_of(P, b, false);
-    const int want = __ldcg(P.w.want + b);
-    int32_t* const row = p.page_table + b * p.table_stride;
-    int need = max(r.c1 - r.held, 0);
-    if (want >= 0) {
-      const bool copied = copies(P, b, want);
-      need += copied;
-      if (lane == 0 && copied) row[r.c0] = marked(want);
-    }
-    for (int c0 = r.c0 + (r.part > 0); c0 < r.held; c0 += 32) {
-      const int c = c0 + lane, id = c < r.held ? row[c] : 0;
-      const bool bad = c < r.held && !in_pool(p, id);
-      const bool fresh = bad || (c < r.held && __ldcg(p.refs + id) > 1);
-      if (bad) report(p, RR_STATUS_BAD_INDEX);
-      if (fresh) row[c] = bad ? MARKED_NONE : marked(id);
-      need += __popc(__ballot_sync(0xFFFFFFFFu, fresh));
-    }
-    if (lane == 0) P.w.need[b] = need;
+  // 2. nothing changes now.  The free pages of this thread; the rows' entries to be replaced: a page that others hold too and that not all who hold it
+  // go on writing with this row as the first of them, and pages behind it that others hold
+  int near_refs[NEAR];
+  if (threadIdx.x < p.batch) {
+#pragma unroll
+    for (int i = 0; i < NEAR; ++i) near_refs[i] = in_pool(p, ids[i]) ? __ldcg(p.refs + ids[i]) : 2;
   }
-  cl.sync();
-  // 3. each row's first rank: every CTA adds up all rows and keeps those of its own warps
+  uint32_t bits = free_bits(p.refs, p.num_pages, first_page(cl, 0));
+  for (int b = threadIdx.x; b < p.batch; b += NT) {
+    const int want = rows[b].want;
+    if (want < 0) continue;
+    const int holders = __ldcg(p.refs + want);
+    rows[b].first = holders;
+    if (holders > 1) {
+      Slot* const t = slot_of(slots, P.slots - 1, want, true);
+      atomicAdd(&t->n, 1);
+      atomicMin(&t->first, b);
+    }
+  }
+  __syncthreads();
+  if (longest) {                                        // (a warp per row, each row once in the cluster)
+    const int each = (p.batch + CL * NW - 1) / (CL * NW);
+    for (int b = warp * each; b < min((warp + 1) * each, p.batch); ++b) {
+      const Row r = rows[b];
+      const int32_t* const row = p.page_table + b * p.table_stride;
+      int n = 0;
+      for (int at = r.c0 + (r.part > 0); at < r.held; at += 32 * LOOK) {
+        int id[LOOK], n_refs[LOOK];
+#pragma unroll
+        for (int i = 0; i < LOOK; ++i) { const int c = at + 32 * i + lane; id[i] = c < r.held ? __ldcg(row + c) : -1; }
+#pragma unroll
+        for (int i = 0; i < LOOK; ++i) n_refs[i] = in_pool(p, id[i]) ? __ldcg(p.refs + id[i]) : 2;
+#pragma unroll
+        for (int i = 0; i < LOOK; ++i) {
+          const int c = at + 32 * i + lane;
+          const unsigned fresh = __ballot_sync(0xFFFFFFFFu, c < r.held && n_refs[i] > 1);
+          if (c < r.held && !in_pool(p, id[i])) report(p, RR_STATUS_BAD_INDEX);
+          if (fresh >> lane & 1) replaced_of(P, b)[n + __popc(fresh & ((1u << lane) - 1))] = c;
+          n += __popc(fresh);
+        }
+      }
+      if (lane == 0) P.w.replaced[b] = n;
+    }
+    cl.sync();
+  }
   int total = 0;
   for (int at = 0; at < p.batch; at += NT) {
-    const int b = at + threadIdx.x, need = b < p.batch ? __ldcg(P.w.need + b) : 0;
-    int x = need;
+    const int b = at + threadIdx.x;
+    int need = 0, replaced = 0, copied = 0;
+    if (b < p.batch) {
+      const Row r = rows[b];
+      int32_t* const list = replaced_of(P, b);
+      const bool mine = b % CL == rank;                 // whoever writes what all CTAs find out
+      if (r.want >= 0 && r.first > 1) {
+        const Slot* const t = slot_of(slots, P.slots - 1, r.want, false);
+        copied = *(volatile int*)&t->n != r.first || *(volatile int*)&t->first != b;
+      }
+      if (longest) {
+        replaced = __ldcg(P.w.replaced + b);
+      } else {
+        const int c = r.c0 + (r.part > 0);
+        if (at > 0) {
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) { const int y = __shfl_up_sync(0xFFFFFFFFu, x, d); if (lane >= d) x += y; }
-    if (lane == 31) s_warp[my_warp] = x;
+          for (int i = 0; i < NEAR; ++i) ids[i] = c + i < r.held ? __ldcg(p.page_table + b * p.table_stride + c + i) : -1;
+#pragma unroll
+          for (int i = 0; i < NEAR; ++i) near_refs[i] = in_pool(p, ids[i]) ? __ldcg(p.refs + ids[i]) : 2;
+        }
+#pragma unroll
+        for (int i = 0; i < NEAR; ++i) {
+          if (c + i >= r.held || near_refs[i] <= 1) continue;
+          if (mine && !in_pool(p, ids[i])) report(p, RR_STATUS_BAD_INDEX);
+          if (mine) list[replaced] = c + i;
+          ++replaced;
+        }
+      }
+      replaced += copied;
+      need = replaced + r.c1 - r.held;
+    }
+    const int x = warp_prefix(need);
+    if (lane == 31) s_scan[my_warp] = x;
     __syncthreads();
-    int before = warp_sum(lane < my_warp ? s_warp[lane] : 0);
-    const int all = warp_sum(s_warp[lane]);
+    const int before = warp_sum(lane < my_warp ? s_scan[lane] : 0), all = warp_sum(lane < NW ? s_scan[lane] : 0);
     __syncthreads();
-    if (b < p.batch && b % (CL * NW) / NW == (int)cl.block_rank()) P.w.rank[b] = total + before + x - need;
+    if (b < p.batch) {
+      rows[b].replaced = 2 * replaced + copied;
+      rows[b].first = total + before + x - need;
+    }
     total += all;
   }
-  const int found = total > 0 ? find_free(cl, P, s, total, round) : 0;
-  cl.sync();
-  // 4. the pages are handed out
-  const bool enough = found >= total;
-  if (!enough && warp == 0 && lane == 0) report(p, RR_STATUS_NO_PAGES);
-  for (int b = warp; b < p.batch; b += CL * NW) {
-    const Room r = room_of(P, b, false);
-    const int want = __ldcg(P.w.want + b);
-    int32_t* const row = p.page_table + b * p.table_stride;
-    const int32_t* next = P.w.list + P.w.rank[b];
-    if (want >= 0 && row[r.c0] == marked(want)) {
-      __syncwarp();
-      if (lane == 0) {
-        row[r.c0] = enough ? __ldcg(next) : want;
-        if (enough) {
-          p.refs[__ldcg(next)] = 1;
-          freed += release(p, want) - 1;
-          P.w.move[atomicAdd(P.w.moves, 1)] = Move{want, __ldcg(next), r.part};
-        }
+  // 3. free pages get their ranks, and each goes to the entry of its rank.  Free pages lie together, often all in one warp, so they are shared by the CTA's
+  // threads; many, or those of a pool of several rounds (where a page may come free while the last rounds are still looked at), by the cluster's.
+  int freed_now = 0;
+  bool enough = true;
+  if (total > 0) {
+    const bool near = p.num_pages <= ROUND && total <= GIVEN;
+    int found = 0, from = 0;
+    for (long long at = 0; at < p.num_pages && found < total; at += ROUND) {
+      const long long first = first_page(cl, at);
+      if (at > 0) bits = free_bits(p.refs, p.num_pages, first);
+      const int2 n = cluster_prefix(cl, s, warp_sum(__popc(bits)), round);
+      if (near) {
+        if (my_warp == 0) s_scan[0] = n.x;
+        if (my_warp == NW - 1) s_scan[1] = n.x + warp_sum(__popc(bits));
+        __syncthreads();
+        from = s_scan[0];
       }
-      ++next;
+      int32_t* const out = near ? given - from : P.w.ranked;
+      if (found + n.x < total) {
+        int r = found + n.x + warp_prefix(__popc(bits)) - __popc(bits);
+        for (uint32_t w = bits; w && r < total; w &= w - 1) out[r++] = (int32_t)first + 32 * lane + __ffs(w) - 1;
+      }
+      found += n.y;
     }
-    for (int c0 = r.c0 + (r.part > 0); c0 < r.held; c0 += 32) {
-      const int c = c0 + lane, e = c < r.held ? row[c] : 0;
-      const unsigned fresh = __ballot_sync(0xFFFFFFFFu, e < 0);
-      if (e < 0) {
-        const int id = enough ? __ldcg(next + __popc(fresh & ((1u << lane) - 1))) : -1;
-        row[c] = enough ? id : e == MARKED_NONE ? -1 : -2 - e;
-        if (enough) {
-          p.refs[id] = 1;
-          freed += (e == MARKED_NONE ? 0 : release(p, -2 - e)) - 1;
-        }
-      }
-      next += __popc(fresh);
-    }
-    if (enough && r.c1 > r.held) {
-      for (int c = r.held + lane; c < r.c1; c += 32) {
-        const int id = __ldcg(next + c - r.held);
-        row[c] = id;
-        p.refs[id] = 1;
-        --freed;
-      }
-      __syncwarp();
-      if (lane == 0) p.held[b] = r.c1;
+    enough = found >= total;
+    if (near) __syncthreads();
+    else cl.sync();
+    if (enough) {
+      const volatile int32_t* const list = near ? given - from : P.w.ranked;
+      const int end = near ? min(s_scan[1], total) : total;
+      Hand hand{P, rows};
+#pragma unroll 1
+      for (int r = near ? from + (int)threadIdx.x : warp * 32 + lane; r < end; r += near ? NT : CL * NT) hand.give(list[r], r);
+      freed_now = hand.freed;
     }
   }
-  freed = warp_sum(freed);
-  if (lane == 0 && freed) atomicAdd(p.free_pages, freed);
-  cl.sync();                                            // no CTA leaves while another one may read its counts
+  if (!enough && warp == 0 && lane == 0) report(p, RR_STATUS_NO_PAGES);
+  for (int b = threadIdx.x; b < p.batch; b += NT) {
+    if (b % CL != rank) continue;
+    const int held = enough ? rows[b].c1 : rows[b].held;
+    if (__ldcg(p.held + b) != held) p.held[b] = held;
+  }
+  add_free(p, freed + freed_now);
 }
 
 // ---- compact ----------------------------------------------------------------------------------------------------
@@ -381,39 +486,48 @@ compact_kernel(const __grid_constant__ PoolParams P) {
   __shared__ Shared s;
   cg::cluster_group cl = cg::this_cluster();
   const rr_page_pool& p = P.p;
-  const int my_warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
   rr_pdl_wait();
   rr_pdl_trigger();
+  const bool one_round = p.num_pages <= ROUND;
+  cl.sync();                                            // all CTAs run: their memory may be written from here on
   int round = 0, free_all = 0;
   uint32_t bits = 0;
+  int2 n = make_int2(0, 0);
   for (long long at = 0; at < p.num_pages; at += ROUND) {
-    bits = free_bits(p, at + (long long)cl.block_rank() * CTA_PAGES + my_warp * WARP_PAGES);
-    free_all += cluster_prefix(cl, s, warp_sum(__popc(bits)), round).y;
+    bits = free_bits(p.refs, p.num_pages, first_page(cl, at));
+    n = cluster_prefix(cl, s, warp_sum(__popc(bits)), round);
+    free_all += n.y;
   }
   const int live = p.num_pages - free_all;
   // Free pages below `live` by their rank, pages in use from there on by their rank among all in use: the last as many of them as there are free ones below.
   int32_t* const dst = P.w.list;
   int32_t* const src = P.w.list + p.num_pages;
-  int before = 0, moves = 0;
+  int before = 0, low = 0;
   for (long long at = 0; at < p.num_pages; at += ROUND) {
-    const long long first = at + (long long)cl.block_rank() * CTA_PAGES + my_warp * WARP_PAGES;
-    if (p.num_pages > ROUND) bits = free_bits(p, first);
-    int low = 0;
-    const int2 n = cluster_prefix(cl, s, warp_sum(__popc(bits)), round);
-    each_page(bits, before + n.x, first, [&](long long page, int rank, bool is_free) {
-      if (page >= p.num_pages) return;
-      if (is_free && page < live) dst[rank] = (int32_t)page, ++low;
-      if (!is_free && page >= live) src[page - rank] = (int32_t)page;
-      else P.remap[page] = (int32_t)page;
-    });
-    moves += cluster_prefix(cl, s, warp_sum(low), round).y;
+    const long long first = first_page(cl, at);
+    if (!one_round) {
+      bits = free_bits(p.refs, p.num_pages, first);
+      n = cluster_prefix(cl, s, warp_sum(__popc(bits)), round);
+    }
+    const int upto = before + n.x + warp_prefix(__popc(bits)) - __popc(bits);
+#pragma unroll 1
+    for (int k = 0; k < 32 && first + 32 * k < p.num_pages; ++k) {
+      const uint32_t word = __shfl_sync(0xFFFFFFFFu, bits, k);
+      const int page = (int)first + 32 * k + lane, rank = __shfl_sync(0xFFFFFFFFu, upto, k) + __popc(word & ((1u << lane) - 1));
+      const bool is_free = word >> lane & 1;
+      if (page >= p.num_pages) continue;
+      if (is_free && page < live) dst[rank] = page, ++low;
+      if (!is_free && page >= live) src[page - rank] = page;
+      else P.remap[page] = page;
+    }
     before += n.y;
   }
-  cl.sync();
+  const int moves = cluster_prefix(cl, s, warp_sum(low), round).y;
   for (int i = cl.block_rank() * NT + threadIdx.x; i < moves; i += CL * NT) {
     const int from = __ldcg(src + live - moves + i), to = __ldcg(dst + i);
     P.remap[from] = to;
-    p.refs[to] = p.refs[from];
+    p.refs[to] = __ldcg(p.refs + from);
     p.refs[from] = 0;
     P.w.move[i] = Move{from, to, p.page_tokens};
   }
@@ -422,77 +536,168 @@ compact_kernel(const __grid_constant__ PoolParams P) {
     P.w.moves[1] = live;
     *p.free_pages = free_all;
   }
-  cl.sync();
 }
 
 // ---- copies -----------------------------------------------------------------------------------------------------
-// A page of one layer's keys or values as units of 16 bytes (or of an entry, where strides or addresses do not split): the outer of heads and tokens,
-// the inner one, the units of a head's entries.  What lies side by side is merged.
+// A page of one layer's keys or values: the outer of heads and tokens, the inner one, the entries of a head.
 struct Layer {
   char* base[2];                                        // keys, values
   int64_t page, outer, mid;                             // bytes
-  int32_t heads, row;                                   // units of a head's entries
-  int8_t unit, token_major, joined;                     // joined: the inner of heads and tokens lies side by side
+  int32_t heads, row;                                   // bytes of a head's entries
+  int8_t unit, token_major, joined;                     // unit: bytes that addresses and strides split into; joined: the inner of heads and tokens lies side by side
 };
 
 struct CopyParams {
   Work w;
   int32_t page_tokens, layers;
-  // compaction: the table, too
-  int32_t remapped;
   rr_page_pool p;
-  const int32_t* remap;
+  const int32_t* remap;                                 // of a compaction (with a row of CTAs more for the table), else NULL
   Layer layer[MAX_LAYERS];
 };
 
-// Eight units in flight per thread.  Sources and destinations are different pages.
+// The table of a compacted pool.
+__device__ __forceinline__ void renumber(const CopyParams& P, int moves) {
+  const int live = __ldcg(P.w.moves + 1);
+  for (int b = blockIdx.x; b < P.p.batch && moves > 0; b += gridDim.x) {
+    int32_t* const row = P.p.page_table + b * P.p.table_stride;
+    const int held = held_of(P.p, b);
+#pragma unroll 4
+    for (int c = threadIdx.x; c < held; c += blockDim.x) {
+      const int id = row[c];
+      if (!in_pool(P.p, id)) report(P.p, RR_STATUS_BAD_INDEX);
+      else if (id >= live) row[c] = __ldcg(P.remap + id);
+    }
+  }
+}
+
+// Where all runs lie on 16 bytes: one thread of a CTA moves pieces of up to 8 KB through a ring in shared memory with bulk copies, three loads ahead of the stores, four
+// CTAs per SM.  A piece costs it some hundred instructions, whatever its length; with registers and 16-byte loads the addresses alone took longer
+// than the memory.
+constexpr int COPY_NT = 128, PIECE = 8192, STAGES = 6, AHEAD = 3;
+constexpr size_t COPY_SMEM = STAGES * PIECE;
+
+__device__ __forceinline__ void bulk_load(void* smem, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(sm100::smem_u32(smem)), "l"(src), "r"(bytes),
+               "r"(sm100::smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* dst, const void* smem, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;" ::"l"(dst), "r"(sm100::smem_u32(smem)), "r"(bytes) : "memory");
+}
+
+__global__ void __launch_bounds__(COPY_NT)
+copy_bulk_kernel(const __grid_constant__ CopyParams P) {
+  extern __shared__ __align__(128) char ring[];
+  __shared__ uint64_t full[STAGES];
+  __shared__ char* s_dst[STAGES];
+  __shared__ uint32_t s_bytes[STAGES];
+  __shared__ uint32_t s_abort;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < STAGES; ++i) sm100::mbar_init(full + i, 1);
+    sm100::mbar_fence_init();
+    s_abort = 0;
+  }
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  const int moves = __ldcg(P.w.moves);
+  if ((int)blockIdx.y == 2 * P.layers) {
+    renumber(P, moves);
+    return;
+  }
+  if (threadIdx.x != 0) return;
+  const Layer& L = P.layer[blockIdx.y >> 1];
+  char* const base = L.base[blockIdx.y & 1];
+  const int outers = L.token_major ? P.page_tokens : L.heads;
+  const int64_t inner = (int64_t)(L.token_major ? L.heads : P.page_tokens) * L.row;      // bytes of a whole run
+  const unsigned most = (unsigned)outers * (unsigned)((inner + PIECE - 1) / PIECE);
+  const long long items = (long long)moves * most;
+  int loaded = 0, stored = 0;
+  auto store = [&] {
+    const int st = stored % STAGES;
+    if (!sm100::mbar_wait(full + st, stored / STAGES & 1, &s_abort)) return false;
+    bulk_store(s_dst[st], ring + st * PIECE, s_bytes[st]);
+    ++stored;
+    return true;
+  };
+  auto move_at = [&](long long item) {
+    const Move* const m = P.w.move + (item < items ? item / most : 0);
+    return Move{__ldcg(&m->src), __ldcg(&m->dst), __ldcg(&m->tokens)};
+  };
+  bool ok = true;
+  Move next = moves > 0 ? move_at(blockIdx.x) : Move{};
+  for (long long item = blockIdx.x; ok && item < items; item += gridDim.x) {
+    const Move mv = next;
+    next = move_at(item + gridDim.x);
+    const unsigned i = (unsigned)(item % most);
+    // the runs of this move: one where everything that is copied lies side by side
+    const int64_t length = L.token_major ? inner : (int64_t)mv.tokens * L.row;
+    const bool whole = length == L.outer;
+    const int runs = whole ? 1 : L.token_major ? mv.tokens : L.heads;
+    const int64_t bytes = whole ? length * (L.token_major ? mv.tokens : L.heads) : length;
+    const unsigned pieces = (unsigned)((bytes + PIECE - 1) / PIECE), run = i / pieces;
+    if (run >= (unsigned)runs) continue;
+    const int64_t at = (int64_t)(i - run * pieces) * PIECE, off = run * L.outer + at;
+    const uint32_t n = (uint32_t)min(bytes - at, (int64_t)PIECE);
+    const int st = loaded % STAGES;
+    // the store that read this stage last: AHEAD loads are not stored yet, so it is the (STAGES - AHEAD)-th last one
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(STAGES - AHEAD - 1) : "memory");
+    s_dst[st] = base + mv.dst * L.page + off;
+    s_bytes[st] = n;
+    sm100::mbar_expect_tx(full + st, n);
+    bulk_load(ring + st * PIECE, base + mv.src * L.page + off, n, full + st);
+    ++loaded;
+    if (loaded - stored > AHEAD) ok = store();
+  }
+  while (ok && stored < loaded) ok = store();
+  if (!ok) {
+    report(P.p, RR_STATUS_TIMEOUT);
+    for (int i = stored + 1; i < loaded; ++i) {         // its own copies in flight, again with a limit
+      s_abort = 0;
+      sm100::mbar_wait(full + i % STAGES, i / STAGES & 1, &s_abort);
+    }
+  }
+  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
+// Everything else: units of 16 bytes (or of an entry, where strides or addresses do not split), eight in flight per thread.
+constexpr int UNITS_NT = 256, COPY_UNITS = 8 * UNITS_NT;
+
 template <typename U>
 __device__ __forceinline__ void copy_units(const Layer& L, const char* src, char* dst, unsigned first, unsigned units, unsigned inner) {
-  U v[COPY_UNITS / COPY_NT];
-  int64_t at[COPY_UNITS / COPY_NT];
+  U v[COPY_UNITS / UNITS_NT];
+  int64_t at[COPY_UNITS / UNITS_NT];
+  const unsigned row = L.row / sizeof(U);
 #pragma unroll
-  for (int i = 0; i < COPY_UNITS / COPY_NT; ++i) {
-    const unsigned u = first + i * COPY_NT + threadIdx.x;
+  for (int i = 0; i < COPY_UNITS / UNITS_NT; ++i) {
+    const unsigned u = first + i * UNITS_NT + threadIdx.x;
     at[i] = -1;
     if (u < units) {
-      const unsigned o = u / inner, r = u - o * inner;
-      at[i] = o * L.outer;
-      if (L.joined) at[i] += (int64_t)r * sizeof(U);
-      else { const unsigned m = r / L.row; at[i] += m * L.mid + (int64_t)(r - m * L.row) * sizeof(U); }
+      const unsigned o = u / inner, r = u - o * inner, m = r / row;
+      at[i] = o * L.outer + m * L.mid + (int64_t)(r - m * row) * sizeof(U);
       v[i] = *(const U*)(src + at[i]);
     }
   }
 #pragma unroll
-  for (int i = 0; i < COPY_UNITS / COPY_NT; ++i)
+  for (int i = 0; i < COPY_UNITS / UNITS_NT; ++i)
     if (at[i] >= 0) *(U*)(dst + at[i]) = v[i];
 }
 
-__global__ void __launch_bounds__(COPY_NT)
-copy_kernel(const __grid_constant__ CopyParams P) {
+__global__ void __launch_bounds__(UNITS_NT)
+copy_units_kernel(const __grid_constant__ CopyParams P) {
   rr_pdl_wait();
   rr_pdl_trigger();
   const int moves = __ldcg(P.w.moves);
-  if ((int)blockIdx.y == 2 * P.layers) {                // the table of a compacted pool
-    const int live = __ldcg(P.w.moves + 1);
-    for (int b = blockIdx.x; b < P.p.batch && moves > 0; b += gridDim.x) {
-      int32_t* const row = P.p.page_table + b * P.p.table_stride;
-      const int held = held_of(P.p, b);
-      for (int c = threadIdx.x; c < held; c += COPY_NT) {
-        const int id = row[c];
-        if (!in_pool(P.p, id)) report(P.p, RR_STATUS_BAD_INDEX);
-        else if (id >= live) row[c] = __ldcg(P.remap + id);
-      }
-    }
+  if ((int)blockIdx.y == 2 * P.layers) {
+    renumber(P, moves);
     return;
   }
   const Layer& L = P.layer[blockIdx.y >> 1];
   char* const base = L.base[blockIdx.y & 1];
-  const unsigned chunks = ((unsigned)L.heads * P.page_tokens * L.row + COPY_UNITS - 1) / COPY_UNITS;
+  const unsigned row = L.row / L.unit, chunks = ((unsigned)L.heads * P.page_tokens * row + COPY_UNITS - 1) / COPY_UNITS;
   for (long long item = blockIdx.x; item < (long long)moves * chunks; item += gridDim.x) {
     const int m = (int)(item / chunks);
     const Move mv{__ldcg(&P.w.move[m].src), __ldcg(&P.w.move[m].dst), __ldcg(&P.w.move[m].tokens)};
     const unsigned first = (unsigned)(item - (long long)m * chunks) * COPY_UNITS;
-    const unsigned units = (unsigned)L.heads * mv.tokens * L.row, inner = (unsigned)(L.token_major ? L.heads : mv.tokens) * L.row;
+    const unsigned units = (unsigned)L.heads * mv.tokens * row, inner = (unsigned)(L.token_major ? L.heads : mv.tokens) * row;
     if (first >= units) continue;
     const char* const src = base + mv.src * L.page;
     char* const dst = base + mv.dst * L.page;
@@ -543,38 +748,45 @@ Layer layer_of(const rr_paged_kv& c) {
   const uint64_t all = (uint64_t)L.page | L.outer | L.mid | row | (uintptr_t)c.k | (uintptr_t)c.v;
   L.unit = all % 16 == 0 ? 16 : (int8_t)e;
   L.heads = c.kv_heads;
-  L.row = (int32_t)(row / L.unit);
+  L.row = (int32_t)row;
   return L;
 }
 
 // The copies that the bookkeeping kernel has listed, in all caches; of a compaction also the table.
 int launch_copies(const PoolParams& P, const rr_paged_kv* caches, int n, bool compact, cudaStream_t st, const char* who) {
+  static unsigned long long done = 0;
+  cudaError_t e = rr_once_per_device(done, [] { return cudaFuncSetAttribute(copy_bulk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)COPY_SMEM); });
+  if (e != cudaSuccess) return rr_cuda_fail(e, who);
   for (int at = 0; at < n; at += MAX_LAYERS) {
     CopyParams C;
     C.w = P.w;
     C.page_tokens = P.p.page_tokens;
     C.layers = n - at < MAX_LAYERS ? n - at : MAX_LAYERS;
-    C.remapped = compact && at == 0;
     C.p = P.p;
-    C.remap = P.remap;
-    for (int i = 0; i < C.layers; ++i) C.layer[i] = layer_of(caches[at + i]);
-    const int rows = 2 * C.layers + C.remapped, ctas = rr_sm_count() * 4;
+    C.remap = compact && at == 0 ? P.remap : nullptr;
+    bool bulk = true;
+    for (int i = 0; i < C.layers; ++i) {
+      C.layer[i] = layer_of(caches[at + i]);
+      bulk = bulk && C.layer[i].unit == 16 && C.layer[i].joined;
+    }
+    const int rows = 2 * C.layers + (C.remap != nullptr), ctas = rr_sm_count() * 4;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((ctas + rows - 1) / rows, rows);
-    cfg.blockDim = dim3(COPY_NT);
+    cfg.gridDim = dim3(ctas / rows > 0 ? ctas / rows : 1, rows);
+    cfg.blockDim = dim3(bulk ? COPY_NT : UNITS_NT);
+    cfg.dynamicSmemBytes = bulk ? COPY_SMEM : 0;
     cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
     rr_count_launch();
-    if (const cudaError_t e = cudaLaunchKernelEx(&cfg, copy_kernel, C); e != cudaSuccess) return rr_cuda_fail(e, who);
+    if ((e = cudaLaunchKernelEx(&cfg, bulk ? copy_bulk_kernel : copy_units_kernel, C)) != cudaSuccess) return rr_cuda_fail(e, who);
   }
   return RR_OK;
 }
 
-int launch_pool(void (*kernel)(PoolParams), const PoolParams& P, cudaStream_t st, const char* who) {
+int launch_pool(void (*kernel)(PoolParams), const PoolParams& P, int threads, size_t smem, cudaStream_t st, const char* who) {
   rr_count_launch();
-  const cudaError_t e = rr_launch_pdl(kernel, CL, NT, 0, st, P);
+  const cudaError_t e = rr_launch_pdl(kernel, CL, threads, smem, st, P);
   return e == cudaSuccess ? RR_OK : rr_cuda_fail(e, who);
 }
 
@@ -595,8 +807,8 @@ extern "C" int rr_pages_fork(const rr_page_pool* pool, const int32_t* parents, c
   if (!parents || !lens || !new_lens || lens == new_lens || parents == new_lens) return RR_ERR_INVALID_ARG;
   if (((uintptr_t)parents | (uintptr_t)lens | (uintptr_t)new_lens) & 3) return RR_ERR_INVALID_ARG;
   if ((rc = check_workspace(pool, workspace, bytes)) != RR_OK) return rc;
-  PoolParams P{*pool, work_of(*pool, workspace), parents, lens, new_lens, nullptr, 0};
-  return launch_pool(fork_kernel, P, (cudaStream_t)stream, "rr_pages_fork");
+  PoolParams P{*pool, work_of(*pool, workspace), parents, lens, new_lens, nullptr, 0, 0};
+  return launch_pool(fork_kernel, P, FORK_NT, pool->batch > ROWS_ON_CHIP ? 0 : sizeof(Heir) * pool->batch, (cudaStream_t)stream, "rr_pages_fork");
 }
 
 extern "C" int rr_pages_reserve(const rr_page_pool* pool, const int32_t* lens, const int32_t* new_tokens, int32_t new_each, const rr_paged_kv* caches,
@@ -606,8 +818,12 @@ extern "C" int rr_pages_reserve(const rr_page_pool* pool, const int32_t* lens, c
   if (!lens || (((uintptr_t)lens | (uintptr_t)new_tokens) & 3) || (!new_tokens && new_each < 0)) return RR_ERR_INVALID_ARG;
   if ((rc = check_caches(pool, caches, n)) != RR_OK) return rc;
   if ((rc = check_workspace(pool, workspace, bytes)) != RR_OK) return rc;
-  PoolParams P{*pool, work_of(*pool, workspace), new_tokens, lens, nullptr, nullptr, new_each};
-  rc = launch_pool(reserve_kernel, P, (cudaStream_t)stream, "rr_pages_reserve");
+  PoolParams P{*pool, work_of(*pool, workspace), new_tokens, lens, nullptr, nullptr, new_each, slots_of(pool->batch)};
+  static unsigned long long done = 0;
+  constexpr size_t given = GIVEN * 4, most = given + sizeof(Row) * ROWS_ON_CHIP + sizeof(Slot) * 2 * ROWS_ON_CHIP;
+  const cudaError_t e = rr_once_per_device(done, [] { return cudaFuncSetAttribute(reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most); });
+  if (e != cudaSuccess) return rr_cuda_fail(e, "rr_pages_reserve");
+  rc = launch_pool(reserve_kernel, P, NT, given + (pool->batch > ROWS_ON_CHIP ? 0 : row_state(*pool)), (cudaStream_t)stream, "rr_pages_reserve");
   return rc != RR_OK ? rc : launch_copies(P, caches, n, false, (cudaStream_t)stream, "rr_pages_reserve");
 }
 
@@ -618,8 +834,8 @@ extern "C" int rr_pages_compact(const rr_page_pool* pool, const rr_paged_kv* cac
   if ((uintptr_t)new_ids & 3) return RR_ERR_INVALID_ARG;
   if ((rc = check_caches(pool, caches, n)) != RR_OK) return rc;
   if ((rc = check_workspace(pool, workspace, bytes)) != RR_OK) return rc;
-  PoolParams P{*pool, work_of(*pool, workspace), nullptr, nullptr, nullptr, new_ids, 0};
-  if (!P.remap) P.remap = P.w.list + 2 * (size_t)pool->num_pages;
-  rc = launch_pool(compact_kernel, P, (cudaStream_t)stream, "rr_pages_compact");
+  PoolParams P{*pool, work_of(*pool, workspace), nullptr, nullptr, nullptr, new_ids, 0, 0};
+  if (!P.remap) P.remap = P.w.ranked;
+  rc = launch_pool(compact_kernel, P, NT, 0, (cudaStream_t)stream, "rr_pages_compact");
   return rc != RR_OK ? rc : launch_copies(P, caches, n, true, (cudaStream_t)stream, "rr_pages_compact");
 }

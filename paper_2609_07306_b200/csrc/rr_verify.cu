@@ -6,13 +6,15 @@
 // Greedy:   draft x is accepted if it is the row's lowest best.
 //
 // Sampled, a step reads two numbers a draft and one row (two, if a draft was rejected) a sequence; greedy, all rows.  Bound by memory for
-// batches, by latency for one sequence.  A cluster takes a sequence, each CTA a run of blocks of the vocabulary; which drafts are accepted every CTA
-// finds for itself (a few dependent loads, instead of a barrier).  Sampled: a warp adds up a block of 256 entries at a time, eight per lane in
-// flight from each row, and leaves the block's sum; the CTAs exchange their sums, the one that has the threshold finds block and entry, so the row is
-// read once but for that block.  Products, differences and sums are 64-bit: the first two are exact for probabilities of up to 24 bits,
-// and a sum over the vocabulary is off by some 1e-14, so that a random number falls between two results about never.
-// Greedy: 16 bytes at a time where rows allow it; only maxima are taken (a packed maximum of two bf16 costs one instruction), a thread keeps its first best
-// vector, and the entry inside it is looked up at the end.
+// batches, by latency for one sequence.
+// Sampled: a cluster takes a sequence, each CTA a run of blocks of the vocabulary; which drafts are accepted every CTA
+// finds for itself (a few dependent loads, instead of a barrier).  A warp reads a block of 256 entries at a time, eight per lane from each row, the next block's loads
+// in front of this one's arithmetic, and leaves its lanes' sums; the CTAs exchange their totals, the one that has the threshold finds block and
+// entry, so the row is read once but for that block.  Products, differences and sums are 64-bit: the first two are exact for probabilities of up
+// to 24 bits, and a sum over the vocabulary is off by some 1e-14, so that a random number falls between two results about never.
+// Greedy: a cluster takes a row, whoever's it is (sequences with many drafts would hold up the others), 16 bytes at a time where rows
+// allow it; only maxima are taken (a packed maximum of two bf16 costs one instruction), a thread keeps its first best vector, and the entry inside it is looked
+// up at the end.  The rows' best tokens go to `out`, where a second kernel, a warp per sequence, compares them with the drafts.
 #include <cooperative_groups.h>
 #include "rr_paged.cuh"
 
@@ -20,9 +22,8 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int NT = 512, NW = NT / 32, BLOCK = 256, MAX_CL = 8;
-constexpr int MAX_SUMS = 1024;                          // blocks' sums that a CTA keeps
-constexpr int ROWS = 16;                                // greedy: rows looked at between two exchanges
+constexpr int NT = 256, NW = NT / 32, BLOCK = 256, MAX_CL = 8;
+constexpr int SUMS = 64;                                // blocks' sums that a CTA keeps
 
 struct Span { int first, n; };                          // a sequence's first row, its drafts (-1: it has no rows)
 
@@ -31,15 +32,11 @@ __device__ __forceinline__ Span span_of(const rr_verify_args& a, int b) {
   return Span{first, max(end - first, 0) - 1};
 }
 
-// Probabilities are finite and positive, or 0.
+// Probabilities are positive and finite (bits 1 to those of the largest number), or 0.
+__device__ __forceinline__ float weight(float x) { return __float_as_uint(x) - 1u < 0x7F7FFFFFu ? x : 0.f; }
 template <typename T>
-__device__ __forceinline__ float weight(T x) {
-  const float f = rr_to_f32(x);
-  return f > 0.f && f <= 3.402823466e38f ? f : 0.f;
-}
-template <typename T>
-__device__ __forceinline__ float probability(const void* rows, int64_t stride, int row, int x) {
-  return weight(__ldg((const T*)rows + row * stride + x));
+__device__ __forceinline__ double probability(const void* rows, int64_t stride, int row, int x) {
+  return weight(rr_to_f32(__ldg((const T*)rows + row * stride + x)));
 }
 
 __device__ __forceinline__ double warp_sum(double x) {
@@ -47,22 +44,16 @@ __device__ __forceinline__ double warp_sum(double x) {
   for (int d = 16; d > 0; d /= 2) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
   return x;
 }
-__device__ __forceinline__ double warp_prefix(double x) {               // inclusive
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) { const double y = __shfl_up_sync(0xFFFFFFFFu, x, d); if (lane >= d) x += y; }
-  return x;
+__device__ __forceinline__ void write_lengths(const rr_verify_args& a, int b, const Span& s, int accepted) {
+  a.accepted[b] = accepted;
+  if (a.new_lens) a.new_lens[b] = a.lens[b] + (s.n < 0 ? 0 : accepted + 1);
 }
-
-// Accepted drafts and lengths, but for the token more.
+// A sequence's results; `more`: the token behind the accepted drafts.
 __device__ __forceinline__ void write_accepted(const rr_verify_args& a, int b, const Span& s, int accepted, int more) {
   const int lane = threadIdx.x & 31;
   for (int i = lane; i <= s.n; i += 32)
     a.out[s.first + i] = i < accepted ? a.tokens[s.first + i + 1] : i == accepted ? more : -1;
-  if (lane == 0) {
-    a.accepted[b] = accepted;
-    if (a.new_lens) a.new_lens[b] = a.lens[b] + (s.n < 0 ? 0 : accepted + 1);
-  }
+  if (lane == 0) write_lengths(a, b, s, accepted);
 }
 
 // A drafted token is in the vocabulary.
@@ -73,53 +64,92 @@ __device__ __forceinline__ bool in_vocab(const rr_verify_args& a, int x) {
 }
 
 // ---- sampled ----------------------------------------------------------------------------------------------------
-// The weights of a row: p - q where there is q, without the entry `but` (-1: none).
-template <typename T> struct Weights {
-  const T* p;
-  const T* q;
-  int but, vocab;
-  __device__ __forceinline__ double at(int j) const {
-    if (j >= vocab || j == but) return 0.0;
-    const double w = (double)weight(__ldg(p + j)) - (q ? (double)weight(__ldg(q + j)) : 0.0);
-    return w > 0.0 ? w : 0.0;
-  }
-  // Entries first + lane + 32 i of a block: the loads in front of the arithmetic.
-  __device__ __forceinline__ void block(int first, double (&w)[8]) const {
-    T x[8], y[8];
+// A block of a row of the target's and of one of the draft's (0 where there is none): entries first + lane + 32 i.
+template <typename T> struct Block {
+  T p[8], q[8];
+  __device__ __forceinline__ void load(const T* prow, const T* qrow, int vocab, int first) {
     const int j0 = first + (threadIdx.x & 31);
+    if (first + BLOCK <= vocab) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = __ldg(prow + j0 + 32 * i);
+      if (qrow) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = __ldg(qrow + j0 + 32 * i);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool in = j0 + 32 * i < vocab;
+        p[i] = in ? __ldg(prow + j0 + 32 * i) : rr_from_f32<T>(0.f);
+        q[i] = in && qrow ? __ldg(qrow + j0 + 32 * i) : rr_from_f32<T>(0.f);
+      }
+    }
+  }
+  // max(p - q, 0), 0 at the entry `but` (-1: none)
+  __device__ __forceinline__ double weight_at(int i, int first, int but, bool with_q) const {
+    const float x = weight(rr_to_f32(p[i])), y = with_q ? weight(rr_to_f32(q[i])) : 0.f;
+    return x > y && first + (int)(threadIdx.x & 31) + 32 * i != but ? (double)x - (double)y : 0.0;
+  }
+  // The sum of the lane's eight weights.  Where x > y >= 0, x - y is d = fl(x - y) and the rest (x - d) - y, which FP32 holds without error: one conversion
+  // instead of two; the rests, 2^-24 of their terms and less, are added in FP32.
+  __device__ __forceinline__ double sum(int first, int but, bool with_q) const {
+    if (but >= first && but < first + BLOCK) {          // (one block of a row)
+      double s = 0.0;
+#pragma unroll 1
+      for (int j = 0; j < 8; ++j) {
+        T pj = p[0], qj = q[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) if (i == j) pj = p[i], qj = q[i];
+        const float x = weight(rr_to_f32(pj)), y = with_q ? weight(rr_to_f32(qj)) : 0.f;
+        s += x > y && first + (int)(threadIdx.x & 31) + 32 * j != but ? (double)x - (double)y : 0.0;
+      }
+      return s;
+    }
+    double s[2] = {0.0, 0.0};
+    float rest = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int j = j0 + 32 * i;
-      const bool in = j < vocab;
-      x[i] = in ? __ldg(p + j) : rr_from_f32<T>(0.f);
-      y[i] = in && q ? __ldg(q + j) : rr_from_f32<T>(0.f);
+      const float x = rr_to_f32(p[i]);
+      if (with_q) {
+        const float y = weight(rr_to_f32(q[i])), d = x - y, w = weight(d);       // (an x that is none of a probability makes no positive and finite d)
+        rest += w != 0.f ? (x - d) - y : 0.f;
+        s[i & 1] += (double)w;
+      } else {
+        s[i & 1] += (double)weight(x);
+      }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const double d = (double)weight(x[i]) - (double)weight(y[i]);
-      w[i] = d > 0.0 && j0 + 32 * i != but ? d : 0.0;
-    }
+    return s[0] + s[1] + (double)rest;
   }
 };
 
-struct Found { double sums[MAX_SUMS]; double total; double warp[NW]; };
+struct Found { double lanes[SUMS][33]; double sums[SUMS]; double total; };
 
-// The first entry of a warp's 32 whose running sum, from `run` on, is over `limit`, else the last one with a weight; 32 if none has.
-__device__ __forceinline__ int first_over(double w, double run, double limit) {
-  const double upto = run + warp_prefix(w);             // (by all lanes)
-  const unsigned over = __ballot_sync(0xFFFFFFFFu, w > 0.0 && upto > limit);
-  if (over) return __ffs(over) - 1;
-  const unsigned some = __ballot_sync(0xFFFFFFFFu, w > 0.0);
-  return some ? 31 - __clz(some) : 32;
+// Of a warp's 32 weights the first whose running sum, from `run` on, is over `limit`, else the last one that is not 0 (at = 32: none is).
+struct Hit { int at; bool over; double before, end; };  // the sums before it and behind all
+__device__ __noinline__ Hit find(double w, double run, double limit) {
+  const int lane = threadIdx.x & 31;
+  double upto = w;
+#pragma unroll 1
+  for (int d = 1; d < 32; d *= 2) { const double y = __shfl_up_sync(0xFFFFFFFFu, upto, d); if (lane >= d) upto += y; }
+  upto += run;
+  const unsigned over = __ballot_sync(0xFFFFFFFFu, w > 0.0 && upto > limit), some = __ballot_sync(0xFFFFFFFFu, w > 0.0);
+  Hit h;
+  h.at = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : 32;
+  h.over = over != 0;
+  h.before = __shfl_sync(0xFFFFFFFFu, upto - w, h.at & 31);
+  h.end = __shfl_sync(0xFFFFFFFFu, upto, 31);
+  return h;
 }
 
 template <typename T>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(NT, 4)
 verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
   __shared__ Found f;
   cg::cluster_group cl = cg::this_cluster();
   const int ctas = cl.num_blocks(), cta = cl.block_rank(), b = blockIdx.x / ctas;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  rr_pdl_wait();
+  rr_pdl_trigger();
   const Span s = span_of(a, b);
   if (s.n < 0) {                                        // (uniform in the cluster)
     if (cta == 0 && warp == 0) write_accepted(a, b, s, 0, -1);
@@ -132,10 +162,11 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
     bool ok = true;
     if (i < s.n) {
       const int x = __ldg(a.tokens + t + 1);
+      const double u = __ldg(a.uniform + t);
       ok = in_vocab(a, x);
       if (ok) {
         const double p = probability<T>(a.target, a.target_stride, t, x), q = a.draft ? probability<T>(a.draft, a.draft_stride, t, x) : 1.0;
-        ok = p > (double)__ldg(a.uniform + t) * q;
+        ok = p > u * q;
       }
     }
     const unsigned rejected = __ballot_sync(0xFFFFFFFFu, !ok);
@@ -143,77 +174,96 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
     accepted = min(i0 + 32, s.n);
   }
   const int row = s.first + accepted;
-  Weights<T> w{(const T*)a.target + row * a.target_stride, nullptr, -1, a.vocab};
+  const T* const p = (const T*)a.target + row * a.target_stride;
+  const T* q = nullptr;
+  int but = -1;
   if (accepted < s.n) {
-    if (a.draft) w.q = (const T*)a.draft + row * a.draft_stride;
-    else w.but = __ldg(a.tokens + row + 1);
+    if (a.draft) q = (const T*)a.draft + row * a.draft_stride;
+    else but = __ldg(a.tokens + row + 1);
   }
   const double u = fmax((double)__ldg(a.uniform + s.first + s.n), 0.0);
   // blocks of this CTA; a kept sum stands for `per` of them
   const int blocks = (a.vocab + BLOCK - 1) / BLOCK, share = (blocks + ctas - 1) / ctas, from = min(cta * share, blocks), mine = min(share, blocks - from);
-  const int per = (share + MAX_SUMS - 1) / MAX_SUMS, sums = (mine + per - 1) / per;
+  const int per = (share + SUMS - 1) / SUMS, sums = (mine + per - 1) / per;
   int token = -1;
   bool here = false, none = false;
   for (int pass = 0; pass < 2; ++pass) {
-    for (int k = warp; k < sums; k += NW) {
-      double sum = 0.0;
-      for (int i = k * per; i < min((k + 1) * per, mine); ++i) {
-        double x[8];
-        w.block((from + i) * BLOCK, x);
-        sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    Block<T> now, next;
+    int k = warp, i = warp * per;                       // kept sum and block
+    double sum = 0.0;
+    if (k < sums) now.load(p, q, a.vocab, (from + i) * BLOCK);
+    while (k < sums) {
+      const int at = (from + i) * BLOCK;
+      const bool last = i + 1 >= min((k + 1) * per, mine);
+      const int k_next = last ? k + NW : k, i_next = last ? k_next * per : i + 1;
+      if (k_next < sums) next.load(p, q, a.vocab, (from + i_next) * BLOCK);
+      sum += now.sum(at, but, q != nullptr);
+      if (last) {
+        f.lanes[k][lane] = sum;
+        sum = 0.0;
       }
-      sum = warp_sum(sum);
-      if (lane == 0) f.sums[k] = sum;
+      now = next;
+      k = k_next;
+      i = i_next;
+    }
+    __syncthreads();
+    {                                                   // four threads add up a kept sum's lanes
+      const int k = threadIdx.x / 4, part = threadIdx.x & 3;
+      double x = 0.0;
+      if (k < sums)
+        for (int i = 0; i < 8; ++i) x += f.lanes[k][8 * part + i];
+      x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
+      x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
+      if (part == 0) f.sums[k] = x;
     }
     __syncthreads();
     if (warp == 0) {
-      double sum = 0.0;
-      for (int k = lane; k < sums; k += 32) sum += f.sums[k];
-      sum = warp_sum(sum);
-      if (lane == 0) f.total = sum;
+      const double x = warp_sum(f.sums[lane] + f.sums[lane + 32]);
+      if (lane == 0) f.total = x;
     }
     cl.sync();
     // every warp finds the CTA that has the threshold
     const double theirs = lane < ctas ? *cl.map_shared_rank(&f.total, lane) : 0.0;
-    const double run = warp_prefix(theirs), total = __shfl_sync(0xFFFFFFFFu, run, 31), limit = u * total;
-    const int who = first_over(theirs, 0.0, limit);
-    cl.sync();                                          // the sums have been read (nothing of another CTA's is read from here on)
-    if (who == 32) {                                    // no weight: the rejected row has no more than the draft's anywhere
-      none = !w.q && w.but < 0;
+    const double limit = u * warp_sum(theirs);
+    Hit h = find(theirs, 0.0, limit);
+    cl.sync();                                          // the totals have been read (nothing of another CTA's is read from here on)
+    if (h.at == 32) {                                   // no weight: the rejected row has no more than the draft's anywhere
+      none = !q && but < 0;
       if (none) break;
-      w.q = nullptr;
-      w.but = -1;
+      q = nullptr;
+      but = -1;
       continue;
     }
-    here = who == cta;
+    here = h.at == cta;
     if (!here || warp != 0) break;
     // the kept sum, then the block, then the entry
-    double before = __shfl_sync(0xFFFFFFFFu, run - theirs, who), before_k = before;
-    int k = 0;
-    for (int k0 = 0; k0 < sums; k0 += 32) {
-      const double x = k0 + lane < sums ? f.sums[k0 + lane] : 0.0, upto = warp_prefix(x);
-      const int l = first_over(x, before, limit);
-      if (l < 32) k = k0 + l, before_k = before + __shfl_sync(0xFFFFFFFFu, upto - x, l);
-      if (__any_sync(0xFFFFFFFFu, x > 0.0 && before + upto > limit)) break;
-      before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+    double before = h.before, run = before;
+    k = 0;
+    h.over = false;
+#pragma unroll 1
+    for (int k0 = 0; k0 < sums && !h.over; k0 += 32) {
+      h = find(k0 + lane < sums ? f.sums[k0 + lane] : 0.0, run, limit);
+      if (h.at < 32) k = k0 + h.at, before = h.before;
+      run = h.end;
     }
-    before = before_k;
-    bool over = false;
-    for (int i = k * per; i < min((k + 1) * per, mine) && !over; ++i) {
-      double x[8];
-      w.block((from + i) * BLOCK, x);
+    run = before;
+    h.over = false;
+#pragma unroll 1
+    for (int i = k * per; i < min((k + 1) * per, mine) && !h.over; ++i) {
+      const int at = (from + i) * BLOCK;
+      now.load(p, q, a.vocab, at);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const double upto = warp_prefix(x[e]);
-        const int l = first_over(x[e], before, limit);
-        if (!over && l < 32) token = (from + i) * BLOCK + 32 * e + l;
-        over = over || __any_sync(0xFFFFFFFFu, x[e] > 0.0 && before + upto > limit);
-        before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+      for (int e = 0; e < 8; ++e) f.lanes[e][lane] = now.weight_at(e, at, but, q != nullptr);          // (each lane's own, again below)
+#pragma unroll 1
+      for (int e = 0; e < 8 && !h.over; ++e) {
+        h = find(f.lanes[e][lane], run, limit);
+        if (h.at < 32) token = at + 32 * e + h.at;
+        run = h.end;
       }
     }
     break;
   }
-  // a CTA that has the token, or the first one where all weights are 0
+  // the CTA that has the token, or the first one where all weights are 0
   if (warp == 0 && (here || (none && cta == 0))) write_accepted(a, b, s, accepted, token);
 }
 
@@ -246,96 +296,94 @@ __device__ __forceinline__ Best warp_best(Best x) {
   return Best{key, __reduce_min_sync(0xFFFFFFFFu, x.key == key ? x.at : INT32_MAX)};
 }
 
+// The best token of each row, -1 where all scores are NaN.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(NT)
-verify_greedy_kernel(const __grid_constant__ rr_verify_args a) {
-  __shared__ Best s_warp[ROWS][NW], s_cta[ROWS];
-  __shared__ int s_best[ROWS];
-  static_assert(ROWS == NW, "a warp per row");
+best_kernel(const __grid_constant__ rr_verify_args a) {
+  __shared__ Best s_warp[NW], s_cta;
   cg::cluster_group cl = cg::this_cluster();
-  const int ctas = cl.num_blocks(), cta = cl.block_rank(), b = blockIdx.x / ctas;
+  const int ctas = cl.num_blocks(), cta = cl.block_rank(), t = blockIdx.x / ctas;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Span s = span_of(a, b);
-  if (s.n < 0) {
-    if (cta == 0 && warp == 0) write_accepted(a, b, s, 0, -1);
-    return;
-  }
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  if (a.cu && t >= __ldg(a.cu + a.batch)) return;       // padding (uniform in the cluster)
   using V = Vec<T, VEC>;
   const int vecs = a.vocab / VEC, share = (vecs + ctas - 1) / ctas, from = min(cta * share, vecs), to = min(from + share, vecs);
-  const bool tail = cta == ctas - 1 && threadIdx.x == 0;                // the entries behind the last vector
-  int accepted = 0, more = -1;
-  for (int i0 = 0;; i0 += ROWS) {
-    const int rows = min(ROWS, s.n + 1 - i0);
-    for (int r = 0; r < rows; ++r) {
-      const T* const row = (const T*)a.target + (s.first + i0 + r) * a.target_stride;
-      Best x{0u, INT32_MAX};
-#pragma unroll 4
-      for (int v = from + threadIdx.x; v < to; v += NT) {
-        V e;
-        if constexpr (VEC == 1) e.v = __ldg(row + v);
-        else { const uint4 raw = __ldg((const uint4*)row + v); e = *(const V*)&raw; }
-        const uint32_t key = score_key(e.best());
-        if (key > x.key) x = Best{key, v};
-      }
-      if (tail)
-        for (int j = vecs * VEC; j < a.vocab; ++j)
-          if (const uint32_t key = score_key(rr_to_f32(__ldg(row + j))); key > x.key) x = Best{key, vecs};
-      x = warp_best(x);
-      if (lane == 0) s_warp[r][warp] = x;
-    }
-    __syncthreads();
-    if (warp < rows) {
-      const Best x = warp_best(lane < NW ? s_warp[warp][lane] : Best{0u, INT32_MAX});
-      // the first entry of the vector that is as good
-      const T* const row = (const T*)a.target + (s.first + i0 + warp) * a.target_stride;
-      const int j = x.key ? x.at * VEC + lane : 0;
-      const unsigned same = __ballot_sync(0xFFFFFFFFu, x.key && lane < VEC && j < a.vocab && score_key(rr_to_f32(__ldg(row + j))) == x.key);
-      if (lane == 0) s_cta[warp] = Best{x.key, x.key ? x.at * VEC + __ffs(same) - 1 : INT32_MAX};
-    }
-    cl.sync();
-    if (warp < rows) {
-      const Best x = warp_best(lane < ctas ? *cl.map_shared_rank(&s_cta[warp], lane) : Best{0u, INT32_MAX});
-      if (lane == 0) s_best[warp] = x.key ? x.at : -1;
-    }
-    cl.sync();
+  const T* const row = (const T*)a.target + t * a.target_stride;
+  Best x{0u, INT32_MAX};
+#pragma unroll 8
+  for (int v = from + threadIdx.x; v < to; v += NT) {
+    V e;
+    if constexpr (VEC == 1) e.v = __ldg(row + v);
+    else { const uint4 raw = __ldg((const uint4*)row + v); e = *(const V*)&raw; }
+    const uint32_t key = score_key(e.best());
+    if (key > x.key) x = Best{key, v};
+  }
+  if (cta == ctas - 1 && threadIdx.x == 0)              // the entries behind the last vector
+    for (int j = vecs * VEC; j < a.vocab; ++j)
+      if (const uint32_t key = score_key(rr_to_f32(__ldg(row + j))); key > x.key) x = Best{key, vecs};
+  x = warp_best(x);
+  if (lane == 0) s_warp[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    x = warp_best(lane < NW ? s_warp[lane] : Best{0u, INT32_MAX});
+    // the first entry of the vector that is as good
+    const int j = x.key ? x.at * VEC + lane : 0;
+    const unsigned same = __ballot_sync(0xFFFFFFFFu, x.key && lane < VEC && j < a.vocab && score_key(rr_to_f32(__ldg(row + j))) == x.key);
+    if (lane == 0) s_cta = Best{x.key, x.key ? x.at * VEC + __ffs(same) - 1 : INT32_MAX};
+  }
+  cl.sync();
+  if (cta == 0 && warp == 0) {
+    x = warp_best(lane < ctas ? *cl.map_shared_rank(&s_cta, lane) : Best{0u, INT32_MAX});
+    if (lane == 0) a.out[t] = x.key ? x.at : -1;
+  }
+  cl.sync();                                            // no CTA leaves before its best has been read
+}
+
+// The drafts against the rows' best tokens, which are in `out`: up to the first that differs they are the accepted tokens and the one more.
+__global__ void __launch_bounds__(128)
+compare_kernel(const __grid_constant__ rr_verify_args a) {
+  const int lane = threadIdx.x & 31, b = blockIdx.x * 4 + (threadIdx.x >> 5);
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  if (b >= a.batch) return;
+  const Span s = span_of(a, b);
+  int accepted = max(s.n, 0);
+  for (int i0 = 0; i0 < s.n; i0 += 32) {
     const int i = i0 + lane;
     bool ok = true;
-    if (lane < rows && i < s.n) {
+    if (i < s.n) {
       const int x = __ldg(a.tokens + s.first + i + 1);
-      ok = in_vocab(a, x) && x == s_best[lane];
-    } else if (lane == rows - 1) {
-      ok = false;                                       // the row behind the last draft
+      ok = in_vocab(a, x) && x == __ldcg(a.out + s.first + i);
     }
-    const unsigned stop = __ballot_sync(0xFFFFFFFFu, !ok);
-    if (stop) {
-      accepted = i0 + __ffs(stop) - 1;
-      more = s_best[__ffs(stop) - 1];
-      break;
-    }
-    __syncthreads();                                    // (before the next rows' results)
+    const unsigned rejected = __ballot_sync(0xFFFFFFFFu, !ok);
+    if (rejected) { accepted = i0 + __ffs(rejected) - 1; break; }
   }
-  if (cta == 0 && warp == 0) write_accepted(a, b, s, accepted, more);
+  for (int i = accepted + 1 + lane; i <= s.n; i += 32) a.out[s.first + i] = -1;
+  if (lane == 0) write_lengths(a, b, s, accepted);
 }
 
-// CTAs per sequence: eight share one, fewer where a CTA would get less than a block of the vocabulary for each of its warps.
-int cluster_of(int vocab) {
-  int n = MAX_CL;
-  while (n > 1 && vocab < n * NW * BLOCK) n /= 2;
-  return n;
+// CTAs that share `n` things (sequences, rows) of `work` entries each: at most eight a thing, no less than `least` entries for one, and no more in all than run at once (four per SM).
+int cluster_of(int n, int work, int least, int per_sm) {
+  int c = MAX_CL;
+  while (c > 1 && (work < c * least || (int64_t)n * c > per_sm * rr_sm_count())) c /= 2;
+  return c;
 }
 
-int launch(void (*kernel)(rr_verify_args), const rr_verify_args& a, cudaStream_t st) {
+cudaError_t launch(void (*kernel)(rr_verify_args), const rr_verify_args& a, int n, int cluster, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr{};
-  const int n = cluster_of(a.vocab);
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = n; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-  cfg.gridDim = dim3((unsigned)(a.batch * n)); cfg.blockDim = dim3(NT);
-  cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3((unsigned)(n * cluster)); cfg.blockDim = dim3(NT);
+  cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
   rr_count_launch();
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
-  return e == cudaSuccess ? RR_OK : rr_cuda_fail(e, "rr_verify_drafts");
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
+
+int done(cudaError_t e) { return e == cudaSuccess ? RR_OK : rr_cuda_fail(e, "rr_verify_drafts"); }
 
 }  // namespace
 
@@ -351,8 +399,15 @@ extern "C" int rr_verify_drafts(const rr_verify_args* a, void* stream) {
         (uintptr_t)a->new_lens | (uintptr_t)a->status) & 3)) return RR_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
   const bool bf16 = a->dtype == RR_BF16;
-  if (a->uniform) return launch(bf16 ? verify_sampled_kernel<__nv_bfloat16> : verify_sampled_kernel<float>, *a, st);
-  const bool vec = ((uintptr_t)a->target & 15) == 0 && (a->target_stride * (bf16 ? 2 : 4)) % 16 == 0;
-  if (bf16) return launch(vec ? verify_greedy_kernel<__nv_bfloat16, 8> : verify_greedy_kernel<__nv_bfloat16, 1>, *a, st);
-  return launch(vec ? verify_greedy_kernel<float, 4> : verify_greedy_kernel<float, 1>, *a, st);
+  if (a->uniform) {
+    const int cluster = cluster_of(a->batch, a->vocab, NW * BLOCK, 4);
+    return done(launch(bf16 ? verify_sampled_kernel<__nv_bfloat16> : verify_sampled_kernel<float>, *a, a->batch, cluster, st));
+  }
+  if (a->rows > 0) {
+    const bool vec = ((uintptr_t)a->target & 15) == 0 && (a->target_stride * (bf16 ? 2 : 4)) % 16 == 0;
+    auto* const kernel = bf16 ? (vec ? best_kernel<__nv_bfloat16, 8> : best_kernel<__nv_bfloat16, 1>) : (vec ? best_kernel<float, 4> : best_kernel<float, 1>);
+    if (const cudaError_t e = launch(kernel, *a, a->rows, cluster_of(a->rows, a->vocab, NT * 32, 16), st); e != cudaSuccess) return done(e);
+  }
+  rr_count_launch();
+  return done(rr_launch_pdl(compare_kernel, (a->batch + 3) / 4, 128, 0, st, *a));
 }

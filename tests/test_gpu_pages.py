@@ -331,3 +331,28 @@ def test_what_the_wrapper_refuses():
             setattr(pool, name, None)
     empty = PagePool.empty([kv])
     assert empty.free.item() == 12 and (empty.page_table == -1).all() and empty.page_table is table
+
+
+@pytest.mark.parametrize("pages", [7000, 140000])
+def test_many_pages_at_once(pages):
+    """More new pages than a CTA hands out by itself, from the gaps of a pool; copies and replaced pages among them."""
+    pool, flat, want = make(12, 900, pages, 2)
+    rng = random.Random(pages)
+    keep = {p: 1 for p in range(pages) if rng.random() < 0.2}
+    want.outside = dict(keep)
+    pool.refs[list(keep)] = 1
+    pool.free.fill_(pages - len(keep))
+    for lens, new, parents in (([0] * 12, [700] * 6 + [0] * 6, [0, 0, 0, 3, 4, 5, 1, 1, 5, 5, 9, -1]),
+                               ([700, 301, 401, 700, 3, 99, 1, 0, 1, 700, 0, 0], [900, 1, 1200, 0, 800, 777, 899, 1100, 0, 2, 0, 0], list(range(12)))):
+        pool.reserve(ints(lens), ints(new))
+        assert want.reserve(lens, new)
+        want.check(pool, flat)
+        out = ints([0] * 12)
+        after = [x + n for x, n in zip(lens, new)]
+        pool.fork(ints(parents), ints(after), out)
+        assert out.tolist() == want.fork(parents, after)
+        want.check(pool, flat)
+    pool.compact()
+    want.compact()
+    want.check(pool, flat)
+    assert pool.status.item() == 0
