@@ -253,13 +253,20 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
       const int at = (from + i) * BLOCK;
       now.load(p, q, a.vocab, at);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f.lanes[e][lane] = now.weight_at(e, at, but, q != nullptr);          // (each lane's own, again below)
-#pragma unroll 1
-      for (int e = 0; e < 8 && !h.over; ++e) {
-        h = find(f.lanes[e][lane], run, limit);
-        if (h.at < 32) token = at + 32 * e + h.at;
-        run = h.end;
+      for (int e = 0; e < 8; ++e) f.lanes[e][lane] = now.weight_at(e, at, but, q != nullptr);
+      __syncwarp();
+      double x = 0.0;                                   // four lanes add up 32 entries, then these
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x += f.lanes[lane / 4][8 * (lane & 3) + e];
+      x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
+      x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
+      h = find((lane & 3) ? 0.0 : x, run, limit);
+      run = h.end;
+      if (h.at < 32) {
+        const int e = h.at / 4;
+        token = at + 32 * e + find(f.lanes[e][lane], h.before, limit).at;
       }
+      __syncwarp();
     }
     break;
   }
