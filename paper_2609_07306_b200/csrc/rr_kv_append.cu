@@ -9,15 +9,15 @@
 // the token goes in the cache is still counted in tokens.  That build has one load in front of another more (the pair's axis, then its position).
 //
 // The work is one read and one write of every entry: bound by memory for prompts, by latency for a decoding
-// step.  A CTA takes a token; its threads take 16 bytes each (the two halves of eight or four pairs), read them before
-// the angles are there, and rotate in FP32 with one rounding.  Shapes and strides that do not split into 16-byte pieces
-// go entry by entry.  Measured: 17282 tokens of 32 query and 8 key heads of 128, bf16 (425 MB): 73 us, 5.8 TB/s, 90 % of a copy's rate; one
-// token for each of 64 sequences: 3.7 us.
+// step.  A CTA takes a token; its threads take 16 bytes each (the two halves of eight or four pairs) and rotate in FP32 with one
+// rounding.  Shapes and strides that do not split into 16-byte pieces go entry by entry.  Measured: 17282 tokens of 32 query and 8 key heads of
+// 128, bf16 (425 MB): 68 us, 6.3 TB/s, 96 % of a copy's rate, with positions of three axes (418 MB) 69 us; one token for each of 64 sequences: 3.4 us, with axes
+// 3.9 us.  (Loads in front of the angles, two pieces a thread: 130 us; the pieces' places have to be worked out twice then.)
 #include "rr_paged.cuh"
 
 namespace {
 
-constexpr int NT = 256;
+constexpr int MOST_NT = 256;                           // threads of a CTA: this, or half of them
 
 struct AppendParams {
   rr_paged_kv kv;
@@ -28,14 +28,14 @@ struct AppendParams {
 template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Piece { T x[VEC]; };
 
 template <typename T, int VEC, bool AXES>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(MOST_NT)
 kv_append_kernel(const __grid_constant__ AppendParams P) {
   __shared__ float s_cos[RR_PAGED_MAX_DH / 2], s_sin[RR_PAGED_MAX_DH / 2];
   __shared__ int s_pos;
   __shared__ long long s_at;                           // element offset of the token's place in the cache; -1: left out
   const rr_paged_kv& kv = P.kv;
   const rr_append_args& a = P.a;
-  const int tid = threadIdx.x, t = blockIdx.x;
+  const int tid = threadIdx.x, NT = blockDim.x, t = blockIdx.x;
   if (blockIdx.x == gridDim.x - 1 && a.new_lens)
     for (int b = tid; b < kv.batch; b += NT) {
       const int n = a.cu ? a.cu[b + 1] - a.cu[b] : 1;
@@ -169,6 +169,9 @@ int append(const rr_paged_kv* kv, const rr_append_args* a, const rr_axes_args* x
   if (a->tokens == 0 && !a->new_lens) return RR_OK;
   const AppendParams P{*kv, *a, x ? *x : rr_axes_args{}};
   const int grid = a->tokens > 0 ? a->tokens : 1;
+  // Few tokens: a token's own time counts, which more threads make shorter (64 tokens: 3.7 us, 4.4 with half of them).  Many: what all warps of a CTA do alike
+  // -- barriers, the sequence, the angles' loop -- costs issue slots, which half of them halve (17000 tokens, 418 MB: 79 us with 256 threads, 69 with 128).
+  const int NT = grid > 32 * rr_sm_count() ? MOST_NT / 2 : MOST_NT;
   cudaStream_t st = (cudaStream_t)stream;
   if (kv->dtype == RR_BF16) {
     if (pieces(*kv, *a, 8, 16)) kv_append_kernel<__nv_bfloat16, 8, AXES><<<grid, NT, 0, st>>>(P);
