@@ -470,7 +470,8 @@ int rr_attend_paged_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, void*
  *   page_table  the first held[b] entries of row b are the sequence's pages, in order; the others are -1
  *   refs        how many entries of the table hold a page; 0: the page is free.  (Entries outside the table that the caller keeps,
  *               a prefix for later sequences for instance, count too: the caller adds them, and takes them off, when no call is in flight.)
- *   free_pages  how many pages are free
+ *   free_pages  how many pages are free, kept by differences: whoever changes refs from or to 0 changes it, too (a compaction counts anew).  For the
+ *               caller; no call goes by it
  * Pages are handed out in ascending order of their numbers, the lowest free ones first, to the sequences in their order: the
  * results do not depend on timing.  Ids outside the pool, negative lengths and lengths behind the table's end set RR_STATUS_BAD_INDEX in
  * *status; an id is left out, a length taken as the nearest that the table holds.

@@ -15,7 +15,8 @@ class PagePool:
     page_tokens tokens of a page
     refs        [pages] int32: how many entries of the table hold a page (and how many holders the caller counts besides); 0: free
     held        [batch] int32
-    free        [1] int32: how many pages are free; None: counted from refs
+    free        [1] int32: how many pages are free; None: counted from refs.  It is kept by differences (compact counts anew): whoever frees or takes a
+                page by writing to refs changes it, too
     caches      the layers' caches (PagedKV), all of this pool's number and size of pages, and of this table or one that is kept like it
     status      optional [1] int32: RR_STATUS_* bits are OR-ed into it (RR_STATUS_BAD_INDEX: a page id outside the pool, a negative length or one
                 behind the table's end; RR_STATUS_NO_PAGES: fewer free pages than a call of reserve needed, which then gave none)
@@ -55,7 +56,7 @@ class PagePool:
         self._lib = B.lib()
         self._bytes = B.rr_pages_workspace(self._pool)
         self._ws = torch.empty(self._bytes, dtype=torch.uint8, device=self.device)
-        self._at = C.addressof(self._pool), C.addressof(self._caches), len(caches), self._ws.data_ptr()
+        self._at, self._caches_at, self._layers, self._ws_at = C.addressof(self._pool), C.addressof(self._caches), len(caches), self._ws.data_ptr()
 
     @classmethod
     def empty(cls, caches: "list[PagedKV] | tuple[PagedKV, ...]", status: torch.Tensor | None = None) -> "PagePool":
@@ -79,16 +80,13 @@ class PagePool:
 
     _ints = PagedKV._ints
 
-    def _run(self, call):
-        """One library call, given the current stream of the pool's device."""
-        if self._index != torch._C._cuda_getDevice():
-            with torch.cuda.device(self.device):
-                return self._run(call)
-        return call(torch._C._cuda_getCurrentRawStream(self._index))
+    def _stream(self):
+        """The current stream of the pool's device; None where another device is the current one."""
+        return torch._C._cuda_getCurrentRawStream(self._index) if self._index == torch._C._cuda_getDevice() else None
 
-    def _need_caches(self, what):
-        if not self._at[2]:
-            raise ValueError(f"{what} copies pages: the pool needs its caches")
+    def _done(self, rc, name):
+        if rc != B.RR_OK:
+            raise B.RouteRelayError(rc, name)
 
     def fork(self, parents: torch.Tensor, lens: torch.Tensor, new_lens: torch.Tensor) -> None:
         """Row b becomes what row parents[b] was, all rows at once; parents[b] == b: it stays, -1: its sequence has ended and the
@@ -100,10 +98,11 @@ class PagePool:
         self._ints(parents, "parents", shape)
         self._ints(lens, "lens", shape)
         self._ints(new_lens, "new_lens", shape)
-        pool, _, _, ws = self._at
-        rc = self._run(lambda stream: self._lib.rr_pages_fork(pool, parents.data_ptr(), lens.data_ptr(), new_lens.data_ptr(), ws, self._bytes, stream))
-        if rc != B.RR_OK:
-            raise B.RouteRelayError(rc, "rr_pages_fork")
+        stream = self._stream()
+        if stream is None:
+            with torch.cuda.device(self.device):
+                return self.fork(parents, lens, new_lens)
+        self._done(self._lib.rr_pages_fork(self._at, parents.data_ptr(), lens.data_ptr(), new_lens.data_ptr(), self._ws_at, self._bytes, stream), "rr_pages_fork")
 
     def reserve(self, lens: torch.Tensor, new: "torch.Tensor | int" = 0) -> None:
         """Sequence b keeps its first lens[b] tokens and may be appended to by new (or new[b]) tokens: pages behind that are released,
@@ -122,12 +121,14 @@ class PagePool:
             if not 0 <= new <= 0x7FFFFFFF:
                 raise ValueError(f"new must be between 0 and 2^31 - 1, not {new}")
             tokens, each = None, int(new)
-        pool, caches, n, ws = self._at
-        if not n:
-            self._need_caches("reserve")
-        rc = self._run(lambda stream: self._lib.rr_pages_reserve(pool, lens.data_ptr(), tokens, each, caches, n, ws, self._bytes, stream))
-        if rc != B.RR_OK:
-            raise B.RouteRelayError(rc, "rr_pages_reserve")
+        if not self._layers:
+            raise ValueError("reserve copies pages: the pool needs its caches")
+        stream = self._stream()
+        if stream is None:
+            with torch.cuda.device(self.device):
+                return self.reserve(lens, new)
+        self._done(self._lib.rr_pages_reserve(self._at, lens.data_ptr(), tokens, each, self._caches_at, self._layers, self._ws_at, self._bytes, stream),
+                   "rr_pages_reserve")
 
     def compact(self, new_ids: torch.Tensor | None = None) -> None:
         """The pages in use become the first ones of the pool, in the table, in refs and in all caches: of L pages in use, the i-th of those
@@ -135,9 +136,11 @@ class PagePool:
         new_ids  [pages] int32: gets where each page is now, for ids kept outside the table (a prefix's pages, for instance)"""
         if new_ids is not None:
             self._ints(new_ids, "new_ids", (self.num_pages,))
-        self._need_caches("compact")
-        pool, caches, n, ws = self._at
-        ids = None if new_ids is None else new_ids.data_ptr()
-        rc = self._run(lambda stream: self._lib.rr_pages_compact(pool, caches, n, ids, ws, self._bytes, stream))
-        if rc != B.RR_OK:
-            raise B.RouteRelayError(rc, "rr_pages_compact")
+        if not self._layers:
+            raise ValueError("compact copies pages: the pool needs its caches")
+        stream = self._stream()
+        if stream is None:
+            with torch.cuda.device(self.device):
+                return self.compact(new_ids)
+        self._done(self._lib.rr_pages_compact(self._at, self._caches_at, self._layers, None if new_ids is None else new_ids.data_ptr(), self._ws_at, self._bytes,
+                                              stream), "rr_pages_compact")

@@ -24,13 +24,16 @@ def _tensor(t, name, dtype, shape, index):
 
 def _rows(t, name, dtype, shape, index):
     """t has this type, shape and device and contiguous rows; its row stride."""
+    apart, side = t.stride()
+    if t.dtype is dtype and t.get_device() == index and side == 1 and not t.requires_grad and t.shape == shape:
+        return apart
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, which the verification does not have: call it under torch.no_grad()")
     if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)} on cuda:{index}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    if shape[1] > 1 and shape[0] > 0 and t.stride(1) != 1:
+    if shape[1] > 1 and shape[0] > 0 and side != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
-    return t.stride(0)
+    return apart
 
 
 def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor | None = None, *, draft: torch.Tensor | None = None,
@@ -63,8 +66,7 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor |
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
             return verify_drafts(target, tokens, cu, draft=draft, uniform=uniform, lens=lens, new_lens=new_lens, status=status)
-    shape = target.shape
-    rows, vocab = shape
+    rows, vocab = shape = tuple(target.shape)
     stride = _rows(target, "target", target.dtype, shape, index)
     i32, one = torch.int32, (rows,)
     p_tokens = _tensor(tokens, "tokens", i32, one, index)
@@ -80,17 +82,22 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor |
     if uniform is not None:
         p_uniform = _tensor(uniform, "uniform", torch.float32, one, index)
         if draft is not None:
+            if draft.dim() != 2:
+                raise ValueError("draft must be [rows, vocab]")
             draft_stride = _rows(draft, "draft", target.dtype, shape, index)
             p_draft = draft.data_ptr()
     elif draft is not None:
         raise ValueError("draft without uniform: greedy verification has no probabilities")
+    if lens is not None:
+        p_lens = _tensor(lens, "lens", i32, (batch,), index)
     if new_lens is not None:
         if lens is None:
             raise ValueError("new_lens without lens")
-        p_lens, p_new = _tensor(lens, "lens", i32, (batch,), index), _tensor(new_lens, "new_lens", i32, (batch,), index)
+        p_new = _tensor(new_lens, "new_lens", i32, (batch,), index)
     if status is not None:
         p_status = _tensor(status, "status", i32, (1,), index)
-    after, accepted = tokens.new_empty(one), tokens.new_empty((batch,))
+    after = torch.empty_like(tokens)
+    accepted = tokens.new_empty((batch,)) if lens is None else torch.empty_like(lens)
     if rows == 0:                                      # (an empty tensor has no address, and nothing is read)
         p_tokens = p_out = p_cu
         p_uniform = p_draft = 0
