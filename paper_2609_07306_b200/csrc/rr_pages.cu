@@ -22,7 +22,7 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int CL = 8, NT = 512, NW = NT / 32;
-constexpr int WARP_PAGES = 1024, CTA_PAGES = NW * WARP_PAGES, ROUND = CL * CTA_PAGES;
+constexpr int ROUND = CL * NT * 32;                     // pages of a round: 32 per thread
 constexpr int COLS = 256;                               // entries of a row that a warp looks at
 constexpr int ROWS_ON_CHIP = 2048;                      // rows whose state fits shared memory
 constexpr int GIVEN = 4096;                             // pages that a CTA hands out at a time
@@ -48,11 +48,13 @@ struct PoolParams {
   int32_t* new_lens;
   int32_t* remap;
   int32_t new_each, slots;                              // slots of the table of pages that rows go on writing
+  int32_t words;                                        // of 32 pages that a warp looks at in a round: 32, fewer in a small pool, whose pages all warps share
 };
 
 // A row of a call of reserve: tokens up to column c0 and `part` of it, room up to column c1, pages up to column `held` (of those that stay).
 struct Row {
   int c0, part, c1, held;
+  int was;                                              // pages before the call
   int want;                                             // the page that the row goes on writing, -1: none
   int replaced;                                         // twice the entries to be replaced, + 1 if that one is among them
   int first;                                            // how many hold it; then the rank of the row's first new page
@@ -64,6 +66,10 @@ int slots_of(int batch) {
   int n = 64;
   while (n < 2 * batch) n *= 2;
   return n;
+}
+int words_of(const rr_page_pool& p) {
+  const int n = (p.num_pages + ROUND / 32 - 1) / (ROUND / 32);
+  return n < 32 ? n : 32;
 }
 size_t row_state(const rr_page_pool& p) { return sizeof(Row) * up4(p.batch) + sizeof(Slot) * slots_of(p.batch); }
 size_t list_ints(const rr_page_pool& p) {
@@ -114,12 +120,16 @@ __device__ __forceinline__ int2 cluster_prefix(cg::cluster_group& cl, Shared& s,
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (lane == 0) s.warp[warp] = count;
   __syncthreads();
-  const int x = warp_prefix(lane < NW ? s.warp[lane] : 0);
-  const int before = __shfl_sync(0xFFFFFFFFu, x, warp) - count, cta = __shfl_sync(0xFFFFFFFFu, x, 31);
+  const int x = lane < NW ? s.warp[lane] : 0;
   int* const places = s.cta[round & 1];
   ++round;
-  if (threadIdx.x < CL) *cl.map_shared_rank(places + cl.block_rank(), threadIdx.x) = cta;
-  cl.sync();
+  if (warp == 0) {
+    const int cta = warp_sum(x);
+    if (lane < CL) *cl.map_shared_rank(places + cl.block_rank(), lane) = cta;
+  }
+  auto all_here = cl.barrier_arrive();
+  const int before = warp_sum(lane < warp ? x : 0);
+  cl.barrier_wait(std::move(all_here));
   const int theirs = lane < CL ? places[lane] : 0;
   return make_int2(before + warp_sum(lane < (int)cl.block_rank() ? theirs : 0), warp_sum(theirs));
 }
@@ -127,25 +137,29 @@ __device__ __forceinline__ int2 cluster_prefix(cg::cluster_group& cl, Shared& s,
 // Code is kept short, with loops left as loops where nothing waits for them: a kernel of this kind runs every instruction about once, and what it
 // spent most of its time on was fetching 70 KB of them.
 
-// Bit l of lane k: page first + 32 k + l is free.
-__device__ __noinline__ uint32_t free_bits(const int32_t* refs, int num_pages, long long first) {
-  const int lane = threadIdx.x & 31;
-  if (first >= num_pages) return 0;
-  const int n = (int)min((long long)num_pages - first, (long long)WARP_PAGES) - lane;
-  int v[32];
-#pragma unroll
-  for (int k = 0; k < 32; ++k) v[k] = 32 * k < n ? __ldcg(refs + first + lane + 32 * k) : 1;
-  uint32_t bits = 0;
-#pragma unroll
-  for (int k = 0; k < 32; ++k) {
-    const uint32_t word = __ballot_sync(0xFFFFFFFFu, v[k] == 0);
-    if (lane == k) bits = word;
-  }
-  return bits;
+// The first page of this warp in a round that begins at page `at`.
+__device__ __forceinline__ long long first_page(cg::cluster_group& cl, int words, long long at) {
+  return at + ((long long)cl.block_rank() * NW + (threadIdx.x >> 5)) * 32 * words;
 }
 
-__device__ __forceinline__ long long first_page(cg::cluster_group& cl, long long round) {
-  return round + (long long)cl.block_rank() * CTA_PAGES + (threadIdx.x >> 5) * WARP_PAGES;
+// Bit l of lane k (< words): page first + 32 k + l is free.
+__device__ __noinline__ uint32_t free_bits(const int32_t* refs, int num_pages, int words, long long first) {
+  const int lane = threadIdx.x & 31;
+  if (first >= num_pages) return 0;
+  const int n = (int)min((long long)num_pages - first, 32LL * words) - lane;
+  uint32_t bits = 0;
+#pragma unroll 1
+  for (int k0 = 0; k0 < words; k0 += 8) {
+    int v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 32 * (k0 + k) < n ? __ldcg(refs + first + lane + 32 * (k0 + k)) : 1;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t word = __ballot_sync(0xFFFFFFFFu, v[k] == 0);
+      if (lane == k0 + k) bits = word;
+    }
+  }
+  return bits;
 }
 
 // ---- fork -------------------------------------------------------------------------------------------------------
@@ -215,11 +229,11 @@ fork_kernel(const __grid_constant__ PoolParams P) {
 }
 
 // ---- reserve ----------------------------------------------------------------------------------------------------
-__device__ __forceinline__ Row row_of(const PoolParams& P, int b, int& held, bool tell) {
+__device__ __forceinline__ Row row_of(const PoolParams& P, int b, bool tell) {
   const rr_page_pool& p = P.p;
   const long long cap = (long long)p.page_tokens * p.pages_per_seq;
   int len = P.lens[b], more = P.arg ? P.arg[b] : P.new_each;
-  held = held_of(p, b);
+  const int held = held_of(p, b);
   const bool bad = len < 0 || more < 0 || (long long)len + more > cap;
   if (bad) {
     if (tell) report(p, RR_STATUS_BAD_INDEX);
@@ -232,6 +246,7 @@ __device__ __forceinline__ Row row_of(const PoolParams& P, int b, int& held, boo
   r.part = (int)((unsigned)len - (unsigned)r.c0 * page);
   r.c1 = (int)(upto / page);
   r.c1 += (unsigned)r.c1 * page != upto;
+  r.was = held;
   r.held = min(held, r.c1);
   r.want = more > 0 && r.part > 0 && r.c0 < r.held ? 0 : -1;
   r.replaced = r.first = 0;
@@ -286,7 +301,7 @@ __device__ __forceinline__ Slot* slot_of(Slot* slots, int mask, int page, bool a
   }
 }
 
-constexpr int LOOK = 8;                                 // entries of a row that a lane loads together
+constexpr int LOOK = 4;                                 // entries of a row that a lane loads together
 constexpr int NEAR = 4;                                 // entries behind a row's tokens that its thread looks at itself
 
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT, 1)
@@ -311,8 +326,7 @@ reserve_kernel(const __grid_constant__ PoolParams P) {
   bool longest = false, shorter = false;
   for (int i = threadIdx.x; i < P.slots; i += NT) slots[i] = Slot{-1, 0, INT32_MAX};
   for (int b = threadIdx.x; b < p.batch; b += NT) {
-    int held;
-    Row r = row_of(P, b, held, rank == 0);
+    Row r = row_of(P, b, rank == 0);
     const int32_t* const row = p.page_table + b * p.table_stride;
     const int c = r.c0 + (r.part > 0);
     if (r.want == 0) r.want = __ldcg(row + r.c0);
@@ -325,7 +339,7 @@ reserve_kernel(const __grid_constant__ PoolParams P) {
       if (rank == 0) report(p, RR_STATUS_BAD_INDEX);
     }
     longest |= r.held - c > NEAR;
-    shorter |= held > r.c1;
+    shorter |= r.was > r.c1;
     rows[b] = r;
   }
   longest = __syncthreads_or(longest);
@@ -334,10 +348,10 @@ reserve_kernel(const __grid_constant__ PoolParams P) {
     const int parts = (p.pages_per_seq + COLS - 1) / COLS;
     const int each = (p.batch * parts + CL * NW - 1) / (CL * NW);       // (neighbours by one warp: rows that end tend to alternate with such that stay)
     for (int u = warp * each; u < min((warp + 1) * each, p.batch * parts); ++u) {
-      const int b = u / parts, c0 = (u - b * parts) * COLS, held = held_of(p, b);
+      const int b = u / parts, c0 = (u - b * parts) * COLS, end = min(rows[b].was, c0 + COLS);
       int32_t* const row = p.page_table + b * p.table_stride;
-#pragma unroll 2
-      for (int c = max(rows[b].c1, c0) + lane; c < min(held, c0 + COLS); c += 32) {
+#pragma unroll 4
+      for (int c = max(rows[b].c1, c0) + lane; c < end; c += 32) {
         const int id = row[c];
         row[c] = -1;
         if (in_pool(p, id)) freed += release(p, id);
@@ -348,16 +362,17 @@ reserve_kernel(const __grid_constant__ PoolParams P) {
   }
   // 2. nothing changes now.  The free pages of this thread; the rows' entries to be replaced: a page that others hold too and that not all who hold it
   // go on writing with this row as the first of them, and pages behind it that others hold
-  int near_refs[NEAR];
+  int near_refs[NEAR], holders_first = 0;
   if (threadIdx.x < p.batch) {
 #pragma unroll
     for (int i = 0; i < NEAR; ++i) near_refs[i] = in_pool(p, ids[i]) ? __ldcg(p.refs + ids[i]) : 2;
+    if (const int want = rows[threadIdx.x].want; want >= 0) holders_first = __ldcg(p.refs + want);
   }
-  uint32_t bits = free_bits(p.refs, p.num_pages, first_page(cl, 0));
+  uint32_t bits = free_bits(p.refs, p.num_pages, P.words, first_page(cl, P.words, 0));
   for (int b = threadIdx.x; b < p.batch; b += NT) {
     const int want = rows[b].want;
     if (want < 0) continue;
-    const int holders = __ldcg(p.refs + want);
+    const int holders = b == threadIdx.x ? holders_first : __ldcg(p.refs + want);
     rows[b].first = holders;
     if (holders > 1) {
       Slot* const t = slot_of(slots, P.slots - 1, want, true);
@@ -443,8 +458,8 @@ reserve_kernel(const __grid_constant__ PoolParams P) {
     const bool near = p.num_pages <= ROUND && total <= GIVEN;
     int found = 0, from = 0;
     for (long long at = 0; at < p.num_pages && found < total; at += ROUND) {
-      const long long first = first_page(cl, at);
-      if (at > 0) bits = free_bits(p.refs, p.num_pages, first);
+      const long long first = first_page(cl, P.words, at);
+      if (at > 0) bits = free_bits(p.refs, p.num_pages, P.words, first);
       const int2 n = cluster_prefix(cl, s, warp_sum(__popc(bits)), round);
       if (near) {
         if (my_warp == 0) s_scan[0] = n.x;
@@ -475,7 +490,7 @@ reserve_kernel(const __grid_constant__ PoolParams P) {
   for (int b = threadIdx.x; b < p.batch; b += NT) {
     if (b % CL != rank) continue;
     const int held = enough ? rows[b].c1 : rows[b].held;
-    if (__ldcg(p.held + b) != held) p.held[b] = held;
+    if (rows[b].was != held) p.held[b] = held;
   }
   add_free(p, freed + freed_now);
 }
@@ -495,7 +510,7 @@ compact_kernel(const __grid_constant__ PoolParams P) {
   uint32_t bits = 0;
   int2 n = make_int2(0, 0);
   for (long long at = 0; at < p.num_pages; at += ROUND) {
-    bits = free_bits(p.refs, p.num_pages, first_page(cl, at));
+    bits = free_bits(p.refs, p.num_pages, P.words, first_page(cl, P.words, at));
     n = cluster_prefix(cl, s, warp_sum(__popc(bits)), round);
     free_all += n.y;
   }
@@ -505,14 +520,14 @@ compact_kernel(const __grid_constant__ PoolParams P) {
   int32_t* const src = P.w.list + p.num_pages;
   int before = 0, low = 0;
   for (long long at = 0; at < p.num_pages; at += ROUND) {
-    const long long first = first_page(cl, at);
+    const long long first = first_page(cl, P.words, at);
     if (!one_round) {
-      bits = free_bits(p.refs, p.num_pages, first);
+      bits = free_bits(p.refs, p.num_pages, P.words, first);
       n = cluster_prefix(cl, s, warp_sum(__popc(bits)), round);
     }
     const int upto = before + n.x + warp_prefix(__popc(bits)) - __popc(bits);
 #pragma unroll 1
-    for (int k = 0; k < 32 && first + 32 * k < p.num_pages; ++k) {
+    for (int k = 0; k < P.words && first + 32 * k < p.num_pages; ++k) {
       const uint32_t word = __shfl_sync(0xFFFFFFFFu, bits, k);
       const int page = (int)first + 32 * k + lane, rank = __shfl_sync(0xFFFFFFFFu, upto, k) + __popc(word & ((1u << lane) - 1));
       const bool is_free = word >> lane & 1;
@@ -810,7 +825,7 @@ extern "C" int rr_pages_fork(const rr_page_pool* pool, const int32_t* parents, c
   if (!parents || !lens || !new_lens || lens == new_lens || parents == new_lens) return RR_ERR_INVALID_ARG;
   if (((uintptr_t)parents | (uintptr_t)lens | (uintptr_t)new_lens) & 3) return RR_ERR_INVALID_ARG;
   if ((rc = check_workspace(pool, workspace, bytes)) != RR_OK) return rc;
-  PoolParams P{*pool, work_of(*pool, workspace), parents, lens, new_lens, nullptr, 0, 0};
+  PoolParams P{*pool, work_of(*pool, workspace), parents, lens, new_lens, nullptr, 0, 0, 0};
   return launch_pool(fork_kernel, P, FORK_NT, pool->batch > ROWS_ON_CHIP ? 0 : sizeof(Heir) * pool->batch, (cudaStream_t)stream, "rr_pages_fork");
 }
 
@@ -821,7 +836,7 @@ extern "C" int rr_pages_reserve(const rr_page_pool* pool, const int32_t* lens, c
   if (!lens || (((uintptr_t)lens | (uintptr_t)new_tokens) & 3) || (!new_tokens && new_each < 0)) return RR_ERR_INVALID_ARG;
   if ((rc = check_caches(pool, caches, n)) != RR_OK) return rc;
   if ((rc = check_workspace(pool, workspace, bytes)) != RR_OK) return rc;
-  PoolParams P{*pool, work_of(*pool, workspace), new_tokens, lens, nullptr, nullptr, new_each, slots_of(pool->batch)};
+  PoolParams P{*pool, work_of(*pool, workspace), new_tokens, lens, nullptr, nullptr, new_each, slots_of(pool->batch), words_of(*pool)};
   static unsigned long long done = 0;
   constexpr size_t given = GIVEN * 4, most = given + sizeof(Row) * ROWS_ON_CHIP + sizeof(Slot) * 2 * ROWS_ON_CHIP;
   const cudaError_t e = rr_once_per_device(done, [] { return cudaFuncSetAttribute(reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most); });
@@ -837,7 +852,7 @@ extern "C" int rr_pages_compact(const rr_page_pool* pool, const rr_paged_kv* cac
   if ((uintptr_t)new_ids & 3) return RR_ERR_INVALID_ARG;
   if ((rc = check_caches(pool, caches, n)) != RR_OK) return rc;
   if ((rc = check_workspace(pool, workspace, bytes)) != RR_OK) return rc;
-  PoolParams P{*pool, work_of(*pool, workspace), nullptr, nullptr, nullptr, new_ids, 0, 0};
+  PoolParams P{*pool, work_of(*pool, workspace), nullptr, nullptr, nullptr, new_ids, 0, 0, words_of(*pool)};
   if (!P.remap) P.remap = P.w.ranked;
   rc = launch_pool(compact_kernel, P, NT, 0, (cudaStream_t)stream, "rr_pages_compact");
   return rc != RR_OK ? rc : launch_copies(P, caches, n, true, (cudaStream_t)stream, "rr_pages_compact");
