@@ -478,6 +478,7 @@ int rr_attend_paged_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, void*
  * Calls only enqueue work and may be captured.  A pool's calls change its state: order them on one stream (or
  * by events), with the operators that read the table.  The workspace holds nothing between calls. */
 #define RR_PAGES_MAX_PAGES (1 << 28)
+#define RR_PAGES_MAX_BATCH (1 << 20)
 typedef struct rr_page_pool {
   int32_t* page_table;       /* [batch, pages_per_seq], rows table_stride apart                   */
   int32_t* refs;             /* [num_pages]                                                       */

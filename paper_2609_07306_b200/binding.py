@@ -28,6 +28,7 @@ RR_STATUS_TIMEOUT = 1
 RR_STATUS_BAD_INDEX = 2
 RR_STATUS_NO_PAGES = 4
 RR_PAGES_MAX_PAGES = 1 << 28
+RR_PAGES_MAX_BATCH = 1 << 20
 RR_NUM_COUNTERS = 8
 RR_NUM_KINDS = 12
 COUNTER_NAMES = ("layer_calls", "anchor_rows", "relay_rows", "flagged_rows", "cand_pairs",

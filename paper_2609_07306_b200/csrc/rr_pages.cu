@@ -170,7 +170,7 @@ struct Heir { int parent, held, takes; };               // pages that the row he
 
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(FORK_NT, 1)
 fork_kernel(const __grid_constant__ PoolParams P) {
-  extern __shared__ char on_chip[];
+  extern __shared__ __align__(16) char on_chip[];
   cg::cluster_group cl = cg::this_cluster();
   const rr_page_pool& p = P.p;
   const int lane = threadIdx.x & 31, rank = cl.block_rank(), warp = (threadIdx.x >> 5) * CL + rank;
@@ -306,7 +306,7 @@ constexpr int NEAR = 4;                                 // entries behind a row'
 
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT, 1)
 reserve_kernel(const __grid_constant__ PoolParams P) {
-  extern __shared__ char on_chip[];
+  extern __shared__ __align__(16) char on_chip[];
   __shared__ Shared s;
   __shared__ int s_scan[NW];
   cg::cluster_group cl = cg::this_cluster();
@@ -731,7 +731,7 @@ int check_pool(const rr_page_pool* p) {
   if (p->num_pages < 1 || p->page_tokens < 1 || p->batch < 1 || p->pages_per_seq < 1) return RR_ERR_INVALID_ARG;
   if (p->table_stride < (p->batch > 1 ? p->pages_per_seq : 0)) return RR_ERR_INVALID_ARG;
   if (((uintptr_t)p->page_table | (uintptr_t)p->refs | (uintptr_t)p->held | (uintptr_t)p->free_pages | (uintptr_t)p->status) & 3) return RR_ERR_INVALID_ARG;
-  if (p->num_pages > RR_PAGES_MAX_PAGES || (int64_t)p->batch * p->pages_per_seq > (1 << 30)) return RR_ERR_TOO_LARGE;
+  if (p->num_pages > RR_PAGES_MAX_PAGES || p->batch > RR_PAGES_MAX_BATCH || (int64_t)p->batch * p->pages_per_seq > (1 << 30)) return RR_ERR_TOO_LARGE;
   return RR_OK;
 }
 int check_workspace(const rr_page_pool* p, const void* ws, size_t bytes) {

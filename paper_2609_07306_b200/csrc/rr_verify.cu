@@ -16,6 +16,7 @@
 // allow it; only maxima are taken (a packed maximum of two bf16 costs one instruction), a thread keeps its first best vector, and the entry inside it is looked
 // up at the end.  The rows' best tokens go to `out`, where a second kernel, a warp per sequence, compares them with the drafts.
 #include <cooperative_groups.h>
+#include <utility>
 #include "rr_paged.cuh"
 
 namespace cg = cooperative_groups;
@@ -225,17 +226,21 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
     // every warp finds the CTA that has the threshold
     const double theirs = lane < ctas ? *cl.map_shared_rank(&f.total, lane) : 0.0;
     const double limit = u * warp_sum(theirs);
+    auto read = cl.barrier_arrive();                    // (each CTA waits for the others to have read its total before it ends or writes another one)
     Hit h = find(theirs, 0.0, limit);
-    cl.sync();                                          // the totals have been read (nothing of another CTA's is read from here on)
     if (h.at == 32) {                                   // no weight: the rejected row has no more than the draft's anywhere
       none = !q && but < 0;
+      cl.barrier_wait(std::move(read));
       if (none) break;
       q = nullptr;
       but = -1;
       continue;
     }
     here = h.at == cta;
-    if (!here || warp != 0) break;
+    if (!here || warp != 0) {
+      cl.barrier_wait(std::move(read));
+      break;
+    }
     // the kept sum, then the block, then the entry
     double before = h.before, run = before;
     k = 0;
@@ -268,6 +273,7 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
       }
       __syncwarp();
     }
+    cl.barrier_wait(std::move(read));
     break;
   }
   // the CTA that has the token, or the first one where all weights are 0

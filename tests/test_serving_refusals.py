@@ -87,7 +87,7 @@ BIG = 1 << 40
 POOL = [(dict(page_table=None), INVALID), (dict(refs=None), INVALID), (dict(held=None), INVALID), (dict(free_pages=None), INVALID),
         (dict(num_pages=0), INVALID), (dict(page_tokens=0), INVALID), (dict(batch=0), INVALID), (dict(pages_per_seq=0), INVALID),
         (dict(table_stride=7), INVALID), (dict(table_stride=-1, batch=1), INVALID), (dict(refs=0x40002), INVALID), (dict(status=0x40001), INVALID),
-        (dict(num_pages=B.RR_PAGES_MAX_PAGES + 1), TOO_LARGE), (dict(batch=1 << 20, pages_per_seq=1 << 12, table_stride=1 << 12), TOO_LARGE)]
+        (dict(num_pages=B.RR_PAGES_MAX_PAGES + 1), TOO_LARGE), (dict(batch=B.RR_PAGES_MAX_BATCH + 1, pages_per_seq=1), TOO_LARGE), (dict(batch=1 << 20, pages_per_seq=1 << 12, table_stride=1 << 12), TOO_LARGE)]
 
 
 def calls(p, caches, n, ws=0x100, nbytes=BIG, lens=0x1000, arg=0x2000, out=0x3000, each=0, ids=None):
