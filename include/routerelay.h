@@ -475,6 +475,7 @@ int rr_attend_paged_ranges(const rr_paged_kv* kv, const rr_ranges_args* a, void*
  * Pages are handed out in ascending order of their numbers, the lowest free ones first, to the sequences in their order: the
  * results do not depend on timing.  Ids outside the pool, negative lengths and lengths behind the table's end set RR_STATUS_BAD_INDEX in
  * *status; an id is left out, a length taken as the nearest that the table holds.
+ * RR_STATUS_TIMEOUT, as with the operators above, means that copies of pages are missing.
  * Calls only enqueue work and may be captured.  A pool's calls change its state: order them on one stream (or
  * by events), with the operators that read the table.  The workspace holds nothing between calls. */
 #define RR_PAGES_MAX_PAGES (1 << 28)
@@ -525,7 +526,7 @@ int rr_pages_compact(const rr_page_pool* pool, const rr_paged_kv* caches, int32_
  * Writes, for each row of a sequence, the token that follows it: the accepted drafts, the token more, then -1; rows behind cu[batch] are left as they
  * were.  accepted[b] is the number of accepted drafts, new_lens[b] (if given) = lens[b] + accepted[b] + 1, the tokens that stay of a sequence that had
  * lens[b] before its rows were appended (a sequence without rows: 0 accepted, lens[b]).  A drafted token outside the vocabulary is rejected and sets
- * RR_STATUS_BAD_INDEX in *status (if given).  No workspace. */
+ * RR_STATUS_BAD_INDEX in *status (if given); RR_STATUS_TIMEOUT there, as with the paged operators, means that the results are not to be used.  No workspace. */
 typedef struct rr_verify_args {
   const void* target;        /* [rows, vocab], rows target_stride apart                           */
   const void* draft;         /* [rows, vocab], rows draft_stride apart, or NULL; a sequence's last row is not read */

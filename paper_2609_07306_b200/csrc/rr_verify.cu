@@ -11,7 +11,9 @@
 // finds for itself (a few dependent loads, instead of a barrier).  A warp reads a block of 256 entries at a time, eight per lane from each row, the next block's loads
 // in front of this one's arithmetic, and leaves its lanes' sums; the CTAs exchange their totals, the one that has the threshold finds block and
 // entry, so the row is read once but for that block.  Products, differences and sums are 64-bit: the first two are exact for probabilities of up
-// to 24 bits, and a sum over the vocabulary is off by some 1e-14, so that a random number falls between two results about never.
+// to 24 bits, and a sum over the vocabulary is off by some 1e-14, so that a random number falls between two results about never.  That arithmetic costs as
+// much as the memory: 64 sequences against 131071 tokens (49 MB read) 21 us with two conversions and four selections an entry, 17 us with eight instructions.
+// (Rings of blocks in shared memory, filled by bulk copies: 27 us; fewer warps fit, and each has its chain of 64-bit sums.)
 // Greedy: a cluster takes a row, whoever's it is (sequences with many drafts would hold up the others), 16 bytes at a time where rows
 // allow it; only maxima are taken (a packed maximum of two bf16 costs one instruction), a thread keeps its first best vector, and the entry inside it is looked
 // up at the end.  The rows' best tokens go to `out`, where a second kernel, a warp per sequence, compares them with the drafts.
@@ -65,6 +67,21 @@ __device__ __forceinline__ bool in_vocab(const rr_verify_args& a, int x) {
 }
 
 // ---- sampled ----------------------------------------------------------------------------------------------------
+// max(p - q, 0) of an entry, 0 at the entry `but` (-1: none) and behind the row.
+template <typename T>
+__device__ __forceinline__ double weight_of(const T* prow, const T* qrow, int vocab, int j, int but) {
+  if (j >= vocab || j == but) return 0.0;
+  const float x = weight(rr_to_f32(__ldg(prow + j))), y = qrow ? weight(rr_to_f32(__ldg(qrow + j))) : 0.f;
+  return x > y ? (double)x - (double)y : 0.0;
+}
+template <typename T>
+__device__ __noinline__ double one_by_one(const T* prow, const T* qrow, int vocab, int first, int but) {
+  double s = 0.0;
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) s += weight_of(prow, qrow, vocab, first + (int)(threadIdx.x & 31) + 32 * i, but);
+  return s;
+}
+
 // A block of a row of the target's and of one of the draft's (0 where there is none): entries first + lane + 32 i.
 template <typename T> struct Block {
   T p[8], q[8];
@@ -86,40 +103,25 @@ template <typename T> struct Block {
       }
     }
   }
-  // max(p - q, 0), 0 at the entry `but` (-1: none)
-  __device__ __forceinline__ double weight_at(int i, int first, int but, bool with_q) const {
-    const float x = weight(rr_to_f32(p[i])), y = with_q ? weight(rr_to_f32(q[i])) : 0.f;
-    return x > y && first + (int)(threadIdx.x & 31) + 32 * i != but ? (double)x - (double)y : 0.0;
-  }
-  // The sum of the lane's eight weights.  Where x > y >= 0, x - y is d = fl(x - y) and the rest (x - d) - y, which FP32 holds without error: one conversion
-  // instead of two; the rests, 2^-24 of their terms and less, are added in FP32.
-  __device__ __forceinline__ double sum(int first, int but, bool with_q) const {
-    if (but >= first && but < first + BLOCK) {          // (one block of a row)
-      double s = 0.0;
-#pragma unroll 1
-      for (int j = 0; j < 8; ++j) {
-        T pj = p[0], qj = q[0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) if (i == j) pj = p[i], qj = q[i];
-        const float x = weight(rr_to_f32(pj)), y = with_q ? weight(rr_to_f32(qj)) : 0.f;
-        s += x > y && first + (int)(threadIdx.x & 31) + 32 * j != but ? (double)x - (double)y : 0.0;
-      }
-      return s;
-    }
+  // The sum of the lane's eight weights, by eight instructions each.  With z = max(x, y), where x - y is below 0 or x is NaN it is 0; elsewhere z - y is d = fl(z - y) and the
+  // rest (z - d) - y, which FP32 holds without error, as z >= y >= 0: one conversion instead of two; the rests, 2^-24 of their terms and less, are added in
+  // FP32.  An infinite number makes a sum that is none, and the eight are looked at one by one, as are those of the block with `but`.
+  __device__ __forceinline__ double sum(const T* prow, const T* qrow, int vocab, int first, int but) const {
     double s[2] = {0.0, 0.0};
     float rest = 0.f;
+    if (qrow) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float x = rr_to_f32(p[i]);
-      if (with_q) {
-        const float y = weight(rr_to_f32(q[i])), d = x - y, w = weight(d);       // (an x that is none of a probability makes no positive and finite d)
-        rest += w != 0.f ? (x - d) - y : 0.f;
-        s[i & 1] += (double)w;
-      } else {
-        s[i & 1] += (double)weight(x);
+      for (int i = 0; i < 8; ++i) {
+        const float y = fmaxf(rr_to_f32(q[i]), 0.f), z = fmaxf(rr_to_f32(p[i]), y), d = z - y;
+        rest += (z - d) - y;
+        s[i & 1] += (double)d;
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i & 1] += (double)fmaxf(rr_to_f32(p[i]), 0.f);
     }
-    return s[0] + s[1] + (double)rest;
+    const double all = s[0] + s[1] + (double)rest;
+    return !isfinite(all) || (but >= first && but < first + BLOCK) ? one_by_one(prow, qrow, vocab, first, but) : all;
   }
 };
 
@@ -198,7 +200,7 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
       const bool last = i + 1 >= min((k + 1) * per, mine);
       const int k_next = last ? k + NW : k, i_next = last ? k_next * per : i + 1;
       if (k_next < sums) next.load(p, q, a.vocab, (from + i_next) * BLOCK);
-      sum += now.sum(at, but, q != nullptr);
+      sum += now.sum(p, q, a.vocab, at, but);
       if (last) {
         f.lanes[k][lane] = sum;
         sum = 0.0;
@@ -256,9 +258,8 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
 #pragma unroll 1
     for (int i = k * per; i < min((k + 1) * per, mine) && !h.over; ++i) {
       const int at = (from + i) * BLOCK;
-      now.load(p, q, a.vocab, at);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f.lanes[e][lane] = now.weight_at(e, at, but, q != nullptr);
+      for (int e = 0; e < 8; ++e) f.lanes[e][lane] = weight_of(p, q, a.vocab, at + lane + 32 * e, but);
       __syncwarp();
       double x = 0.0;                                   // four lanes add up 32 entries, then these
 #pragma unroll
