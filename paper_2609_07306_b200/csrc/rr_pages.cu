@@ -179,12 +179,12 @@ fork_kernel(const __grid_constant__ PoolParams P) {
   rr_pdl_trigger();
   for (int b = threadIdx.x; b < p.batch; b += FORK_NT) {     // in every CTA
     const bool tell = rank == 0;
-    Heir h{P.arg[b], held_of(p, b), -1};
+    Heir h{__ldcg(P.arg + b), held_of(p, b), -1};
     if (h.parent < -1 || h.parent >= p.batch) {
       if (tell) report(p, RR_STATUS_BAD_INDEX);
       h.parent = b;
     }
-    const int len = h.parent < 0 ? 0 : P.lens[h.parent];
+    const int len = h.parent < 0 ? 0 : __ldcg(P.lens + h.parent);
     if (h.parent != b) h.takes = h.parent < 0 ? 0 : (int)min((unsigned)held_of(p, h.parent), ((unsigned)max(len, 0) + p.page_tokens - 1) / p.page_tokens);
     if (tell) {
       if (len < 0) report(p, RR_STATUS_BAD_INDEX);
@@ -205,7 +205,7 @@ fork_kernel(const __grid_constant__ PoolParams P) {
     const int end = min(max(h.held, h.takes), c0 + COLS);
 #pragma unroll 2
     for (int c = c0 + lane; c < end; c += 32) {
-      const int was = c < h.held ? mine[c] : -1, is = c < h.takes ? theirs[c] : -1;
+      const int was = c < h.held ? __ldcg(mine + c) : -1, is = c < h.takes ? __ldcg(theirs + c) : -1;
       stage[c] = is;
       if (was == is) continue;
       if (in_pool(p, is)) freed -= atomicAdd(p.refs + is, 1) == 0;      // (one row may let go of a page before another takes it)
@@ -232,7 +232,7 @@ fork_kernel(const __grid_constant__ PoolParams P) {
 __device__ __forceinline__ Row row_of(const PoolParams& P, int b, bool tell) {
   const rr_page_pool& p = P.p;
   const long long cap = (long long)p.page_tokens * p.pages_per_seq;
-  int len = P.lens[b], more = P.arg ? P.arg[b] : P.new_each;
+  int len = __ldcg(P.lens + b), more = P.arg ? __ldcg(P.arg + b) : P.new_each;
   const int held = held_of(p, b);
   const bool bad = len < 0 || more < 0 || (long long)len + more > cap;
   if (bad) {
@@ -352,7 +352,7 @@ reserve_kernel(const __grid_constant__ PoolParams P) {
       int32_t* const row = p.page_table + b * p.table_stride;
 #pragma unroll 4
       for (int c = max(rows[b].c1, c0) + lane; c < end; c += 32) {
-        const int id = row[c];
+        const int id = __ldcg(row + c);
         row[c] = -1;
         if (in_pool(p, id)) freed += release(p, id);
         else report(p, RR_STATUS_BAD_INDEX);
@@ -578,7 +578,7 @@ __device__ __forceinline__ void renumber(const CopyParams& P, int moves) {
     const int held = held_of(P.p, b);
 #pragma unroll 4
     for (int c = threadIdx.x; c < held; c += blockDim.x) {
-      const int id = row[c];
+      const int id = __ldcg(row + c);
       if (!in_pool(P.p, id)) report(P.p, RR_STATUS_BAD_INDEX);
       else if (id >= live) row[c] = __ldcg(P.remap + id);
     }

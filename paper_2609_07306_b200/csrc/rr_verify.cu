@@ -25,13 +25,16 @@ namespace cg = cooperative_groups;
 
 namespace {
 
+// The kernels may be launched before the one in front of them has ended (rr_launch_pdl): what they read comes from L2, where that one's results are
+// when rr_pdl_wait returns, and never by way of the read-only path.
+
 constexpr int NT = 256, NW = NT / 32, BLOCK = 256, MAX_CL = 8;
 constexpr int SUMS = 64;                                // blocks' sums that a CTA keeps
 
 struct Span { int first, n; };                          // a sequence's first row, its drafts (-1: it has no rows)
 
 __device__ __forceinline__ Span span_of(const rr_verify_args& a, int b) {
-  const int first = a.cu ? max(__ldg(a.cu + b), 0) : b, end = a.cu ? min(__ldg(a.cu + b + 1), a.rows) : b + 1;
+  const int first = a.cu ? max(__ldcg(a.cu + b), 0) : b, end = a.cu ? min(__ldcg(a.cu + b + 1), a.rows) : b + 1;
   return Span{first, max(end - first, 0) - 1};
 }
 
@@ -39,7 +42,7 @@ __device__ __forceinline__ Span span_of(const rr_verify_args& a, int b) {
 __device__ __forceinline__ float weight(float x) { return __float_as_uint(x) - 1u < 0x7F7FFFFFu ? x : 0.f; }
 template <typename T>
 __device__ __forceinline__ double probability(const void* rows, int64_t stride, int row, int x) {
-  return weight(rr_to_f32(__ldg((const T*)rows + row * stride + x)));
+  return weight(rr_to_f32(__ldcg((const T*)rows + row * stride + x)));
 }
 
 __device__ __forceinline__ double warp_sum(double x) {
@@ -49,13 +52,13 @@ __device__ __forceinline__ double warp_sum(double x) {
 }
 __device__ __forceinline__ void write_lengths(const rr_verify_args& a, int b, const Span& s, int accepted) {
   a.accepted[b] = accepted;
-  if (a.new_lens) a.new_lens[b] = a.lens[b] + (s.n < 0 ? 0 : accepted + 1);
+  if (a.new_lens) a.new_lens[b] = __ldcg(a.lens + b) + (s.n < 0 ? 0 : accepted + 1);
 }
 // A sequence's results; `more`: the token behind the accepted drafts.
 __device__ __forceinline__ void write_accepted(const rr_verify_args& a, int b, const Span& s, int accepted, int more) {
   const int lane = threadIdx.x & 31;
   for (int i = lane; i <= s.n; i += 32)
-    a.out[s.first + i] = i < accepted ? a.tokens[s.first + i + 1] : i == accepted ? more : -1;
+    a.out[s.first + i] = i < accepted ? __ldcg(a.tokens + s.first + i + 1) : i == accepted ? more : -1;
   if (lane == 0) write_lengths(a, b, s, accepted);
 }
 
@@ -71,7 +74,7 @@ __device__ __forceinline__ bool in_vocab(const rr_verify_args& a, int x) {
 template <typename T>
 __device__ __forceinline__ double weight_of(const T* prow, const T* qrow, int vocab, int j, int but) {
   if (j >= vocab || j == but) return 0.0;
-  const float x = weight(rr_to_f32(__ldg(prow + j))), y = qrow ? weight(rr_to_f32(__ldg(qrow + j))) : 0.f;
+  const float x = weight(rr_to_f32(__ldcg(prow + j))), y = qrow ? weight(rr_to_f32(__ldcg(qrow + j))) : 0.f;
   return x > y ? (double)x - (double)y : 0.0;
 }
 template <typename T>
@@ -89,17 +92,17 @@ template <typename T> struct Block {
     const int j0 = first + (threadIdx.x & 31);
     if (first + BLOCK <= vocab) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = __ldg(prow + j0 + 32 * i);
+      for (int i = 0; i < 8; ++i) p[i] = __ldcg(prow + j0 + 32 * i);
       if (qrow) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = __ldg(qrow + j0 + 32 * i);
+        for (int i = 0; i < 8; ++i) q[i] = __ldcg(qrow + j0 + 32 * i);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const bool in = j0 + 32 * i < vocab;
-        p[i] = in ? __ldg(prow + j0 + 32 * i) : rr_from_f32<T>(0.f);
-        q[i] = in && qrow ? __ldg(qrow + j0 + 32 * i) : rr_from_f32<T>(0.f);
+        p[i] = in ? __ldcg(prow + j0 + 32 * i) : rr_from_f32<T>(0.f);
+        q[i] = in && qrow ? __ldcg(qrow + j0 + 32 * i) : rr_from_f32<T>(0.f);
       }
     }
   }
@@ -164,8 +167,8 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
     const int i = i0 + lane, t = s.first + i;
     bool ok = true;
     if (i < s.n) {
-      const int x = __ldg(a.tokens + t + 1);
-      const double u = __ldg(a.uniform + t);
+      const int x = __ldcg(a.tokens + t + 1);
+      const double u = __ldcg(a.uniform + t);
       ok = in_vocab(a, x);
       if (ok) {
         const double p = probability<T>(a.target, a.target_stride, t, x), q = a.draft ? probability<T>(a.draft, a.draft_stride, t, x) : 1.0;
@@ -182,9 +185,9 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
   int but = -1;
   if (accepted < s.n) {
     if (a.draft) q = (const T*)a.draft + row * a.draft_stride;
-    else but = __ldg(a.tokens + row + 1);
+    else but = __ldcg(a.tokens + row + 1);
   }
-  const double u = fmax((double)__ldg(a.uniform + s.first + s.n), 0.0);
+  const double u = fmax((double)__ldcg(a.uniform + s.first + s.n), 0.0);
   // blocks of this CTA; a kept sum stands for `per` of them
   const int blocks = (a.vocab + BLOCK - 1) / BLOCK, share = (blocks + ctas - 1) / ctas, from = min(cta * share, blocks), mine = min(share, blocks - from);
   const int per = (share + SUMS - 1) / SUMS, sums = (mine + per - 1) / per;
@@ -320,7 +323,7 @@ best_kernel(const __grid_constant__ rr_verify_args a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   rr_pdl_wait();
   rr_pdl_trigger();
-  if (a.cu && t >= __ldg(a.cu + a.batch)) return;       // padding (uniform in the cluster)
+  if (a.cu && t >= __ldcg(a.cu + a.batch)) return;       // padding (uniform in the cluster)
   using V = Vec<T, VEC>;
   const int vecs = a.vocab / VEC, share = (vecs + ctas - 1) / ctas, from = min(cta * share, vecs), to = min(from + share, vecs);
   const T* const row = (const T*)a.target + t * a.target_stride;
@@ -328,14 +331,14 @@ best_kernel(const __grid_constant__ rr_verify_args a) {
 #pragma unroll 8
   for (int v = from + threadIdx.x; v < to; v += NT) {
     V e;
-    if constexpr (VEC == 1) e.v = __ldg(row + v);
-    else { const uint4 raw = __ldg((const uint4*)row + v); e = *(const V*)&raw; }
+    if constexpr (VEC == 1) e.v = __ldcg(row + v);
+    else { const uint4 raw = __ldcg((const uint4*)row + v); e = *(const V*)&raw; }
     const uint32_t key = score_key(e.best());
     if (key > x.key) x = Best{key, v};
   }
   if (cta == ctas - 1 && threadIdx.x == 0)              // the entries behind the last vector
     for (int j = vecs * VEC; j < a.vocab; ++j)
-      if (const uint32_t key = score_key(rr_to_f32(__ldg(row + j))); key > x.key) x = Best{key, vecs};
+      if (const uint32_t key = score_key(rr_to_f32(__ldcg(row + j))); key > x.key) x = Best{key, vecs};
   x = warp_best(x);
   if (lane == 0) s_warp[warp] = x;
   __syncthreads();
@@ -343,7 +346,7 @@ best_kernel(const __grid_constant__ rr_verify_args a) {
     x = warp_best(lane < NW ? s_warp[lane] : Best{0u, INT32_MAX});
     // the first entry of the vector that is as good
     const int j = x.key ? x.at * VEC + lane : 0;
-    const unsigned same = __ballot_sync(0xFFFFFFFFu, x.key && lane < VEC && j < a.vocab && score_key(rr_to_f32(__ldg(row + j))) == x.key);
+    const unsigned same = __ballot_sync(0xFFFFFFFFu, x.key && lane < VEC && j < a.vocab && score_key(rr_to_f32(__ldcg(row + j))) == x.key);
     if (lane == 0) s_cta = Best{x.key, x.key ? x.at * VEC + __ffs(same) - 1 : INT32_MAX};
   }
   cl.sync();
@@ -367,7 +370,7 @@ compare_kernel(const __grid_constant__ rr_verify_args a) {
     const int i = i0 + lane;
     bool ok = true;
     if (i < s.n) {
-      const int x = __ldg(a.tokens + s.first + i + 1);
+      const int x = __ldcg(a.tokens + s.first + i + 1);
       ok = in_vocab(a, x) && x == __ldcg(a.out + s.first + i);
     }
     const unsigned rejected = __ballot_sync(0xFFFFFFFFu, !ok);
