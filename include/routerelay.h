@@ -534,7 +534,7 @@ typedef struct rr_verify_args {
   const int32_t* cu;         /* [batch + 1] ascending, cu[0] = 0; or NULL                         */
   const float* uniform;      /* [rows] in [0, 1), or NULL                                         */
   const int32_t* lens;       /* [batch], with new_lens                                            */
-  int32_t* out;              /* [rows]                                                            */
+  int32_t* out;              /* [rows], other memory than tokens                                  */
   int32_t* accepted;         /* [batch]                                                           */
   int32_t* new_lens;         /* [batch] or NULL; may be lens itself                               */
   uint32_t* status;

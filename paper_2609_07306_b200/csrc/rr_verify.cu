@@ -25,8 +25,8 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-// The kernels may be launched before the one in front of them has ended (rr_launch_pdl): what they read comes from L2, where that one's results are
-// when rr_pdl_wait returns, and never by way of the read-only path.
+// The kernels may be launched before the one in front of them has ended (rr_launch_pdl), so nothing is read by way of the read-only path.  Every CTA reads
+// the same few numbers in the beginning: through L1 (all from L2: 2 us more).
 
 constexpr int NT = 256, NW = NT / 32, BLOCK = 256, MAX_CL = 8;
 constexpr int SUMS = 64;                                // blocks' sums that a CTA keeps
@@ -34,7 +34,7 @@ constexpr int SUMS = 64;                                // blocks' sums that a C
 struct Span { int first, n; };                          // a sequence's first row, its drafts (-1: it has no rows)
 
 __device__ __forceinline__ Span span_of(const rr_verify_args& a, int b) {
-  const int first = a.cu ? max(__ldcg(a.cu + b), 0) : b, end = a.cu ? min(__ldcg(a.cu + b + 1), a.rows) : b + 1;
+  const int first = a.cu ? max(a.cu[b], 0) : b, end = a.cu ? min(a.cu[b + 1], a.rows) : b + 1;
   return Span{first, max(end - first, 0) - 1};
 }
 
@@ -42,7 +42,7 @@ __device__ __forceinline__ Span span_of(const rr_verify_args& a, int b) {
 __device__ __forceinline__ float weight(float x) { return __float_as_uint(x) - 1u < 0x7F7FFFFFu ? x : 0.f; }
 template <typename T>
 __device__ __forceinline__ double probability(const void* rows, int64_t stride, int row, int x) {
-  return weight(rr_to_f32(__ldcg((const T*)rows + row * stride + x)));
+  return weight(rr_to_f32(((const T*)rows)[row * stride + x]));
 }
 
 __device__ __forceinline__ double warp_sum(double x) {
@@ -52,13 +52,13 @@ __device__ __forceinline__ double warp_sum(double x) {
 }
 __device__ __forceinline__ void write_lengths(const rr_verify_args& a, int b, const Span& s, int accepted) {
   a.accepted[b] = accepted;
-  if (a.new_lens) a.new_lens[b] = __ldcg(a.lens + b) + (s.n < 0 ? 0 : accepted + 1);
+  if (a.new_lens) a.new_lens[b] = a.lens[b] + (s.n < 0 ? 0 : accepted + 1);
 }
-// A sequence's results; `more`: the token behind the accepted drafts.
-__device__ __forceinline__ void write_accepted(const rr_verify_args& a, int b, const Span& s, int accepted, int more) {
+// A sequence's results but the token behind the accepted drafts.
+__device__ __forceinline__ void write_accepted(const rr_verify_args& a, int b, const Span& s, int accepted) {
   const int lane = threadIdx.x & 31;
   for (int i = lane; i <= s.n; i += 32)
-    a.out[s.first + i] = i < accepted ? __ldcg(a.tokens + s.first + i + 1) : i == accepted ? more : -1;
+    if (i != accepted) a.out[s.first + i] = i < accepted ? a.tokens[s.first + i + 1] : -1;
   if (lane == 0) write_lengths(a, b, s, accepted);
 }
 
@@ -70,18 +70,20 @@ __device__ __forceinline__ bool in_vocab(const rr_verify_args& a, int x) {
 }
 
 // ---- sampled ----------------------------------------------------------------------------------------------------
-// max(p - q, 0) of an entry, 0 at the entry `but` (-1: none) and behind the row.
-template <typename T>
-__device__ __forceinline__ double weight_of(const T* prow, const T* qrow, int vocab, int j, int but) {
-  if (j >= vocab || j == but) return 0.0;
-  const float x = weight(rr_to_f32(__ldcg(prow + j))), y = qrow ? weight(rr_to_f32(__ldcg(qrow + j))) : 0.f;
-  return x > y ? (double)x - (double)y : 0.0;
+// max(p - q, 0) of an entry, 0 if it is left out.
+__device__ __forceinline__ double weight_of(float p, float q, bool out) {
+  const float x = weight(p), y = weight(q);
+  return x > y && !out ? (double)x - (double)y : 0.0;
 }
+// The lane's eight of a block, without the entry `but`.
 template <typename T>
 __device__ __noinline__ double one_by_one(const T* prow, const T* qrow, int vocab, int first, int but) {
   double s = 0.0;
 #pragma unroll 1
-  for (int i = 0; i < 8; ++i) s += weight_of(prow, qrow, vocab, first + (int)(threadIdx.x & 31) + 32 * i, but);
+  for (int i = 0; i < 8; ++i) {
+    const int j = first + (int)(threadIdx.x & 31) + 32 * i;
+    if (j < vocab) s += weight_of(rr_to_f32(prow[j]), qrow ? rr_to_f32(qrow[j]) : 0.f, j == but);
+  }
   return s;
 }
 
@@ -92,17 +94,17 @@ template <typename T> struct Block {
     const int j0 = first + (threadIdx.x & 31);
     if (first + BLOCK <= vocab) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = __ldcg(prow + j0 + 32 * i);
+      for (int i = 0; i < 8; ++i) p[i] = prow[j0 + 32 * i];
       if (qrow) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = __ldcg(qrow + j0 + 32 * i);
+        for (int i = 0; i < 8; ++i) q[i] = qrow[j0 + 32 * i];
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const bool in = j0 + 32 * i < vocab;
-        p[i] = in ? __ldcg(prow + j0 + 32 * i) : rr_from_f32<T>(0.f);
-        q[i] = in && qrow ? __ldcg(qrow + j0 + 32 * i) : rr_from_f32<T>(0.f);
+        p[i] = in ? prow[j0 + 32 * i] : rr_from_f32<T>(0.f);
+        q[i] = in && qrow ? qrow[j0 + 32 * i] : rr_from_f32<T>(0.f);
       }
     }
   }
@@ -158,36 +160,37 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
   rr_pdl_trigger();
   const Span s = span_of(a, b);
   if (s.n < 0) {                                        // (uniform in the cluster)
-    if (cta == 0 && warp == 0) write_accepted(a, b, s, 0, -1);
+    if (cta == 0 && warp == 0) write_accepted(a, b, s, 0);
     return;
   }
   // which drafts are accepted: every warp for itself
+  const double u = fmax((double)a.uniform[s.first + s.n], 0.0);
   int accepted = 0;
   for (int i0 = 0; i0 < s.n; i0 += 32) {
     const int i = i0 + lane, t = s.first + i;
     bool ok = true;
     if (i < s.n) {
-      const int x = __ldcg(a.tokens + t + 1);
-      const double u = __ldcg(a.uniform + t);
+      const int x = a.tokens[t + 1];
+      const double r = a.uniform[t];
       ok = in_vocab(a, x);
       if (ok) {
         const double p = probability<T>(a.target, a.target_stride, t, x), q = a.draft ? probability<T>(a.draft, a.draft_stride, t, x) : 1.0;
-        ok = p > u * q;
+        ok = p > r * q;
       }
     }
     const unsigned rejected = __ballot_sync(0xFFFFFFFFu, !ok);
     if (rejected) { accepted = i0 + __ffs(rejected) - 1; break; }
     accepted = min(i0 + 32, s.n);
   }
+  if (cta == 0 && warp == NW - 1) write_accepted(a, b, s, accepted);
   const int row = s.first + accepted;
   const T* const p = (const T*)a.target + row * a.target_stride;
   const T* q = nullptr;
   int but = -1;
   if (accepted < s.n) {
     if (a.draft) q = (const T*)a.draft + row * a.draft_stride;
-    else but = __ldcg(a.tokens + row + 1);
+    else but = a.tokens[row + 1];
   }
-  const double u = fmax((double)__ldcg(a.uniform + s.first + s.n), 0.0);
   // blocks of this CTA; a kept sum stands for `per` of them
   const int blocks = (a.vocab + BLOCK - 1) / BLOCK, share = (blocks + ctas - 1) / ctas, from = min(cta * share, blocks), mine = min(share, blocks - from);
   const int per = (share + SUMS - 1) / SUMS, sums = (mine + per - 1) / per;
@@ -246,23 +249,20 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
       cl.barrier_wait(std::move(read));
       break;
     }
-    // the kept sum, then the block, then the entry
-    double before = h.before, run = before;
-    k = 0;
-    h.over = false;
-#pragma unroll 1
-    for (int k0 = 0; k0 < sums && !h.over; k0 += 32) {
-      h = find(k0 + lane < sums ? f.sums[k0 + lane] : 0.0, run, limit);
-      if (h.at < 32) k = k0 + h.at, before = h.before;
-      run = h.end;
-    }
-    run = before;
+    // the kept sum (two lie side by side in a lane), then the block, then the entry
+    static_assert(SUMS == 64, "two per lane");
+    h = find(f.sums[2 * lane] + f.sums[2 * lane + 1], h.before, limit);
+    k = 2 * h.at;
+    double run = h.before;
+    const double first = f.sums[k], second = f.sums[k + 1];
+    if (!(first > 0.0 && (run + first > limit || !(second > 0.0)))) ++k, run += first;
     h.over = false;
 #pragma unroll 1
     for (int i = k * per; i < min((k + 1) * per, mine) && !h.over; ++i) {
       const int at = (from + i) * BLOCK;
+      now.load(p, q, a.vocab, at);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f.lanes[e][lane] = weight_of(p, q, a.vocab, at + lane + 32 * e, but);
+      for (int e = 0; e < 8; ++e) f.lanes[e][lane] = weight_of(rr_to_f32(now.p[e]), q ? rr_to_f32(now.q[e]) : 0.f, at + lane + 32 * e == but);
       __syncwarp();
       double x = 0.0;                                   // four lanes add up 32 entries, then these
 #pragma unroll
@@ -281,7 +281,7 @@ verify_sampled_kernel(const __grid_constant__ rr_verify_args a) {
     break;
   }
   // the CTA that has the token, or the first one where all weights are 0
-  if (warp == 0 && (here || (none && cta == 0))) write_accepted(a, b, s, accepted, token);
+  if (threadIdx.x == 0 && (here || (none && cta == 0))) a.out[row] = token;
 }
 
 // ---- greedy -----------------------------------------------------------------------------------------------------
@@ -323,7 +323,7 @@ best_kernel(const __grid_constant__ rr_verify_args a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   rr_pdl_wait();
   rr_pdl_trigger();
-  if (a.cu && t >= __ldcg(a.cu + a.batch)) return;       // padding (uniform in the cluster)
+  if (a.cu && t >= a.cu[a.batch]) return;       // padding (uniform in the cluster)
   using V = Vec<T, VEC>;
   const int vecs = a.vocab / VEC, share = (vecs + ctas - 1) / ctas, from = min(cta * share, vecs), to = min(from + share, vecs);
   const T* const row = (const T*)a.target + t * a.target_stride;
@@ -331,14 +331,14 @@ best_kernel(const __grid_constant__ rr_verify_args a) {
 #pragma unroll 8
   for (int v = from + threadIdx.x; v < to; v += NT) {
     V e;
-    if constexpr (VEC == 1) e.v = __ldcg(row + v);
-    else { const uint4 raw = __ldcg((const uint4*)row + v); e = *(const V*)&raw; }
+    if constexpr (VEC == 1) e.v = row[v];
+    else { const uint4 raw = ((const uint4*)row)[v]; e = *(const V*)&raw; }
     const uint32_t key = score_key(e.best());
     if (key > x.key) x = Best{key, v};
   }
   if (cta == ctas - 1 && threadIdx.x == 0)              // the entries behind the last vector
     for (int j = vecs * VEC; j < a.vocab; ++j)
-      if (const uint32_t key = score_key(rr_to_f32(__ldcg(row + j))); key > x.key) x = Best{key, vecs};
+      if (const uint32_t key = score_key(rr_to_f32(row[j])); key > x.key) x = Best{key, vecs};
   x = warp_best(x);
   if (lane == 0) s_warp[warp] = x;
   __syncthreads();
@@ -346,7 +346,7 @@ best_kernel(const __grid_constant__ rr_verify_args a) {
     x = warp_best(lane < NW ? s_warp[lane] : Best{0u, INT32_MAX});
     // the first entry of the vector that is as good
     const int j = x.key ? x.at * VEC + lane : 0;
-    const unsigned same = __ballot_sync(0xFFFFFFFFu, x.key && lane < VEC && j < a.vocab && score_key(rr_to_f32(__ldcg(row + j))) == x.key);
+    const unsigned same = __ballot_sync(0xFFFFFFFFu, x.key && lane < VEC && j < a.vocab && score_key(rr_to_f32(row[j])) == x.key);
     if (lane == 0) s_cta = Best{x.key, x.key ? x.at * VEC + __ffs(same) - 1 : INT32_MAX};
   }
   cl.sync();
@@ -370,7 +370,7 @@ compare_kernel(const __grid_constant__ rr_verify_args a) {
     const int i = i0 + lane;
     bool ok = true;
     if (i < s.n) {
-      const int x = __ldcg(a.tokens + s.first + i + 1);
+      const int x = a.tokens[s.first + i + 1];
       ok = in_vocab(a, x) && x == __ldcg(a.out + s.first + i);
     }
     const unsigned rejected = __ballot_sync(0xFFFFFFFFu, !ok);
@@ -408,6 +408,7 @@ int done(cudaError_t e) { return e == cudaSuccess ? RR_OK : rr_cuda_fail(e, "rr_
 extern "C" int rr_verify_drafts(const rr_verify_args* a, void* stream) {
   if (!a || !a->out || !a->accepted || !a->tokens || (!a->target && a->rows > 0)) return RR_ERR_INVALID_ARG;
   if (a->rows < 0 || a->batch < 1 || a->vocab < 1 || (!a->cu && a->rows != a->batch)) return RR_ERR_INVALID_ARG;
+  if (a->out == a->tokens && a->rows > 0) return RR_ERR_INVALID_ARG;                       // (tokens are read while results are written)
   if (a->target_stride < 0 || a->draft_stride < 0 || (a->new_lens && !a->lens) || (a->draft && !a->uniform)) return RR_ERR_INVALID_ARG;
   if (a->dtype != RR_BF16 && a->dtype != RR_F32) return RR_ERR_UNSUPPORTED;
   if (a->vocab > (1 << 30) || a->batch > (1 << 27)) return RR_ERR_TOO_LARGE;

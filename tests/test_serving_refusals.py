@@ -136,7 +136,7 @@ def test_reserve_and_compact():
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(target=None), INVALID), (dict(tokens=None), INVALID), (dict(out=None), INVALID), (dict(accepted=None), INVALID), (dict(lens=None), INVALID),
+    (dict(target=None), INVALID), (dict(tokens=None), INVALID), (dict(out=None), INVALID), (dict(out=0x30000), INVALID), (dict(accepted=None), INVALID), (dict(lens=None), INVALID),
     (dict(uniform=None), INVALID), (dict(cu=None), INVALID), (dict(rows=-1), INVALID), (dict(batch=0), INVALID), (dict(vocab=0), INVALID),
     (dict(target_stride=-1), INVALID), (dict(draft_stride=-5), INVALID), (dict(dtype=2), UNSUPPORTED), (dict(vocab=(1 << 30) + 1), TOO_LARGE),
     (dict(batch=(1 << 27) + 1), TOO_LARGE), (dict(target=0x10002), INVALID), (dict(draft=0x20001), INVALID), (dict(tokens=0x30001), INVALID),
