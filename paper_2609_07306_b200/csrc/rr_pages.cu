@@ -7,7 +7,7 @@
 //
 // The bookkeeping is a few integers per row and one pass over refs: bound by latency, not by bytes.  It runs in one cluster of eight
 // CTAs, whose hardware barrier separates the steps (a barrier costs less than a launch, and no wait on memory is needed).  What is cheap to know
-// about the rows every CTA finds out for itself, a thread per row, instead of a barrier; work on the table's entries is shared by all warps, 256
+// about the rows every CTA finds out for itself, a thread per row, instead of a barrier; work on the table's entries is shared by all warps, 128 or 256
 // entries of a row at a time.  Free pages are found by all threads together, up to 32 pages per thread, in rounds of 131072
 // pages; counts are exchanged through distributed shared memory, and the threads of a CTA look up which entries its free pages' ranks belong to.
 // Which page goes where follows from ranks, never from the order of atomics, which only add to counters.  Copies of pages are a second
@@ -25,9 +25,10 @@ namespace {
 
 constexpr int CL = 8, NT = 512, NW = NT / 32;
 constexpr int ROUND = CL * NT * 32;                     // pages of a round: 32 per thread
-constexpr int COLS = 256;                               // entries of a row that a warp looks at
+constexpr int COLS = 256;                               // entries of a row that a warp releases
 constexpr int ROWS_ON_CHIP = 2048;                      // rows whose state fits shared memory
 constexpr int GIVEN = 4096;                             // pages that a CTA hands out at a time
+constexpr int64_t LONG_TABLE = 1 << 16;                 // entries of a table from which a fork takes all SMs
 constexpr int MAX_LAYERS = 64;                          // of one launch of the copy
 
 struct Move { int32_t src, dst, tokens; };
@@ -35,7 +36,8 @@ struct Move { int32_t src, dst, tokens; };
 // The workspace.  `list`: new rows (fork), entries to be replaced or free pages in rank order (reserve), sources, destinations and new ids (compact).
 struct Work {
   int32_t* moves;                                       // [0] how many, [1] pages in use (compact)
-  int32_t* replaced;                                    // [batch] entries to be replaced behind the one that the row goes on writing
+  int32_t* replaced;                                    // [batch] entries to be replaced behind the one that the row goes on writing; fork: pages that the row takes
+  int32_t* was;                                         // [batch] fork: pages that it held
   int32_t* list;
   int32_t* ranked;                                      // [num_pages]
   Move* move;
@@ -83,13 +85,14 @@ size_t move_bytes(const rr_page_pool& p) {
   return 4 * up4(3 * most);
 }
 size_t workspace_bytes(const rr_page_pool& p) {
-  return 64 + 4 * (up4(p.batch) + list_ints(p) + up4(p.num_pages)) + move_bytes(p) + (p.batch > ROWS_ON_CHIP ? CL * row_state(p) : 0);
+  return 64 + 4 * (2 * up4(p.batch) + list_ints(p) + up4(p.num_pages)) + move_bytes(p) + (p.batch > ROWS_ON_CHIP ? CL * row_state(p) : 0);
 }
 Work work_of(const rr_page_pool& p, void* ws) {
   Work w;
   w.moves = (int32_t*)ws;
   w.replaced = w.moves + 16;
-  w.list = w.replaced + up4(p.batch);
+  w.was = w.replaced + up4(p.batch);
+  w.list = w.was + up4(p.batch);
   w.ranked = w.list + list_ints(p);
   w.move = (Move*)(w.ranked + up4(p.num_pages));
   w.rows = (char*)w.move + move_bytes(p);
@@ -167,67 +170,102 @@ __device__ __noinline__ uint32_t free_bits(const int32_t* refs, int num_pages, i
 // ---- fork -------------------------------------------------------------------------------------------------------
 // A row is compared with its parent's: beams differ from one another in their last pages only, and equal entries cost two loads.  New entries
 // are staged, as a parent's row may be rewritten in the same call.
+// Long tables take two ordinary launches over all SMs instead of one cluster (where one group of four in each descends from its first: 512 rows of 2048 entries 9.5 us
+// instead of 66, 512 of 256 7.1 instead of 15; 64 of 256 6.0 in the cluster, 8.4 by two launches).
 constexpr int FORK_NT = 1024;                           // (a warp per row for 256 rows)
+constexpr int LONG_NT = 512;
+constexpr int RUN = 128;                                // entries of a row that a warp compares
 struct Heir { int parent, held, takes; };               // pages that the row held and takes (-1: it stays)
+
+__device__ __forceinline__ Heir heir_of(const PoolParams& P, int b, bool tell) {
+  const rr_page_pool& p = P.p;
+  Heir h{__ldcg(P.arg + b), held_of(p, b), -1};
+  if (h.parent < -1 || h.parent >= p.batch) {
+    if (tell) report(p, RR_STATUS_BAD_INDEX);
+    h.parent = b;
+  }
+  const int len = h.parent < 0 ? 0 : __ldcg(P.lens + h.parent);
+  if (h.parent != b) h.takes = h.parent < 0 ? 0 : (int)min((unsigned)held_of(p, h.parent), ((unsigned)max(len, 0) + p.page_tokens - 1) / p.page_tokens);
+  if (tell) {
+    if (len < 0) report(p, RR_STATUS_BAD_INDEX);
+    P.new_lens[b] = max(len, 0);
+  }
+  return h;
+}
+
+// A run of a row's new entries: staged, with the holders of pages that change; how many pages came free.
+__device__ __forceinline__ int stage_run(const PoolParams& P, int b, int c0, const Heir& h) {
+  const rr_page_pool& p = P.p;
+  const int32_t* const mine = p.page_table + b * p.table_stride;
+  const int32_t* const theirs = p.page_table + h.parent * p.table_stride;
+  int32_t* const stage = P.w.list + (size_t)b * p.pages_per_seq;
+  const int end = min(max(h.held, h.takes), c0 + RUN);
+  int freed = 0;
+#pragma unroll 2
+  for (int c = c0 + (threadIdx.x & 31); c < end; c += 32) {
+    const int was = c < h.held ? __ldcg(mine + c) : -1, is = c < h.takes ? __ldcg(theirs + c) : -1;
+    stage[c] = is;
+    if (was == is) continue;
+    if (in_pool(p, is)) freed -= atomicAdd(p.refs + is, 1) == 0;        // (one row may let go of a page before another takes it)
+    else if (c < h.takes) report(p, RR_STATUS_BAD_INDEX);
+    if (in_pool(p, was)) freed += release(p, was);
+    else if (c < h.held) report(p, RR_STATUS_BAD_INDEX);
+  }
+  return freed;
+}
+__device__ __forceinline__ void write_run(const PoolParams& P, int b, int c0, int held, int takes) {
+  int32_t* const mine = P.p.page_table + b * P.p.table_stride;
+  const int32_t* const stage = P.w.list + (size_t)b * P.p.pages_per_seq;
+#pragma unroll 2
+  for (int c = c0 + (threadIdx.x & 31); c < min(max(held, takes), c0 + RUN); c += 32) mine[c] = __ldcg(stage + c);
+  if (c0 == 0 && (threadIdx.x & 31) == 0) P.p.held[b] = takes;
+}
 
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(FORK_NT, 1)
 fork_kernel(const __grid_constant__ PoolParams P) {
   extern __shared__ __align__(16) char on_chip[];
   cg::cluster_group cl = cg::this_cluster();
   const rr_page_pool& p = P.p;
-  const int lane = threadIdx.x & 31, rank = cl.block_rank(), warp = (threadIdx.x >> 5) * CL + rank;
+  const int rank = cl.block_rank(), warp = (threadIdx.x >> 5) * CL + rank;
   Heir* const heirs = p.batch > ROWS_ON_CHIP ? (Heir*)(P.w.rows + rank * (sizeof(Heir) * ((p.batch + 3) & ~3))) : (Heir*)on_chip;
   rr_pdl_wait();
   rr_pdl_trigger();
-  for (int b = threadIdx.x; b < p.batch; b += FORK_NT) {     // in every CTA
-    const bool tell = rank == 0;
-    Heir h{__ldcg(P.arg + b), held_of(p, b), -1};
-    if (h.parent < -1 || h.parent >= p.batch) {
-      if (tell) report(p, RR_STATUS_BAD_INDEX);
-      h.parent = b;
-    }
-    const int len = h.parent < 0 ? 0 : __ldcg(P.lens + h.parent);
-    if (h.parent != b) h.takes = h.parent < 0 ? 0 : (int)min((unsigned)held_of(p, h.parent), ((unsigned)max(len, 0) + p.page_tokens - 1) / p.page_tokens);
-    if (tell) {
-      if (len < 0) report(p, RR_STATUS_BAD_INDEX);
-      P.new_lens[b] = max(len, 0);
-    }
-    heirs[b] = h;
-  }
+  for (int b = threadIdx.x; b < p.batch; b += FORK_NT) heirs[b] = heir_of(P, b, rank == 0);     // in every CTA
   __syncthreads();
-  const int parts = (p.pages_per_seq + COLS - 1) / COLS, units = p.batch * parts, each = (units + CL * (FORK_NT / 32) - 1) / (CL * (FORK_NT / 32));
+  const int parts = (p.pages_per_seq + RUN - 1) / RUN, units = p.batch * parts, each = (units + CL * (FORK_NT / 32) - 1) / (CL * (FORK_NT / 32));
   int freed = 0;
-  for (int u = warp * each; u < min((warp + 1) * each, units); ++u) {
-    const int b = u / parts, c0 = (u - b * parts) * COLS;
-    const Heir h = heirs[b];
-    if (h.takes < 0) continue;
-    const int32_t* const mine = p.page_table + b * p.table_stride;
-    const int32_t* const theirs = p.page_table + h.parent * p.table_stride;
-    int32_t* const stage = P.w.list + (size_t)b * p.pages_per_seq;
-    const int end = min(max(h.held, h.takes), c0 + COLS);
-#pragma unroll 2
-    for (int c = c0 + lane; c < end; c += 32) {
-      const int was = c < h.held ? __ldcg(mine + c) : -1, is = c < h.takes ? __ldcg(theirs + c) : -1;
-      stage[c] = is;
-      if (was == is) continue;
-      if (in_pool(p, is)) freed -= atomicAdd(p.refs + is, 1) == 0;      // (one row may let go of a page before another takes it)
-      else if (c < h.takes) report(p, RR_STATUS_BAD_INDEX);
-      if (in_pool(p, was)) freed += release(p, was);
-      else if (c < h.held) report(p, RR_STATUS_BAD_INDEX);
-    }
-  }
+  for (int u = warp * each; u < min((warp + 1) * each, units); ++u)
+    if (const Heir h = heirs[u / parts]; h.takes >= 0) freed += stage_run(P, u / parts, u % parts * RUN, h);
   cl.sync();
-  for (int u = warp * each; u < min((warp + 1) * each, units); ++u) {
-    const int b = u / parts, c0 = (u - b * parts) * COLS;
-    const Heir h = heirs[b];
-    if (h.takes < 0) continue;
-    int32_t* const mine = p.page_table + b * p.table_stride;
-    const int32_t* const stage = P.w.list + (size_t)b * p.pages_per_seq;
-#pragma unroll 2
-    for (int c = c0 + lane; c < min(max(h.held, h.takes), c0 + COLS); c += 32) mine[c] = stage[c];
-    if (c0 == 0 && lane == 0) p.held[b] = h.takes;
+  for (int u = warp * each; u < min((warp + 1) * each, units); ++u)
+    if (const Heir h = heirs[u / parts]; h.takes >= 0) write_run(P, u / parts, u % parts * RUN, h.held, h.takes);
+  add_free(p, freed);
+}
+
+__global__ void __launch_bounds__(LONG_NT)
+fork_stage_kernel(const __grid_constant__ PoolParams P) {
+  const rr_page_pool& p = P.p;
+  const int lane = threadIdx.x & 31, parts = (p.pages_per_seq + RUN - 1) / RUN, units = p.batch * parts;
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  int freed = 0;
+  for (int u = blockIdx.x * (LONG_NT / 32) + (threadIdx.x >> 5); u < units; u += gridDim.x * (LONG_NT / 32)) {
+    const int b = u / parts, part = u - b * parts;
+    const Heir h = heir_of(P, b, part == 0 && lane == 0);
+    if (part == 0 && lane == 0) P.w.replaced[b] = h.takes, P.w.was[b] = h.held;
+    if (h.takes >= 0) freed += stage_run(P, b, part * RUN, h);
   }
   add_free(p, freed);
+}
+__global__ void __launch_bounds__(LONG_NT)
+fork_write_kernel(const __grid_constant__ PoolParams P) {
+  const int parts = (P.p.pages_per_seq + RUN - 1) / RUN, units = P.p.batch * parts;
+  rr_pdl_wait();
+  rr_pdl_trigger();
+  for (int u = blockIdx.x * (LONG_NT / 32) + (threadIdx.x >> 5); u < units; u += gridDim.x * (LONG_NT / 32)) {
+    const int b = u / parts, takes = __ldcg(P.w.replaced + b);
+    if (takes >= 0) write_run(P, b, (u - b * parts) * RUN, __ldcg(P.w.was + b), takes);
+  }
 }
 
 // ---- reserve ----------------------------------------------------------------------------------------------------
@@ -804,9 +842,9 @@ int launch_copies(const PoolParams& P, const rr_paged_kv* caches, int n, bool co
   return RR_OK;
 }
 
-int launch_pool(void (*kernel)(PoolParams), const PoolParams& P, int threads, size_t smem, cudaStream_t st, const char* who) {
+int launch_pool(void (*kernel)(PoolParams), const PoolParams& P, int ctas, int threads, size_t smem, cudaStream_t st, const char* who) {
   rr_count_launch();
-  const cudaError_t e = rr_launch_pdl(kernel, CL, threads, smem, st, P);
+  const cudaError_t e = rr_launch_pdl(kernel, ctas, threads, smem, st, P);
   return e == cudaSuccess ? RR_OK : rr_cuda_fail(e, who);
 }
 
@@ -828,7 +866,12 @@ extern "C" int rr_pages_fork(const rr_page_pool* pool, const int32_t* parents, c
   if (((uintptr_t)parents | (uintptr_t)lens | (uintptr_t)new_lens) & 3) return RR_ERR_INVALID_ARG;
   if ((rc = check_workspace(pool, workspace, bytes)) != RR_OK) return rc;
   PoolParams P{*pool, work_of(*pool, workspace), parents, lens, new_lens, nullptr, 0, 0, 0};
-  return launch_pool(fork_kernel, P, FORK_NT, pool->batch > ROWS_ON_CHIP ? 0 : sizeof(Heir) * pool->batch, (cudaStream_t)stream, "rr_pages_fork");
+  cudaStream_t st = (cudaStream_t)stream;
+  if ((int64_t)pool->batch * pool->pages_per_seq <= LONG_TABLE)
+    return launch_pool(fork_kernel, P, CL, FORK_NT, pool->batch > ROWS_ON_CHIP ? 0 : sizeof(Heir) * pool->batch, st, "rr_pages_fork");
+  const int64_t units = (int64_t)pool->batch * ((pool->pages_per_seq + RUN - 1) / RUN), ctas = (units + LONG_NT / 32 - 1) / (LONG_NT / 32), most = 4 * rr_sm_count();
+  if ((rc = launch_pool(fork_stage_kernel, P, (int)(ctas < most ? ctas : most), LONG_NT, 0, st, "rr_pages_fork")) != RR_OK) return rc;
+  return launch_pool(fork_write_kernel, P, (int)(ctas < most ? ctas : most), LONG_NT, 0, st, "rr_pages_fork");
 }
 
 extern "C" int rr_pages_reserve(const rr_page_pool* pool, const int32_t* lens, const int32_t* new_tokens, int32_t new_each, const rr_paged_kv* caches,
@@ -843,7 +886,7 @@ extern "C" int rr_pages_reserve(const rr_page_pool* pool, const int32_t* lens, c
   constexpr size_t given = GIVEN * 4, most = given + sizeof(Row) * ROWS_ON_CHIP + sizeof(Slot) * 2 * ROWS_ON_CHIP;
   const cudaError_t e = rr_once_per_device(done, [] { return cudaFuncSetAttribute(reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most); });
   if (e != cudaSuccess) return rr_cuda_fail(e, "rr_pages_reserve");
-  rc = launch_pool(reserve_kernel, P, NT, given + (pool->batch > ROWS_ON_CHIP ? 0 : row_state(*pool)), (cudaStream_t)stream, "rr_pages_reserve");
+  rc = launch_pool(reserve_kernel, P, CL, NT, given + (pool->batch > ROWS_ON_CHIP ? 0 : row_state(*pool)), (cudaStream_t)stream, "rr_pages_reserve");
   return rc != RR_OK ? rc : launch_copies(P, caches, n, false, (cudaStream_t)stream, "rr_pages_reserve");
 }
 
@@ -856,6 +899,6 @@ extern "C" int rr_pages_compact(const rr_page_pool* pool, const rr_paged_kv* cac
   if ((rc = check_workspace(pool, workspace, bytes)) != RR_OK) return rc;
   PoolParams P{*pool, work_of(*pool, workspace), nullptr, nullptr, nullptr, new_ids, 0, 0, words_of(*pool)};
   if (!P.remap) P.remap = P.w.ranked;
-  rc = launch_pool(compact_kernel, P, NT, 0, (cudaStream_t)stream, "rr_pages_compact");
+  rc = launch_pool(compact_kernel, P, CL, NT, 0, (cudaStream_t)stream, "rr_pages_compact");
   return rc != RR_OK ? rc : launch_copies(P, caches, n, true, (cudaStream_t)stream, "rr_pages_compact");
 }

@@ -38,7 +38,7 @@ class Pages:
         rows, moves = [], []
         for b, r in enumerate(self.rows):
             out = list(r[:lens[b] // page])
-            for c in range(lens[b] // page, max(len(r), upto[b])):
+            for c in range(len(out), max(len(r), upto[b])):             # (pages that its tokens should have and that it lacks are new ones, too)
                 used = lens[b] % page if c == lens[b] // page else 0
                 if c < len(r):
                     p = r[c]

@@ -356,3 +356,25 @@ def test_many_pages_at_once(pages):
     want.compact()
     want.check(pool, flat)
     assert pool.status.item() == 0
+
+
+@pytest.mark.parametrize("batch,width", [(33, 2000), (700, 97), (2200, 31)])
+def test_forks_of_long_tables(batch, width):
+    """Tables that take all SMs, forked one call behind the other, with rows that end and parents that there are not."""
+    pool, flat, want = make(batch, width, batch * width + 9, 2)
+    rng = random.Random(width)
+    lens = [rng.randint(0, 2 * width - 2) for _ in range(batch)]
+    pool.reserve(ints(lens), 1)
+    assert want.reserve(lens, [1] * batch)
+    now, other = ints(lens), ints([0] * batch)
+    for call in range(4):
+        p = [rng.randrange(-1, batch) if rng.random() < 0.7 else b for b in range(batch)]
+        bad = list(p)
+        if call == 2:
+            bad[1], bad[5], p[1], p[5] = batch, -2, 1, 5
+        pool.fork(ints(bad), now, other)
+        now, other = other, now
+        lens = want.fork(p, lens)
+    assert pool.status.item() == B.RR_STATUS_BAD_INDEX
+    assert now.tolist() == lens
+    want.check(pool, flat)

@@ -111,8 +111,8 @@ def test_workspace():
     assert calls(pool(), [kv()], 1, ws=None) == (INVALID,) * 3
     assert calls(pool(), [kv()], 1, ws=0x108) == (INVALID,) * 3
     sizes = [B.rr_pages_workspace(pool(num_pages=p, batch=b, pages_per_seq=w, table_stride=w)) for p, b, w in ((10, 3, 8), (1000, 3, 8), (1000, 200, 64))]
-    # a number for every entry, row and page, three for every move; each list rounded up to 16 bytes, and 64 bytes in front
-    assert sizes == sorted(sizes) and sizes[0] < sizes[2] <= 64 + 4 * (200 * 64 + 200 + 1000 + 3 * 501 + 4 * 3)
+    # a number for every entry and page, two for every row, three for every move; each list rounded up to 16 bytes, and 64 bytes in front
+    assert sizes == sorted(sizes) and sizes[0] < sizes[2] <= 64 + 4 * (200 * 64 + 2 * 200 + 1000 + 3 * 501 + 4 * 3)
 
 
 def test_fork():
