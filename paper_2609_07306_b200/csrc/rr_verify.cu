@@ -51,16 +51,16 @@ __device__ __forceinline__ double warp_sum(double x) {
   for (int d = 16; d > 0; d /= 2) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
   return x;
 }
-__device__ __forceinline__ void write_lengths(const rr_verify_args& a, int b, const Span& s, int accepted) {
+__device__ __forceinline__ void write_lengths(const rr_verify_args& a, int b, const Span& s, int accepted, int len) {
   a.accepted[b] = accepted;
-  if (a.new_lens) a.new_lens[b] = a.lens[b] + (s.n < 0 ? 0 : accepted + 1);
+  if (a.new_lens) a.new_lens[b] = len + (s.n < 0 ? 0 : accepted + 1);
 }
 // A sequence's results but the token behind the accepted drafts.
 __device__ __forceinline__ void write_accepted(const rr_verify_args& a, int b, const Span& s, int accepted) {
   const int lane = threadIdx.x & 31;
   for (int i = lane; i <= s.n; i += 32)
     if (i != accepted) a.out[s.first + i] = i < accepted ? a.tokens[s.first + i + 1] : -1;
-  if (lane == 0) write_lengths(a, b, s, accepted);
+  if (lane == 0) write_lengths(a, b, s, accepted, a.new_lens ? a.lens[b] : 0);
 }
 
 // A drafted token is in the vocabulary.
@@ -358,27 +358,31 @@ best_kernel(const __grid_constant__ rr_verify_args a) {
   cl.sync();                                            // no CTA leaves before its best has been read
 }
 
-// The drafts against the rows' best tokens, which are in `out`: up to the first that differs they are the accepted tokens and the one more.
+// The drafts against the rows' best tokens, which are in `out`: up to the first that differs they are the accepted tokens and the one more.  Launched along with
+// best_kernel, which starts it when all before itself has ended, so only `out` has to be waited for.
 __global__ void __launch_bounds__(128)
 compare_kernel(const __grid_constant__ rr_verify_args a) {
   const int lane = threadIdx.x & 31, b = blockIdx.x * 4 + (threadIdx.x >> 5);
+  const bool mine = b < a.batch;
+  const Span s = mine ? span_of(a, b) : Span{0, -1};
+  int x = lane < s.n ? a.tokens[s.first + lane + 1] : 0;
+  const int len = mine && a.new_lens ? a.lens[b] : 0;
   rr_pdl_wait();
   rr_pdl_trigger();
-  if (b >= a.batch) return;
-  const Span s = span_of(a, b);
+  if (!mine) return;
   int accepted = max(s.n, 0);
   for (int i0 = 0; i0 < s.n; i0 += 32) {
     const int i = i0 + lane;
     bool ok = true;
     if (i < s.n) {
-      const int x = a.tokens[s.first + i + 1];
+      if (i0 > 0) x = a.tokens[s.first + i + 1];
       ok = in_vocab(a, x) && x == __ldcg(a.out + s.first + i);
     }
     const unsigned rejected = __ballot_sync(0xFFFFFFFFu, !ok);
     if (rejected) { accepted = i0 + __ffs(rejected) - 1; break; }
   }
   for (int i = accepted + 1 + lane; i <= s.n; i += 32) a.out[s.first + i] = -1;
-  if (lane == 0) write_lengths(a, b, s, accepted);
+  if (lane == 0) write_lengths(a, b, s, accepted, len);
 }
 
 // CTAs that share each of `n` things (sequences, rows) of `work` entries: at most eight, no less than `least` entries for one, and no more in all than run at
@@ -423,11 +427,15 @@ extern "C" int rr_verify_drafts(const rr_verify_args* a, void* stream) {
     const int cluster = cluster_of(a->batch, a->vocab, NW * BLOCK, 4);
     return done(launch(bf16 ? verify_sampled_kernel<__nv_bfloat16> : verify_sampled_kernel<float>, *a, a->batch, cluster, st));
   }
-  if (a->rows > 0) {
-    const bool vec = ((uintptr_t)a->target & 15) == 0 && (a->target_stride * (bf16 ? 2 : 4)) % 16 == 0;
-    auto* const kernel = bf16 ? (vec ? best_kernel<__nv_bfloat16, 8> : best_kernel<__nv_bfloat16, 1>) : (vec ? best_kernel<float, 4> : best_kernel<float, 1>);
-    if (const cudaError_t e = launch(kernel, *a, a->rows, cluster_of(a->rows, a->vocab, NT * 32, 8), st); e != cudaSuccess) return done(e);
+  const int ctas = (a->batch + 3) / 4;
+  if (a->rows == 0) {                                   // (nothing to be launched along with)
+    rr_count_launch();
+    compare_kernel<<<ctas, 128, 0, st>>>(*a);
+    return done(cudaPeekAtLastError());
   }
+  const bool vec = ((uintptr_t)a->target & 15) == 0 && (a->target_stride * (bf16 ? 2 : 4)) % 16 == 0;
+  auto* const kernel = bf16 ? (vec ? best_kernel<__nv_bfloat16, 8> : best_kernel<__nv_bfloat16, 1>) : (vec ? best_kernel<float, 4> : best_kernel<float, 1>);
+  if (const cudaError_t e = launch(kernel, *a, a->rows, cluster_of(a->rows, a->vocab, NT * 32, 8), st); e != cudaSuccess) return done(e);
   rr_count_launch();
-  return done(rr_launch_pdl(compare_kernel, (a->batch + 3) / 4, 128, 0, st, *a));
+  return done(rr_launch_pdl(compare_kernel, ctas, 128, 0, st, *a));
 }

@@ -23,7 +23,8 @@ class PagePool:
 
     PagePool.empty makes the state of a pool whose pages are all free.  The object keeps the tensors (they are written to, not exchanged) and one
     workspace.  Its calls change the state: order them, and the operators that read the table, on one stream or by events;
-    graphs that hold them may not run at the same time.  Work goes to the current stream of the table's device, whichever device is the current one."""
+    graphs that hold them may not run at the same time.  Keep the object until its work on streams other than the one that it was made on has
+    ended.  Work goes to the current stream of the table's device, whichever device is the current one."""
 
     def __init__(self, page_table: torch.Tensor, page_tokens: int, refs: torch.Tensor, held: torch.Tensor,
                  free: torch.Tensor | None = None, caches: "list[PagedKV] | tuple[PagedKV, ...]" = (), status: torch.Tensor | None = None):

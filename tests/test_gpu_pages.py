@@ -76,7 +76,7 @@ def run(pool, flat, want, steps, seed, every=1):
                 lens = [0 if rng.random() < 0.3 else x for x in lens]
                 new = [0] * batch
             elif kind == "admit":
-                new = [rng.randint(1, width * page // 2) if x == 0 else 1 for x in lens]
+                new = [rng.randint(1, max(1, width * page // 2)) if x == 0 else 1 for x in lens]
             new = [min(n, width * page - x) for x, n in zip(lens, new)]
             if rng.random() < 0.3 and len(set(new)) == 1:
                 pool.reserve(ints(lens), new[0])
@@ -378,3 +378,11 @@ def test_forks_of_long_tables(batch, width):
     assert pool.status.item() == B.RR_STATUS_BAD_INDEX
     assert now.tolist() == lens
     want.check(pool, flat)
+
+
+@pytest.mark.parametrize("batch,width,pages,page,kinds", [
+    (1, 1, 1, 1, [(BF, 1, 1, "plain")]), (1, 1, 2, 1, [(F32, 1, 1, "tokens")]), (2, 1, 3, 7, [(BF, 3, 1, "pair")]), (3, 2, 4, 1000, [(BF, 1, 256, "plain")]),
+    (2, 2, 5, 3, [(F32, 1, 3, "tokens")]), (4, 600, 2500, 1, [(BF, 8, 128, "plain")]), (2, 3, 8, 2048, [(BF, 2, 64, "tokens")]),
+    (3, 4, 14, 33, [(BF, 7, 72, "tokens"), (F32, 5, 12, "plain")])])
+def test_smallest_and_odd_sizes(batch, width, pages, page, kinds):
+    run(*make(batch, width, pages, page, kinds), steps=40, seed=page)
