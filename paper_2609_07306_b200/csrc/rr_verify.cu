@@ -17,7 +17,7 @@
 // Greedy: a cluster takes a row, whoever's it is (sequences with many drafts would hold up the others), 16 bytes at a time where rows
 // allow it; only maxima are taken (a packed maximum of two bf16 costs one instruction), a thread keeps its first best vector, and the entry inside it is looked
 // up at the end.  The rows' best tokens go to `out`, where a second kernel, a warp per sequence, compares them with the drafts.
-// Measured: those 64 sequences 15.7 us, 19.7 from memory; one sequence against 32768 tokens 6.4 us; greedy, 415 rows of 131072 in bf16 (109 MB) 18 to 19 us, 23 from memory.
+// Measured: those 64 sequences 15.7 us, 19.7 from memory; one sequence against 32768 tokens 6.4 us; greedy, 415 rows of 131072 in bf16 (109 MB) 22 us from memory.
 #include <cooperative_groups.h>
 #include <utility>
 #include "rr_paged.cuh"

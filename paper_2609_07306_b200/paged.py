@@ -183,8 +183,8 @@ class PagedKV:
                 raise ValueError("q must be [tokens, heads, dh]")
             shape = (n, q.shape[1], self.dh)
             qs = self._heads(q, "q", shape)
-            if q_out is None:
-                q_out = q.new_empty(shape)
+            if q_out is None:                          # (contiguous: like q, where that is the order of q's strides, costs less than by its shape)
+                q_out = torch.empty_like(q) if qs[0] > qs[1] >= self.dh else q.new_empty(shape)
                 os = (shape[1] * self.dh, self.dh)
             else:
                 os = self._heads(q_out, "q_out", shape)
