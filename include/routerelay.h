@@ -389,7 +389,9 @@ typedef struct rr_paged_kv {
  * With rot > 0 the first `rot` entries of every key head, and of every query head, are rotated by the
  * token's position p: pair j is turned by the angle p * inv_freq[j]; the pair is (j, j + rot / 2), or with
  * interleaved != 0 (2 j, 2 j + 1).  The product p * inv_freq[j] is formed and reduced in 64 bits, at any position.
- * Writes lens[b] + number of new tokens to new_lens[b] if new_lens is given (not lens itself). */
+ * Writes lens[b] + number of new tokens to new_lens[b] if new_lens is given (not lens itself).
+ * With `room`, a sequence of which lens[b] + number of new tokens is above room[b] gets none of them: nothing is written to its pages,
+ * new_lens[b] is lens[b], and RR_STATUS_NO_PAGES is set in *status.  (Queries are rotated all the same.) */
 typedef struct rr_append_args {
   const void* k;             /* [tokens, kv_heads, dh]                                            */
   const void* v;
@@ -399,6 +401,7 @@ typedef struct rr_append_args {
   const int32_t* cu;         /* [batch + 1] ascending, cu[0] = 0; or NULL                         */
   int32_t* new_lens;         /* [batch] or NULL                                                   */
   const float* inv_freq;     /* [rot / 2]; may be NULL if rot == 0                                */
+  const int32_t* room;       /* [batch] of rr_page_pool, or NULL                                  */
   int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
   int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
   int32_t tokens, q_heads;
@@ -486,6 +489,7 @@ typedef struct rr_page_pool {
   int32_t* held;             /* [batch]                                                           */
   int32_t* free_pages;       /* [1]                                                               */
   uint32_t* status;          /* [1] RR_STATUS_* bits are OR-ed into it; may be NULL               */
+  int32_t* room;             /* [batch] written by rr_pages_reserve, read by rr_kv_append and rr_verify_drafts; may be NULL */
   int64_t table_stride;
   int32_t num_pages, page_tokens, batch, pages_per_seq;
 } rr_page_pool;
@@ -501,8 +505,10 @@ int rr_pages_fork(const rr_page_pool* pool, const int32_t* parents, const int32_
  *   - pages behind the last of these tokens are released (lens 0 and nothing new: the sequence has ended), missing ones are given,
  *   - a page that will be written and is held by others too becomes the sequence's own: one that begins with some of its tokens is
  *     copied, as far as they reach, in all `n` caches; if all who hold it are to write to it, the first keeps it.
- * If there are fewer free pages than the call needs, none is given: rows are only shortened, and RR_STATUS_NO_PAGES is set in *status (read it before
- * tokens are appended, or see from free_pages that new / page_tokens + 2 pages a sequence are there).
+ * If there are fewer free pages than the call needs, none is given: rows are only shortened, and RR_STATUS_NO_PAGES is set in *status.  A sequence's page may
+ * then still be another's, too.  `room` says so to what follows on the device: room[b] becomes the first place behind which sequence b's pages are
+ * another's or missing, 2^31 - 1 where nothing was missing for it, and for all after a call that gave everything.  An append that has it
+ * leaves such a sequence alone.  Without it, read the status before tokens are appended (new / page_tokens + 2 free pages a sequence are always enough).
  * caches: host array of the layers' caches, with the pool's number and size of pages; heads, widths, types and strides are each one's own. */
 int rr_pages_reserve(const rr_page_pool* pool, const int32_t* lens, const int32_t* new_tokens, int32_t new_each,
                      const rr_paged_kv* caches, int32_t n, void* workspace, size_t bytes, void* stream);
@@ -525,7 +531,8 @@ int rr_pages_compact(const rr_page_pool* pool, const rr_paged_kv* caches, int32_
  *                   the best of the next row.  draft is NULL.
  * Writes, for each row of a sequence, the token that follows it: the accepted drafts, the token more, then -1; rows behind cu[batch] are left as they
  * were.  accepted[b] is the number of accepted drafts, new_lens[b] (if given) = lens[b] + accepted[b] + 1, the tokens that stay of a sequence that had
- * lens[b] before its rows were appended (a sequence without rows: 0 accepted, lens[b]).  A drafted token outside the vocabulary is rejected and sets
+ * lens[b] before its rows were appended (a sequence without rows: 0 accepted, lens[b]).  With `room` (and lens), a sequence of which lens[b] + rows is above room[b],
+ * whose rows were therefore not appended, has accepted[b] = -1, and its lens[b] stays; its entries of `out` are not to be used.  A drafted token outside the vocabulary is rejected and sets
  * RR_STATUS_BAD_INDEX in *status (if given); RR_STATUS_TIMEOUT there, as with the paged operators, means that the results are not to be used.  No workspace. */
 typedef struct rr_verify_args {
   const void* target;        /* [rows, vocab], rows target_stride apart                           */
@@ -538,6 +545,7 @@ typedef struct rr_verify_args {
   int32_t* accepted;         /* [batch]                                                           */
   int32_t* new_lens;         /* [batch] or NULL; may be lens itself                               */
   uint32_t* status;
+  const int32_t* room;       /* [batch] of rr_page_pool, with lens; or NULL                       */
   int64_t target_stride, draft_stride;
   int32_t dtype;             /* RR_BF16 or RR_F32, of target and draft                            */
   int32_t rows, batch, vocab;

@@ -69,7 +69,7 @@ class rr_paged_kv(C.Structure):
 
 
 class rr_append_args(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "q", "q_out", "lens", "cu", "new_lens", "inv_freq")] + \
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "q", "q_out", "lens", "cu", "new_lens", "inv_freq", "room")] + \
                [(n, C.c_int64) for n in (
                    "k_token_stride", "k_head_stride", "v_token_stride", "v_head_stride",
                    "q_token_stride", "q_head_stride", "out_token_stride", "out_head_stride")] + \
@@ -96,12 +96,12 @@ class rr_ranges_args(C.Structure):
 
 
 class rr_page_pool(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("page_table", "refs", "held", "free_pages", "status")] + [("table_stride", C.c_int64)] + \
+    _fields_ = [(n, C.c_void_p) for n in ("page_table", "refs", "held", "free_pages", "status", "room")] + [("table_stride", C.c_int64)] + \
                [(n, C.c_int32) for n in ("num_pages", "page_tokens", "batch", "pages_per_seq")]
 
 
 class rr_verify_args(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("target", "draft", "tokens", "cu", "uniform", "lens", "out", "accepted", "new_lens", "status")] + \
+    _fields_ = [(n, C.c_void_p) for n in ("target", "draft", "tokens", "cu", "uniform", "lens", "out", "accepted", "new_lens", "status", "room")] + \
                [("target_stride", C.c_int64), ("draft_stride", C.c_int64)] + \
                [(n, C.c_int32) for n in ("dtype", "rows", "batch", "vocab")]
 

@@ -27,6 +27,9 @@ struct AppendParams {
 
 template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Piece { T x[VEC]; };
 
+// All of a sequence's new tokens have room: a page may otherwise be another sequence's, too.
+__device__ __forceinline__ bool has_room(const rr_append_args& a, int b, int n) { return !a.room || (long long)a.lens[b] + n <= a.room[b]; }
+
 template <typename T, int VEC, bool AXES>
 __global__ void __launch_bounds__(MOST_NT)
 kv_append_kernel(const __grid_constant__ AppendParams P) {
@@ -38,8 +41,8 @@ kv_append_kernel(const __grid_constant__ AppendParams P) {
   const int tid = threadIdx.x, NT = blockDim.x, t = blockIdx.x;
   if (blockIdx.x == gridDim.x - 1 && a.new_lens)
     for (int b = tid; b < kv.batch; b += NT) {
-      const int n = a.cu ? a.cu[b + 1] - a.cu[b] : 1;
-      a.new_lens[b] = a.lens[b] + max(n, 0);
+      const int n = max(a.cu ? a.cu[b + 1] - a.cu[b] : 1, 0);
+      a.new_lens[b] = a.lens[b] + (has_room(a, b, n) ? n : 0);
     }
   if (t >= a.tokens) return;
   if (tid < 32) {
@@ -50,12 +53,13 @@ kv_append_kernel(const __grid_constant__ AppendParams P) {
       if (b >= 0) {
         const long long p = (long long)a.lens[b] + (a.cu ? t - a.cu[b] : 0);
         const long long col = p / kv.page_tokens;
+        const bool room = has_room(a, b, a.cu ? a.cu[b + 1] - a.cu[b] : 1);
         bool ok = p >= 0 && col < kv.pages_per_seq;
         int page = -1;
         if (ok) page = kv.page_table[b * kv.table_stride + col];
-        ok = ok && page >= 0 && page < kv.num_pages;
+        ok = ok && page >= 0 && page < kv.num_pages && room;
         if (ok) at = page * kv.page_stride + (p - col * kv.page_tokens) * kv.token_stride;
-        else if (kv.status) atomicOr(kv.status, RR_STATUS_BAD_INDEX);
+        else if (kv.status) atomicOr(kv.status, room ? RR_STATUS_BAD_INDEX : RR_STATUS_NO_PAGES);
         pos = p < 0 ? 0 : (int)min(p, 0x7FFFFFFFLL);
       }
       s_pos = pos;
@@ -161,7 +165,7 @@ int append(const rr_paged_kv* kv, const rr_append_args* a, const rr_axes_args* x
       a->q_head_stride < 0 || a->out_token_stride < 0 || a->out_head_stride < 0) return RR_ERR_INVALID_ARG;
   const uintptr_t e = kv->dtype == RR_BF16 ? 1 : 3;
   if ((((uintptr_t)a->k | (uintptr_t)a->v | (uintptr_t)a->q | (uintptr_t)(a->q ? a->q_out : nullptr)) & e) ||
-      (((uintptr_t)a->lens | (uintptr_t)a->cu | (uintptr_t)a->new_lens | (uintptr_t)a->inv_freq) & 3)) return RR_ERR_INVALID_ARG;
+      (((uintptr_t)a->lens | (uintptr_t)a->cu | (uintptr_t)a->new_lens | (uintptr_t)a->inv_freq | (uintptr_t)a->room) & 3)) return RR_ERR_INVALID_ARG;
   if constexpr (AXES) {
     if (!x || !x->positions || a->rot == 0 || x->axes < 1 || x->axis_stride < 0 || x->token_stride < 0) return RR_ERR_INVALID_ARG;
     if (((uintptr_t)x->positions | (uintptr_t)x->axis_of) & 3) return RR_ERR_INVALID_ARG;

@@ -341,6 +341,18 @@ __device__ __forceinline__ Slot* slot_of(Slot* slots, int mask, int page, bool a
   }
 }
 
+// Up to which place a row may be written after a call that has given nothing: to the first entry that would have been replaced, be it by a page of its own or, of a page
+// that all who hold it go on writing, by those of the others; else to the end of its pages, if some are missing.  refs and table do not change any more.
+__device__ __noinline__ int room_of(const PoolParams& P, const Row& r, int b) {
+  const rr_page_pool& p = P.p;
+  const int replaced = r.replaced >> 1, copied = r.replaced & 1;
+  int col = r.held;
+  if (r.want >= 0 && __ldcg(p.refs + r.want) > 1) col = r.c0;
+  else if (replaced > copied) col = __ldcg(replaced_of(P, b));
+  else if (r.held == r.c1) return INT32_MAX;
+  return (int)min((long long)col * p.page_tokens, (long long)INT32_MAX);
+}
+
 constexpr int LOOK = 4;                                 // entries of a row that a lane loads together
 constexpr int NEAR = 4;                                 // entries behind a row's tokens that its thread looks at itself
 
@@ -531,6 +543,7 @@ reserve_kernel(const __grid_constant__ PoolParams P) {
     if (b % CL != rank) continue;
     const int held = enough ? rows[b].c1 : rows[b].held;
     if (rows[b].was != held) p.held[b] = held;
+    if (p.room) p.room[b] = enough ? INT32_MAX : room_of(P, rows[b], b);
   }
   add_free(p, freed + freed_now);
 }
@@ -770,7 +783,7 @@ int check_pool(const rr_page_pool* p) {
   if (!p || !p->page_table || !p->refs || !p->held || !p->free_pages) return RR_ERR_INVALID_ARG;
   if (p->num_pages < 1 || p->page_tokens < 1 || p->batch < 1 || p->pages_per_seq < 1) return RR_ERR_INVALID_ARG;
   if (p->table_stride < (p->batch > 1 ? p->pages_per_seq : 0)) return RR_ERR_INVALID_ARG;
-  if (((uintptr_t)p->page_table | (uintptr_t)p->refs | (uintptr_t)p->held | (uintptr_t)p->free_pages | (uintptr_t)p->status) & 3) return RR_ERR_INVALID_ARG;
+  if (((uintptr_t)p->page_table | (uintptr_t)p->refs | (uintptr_t)p->held | (uintptr_t)p->free_pages | (uintptr_t)p->status | (uintptr_t)p->room) & 3) return RR_ERR_INVALID_ARG;
   if (p->num_pages > RR_PAGES_MAX_PAGES || p->batch > RR_PAGES_MAX_BATCH || (int64_t)p->batch * p->pages_per_seq > (1 << 30)) return RR_ERR_TOO_LARGE;
   return RR_OK;
 }

@@ -52,6 +52,7 @@ __device__ __forceinline__ double warp_sum(double x) {
   return x;
 }
 __device__ __forceinline__ void write_lengths(const rr_verify_args& a, int b, const Span& s, int accepted, int len) {
+  if (a.room && s.n >= 0 && (long long)len + s.n + 1 > a.room[b]) accepted = -1;       // (its rows are not in the cache)
   a.accepted[b] = accepted;
   if (a.new_lens) a.new_lens[b] = len + (s.n < 0 ? 0 : accepted + 1);
 }
@@ -60,7 +61,7 @@ __device__ __forceinline__ void write_accepted(const rr_verify_args& a, int b, c
   const int lane = threadIdx.x & 31;
   for (int i = lane; i <= s.n; i += 32)
     if (i != accepted) a.out[s.first + i] = i < accepted ? a.tokens[s.first + i + 1] : -1;
-  if (lane == 0) write_lengths(a, b, s, accepted, a.new_lens ? a.lens[b] : 0);
+  if (lane == 0) write_lengths(a, b, s, accepted, a.new_lens || a.room ? a.lens[b] : 0);
 }
 
 // A drafted token is in the vocabulary.
@@ -366,7 +367,7 @@ compare_kernel(const __grid_constant__ rr_verify_args a) {
   const bool mine = b < a.batch;
   const Span s = mine ? span_of(a, b) : Span{0, -1};
   int x = lane < s.n ? a.tokens[s.first + lane + 1] : 0;
-  const int len = mine && a.new_lens ? a.lens[b] : 0;
+  const int len = mine && (a.new_lens || a.room) ? a.lens[b] : 0;
   rr_pdl_wait();
   rr_pdl_trigger();
   if (!mine) return;
@@ -414,13 +415,13 @@ extern "C" int rr_verify_drafts(const rr_verify_args* a, void* stream) {
   if (!a || !a->out || !a->accepted || !a->tokens || (!a->target && a->rows > 0)) return RR_ERR_INVALID_ARG;
   if (a->rows < 0 || a->batch < 1 || a->vocab < 1 || (!a->cu && a->rows != a->batch)) return RR_ERR_INVALID_ARG;
   if (a->out == a->tokens && a->rows > 0) return RR_ERR_INVALID_ARG;                       // (tokens are read while results are written)
-  if (a->target_stride < 0 || a->draft_stride < 0 || (a->new_lens && !a->lens) || (a->draft && !a->uniform)) return RR_ERR_INVALID_ARG;
+  if (a->target_stride < 0 || a->draft_stride < 0 || ((a->new_lens || a->room) && !a->lens) || (a->draft && !a->uniform)) return RR_ERR_INVALID_ARG;
   if (a->dtype != RR_BF16 && a->dtype != RR_F32) return RR_ERR_UNSUPPORTED;
   if (a->vocab > (1 << 30) || a->batch > (1 << 27)) return RR_ERR_TOO_LARGE;
   const uintptr_t e = a->dtype == RR_BF16 ? 1 : 3;
   if ((((uintptr_t)a->target | (uintptr_t)a->draft) & e) ||
       (((uintptr_t)a->tokens | (uintptr_t)a->cu | (uintptr_t)a->uniform | (uintptr_t)a->lens | (uintptr_t)a->out | (uintptr_t)a->accepted |
-        (uintptr_t)a->new_lens | (uintptr_t)a->status) & 3)) return RR_ERR_INVALID_ARG;
+        (uintptr_t)a->new_lens | (uintptr_t)a->status | (uintptr_t)a->room) & 3)) return RR_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
   const bool bf16 = a->dtype == RR_BF16;
   if (a->uniform) {

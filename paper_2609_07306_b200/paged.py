@@ -11,7 +11,7 @@ import torch
 from . import binding as B
 
 # rr_append_args, rr_axes_args, rr_shared_args and rr_ranges_args as bytes (a call's arguments in one step; 64-bit alignment throughout)
-_APPEND = struct.Struct("@8P8q4i")
+_APPEND = struct.Struct("@9P8q4i")
 _AXES = struct.Struct("@2P2qi4x")
 _SHARED = struct.Struct("@5P4q4if4x")
 _RANGES = struct.Struct("@4P6q6if4x")
@@ -82,6 +82,7 @@ class PagedKV:
             pages_per_seq=page_table.shape[1])
         self._at = C.addressof(self._kv)
         self._lib = B.lib()
+        self._room, self._p_room = None, 0             # a PagePool's (pages.py)
 
     # what the description points to: the tensors are written to, not exchanged
     k_cache = property(lambda self: self._tensors[0])
@@ -153,6 +154,8 @@ class PagedKV:
         inv_freq  [rot / 2] float32, rotates the first rot entries of a head: the pairs (j, j + rot / 2), or with
                   interleaved=True (2 j, 2 j + 1); None: nothing is rotated
         new_lens  [batch] int32: gets lens + new tokens (another tensor than lens)
+        (A sequence for which the last PagePool.reserve of a pool over this cache could not give all pages, and whose tokens would reach behind its room: none of them
+        is written, new_lens stays at lens, RR_STATUS_NO_PAGES is set.)
         positions [axes, tokens] int32 (any strides): the tokens' positions on every axis -- time, height and width of the patches of images
                   and videos, or one axis of other positions than the places in the cache; None: lens and on
         axis_of   [rot / 2] int32: the axis that turns each pair (axis_sections makes one); None: there is one axis"""
@@ -198,7 +201,7 @@ class PagedKV:
         self._run("rr_kv_append" if more is None else "rr_kv_append_axes", _APPEND.pack(
             k.data_ptr(), v.data_ptr(), q.data_ptr() if heads else 0, q_out.data_ptr() if heads else 0, lens.data_ptr(),
             0 if cu is None else cu.data_ptr(), 0 if new_lens is None else new_lens.data_ptr(),
-            0 if rot == 0 else inv_freq.data_ptr(), ks[0], ks[1], vs[0], vs[1], *q_strides, n, heads, rot,
+            0 if rot == 0 else inv_freq.data_ptr(), self._p_room, ks[0], ks[1], vs[0], vs[1], *q_strides, n, heads, rot,
             1 if interleaved else 0), None, more)
         return q_out
 

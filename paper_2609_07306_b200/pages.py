@@ -21,6 +21,9 @@ class PagePool:
     status      optional [1] int32: RR_STATUS_* bits are OR-ed into it (RR_STATUS_BAD_INDEX: a page id outside the pool, a negative length or one
                 behind the table's end; RR_STATUS_NO_PAGES: fewer free pages than a call of reserve needed, which then gave none)
 
+    room        [batch] int32, made by the pool: up to which place each sequence may be written to, 2^31 - 1 unless the last call of reserve could not give it all of its pages.
+                The caches' append goes by the room of the pool that was made over them last (calls that are captured later, not those in an older graph)
+
     PagePool.empty makes the state of a pool whose pages are all free.  The object keeps the tensors (they are written to, not exchanged) and one
     workspace.  Its calls change the state: order them, and the operators that read the table, on one stream or by events;
     graphs that hold them may not run at the same time.  Keep the object until its work on streams other than the one that it was made on has
@@ -48,16 +51,20 @@ class PagePool:
                 raise ValueError(f"cache {i} is on {kv.device}, the page table on {self.device}")
             if kv.page_tokens != page_tokens or kv.k_cache.shape[0] != self.num_pages:
                 raise ValueError(f"cache {i} has {kv.k_cache.shape[0]} pages of {kv.page_tokens} tokens, the pool {self.num_pages} of {page_tokens}")
-        self._tensors = (page_table, refs, held, free, status, caches)
+        # (a cache of a table that is kept like this one may have more rows, which no call closes)
+        room = torch.full((max([self.batch] + [kv.batch for kv in caches]),), 0x7FFFFFFF, dtype=torch.int32, device=self.device)
+        self._tensors = (page_table, refs, held, free, status, caches, room[:self.batch])
         self._pool = B.rr_page_pool(
             page_table=page_table.data_ptr(), refs=refs.data_ptr(), held=held.data_ptr(), free_pages=free.data_ptr(),
-            status=None if status is None else status.data_ptr(), table_stride=page_table.stride(0), num_pages=self.num_pages,
+            status=None if status is None else status.data_ptr(), room=room.data_ptr(), table_stride=page_table.stride(0), num_pages=self.num_pages,
             page_tokens=page_tokens, batch=self.batch, pages_per_seq=page_table.shape[1])
         self._caches = (B.rr_paged_kv * max(1, len(caches)))(*[kv._kv for kv in caches])
         self._lib = B.lib()
         self._bytes = B.rr_pages_workspace(self._pool)
         self._ws = torch.empty(self._bytes, dtype=torch.uint8, device=self.device)
         self._at, self._caches_at, self._layers, self._ws_at = C.addressof(self._pool), C.addressof(self._caches), len(caches), self._ws.data_ptr()
+        for kv in caches:
+            kv._room, kv._p_room = room, room.data_ptr()
 
     @classmethod
     def empty(cls, caches: "list[PagedKV] | tuple[PagedKV, ...]", status: torch.Tensor | None = None) -> "PagePool":
@@ -78,6 +85,7 @@ class PagePool:
     free = property(lambda self: self._tensors[3])
     status = property(lambda self: self._tensors[4])
     caches = property(lambda self: self._tensors[5])
+    room = property(lambda self: self._tensors[6])
 
     _ints = PagedKV._ints
 
@@ -111,8 +119,10 @@ class PagePool:
         too becomes the sequence's own, its tokens copied in all caches.  reserve(lens) with lens[b] = 0 frees a sequence.
         lens  [batch] int32
         new   an int, or [batch] int32
-        If the pool has fewer free pages than the call needs, none is given (RR_STATUS_NO_PAGES) and rows are only shortened:
-        with new / page_tokens + 2 free pages per sequence there are always enough."""
+        If the pool has fewer free pages than the call needs, none is given (RR_STATUS_NO_PAGES) and rows are only shortened; with new / page_tokens + 2 free
+        pages per sequence there are always enough.  A sequence that lacks pages, or whose page is another's, too, is closed until a call succeeds: the caches' append
+        writes none of its tokens and leaves its length (room; give it to verify_drafts as well), so that a captured step that is not looked at in between harms
+        no other sequence.  What else writes to the caches has to go by the status or by room."""
         shape = (self.batch,)
         self._ints(lens, "lens", shape)
         if isinstance(new, torch.Tensor):

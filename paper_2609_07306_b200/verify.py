@@ -9,7 +9,7 @@ import torch
 from . import binding as B
 
 # rr_verify_args as bytes
-_VERIFY = struct.Struct("@10P2q4i")
+_VERIFY = struct.Struct("@11P2q4i")
 
 _DTYPES = {torch.bfloat16: B.RR_BF16, torch.float32: B.RR_F32}
 
@@ -38,7 +38,7 @@ def _rows(t, name, dtype, shape, index):
 
 def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor | None = None, *, draft: torch.Tensor | None = None,
                   uniform: torch.Tensor | None = None, lens: torch.Tensor | None = None, new_lens: torch.Tensor | None = None,
-                  status: torch.Tensor | None = None) -> "tuple[torch.Tensor, torch.Tensor]":
+                  status: torch.Tensor | None = None, room: torch.Tensor | None = None) -> "tuple[torch.Tensor, torch.Tensor]":
     """Verifies the drafted tokens of a step.  Sequence b owns the rows cu[b] .. cu[b + 1] - 1: its last known token and the drafts behind it;
     rows behind cu[batch] are padding.  Returns (next, accepted):
         next      [rows] int32: the token that follows each row: the accepted drafts, one token more, then -1 (padding: not written)
@@ -55,6 +55,8 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor |
     new_lens  [batch] int32: gets lens + accepted + 1, the tokens that stay of sequences that had lens tokens before the step's rows were
               appended (may be lens itself): what PagePool.reserve takes next
     status    [1] int32: RR_STATUS_BAD_INDEX is OR-ed into it if a drafted token is outside the vocabulary (it is rejected)
+    room      [batch] int32, PagePool.room, with lens: a sequence whose rows had no room, so that they were not appended, has accepted = -1 and keeps its lens; its
+              next tokens are not to be used
     Work goes to the current stream of target's device.  No gradient."""
     if target.dim() != 2 or tokens.dim() != 1:
         raise ValueError("target must be [rows, vocab] and tokens [rows]")
@@ -65,12 +67,12 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor |
         raise ValueError("target must be on a CUDA device (there is no CPU path)")
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
-            return verify_drafts(target, tokens, cu, draft=draft, uniform=uniform, lens=lens, new_lens=new_lens, status=status)
+            return verify_drafts(target, tokens, cu, draft=draft, uniform=uniform, lens=lens, new_lens=new_lens, status=status, room=room)
     rows, vocab = shape = tuple(target.shape)
     stride = _rows(target, "target", target.dtype, shape, index)
     i32, one = torch.int32, (rows,)
     p_tokens = _tensor(tokens, "tokens", i32, one, index)
-    p_cu = p_draft = p_uniform = p_lens = p_new = p_status = draft_stride = 0
+    p_cu = p_draft = p_uniform = p_lens = p_new = p_status = p_room = draft_stride = 0
     batch = rows
     if cu is not None:
         batch = cu.shape[0] - 1 if cu.dim() == 1 else 0
@@ -96,6 +98,10 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor |
         p_new = _tensor(new_lens, "new_lens", i32, (batch,), index)
     if status is not None:
         p_status = _tensor(status, "status", i32, (1,), index)
+    if room is not None:
+        if lens is None:
+            raise ValueError("room without lens")
+        p_room = _tensor(room, "room", i32, (batch,), index)
     after = torch.empty_like(tokens)
     accepted = tokens.new_empty((batch,)) if lens is None else torch.empty_like(lens)
     if rows == 0:                                      # (an empty tensor has no address, and nothing is read)
@@ -103,7 +109,7 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor |
         p_uniform = p_draft = 0
     else:
         p_out = after.data_ptr()
-    rc = B.lib().rr_verify_drafts(_VERIFY.pack(target.data_ptr(), p_draft, p_tokens, p_cu, p_uniform, p_lens, p_out, accepted.data_ptr(), p_new, p_status,
+    rc = B.lib().rr_verify_drafts(_VERIFY.pack(target.data_ptr(), p_draft, p_tokens, p_cu, p_uniform, p_lens, p_out, accepted.data_ptr(), p_new, p_status, p_room,
                                                stride, draft_stride, code, rows, batch, vocab),
                                   torch._C._cuda_getCurrentRawStream(index))
     if rc != B.RR_OK:
