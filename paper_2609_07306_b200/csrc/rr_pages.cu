@@ -184,11 +184,12 @@ __device__ __forceinline__ Heir heir_of(const PoolParams& P, int b, bool tell) {
     if (tell) report(p, RR_STATUS_BAD_INDEX);
     h.parent = b;
   }
-  const int len = h.parent < 0 ? 0 : __ldcg(P.lens + h.parent);
-  if (h.parent != b) h.takes = h.parent < 0 ? 0 : (int)min((unsigned)held_of(p, h.parent), ((unsigned)max(len, 0) + p.page_tokens - 1) / p.page_tokens);
+  const int given = h.parent < 0 ? 0 : __ldcg(P.lens + h.parent);
+  const int len = (int)min((long long)max(given, 0), (long long)p.page_tokens * p.pages_per_seq);
+  if (h.parent != b) h.takes = h.parent < 0 ? 0 : (int)min((unsigned)held_of(p, h.parent), ((unsigned)len + p.page_tokens - 1) / p.page_tokens);
   if (tell) {
-    if (len < 0) report(p, RR_STATUS_BAD_INDEX);
-    P.new_lens[b] = max(len, 0);
+    if (len != given) report(p, RR_STATUS_BAD_INDEX);
+    P.new_lens[b] = len;
   }
   return h;
 }
