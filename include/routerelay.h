@@ -497,7 +497,7 @@ int rr_pages_workspace(const rr_page_pool* pool, size_t* bytes);
 
 /* Row b becomes what row parents[b] was before the call, all rows at once: beams that descend from others, samples of one
  * prompt.  parents[b] == b: the row stays, parents[b] == -1: the sequence has ended and its row is emptied.  A child holds the pages of its
- * parent's lens tokens together with it, no page is copied.  Writes the new lengths to new_lens (not lens itself). */
+ * parent's lens tokens together with it, no page is copied (an entry with an id outside the pool becomes -1).  Writes the new lengths to new_lens (not lens itself). */
 int rr_pages_fork(const rr_page_pool* pool, const int32_t* parents, const int32_t* lens, int32_t* new_lens,
                   void* workspace, size_t bytes, void* stream);
 

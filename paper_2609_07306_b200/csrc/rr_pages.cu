@@ -204,11 +204,15 @@ __device__ __forceinline__ int stage_run(const PoolParams& P, int b, int c0, con
   int freed = 0;
 #pragma unroll 2
   for (int c = c0 + (threadIdx.x & 31); c < end; c += 32) {
-    const int was = c < h.held ? __ldcg(mine + c) : -1, is = c < h.takes ? __ldcg(theirs + c) : -1;
+    const int was = c < h.held ? __ldcg(mine + c) : -1;
+    int is = c < h.takes ? __ldcg(theirs + c) : -1;
+    if (c < h.takes && !in_pool(p, is)) {               // left out: the column stays, without a page
+      is = -1;
+      report(p, RR_STATUS_BAD_INDEX);
+    }
     stage[c] = is;
     if (was == is) continue;
-    if (in_pool(p, is)) freed -= atomicAdd(p.refs + is, 1) == 0;        // (one row may let go of a page before another takes it)
-    else if (c < h.takes) report(p, RR_STATUS_BAD_INDEX);
+    if (is >= 0) freed -= atomicAdd(p.refs + is, 1) == 0;               // (one row may let go of a page before another takes it)
     if (in_pool(p, was)) freed += release(p, was);
     else if (c < h.held) report(p, RR_STATUS_BAD_INDEX);
   }

@@ -42,3 +42,21 @@ def test_lengths_behind_the_table(batch, width):
     pool.status.zero_()
     pool.fork(ints([0, 1, 0] + [-1] * (batch - 3)), ints([cap, 7, cap] + [0] * (batch - 3)), new)     # as long as the table: nothing to report
     assert new.tolist() == [cap, 7, cap] + [0] * (batch - 3) and pool.status.item() == 0
+
+
+@pytest.mark.parametrize("batch,width", SHAPES)
+@pytest.mark.parametrize("bad", [-1, -5, "pages", 0x7FFFFFFF])
+def test_ids_outside_the_pool(batch, width, bad):
+    """They are left out of the rows that are forked, reported, and held by nobody; the row that has one stays as it is."""
+    pages = 3 * width
+    bad = pages if bad == "pages" else bad
+    pool = make(batch, width, pages)
+    pool.reserve(ints([0] * batch), ints([11, 5, 9] + [0] * (batch - 3)))          # pages 0 1 2, 3 4, 5 6 7
+    pool.page_table[0, 1] = bad
+    pool.page_table[1, 1] = bad
+    new = ints([0] * batch)
+    pool.fork(ints([0, 0, 0] + [-1] * (batch - 3)), ints([11, 5, 9] + [0] * (batch - 3)), new)
+    assert pool.status.item() == B.RR_STATUS_BAD_INDEX and new.tolist()[:3] == [11] * 3 and pool.held.tolist()[:3] == [3] * 3
+    assert pool.page_table[:3, :4].tolist() == [[0, bad, 2, -1], [0, -1, 2, -1], [0, -1, 2, -1]]
+    # page 1 was row 0's before its entry went wrong, page 4 row 1's: nobody has taken them off
+    assert pool.refs.tolist()[:9] == [3, 1, 3, 0, 1, 0, 0, 0, 0] and pool.free.item() == pages - 4
