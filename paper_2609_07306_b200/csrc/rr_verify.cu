@@ -26,16 +26,18 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-// The kernels may be launched before the one in front of them has ended (rr_launch_pdl), so nothing is read by way of the read-only path.  Every CTA reads
-// the same few numbers in the beginning: through L1 (all from L2: 2 us more).
+// The kernels may be launched before the one in front of them has ended (rr_launch_pdl), so nothing is read by way of the read-only path.  Behind
+// its wait every CTA reads the same few numbers in the beginning: through L1 (all from L2: 2 us more).
 
 constexpr int NT = 256, NW = NT / 32, BLOCK = 256, MAX_CL = 8;
 constexpr int SUMS = 64;                                // blocks' sums that a CTA keeps
 
 struct Span { int first, n; };                          // a sequence's first row, its drafts (-1: it has no rows)
 
+template <bool L2 = false> __device__ __forceinline__ int load(const int32_t* p) { return L2 ? __ldcg(p) : *p; }
+template <bool L2 = false>
 __device__ __forceinline__ Span span_of(const rr_verify_args& a, int b) {
-  const int first = a.cu ? max(a.cu[b], 0) : b, end = a.cu ? min(a.cu[b + 1], a.rows) : b + 1;
+  const int first = a.cu ? max(load<L2>(a.cu + b), 0) : b, end = a.cu ? min(load<L2>(a.cu + b + 1), a.rows) : b + 1;
   return Span{first, max(end - first, 0) - 1};
 }
 
@@ -360,14 +362,15 @@ best_kernel(const __grid_constant__ rr_verify_args a) {
 }
 
 // The drafts against the rows' best tokens, which are in `out`: up to the first that differs they are the accepted tokens and the one more.  Launched along with
-// best_kernel, which starts it when all before itself has ended, so only `out` has to be waited for.
+// best_kernel, which starts it when all before itself has ended, so only `out` has to be waited for.  What is read in front of the wait comes by way of L2, where the ended
+// kernels have left it; that L1 holds nothing older is certain behind the wait only.
 __global__ void __launch_bounds__(128)
 compare_kernel(const __grid_constant__ rr_verify_args a) {
   const int lane = threadIdx.x & 31, b = blockIdx.x * 4 + (threadIdx.x >> 5);
   const bool mine = b < a.batch;
-  const Span s = mine ? span_of(a, b) : Span{0, -1};
-  int x = lane < s.n ? a.tokens[s.first + lane + 1] : 0;
-  const int len = mine && (a.new_lens || a.room) ? a.lens[b] : 0;
+  const Span s = mine ? span_of<true>(a, b) : Span{0, -1};
+  int x = lane < s.n ? load<true>(a.tokens + s.first + lane + 1) : 0;
+  const int len = mine && (a.new_lens || a.room) ? load<true>(a.lens + b) : 0;
   rr_pdl_wait();
   rr_pdl_trigger();
   if (!mine) return;
