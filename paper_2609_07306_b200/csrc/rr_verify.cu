@@ -11,13 +11,14 @@
 // finds for itself (a few dependent loads, instead of a barrier).  A warp reads a block of 256 entries at a time, eight per lane from each row, the next block's loads
 // in front of this one's arithmetic, and leaves its lanes' sums; the CTAs exchange their totals, the one that has the threshold finds block and
 // entry, so the row is read once but for that block.  Products, differences and sums are 64-bit: the first two are exact for probabilities of up
-// to 24 bits, and a sum over the vocabulary is off by some 1e-14, so that a random number falls between two results about never.  That arithmetic costs as
-// much as the memory: 64 sequences against 131071 tokens (49 MB read from L2) took 19 us with two conversions and four selections an entry, 17 us with eight instructions.
+// to 24 bits, and a sum over the vocabulary is off by some 1e-14, so that a random number falls between two results about never.  For 64 sequences
+// against 131071 tokens (49 MB) two conversions, two selections and two 64-bit sums an entry are, by their number, some 2 us; the rest is the rows, an uneven end (one row or two for
+// the same CTAs) and the search behind them.
 // (Rings of blocks in shared memory, filled by bulk copies: 27 us; fewer warps fit, and each has its chain of 64-bit sums.)
 // Greedy: a cluster takes a row, whoever's it is (sequences with many drafts would hold up the others), 16 bytes at a time where rows
 // allow it; only maxima are taken (a packed maximum of two bf16 costs one instruction), a thread keeps its first best vector, and the entry inside it is looked
 // up at the end.  The rows' best tokens go to `out`, where a second kernel, a warp per sequence, compares them with the drafts.
-// Measured: those 64 sequences 15.7 us, 19.7 from memory; one sequence against 32768 tokens 6.4 us; greedy, 415 rows of 131072 in bf16 (109 MB) 22 us from memory.
+// Measured: those 64 sequences 15.9 us, 20.1 from memory, in bf16 15.0 and 17.2, without the draft's probabilities 13.8 and 16.5; one sequence against 32768 tokens 6.4 us; greedy, 415 rows of 131072 in bf16 (109 MB) 22 us from memory.
 #include <cooperative_groups.h>
 #include <utility>
 #include "rr_paged.cuh"
@@ -112,24 +113,22 @@ template <typename T> struct Block {
       }
     }
   }
-  // The sum of the lane's eight weights, by eight instructions each.  With z = max(x, y), where x - y is below 0 or x is NaN it is 0; elsewhere z - y is d = fl(z - y) and the
-  // rest (z - d) - y, which FP32 holds without error, as z >= y >= 0: one conversion instead of two; the rests, 2^-24 of their terms and less, are added in
-  // FP32.  An infinite number makes a sum that is none, and the eight are looked at one by one, as are those of the block with `but`.
+  // The sum of the lane's eight weights, in 64 bits throughout.  With z = max(x, y) the weight is z - y: 0 where x - y is below 0 or x is NaN.
+  // An infinite number makes a sum that is none, and the eight are looked at one by one, as are those of the block with `but`.  (One conversion an entry instead of
+  // two, of the difference rounded to FP32, with its rest added in FP32: sums of eight off by up to 7e-15, and slower, 17.1 against 15.9 us for 64 sequences of 131071.)
   __device__ __forceinline__ double sum(const T* prow, const T* qrow, int vocab, int first, int but) const {
     double s[2] = {0.0, 0.0};
-    float rest = 0.f;
     if (qrow) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float y = fmaxf(rr_to_f32(q[i]), 0.f), z = fmaxf(rr_to_f32(p[i]), y), d = z - y;
-        rest += (z - d) - y;
-        s[i & 1] += (double)d;
+        const float y = fmaxf(rr_to_f32(q[i]), 0.f), z = fmaxf(rr_to_f32(p[i]), y);
+        s[i & 1] += (double)z - (double)y;
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i & 1] += (double)fmaxf(rr_to_f32(p[i]), 0.f);
     }
-    const double all = s[0] + s[1] + (double)rest;
+    const double all = s[0] + s[1];
     return !isfinite(all) || (but >= first && but < first + BLOCK) ? one_by_one(prow, qrow, vocab, first, but) : all;
   }
 };
