@@ -75,9 +75,10 @@ class PagePool:
         table, pages = caches[0].page_table, caches[0].k_cache.shape[0]
         if any(kv.page_table.data_ptr() != table.data_ptr() or kv.page_table.shape != table.shape for kv in caches):
             raise ValueError("the caches must have one page table")
-        table.fill_(-1)
         zeros = [torch.zeros(n, dtype=torch.int32, device=table.device) for n in (pages, table.shape[0])]
-        return cls(table, caches[0].page_tokens, *zeros, torch.full((1,), pages, dtype=torch.int32, device=table.device), caches, status)
+        pool = cls(table, caches[0].page_tokens, *zeros, torch.full((1,), pages, dtype=torch.int32, device=table.device), caches, status)
+        table.fill_(-1)                                # (caches that do not go together have been refused by now)
+        return pool
 
     page_table = property(lambda self: self._tensors[0])
     refs = property(lambda self: self._tensors[1])
