@@ -3,6 +3,7 @@ bookkeeping and the copies of pages run in the library's kernels; PyTorch is use
 from __future__ import annotations
 
 import ctypes as C
+from operator import index
 
 import torch
 
@@ -130,9 +131,9 @@ class PagePool:
             self._ints(new, "new", shape)
             tokens, each = new.data_ptr(), 0
         else:
-            if not 0 <= new <= 0x7FFFFFFF:
+            tokens, each = None, index(new)                # (a number that is not whole is refused, not cut)
+            if not 0 <= each <= 0x7FFFFFFF:
                 raise ValueError(f"new must be between 0 and 2^31 - 1, not {new}")
-            tokens, each = None, int(new)
         if not self._layers:
             raise ValueError("reserve copies pages: the pool needs its caches")
         stream = self._stream()

@@ -1,4 +1,5 @@
-"""What making a pool refuses: nothing is written by a call that is refused."""
+"""What making a pool and asking it for room refuse: nothing is written by a call that is refused."""
+import numpy as np
 import pytest
 import torch
 
@@ -27,3 +28,14 @@ def test_a_refused_pool_leaves_the_table(other):
         PagePool.empty([cache(table)], status=ints([0, 0]))
     assert torch.equal(table, was)
     assert (PagePool.empty([cache(table)]).page_table == -1).all() and (table == -1).all()
+
+
+def test_room_for_a_number_that_is_whole():
+    table = torch.zeros((3, 4), dtype=torch.int32, device="cuda")
+    pool = PagePool.empty([cache(table)])
+    for new in (2.5, 2.0, "2", None, np.float32(1)):
+        with pytest.raises(TypeError):
+            pool.reserve(ints([0] * 3), new)
+    assert (pool.refs == 0).all()
+    pool.reserve(ints([0] * 3), np.int64(5))
+    assert pool.held.tolist() == [2] * 3
