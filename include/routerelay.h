@@ -389,7 +389,7 @@ typedef struct rr_paged_kv {
  * With rot > 0 the first `rot` entries of every key head, and of every query head, are rotated by the
  * token's position p: pair j is turned by the angle p * inv_freq[j]; the pair is (j, j + rot / 2), or with
  * interleaved != 0 (2 j, 2 j + 1).  The product p * inv_freq[j] is formed and reduced in 64 bits, at any position.
- * Writes lens[b] + number of new tokens to new_lens[b] if new_lens is given (not lens itself).
+ * Writes lens[b] + number of new tokens to new_lens[b] if new_lens is given (memory that neither lens nor cu has any of).
  * With `room`, a sequence of which lens[b] + number of new tokens is above room[b] gets none of them: nothing is written to its pages,
  * new_lens[b] is lens[b], and RR_STATUS_NO_PAGES is set in *status.  (Queries are rotated all the same.) */
 typedef struct rr_append_args {
@@ -497,7 +497,8 @@ int rr_pages_workspace(const rr_page_pool* pool, size_t* bytes);
 
 /* Row b becomes what row parents[b] was before the call, all rows at once: beams that descend from others, samples of one
  * prompt.  parents[b] == b: the row stays, parents[b] == -1: the sequence has ended and its row is emptied.  A child holds the pages of its
- * parent's lens tokens together with it, no page is copied (an entry with an id outside the pool becomes -1).  Writes the new lengths to new_lens (not lens itself). */
+ * parent's lens tokens together with it, no page is copied (an entry with an id outside the pool becomes -1).  Writes the new lengths to new_lens (memory that
+ * neither lens, parents nor the pool has any of). */
 int rr_pages_fork(const rr_page_pool* pool, const int32_t* parents, const int32_t* lens, int32_t* new_lens,
                   void* workspace, size_t bytes, void* stream);
 
@@ -541,9 +542,9 @@ typedef struct rr_verify_args {
   const int32_t* cu;         /* [batch + 1] ascending, cu[0] = 0; or NULL                         */
   const float* uniform;      /* [rows] in [0, 1), or NULL                                         */
   const int32_t* lens;       /* [batch], with new_lens                                            */
-  int32_t* out;              /* [rows], other memory than tokens                                  */
+  int32_t* out;              /* [rows]; results: other memory than the inputs and than each other, but for: */
   int32_t* accepted;         /* [batch]                                                           */
-  int32_t* new_lens;         /* [batch] or NULL; may be lens itself                               */
+  int32_t* new_lens;         /* [batch] or NULL; may be lens itself, entry by entry                */
   uint32_t* status;
   const int32_t* room;       /* [batch] of rr_page_pool, with lens; or NULL                       */
   int64_t target_stride, draft_stride;

@@ -160,7 +160,10 @@ int append(const rr_paged_kv* kv, const rr_append_args* a, const rr_axes_args* x
   if (a->q && (!a->q_out || a->q_heads < 1)) return RR_ERR_INVALID_ARG;
   if (a->rot < 0 || a->rot > kv->dh || (a->rot & 1) || (a->rot > 0 && !a->inv_freq)) return RR_ERR_INVALID_ARG;
   if (a->interleaved != 0 && a->interleaved != 1) return RR_ERR_INVALID_ARG;
-  if (a->new_lens == a->lens) return RR_ERR_INVALID_ARG;
+  const int64_t row = 4 * (int64_t)kv->batch;
+  // (lengths are written while others are read)
+  if (a->new_lens == a->lens || !rr_apart(a->new_lens, row, a->lens, row) || !rr_apart(a->new_lens, row, a->cu, row + 4) || !rr_apart(a->new_lens, row, a->room, row))
+    return RR_ERR_INVALID_ARG;
   if (a->k_token_stride < 0 || a->k_head_stride < 0 || a->v_token_stride < 0 || a->v_head_stride < 0 || a->q_token_stride < 0 ||
       a->q_head_stride < 0 || a->out_token_stride < 0 || a->out_head_stride < 0) return RR_ERR_INVALID_ARG;
   const uintptr_t e = kv->dtype == RR_BF16 ? 1 : 3;

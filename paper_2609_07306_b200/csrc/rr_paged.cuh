@@ -16,6 +16,12 @@ inline int rr_paged_check(const rr_paged_kv* kv) {
   return RR_OK;
 }
 
+// Whether two runs of bytes have none in common (an empty one, or one that is not given, has none).
+inline bool rr_apart(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return !a || !b || na <= 0 || nb <= 0 || (x < y ? y - x >= (uint64_t)na : x - y >= (uint64_t)nb);
+}
+
 template <typename T> __device__ __forceinline__ float rr_to_f32(T x);
 template <> __device__ __forceinline__ float rr_to_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ float rr_to_f32<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }

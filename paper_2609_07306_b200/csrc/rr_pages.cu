@@ -880,7 +880,13 @@ extern "C" int rr_pages_fork(const rr_page_pool* pool, const int32_t* parents, c
                              void* stream) {
   int rc = check_pool(pool);
   if (rc != RR_OK) return rc;
-  if (!parents || !lens || !new_lens || lens == new_lens || parents == new_lens) return RR_ERR_INVALID_ARG;
+  if (!parents || !lens || !new_lens) return RR_ERR_INVALID_ARG;
+  // new_lens is written while parents, lens and the pool's state are read
+  const int64_t row = 4 * (int64_t)pool->batch, table = 4 * ((pool->batch - 1) * pool->table_stride + pool->pages_per_seq);
+  const bool apart = rr_apart(new_lens, row, parents, row) && rr_apart(new_lens, row, lens, row) && rr_apart(new_lens, row, pool->held, row) &&
+                     rr_apart(new_lens, row, pool->room, row) && rr_apart(new_lens, row, pool->refs, 4 * (int64_t)pool->num_pages) &&
+                     rr_apart(new_lens, row, pool->free_pages, 4) && rr_apart(new_lens, row, pool->status, 4) && rr_apart(new_lens, row, pool->page_table, table);
+  if (!apart) return RR_ERR_INVALID_ARG;
   if (((uintptr_t)parents | (uintptr_t)lens | (uintptr_t)new_lens) & 3) return RR_ERR_INVALID_ARG;
   if ((rc = check_workspace(pool, workspace, bytes)) != RR_OK) return rc;
   PoolParams P{*pool, work_of(*pool, workspace), parents, lens, new_lens, nullptr, 0, 0, 0};

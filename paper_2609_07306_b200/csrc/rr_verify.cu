@@ -416,7 +416,6 @@ int done(cudaError_t e) { return e == cudaSuccess ? RR_OK : rr_cuda_fail(e, "rr_
 extern "C" int rr_verify_drafts(const rr_verify_args* a, void* stream) {
   if (!a || !a->out || !a->accepted || !a->tokens || (!a->target && a->rows > 0)) return RR_ERR_INVALID_ARG;
   if (a->rows < 0 || a->batch < 1 || a->vocab < 1 || (!a->cu && a->rows != a->batch)) return RR_ERR_INVALID_ARG;
-  if (a->out == a->tokens && a->rows > 0) return RR_ERR_INVALID_ARG;                       // (tokens are read while results are written)
   if (a->target_stride < 0 || a->draft_stride < 0 || ((a->new_lens || a->room) && !a->lens) || (a->draft && !a->uniform)) return RR_ERR_INVALID_ARG;
   if (a->dtype != RR_BF16 && a->dtype != RR_F32) return RR_ERR_UNSUPPORTED;
   if (a->vocab > (1 << 30) || a->batch > (1 << 27)) return RR_ERR_TOO_LARGE;
@@ -424,8 +423,20 @@ extern "C" int rr_verify_drafts(const rr_verify_args* a, void* stream) {
   if ((((uintptr_t)a->target | (uintptr_t)a->draft) & e) ||
       (((uintptr_t)a->tokens | (uintptr_t)a->cu | (uintptr_t)a->uniform | (uintptr_t)a->lens | (uintptr_t)a->out | (uintptr_t)a->accepted |
         (uintptr_t)a->new_lens | (uintptr_t)a->status | (uintptr_t)a->room) & 3)) return RR_ERR_INVALID_ARG;
-  cudaStream_t st = (cudaStream_t)stream;
+  // Results are written while inputs are read.  (A sequence's length is read by the thread that writes its results: these may take its place.)
   const bool bf16 = a->dtype == RR_BF16;
+  const int64_t rows = 4 * (int64_t)a->rows, row = 4 * (int64_t)a->batch, entry = bf16 ? 2 : 4;
+  const struct { const void* p; int64_t n; } results[] = {{a->out, rows}, {a->accepted, row}, {a->new_lens, row}},
+    inputs[] = {{a->tokens, rows}, {a->cu, row + 4}, {a->uniform, rows}, {a->lens, row}, {a->room, row}, {a->status, 4},
+                {a->target, a->rows > 0 ? entry * ((a->rows - 1) * a->target_stride + a->vocab) : 0},
+                {a->draft, a->rows > 0 ? entry * ((a->rows - 1) * a->draft_stride + a->vocab) : 0}};
+  for (int i = 0; i < 3; ++i) {
+    for (const auto& in : inputs)
+      if (!(in.p == a->lens && results[i].p == a->lens && i > 0) && !rr_apart(results[i].p, results[i].n, in.p, in.n)) return RR_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (!rr_apart(results[i].p, results[i].n, results[j].p, results[j].n)) return RR_ERR_INVALID_ARG;
+  }
+  cudaStream_t st = (cudaStream_t)stream;
   if (a->uniform) {
     const int cluster = cluster_of(a->batch, a->vocab, NW * BLOCK, 4);
     return done(launch(bf16 ? verify_sampled_kernel<__nv_bfloat16> : verify_sampled_kernel<float>, *a, a->batch, cluster, st));

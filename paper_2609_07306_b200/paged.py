@@ -153,7 +153,7 @@ class PagedKV:
                   and written nowhere; None: one token per sequence
         inv_freq  [rot / 2] float32, rotates the first rot entries of a head: the pairs (j, j + rot / 2), or with
                   interleaved=True (2 j, 2 j + 1); None: nothing is rotated
-        new_lens  [batch] int32: gets lens + new tokens (another tensor than lens)
+        new_lens  [batch] int32: gets lens + new tokens (memory that neither lens nor cu has any of)
         (A sequence for which the last PagePool.reserve of a pool over this cache could not give all pages, and whose tokens would reach behind its room: none of them
         is written, new_lens stays at lens, RR_STATUS_NO_PAGES is set.)
         positions [axes, tokens] int32 (any strides): the tokens' positions on every axis -- time, height and width of the patches of images

@@ -104,7 +104,7 @@ class PagePool:
         row is emptied.  A child holds the pages of its parent's tokens together with it; nothing is copied before one of them is written to (reserve).
         parents   [batch] int32
         lens      [batch] int32 tokens of the sequences
-        new_lens  [batch] int32: gets lens[parents[b]] (at most what the table holds), 0 for rows that were emptied (another tensor than lens)"""
+        new_lens  [batch] int32: gets lens[parents[b]] (at most what the table holds), 0 for rows that were emptied (memory that neither lens, parents nor the pool has any of)"""
         shape = (self.batch,)
         self._ints(parents, "parents", shape)
         self._ints(lens, "lens", shape)

@@ -53,7 +53,7 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor |
     draft     [rows, vocab] as target: row t is what tokens[t + 1] was drawn from (a sequence's last row is not read); None: the draft's
               probability was 1
     new_lens  [batch] int32: gets lens + accepted + 1, the tokens that stay of sequences that had lens tokens before the step's rows were
-              appended (may be lens itself): what PagePool.reserve takes next
+              appended (may be lens itself, else memory of its own): what PagePool.reserve takes next
     status    [1] int32: RR_STATUS_BAD_INDEX is OR-ed into it if a drafted token is outside the vocabulary (it is rejected)
     room      [batch] int32, PagePool.room, with lens: a sequence whose rows had no room, so that they were not appended, has accepted = -1 and keeps its lens; its
               next tokens are not to be used
