@@ -10,8 +10,8 @@
 //
 // The work is one read and one write of every entry: bound by memory for prompts, by latency for a decoding
 // step.  A CTA takes a token; its threads take 16 bytes each (the two halves of eight or four pairs) and rotate in FP32 with one
-// rounding.  Shapes and strides that do not split into 16-byte pieces go entry by entry.  Measured: 17282 tokens of 32 query and 8 key heads of
-// 128, bf16 (425 MB): 68 us, 6.3 TB/s, 96 % of a copy's rate, with positions of three axes (418 MB) 69 us; one token for each of 64 sequences: 3.4 us, with axes
+// rounding.  Shapes and strides that do not split into 16-byte pieces go entry by entry.  Measured: 17000 tokens of 32 query and 8 key heads of
+// 128, bf16 (418 MB): 67 us, 6.2 TB/s, 95 % of a copy's rate, with positions of three axes 70 us, entry by entry 214 us; one token for each of 64 sequences: 3.5 us, with axes
 // 3.9 us.  (Loads in front of the angles, two pieces a thread: 130 us; the pieces' places have to be worked out twice then.)
 #include "rr_paged.cuh"
 
@@ -176,8 +176,8 @@ int append(const rr_paged_kv* kv, const rr_append_args* a, const rr_axes_args* x
   if (a->tokens == 0 && !a->new_lens) return RR_OK;
   const AppendParams P{*kv, *a, x ? *x : rr_axes_args{}};
   const int grid = a->tokens > 0 ? a->tokens : 1;
-  // Few tokens: a token's own time counts, which more threads make shorter (64 tokens: 3.7 us, 4.4 with half of them).  Many: what all warps of a CTA do alike
-  // -- barriers, the sequence, the angles' loop -- costs issue slots, which half of them halve (17000 tokens, 418 MB: 79 us with 256 threads, 69 with 128).
+  // Few tokens: a token's own time counts, which more threads make shorter (64 tokens: 0.7 us less than with half of them).  Many: what all warps of a CTA do alike
+  // -- barriers, the sequence, the angles' loop -- costs issue slots, which half of them halve (17000 tokens, 418 MB: 79 us with 256 threads, 69 with 128; 4737 tokens 22.6 us with 128, 4736 24.3 with 256).
   const int NT = grid > 32 * rr_sm_count() ? MOST_NT / 2 : MOST_NT;
   cudaStream_t st = (cudaStream_t)stream;
   if (kv->dtype == RR_BF16) {

@@ -18,7 +18,8 @@
 // Greedy: a cluster takes a row, whoever's it is (sequences with many drafts would hold up the others), 16 bytes at a time where rows
 // allow it; only maxima are taken (a packed maximum of two bf16 costs one instruction), a thread keeps its first best vector, and the entry inside it is looked
 // up at the end.  The rows' best tokens go to `out`, where a second kernel, a warp per sequence, compares them with the drafts.
-// Measured: those 64 sequences 15.9 us, 20.1 from memory, in bf16 15.0 and 17.2, without the draft's probabilities 13.8 and 16.5; one sequence against 32768 tokens 6.4 us; greedy, 415 rows of 131072 in bf16 (109 MB) 22 us from memory.
+// Measured: those 64 sequences 15.9 us, 20.1 from memory, in bf16 15.0 and 17.2, without the draft's probabilities 13.8 and 16.5; one sequence against 32768 tokens 6.4 us; greedy, 415 rows of 131072 in bf16 (109 MB) 22 us
+// from memory, 36 us where rows do not lie on 16 bytes.  The sampled kernel has 64 registers, for four CTAs an SM, and spills 56 bytes (bf16: 16).
 #include <cooperative_groups.h>
 #include <utility>
 #include "rr_paged.cuh"
@@ -388,8 +389,10 @@ compare_kernel(const __grid_constant__ rr_verify_args a) {
   if (lane == 0) write_lengths(a, b, s, accepted, len);
 }
 
-// CTAs that share each of `n` things (sequences, rows) of `work` entries: at most eight, no less than `least` entries for one, and no more in all than run at
-// once (415 rows of 131072: one CTA a row 21.8 us, two 17.4, four 23.3, of which the last ones wait for places; 6 rows: 9.2, 6.7, 5.5).
+// CTAs that share each of `n` things (sequences, rows) of `work` entries: at most eight, no less than `least` entries for one, and no more than per_sm in all for an
+// SM (415 rows of 131072: one CTA a row 21.8 us, two 17.4, four 23.3, of which the last ones wait for places; 6 rows: 9.2, 6.7, 5.5).  Four CTAs of the sampled kernel
+// run on an SM; of the greedy kernel's vector builds six (34 registers), while per_sm is eight, as for the others: between 112 and 148, 223 and 296, 445 and 592 rows
+// some CTAs wait (440 rows 22.7 us, 500 30.7).
 int cluster_of(int n, int work, int least, int per_sm) {
   int c = MAX_CL;
   while (c > 1 && (work < c * least || (int64_t)n * c > per_sm * rr_sm_count())) c /= 2;
